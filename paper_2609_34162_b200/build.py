@@ -13,10 +13,12 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libslidedp.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("common.cu", "context.cu", "update.cu", "stream.cu",
-                                           "model.cu", "ipc.cu")]
+                                           "model.cu", "ipc.cu", "qk_norm_rope.cu", "distill.cu",
+                                           "attention.cu")]
 DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in ("kernels.cuh", "cast_kernel.cuh",
-                                                     "device_utils.cuh", "types.h", "internal.h")]
-DEPENDS.append(os.path.join(ROOT, "include", "slidedp.h"))
+                                                     "device_utils.cuh", "types.h", "internal.h",
+                                                     "ops_internal.h", "attention.h")]
+DEPENDS += [os.path.join(ROOT, "include", f) for f in ("slidedp.h", "slidedp_ops.h")]
 
 
 def nvcc() -> str:
@@ -32,6 +34,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if force or stale:
         tmp = LIB + ".tmp.%d" % os.getpid()
         cmd = [nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3",
+               "--threads", "0",
                "-std=c++17", "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
                "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", tmp] + SOURCES
         if verbose:
