@@ -14,10 +14,11 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libslidedp.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("common.cu", "context.cu", "update.cu", "stream.cu",
                                            "model.cu", "ipc.cu", "qk_norm_rope.cu", "distill.cu",
-                                           "attention.cu")]
+                                           "attention.cu", "attention_mma.cu")]
 DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in ("kernels.cuh", "cast_kernel.cuh",
                                                      "device_utils.cuh", "types.h", "internal.h",
-                                                     "ops_internal.h", "attention.h")]
+                                                     "ops_internal.h", "attention.h",
+                                                     "attention_rows.cuh", "tcgen05.cuh")]
 DEPENDS += [os.path.join(ROOT, "include", f) for f in ("slidedp.h", "slidedp_ops.h")]
 
 

@@ -1,136 +1,30 @@
 // libslidedp: attention over packed documents: argument checks, dispatch, and the kernels for the views
 // that the tensor-core kernels do not take. See include/slidedp_ops.h for the contract.
-#include "attention.h"
-#include "device_utils.cuh"
+#include "attention_rows.cuh"
 
 namespace slidedp {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRowTile = 128;            // the row statistics are padded to this many rows per head
 constexpr int kGeneralThreads = 128;
-constexpr int kLanes = 32;
-constexpr int kMaxPer = host::kMaxHeadDim / kLanes;
 
 // ---- kernels without tensor cores -------------------------------------------------------------------
-// One warp per row (a query, or a key of the backward pass), lanes over the head's values, one partner
-// row at a time with a running maximum: any head_dim and stride, no shared memory. They serve head_dim
-// above 128 or not a multiple of 8 and views that are not 16-byte aligned, which TMA cannot address.
-
-__device__ __forceinline__ float load_bf16(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
-
-__device__ __forceinline__ void load_row(const AttnView& v, int t, int h, int n, float* x) {
-  const uint16_t* row = v.p + t * v.t + h * v.h;
-  const int lane = threadIdx.x % kLanes;
-#pragma unroll
-  for (int i = 0; i < kMaxPer; ++i) x[i] = lane + i * kLanes < n ? load_bf16(row + lane + i * kLanes) : 0.0f;
-}
-__device__ __forceinline__ void store_row(const AttnView& v, int t, int h, int n, const float* x) {
-  uint16_t* row = v.p + t * v.t + h * v.h;
-  const int lane = threadIdx.x % kLanes;
-#pragma unroll
-  for (int i = 0; i < kMaxPer; ++i)
-    if (lane + i * kLanes < n) row[lane + i * kLanes] = (uint16_t)f32_to_bf16_bits(x[i]);
-}
-__device__ __forceinline__ float dot(const float* a, const float* b) {
-  float s = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kMaxPer; ++i) s = fmaf(a[i], b[i], s);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  return s;
-}
-// Score of one pair in units of log2 e from the raw product, and d score / d (scale * product).
-__device__ __forceinline__ float score(const AttnParams& p, float raw, float slope, int distance, float* grad) {
-  float s = raw * p.scale;
-  *grad = 1.0f;
-  if (p.softcap > 0.0f) {
-    const float th = tanhf(s / p.softcap);
-    s = p.softcap * th;
-    *grad = 1.0f - th * th;
-  }
-  return (s - slope * (float)abs(distance)) * kLog2e;
-}
+// One warp per row. They serve head_dim above 128 or not a multiple of 8 and views that are not 16-byte
+// aligned, which TMA cannot address.
 
 __global__ void __launch_bounds__(kGeneralThreads) attention_forward_general_kernel(const __grid_constant__ AttnParams p) {
-  const int i = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes, h = blockIdx.y;
-  if (i >= p.tokens) return;
-  const int hk = h / p.group;
-  const float slope = p.slopes ? p.slopes[h] : 0.0f;
-  float q[kMaxPer], o[kMaxPer] = {};
-  load_row(p.q, i, h, p.head_dim, q);
-  int lo, hi;
-  p.mask.keys_of(i, &lo, &hi);
-  float m = -INFINITY, l = 0.0f;
-  for (int j = lo; j < hi; ++j) {
-    float x[kMaxPer], g;
-    load_row(p.k, j, hk, p.head_dim, x);
-    const float s = score(p, dot(q, x), slope, i - j, &g);
-    load_row(p.v, j, hk, p.head_dim, x);
-    const float top = fmaxf(m, s), keep = exp2f(m - top), e = exp2f(s - top);
-    m = top;
-    l = l * keep + e;
-#pragma unroll
-    for (int d = 0; d < kMaxPer; ++d) o[d] = fmaf(e, x[d], o[d] * keep);
-  }
-  const float inv = lo < hi ? 1.0f / l : 0.0f;
-#pragma unroll
-  for (int d = 0; d < kMaxPer; ++d) o[d] *= inv;
-  store_row(p.o, i, h, p.head_dim, o);
-  if (threadIdx.x % kLanes == 0) p.lse[(int64_t)h * p.tokens + i] = lo < hi ? (m + log2f(l)) / kLog2e : -INFINITY;
+  const int i = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
+  if (i < p.tokens) attention_out_row(p, i, blockIdx.y, true);
 }
-
 __global__ void __launch_bounds__(kGeneralThreads) attention_dq_general_kernel(const __grid_constant__ AttnParams p) {
-  const int i = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes, h = blockIdx.y;
-  if (i >= p.tokens) return;
-  const int hk = h / p.group;
-  const float slope = p.slopes ? p.slopes[h] : 0.0f;
-  float q[kMaxPer], go[kMaxPer], dq[kMaxPer] = {};
-  load_row(p.q, i, h, p.head_dim, q);
-  load_row(p.dout, i, h, p.head_dim, go);
-  const float2 row = p.rows[h * p.pitch + i];
-  int lo, hi;
-  p.mask.keys_of(i, &lo, &hi);
-  for (int j = lo; j < hi; ++j) {
-    float k[kMaxPer], v[kMaxPer], g;
-    load_row(p.k, j, hk, p.head_dim, k);
-    load_row(p.v, j, hk, p.head_dim, v);
-    const float pr = exp2f(score(p, dot(q, k), slope, i - j, &g) - row.x);
-    const float ds = pr * (dot(go, v) - row.y) * g * p.scale;
-#pragma unroll
-    for (int d = 0; d < kMaxPer; ++d) dq[d] = fmaf(ds, k[d], dq[d]);
-  }
-  store_row(p.dq, i, h, p.head_dim, dq);
+  const int i = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
+  if (i < p.tokens) attention_dq_row(p, i, blockIdx.y);
 }
-
 __global__ void __launch_bounds__(kGeneralThreads) attention_dkv_general_kernel(const __grid_constant__ AttnParams p) {
-  const int j = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes, hk = blockIdx.y;
-  if (j >= p.tokens) return;
-  float k[kMaxPer], v[kMaxPer], dk[kMaxPer] = {}, dv[kMaxPer] = {};
-  load_row(p.k, j, hk, p.head_dim, k);
-  load_row(p.v, j, hk, p.head_dim, v);
-  int lo, hi;
-  p.mask.queries_of(j, &lo, &hi);
-  for (int h = hk * p.group; h < (hk + 1) * p.group; ++h) {
-    const float slope = p.slopes ? p.slopes[h] : 0.0f;
-    for (int i = lo; i < hi; ++i) {
-      float q[kMaxPer], go[kMaxPer], g;
-      load_row(p.q, i, h, p.head_dim, q);
-      load_row(p.dout, i, h, p.head_dim, go);
-      const float2 row = p.rows[h * p.pitch + i];
-      const float pr = exp2f(score(p, dot(q, k), slope, i - j, &g) - row.x);
-      const float ds = pr * (dot(go, v) - row.y) * g * p.scale;
-#pragma unroll
-      for (int d = 0; d < kMaxPer; ++d) {
-        dv[d] = fmaf(pr, go[d], dv[d]);
-        dk[d] = fmaf(ds, q[d], dk[d]);
-      }
-    }
-  }
-  store_row(p.dk, j, hk, p.head_dim, dk);
-  store_row(p.dv, j, hk, p.head_dim, dv);
+  const int j = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
+  if (j < p.tokens) attention_dkv_row(p, j, blockIdx.y);
 }
 
-// rows[h][i] = (lse log2 e, sum_d dout out), zeros for the rows of the padding: one warp per row.
+// row_lse[h][i] = lse log2 e, row_delta[h][i] = sum_d dout out, zeros for the rows of the padding: one warp per row.
 // Bound: HBM, one read of out and dout.
 __global__ void __launch_bounds__(kGeneralThreads) attention_rows_kernel(const __grid_constant__ AttnParams p) {
   const int64_t i = (int64_t)blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
@@ -144,7 +38,10 @@ __global__ void __launch_bounds__(kGeneralThreads) attention_rows_kernel(const _
     s = dot(a, b);
     l = p.lse[(int64_t)h * p.tokens + i] * kLog2e;
   }
-  if (threadIdx.x % kLanes == 0) p.rows[h * p.pitch + i] = make_float2(l, s);
+  if (threadIdx.x % kLanes == 0) {
+    p.row_lse[h * p.pitch + i] = l;
+    p.row_delta[h * p.pitch + i] = s;
+  }
 }
 
 }  // namespace slidedp
@@ -193,6 +90,22 @@ AttnParams make_params(const slidedp_attn_args* a, const slidedp_heads* q, const
   return p;
 }
 
+bool tensor_core_dim(int head_dim) { return head_dim % 8 == 0 && head_dim <= 128; }
+
+// Whether TMA can address a view: 16-byte base and strides, none of them zero where it is used.
+bool tma_view(const slidedp_heads* v, int64_t tokens, int heads) {
+  return heads_aligned(v, 2, 16, tokens, heads) && (tokens <= 1 || v->stride_token > 0) &&
+         (heads <= 1 || v->stride_head > 0) && v->stride_token < (1ll << 38) && v->stride_head < (1ll << 38);
+}
+
+// A wait inside an earlier kernel of the context ran out.
+int check_kernel_error(slidedp_ctx* ctx) {
+  volatile int* e = ctx->kernel_error;
+  if (*e == 0) return SLIDEDP_OK;
+  *e = 0;
+  return SLIDEDP_ERR_TIMEOUT;
+}
+
 unsigned general_blocks(int64_t rows) {
   return (unsigned)((rows + kGeneralThreads / kLanes - 1) / (kGeneralThreads / kLanes));
 }
@@ -208,10 +121,16 @@ int slidedp_attention(slidedp_ctx* ctx, const slidedp_attn_args* a, const slided
   if (!heads_ok(q, 2) || !heads_ok(k, 2) || !heads_ok(v, 2) || !heads_ok(out, 2) || !lse ||
       reinterpret_cast<uintptr_t>(lse) % 4 != 0)
     return SLIDEDP_ERR_INVALID_ARG;
-  const AttnParams p = make_params(a, q, k, v, out, lse);
+  AttnParams p = make_params(a, q, k, v, out, lse);
+  p.error = ctx->kernel_error;
+  const int rc = check_kernel_error(ctx);
+  if (rc != SLIDEDP_OK) return rc;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (tensor_core_dim(p.head_dim) && tma_view(q, p.tokens, p.heads_q) && tma_view(k, p.tokens, p.heads_kv) &&
+      tma_view(v, p.tokens, p.heads_kv) && tma_view(out, p.tokens, p.heads_q))
+    return attention_forward_mma(ctx, p, st);
   FAULT_POINT();
   attention_forward_general_kernel<<<dim3(general_blocks(p.tokens), p.heads_q), kGeneralThreads, 0, st>>>(p);
   ctx->launches += 1;
@@ -221,7 +140,7 @@ int slidedp_attention(slidedp_ctx* ctx, const slidedp_attn_args* a, const slided
 
 size_t slidedp_attention_workspace(const slidedp_attn_args* a) {
   if (check_attn(a) != SLIDEDP_OK) return 0;
-  return (size_t)a->heads_q * row_pitch(a->tokens) * sizeof(float2);
+  return (size_t)a->heads_q * row_pitch(a->tokens) * 2 * sizeof(float);
 }
 
 int slidedp_attention_backward(slidedp_ctx* ctx, const slidedp_attn_args* a, const slidedp_heads* q,
@@ -240,7 +159,11 @@ int slidedp_attention_backward(slidedp_ctx* ctx, const slidedp_attn_args* a, con
   p.dq = view(dq);
   p.dk = view(dk);
   p.dv = view(dv);
-  p.rows = static_cast<float2*>(workspace);
+  p.error = ctx->kernel_error;
+  const int rc = check_kernel_error(ctx);
+  if (rc != SLIDEDP_OK) return rc;
+  p.row_lse = static_cast<float*>(workspace);
+  p.row_delta = p.row_lse + a->heads_q * p.pitch;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -248,6 +171,10 @@ int slidedp_attention_backward(slidedp_ctx* ctx, const slidedp_attn_args* a, con
   attention_rows_kernel<<<dim3(general_blocks(p.pitch), p.heads_q), kGeneralThreads, 0, st>>>(p);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
+  if (tensor_core_dim(p.head_dim) && tma_view(q, p.tokens, p.heads_q) && tma_view(k, p.tokens, p.heads_kv) &&
+      tma_view(v, p.tokens, p.heads_kv) && tma_view(d_out, p.tokens, p.heads_q) && tma_view(dq, p.tokens, p.heads_q) &&
+      tma_view(dk, p.tokens, p.heads_kv) && tma_view(dv, p.tokens, p.heads_kv))
+    return attention_backward_mma(ctx, p, st);
   FAULT_POINT();
   attention_dq_general_kernel<<<dim3(general_blocks(p.tokens), p.heads_q), kGeneralThreads, 0, st>>>(p);
   ctx->launches += 1;

@@ -61,8 +61,10 @@ struct AttnView {
 struct AttnParams {
   AttnView q, k, v, o, dout, dq, dk, dv;
   float* lse;          // [heads_q][tokens]
-  float2* rows;        // backward: (lse * log2 e, sum_d dout * out) as [heads_q][pitch], zeros past tokens
+  float* row_lse;      // backward: lse * log2 e as [heads_q][pitch], zeros past tokens
+  float* row_delta;    // backward: sum_d dout * out, likewise
   int64_t pitch;
+  int* error;          // pinned host word that a wait which runs out sets
   const float* slopes;
   DocMask mask;
   int tokens, heads_q, heads_kv, group, head_dim;

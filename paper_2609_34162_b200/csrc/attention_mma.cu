@@ -1,0 +1,954 @@
+// libslidedp: attention over packed documents on the tensor cores (tcgen05, TMA, TMEM), forward and
+// backward, for head_dim a multiple of 8 up to 128. See include/slidedp_ops.h for the contract.
+//
+// Bound: the tensor cores, 4 head_dim flops per visible pair and query head forward, 10 backward (14 here,
+// see the backward kernels). Everything else hides behind them: one block per SM, whose warps are an
+// issuer of matrix products, a producer of TMA loads, and two warpgroups that turn scores into
+// probabilities with one TMEM lane (row of the tile) per thread.
+//
+// BF16 roundings: probabilities and score gradients are BF16 operands of the second products (half an ulp,
+// 2^-9 of each term, like the inputs they meet); scores, statistics and accumulators are FP32.
+#include <atomic>
+
+#include "attention_rows.cuh"
+#include "tcgen05.cuh"
+
+namespace slidedp {
+
+constexpr int kTile = 128;                 // rows of a tile: TMEM lanes, and keys or queries per step
+constexpr int kHalfBytes = kTile * 128;    // 64 BF16 columns of a tile, as TMA writes them
+// Eight warps of rows and a warpgroup with the issuer and the producer. Launched with 168 registers per
+// thread (65536 / 384); the row warpgroups then take 216 and the third keeps 72: 2 * 216 + 72 = 3 * 168.
+constexpr int kMmaThreads = 384;
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
+constexpr int kTmemColumns = 512;
+constexpr uint32_t kKStep = 32 >> 4;       // descriptor step of 16 contracted values along a row
+constexpr uint32_t kRowStep = 16 * 128 >> 4;   // and of 16 contracted rows
+constexpr float kRescaleAbove = 8.0f;      // log2: how far a row's maximum may run ahead of its scale
+
+// Waits that outlive the early exit: for copies and products of this thread still in flight.
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
+  for (uint32_t n = 0; n < kSpinLimit; ++n)
+    if (mbar_try(bar, parity)) return;
+}
+
+template <int HALVES>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int head, int row, uint32_t bar) {
+#pragma unroll
+  for (int c = 0; c < HALVES; ++c) tma_load_3d(dst + c * kHalfBytes, map, c * 64, head, row, bar);
+}
+
+// D (+)= A B^T over the heads' values: A and B tiles in shared memory, both contracted along their rows.
+__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, int steps, uint32_t desc) {
+  for (int k = 0; k < steps; ++k) {
+    const uint32_t off = (k >> 2) * kHalfBytes;
+    mma_ss(d, smem_desc_k_major(a + off) + (k & 3) * kKStep, smem_desc_k_major(b + off) + (k & 3) * kKStep, desc, k > 0);
+  }
+}
+// D (+)= A B with A (BF16, 128 contracted columns) in TMEM and B a tile contracted over its rows. A's columns
+// 64..127 start `second` TMEM columns after the first 64 (32 when all lie together).
+__device__ __forceinline__ void product_tmem(uint32_t d, uint32_t a, uint32_t second, uint32_t b, uint32_t desc, bool add) {
+#pragma unroll
+  for (int k = 0; k < kTile / 16; ++k)
+    mma_ts(d, a + (k >> 2) * second + (k & 3) * 8, smem_desc_mn_major(b, kHalfBytes) + k * kRowStep, desc, add || k > 0);
+}
+
+// Capped and biased scores, in units of log2 e, and the factor of d score / d product.
+struct ScoreMod {
+  float scale;          // natural units
+  float cap, inv_cap;   // cap 0: none
+  float slope;          // log2 units
+  __device__ ScoreMod(const AttnParams& p, int h) {
+    scale = p.scale;
+    cap = p.softcap;
+    inv_cap = p.softcap > 0.0f ? 1.0f / p.softcap : 0.0f;
+    slope = p.slopes ? p.slopes[h] * kLog2e : 0.0f;
+  }
+  // distance: query minus key
+  __device__ __forceinline__ float operator()(float raw, float distance, float* grad) const {
+    float s = raw * scale;
+    *grad = 1.0f;
+    if (cap > 0.0f) {
+      // tanh y = 1 - 2 / (1 + exp 2y): absolute error near 2^-23, and 1 and -1 at the ends
+      const float th = fmaf(-2.0f, rcp_approx(1.0f + exp2_approx(s * inv_cap * (2.0f * kLog2e))), 1.0f);
+      s = cap * th;
+      *grad = fmaf(-th, th, 1.0f);
+    }
+    return fmaf(s, kLog2e, -slope * fabsf(distance));
+  }
+};
+
+// ---- forward -------------------------------------------------------------------------------------------
+//
+// A block takes 256 queries of one head as two tiles of 128 (one per row warpgroup) and walks the keys they
+// see in steps of 128. TMEM: scores of the tiles (128 columns each, overwritten by their BF16
+// probabilities) and their outputs. The issuer alternates between the tiles, so that one's products run
+// while the other's warpgroup exponentiates. A row's accumulators are rescaled only when its
+// maximum has grown by more than 2^8 since the last time.
+
+template <int HALVES> struct ForwardShape {
+  static constexpr int kStages = HALVES == 2 ? 2 : 4;
+  static constexpr int kTileBytes = HALVES * kHalfBytes;
+  static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + 1024;
+};
+
+struct ForwardControl {
+  uint64_t q_full, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_ready[2], o_full[2], done;
+  uint32_t tmem, dead;
+  int lo[2], hi[2];   // keys that the tiles' rows see
+};
+
+template <int HALVES, bool kMod>
+__global__ void __launch_bounds__(kMmaThreads, 1)
+    attention_forward_mma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
+                                 const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  using Shape = ForwardShape<HALVES>;
+  constexpr int S = Shape::kStages;
+  extern __shared__ uint8_t raw_smem[];
+  __shared__ ForwardControl ctl;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int tiles = (p.tokens + 2 * kTile - 1) / (2 * kTile);
+  // the last queries see the most keys when causal: start with them
+  const int h = blockIdx.x % p.heads_q, m0 = (tiles - 1 - (int)(blockIdx.x / p.heads_q)) * 2 * kTile;
+  const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
+  const uint32_t smem_q = base, smem_k = base + 2 * Shape::kTileBytes, smem_v = smem_k + S * Shape::kTileBytes;
+  const Waiter wait{&ctl.dead, p.error};
+
+  if (threadIdx.x == 0) {
+    mbar_init(smem_addr(&ctl.q_full), 1);
+    for (int i = 0; i < S; ++i) {
+      mbar_init(smem_addr(&ctl.k_full[i]), 1);
+      mbar_init(smem_addr(&ctl.k_empty[i]), 1);
+      mbar_init(smem_addr(&ctl.v_full[i]), 1);
+      mbar_init(smem_addr(&ctl.v_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_addr(&ctl.s_full[i]), 1);
+      mbar_init(smem_addr(&ctl.p_ready[i]), kTile);
+      mbar_init(smem_addr(&ctl.o_full[i]), 1);
+    }
+    mbar_init(smem_addr(&ctl.done), 1);
+    ctl.dead = 0;
+    mbar_init_fence();
+  }
+  if (threadIdx.x >= 64 && threadIdx.x < 66) {
+    const int s = threadIdx.x - 64, r0 = m0 + s * kTile;
+    int lo = 0, hi = 0, x;
+    if (r0 < p.tokens) {
+      p.mask.keys_of(r0, &lo, &x);
+      p.mask.keys_of(r0 + kTile - 1 < p.tokens ? r0 + kTile - 1 : p.tokens - 1, &x, &hi);
+    }
+    ctl.lo[s] = lo;
+    ctl.hi[s] = hi > lo ? hi : lo;
+  }
+  if (warp == 8) tmem_alloc(smem_addr(&ctl.tmem), kTmemColumns);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ctl.tmem;
+
+  // steps [first[s], last[s]) of the walk concern tile s
+  int n_lo = 0, steps = 0, first[2], last[2];
+  {
+    const bool on0 = ctl.lo[0] < ctl.hi[0], on1 = ctl.lo[1] < ctl.hi[1];
+    n_lo = on0 && (!on1 || ctl.lo[0] < ctl.lo[1]) ? ctl.lo[0] : on1 ? ctl.lo[1] : 0;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const bool on = s ? on1 : on0;
+      first[s] = on ? (ctl.lo[s] - n_lo) / kTile : 0;
+      last[s] = on ? (ctl.hi[s] - n_lo + kTile - 1) / kTile : 0;
+      if (last[s] > steps) steps = last[s];
+    }
+  }
+
+  if (warp >= 8) {
+    fewer_registers();
+    if (warp == 9 && lane == 0) {   // ---- producer
+      const int hk = h / p.group;
+      int k_sent = 0, v_sent = 0, q_tiles = 0;
+      bool ok = true;
+      for (int s = 0; s < 2; ++s) q_tiles += first[s] < last[s];
+      if (q_tiles > 0) {
+        mbar_expect(smem_addr(&ctl.q_full), q_tiles * Shape::kTileBytes);
+        for (int s = 0; s < 2; ++s)
+          if (first[s] < last[s])
+            load_tile<HALVES>(smem_q + s * Shape::kTileBytes, &map_q, h, m0 + s * kTile, smem_addr(&ctl.q_full));
+      }
+      for (int j = 0; j < steps && ok; ++j) {
+        const int st = j % S;
+        const uint32_t turn = (uint32_t)(j / S + 1) & 1;   // parity of the previous use's release
+        if (j >= S && !(ok = wait(smem_addr(&ctl.k_empty[st]), turn))) break;
+        mbar_expect(smem_addr(&ctl.k_full[st]), Shape::kTileBytes);
+        load_tile<HALVES>(smem_k + st * Shape::kTileBytes, &map_k, hk, n_lo + j * kTile, smem_addr(&ctl.k_full[st]));
+        ++k_sent;
+        if (j >= S && !(ok = wait(smem_addr(&ctl.v_empty[st]), turn))) break;
+        mbar_expect(smem_addr(&ctl.v_full[st]), Shape::kTileBytes);
+        load_tile<HALVES>(smem_v + st * Shape::kTileBytes, &map_v, hk, n_lo + j * kTile, smem_addr(&ctl.v_full[st]));
+        ++v_sent;
+      }
+      if (ctl.dead) {   // leave no copy in flight
+        if (q_tiles > 0) drain(smem_addr(&ctl.q_full), 0);
+        for (int j = k_sent > S ? k_sent - S : 0; j < k_sent; ++j) drain(smem_addr(&ctl.k_full[j % S]), (j / S) & 1);
+        for (int j = v_sent > S ? v_sent - S : 0; j < v_sent; ++j) drain(smem_addr(&ctl.v_full[j % S]), (j / S) & 1);
+      }
+    } else if (warp == 8 && lane == 0) {   // ---- issuer
+      const int k_steps = (p.head_dim + 15) / 16;
+      const uint32_t desc_s = mma_desc_bf16(kTile, false), desc_o = mma_desc_bf16(k_steps * 16, true);
+      bool ok = steps == 0 || wait(smem_addr(&ctl.q_full), 0);
+      for (int j = -1; j < steps && ok; ++j) {
+        // products of step j's probabilities, and step j + 1's scores
+        const int st = j % S, nx = (j + 1) % S;
+        bool have_k = false;
+        if (j >= 0 && !(ok = wait(smem_addr(&ctl.v_full[st]), (j / S) & 1))) break;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          if (j >= first[s] && j < last[s]) {
+            if (!(ok = wait(smem_addr(&ctl.p_ready[s]), (j - first[s]) & 1))) break;
+            tc_fence_after();
+            product_tmem(tmem + 256 + s * 128, tmem + s * 128, 32, smem_v + st * Shape::kTileBytes, desc_o, j > first[s]);
+            if (j == last[s] - 1) mma_commit(smem_addr(&ctl.o_full[s]));
+          }
+          if (j + 1 >= first[s] && j + 1 < last[s]) {
+            if (!have_k) {
+              if (!(ok = wait(smem_addr(&ctl.k_full[nx]), ((j + 1) / S) & 1))) break;
+              have_k = true;
+            }
+            product_rows(tmem + s * 128, smem_q + s * Shape::kTileBytes, smem_k + nx * Shape::kTileBytes, k_steps, desc_s);
+            mma_commit(smem_addr(&ctl.s_full[s]));
+          }
+        }
+        if (!ok) break;
+        if (j >= 0) mma_commit(smem_addr(&ctl.v_empty[st]));
+        if (j + 1 < steps) {
+          if (!have_k && !(ok = wait(smem_addr(&ctl.k_full[nx]), ((j + 1) / S) & 1))) break;
+          mma_commit(smem_addr(&ctl.k_empty[nx]));
+        }
+      }
+      if (ctl.dead) {
+        mma_commit(smem_addr(&ctl.done));
+        drain(smem_addr(&ctl.done), 0);
+      }
+    }
+  } else {   // ---- rows
+    more_registers();
+    const int s = warp / 4, r = (warp % 4) * 32;
+    const int i = m0 + s * kTile + r + lane;
+    const uint32_t at = tmem + ((uint32_t)r << 16) + s * 128, at_o = at + 256;
+    const int from = s ? first[1] : first[0], to = s ? last[1] : last[0];
+    const ScoreMod mod(p, h);
+    int lo = 0, hi = 0;
+    if (i < p.tokens) p.mask.keys_of(i, &lo, &hi);
+    const float unit = kMod ? 1.0f : p.scale_log2;   // log2 per unit of the values compared
+    float m = -INFINITY, l = 0.0f;
+    bool ok = true;
+    for (int j = from; j < to; ++j) {
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.s_full[s]), (j - from) & 1));
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t x[128];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_load32(at + c * 32, x + c * 32);
+      tmem_wait_load();
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_landed(x + c * 32);
+      const int n0 = n_lo + j * kTile;
+      if constexpr (kMod) {
+        const float d0 = (float)(i - n0);
+        float g;
+#pragma unroll
+        for (int c = 0; c < 128; ++c) x[c] = __float_as_uint(mod(__uint_as_float(x[c]), d0 - (float)c, &g));
+      }
+      // rows past the sequence are not stored: they need no mask
+      if (!__all_sync(0xffffffffu, i >= p.tokens || (lo <= n0 && hi >= n0 + kTile))) {
+        const int a = lo - n0, b = hi - n0;
+#pragma unroll
+        for (int c = 0; c < 128; ++c) x[c] = c >= a && c < b ? x[c] : 0xff800000u;
+      }
+      float top[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) top[c] = __uint_as_float(x[c]);
+#pragma unroll
+      for (int c = 4; c < 128; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(x[c]));
+      const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+      const bool grow = mx > -INFINITY && (m == -INFINITY || (mx - m) * unit > kRescaleAbove);
+      if (__any_sync(0xffffffffu, grow)) {
+        const float keep = !grow ? 1.0f : m == -INFINITY ? 0.0f : exp2_approx((m - mx) * unit);
+        if (grow) m = mx;
+        l *= keep;
+        if (j > from) {   // the products before these scores are complete: they were issued earlier
+#pragma unroll
+          for (int c = 0; c < HALVES * 2; ++c) {
+            uint32_t o[32];
+            tmem_load32(at_o + c * 32, o);
+            tmem_wait_load();
+            tmem_landed(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+            tmem_store32(at_o + c * 32, o);
+          }
+        }
+      }
+      const float shift = m == -INFINITY ? 0.0f : m * unit;
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t pk[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          const float e0 = exp2_approx(fmaf(__uint_as_float(x[half * 64 + 2 * c]), unit, -shift));
+          const float e1 = exp2_approx(fmaf(__uint_as_float(x[half * 64 + 2 * c + 1]), unit, -shift));
+          sum[(2 * c) & 3] += e0;
+          sum[(2 * c + 1) & 3] += e1;
+          pk[c] = pack_bf16(e0, e1);
+        }
+        tmem_store32(at + half * 32, pk);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tmem_wait_store();
+      tc_fence_before();
+      mbar_arrive(smem_addr(&ctl.p_ready[s]));
+    }
+    if (ok && from < to) {
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.o_full[s]), 0));
+      tc_fence_after();
+    }
+    if (ok) {
+      const bool live = i < p.tokens, some = lo < hi;
+      const float inv = some ? 1.0f / l : 0.0f;
+      uint16_t* row = p.o.p + (int64_t)i * p.o.t + h * p.o.h;
+      bool nan = false;
+#pragma unroll
+      for (int c = 0; c < HALVES * 2; ++c) {
+        uint32_t o[32];
+        if (from < to) {
+          tmem_load32(at_o + c * 32, o);
+          tmem_wait_load();
+          tmem_landed(o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int d = c * 32 + e * 8;
+          float y[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[e * 8 + k]) * inv;
+          if (live && d < p.head_dim) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) nan |= y[k] != y[k];
+            *reinterpret_cast<uint4*>(row + d) =
+                make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+          }
+        }
+      }
+      if (live) p.lse[(int64_t)h * p.tokens + i] = some ? (m * unit + log2f(l)) * (1.0f / kLog2e) : -INFINITY;
+      for (uint32_t redo = __ballot_sync(0xffffffffu, nan); redo; redo &= redo - 1)
+        attention_out_row(p, i - lane + __ffs(redo) - 1, h, false);   // its lse is right: masked scores are dropped
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) tmem_free(tmem, kTmemColumns);
+}
+
+// ---- backward -------------------------------------------------------------------------------------------
+//
+// With P = exp2(s - lse), dP = dO V^T and dS = P (dP - delta) (d score / d product):
+//   dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K.
+// Two kernels, one walking the queries of a tile of keys and one the keys of a tile of queries, so that every
+// sum is taken by one block in a fixed order. That costs the scores and dP twice (14 head_dim flops per
+// pair instead of 10) and buys the same bits in every run without FP32 atomics on dQ.
+
+// Keys: a block takes 128 keys of one key head and walks all queries that see them, for every query head of
+// the group. Rows of the tiles (TMEM lanes) are keys: S^T = K Q^T and dP^T = V dO^T, so that P^T and dS^T
+// are, as they stand, the left operands of dV and dK. TMEM: S^T, dP^T (overwritten by P^T and dS^T, each
+// warpgroup within its own 64 columns), dV, dK.
+template <int HALVES> struct KeysShape {
+  static constexpr int kStages = 2;
+  static constexpr int kTileBytes = HALVES * kHalfBytes;
+  static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + 1024;
+};
+
+struct KeysControl {
+  alignas(16) float lse[2][kTile];
+  alignas(16) float delta[2][kTile];
+  uint64_t kv_full, q_full[2], q_empty[2], do_full[2], do_empty[2], s_full, dp_full, p_ready, ds_ready, acc_full, done;
+  uint32_t tmem, dead;
+  int lo, hi;
+  uint32_t redo[4];
+};
+
+template <int HALVES, bool kMod>
+__global__ void __launch_bounds__(kMmaThreads, 1)
+    attention_dkv_mma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
+                             const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                             const __grid_constant__ CUtensorMap map_do) {
+  using Shape = KeysShape<HALVES>;
+  constexpr int S = Shape::kStages;
+  extern __shared__ uint8_t raw_smem[];
+  __shared__ KeysControl ctl;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int hk = blockIdx.x % p.heads_kv, n0 = (int)(blockIdx.x / p.heads_kv) * kTile;   // first keys: most queries
+  const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
+  const uint32_t smem_k = base, smem_v = smem_k + Shape::kTileBytes, smem_q = smem_v + Shape::kTileBytes,
+                 smem_do = smem_q + S * Shape::kTileBytes;
+  const Waiter wait{&ctl.dead, p.error};
+
+  if (threadIdx.x == 0) {
+    mbar_init(smem_addr(&ctl.kv_full), 1);
+    for (int i = 0; i < S; ++i) {
+      mbar_init(smem_addr(&ctl.q_full[i]), 1);
+      mbar_init(smem_addr(&ctl.q_empty[i]), 1);
+      mbar_init(smem_addr(&ctl.do_full[i]), 1);
+      mbar_init(smem_addr(&ctl.do_empty[i]), 1);
+    }
+    mbar_init(smem_addr(&ctl.s_full), 1);
+    mbar_init(smem_addr(&ctl.dp_full), 1);
+    mbar_init(smem_addr(&ctl.p_ready), 2 * kTile);
+    mbar_init(smem_addr(&ctl.ds_ready), 2 * kTile);
+    mbar_init(smem_addr(&ctl.acc_full), 1);
+    mbar_init(smem_addr(&ctl.done), 1);
+    ctl.dead = 0;
+    for (int i = 0; i < 4; ++i) ctl.redo[i] = 0;
+    mbar_init_fence();
+  }
+  if (threadIdx.x == 64) {
+    int lo, hi, x;
+    p.mask.queries_of(n0, &lo, &x);
+    p.mask.queries_of(n0 + kTile - 1 < p.tokens ? n0 + kTile - 1 : p.tokens - 1, &x, &hi);
+    ctl.lo = lo / kTile;                              // in tiles of queries
+    ctl.hi = hi > lo ? (hi + kTile - 1) / kTile : ctl.lo;
+  }
+  if (warp == 8) tmem_alloc(smem_addr(&ctl.tmem), kTmemColumns);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ctl.tmem, at_s = tmem, at_dp = tmem + 128, at_dv = tmem + 256, at_dk = tmem + 384;
+  const int q_lo = ctl.lo, per_head = ctl.hi - ctl.lo, steps = per_head * p.group;
+
+  if (warp >= 8) {
+    fewer_registers();
+    if (warp == 9 && lane == 0) {   // ---- producer
+      int q_sent = 0, do_sent = 0;
+      bool ok = true;
+      if (steps > 0) {
+        mbar_expect(smem_addr(&ctl.kv_full), 2 * Shape::kTileBytes);
+        load_tile<HALVES>(smem_k, &map_k, hk, n0, smem_addr(&ctl.kv_full));
+        load_tile<HALVES>(smem_v, &map_v, hk, n0, smem_addr(&ctl.kv_full));
+      }
+      for (int it = 0; it < steps && ok; ++it) {
+        const int st = it % S, h = hk * p.group + it / per_head, m0 = (q_lo + it % per_head) * kTile;
+        const uint32_t turn = (uint32_t)(it / S + 1) & 1;
+        if (it >= S && !(ok = wait(smem_addr(&ctl.q_empty[st]), turn))) break;
+        mbar_expect(smem_addr(&ctl.q_full[st]), Shape::kTileBytes + 2 * kTile * sizeof(float));
+        load_tile<HALVES>(smem_q + st * Shape::kTileBytes, &map_q, h, m0, smem_addr(&ctl.q_full[st]));
+        bulk_load(smem_addr(ctl.lse[st]), p.row_lse + h * p.pitch + m0, kTile * sizeof(float), smem_addr(&ctl.q_full[st]));
+        bulk_load(smem_addr(ctl.delta[st]), p.row_delta + h * p.pitch + m0, kTile * sizeof(float), smem_addr(&ctl.q_full[st]));
+        ++q_sent;
+        if (it >= S && !(ok = wait(smem_addr(&ctl.do_empty[st]), turn))) break;
+        mbar_expect(smem_addr(&ctl.do_full[st]), Shape::kTileBytes);
+        load_tile<HALVES>(smem_do + st * Shape::kTileBytes, &map_do, h, m0, smem_addr(&ctl.do_full[st]));
+        ++do_sent;
+      }
+      if (ctl.dead) {
+        if (steps > 0) drain(smem_addr(&ctl.kv_full), 0);
+        for (int j = q_sent > S ? q_sent - S : 0; j < q_sent; ++j) drain(smem_addr(&ctl.q_full[j % S]), (j / S) & 1);
+        for (int j = do_sent > S ? do_sent - S : 0; j < do_sent; ++j) drain(smem_addr(&ctl.do_full[j % S]), (j / S) & 1);
+      }
+    } else if (warp == 8 && lane == 0) {   // ---- issuer
+      const int k_steps = (p.head_dim + 15) / 16;
+      const uint32_t desc_s = mma_desc_bf16(kTile, false), desc_acc = mma_desc_bf16(k_steps * 16, true);
+      bool ok = steps == 0 || wait(smem_addr(&ctl.kv_full), 0);
+      for (int it = -1; it < steps && ok; ++it) {
+        const int st = it % S, nx = (it + 1) % S;
+        const bool more = it + 1 < steps;
+        const uint32_t next_turn = ((it + 1) / S) & 1;
+        if (it >= 0) {
+          if (!(ok = wait(smem_addr(&ctl.p_ready), it & 1))) break;
+          tc_fence_after();
+          product_tmem(at_dv, at_s, 64, smem_do + st * Shape::kTileBytes, desc_acc, it > 0);
+          mma_commit(smem_addr(&ctl.do_empty[st]));
+        }
+        if (more) {
+          if (!(ok = wait(smem_addr(&ctl.q_full[nx]), next_turn))) break;
+          product_rows(at_s, smem_k, smem_q + nx * Shape::kTileBytes, k_steps, desc_s);
+          mma_commit(smem_addr(&ctl.s_full));
+        }
+        if (it >= 0) {
+          if (!(ok = wait(smem_addr(&ctl.ds_ready), it & 1))) break;
+          tc_fence_after();
+          product_tmem(at_dk, at_dp, 64, smem_q + st * Shape::kTileBytes, desc_acc, it > 0);
+          mma_commit(smem_addr(&ctl.q_empty[st]));
+        }
+        if (more) {
+          if (!(ok = wait(smem_addr(&ctl.do_full[nx]), next_turn))) break;
+          product_rows(at_dp, smem_v, smem_do + nx * Shape::kTileBytes, k_steps, desc_s);
+          mma_commit(smem_addr(&ctl.dp_full));
+        }
+      }
+      if (ok && steps > 0) mma_commit(smem_addr(&ctl.acc_full));
+      if (ctl.dead) {
+        mma_commit(smem_addr(&ctl.done));
+        drain(smem_addr(&ctl.done), 0);
+      }
+    }
+  } else {   // ---- rows: keys; the warpgroups take 64 of a step's queries each
+    more_registers();
+    const int g = warp / 4, r = (warp % 4) * 32;
+    const int j = n0 + r + lane;
+    const uint32_t at = ((uint32_t)r << 16) + g * 64;
+    int lo = 0, hi = 0;
+    if (j < p.tokens) p.mask.queries_of(j, &lo, &hi);
+    bool ok = true;
+    for (int it = 0; it < steps; ++it) {
+      const int st = it % S, m0 = (q_lo + it % per_head) * kTile + g * 64;
+      const ScoreMod mod(p, hk * p.group + it / per_head);
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.q_full[st]), (it / S) & 1) && wait(smem_addr(&ctl.s_full), it & 1));
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t x[64];
+      tmem_load32(at_s + at, x);
+      tmem_load32(at_s + at + 32, x + 32);
+      tmem_wait_load();
+      tmem_landed(x);
+      tmem_landed(x + 32);
+      const bool whole = __all_sync(0xffffffffu, j >= p.tokens || (lo <= m0 && hi >= m0 + 64));
+      const int a = lo - m0, b = hi - m0;
+      const float4* lse4 = reinterpret_cast<const float4*>(&ctl.lse[st][g * 64]);
+      float pr[64];   // P, and from the second half on P (d score / d product)
+      {
+        uint32_t pk[32];
+#pragma unroll
+        for (int c4 = 0; c4 < 16; ++c4) {
+          const float4 l4 = lse4[c4];
+          const float l[4] = {l4.x, l4.y, l4.z, l4.w};
+          float e[4], grad[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int c = c4 * 4 + k;
+            if constexpr (kMod) e[k] = mod(__uint_as_float(x[c]), (float)(j - m0) - (float)c, &grad[k]) - l[k];
+            else e[k] = fmaf(__uint_as_float(x[c]), p.scale_log2, -l[k]);
+            e[k] = exp2_approx(e[k]);
+            if (!whole) e[k] = c >= a && c < b ? e[k] : 0.0f;
+          }
+          pk[c4 * 2] = pack_bf16(e[0], e[1]);
+          pk[c4 * 2 + 1] = pack_bf16(e[2], e[3]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) pr[c4 * 4 + k] = kMod ? e[k] * grad[k] : e[k];
+        }
+        tmem_store32(at_s + at, pk);
+      }
+      tmem_wait_store();
+      tc_fence_before();
+      mbar_arrive(smem_addr(&ctl.p_ready));
+
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.dp_full), it & 1));
+      if (!ok) break;
+      tc_fence_after();
+      tmem_load32(at_dp + at, x);
+      tmem_load32(at_dp + at + 32, x + 32);
+      tmem_wait_load();
+      tmem_landed(x);
+      tmem_landed(x + 32);
+      const float4* delta4 = reinterpret_cast<const float4*>(&ctl.delta[st][g * 64]);
+      {
+        uint32_t pk[32];
+#pragma unroll
+        for (int c4 = 0; c4 < 16; ++c4) {
+          const float4 d4 = delta4[c4];
+          const float d[4] = {d4.x, d4.y, d4.z, d4.w};
+          float e[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int c = c4 * 4 + k;
+            e[k] = pr[c] * (__uint_as_float(x[c]) - d[k]);
+            if (!whole) e[k] = c >= a && c < b ? e[k] : 0.0f;   // not zero times what a masked pair holds
+          }
+          pk[c4 * 2] = pack_bf16(e[0], e[1]);
+          pk[c4 * 2 + 1] = pack_bf16(e[2], e[3]);
+        }
+        tmem_store32(at_dp + at, pk);
+      }
+      tmem_wait_store();
+      tc_fence_before();
+      mbar_arrive(smem_addr(&ctl.ds_ready));
+    }
+    if (ok && steps > 0) {
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.acc_full), 0));
+      tc_fence_after();
+    }
+    bool nan = false;
+    if (ok) {
+      // warpgroup 0 stores dV, warpgroup 1 dK
+      const AttnView& out = g ? p.dk : p.dv;
+      const uint32_t src = (g ? at_dk : at_dv) + ((uint32_t)r << 16);
+      const float factor = g ? p.scale : 1.0f;
+      uint16_t* row = out.p + (int64_t)j * out.t + hk * out.h;
+#pragma unroll
+      for (int c = 0; c < HALVES * 2; ++c) {
+        uint32_t o[32];
+        if (steps > 0) {
+          tmem_load32(src + c * 32, o);
+          tmem_wait_load();
+          tmem_landed(o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int d = c * 32 + e * 8;
+          float y[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[e * 8 + k]) * factor;
+          if (j < p.tokens && d < p.head_dim) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) nan |= y[k] != y[k];
+            *reinterpret_cast<uint4*>(row + d) =
+                make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+          }
+        }
+      }
+    }
+    const uint32_t mine = __ballot_sync(0xffffffffu, nan);
+    if (lane == 0 && mine) atomicOr(&ctl.redo[warp % 4], mine);
+    asm volatile("bar.sync 1, 256;" ::: "memory");   // both warpgroups have stored
+    if (g == 0)
+      for (uint32_t redo = ctl.redo[warp % 4]; redo; redo &= redo - 1) attention_dkv_row(p, n0 + r + __ffs(redo) - 1, hk);
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) tmem_free(tmem, kTmemColumns);
+}
+
+// Queries: a block takes 128 queries of one head and walks the keys that they see. Rows are queries; dS goes
+// where its scores were. TMEM: two buffers of scores (the next step's are made while this one's are
+// worked on), dP, dQ.
+template <int HALVES> struct QueriesShape {
+  static constexpr int kKStages = 3;   // the next step's scores need K beside this step's dS K
+  static constexpr int kVStages = 2;
+  static constexpr int kTileBytes = HALVES * kHalfBytes;
+  static constexpr int kSmem = (2 + kKStages + kVStages) * kTileBytes + 1024;
+};
+
+struct QueriesControl {
+  uint64_t q_full, k_full[3], k_empty[3], v_full[2], v_empty[2], s_full[2], dp_full, ds_ready, acc_full, done;
+  uint32_t tmem, dead;
+  int lo, hi;
+  uint32_t redo[4];
+};
+
+template <int HALVES, bool kMod>
+__global__ void __launch_bounds__(kMmaThreads, 1)
+    attention_dq_mma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
+                            const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                            const __grid_constant__ CUtensorMap map_do) {
+  using Shape = QueriesShape<HALVES>;
+  constexpr int SK = Shape::kKStages, SV = Shape::kVStages;
+  extern __shared__ uint8_t raw_smem[];
+  __shared__ QueriesControl ctl;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int tiles = (p.tokens + kTile - 1) / kTile;
+  const int h = blockIdx.x % p.heads_q, m0 = (tiles - 1 - (int)(blockIdx.x / p.heads_q)) * kTile;
+  const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
+  const uint32_t smem_q = base, smem_do = smem_q + Shape::kTileBytes, smem_k = smem_do + Shape::kTileBytes,
+                 smem_v = smem_k + SK * Shape::kTileBytes;
+  const Waiter wait{&ctl.dead, p.error};
+
+  if (threadIdx.x == 0) {
+    mbar_init(smem_addr(&ctl.q_full), 1);
+    for (int i = 0; i < SK; ++i) {
+      mbar_init(smem_addr(&ctl.k_full[i]), 1);
+      mbar_init(smem_addr(&ctl.k_empty[i]), 1);
+    }
+    for (int i = 0; i < SV; ++i) {
+      mbar_init(smem_addr(&ctl.v_full[i]), 1);
+      mbar_init(smem_addr(&ctl.v_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&ctl.s_full[i]), 1);
+    mbar_init(smem_addr(&ctl.dp_full), 1);
+    mbar_init(smem_addr(&ctl.ds_ready), 2 * kTile);
+    mbar_init(smem_addr(&ctl.acc_full), 1);
+    mbar_init(smem_addr(&ctl.done), 1);
+    ctl.dead = 0;
+    for (int i = 0; i < 4; ++i) ctl.redo[i] = 0;
+    mbar_init_fence();
+  }
+  if (threadIdx.x == 64) {
+    int lo, hi, x;
+    p.mask.keys_of(m0, &lo, &x);
+    p.mask.keys_of(m0 + kTile - 1 < p.tokens ? m0 + kTile - 1 : p.tokens - 1, &x, &hi);
+    ctl.lo = lo;
+    ctl.hi = hi > lo ? hi : lo;
+  }
+  if (warp == 8) tmem_alloc(smem_addr(&ctl.tmem), kTmemColumns);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ctl.tmem, at_s = tmem, at_dp = tmem + 256, at_dq = tmem + 384;   // at_s: two buffers
+  const int n_lo = ctl.lo, steps = (ctl.hi - ctl.lo + kTile - 1) / kTile;
+
+  if (warp >= 8) {
+    fewer_registers();
+    if (warp == 9 && lane == 0) {   // ---- producer
+      const int hk = h / p.group;
+      int k_sent = 0, v_sent = 0;
+      bool ok = true;
+      if (steps > 0) {
+        mbar_expect(smem_addr(&ctl.q_full), 2 * Shape::kTileBytes);
+        load_tile<HALVES>(smem_q, &map_q, h, m0, smem_addr(&ctl.q_full));
+        load_tile<HALVES>(smem_do, &map_do, h, m0, smem_addr(&ctl.q_full));
+      }
+      for (int j = 0; j < steps && ok; ++j) {
+        const int sk = j % SK, sv = j % SV;
+        if (j >= SK && !(ok = wait(smem_addr(&ctl.k_empty[sk]), (uint32_t)(j / SK + 1) & 1))) break;
+        mbar_expect(smem_addr(&ctl.k_full[sk]), Shape::kTileBytes);
+        load_tile<HALVES>(smem_k + sk * Shape::kTileBytes, &map_k, hk, n_lo + j * kTile, smem_addr(&ctl.k_full[sk]));
+        ++k_sent;
+        if (j >= SV && !(ok = wait(smem_addr(&ctl.v_empty[sv]), (uint32_t)(j / SV + 1) & 1))) break;
+        mbar_expect(smem_addr(&ctl.v_full[sv]), Shape::kTileBytes);
+        load_tile<HALVES>(smem_v + sv * Shape::kTileBytes, &map_v, hk, n_lo + j * kTile, smem_addr(&ctl.v_full[sv]));
+        ++v_sent;
+      }
+      if (ctl.dead) {
+        if (steps > 0) drain(smem_addr(&ctl.q_full), 0);
+        for (int j = k_sent > SK ? k_sent - SK : 0; j < k_sent; ++j) drain(smem_addr(&ctl.k_full[j % SK]), (j / SK) & 1);
+        for (int j = v_sent > SV ? v_sent - SV : 0; j < v_sent; ++j) drain(smem_addr(&ctl.v_full[j % SV]), (j / SV) & 1);
+      }
+    } else if (warp == 8 && lane == 0) {   // ---- issuer
+      const int k_steps = (p.head_dim + 15) / 16;
+      const uint32_t desc_s = mma_desc_bf16(kTile, false), desc_acc = mma_desc_bf16(k_steps * 16, true);
+      bool ok = steps == 0 || wait(smem_addr(&ctl.q_full), 0);
+      for (int j = -1; j < steps && ok; ++j) {
+        const int nk = (j + 1) % SK, nv = (j + 1) % SV;
+        const bool more = j + 1 < steps;
+        if (more) {
+          if (!(ok = wait(smem_addr(&ctl.k_full[nk]), ((j + 1) / SK) & 1))) break;
+          product_rows(at_s + ((j + 1) & 1) * 128, smem_q, smem_k + nk * Shape::kTileBytes, k_steps, desc_s);
+          mma_commit(smem_addr(&ctl.s_full[(j + 1) & 1]));
+        }
+        if (j >= 0) {
+          if (!(ok = wait(smem_addr(&ctl.ds_ready), j & 1))) break;
+          tc_fence_after();
+        }
+        if (more) {
+          if (!(ok = wait(smem_addr(&ctl.v_full[nv]), ((j + 1) / SV) & 1))) break;
+          product_rows(at_dp, smem_do, smem_v + nv * Shape::kTileBytes, k_steps, desc_s);
+          mma_commit(smem_addr(&ctl.dp_full));
+          mma_commit(smem_addr(&ctl.v_empty[nv]));
+        }
+        if (j >= 0) {
+          product_tmem(at_dq, at_s + (j & 1) * 128, 64, smem_k + (j % SK) * Shape::kTileBytes, desc_acc, j > 0);
+          mma_commit(smem_addr(&ctl.k_empty[j % SK]));
+        }
+      }
+      if (ok && steps > 0) mma_commit(smem_addr(&ctl.acc_full));
+      if (ctl.dead) {
+        mma_commit(smem_addr(&ctl.done));
+        drain(smem_addr(&ctl.done), 0);
+      }
+    }
+  } else {   // ---- rows: queries; the warpgroups take 64 of a step's keys each
+    more_registers();
+    const int g = warp / 4, r = (warp % 4) * 32;
+    const int i = m0 + r + lane;
+    const uint32_t at = ((uint32_t)r << 16) + g * 64;
+    const ScoreMod mod(p, h);
+    int lo = 0, hi = 0;
+    float lse = 0.0f, delta = 0.0f;
+    if (i < p.tokens) {
+      p.mask.keys_of(i, &lo, &hi);
+      lse = p.row_lse[h * p.pitch + i];
+      delta = p.row_delta[h * p.pitch + i];
+    }
+    bool ok = true;
+    for (int j = 0; j < steps; ++j) {
+      const uint32_t buf = at_s + (j & 1) * 128 + at;
+      const int c0 = n_lo + j * kTile + g * 64;
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.s_full[j & 1]), (j >> 1) & 1));
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t x[64];
+      tmem_load32(buf, x);
+      tmem_load32(buf + 32, x + 32);
+      tmem_wait_load();
+      tmem_landed(x);
+      tmem_landed(x + 32);
+      const bool whole = __all_sync(0xffffffffu, i >= p.tokens || (lo <= c0 && hi >= c0 + 64));
+      const int a = lo - c0, b = hi - c0;
+      float pr[64];
+#pragma unroll
+      for (int c = 0; c < 64; ++c) {
+        float e, grad = 1.0f;
+        if constexpr (kMod) e = mod(__uint_as_float(x[c]), (float)(i - c0) - (float)c, &grad) - lse;
+        else e = fmaf(__uint_as_float(x[c]), p.scale_log2, -lse);
+        pr[c] = exp2_approx(e) * grad;
+      }
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.dp_full), j & 1));
+      if (!ok) break;
+      tc_fence_after();
+      tmem_load32(at_dp + at, x);
+      tmem_load32(at_dp + at + 32, x + 32);
+      tmem_wait_load();
+      tmem_landed(x);
+      tmem_landed(x + 32);
+      uint32_t pk[32];
+#pragma unroll
+      for (int c = 0; c < 32; ++c) {
+        float e0 = pr[2 * c] * (__uint_as_float(x[2 * c]) - delta);
+        float e1 = pr[2 * c + 1] * (__uint_as_float(x[2 * c + 1]) - delta);
+        if (!whole) {
+          e0 = 2 * c >= a && 2 * c < b ? e0 : 0.0f;
+          e1 = 2 * c + 1 >= a && 2 * c + 1 < b ? e1 : 0.0f;
+        }
+        pk[c] = pack_bf16(e0, e1);
+      }
+      tmem_store32(buf, pk);
+      tmem_wait_store();
+      tc_fence_before();
+      mbar_arrive(smem_addr(&ctl.ds_ready));
+    }
+    if (ok && steps > 0) {
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.acc_full), 0));
+      tc_fence_after();
+    }
+    bool nan = false;
+    if (ok) {
+      uint16_t* row = p.dq.p + (int64_t)i * p.dq.t + h * p.dq.h;
+#pragma unroll
+      for (int c = 0; c < HALVES; ++c) {   // the warpgroups store half of the columns each
+        const int d0 = g * HALVES * 32 + c * 32;
+        uint32_t o[32];
+        if (steps > 0) {
+          tmem_load32(at_dq + ((uint32_t)r << 16) + d0, o);
+          tmem_wait_load();
+          tmem_landed(o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int d = d0 + e * 8;
+          float y[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[e * 8 + k]) * p.scale;
+          if (i < p.tokens && d < p.head_dim) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) nan |= y[k] != y[k];
+            *reinterpret_cast<uint4*>(row + d) =
+                make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+          }
+        }
+      }
+    }
+    const uint32_t mine = __ballot_sync(0xffffffffu, nan);
+    if (lane == 0 && mine) atomicOr(&ctl.redo[warp % 4], mine);
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (g == 0)
+      for (uint32_t redo = ctl.redo[warp % 4]; redo; redo &= redo - 1) attention_dq_row(p, m0 + r + __ffs(redo) - 1, h);
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) tmem_free(tmem, kTmemColumns);
+}
+
+// ---- host -------------------------------------------------------------------------------------------------
+
+namespace host {
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeTiled encode_tiled() {
+  static std::atomic<void*> cached{nullptr};
+  void* f = cached.load();
+  if (!f) {
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      return nullptr;
+    cached.store(f);
+  }
+  return reinterpret_cast<EncodeTiled>(f);
+}
+
+// A view as (value, head, token) with boxes of 64 values of 128 tokens of one head; zeros outside.
+static bool make_map(CUtensorMap* map, const AttnView& v, const AttnParams& p, int heads) {
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)p.head_dim, (cuuint64_t)heads, (cuuint64_t)p.tokens};
+  // the stride of an axis of one entry is not used, but must be valid
+  const cuuint64_t strides[2] = {(cuuint64_t)(heads > 1 ? v.h * 2 : p.head_dim * 2), (cuuint64_t)(p.tokens > 1 ? v.t * 2 : p.head_dim * 2)};
+  const cuuint32_t box[3] = {64, 1, (cuuint32_t)kTile}, ones[3] = {1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, v.p, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The shared memory that a kernel needs beyond the default is asked for once per device and kernel.
+template <typename K>
+static cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>* done, int device) {
+  const uint64_t bit = 1ull << (device & 63);
+  if (done->load() & bit) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done->fetch_or(bit);
+  return e;
+}
+
+static bool plain_scores(const AttnParams& p) { return p.softcap == 0.0f && !p.slopes && p.scale_log2 > 0.0f; }
+
+template <int HALVES, bool kMod>
+static int forward(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
+  static std::atomic<uint64_t> ready{0};
+  CUtensorMap q, k, v;
+  if (!make_map(&q, p.q, p, p.heads_q) || !make_map(&k, p.k, p, p.heads_kv) || !make_map(&v, p.v, p, p.heads_kv))
+    return SLIDEDP_ERR_CUDA;
+  CU(allow_smem(attention_forward_mma_kernel<HALVES, kMod>, ForwardShape<HALVES>::kSmem, &ready, ctx->device));
+  const int64_t blocks = (int64_t)((p.tokens + 2 * kTile - 1) / (2 * kTile)) * p.heads_q;
+  if (blocks > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
+  attention_forward_mma_kernel<HALVES, kMod><<<(unsigned)blocks, kMmaThreads, ForwardShape<HALVES>::kSmem, st>>>(p, q, k, v);
+  ctx->launches += 1;
+  CU_AFTER_LAUNCH();
+  return SLIDEDP_OK;
+}
+
+template <int HALVES, bool kMod>
+static int backward(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
+  static std::atomic<uint64_t> ready_q{0}, ready_k{0};
+  CUtensorMap q, k, v, d;
+  if (!make_map(&q, p.q, p, p.heads_q) || !make_map(&k, p.k, p, p.heads_kv) || !make_map(&v, p.v, p, p.heads_kv) ||
+      !make_map(&d, p.dout, p, p.heads_q))
+    return SLIDEDP_ERR_CUDA;
+  CU(allow_smem(attention_dkv_mma_kernel<HALVES, kMod>, KeysShape<HALVES>::kSmem, &ready_k, ctx->device));
+  CU(allow_smem(attention_dq_mma_kernel<HALVES, kMod>, QueriesShape<HALVES>::kSmem, &ready_q, ctx->device));
+  const int64_t tiles = (p.tokens + kTile - 1) / kTile;
+  if (tiles * p.heads_q > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
+  FAULT_POINT();
+  attention_dkv_mma_kernel<HALVES, kMod><<<(unsigned)(tiles * p.heads_kv), kMmaThreads, KeysShape<HALVES>::kSmem, st>>>(p, q, k, v, d);
+  ctx->launches += 1;
+  CU_AFTER_LAUNCH();
+  FAULT_POINT();
+  attention_dq_mma_kernel<HALVES, kMod><<<(unsigned)(tiles * p.heads_q), kMmaThreads, QueriesShape<HALVES>::kSmem, st>>>(p, q, k, v, d);
+  ctx->launches += 1;
+  CU_AFTER_LAUNCH();
+  return SLIDEDP_OK;
+}
+
+int attention_forward_mma(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
+  if (p.head_dim <= 64) return plain_scores(p) ? forward<1, false>(ctx, p, st) : forward<1, true>(ctx, p, st);
+  return plain_scores(p) ? forward<2, false>(ctx, p, st) : forward<2, true>(ctx, p, st);
+}
+
+int attention_backward_mma(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
+  if (p.head_dim <= 64) return plain_scores(p) ? backward<1, false>(ctx, p, st) : backward<1, true>(ctx, p, st);
+  return plain_scores(p) ? backward<2, false>(ctx, p, st) : backward<2, true>(ctx, p, st);
+}
+
+}  // namespace host
+}  // namespace slidedp

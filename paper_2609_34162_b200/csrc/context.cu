@@ -62,6 +62,8 @@ int slidedp_create(slidedp_ctx** out, int device, size_t gpu_budget_bytes) {
   ctx->partials_cap = kInitialPartials;
   step(cudaMalloc(&ctx->scalars, 4 * sizeof(double)));
   step(cudaMallocHost(&ctx->host_scalars, 4 * sizeof(double)));
+  step(cudaMallocHost(&ctx->kernel_error, sizeof(int)));
+  if (e == cudaSuccess) *ctx->kernel_error = 0;
   step(cudaStreamCreateWithFlags(&ctx->s_in, cudaStreamNonBlocking));
   step(cudaStreamCreateWithFlags(&ctx->s_compute, cudaStreamNonBlocking));
   step(cudaStreamCreateWithFlags(&ctx->s_out, cudaStreamNonBlocking));
@@ -114,6 +116,7 @@ int slidedp_destroy(slidedp_ctx* ctx) {
   if (ctx->partials) cudaFree(ctx->partials);
   if (ctx->scalars) cudaFree(ctx->scalars);
   if (ctx->host_scalars) cudaFreeHost(ctx->host_scalars);
+  if (ctx->kernel_error) cudaFreeHost(ctx->kernel_error);
   (void)cudaGetLastError();
   delete ctx;
   return rc;

@@ -51,6 +51,7 @@ struct slidedp_ctx {
   double* scalars = nullptr;        // device: sumsq, norm, coef, nonfinite
   double* host_scalars = nullptr;   // pinned mirror
   bool norm_issued = false;
+  int* kernel_error = nullptr;      // pinned: set by a kernel whose bounded wait ran out
   cudaEvent_t scalar_event = nullptr;
   // host-resident streaming
   cudaStream_t s_in = nullptr, s_compute = nullptr, s_out = nullptr;

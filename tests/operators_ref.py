@@ -78,7 +78,7 @@ def attention(q, k, v, scale, ok, softcap=0.0, slopes=None, do=None):
         for n, x in (("dq", q), ("dk", k), ("dv", v)):
             res[n], res[n + "_bound"] = torch.zeros_like(x), torch.zeros_like(x)
     dist = (torch.arange(T, device=dev)[:, None] - torch.arange(T, device=dev)[None, :]).abs().double()
-    u = 2.0 ** -9                                    # half an ulp of BF16, relative
+    u = 2.0 ** -8       # BF16 has 8 significant bits: rounding moves a value of [1, 2) by up to 2^-8
     for h in range(Hq):
         kk, vv = k[:, h // G], v[:, h // G]
         s = q[:, h] @ kk.T * scale
