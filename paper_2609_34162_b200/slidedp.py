@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -154,10 +155,6 @@ _lib.slidedp_model_stream_step.argtypes = [ctypes.c_int64, ctypes.c_int, ctypes.
                                            ctypes.POINTER(ctypes.c_double)]
 
 
-class _Heads(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("stride_token", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
-
-
 class _QkArgs(ctypes.Structure):
     _fields_ = [("tokens", ctypes.c_int64), ("heads_q", ctypes.c_int32), ("heads_k", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("rope_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
@@ -177,19 +174,20 @@ class _DistillArgs(ctypes.Structure):
                 ("temperature", ctypes.c_double), ("w_teacher", ctypes.c_double), ("w_label", ctypes.c_double)]
 
 
-_hp, _qp, _ap, _dp = (ctypes.POINTER(t) for t in (_Heads, _QkArgs, _AttnArgs, _DistillArgs))
+_qp, _ap, _dp = (ctypes.POINTER(t) for t in (_QkArgs, _AttnArgs, _DistillArgs))
+_HEADS = 24                                     # sizeof(slidedp_heads): address and two strides
+_pack_heads = {n: struct.Struct("@" + "Qqq" * n).pack_into for n in (4, 6, 8)}
+# views are passed as addresses of the context's argument block (_HEADS bytes each)
 for _name, _res, _args in (
-        ("slidedp_qk_norm_rope", ctypes.c_int, [_vp, _qp, _hp, _hp, _vp, _vp, _vp, _vp, _hp, _hp, _vp]),
-        ("slidedp_qk_norm_rope_backward", ctypes.c_int,
-         [_vp, _qp, _hp, _hp, _vp, _vp, _vp, _vp, _hp, _hp, _hp, _hp, _vp, _vp, _vp, _vp]),
+        ("slidedp_qk_norm_rope", ctypes.c_int, [_vp, _qp] + [_vp] * 9),
+        ("slidedp_qk_norm_rope_backward", ctypes.c_int, [_vp, _qp] + [_vp] * 14),
         ("slidedp_qk_norm_rope_workspace", ctypes.c_size_t, [_qp]),
-        ("slidedp_attention", ctypes.c_int, [_vp, _ap, _hp, _hp, _hp, _hp, _vp, _vp]),
-        ("slidedp_attention_backward", ctypes.c_int,
-         [_vp, _ap, _hp, _hp, _hp, _hp, _vp, _hp, _hp, _hp, _hp, _vp, _vp]),
+        ("slidedp_attention", ctypes.c_int, [_vp, _ap] + [_vp] * 6),
+        ("slidedp_attention_backward", ctypes.c_int, [_vp, _ap] + [_vp] * 11),
         ("slidedp_attention_workspace", ctypes.c_size_t, [_ap]),
-        ("slidedp_distill_loss", ctypes.c_int, [_vp, _dp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
-        ("slidedp_distill_loss_backward", ctypes.c_int, [_vp, _dp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
-        ("slidedp_distill_step", ctypes.c_int, [_vp, _dp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp])):
+        ("slidedp_distill_loss", ctypes.c_int, [_vp, _dp] + [_vp] * 7),
+        ("slidedp_distill_loss_backward", ctypes.c_int, [_vp, _dp] + [_vp] * 8),
+        ("slidedp_distill_step", ctypes.c_int, [_vp, _dp] + [_vp] * 9)):
     getattr(_lib, _name).restype, getattr(_lib, _name).argtypes = _res, _args
 
 
@@ -224,8 +222,8 @@ def _grad_array(grads):
 
 
 def _stream(stream) -> int:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:       # the current stream's handle, without building a Stream object around it
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -234,37 +232,47 @@ def _stream(stream) -> int:
 _DTYPES = {torch.bfloat16: 0, torch.float32: 1}      # slidedp_dtype
 
 
-def _want(x, what: str, dtype, shape=None, contiguous: bool = True):
-    """What the library cannot see of a raw pointer: type, shape, device and layout of a tensor."""
-    if not isinstance(x, torch.Tensor) or x.dtype != dtype or not (x.is_cuda or x.numel() == 0):
+def _refuse(x, what: str, dtype, shape):
+    if not isinstance(x, torch.Tensor) or x.dtype != dtype or not x.is_cuda:
         raise TypeError(f"{what} must be a CUDA tensor of {dtype}")
     if shape is not None and tuple(x.shape) != tuple(shape):
         raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(x.shape)}")
-    if contiguous and not x.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
-    return x
+    raise ValueError(f"{what} must be contiguous")
+
+
+def _flat(x, what: str, dtype, shape=None) -> int:
+    """Address of a contiguous tensor, after what the library cannot see of an address: its type, shape,
+    device and layout."""
+    if (not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or not x.is_contiguous()
+            or (shape is not None and x.shape != shape)):
+        _refuse(x, what, dtype, shape)
+    return x.data_ptr()
 
 
 def _heads(x, what: str, dtype, shape):
-    """A [tokens, heads, head_dim] tensor, its last axis contiguous, as a slidedp_heads view."""
-    _want(x, what, dtype, shape, contiguous=False)
-    if x.shape[-1] > 1 and x.stride(-1) != 1:
+    """Address and strides of a [tokens, heads, head_dim] tensor whose last axis is contiguous."""
+    if not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or x.shape != shape:
+        _refuse(x, what, dtype, shape)
+    t, h, d = x.stride()
+    if d != 1 and shape[2] > 1:
         raise ValueError(f"the last axis of {what} must be contiguous")
-    return _Heads(x.data_ptr() or None, x.stride(0), x.stride(1))
+    return x.data_ptr(), t, h
 
 
 def _matrix(x, what: str, dtype, shape) -> int:
-    """A [rows, columns] tensor, its last axis contiguous; returns its row stride."""
-    _want(x, what, dtype, shape, contiguous=False)
-    if x.shape[1] > 1 and x.stride(1) != 1:
+    """Row stride of a [rows, columns] tensor whose last axis is contiguous."""
+    if not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or x.shape != shape:
+        _refuse(x, what, dtype, shape)
+    t, c = x.stride()
+    if c != 1 and shape[1] > 1:
         raise ValueError(f"the last axis of {what} must be contiguous")
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    return t if shape[0] > 1 else shape[1]
 
 
-def _workspace(x, nbytes: int):
+def _workspace(x, nbytes: int) -> int:
     if x is None or not x.is_cuda or not x.is_contiguous() or x.numel() * x.element_size() < nbytes:
         raise ValueError(f"workspace must be a contiguous CUDA tensor of at least {nbytes} bytes")
-    return x
+    return x.data_ptr()
 
 
 class Context:
@@ -277,6 +285,9 @@ class Context:
             self._h = _vp()
             raise SlideDPError(rc)
         self.device = device
+        self._views = ctypes.create_string_buffer(8 * _HEADS)      # slidedp_heads of the call being made
+        at = ctypes.addressof(self._views)
+        self._at = [at + i * _HEADS for i in range(8)]
 
     def _check(self, rc: int):
         if rc != OK:
@@ -465,73 +476,63 @@ class Context:
             raise TypeError("q and k must be bfloat16 or float32")
         if q.dim() != 3 or k.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
             raise ValueError("q and k must be [tokens, heads, head_dim] with the same tokens and head_dim")
+        T, H, D = q.shape
         rows, rope = cos_sin.shape if cos_sin is not None else (0, 0)
-        return _QkArgs(q.shape[0], q.shape[1], k.shape[1], q.shape[2], rope, int(interleaved), _DTYPES[q.dtype],
-                       rows, eps)
+        return _QkArgs(T, H, k.shape[1], D, rope, bool(interleaved), _DTYPES[q.dtype], rows, eps)
 
     @staticmethod
-    def _qk_common(q, k, w_q, w_k, cos_sin, positions):
-        D = q.shape[2]
-        for w, what in ((w_q, "w_q"), (w_k, "w_k")):
-            if w is not None:
-                _want(w, what, q.dtype, (D,))
-        if cos_sin is not None:
-            _want(cos_sin, "cos_sin", torch.float32)
-        if positions is not None:
-            _want(positions, "positions", torch.int32, (q.shape[0],))
-        return (ctypes.byref(_heads(q, "q", q.dtype, q.shape)), ctypes.byref(_heads(k, "k", q.dtype, k.shape)),
-                _ptr(w_q), _ptr(w_k), _ptr(cos_sin), _ptr(positions))
+    def _qk_tables(a, dtype, w_q, w_k, cos_sin, positions):
+        D = (a.head_dim,)
+        return (None if w_q is None else _flat(w_q, "w_q", dtype, D), None if w_k is None else _flat(w_k, "w_k", dtype, D),
+                None if cos_sin is None else _flat(cos_sin, "cos_sin", torch.float32),
+                None if positions is None else _flat(positions, "positions", torch.int32, (a.tokens,)))
 
     def slidedp_qk_norm_rope(self, q, k, w_q, w_k, cos_sin, positions, q_out, k_out, eps: float = 1e-6,
                              interleaved: bool = False, stream=None) -> None:
         """RMS norm of every head of ``q`` and ``k`` ([tokens, heads, head_dim]) and the rotation by
         ``cos_sin`` ([rows, rope_dim]: cosines, then sines; None: no rotation) at ``positions``
         (int32 per token; None: 0, 1, ..)."""
-        a = self._qk_args(q, k, cos_sin, eps, interleaved)
-        self._check(_lib.slidedp_qk_norm_rope(
-            self._h, ctypes.byref(a), *self._qk_common(q, k, w_q, w_k, cos_sin, positions),
-            ctypes.byref(_heads(q_out, "q_out", q.dtype, q.shape)),
-            ctypes.byref(_heads(k_out, "k_out", q.dtype, k.shape)), _stream(stream)))
+        a, dt, at = self._qk_args(q, k, cos_sin, eps, interleaved), q.dtype, self._at
+        _pack_heads[4](self._views, 0, *_heads(q, "q", dt, q.shape), *_heads(k, "k", dt, k.shape),
+                       *_heads(q_out, "q_out", dt, q.shape), *_heads(k_out, "k_out", dt, k.shape))
+        self._check(_lib.slidedp_qk_norm_rope(self._h, a, at[0], at[1], *self._qk_tables(a, dt, w_q, w_k, cos_sin, positions),
+                                              at[2], at[3], _stream(stream)))
 
     def slidedp_qk_norm_rope_workspace(self, q, k) -> int:
         """Bytes of workspace that ``slidedp_qk_norm_rope_backward`` needs for these heads."""
-        return int(_lib.slidedp_qk_norm_rope_workspace(ctypes.byref(self._qk_args(q, k, None, 0.0, False))))
+        return int(_lib.slidedp_qk_norm_rope_workspace(self._qk_args(q, k, None, 0.0, False)))
 
     def slidedp_qk_norm_rope_backward(self, q, k, w_q, w_k, cos_sin, positions, dq_out, dk_out, dq, dk, dw_q,
                                       dw_k, workspace, eps: float = 1e-6, interleaved: bool = False,
                                       stream=None) -> None:
         """Gradients ``dq``, ``dk`` and (float32, may be None) ``dw_q``, ``dw_k`` from those of the outputs."""
-        a = self._qk_args(q, k, cos_sin, eps, interleaved)
-        D = q.shape[2]
-        for w, what in ((dw_q, "dw_q"), (dw_k, "dw_k")):
-            if w is not None:
-                _want(w, what, torch.float32, (D,))
+        a, dt, at = self._qk_args(q, k, cos_sin, eps, interleaved), q.dtype, self._at
+        D, f32, ws = (a.head_dim,), torch.float32, None
         if dw_q is not None or dw_k is not None:
-            _workspace(workspace, _lib.slidedp_qk_norm_rope_workspace(ctypes.byref(a)))
+            ws = _workspace(workspace, _lib.slidedp_qk_norm_rope_workspace(a))
+        _pack_heads[6](self._views, 0, *_heads(q, "q", dt, q.shape), *_heads(k, "k", dt, k.shape),
+                       *_heads(dq_out, "dq_out", dt, q.shape), *_heads(dk_out, "dk_out", dt, k.shape),
+                       *_heads(dq, "dq", dt, q.shape), *_heads(dk, "dk", dt, k.shape))
         self._check(_lib.slidedp_qk_norm_rope_backward(
-            self._h, ctypes.byref(a), *self._qk_common(q, k, w_q, w_k, cos_sin, positions),
-            ctypes.byref(_heads(dq_out, "dq_out", q.dtype, q.shape)),
-            ctypes.byref(_heads(dk_out, "dk_out", q.dtype, k.shape)),
-            ctypes.byref(_heads(dq, "dq", q.dtype, q.shape)), ctypes.byref(_heads(dk, "dk", q.dtype, k.shape)),
-            _ptr(dw_q), _ptr(dw_k), _ptr(workspace), _stream(stream)))
+            self._h, a, at[0], at[1], *self._qk_tables(a, dt, w_q, w_k, cos_sin, positions), at[2], at[3], at[4], at[5],
+            None if dw_q is None else _flat(dw_q, "dw_q", f32, D), None if dw_k is None else _flat(dw_k, "dw_k", f32, D),
+            ws, _stream(stream)))
 
     @staticmethod
     def _attn_args(q, k, cu_docs=None, prefix=None, slopes=None, causal=True, scale=None, softcap=0.0):
         if q.dim() != 3 or k.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
             raise ValueError("q and k must be [tokens, heads, head_dim] with the same tokens and head_dim")
-        docs = 1
+        T, H, D = q.shape
+        docs, cu = 1, None
         if cu_docs is not None:
-            _want(cu_docs, "cu_docs", torch.int32)
+            cu = _flat(cu_docs, "cu_docs", torch.int32)
             if cu_docs.dim() != 1 or cu_docs.numel() < 1:
                 raise ValueError("cu_docs must hold docs + 1 offsets")
             docs = cu_docs.numel() - 1
-        if prefix is not None:
-            _want(prefix, "prefix", torch.int32, (docs,))
-        if slopes is not None:
-            _want(slopes, "slopes", torch.float32, (q.shape[1],))
-        return _AttnArgs(q.shape[0], q.shape[1], k.shape[1], q.shape[2], int(causal), docs, 0, _ptr(cu_docs) or None,
-                         _ptr(prefix) or None, _ptr(slopes) or None,
-                         q.shape[2] ** -0.5 if scale is None else scale, softcap)
+        return _AttnArgs(T, H, k.shape[1], D, bool(causal), docs, 0, cu,
+                         None if prefix is None else _flat(prefix, "prefix", torch.int32, (docs,)) or None,
+                         None if slopes is None else _flat(slopes, "slopes", torch.float32, (H,)),
+                         D ** -0.5 if scale is None else scale, softcap)
 
     def slidedp_attention(self, q, k, v, out, lse, cu_docs=None, prefix=None, slopes=None, causal: bool = True,
                           scale: float | None = None, softcap: float = 0.0, stream=None) -> None:
@@ -539,81 +540,73 @@ class Context:
         packed documents (``cu_docs``: int32 offsets; None: one document). Fills ``out`` and ``lse``
         [heads_q, tokens]. ``scale`` defaults to head_dim ** -0.5."""
         a = self._attn_args(q, k, cu_docs, prefix, slopes, causal, scale, softcap)
-        bf = torch.bfloat16
-        _want(lse, "lse", torch.float32, (q.shape[1], q.shape[0]))
-        self._check(_lib.slidedp_attention(
-            self._h, ctypes.byref(a), ctypes.byref(_heads(q, "q", bf, q.shape)), ctypes.byref(_heads(k, "k", bf, k.shape)),
-            ctypes.byref(_heads(v, "v", bf, k.shape)), ctypes.byref(_heads(out, "out", bf, q.shape)), _ptr(lse),
-            _stream(stream)))
+        bf, at, qs, ks = torch.bfloat16, self._at, q.shape, k.shape
+        _pack_heads[4](self._views, 0, *_heads(q, "q", bf, qs), *_heads(k, "k", bf, ks), *_heads(v, "v", bf, ks),
+                       *_heads(out, "out", bf, qs))
+        self._check(_lib.slidedp_attention(self._h, a, at[0], at[1], at[2], at[3],
+                                           _flat(lse, "lse", torch.float32, (qs[1], qs[0])), _stream(stream)))
 
     def slidedp_attention_workspace(self, q, k) -> int:
         """Bytes of workspace that ``slidedp_attention_backward`` needs."""
-        return int(_lib.slidedp_attention_workspace(ctypes.byref(self._attn_args(q, k))))
+        return int(_lib.slidedp_attention_workspace(self._attn_args(q, k)))
 
     def slidedp_attention_backward(self, q, k, v, out, lse, d_out, dq, dk, dv, workspace, cu_docs=None, prefix=None,
                                    slopes=None, causal: bool = True, scale: float | None = None,
                                    softcap: float = 0.0, stream=None) -> None:
         """Gradients ``dq``, ``dk``, ``dv`` from ``d_out``, with the forward's ``out`` and ``lse``."""
         a = self._attn_args(q, k, cu_docs, prefix, slopes, causal, scale, softcap)
-        bf = torch.bfloat16
-        _want(lse, "lse", torch.float32, (q.shape[1], q.shape[0]))
-        _workspace(workspace, _lib.slidedp_attention_workspace(ctypes.byref(a)))
-        view = lambda x, what, like: ctypes.byref(_heads(x, what, bf, like.shape))  # noqa: E731
+        bf, at, qs, ks = torch.bfloat16, self._at, q.shape, k.shape
+        ws = _workspace(workspace, _lib.slidedp_attention_workspace(a))
+        _pack_heads[8](self._views, 0, *_heads(q, "q", bf, qs), *_heads(k, "k", bf, ks), *_heads(v, "v", bf, ks),
+                       *_heads(out, "out", bf, qs), *_heads(d_out, "d_out", bf, qs), *_heads(dq, "dq", bf, qs),
+                       *_heads(dk, "dk", bf, ks), *_heads(dv, "dv", bf, ks))
         self._check(_lib.slidedp_attention_backward(
-            self._h, ctypes.byref(a), view(q, "q", q), view(k, "k", k), view(v, "v", k), view(out, "out", q), _ptr(lse),
-            view(d_out, "d_out", q), view(dq, "dq", q), view(dk, "dk", k), view(dv, "dv", k), _ptr(workspace),
-            _stream(stream)))
+            self._h, a, at[0], at[1], at[2], at[3], _flat(lse, "lse", torch.float32, (qs[1], qs[0])), at[4], at[5], at[6],
+            at[7], ws, _stream(stream)))
 
     @staticmethod
-    def _distill_args(logits, teacher_ids, teacher_logits, labels, d_logits, temperature, w_teacher, w_label):
+    def _distill_call(logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits, temperature, w_teacher,
+                      w_label):
+        """The arguments that the three calls share: slidedp_distill_args and the addresses of the inputs, of
+        lse and of the row gradients."""
         if logits.dtype not in _DTYPES or logits.dim() != 2:
             raise TypeError("logits must be [rows, vocab] of bfloat16 or float32")
-        rows, vocab = logits.shape
-        stride = _matrix(logits, "logits", logits.dtype, logits.shape)
-        d_stride = _matrix(d_logits, "d_logits", logits.dtype, logits.shape) if d_logits is not None else 0
+        dt, shape, f32, i32 = logits.dtype, logits.shape, torch.float32, torch.int32
+        rows, vocab = shape
         entries = teacher_ids.shape[-1]
-        _want(teacher_ids, "teacher_ids", torch.int32, (rows, entries))
-        _want(teacher_logits, "teacher_logits", torch.float32, (rows, entries))
-        if labels is not None:
-            _want(labels, "labels", torch.int32, (rows,))
-        return _DistillArgs(rows, vocab, entries, _DTYPES[logits.dtype], stride, d_stride, temperature, w_teacher,
-                            w_label)
+        a = _DistillArgs(rows, vocab, entries, _DTYPES[dt], _matrix(logits, "logits", dt, shape),
+                         0 if d_logits is None else _matrix(d_logits, "d_logits", dt, shape), temperature, w_teacher, w_label)
+        return (a, (logits.data_ptr(), _flat(teacher_ids, "teacher_ids", i32, (rows, entries)),
+                    _flat(teacher_logits, "teacher_logits", f32, (rows, entries)),
+                    None if labels is None else _flat(labels, "labels", i32, (rows,))),
+                _flat(lse, "lse", f32, (2, rows)), None if row_grad is None else _flat(row_grad, "row_grad", f32, (rows,)))
 
     def slidedp_distill_loss(self, logits, teacher_ids, teacher_logits, labels, loss, lse, temperature: float = 1.0,
                              w_teacher: float = 1.0, w_label: float = 0.0, stream=None) -> None:
         """Per-row distillation ``loss`` and ``lse`` [2, rows] of ``logits`` [rows, vocab] against the teacher's
         stored entries (int32 ids, float32 logits, both [rows, entries]) and int32 ``labels`` (may be None)."""
-        a = self._distill_args(logits, teacher_ids, teacher_logits, labels, None, temperature, w_teacher, w_label)
-        _want(loss, "loss", torch.float32, (a.rows,))
-        _want(lse, "lse", torch.float32, (2, a.rows))
-        self._check(_lib.slidedp_distill_loss(self._h, ctypes.byref(a), _ptr(logits), _ptr(teacher_ids),
-                                              _ptr(teacher_logits), _ptr(labels), _ptr(loss), _ptr(lse), _stream(stream)))
+        a, ins, l, _ = self._distill_call(logits, teacher_ids, teacher_logits, labels, lse, None, None, temperature,
+                                          w_teacher, w_label)
+        self._check(_lib.slidedp_distill_loss(self._h, a, *ins, _flat(loss, "loss", torch.float32, (a.rows,)), l,
+                                              _stream(stream)))
 
     def slidedp_distill_loss_backward(self, logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits,
                                       temperature: float = 1.0, w_teacher: float = 1.0, w_label: float = 0.0,
                                       stream=None) -> None:
         """``d_logits`` = ``row_grad`` (float32 per row; None: ones) times the loss's gradient, with the forward's
         ``lse``. ``d_logits`` may be ``logits``."""
-        a = self._distill_args(logits, teacher_ids, teacher_logits, labels, d_logits, temperature, w_teacher, w_label)
-        _want(lse, "lse", torch.float32, (2, a.rows))
-        if row_grad is not None:
-            _want(row_grad, "row_grad", torch.float32, (a.rows,))
-        self._check(_lib.slidedp_distill_loss_backward(
-            self._h, ctypes.byref(a), _ptr(logits), _ptr(teacher_ids), _ptr(teacher_logits), _ptr(labels), _ptr(lse),
-            _ptr(row_grad), _ptr(d_logits), _stream(stream)))
+        a, ins, l, g = self._distill_call(logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits,
+                                          temperature, w_teacher, w_label)
+        self._check(_lib.slidedp_distill_loss_backward(self._h, a, *ins, l, g, d_logits.data_ptr(), _stream(stream)))
 
     def slidedp_distill_step(self, logits, teacher_ids, teacher_logits, labels, row_grad, loss, lse, d_logits,
                              temperature: float = 1.0, w_teacher: float = 1.0, w_label: float = 0.0,
                              stream=None) -> None:
         """``loss``, ``lse`` and ``d_logits`` in one pass over the logits."""
-        a = self._distill_args(logits, teacher_ids, teacher_logits, labels, d_logits, temperature, w_teacher, w_label)
-        _want(loss, "loss", torch.float32, (a.rows,))
-        _want(lse, "lse", torch.float32, (2, a.rows))
-        if row_grad is not None:
-            _want(row_grad, "row_grad", torch.float32, (a.rows,))
-        self._check(_lib.slidedp_distill_step(
-            self._h, ctypes.byref(a), _ptr(logits), _ptr(teacher_ids), _ptr(teacher_logits), _ptr(labels),
-            _ptr(row_grad), _ptr(loss), _ptr(lse), _ptr(d_logits), _stream(stream)))
+        a, ins, l, g = self._distill_call(logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits,
+                                          temperature, w_teacher, w_label)
+        self._check(_lib.slidedp_distill_step(self._h, a, *ins, g, _flat(loss, "loss", torch.float32, (a.rows,)), l,
+                                              d_logits.data_ptr(), _stream(stream)))
 
 
 def slidedp_model_stream_step(n_total: int, R: int, chunk_elems: int, nbuf: int, h2d_gbs: float,
