@@ -39,19 +39,22 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, 
   for (int c = 0; c < HALVES; ++c) tma_load_3d(dst + c * kHalfBytes, map, c * 64, head, row, bar);
 }
 
-// D (+)= A B^T over the heads' values: A and B tiles in shared memory, both contracted along their rows.
-__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, int steps, uint32_t desc) {
-  for (int k = 0; k < steps; ++k) {
-    const uint32_t off = (k >> 2) * kHalfBytes;
-    mma_ss(d, smem_desc_k_major(a + off) + (k & 3) * kKStep, smem_desc_k_major(b + off) + (k & 3) * kKStep, desc, k > 0);
+// D = A B^T over the heads' values: A and B tiles in shared memory, both contracted along their rows.
+__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, int steps, uint32_t desc, bool leader) {
+  const uint64_t da = smem_desc_k_major(a), db = smem_desc_k_major(b);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint64_t off = (k >> 2) * (kHalfBytes >> 4) + (k & 3) * kKStep;
+    if (k < steps) mma_ss(d, da + off, db + off, desc, k > 0, leader);
   }
 }
 // D (+)= A B with A (BF16, 128 contracted columns) in TMEM and B a tile contracted over its rows. A's columns
 // 64..127 start `second` TMEM columns after the first 64 (32 when all lie together).
-__device__ __forceinline__ void product_tmem(uint32_t d, uint32_t a, uint32_t second, uint32_t b, uint32_t desc, bool add) {
+__device__ __forceinline__ void product_tmem(uint32_t d, uint32_t a, uint32_t second, uint32_t b, uint32_t desc, bool add, bool leader) {
+  const uint64_t db = smem_desc_mn_major(b, kHalfBytes);
 #pragma unroll
   for (int k = 0; k < kTile / 16; ++k)
-    mma_ts(d, a + (k >> 2) * second + (k & 3) * 8, smem_desc_mn_major(b, kHalfBytes) + k * kRowStep, desc, add || k > 0);
+    mma_ts(d, a + (k >> 2) * second + (k & 3) * 8, db + k * kRowStep, desc, add || k > 0, leader);
 }
 
 // Capped and biased scores, in units of log2 e, and the factor of d score / d product.
@@ -107,7 +110,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   constexpr int S = Shape::kStages;
   extern __shared__ uint8_t raw_smem[];
   __shared__ ForwardControl ctl;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   const int tiles = (p.tokens + 2 * kTile - 1) / (2 * kTile);
   // the last queries see the most keys when causal: start with them
   const int h = blockIdx.x % p.heads_q, m0 = (tiles - 1 - (int)(blockIdx.x / p.heads_q)) * 2 * kTile;
@@ -192,41 +195,43 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         for (int j = k_sent > S ? k_sent - S : 0; j < k_sent; ++j) drain(smem_addr(&ctl.k_full[j % S]), (j / S) & 1);
         for (int j = v_sent > S ? v_sent - S : 0; j < v_sent; ++j) drain(smem_addr(&ctl.v_full[j % S]), (j / S) & 1);
       }
-    } else if (warp == 8 && lane == 0) {   // ---- issuer
+    } else if (warp == 8) {   // ---- issuer
+      const bool leader = elect_leader();
+      const auto wait_all = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
       const int k_steps = (p.head_dim + 15) / 16;
       const uint32_t desc_s = mma_desc_bf16(kTile, false), desc_o = mma_desc_bf16(k_steps * 16, true);
-      bool ok = steps == 0 || wait(smem_addr(&ctl.q_full), 0);
+      bool ok = steps == 0 || wait_all(smem_addr(&ctl.q_full), 0);
       for (int j = -1; j < steps && ok; ++j) {
         // products of step j's probabilities, and step j + 1's scores
         const int st = j % S, nx = (j + 1) % S;
         bool have_k = false;
-        if (j >= 0 && !(ok = wait(smem_addr(&ctl.v_full[st]), (j / S) & 1))) break;
+        if (j >= 0 && !(ok = wait_all(smem_addr(&ctl.v_full[st]), (j / S) & 1))) break;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           if (j >= first[s] && j < last[s]) {
-            if (!(ok = wait(smem_addr(&ctl.p_ready[s]), (j - first[s]) & 1))) break;
+            if (!(ok = wait_all(smem_addr(&ctl.p_ready[s]), (j - first[s]) & 1))) break;
             tc_fence_after();
-            product_tmem(tmem + 256 + s * 128, tmem + s * 128, 32, smem_v + st * Shape::kTileBytes, desc_o, j > first[s]);
-            if (j == last[s] - 1) mma_commit(smem_addr(&ctl.o_full[s]));
+            product_tmem(tmem + 256 + s * 128, tmem + s * 128, 32, smem_v + st * Shape::kTileBytes, desc_o, j > first[s], leader);
+            if (j == last[s] - 1) mma_commit(smem_addr(&ctl.o_full[s]), leader);
           }
           if (j + 1 >= first[s] && j + 1 < last[s]) {
             if (!have_k) {
-              if (!(ok = wait(smem_addr(&ctl.k_full[nx]), ((j + 1) / S) & 1))) break;
+              if (!(ok = wait_all(smem_addr(&ctl.k_full[nx]), ((j + 1) / S) & 1))) break;
               have_k = true;
             }
-            product_rows(tmem + s * 128, smem_q + s * Shape::kTileBytes, smem_k + nx * Shape::kTileBytes, k_steps, desc_s);
-            mma_commit(smem_addr(&ctl.s_full[s]));
+            product_rows(tmem + s * 128, smem_q + s * Shape::kTileBytes, smem_k + nx * Shape::kTileBytes, k_steps, desc_s, leader);
+            mma_commit(smem_addr(&ctl.s_full[s]), leader);
           }
         }
         if (!ok) break;
-        if (j >= 0) mma_commit(smem_addr(&ctl.v_empty[st]));
+        if (j >= 0) mma_commit(smem_addr(&ctl.v_empty[st]), leader);
         if (j + 1 < steps) {
-          if (!have_k && !(ok = wait(smem_addr(&ctl.k_full[nx]), ((j + 1) / S) & 1))) break;
-          mma_commit(smem_addr(&ctl.k_empty[nx]));
+          if (!have_k && !(ok = wait_all(smem_addr(&ctl.k_full[nx]), ((j + 1) / S) & 1))) break;
+          mma_commit(smem_addr(&ctl.k_empty[nx]), leader);
         }
       }
       if (ctl.dead) {
-        mma_commit(smem_addr(&ctl.done));
+        mma_commit(smem_addr(&ctl.done), leader);
         drain(smem_addr(&ctl.done), 0);
       }
     }
@@ -390,7 +395,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   constexpr int S = Shape::kStages;
   extern __shared__ uint8_t raw_smem[];
   __shared__ KeysControl ctl;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   const int hk = blockIdx.x % p.heads_kv, n0 = (int)(blockIdx.x / p.heads_kv) * kTile;   // first keys: most queries
   const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
   const uint32_t smem_k = base, smem_v = smem_k + Shape::kTileBytes, smem_q = smem_v + Shape::kTileBytes,
@@ -458,40 +463,42 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         for (int j = q_sent > S ? q_sent - S : 0; j < q_sent; ++j) drain(smem_addr(&ctl.q_full[j % S]), (j / S) & 1);
         for (int j = do_sent > S ? do_sent - S : 0; j < do_sent; ++j) drain(smem_addr(&ctl.do_full[j % S]), (j / S) & 1);
       }
-    } else if (warp == 8 && lane == 0) {   // ---- issuer
+    } else if (warp == 8) {   // ---- issuer
+      const bool leader = elect_leader();
+      const auto wait_all = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
       const int k_steps = (p.head_dim + 15) / 16;
       const uint32_t desc_s = mma_desc_bf16(kTile, false), desc_acc = mma_desc_bf16(k_steps * 16, true);
-      bool ok = steps == 0 || wait(smem_addr(&ctl.kv_full), 0);
+      bool ok = steps == 0 || wait_all(smem_addr(&ctl.kv_full), 0);
       for (int it = -1; it < steps && ok; ++it) {
         const int st = it % S, nx = (it + 1) % S;
         const bool more = it + 1 < steps;
         const uint32_t next_turn = ((it + 1) / S) & 1;
         if (it >= 0) {
-          if (!(ok = wait(smem_addr(&ctl.p_ready), it & 1))) break;
+          if (!(ok = wait_all(smem_addr(&ctl.p_ready), it & 1))) break;
           tc_fence_after();
-          product_tmem(at_dv, at_s, 64, smem_do + st * Shape::kTileBytes, desc_acc, it > 0);
-          mma_commit(smem_addr(&ctl.do_empty[st]));
+          product_tmem(at_dv, at_s, 64, smem_do + st * Shape::kTileBytes, desc_acc, it > 0, leader);
+          mma_commit(smem_addr(&ctl.do_empty[st]), leader);
         }
         if (more) {
-          if (!(ok = wait(smem_addr(&ctl.q_full[nx]), next_turn))) break;
-          product_rows(at_s, smem_k, smem_q + nx * Shape::kTileBytes, k_steps, desc_s);
-          mma_commit(smem_addr(&ctl.s_full));
+          if (!(ok = wait_all(smem_addr(&ctl.q_full[nx]), next_turn))) break;
+          product_rows(at_s, smem_k, smem_q + nx * Shape::kTileBytes, k_steps, desc_s, leader);
+          mma_commit(smem_addr(&ctl.s_full), leader);
         }
         if (it >= 0) {
-          if (!(ok = wait(smem_addr(&ctl.ds_ready), it & 1))) break;
+          if (!(ok = wait_all(smem_addr(&ctl.ds_ready), it & 1))) break;
           tc_fence_after();
-          product_tmem(at_dk, at_dp, 64, smem_q + st * Shape::kTileBytes, desc_acc, it > 0);
-          mma_commit(smem_addr(&ctl.q_empty[st]));
+          product_tmem(at_dk, at_dp, 64, smem_q + st * Shape::kTileBytes, desc_acc, it > 0, leader);
+          mma_commit(smem_addr(&ctl.q_empty[st]), leader);
         }
         if (more) {
-          if (!(ok = wait(smem_addr(&ctl.do_full[nx]), next_turn))) break;
-          product_rows(at_dp, smem_v, smem_do + nx * Shape::kTileBytes, k_steps, desc_s);
-          mma_commit(smem_addr(&ctl.dp_full));
+          if (!(ok = wait_all(smem_addr(&ctl.do_full[nx]), next_turn))) break;
+          product_rows(at_dp, smem_v, smem_do + nx * Shape::kTileBytes, k_steps, desc_s, leader);
+          mma_commit(smem_addr(&ctl.dp_full), leader);
         }
       }
-      if (ok && steps > 0) mma_commit(smem_addr(&ctl.acc_full));
+      if (ok && steps > 0) mma_commit(smem_addr(&ctl.acc_full), leader);
       if (ctl.dead) {
-        mma_commit(smem_addr(&ctl.done));
+        mma_commit(smem_addr(&ctl.done), leader);
         drain(smem_addr(&ctl.done), 0);
       }
     }
@@ -651,7 +658,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   constexpr int SK = Shape::kKStages, SV = Shape::kVStages;
   extern __shared__ uint8_t raw_smem[];
   __shared__ QueriesControl ctl;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   const int tiles = (p.tokens + kTile - 1) / kTile;
   const int h = blockIdx.x % p.heads_q, m0 = (tiles - 1 - (int)(blockIdx.x / p.heads_q)) * kTile;
   const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
@@ -719,36 +726,38 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         for (int j = k_sent > SK ? k_sent - SK : 0; j < k_sent; ++j) drain(smem_addr(&ctl.k_full[j % SK]), (j / SK) & 1);
         for (int j = v_sent > SV ? v_sent - SV : 0; j < v_sent; ++j) drain(smem_addr(&ctl.v_full[j % SV]), (j / SV) & 1);
       }
-    } else if (warp == 8 && lane == 0) {   // ---- issuer
+    } else if (warp == 8) {   // ---- issuer
+      const bool leader = elect_leader();
+      const auto wait_all = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
       const int k_steps = (p.head_dim + 15) / 16;
       const uint32_t desc_s = mma_desc_bf16(kTile, false), desc_acc = mma_desc_bf16(k_steps * 16, true);
-      bool ok = steps == 0 || wait(smem_addr(&ctl.q_full), 0);
+      bool ok = steps == 0 || wait_all(smem_addr(&ctl.q_full), 0);
       for (int j = -1; j < steps && ok; ++j) {
         const int nk = (j + 1) % SK, nv = (j + 1) % SV;
         const bool more = j + 1 < steps;
         if (more) {
-          if (!(ok = wait(smem_addr(&ctl.k_full[nk]), ((j + 1) / SK) & 1))) break;
-          product_rows(at_s + ((j + 1) & 1) * 128, smem_q, smem_k + nk * Shape::kTileBytes, k_steps, desc_s);
-          mma_commit(smem_addr(&ctl.s_full[(j + 1) & 1]));
+          if (!(ok = wait_all(smem_addr(&ctl.k_full[nk]), ((j + 1) / SK) & 1))) break;
+          product_rows(at_s + ((j + 1) & 1) * 128, smem_q, smem_k + nk * Shape::kTileBytes, k_steps, desc_s, leader);
+          mma_commit(smem_addr(&ctl.s_full[(j + 1) & 1]), leader);
         }
         if (j >= 0) {
-          if (!(ok = wait(smem_addr(&ctl.ds_ready), j & 1))) break;
+          if (!(ok = wait_all(smem_addr(&ctl.ds_ready), j & 1))) break;
           tc_fence_after();
         }
         if (more) {
-          if (!(ok = wait(smem_addr(&ctl.v_full[nv]), ((j + 1) / SV) & 1))) break;
-          product_rows(at_dp, smem_do, smem_v + nv * Shape::kTileBytes, k_steps, desc_s);
-          mma_commit(smem_addr(&ctl.dp_full));
-          mma_commit(smem_addr(&ctl.v_empty[nv]));
+          if (!(ok = wait_all(smem_addr(&ctl.v_full[nv]), ((j + 1) / SV) & 1))) break;
+          product_rows(at_dp, smem_do, smem_v + nv * Shape::kTileBytes, k_steps, desc_s, leader);
+          mma_commit(smem_addr(&ctl.dp_full), leader);
+          mma_commit(smem_addr(&ctl.v_empty[nv]), leader);
         }
         if (j >= 0) {
-          product_tmem(at_dq, at_s + (j & 1) * 128, 64, smem_k + (j % SK) * Shape::kTileBytes, desc_acc, j > 0);
-          mma_commit(smem_addr(&ctl.k_empty[j % SK]));
+          product_tmem(at_dq, at_s + (j & 1) * 128, 64, smem_k + (j % SK) * Shape::kTileBytes, desc_acc, j > 0, leader);
+          mma_commit(smem_addr(&ctl.k_empty[j % SK]), leader);
         }
       }
-      if (ok && steps > 0) mma_commit(smem_addr(&ctl.acc_full));
+      if (ok && steps > 0) mma_commit(smem_addr(&ctl.acc_full), leader);
       if (ctl.dead) {
-        mma_commit(smem_addr(&ctl.done));
+        mma_commit(smem_addr(&ctl.done), leader);
         drain(smem_addr(&ctl.done), 0);
       }
     }

@@ -129,22 +129,35 @@ __device__ __forceinline__ uint64_t smem_desc_mn_major(uint32_t addr, uint32_t h
   return ((uint64_t)(addr >> 4) & 0x3fff) | ((uint64_t)(half_bytes >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
 
-// D[tmem] (+)= A B, K = 16. One thread issues; the instructions of one thread execute in order.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+// D[tmem] (+)= A B, K = 16, and the arrival at a barrier when everything issued so far is done. A whole
+// warp runs the code around them, so that addresses and descriptors stay in uniform registers (one
+// lane alone took over 100 cycles per product to move them there), and `leader`, the same lane
+// throughout, issues: the instructions of one thread execute in order.
+__device__ __forceinline__ bool elect_leader() {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok));
+  return ok != 0;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add, bool leader) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add), "r"((uint32_t)leader)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {   // A in TMEM
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add, bool leader) {   // A in TMEM
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-      "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+      "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add), "r"((uint32_t)leader)
       : "memory");
 }
-// Arrives at the barrier when everything that this thread has issued so far is done.
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void mma_commit(uint32_t bar, bool leader) {
+  asm volatile(
+      "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+      " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar),
+      "r"((uint32_t)leader)
+      : "memory");
 }
 
 // ---- arithmetic ----------------------------------------------------------------------------------------
