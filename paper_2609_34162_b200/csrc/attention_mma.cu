@@ -9,6 +9,7 @@
 // BF16 roundings: probabilities and score gradients are BF16 operands of the second products (half an ulp,
 // 2^-9 of each term, like the inputs they meet); scores, statistics and accumulators are FP32.
 #include <atomic>
+#include <type_traits>
 
 #include "attention_rows.cuh"
 #include "tcgen05.cuh"
@@ -25,6 +26,7 @@ __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec
 constexpr int kTmemColumns = 512;
 constexpr uint32_t kKStep = 32 >> 4;       // descriptor step of 16 contracted values along a row
 constexpr uint32_t kRowStep = 16 * 128 >> 4;   // and of 16 contracted rows
+constexpr int kPolyOfEight = 4;           // pairs of eight that take the polynomial exponential
 constexpr float kRescaleAbove = 8.0f;      // log2: how far a row's maximum may run ahead of its scale
 
 // Waits that outlive the early exit: for copies and products of this thread still in flight.
@@ -49,12 +51,13 @@ __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b,
   }
 }
 // D (+)= A B with A (BF16, 128 contracted columns) in TMEM and B a tile contracted over its rows. A's columns
-// 64..127 start `second` TMEM columns after the first 64 (32 when all lie together).
+// 64..127 start `second` TMEM columns after the first 64 (32 when all lie together). Steps FROM..TO - 1 of 16.
+template <int FROM = 0, int TO = kTile / 16>
 __device__ __forceinline__ void product_tmem(uint32_t d, uint32_t a, uint32_t second, uint32_t b, uint32_t desc, bool add, bool leader) {
   const uint64_t db = smem_desc_mn_major(b, kHalfBytes);
 #pragma unroll
-  for (int k = 0; k < kTile / 16; ++k)
-    mma_ts(d, a + (k >> 2) * second + (k & 3) * 8, db + k * kRowStep, desc, add || k > 0, leader);
+  for (int k = FROM; k < TO; ++k)
+    mma_ts(d, a + (k >> 2) * second + (k & 3) * 8, db + k * kRowStep, desc, add || k > FROM, leader);
 }
 
 // Capped and biased scores, in units of log2 e, and the factor of d score / d product.
@@ -82,6 +85,18 @@ struct ScoreMod {
   }
 };
 
+template <int N>
+__device__ __forceinline__ void load_floats(float* y, const float* from) {
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    const float4 v = reinterpret_cast<const float4*>(from)[i];
+    y[4 * i] = v.x;
+    y[4 * i + 1] = v.y;
+    y[4 * i + 2] = v.z;
+    y[4 * i + 3] = v.w;
+  }
+}
+
 // ---- forward -------------------------------------------------------------------------------------------
 //
 // A block takes 256 queries of one head as two tiles of 128 (one per row warpgroup) and walks the keys they
@@ -97,7 +112,7 @@ template <int HALVES> struct ForwardShape {
 };
 
 struct ForwardControl {
-  uint64_t q_full, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_ready[2], o_full[2], done;
+  uint64_t q_full, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_half[2], p_ready[2], o_full[2], done;
   uint32_t tmem, dead;
   int lo[2], hi[2];   // keys that the tiles' rows see
 };
@@ -128,6 +143,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_addr(&ctl.s_full[i]), 1);
+      mbar_init(smem_addr(&ctl.p_half[i]), kTile);
       mbar_init(smem_addr(&ctl.p_ready[i]), kTile);
       mbar_init(smem_addr(&ctl.o_full[i]), 1);
     }
@@ -209,9 +225,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           if (j >= first[s] && j < last[s]) {
-            if (!(ok = wait_all(smem_addr(&ctl.p_ready[s]), (j - first[s]) & 1))) break;
+            // the first 64 keys' products run while the row warps are on the other 64
+            const uint32_t turn = (j - first[s]) & 1, v = smem_v + st * Shape::kTileBytes;
+            if (!(ok = wait_all(smem_addr(&ctl.p_half[s]), turn))) break;
             tc_fence_after();
-            product_tmem(tmem + 256 + s * 128, tmem + s * 128, 32, smem_v + st * Shape::kTileBytes, desc_o, j > first[s], leader);
+            product_tmem<0, 4>(tmem + 256 + s * 128, tmem + s * 128, 32, v, desc_o, j > first[s], leader);
+            if (!(ok = wait_all(smem_addr(&ctl.p_ready[s]), turn))) break;
+            tc_fence_after();
+            product_tmem<4, 8>(tmem + 256 + s * 128, tmem + s * 128, 32, v, desc_o, true, leader);
             if (j == last[s] - 1) mma_commit(smem_addr(&ctl.o_full[s]), leader);
           }
           if (j + 1 >= first[s] && j + 1 < last[s]) {
@@ -265,7 +286,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         for (int c = 0; c < 128; ++c) x[c] = __float_as_uint(mod(__uint_as_float(x[c]), d0 - (float)c, &g));
       }
       // rows past the sequence are not stored: they need no mask
-      if (!__all_sync(0xffffffffu, i >= p.tokens || (lo <= n0 && hi >= n0 + kTile))) {
+      const bool whole = __all_sync(0xffffffffu, i >= p.tokens || (lo <= n0 && hi >= n0 + kTile));
+      if (!whole) {
         const int a = lo - n0, b = hi - n0;
 #pragma unroll
         for (int c = 0; c < 128; ++c) x[c] = c >= a && c < b ? x[c] : 0xff800000u;
@@ -295,21 +317,36 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         }
       }
       const float shift = m == -INFINITY ? 0.0f : m * unit;
-      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
+      const uint64_t unit2 = pair(unit, unit), shift2 = pair(-shift, -shift);
+      uint64_t sum2[2] = {0, 0};
+      // Masked values must become exactly zero, so tiles with a mask keep to the special-function pipe.
+      const auto probabilities = [&](auto poly, int half) {
         uint32_t pk[32];
 #pragma unroll
         for (int c = 0; c < 32; ++c) {
-          const float e0 = exp2_approx(fmaf(__uint_as_float(x[half * 64 + 2 * c]), unit, -shift));
-          const float e1 = exp2_approx(fmaf(__uint_as_float(x[half * 64 + 2 * c + 1]), unit, -shift));
-          sum[(2 * c) & 3] += e0;
-          sum[(2 * c + 1) & 3] += e1;
+          const int e = half * 64 + 2 * c;
+          const uint64_t y = fma2(pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), unit2, shift2);
+          float e0, e1;
+          if (decltype(poly)::value && c % 8 < kPolyOfEight) {
+            exp2_pair_poly(y, &e0, &e1);
+          } else {
+            split(y, &e0, &e1);
+            e0 = exp2_approx(e0);
+            e1 = exp2_approx(e1);
+          }
+          sum2[c & 1] = add2(sum2[c & 1], pair(e0, e1));
           pk[c] = pack_bf16(e0, e1);
         }
         tmem_store32(at + half * 32, pk);
-      }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      };
+      if (whole) probabilities(std::true_type(), 0); else probabilities(std::false_type(), 0);
+      tmem_wait_store();
+      tc_fence_before();
+      mbar_arrive(smem_addr(&ctl.p_half[s]));
+      if (whole) probabilities(std::true_type(), 1); else probabilities(std::false_type(), 1);
+      float s0, s1;
+      split(add2(sum2[0], sum2[1]), &s0, &s1);
+      l += s0 + s1;
       tmem_wait_store();
       tc_fence_before();
       mbar_arrive(smem_addr(&ctl.p_ready[s]));
@@ -510,10 +547,21 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     int lo = 0, hi = 0;
     if (j < p.tokens) p.mask.queries_of(j, &lo, &hi);
     bool ok = true;
-    for (int it = 0; it < steps; ++it) {
-      const int st = it % S, m0 = (q_lo + it % per_head) * kTile + g * 64;
-      const ScoreMod mod(p, hk * p.group + it / per_head);
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.q_full[st]), (it / S) & 1) && wait(smem_addr(&ctl.s_full), it & 1));
+    int h = hk * p.group, tile = 0;
+    ScoreMod mod(p, h);
+    for (int it = 0; it < steps; ++it, ++tile) {
+      if (tile == per_head) {
+        tile = 0;
+        mod = ScoreMod(p, ++h);
+      }
+      const int st = it % S, m0 = (q_lo + tile) * kTile + g * 64;
+      // The queries' statistics come from shared memory, which the tensor cores keep busy: they are
+      // fetched in blocks ahead of the waits (one at a time, each use waited 200 cycles).
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.q_full[st]), (it / S) & 1));
+      if (!ok) break;
+      float y[64];
+      load_floats<64>(y, &ctl.lse[st][g * 64]);
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.s_full), it & 1));
       if (!ok) break;
       tc_fence_after();
       uint32_t x[64];
@@ -524,58 +572,57 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       tmem_landed(x + 32);
       const bool whole = __all_sync(0xffffffffu, j >= p.tokens || (lo <= m0 && hi >= m0 + 64));
       const int a = lo - m0, b = hi - m0;
-      const float4* lse4 = reinterpret_cast<const float4*>(&ctl.lse[st][g * 64]);
-      float pr[64];   // P, and from the second half on P (d score / d product)
+      float pr[64];   // P (d score / d product)
       {
         uint32_t pk[32];
+        const float d0 = (float)(j - m0);
+        const auto probabilities = [&](auto masked) {
 #pragma unroll
-        for (int c4 = 0; c4 < 16; ++c4) {
-          const float4 l4 = lse4[c4];
-          const float l[4] = {l4.x, l4.y, l4.z, l4.w};
-          float e[4], grad[4];
+          for (int c = 0; c < 64; c += 2) {
+            float e[2], grad[2] = {1.0f, 1.0f};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int c = c4 * 4 + k;
-            if constexpr (kMod) e[k] = mod(__uint_as_float(x[c]), (float)(j - m0) - (float)c, &grad[k]) - l[k];
-            else e[k] = fmaf(__uint_as_float(x[c]), p.scale_log2, -l[k]);
-            e[k] = exp2_approx(e[k]);
-            if (!whole) e[k] = c >= a && c < b ? e[k] : 0.0f;
+            for (int k = 0; k < 2; ++k) {
+              if constexpr (kMod) e[k] = mod(__uint_as_float(x[c + k]), d0 - (float)(c + k), &grad[k]) - y[c + k];
+              else e[k] = fmaf(__uint_as_float(x[c + k]), p.scale_log2, -y[c + k]);
+              e[k] = exp2_approx(e[k]);
+              if (decltype(masked)::value) e[k] = c + k >= a && c + k < b ? e[k] : 0.0f;
+              pr[c + k] = kMod ? e[k] * grad[k] : e[k];
+            }
+            pk[c / 2] = pack_bf16(e[0], e[1]);
           }
-          pk[c4 * 2] = pack_bf16(e[0], e[1]);
-          pk[c4 * 2 + 1] = pack_bf16(e[2], e[3]);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) pr[c4 * 4 + k] = kMod ? e[k] * grad[k] : e[k];
-        }
+        };
+        if (whole) probabilities(std::false_type()); else probabilities(std::true_type());
         tmem_store32(at_s + at, pk);
       }
       tmem_wait_store();
       tc_fence_before();
       mbar_arrive(smem_addr(&ctl.p_ready));
 
+      load_floats<64>(y, &ctl.delta[st][g * 64]);
       ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.dp_full), it & 1));
       if (!ok) break;
       tc_fence_after();
-      tmem_load32(at_dp + at, x);
-      tmem_load32(at_dp + at + 32, x + 32);
-      tmem_wait_load();
-      tmem_landed(x);
-      tmem_landed(x + 32);
-      const float4* delta4 = reinterpret_cast<const float4*>(&ctl.delta[st][g * 64]);
       {
         uint32_t pk[32];
 #pragma unroll
-        for (int c4 = 0; c4 < 16; ++c4) {
-          const float4 d4 = delta4[c4];
-          const float d[4] = {d4.x, d4.y, d4.z, d4.w};
-          float e[4];
+        for (int half = 0; half < 2; ++half) {
+          uint32_t d[32];
+          tmem_load32(at_dp + at + half * 32, d);
+          tmem_wait_load();
+          tmem_landed(d);
+          const auto gradients = [&](auto masked) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int c = c4 * 4 + k;
-            e[k] = pr[c] * (__uint_as_float(x[c]) - d[k]);
-            if (!whole) e[k] = c >= a && c < b ? e[k] : 0.0f;   // not zero times what a masked pair holds
-          }
-          pk[c4 * 2] = pack_bf16(e[0], e[1]);
-          pk[c4 * 2 + 1] = pack_bf16(e[2], e[3]);
+            for (int c = 0; c < 32; c += 2) {
+              const int n = half * 32 + c;
+              float e0 = pr[n] * (__uint_as_float(d[c]) - y[n]), e1 = pr[n + 1] * (__uint_as_float(d[c + 1]) - y[n + 1]);
+              if (decltype(masked)::value) {   // not zero times what a masked pair holds
+                e0 = n >= a && n < b ? e0 : 0.0f;
+                e1 = n + 1 >= a && n + 1 < b ? e1 : 0.0f;
+              }
+              pk[n / 2] = pack_bf16(e0, e1);
+            }
+          };
+          if (whole) gradients(std::false_type()); else gradients(std::true_type());
         }
         tmem_store32(at_dp + at, pk);
       }
