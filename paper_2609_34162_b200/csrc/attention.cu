@@ -98,14 +98,6 @@ bool tma_view(const slidedp_heads* v, int64_t tokens, int heads) {
          (heads <= 1 || v->stride_head > 0) && v->stride_token < (1ll << 38) && v->stride_head < (1ll << 38);
 }
 
-// A wait inside an earlier kernel of the context ran out.
-int check_kernel_error(slidedp_ctx* ctx) {
-  volatile int* e = ctx->kernel_error;
-  if (*e == 0) return SLIDEDP_OK;
-  *e = 0;
-  return SLIDEDP_ERR_TIMEOUT;
-}
-
 unsigned general_blocks(int64_t rows) {
   return (unsigned)((rows + kGeneralThreads / kLanes - 1) / (kGeneralThreads / kLanes));
 }

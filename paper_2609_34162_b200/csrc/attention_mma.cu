@@ -26,7 +26,7 @@ __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec
 constexpr int kTmemColumns = 512;
 constexpr uint32_t kKStep = 32 >> 4;       // descriptor step of 16 contracted values along a row
 constexpr uint32_t kRowStep = 16 * 128 >> 4;   // and of 16 contracted rows
-constexpr int kPolyOfEight = 4;           // pairs of eight that take the polynomial exponential
+constexpr int kPolyOfEight = 2;           // pairs of eight that take the polynomial exponential
 constexpr float kRescaleAbove = 8.0f;      // log2: how far a row's maximum may run ahead of its scale
 
 // Waits that outlive the early exit: for copies and products of this thread still in flight.

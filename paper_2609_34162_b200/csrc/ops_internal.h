@@ -25,5 +25,13 @@ inline bool heads_aligned(const slidedp_heads* v, int64_t elem_bytes, int64_t by
 }
 inline bool is_finite(double x) { return x - x == 0.0; }
 
+// A wait inside an earlier kernel of the context ran out.
+inline int check_kernel_error(slidedp_ctx* ctx) {
+  volatile int* e = ctx->kernel_error;
+  if (*e == 0) return SLIDEDP_OK;
+  *e = 0;
+  return SLIDEDP_ERR_TIMEOUT;
+}
+
 }  // namespace host
 }  // namespace slidedp
