@@ -319,16 +319,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       const float shift = m == -INFINITY ? 0.0f : m * unit;
       const uint64_t unit2 = pair(unit, unit), shift2 = pair(-shift, -shift);
       uint64_t sum2[2] = {0, 0};
-      // Masked values must become exactly zero, so tiles with a mask keep to the special-function pipe.
-      const auto probabilities = [&](auto poly, int half) {
+      const auto probabilities = [&](int half) {
         uint32_t pk[32];
 #pragma unroll
         for (int c = 0; c < 32; ++c) {
           const int e = half * 64 + 2 * c;
           const uint64_t y = fma2(pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), unit2, shift2);
           float e0, e1;
-          if (decltype(poly)::value && c % 8 < kPolyOfEight) {
-            exp2_pair_poly(y, &e0, &e1);
+          if (c % 8 < kPolyOfEight) {
+            exp2_pair_poly<4>(y, &e0, &e1);
           } else {
             split(y, &e0, &e1);
             e0 = exp2_approx(e0);
@@ -339,11 +338,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         }
         tmem_store32(at + half * 32, pk);
       };
-      if (whole) probabilities(std::true_type(), 0); else probabilities(std::false_type(), 0);
+      probabilities(0);
       tmem_wait_store();
       tc_fence_before();
       mbar_arrive(smem_addr(&ctl.p_half[s]));
-      if (whole) probabilities(std::true_type(), 1); else probabilities(std::false_type(), 1);
+      probabilities(1);
       float s0, s1;
       split(add2(sum2[0], sum2[1]), &s0, &s1);
       l += s0 + s1;

@@ -18,7 +18,7 @@ constexpr int kDistillThreads = 256;
 constexpr int kDistillWarps = kDistillThreads / 32;
 constexpr int kDistillMaxCluster = 8;
 constexpr int kDistillUnroll = 8;       // 16-byte loads in flight per thread, from global memory
-constexpr int kSmemUnroll = 4;          // and from shared memory
+constexpr int kGradientUnroll = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -103,6 +103,12 @@ struct Row {
   }
 };
 
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
+  float lo, hi;
+  split(x, &lo, &hi);
+  return pair(exp2_approx(lo), exp2_approx(hi));
+}
+
 // Running maximum and sums of exp2(k (z - m)) for one or two factors k.
 struct SoftSum {
   float m, s0, s1;
@@ -113,12 +119,21 @@ __device__ __forceinline__ float shifted(float z, float m, float k) {
 }
 // Where only -inf (or NaN) was seen any finite shift gives the sums, zero (or NaN).
 __device__ __forceinline__ float finite_shift(float m) { return m == -INFINITY ? 0.0f : m; }
-__device__ __forceinline__ SoftSum join(const SoftSum& a, const SoftSum& b, float k0, float k1) {
-  SoftSum r;
-  r.m = fmaxf(a.m, b.m);   // never NaN: a NaN logit shows in the sums
-  r.s0 = a.s0 * exp2_approx(shifted(a.m, r.m, k0)) + b.s0 * exp2_approx(shifted(b.m, r.m, k0));
-  r.s1 = a.s1 * exp2_approx(shifted(a.m, r.m, k1)) + b.s1 * exp2_approx(shifted(b.m, r.m, k1));
-  return r;
+// Joins the sums of the lanes that differ in the bits below LANES; all of them get the result.
+template <int LANES, bool kTwo>
+__device__ __forceinline__ SoftSum join_lanes(SoftSum a, float k0, float k1) {
+  float m = a.m;   // never NaN: a NaN logit shows in the sums
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  a.s0 *= exp2_approx(shifted(a.m, m, k0));
+  if (kTwo) a.s1 *= exp2_approx(shifted(a.m, m, k1));
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) {
+    a.s0 += __shfl_xor_sync(0xffffffffu, a.s0, o);
+    if (kTwo) a.s1 += __shfl_xor_sync(0xffffffffu, a.s1, o);
+  }
+  a.m = m;
+  return a;
 }
 // Adds N chunks to a thread's sums. Differences are taken before they are scaled: the type's lowest value
 // times a factor above one would be -inf.
@@ -140,13 +155,8 @@ __device__ __forceinline__ void accumulate(SoftSum& mine, const uint4* a, float 
 #pragma unroll
     for (int e = 0; e < Logit<T>::kPer / 2; ++e) {
       const uint64_t d = add2(v[e], minus);
-      float x, y;
-      split(mul2(d, f0), &x, &y);
-      s0 = add2(s0, pair(exp2_approx(x), exp2_approx(y)));
-      if (kTwo) {
-        split(mul2(d, f1), &x, &y);
-        s1 = add2(s1, pair(exp2_approx(x), exp2_approx(y)));
-      }
+      s0 = add2(s0, exp2_pair(mul2(d, f0)));
+      if (kTwo) s1 = add2(s1, exp2_pair(mul2(d, f1)));
     }
   }
   float x, y;
@@ -160,10 +170,8 @@ __device__ __forceinline__ void accumulate(SoftSum& mine, const uint4* a, float 
 
 struct DistillShared {
   alignas(16) SoftSum warp[kDistillWarps];
-  SoftSum part[kDistillMaxCluster];   // written by the blocks of the cluster
-  alignas(8) uint64_t loaded;
-  uint32_t dead;
-  int some;                           // the row has a teacher term
+  alignas(16) float4 part[kDistillMaxCluster];   // sums written by the blocks of the cluster
+  uint64_t exchanged;
 };
 
 // The row's entries (and, last, its label) in shared memory: id (-1: absent), teacher probability, the student's
@@ -172,34 +180,38 @@ struct Entries {
   int* id;
   float* q;
   float* z;
-  int count;   // stored entries; the label sits at [count]
-  __device__ Entries(void* smem, int n) : id(static_cast<int*>(smem)), q(reinterpret_cast<float*>(id + n + 1)), z(q + n + 1), count(n) {}
-  static __host__ __device__ size_t bytes(int n) { return (size_t)(n + 1) * 12; }
+  int count;   // stored entries; the label sits at [count], absent ones up to a multiple of four
+  __device__ Entries(void* smem, int n) : id(static_cast<int*>(smem)), q(reinterpret_cast<float*>(id + padded(n))), z(q + padded(n)), count(n) {}
+  static __host__ __device__ int padded(int n) { return (n + 4) & ~3; }
+  static __host__ __device__ size_t bytes(int n) { return (size_t)padded(n) * 12; }
 };
 
 // Fetches the entries with all threads of a block. The logits are read here, before any block writes a
-// gradient, which may go to the same memory.
+// gradient, which may go to the same memory. True when the thread saw an entry with some mass.
 template <typename T>
-__device__ __forceinline__ void fetch_entries(const DistillParams& p, int64_t r, const T* z, const Entries& en) {
-  for (int k = threadIdx.x; k <= en.count; k += kDistillThreads) {
+__device__ __forceinline__ bool fetch_entries(const DistillParams& p, int64_t r, const T* z, const Entries& en) {
+  bool some = false;
+  for (int k = threadIdx.x; k < Entries::padded(en.count); k += kDistillThreads) {
     const bool stored = k < en.count;
-    int id = stored ? p.ids[r * en.count + k] : p.labels ? p.labels[r] : -1;
+    const int id = stored ? p.ids[r * en.count + k] : k == en.count && p.labels ? p.labels[r] : -1;
     const float t = stored ? p.t[r * en.count + k] : 0.0f;
     const bool ok = id >= 0 && id < p.vocab;
     en.id[k] = ok ? id : -1;
     en.z[k] = ok ? Logit<T>::load(z + id) : 0.0f;
     en.q[k] = stored && ok ? t : -INFINITY;
+    some |= stored && ok && t != -INFINITY;
   }
+  return some;
 }
 
-// One warp turns the teacher's logits into probabilities, in place. Returns the lane's share of
+// One warp turns the teacher's logits into probabilities, in place. Adds the lane's share of
 // sum q log q and of sum q; log q = (t - max) / tau - log sum.
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
 }
-__device__ __forceinline__ void teacher_softmax(const DistillParams& p, const Entries& en, float* q_log_q, float* q_sum, int* some) {
+__device__ __forceinline__ void teacher_softmax(const DistillParams& p, const Entries& en, float* q_log_q, float* q_sum) {
   const int lane = threadIdx.x % 32;
   const float k0 = p.inv_tau * kLog2e;
   float top = -INFINITY;
@@ -219,84 +231,87 @@ __device__ __forceinline__ void teacher_softmax(const DistillParams& p, const En
     }
     en.q[k] = q;
   }
-  if (lane == 0) {
-    en.q[en.count] = 0.0f;
-    *some = top > -INFINITY;
-  }
+  if (lane == 0) en.q[en.count] = 0.0f;
 }
-// The same warp, once the row's maximum m and log2 sums are known: log p = c (z - m) - log s, differences
-// from the maximum, so that logits far from zero cost the loss no digits.
-__device__ __forceinline__ void write_loss(const DistillParams& p, int64_t r, const Entries& en, float q_log_q, float q_sum, float m,
-                                           float l0, float l1) {
-  const int lane = threadIdx.x % 32;
-  float cross = 0.0f;
-  for (int k = lane; k < en.count; k += 32)
-    if (en.q[k] != 0.0f) cross += en.q[k] * ((en.z[k] - m) * p.inv_tau);
-  const float total = warp_sum(q_sum), kl = warp_sum(q_log_q) - warp_sum(cross) + total * (l0 * kLn2);
-  if (lane == 0) {
-    float loss = p.w_teacher != 0.0f && (total > 0.0f || total != total) ? p.w_teacher * p.tau * p.tau * kl : 0.0f;
-    if (en.id[en.count] >= 0) loss += p.w_label * (l1 * kLn2 - (en.z[en.count] - m));
-    p.loss[r] = loss;
-    p.lse[r] = m * p.inv_tau + l0 * kLn2;
-    p.lse[p.rows + r] = p.labels ? m + l1 * kLn2 : 0.0f;
-  }
+// The row's loss from sum q (z - m) / tau, the label's z - m, and the row's maximum m and log2 sums: log p =
+// c (z - m) - log s, differences from the maximum, so that logits far from zero cost the loss no digits.
+__device__ __forceinline__ void write_loss(const DistillParams& p, int64_t r, bool hard, float q_log_q, float q_sum, float cross, float label,
+                                           float m, float l0, float l1) {
+  const float kl = q_log_q - cross + q_sum * (l0 * kLn2);
+  float loss = p.w_teacher != 0.0f && (q_sum > 0.0f || q_sum != q_sum) ? p.w_teacher * p.tau * p.tau * kl : 0.0f;
+  if (hard) loss += p.w_label * (l1 * kLn2 - label);
+  p.loss[r] = loss;
+  p.lse[r] = m * p.inv_tau + l0 * kLn2;
+  p.lse[p.rows + r] = p.labels ? m + l1 * kLn2 : 0.0f;
 }
 
-// Joins the block's threads, leaving the result with every thread of warp 0.
-__device__ __forceinline__ SoftSum join_block(SoftSum mine, SoftSum* warps, float k0, float k1) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    SoftSum other;
-    other.m = __shfl_xor_sync(0xffffffffu, mine.m, o);
-    other.s0 = __shfl_xor_sync(0xffffffffu, mine.s0, o);
-    other.s1 = __shfl_xor_sync(0xffffffffu, mine.s1, o);
-    mine = join(mine, other, k0, k1);
-  }
+// All threads of a block; with _or, whether x holds for any of them.
+__device__ __forceinline__ bool row_sync_or(bool x) { return __syncthreads_or(x); }
+__device__ __forceinline__ void row_sync() { __syncthreads(); }
+
+// Joins the block's threads; every thread gets the result, and whether `some` held for any.
+template <bool kTwo>
+__device__ __forceinline__ SoftSum join_block(SoftSum mine, SoftSum* warps, float k0, float k1, bool* some) {
+  static_assert(kDistillMaxCluster == 8, "eight lanes join a cluster");
+  mine = join_lanes<32, kTwo>(mine, k0, k1);
   if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = mine;
-  __syncthreads();
-  if (threadIdx.x < 32) {
-    mine = warps[0];
-#pragma unroll
-    for (int i = 1; i < kDistillWarps; ++i) mine = join(mine, warps[i], k0, k1);
+  *some = row_sync_or(*some);
+  return join_lanes<kDistillWarps, kTwo>(warps[threadIdx.x % kDistillWarps], k0, k1);
+}
+
+// Sums travel between the blocks of a cluster as asynchronous stores into the receiver's `part`, which count
+// towards its barrier: nobody waits for more than the sums.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void send_sums(const SoftSum& v, DistillShared& sh, int rank, int size) {
+  if (threadIdx.x == 0) mbar_expect(smem_addr(&sh.exchanged), size * sizeof(float4));
+  if ((int)threadIdx.x >= size) return;
+  uint32_t to, at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(&sh.part[rank])), "r"(threadIdx.x));
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(&sh.exchanged)), "r"(threadIdx.x));
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to), "f"(v.m),
+               "f"(v.s0), "f"(v.s1), "f"(0.0f), "r"(at)
+               : "memory");
+}
+// The cluster's sums in every thread.
+template <bool kTwo>
+__device__ __forceinline__ bool receive_sums(SoftSum* all, DistillShared& sh, int size, float k0, float k1, const Waiter& wait) {
+  const int i = threadIdx.x % 8;
+  const bool ok = __all_sync(0xffffffffu, wait(smem_addr(&sh.exchanged), 0));
+  SoftSum one = {-INFINITY, 0.0f, 0.0f};
+  if (i < size) {
+    const float4 v = sh.part[i];
+    one = SoftSum{v.x, v.y, v.z};
   }
-  return mine;
+  *all = join_lanes<8, kTwo>(one, k0, k1);
+  return ok;
 }
 
-// The cluster's barrier in two halves, and a block's sums sent to the same place in another block.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ void send(SoftSum* place, const SoftSum& v, int block) {
-  uint32_t to;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(place)), "r"(block));
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v.m) : "memory");
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4), "f"(v.s0) : "memory");
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 8), "f"(v.s1) : "memory");
-}
-// Exchanges the blocks' sums; cluster_arrive has been called once before, at the start of the kernel (a
-// block's shared memory may be written once the block runs).
-__device__ __forceinline__ SoftSum join_cluster(SoftSum mine, DistillShared& sh, int rank, int size, float k0, float k1) {
-  cluster_wait();
-  if ((int)threadIdx.x < size) send(&sh.part[rank], mine, threadIdx.x);   // threads of warp 0 hold the block's sums
-  cluster_arrive();
-  cluster_wait();
-  SoftSum all = sh.part[0];
-  for (int i = 1; i < size; ++i) all = join(all, sh.part[i], k0, k1);
-  return all;
-}
-
-// What a block needs of its place: the cluster's row and the block's 16-byte chunks [lo, hi) of it.
+// What a block needs of its place: the cluster's row and the block's 16-byte chunks [lo, hi) of it, of which
+// [mid_lo, mid_lo + n) are whole; the row's first and last chunk may not be.
 template <typename T>
 struct Slice {
-  int rank, size;
+  int rank, size, n;
   int64_t r;
   Row<T> row;
-  int64_t lo, hi;
-  __device__ Slice(const DistillParams& p, int size_)
-      : rank((int)(blockIdx.x % size_)), size(size_), r(blockIdx.x / size_), row(static_cast<const T*>(p.z) + r * p.z_stride, p.vocab) {
+  int64_t lo, hi, mid_lo;
+  const uint4* mid;
+  __device__ Slice(const DistillParams& p, int size_, int rank_, int64_t r_)
+      : rank(rank_), size(size_), r(r_), row(static_cast<const T*>(p.z) + r * p.z_stride, p.vocab) {
     const int64_t chunks = (p.vocab + row.head + Logit<T>::kPer - 1) / Logit<T>::kPer;
     lo = rank * p.chunks_per_block;
     hi = lo + p.chunks_per_block < chunks ? lo + p.chunks_per_block : chunks;
     if (lo > hi) lo = hi;
+    mid_lo = lo < hi && !row.whole(lo) ? lo + 1 : lo;
+    n = (int)((hi > mid_lo && !row.whole(hi - 1) ? hi - 1 : hi) - mid_lo);
+    mid = reinterpret_cast<const uint4*>(row.z + row.first(mid_lo));
+  }
+  // f(which, chunk) for the partial chunks, each by one thread
+  template <typename F>
+  __device__ void edges(F f) const {
+    if (threadIdx.x == 32 && mid_lo > lo) f(0, lo);
+    if (threadIdx.x == 64 && mid_lo + n < hi) f(1, hi - 1);
   }
 };
 
@@ -305,31 +320,51 @@ struct GradFactors {
   float k0, k1, l0, l1, f0, f1;   // f0 exp2(k0 d - l0) + f1 exp2(k1 d - l1)
 };
 template <typename T, bool kTwo>
-__device__ __forceinline__ void write_chunk(const Row<T>& row, T* dz, bool same_grid, int64_t c, uint4 a, float m, const GradFactors& f) {
+__device__ __forceinline__ void gradients(uint4 a, float m, const GradFactors& f, float* g) {
   constexpr int P = Logit<T>::kPer;
   uint64_t v[P / 2];
-  float g[P];
   Logit<T>::unpack(a, v);
   const uint64_t minus = pair(-m, -m);
 #pragma unroll
   for (int e = 0; e < P / 2; ++e) {
     const uint64_t d = add2(v[e], minus);
-    float x, y;
-    split(fma2(d, pair(f.k0, f.k0), pair(-f.l0, -f.l0)), &x, &y);
-    uint64_t out = mul2(pair(exp2_approx(x), exp2_approx(y)), pair(f.f0, f.f0));
-    if (kTwo) {
-      split(fma2(d, pair(f.k1, f.k1), pair(-f.l1, -f.l1)), &x, &y);
-      out = fma2(pair(exp2_approx(x), exp2_approx(y)), pair(f.f1, f.f1), out);
-    }
+    uint64_t out = mul2(exp2_pair(fma2(d, pair(f.k0, f.k0), pair(-f.l0, -f.l0))), pair(f.f0, f.f0));
+    if (kTwo) out = fma2(exp2_pair(fma2(d, pair(f.k1, f.k1), pair(-f.l1, -f.l1))), pair(f.f1, f.f1), out);
     split(out, &g[2 * e], &g[2 * e + 1]);
   }
+}
+// A chunk's gradient value by value: partial chunks, and rows whose gradient lies on another address grid.
+template <typename T, bool kTwo>
+__device__ __forceinline__ void write_values(const Row<T>& row, T* dz, int64_t c, uint4 a, float m, const GradFactors& f) {
+  float g[Logit<T>::kPer];
+  gradients<T, kTwo>(a, m, f, g);
   const int64_t first = row.first(c);
-  if (same_grid && first >= 0 && first + P <= row.vocab) {
-    st_stream(dz + first, Logit<T>::pack(g));
-  } else {
 #pragma unroll
-    for (int e = 0; e < P; ++e)
-      if (first + e >= 0 && first + e < row.vocab) Logit<T>::store(dz + first + e, g[e]);
+  for (int e = 0; e < Logit<T>::kPer; ++e)
+    if (first + e >= 0 && first + e < row.vocab) Logit<T>::store(dz + first + e, g[e]);
+}
+// The gradient of a slice whose whole chunks come from `chunk(i)`, U of them at a time.
+template <typename T, bool kTwo, int U, typename F>
+__device__ __forceinline__ void write_slice(const Slice<T>& s, T* dz, float m, const GradFactors& f, F chunk) {
+  const bool same_grid = (reinterpret_cast<uintptr_t>(dz) & 15u) == (reinterpret_cast<uintptr_t>(s.row.z) & 15u);
+  uint4* out = reinterpret_cast<uint4*>(dz + s.row.first(s.mid_lo));
+  for (int i0 = threadIdx.x; i0 < s.n; i0 += kDistillThreads * U) {
+    uint4 a[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * kDistillThreads < s.n) a[u] = chunk(i0 + u * kDistillThreads);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kDistillThreads;
+      if (i >= s.n) continue;
+      if (same_grid) {
+        float g[Logit<T>::kPer];
+        gradients<T, kTwo>(a[u], m, f, g);
+        st_stream(out + i, Logit<T>::pack(g));
+      } else {
+        write_values<T, kTwo>(s.row, dz, s.mid_lo + i, a[u], m, f);
+      }
+    }
   }
 }
 // The values of the slice with a teacher entry or the label, after the block's other stores: the first
@@ -343,10 +378,14 @@ __device__ __forceinline__ void write_entries(const Slice<T>& s, T* dz, const En
     if (id < 0 || id < own_lo || id >= own_hi) continue;
     float q = 0.0f;
     bool leader = true;
-    for (int j = 0; j <= en.count; ++j) {
-      const bool same = en.id[j] == id;
-      if (same && j < k) leader = false;
-      if (same) q += en.q[j];
+    for (int j4 = 0; j4 <= en.count; j4 += 4) {   // the list is padded with absent entries
+      const int4 four = *reinterpret_cast<const int4*>(en.id + j4);
+      if (four.x != id && four.y != id && four.z != id && four.w != id) continue;
+      for (int j = j4; j < j4 + 4; ++j)
+        if (en.id[j] == id) {
+          leader &= j >= k;
+          q += en.q[j];
+        }
     }
     if (!leader) continue;
     const float d = en.z[k] - m;
@@ -359,145 +398,95 @@ __device__ __forceinline__ void write_entries(const Slice<T>& s, T* dz, const En
 // a0 and a1: the weights of the teacher's and the label's terms in this row's gradient. Without a second softmax
 // the terms share p.
 template <bool kTwo>
-__device__ __forceinline__ GradFactors factors(const DistillParams& p, int64_t r, bool some, bool hard, float l0, float l1, float* a0, float* a1) {
-  const float g = p.row_grad ? p.row_grad[r] : 1.0f;
+__device__ __forceinline__ GradFactors factors(const DistillParams& p, float g, bool some, bool hard, float l0, float l1, float* a0, float* a1) {
   *a0 = some ? g * p.w_teacher * p.tau : 0.0f;
   *a1 = hard ? g * p.w_label : 0.0f;
   return GradFactors{p.inv_tau * kLog2e, kLog2e, l0, l1, kTwo ? *a0 : *a0 + *a1, kTwo ? *a1 : 0.0f};
 }
 
-// Loss: a row per block, or per cluster of blocks when there are few rows. kTwo: the softmax at temperature 1
-// is needed beside the one at tau (label term, tau != 1).
-template <typename T, bool kTwo>
-__global__ void __launch_bounds__(kDistillThreads) distill_loss_kernel(const __grid_constant__ DistillParams p, int cluster) {
+// Loss, and for a step the gradient in the same kernel: a row per block, or per cluster of blocks. kTwo: the softmax at
+// temperature 1 is needed beside the one at tau (label term, tau != 1).
+template <typename T, bool kTwo, bool kGradient>
+__global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(const __grid_constant__ DistillParams p, int cluster) {
   extern __shared__ uint4 dynamic[];
   __shared__ DistillShared sh;
-  if (cluster > 1) cluster_arrive();
-  const Slice<T> s(p, cluster);
+  __shared__ uint32_t dead;
+  if (cluster > 1) {
+    if (threadIdx.x == 0) {
+      mbar_init(smem_addr(&sh.exchanged), 1);
+      dead = 0;
+      mbar_init_fence();
+    }
+    cluster_sync();
+  }
+  const Slice<T> s(p, cluster, blockIdx.x % cluster, blockIdx.x / cluster);
   const Entries en(dynamic, p.entries);
   const float k0 = p.inv_tau * kLog2e, k1 = kLog2e;
+  bool some = false;
+  if (kGradient || s.rank == 0) some = fetch_entries<T>(p, s.r, s.row.z, en);
   SoftSum mine = {-INFINITY, 0.0f, 0.0f};
-  bool fetched = false;
-  for (int64_t c0 = s.lo + threadIdx.x; c0 < s.hi; c0 += (int64_t)kDistillThreads * kDistillUnroll) {
+  for (int i0 = threadIdx.x; i0 < s.n; i0 += kDistillThreads * kDistillUnroll) {
     uint4 a[kDistillUnroll];
 #pragma unroll
-    for (int i = 0; i < kDistillUnroll; ++i) {
-      const int64_t c = c0 + (int64_t)i * kDistillThreads;
-      a[i] = c < s.hi ? s.row.load(c) : Logit<T>::lowest();
+    for (int u = 0; u < kDistillUnroll; ++u) {
+      const int i = i0 + u * kDistillThreads;
+      a[u] = i < s.n ? (kGradient ? s.mid[i] : ld_stream(s.mid + i)) : Logit<T>::lowest();
     }
-    if (!fetched && s.rank == 0) fetch_entries<T>(p, s.r, s.row.z, en);   // behind the first loads of the row
-    fetched = true;
     accumulate<T, kTwo, kDistillUnroll>(mine, a, k0, k1);
   }
-  if (!fetched && s.rank == 0) fetch_entries<T>(p, s.r, s.row.z, en);
-  SoftSum all = join_block(mine, sh.warp, k0, k1);
-  if (cluster > 1) all = join_cluster(all, sh, s.rank, s.size, k0, k1);
+  s.edges([&](int, int64_t c) {
+    const uint4 a = s.row.load(c);
+    accumulate<T, kTwo, 1>(mine, &a, k0, k1);
+  });
+  __syncwarp();
+  mine = join_block<kTwo>(mine, sh.warp, k0, k1, &some);
+  if (cluster > 1) send_sums(mine, sh, s.rank, s.size);
+  float q_log_q = 0.0f, q_sum = 0.0f;
+  if ((kGradient || s.rank == 0) && threadIdx.x < 32) teacher_softmax(p, en, &q_log_q, &q_sum);
+  bool ok = true;
+  if (cluster > 1) ok = receive_sums<kTwo>(&mine, sh, s.size, k0, k1, Waiter{&dead, p.error});
+  __syncwarp();
+  const float m = finite_shift(mine.m), l0 = log2f(mine.s0), l1 = kTwo ? log2f(mine.s1) : l0;
   if (s.rank == 0 && threadIdx.x < 32) {
-    float q_log_q = 0.0f, q_sum = 0.0f;
-    teacher_softmax(p, en, &q_log_q, &q_sum, &sh.some);
-    __syncwarp();
-    const float l0 = log2f(all.s0);
-    write_loss(p, s.r, en, q_log_q, q_sum, finite_shift(all.m), l0, kTwo ? log2f(all.s1) : l0);
+    float cross = 0.0f;
+    for (int k = threadIdx.x; k < en.count; k += 32)
+      if (en.q[k] != 0.0f) cross += en.q[k] * ((en.z[k] - m) * p.inv_tau);
+    q_log_q = warp_sum(q_log_q);
+    q_sum = warp_sum(q_sum);
+    cross = warp_sum(cross);
+    if (threadIdx.x == 0) write_loss(p, s.r, en.id[en.count] >= 0, q_log_q, q_sum, cross, en.z[en.count] - m, m, l0, l1);
   }
+  if (kGradient && ok) {
+    float a0, a1;
+    const GradFactors f = factors<kTwo>(p, p.row_grad ? p.row_grad[s.r] : 1.0f, some, en.id[en.count] >= 0, l0, l1, &a0, &a1);
+    T* dz = static_cast<T*>(p.dz) + s.r * p.dz_stride;
+    write_slice<T, kTwo, kGradientUnroll>(s, dz, m, f, [&](int i) { return ld_stream(s.mid + i); });
+    s.edges([&](int, int64_t c) { write_values<T, kTwo>(s.row, dz, c, s.row.load(c), m, f); });
+    __syncthreads();   // the stores above come before those at the entries
+    write_entries<T, kTwo>(s, dz, en, m, f, a0, a1);
+  }
+  if (cluster > 1) cluster_sync();   // nobody leaves while sums may still be sent to it
 }
 
 // Gradient from the saved lse: blocks of a row share nothing.
 template <typename T, bool kTwo>
 __global__ void __launch_bounds__(kDistillThreads) distill_gradient_kernel(const __grid_constant__ DistillParams p, int parts) {
   extern __shared__ uint4 dynamic[];
-  __shared__ DistillShared sh;
-  const Slice<T> s(p, parts);
+  const Slice<T> s(p, parts, blockIdx.x % parts, blockIdx.x / parts);
   const Entries en(dynamic, p.entries);
-  fetch_entries<T>(p, s.r, s.row.z, en);
   const float l0 = p.lse[s.r] * kLog2e, l1 = p.labels ? p.lse[p.rows + s.r] * kLog2e : l0;
-  __syncthreads();
+  const bool some = __syncthreads_or(fetch_entries<T>(p, s.r, s.row.z, en));
+  float a0, a1;
+  const GradFactors f = factors<kTwo>(p, p.row_grad ? p.row_grad[s.r] : 1.0f, some, en.id[en.count] >= 0, l0, l1, &a0, &a1);
+  T* dz = static_cast<T*>(p.dz) + s.r * p.dz_stride;
+  write_slice<T, kTwo, kGradientUnroll>(s, dz, 0.0f, f, [&](int i) { return ld_stream(s.mid + i); });
+  s.edges([&](int, int64_t c) { write_values<T, kTwo>(s.row, dz, c, s.row.load(c), 0.0f, f); });
   if (threadIdx.x < 32) {
     float unused = 0.0f;
-    teacher_softmax(p, en, &unused, &unused, &sh.some);
-  }
-  __syncthreads();
-  float a0, a1;
-  const GradFactors f = factors<kTwo>(p, s.r, sh.some, en.id[en.count] >= 0, l0, l1, &a0, &a1);
-  T* dz = static_cast<T*>(p.dz) + s.r * p.dz_stride;
-  const bool same_grid = (reinterpret_cast<uintptr_t>(dz) & 15u) == (reinterpret_cast<uintptr_t>(s.row.z) & 15u);
-  for (int64_t c0 = s.lo + threadIdx.x; c0 < s.hi; c0 += (int64_t)kDistillThreads * kSmemUnroll) {
-    uint4 a[kSmemUnroll];
-#pragma unroll
-    for (int i = 0; i < kSmemUnroll; ++i) {
-      const int64_t c = c0 + (int64_t)i * kDistillThreads;
-      if (c < s.hi) a[i] = s.row.load(c);
-    }
-#pragma unroll
-    for (int i = 0; i < kSmemUnroll; ++i) {
-      const int64_t c = c0 + (int64_t)i * kDistillThreads;
-      if (c < s.hi) write_chunk<T, kTwo>(s.row, dz, same_grid, c, a[i], 0.0f, f);
-    }
+    teacher_softmax(p, en, &unused, &unused);
   }
   __syncthreads();
   write_entries<T, kTwo>(s, dz, en, 0.0f, f, a0, a1);
-}
-
-// Loss and gradient in one pass: the block's slice is copied to shared memory by one bulk copy while the
-// teacher's entries are worked on, summed from there, and used a second time for the gradient.
-template <typename T, bool kTwo>
-__global__ void __launch_bounds__(kDistillThreads, 5) distill_step_kernel(const __grid_constant__ DistillParams p, int cluster) {
-  extern __shared__ uint4 dynamic[];
-  __shared__ DistillShared sh;
-  if (cluster > 1) cluster_arrive();
-  const Slice<T> s(p, cluster);
-  uint4* keep = dynamic;
-  const Entries en(dynamic + p.chunks_per_block, p.entries);
-  const float k0 = p.inv_tau * kLog2e, k1 = kLog2e;
-
-  // the row's first and last chunk may be partial: those come by element
-  const int64_t w_lo = s.lo < s.hi && !s.row.whole(s.lo) ? s.lo + 1 : s.lo;
-  const int64_t w_hi = s.hi > w_lo && !s.row.whole(s.hi - 1) ? s.hi - 1 : s.hi;
-  if (threadIdx.x == 0) {
-    mbar_init(smem_addr(&sh.loaded), 1);
-    sh.dead = 0;
-    mbar_init_fence();
-    if (w_lo < w_hi) {
-      mbar_expect(smem_addr(&sh.loaded), (uint32_t)(w_hi - w_lo) * 16);
-      bulk_load(smem_addr(keep + (w_lo - s.lo)), s.row.z + s.row.first(w_lo), (uint32_t)(w_hi - w_lo) * 16, smem_addr(&sh.loaded));
-    }
-  }
-  if (threadIdx.x == 32 && w_lo > s.lo) keep[0] = s.row.load(s.lo);
-  if (threadIdx.x == 64 && w_hi < s.hi) keep[w_hi - s.lo] = s.row.load(w_hi);
-  fetch_entries<T>(p, s.r, s.row.z, en);
-  __syncthreads();
-  float q_log_q = 0.0f, q_sum = 0.0f;
-  if (threadIdx.x < 32) teacher_softmax(p, en, &q_log_q, &q_sum, &sh.some);
-  if (w_lo < w_hi) (void)Waiter{&sh.dead, p.error}(smem_addr(&sh.loaded), 0);
-
-  SoftSum mine = {-INFINITY, 0.0f, 0.0f};
-  for (int64_t c0 = s.lo + threadIdx.x; c0 < s.hi; c0 += kDistillThreads * kSmemUnroll) {
-    uint4 a[kSmemUnroll];
-#pragma unroll
-    for (int i = 0; i < kSmemUnroll; ++i) {
-      const int64_t c = c0 + i * kDistillThreads;
-      a[i] = c < s.hi ? keep[c - s.lo] : Logit<T>::lowest();
-    }
-    accumulate<T, kTwo, kSmemUnroll>(mine, a, k0, k1);
-  }
-  SoftSum all = join_block(mine, sh.warp, k0, k1);
-  if (cluster == 1) {
-    if (threadIdx.x == 0) sh.part[0] = all;
-    __syncthreads();
-    all = sh.part[0];
-  } else {
-    all = join_cluster(all, sh, s.rank, s.size, k0, k1);
-  }
-  const float m = finite_shift(all.m), l0 = log2f(all.s0), l1 = kTwo ? log2f(all.s1) : l0;
-  if (s.rank == 0 && threadIdx.x < 32) write_loss(p, s.r, en, q_log_q, q_sum, m, l0, l1);
-
-  float a0, a1;
-  const GradFactors f = factors<kTwo>(p, s.r, sh.some, en.id[en.count] >= 0, l0, l1, &a0, &a1);
-  T* dz = static_cast<T*>(p.dz) + s.r * p.dz_stride;
-  const bool same_grid = (reinterpret_cast<uintptr_t>(dz) & 15u) == (reinterpret_cast<uintptr_t>(s.row.z) & 15u);
-  for (int64_t c = s.lo + threadIdx.x; c < s.hi; c += kDistillThreads)
-    write_chunk<T, kTwo>(s.row, dz, same_grid, c, keep[c - s.lo], m, f);
-  __syncthreads();
-  write_entries<T, kTwo>(s, dz, en, m, f, a0, a1);
 }
 
 }  // namespace slidedp
@@ -518,39 +507,31 @@ int check_distill(const slidedp_distill_args* a) {
 }
 
 template <typename K>
-cudaError_t launch_distill(K kernel, const DistillParams& p, unsigned blocks_per_row, bool clustered, size_t smem, cudaStream_t st) {
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-  }
+cudaError_t launch_distill(K kernel, const DistillParams& p, unsigned parts, bool clustered, size_t smem, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)p.rows * blocks_per_row);
+  cfg.gridDim = dim3((unsigned)p.rows * parts);
   cfg.blockDim = dim3(kDistillThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = blocks_per_row;
+  attr[0].val.clusterDim.x = parts;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = clustered && blocks_per_row > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, p, (int)blocks_per_row);
+  cfg.numAttrs = clustered && parts > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, p, (int)parts);
 }
 
-// Blocks per row. A step holds its row in shared memory: as many blocks as leave each about 32 KB (five
-// blocks per SM, so that one's loads run beside another's arithmetic and stores). Loss and gradient alone
-// stream a row through one block when the rows fill the device, and cut it, down to 8 KB, when they do
-// not.
-constexpr int64_t kSliceBytes = 32 * 1024;
-constexpr int64_t kMaxSliceBytes = 200 * 1024;
+// Blocks per row: one when the rows fill the device; when they do not, a row is cut, down to 8 KB. A step also
+// cuts rows so that those being worked on (four blocks per SM) stay in L2 for their second reading.
 constexpr int64_t kMinSliceBytes = 8 * 1024;
 constexpr int64_t kEnoughBlocks = 148 * 4;
+constexpr int64_t kResidentBytes = 64ll << 20;
 
 unsigned blocks_per_row(int mode, int64_t rows, int64_t row_bytes) {
   unsigned n = 1;
-  if (mode == kStep) {
-    while (n < (unsigned)kDistillMaxCluster && row_bytes > kSliceBytes * n) n *= 2;
-  }
+  if (mode == kStep)
+    while (n < (unsigned)kDistillMaxCluster && kEnoughBlocks * row_bytes > kResidentBytes * n) n *= 2;
   while (n < (unsigned)kDistillMaxCluster && rows * n < kEnoughBlocks && row_bytes >= 2 * kMinSliceBytes * n) n *= 2;
   return n;
 }
@@ -598,25 +579,18 @@ int run_distill(slidedp_ctx* ctx, const slidedp_distill_args* a, int mode, const
   if (rc != SLIDEDP_OK) return rc;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());
-  // A row too long for a cluster's shared memory is read twice: forward, then backward.
-  if (mode == kStep && p.chunks_per_block * 16 > kMaxSliceBytes) {
-    const int first = run_distill(ctx, a, kForward, logits, ids, t, labels, nullptr, loss, lse, nullptr, st);
-    return first != SLIDEDP_OK ? first : run_distill(ctx, a, kBackward, logits, ids, t, labels, row_grad, nullptr, lse, dz, st);
-  }
-  const size_t smem = (mode == kStep ? (size_t)p.chunks_per_block * 16 : 0) + Entries::bytes(a->entries);
+  const size_t smem = Entries::bytes(a->entries);
   FAULT_POINT();
-  cudaError_t e;
-#define SLIDEDP_LAUNCH(KERNEL)                                                                           \
-  e = f32 ? (two ? launch_distill(KERNEL<float, true>, p, cluster, mode != kBackward, smem, st)          \
-                 : launch_distill(KERNEL<float, false>, p, cluster, mode != kBackward, smem, st))        \
-          : (two ? launch_distill(KERNEL<uint16_t, true>, p, cluster, mode != kBackward, smem, st)       \
-                 : launch_distill(KERNEL<uint16_t, false>, p, cluster, mode != kBackward, smem, st))
-  switch (mode) {
-    case kForward: SLIDEDP_LAUNCH(distill_loss_kernel); break;
-    case kBackward: SLIDEDP_LAUNCH(distill_gradient_kernel); break;
-    default: SLIDEDP_LAUNCH(distill_step_kernel); break;
-  }
-#undef SLIDEDP_LAUNCH
+  const auto run = [&](auto kernel) { return launch_distill(kernel, p, cluster, mode != kBackward, smem, st); };
+#define SLIDEDP_KERNEL(KERNEL, ...) \
+  (f32 ? (two ? run(KERNEL<float, true __VA_ARGS__>) : run(KERNEL<float, false __VA_ARGS__>)) \
+       : (two ? run(KERNEL<uint16_t, true __VA_ARGS__>) : run(KERNEL<uint16_t, false __VA_ARGS__>)))
+#define SLIDEDP_ALSO(x) , x
+  const cudaError_t e = mode == kForward    ? SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(false))
+                        : mode == kBackward ? SLIDEDP_KERNEL(distill_gradient_kernel)
+                                            : SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(true));
+#undef SLIDEDP_ALSO
+#undef SLIDEDP_KERNEL
   if (e != cudaSuccess) return cuda_fail(ctx, e);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();

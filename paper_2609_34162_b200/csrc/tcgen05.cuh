@@ -191,23 +191,35 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-// 2^x on the multiply-add pipe, for a share of the exponentials where the special-function pipe is the
-// bound: x = n + f with n the nearest integer (adding 1.5 * 2^23 leaves n in the low bits), 2^f on
-// [-1/2, 1/2] by the polynomial of degree 4 with the least relative error (2.6e-6, found by Remez
-// exchange; the result is rounded to BF16, 2e-3), n added to the exponent. Below -125 it stays
-// at 2^-125 instead of falling to zero; NaN stays NaN.
+// 2^x on the multiply-add pipe, for a share of the exponentials where the special-function pipe would be the
+// bound: x = n + f with n = floor x (adding 1.5 * 2^23, rounded down, leaves n in the low bits), 2^f on [0, 1)
+// by the polynomial with p(0) = 1 and the least greatest relative error (from a linear program: 2.9e-6 at
+// degree 4, 9.2e-8 at degree 5), n added to the exponent. Below -127 the result is exactly zero; NaN stays
+// NaN; x is at most a few units above zero.
+template <int DEGREE>
 __device__ __forceinline__ void exp2_pair_poly(uint64_t x, float* lo, float* hi) {
+  static_assert(DEGREE == 4 || DEGREE == 5, "");
   float a, b, ta, tb, pa, pb;
   split(x, &a, &b);
-  asm("max.NaN.f32 %0, %0, 0fC2FA0000;" : "+f"(a));   // -125
-  asm("max.NaN.f32 %0, %0, 0fC2FA0000;" : "+f"(b));
+  asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(a));   // -127
+  asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(b));
   x = pair(a, b);
-  const uint64_t t = add2(x, pair(12582912.0f, 12582912.0f));
+  uint64_t t;
+  asm("add.rm.f32x2 %0, %1, %2;" : "=l"(t) : "l"(x), "l"(pair(12582912.0f, 12582912.0f)));
   const uint64_t f = fma2(add2(t, pair(-12582912.0f, -12582912.0f)), pair(-1.0f, -1.0f), x);
-  uint64_t p = fma2(f, pair(0.009570102207362652f, 0.009570102207362652f), pair(0.05591785907745361f, 0.05591785907745361f));
-  p = fma2(p, f, pair(0.240247443318367f, 0.240247443318367f));
-  p = fma2(p, f, pair(0.6931217908859253f, 0.6931217908859253f));
-  p = fma2(p, f, pair(0.9999992847442627f, 0.9999992847442627f));
+  const auto step = [&](uint64_t p, float c) { return fma2(p, f, pair(c, c)); };
+  uint64_t p;
+  if constexpr (DEGREE == 4) {
+    p = step(pair(0.013426683843135834f, 0.013426683843135834f), 0.052242472767829895f);
+    p = step(p, 0.241280198097229f);
+    p = step(p, 0.6930448412895203f);
+  } else {
+    p = step(pair(0.0018671337747946382f, 0.0018671337747946382f), 0.00901702232658863f);
+    p = step(p, 0.05579992011189461f);
+    p = step(p, 0.24016444385051727f);
+    p = step(p, 0.6931512951850891f);
+  }
+  p = step(p, 1.0f);
   split(t, &ta, &tb);
   split(p, &pa, &pb);
   *lo = __int_as_float(__float_as_int(pa) + (__float_as_int(ta) << 23));
