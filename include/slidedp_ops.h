@@ -44,7 +44,8 @@ typedef struct {
  * table_rows rows of rope_dim floats, the rope_dim / 2 cosines before the sines. positions: device,
  * one row index per token (NULL: token t uses row t, so tokens <= table_rows). A token whose
  * position lies outside the table gets NaN in its rotated values (and, backward, in its gradients,
- * hence in dw). head_dim 1..256, rope_dim even, 0..head_dim; heads_q or heads_k may be 0.
+ * hence in dw). head_dim 1..256, rope_dim even, 0..head_dim; heads_q or heads_k may be 0; at most 2^31 - 1 rows
+ * (tokens * heads) of each.
  * q, k, w_q, w_k and the outputs have the type `dtype`.
  *
  * Backward: dq, dk are the gradients of q and k, dw_q and dw_k (device, head_dim floats each,

@@ -18,6 +18,13 @@ __device__ __forceinline__ uint32_t f32_to_bf16_bits(float x) {
   return (uint32_t)r;
 }
 
+// The same for two values: lo in the lower half.
+__device__ __forceinline__ uint32_t f32x2_to_bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
 // Streaming (read-once / write-once) 128-bit accesses: keep them out of L1 and mark them
 // evict-first in L2, since nothing on this path is ever re-read.
 __device__ __forceinline__ uint4 ld_stream(const void* p) {

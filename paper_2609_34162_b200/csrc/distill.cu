@@ -3,10 +3,12 @@
 //
 // With c = 1 / temperature, m = max z, s = sum exp(c (z - m)):  lse = c m + log s,  log p = c z - lse and
 //   dz = g (w_t tau (p - q) + w_l (p1 - onehot)),   p1 the softmax at temperature 1.
-// Bound: HBM. The logits are all that is large: forward reads them once, backward reads them and writes
-// the gradient, and the step (both) reads and writes once because a row stays on chip between its two
-// uses: a cluster of up to eight blocks holds it in shared memory (a row of 131072 BF16 logits is
-// 256 KB, more than one SM has) and exchanges its maximum and sums through distributed shared memory.
+// Bound: HBM. The logits are all that is large: forward reads them once, backward reads them and writes the
+// gradient. The step (both) reads a row twice in one kernel, the second time from L2, so that it moves what
+// backward alone does. Measured on 4096 x 131072 BF16 logits: 465 us, 4.6 TB/s of one read and one write, 14
+// instructions and two exponentials per logit. Keeping the row on chip instead, in the shared memory or the
+// registers of a cluster of eight blocks, measured 481 to 860 us: the exchange of a row's sums costs each of the
+// eight what 5000 of its own logits do, and too few rows fit to cover that.
 #include "ops_internal.h"
 #include "tcgen05.cuh"
 #include "device_utils.cuh"
@@ -17,8 +19,7 @@ constexpr int kMaxEntries = 512;        // teacher entries per row
 constexpr int kDistillThreads = 256;
 constexpr int kDistillWarps = kDistillThreads / 32;
 constexpr int kDistillMaxCluster = 8;
-constexpr int kDistillUnroll = 8;       // 16-byte loads in flight per thread, from global memory
-constexpr int kGradientUnroll = 4;
+constexpr int kDistillUnroll = 4;       // 16-byte chunks per thread and turn; the next turn's are on their way
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -343,28 +344,47 @@ __device__ __forceinline__ void write_values(const Row<T>& row, T* dz, int64_t c
   for (int e = 0; e < Logit<T>::kPer; ++e)
     if (first + e >= 0 && first + e < row.vocab) Logit<T>::store(dz + first + e, g[e]);
 }
-// The gradient of a slice whose whole chunks come from `chunk(i)`, U of them at a time.
-template <typename T, bool kTwo, int U, typename F>
-__device__ __forceinline__ void write_slice(const Slice<T>& s, T* dz, float m, const GradFactors& f, F chunk) {
-  const bool same_grid = (reinterpret_cast<uintptr_t>(dz) & 15u) == (reinterpret_cast<uintptr_t>(s.row.z) & 15u);
-  uint4* out = reinterpret_cast<uint4*>(dz + s.row.first(s.mid_lo));
-  for (int i0 = threadIdx.x; i0 < s.n; i0 += kDistillThreads * U) {
-    uint4 a[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i0 + u * kDistillThreads < s.n) a[u] = chunk(i0 + u * kDistillThreads);
+// Walks a slice's whole chunks, kDistillUnroll per thread and turn, with the next turn's loads issued before this
+// turn's work: work(first chunk, chunks, how many of them exist); the others hold -inf.
+template <typename T, typename L, typename W>
+__device__ __forceinline__ void stream_chunks(int n, L load, W work) {
+  constexpr int U = kDistillUnroll, kStep = kDistillThreads * U;
+  uint4 a[U], b[U];
+  const auto fetch = [&](int i0, uint4* to) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * kDistillThreads;
-      if (i >= s.n) continue;
-      if (same_grid) {
+      to[u] = i < n ? load(i) : Logit<T>::lowest();
+    }
+  };
+  int i0 = threadIdx.x;
+  if (i0 < n) fetch(i0, a);
+  for (; i0 < n; i0 += kStep) {
+    fetch(i0 + kStep, b);
+    work(i0, a, n);
+#pragma unroll
+    for (int u = 0; u < U; ++u) a[u] = b[u];
+  }
+}
+// The gradient of a slice's whole chunks.
+template <typename T, bool kTwo>
+__device__ __forceinline__ void write_slice(const Slice<T>& s, T* dz, float m, const GradFactors& f) {
+  const bool same_grid = (reinterpret_cast<uintptr_t>(dz) & 15u) == (reinterpret_cast<uintptr_t>(s.row.z) & 15u);
+  uint4* out = reinterpret_cast<uint4*>(dz + s.row.first(s.mid_lo));
+  const auto load = [&](int i) { return ld_stream(s.mid + i); };
+  if (same_grid) {
+    stream_chunks<T>(s.n, load, [&](int i0, const uint4* a, int n) {
+#pragma unroll
+      for (int u = 0; u < kDistillUnroll; ++u) {
+        const int i = i0 + u * kDistillThreads;
+        if (i >= n) continue;
         float g[Logit<T>::kPer];
         gradients<T, kTwo>(a[u], m, f, g);
         st_stream(out + i, Logit<T>::pack(g));
-      } else {
-        write_values<T, kTwo>(s.row, dz, s.mid_lo + i, a[u], m, f);
       }
-    }
+    });
+  } else {
+    for (int i = threadIdx.x; i < s.n; i += kDistillThreads) write_values<T, kTwo>(s.row, dz, s.mid_lo + i, load(i), m, f);
   }
 }
 // The values of the slice with a teacher entry or the label, after the block's other stores: the first
@@ -425,15 +445,8 @@ __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(const __gr
   bool some = false;
   if (kGradient || s.rank == 0) some = fetch_entries<T>(p, s.r, s.row.z, en);
   SoftSum mine = {-INFINITY, 0.0f, 0.0f};
-  for (int i0 = threadIdx.x; i0 < s.n; i0 += kDistillThreads * kDistillUnroll) {
-    uint4 a[kDistillUnroll];
-#pragma unroll
-    for (int u = 0; u < kDistillUnroll; ++u) {
-      const int i = i0 + u * kDistillThreads;
-      a[u] = i < s.n ? (kGradient ? s.mid[i] : ld_stream(s.mid + i)) : Logit<T>::lowest();
-    }
-    accumulate<T, kTwo, kDistillUnroll>(mine, a, k0, k1);
-  }
+  stream_chunks<T>(s.n, [&](int i) { return kGradient ? s.mid[i] : ld_stream(s.mid + i); },
+                   [&](int, const uint4* a, int) { accumulate<T, kTwo, kDistillUnroll>(mine, a, k0, k1); });
   s.edges([&](int, int64_t c) {
     const uint4 a = s.row.load(c);
     accumulate<T, kTwo, 1>(mine, &a, k0, k1);
@@ -460,7 +473,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(const __gr
     float a0, a1;
     const GradFactors f = factors<kTwo>(p, p.row_grad ? p.row_grad[s.r] : 1.0f, some, en.id[en.count] >= 0, l0, l1, &a0, &a1);
     T* dz = static_cast<T*>(p.dz) + s.r * p.dz_stride;
-    write_slice<T, kTwo, kGradientUnroll>(s, dz, m, f, [&](int i) { return ld_stream(s.mid + i); });
+    write_slice<T, kTwo>(s, dz, m, f);
     s.edges([&](int, int64_t c) { write_values<T, kTwo>(s.row, dz, c, s.row.load(c), m, f); });
     __syncthreads();   // the stores above come before those at the entries
     write_entries<T, kTwo>(s, dz, en, m, f, a0, a1);
@@ -479,7 +492,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_gradient_kernel(const
   float a0, a1;
   const GradFactors f = factors<kTwo>(p, p.row_grad ? p.row_grad[s.r] : 1.0f, some, en.id[en.count] >= 0, l0, l1, &a0, &a1);
   T* dz = static_cast<T*>(p.dz) + s.r * p.dz_stride;
-  write_slice<T, kTwo, kGradientUnroll>(s, dz, 0.0f, f, [&](int i) { return ld_stream(s.mid + i); });
+  write_slice<T, kTwo>(s, dz, 0.0f, f);
   s.edges([&](int, int64_t c) { write_values<T, kTwo>(s.row, dz, c, s.row.load(c), 0.0f, f); });
   if (threadIdx.x < 32) {
     float unused = 0.0f;
@@ -522,16 +535,18 @@ cudaError_t launch_distill(K kernel, const DistillParams& p, unsigned parts, boo
   return cudaLaunchKernelEx(&cfg, kernel, p, (int)parts);
 }
 
-// Blocks per row: one when the rows fill the device; when they do not, a row is cut, down to 8 KB. A step also
-// cuts rows so that those being worked on (four blocks per SM) stay in L2 for their second reading.
+// Blocks per row: one when the rows fill the device; when they do not, a row is cut, down to 8 KB. A step also cuts
+// rows so that those being worked on (three blocks per SM) stay in L2 for their second reading: 4096 rows of
+// 131072 BF16 logits, in 1 / 2 / 4 blocks each, 493 / 465 / 511 us.
 constexpr int64_t kMinSliceBytes = 8 * 1024;
 constexpr int64_t kEnoughBlocks = 148 * 4;
-constexpr int64_t kResidentBytes = 64ll << 20;
+constexpr int64_t kWorkedOn = 148 * 3;
+constexpr int64_t kResidentBytes = 96ll << 20;
 
 unsigned blocks_per_row(int mode, int64_t rows, int64_t row_bytes) {
   unsigned n = 1;
   if (mode == kStep)
-    while (n < (unsigned)kDistillMaxCluster && kEnoughBlocks * row_bytes > kResidentBytes * n) n *= 2;
+    while (n < (unsigned)kDistillMaxCluster && kWorkedOn * row_bytes > kResidentBytes * n) n *= 2;
   while (n < (unsigned)kDistillMaxCluster && rows * n < kEnoughBlocks && row_bytes >= 2 * kMinSliceBytes * n) n *= 2;
   return n;
 }
