@@ -60,28 +60,131 @@ __device__ __forceinline__ void product_tmem(uint32_t d, uint32_t a, uint32_t se
     mma_ts(d, a + (k >> 2) * second + (k & 3) * 8, db + k * kRowStep, desc, add || k > FROM, leader);
 }
 
-// Capped and biased scores, in units of log2 e, and the factor of d score / d product.
+// How a product becomes a score, chosen per launch: the branches inside a tile's loops would keep the values' long
+// chains of special functions from overlapping (9000 cycles a step where these take a third).
+enum ScoreMode { kPlain = 0, kBias = 1, kCap = 2 };   // kBias also takes scales that are not positive; kCap has the bias as well
+
+// Scores in units of log2 e, and the factor of d score / d (scale product).
+template <int MODE>
 struct ScoreMod {
-  float scale;          // natural units
-  float cap, inv_cap;   // cap 0: none
-  float slope;          // log2 units
+  float scale;   // of the product; with a cap, of 2 log2(e) (scale / cap) product
+  float cap;     // cap log2 e
+  float slope;   // log2 units per position
   __device__ ScoreMod(const AttnParams& p, int h) {
-    scale = p.scale;
-    cap = p.softcap;
-    inv_cap = p.softcap > 0.0f ? 1.0f / p.softcap : 0.0f;
-    slope = p.slopes ? p.slopes[h] * kLog2e : 0.0f;
+    scale = MODE == kCap ? p.scale_log2 * 2.0f / p.softcap : p.scale_log2;
+    cap = p.softcap * kLog2e;
+    slope = p.slopes ? -p.slopes[h] * kLog2e : 0.0f;
   }
   // distance: query minus key
   __device__ __forceinline__ float operator()(float raw, float distance, float* grad) const {
-    float s = raw * scale;
     *grad = 1.0f;
-    if (cap > 0.0f) {
+    if constexpr (MODE == kCap) {
       // tanh y = 1 - 2 / (1 + exp 2y): absolute error near 2^-23, and 1 and -1 at the ends
-      const float th = fmaf(-2.0f, rcp_approx(1.0f + exp2_approx(s * inv_cap * (2.0f * kLog2e))), 1.0f);
-      s = cap * th;
+      const float th = fmaf(-2.0f, rcp_approx(1.0f + exp2_approx(raw * scale)), 1.0f);
       *grad = fmaf(-th, th, 1.0f);
+      return fmaf(slope, fabsf(distance), cap * th);
+    } else {
+      return fmaf(slope, fabsf(distance), raw * scale);
     }
-    return fmaf(s, kLog2e, -slope * fabsf(distance));
+  }
+};
+
+// ---- work --------------------------------------------------------------------------------------------
+//
+// Blocks stay: when one has finished its tile it takes over a block of the grid that has not started yet
+// (cluster launch control), so that a tile's loads and first products run while the rows of the tile before are
+// stored, and tiles of very different lengths fill the SMs. A warp of the block asks for the next tile and works
+// out its range of steps, one tile ahead of the others, who read it from a ring of two.
+template <typename Plan>
+struct WorkRing {
+  alignas(16) uint4 answer;
+  uint64_t answered, full[2], empty[2], ask;
+  Plan plan[2];
+  int item[2];   // -1: no more
+  static constexpr int kReaders = 10;   // warps of rows, the issuer, the producer
+  static constexpr uint32_t kNap = 100;
+  __device__ void init() {   // one thread
+    mbar_init(smem_addr(&answered), 1);
+    mbar_init(smem_addr(&ask), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_addr(&full[i]), 1);
+      mbar_init(smem_addr(&empty[i]), kReaders);
+    }
+  }
+  // The n-th item, for all threads of a reading warp (or for the one thread `alone`).
+  __device__ __forceinline__ bool next(int n, const Waiter& wait, int* it, Plan* pl, bool alone) {
+    const int slot = n & 1;
+    bool ok = wait(smem_addr(&full[slot]), n >> 1 & 1);
+    if (!alone) ok = __all_sync(0xffffffffu, ok);
+    if (!ok) return false;
+    if (alone) {
+      *it = item[slot];
+      *pl = plan[slot];
+    } else {
+      // broadcast, so that all that follows from it is known to be the same for the whole warp
+      *it = __shfl_sync(0xffffffffu, item[slot], 0);
+      const int* from = reinterpret_cast<const int*>(&plan[slot]);
+      int* to = reinterpret_cast<int*>(pl);
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof(Plan) / sizeof(int)); ++i) to[i] = __shfl_sync(0xffffffffu, from[i], 0);
+    }
+    if (alone || threadIdx.x % 32 == 0) mbar_arrive(smem_addr(&empty[slot]));
+    return *it >= 0;
+  }
+  // The producer, when it has sent for all of an item: only now is the next one taken, while the last steps and the
+  // stores are still to come. (Taken a whole item ahead, the long items of a causal walk ended up two to a block:
+  // keys' gradients of one document of 8192 tokens 1035 us.)
+  __device__ __forceinline__ void sent_all() { mbar_arrive(smem_addr(&ask)); }
+  // The asking warp: make(item) returns the item's plan (in every lane).
+  template <typename F>
+  __device__ __forceinline__ void serve(const Waiter& wait, F make) {
+    const int lane = threadIdx.x % 32;
+    int now = (int)blockIdx.x;
+    for (int n = 0;; ++n) {
+      const int slot = n & 1;
+      if (n >= 2 && !__all_sync(0xffffffffu, wait(smem_addr(&empty[slot]), (n >> 1) + 1 & 1, kNap))) return;
+      Plan pl = {};
+      if (now >= 0) pl = make(now);
+      if (lane == 0) {
+        item[slot] = now;
+        plan[slot] = pl;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_addr(&full[slot]));
+      if (now < 0 || !__all_sync(0xffffffffu, wait(smem_addr(&ask), n & 1, kNap))) return;
+      if (lane == 0) {
+        mbar_expect(smem_addr(&answered), 16);
+        take_over_next_block(smem_addr(&answer), smem_addr(&answered));
+      }
+      __syncwarp();
+      if (!__all_sync(0xffffffffu, wait(smem_addr(&answered), n & 1))) {
+        if (lane == 0) drain(smem_addr(&answered), n & 1);
+        return;
+      }
+      now = taken_block(smem_addr(&answer));
+      __syncwarp();
+      fence_async_proxy();   // the answer has been read before the next one is written
+    }
+  }
+};
+
+// The document offsets, when there are not too many, in shared memory: every row looks its document up there.
+constexpr int kDocCache = 128;
+struct DocCache {
+  int32_t cu[kDocCache + 1], prefix[kDocCache];
+  __device__ void fill(const DocMask& m) {   // all threads of the block
+    if (!m.cu || m.docs > kDocCache) return;
+    for (int i = threadIdx.x; i <= m.docs; i += blockDim.x) cu[i] = m.cu[i];
+    if (m.prefix)
+      for (int i = threadIdx.x; i < m.docs; i += blockDim.x) prefix[i] = m.prefix[i];
+  }
+  __device__ DocMask mask(const DocMask& m) const {
+    DocMask r = m;
+    if (m.cu && m.docs <= kDocCache) {
+      r.cu = cu;
+      if (m.prefix) r.prefix = prefix;
+    }
+    return r;
   }
 };
 
@@ -99,8 +202,8 @@ __device__ __forceinline__ void load_floats(float* y, const float* from) {
 
 // ---- forward -------------------------------------------------------------------------------------------
 //
-// A block takes 256 queries of one head as two tiles of 128 (one per row warpgroup) and walks the keys they
-// see in steps of 128. TMEM: scores of the tiles (128 columns each, overwritten by their BF16
+// An item is 256 queries of one head as two tiles of 128 (one per row warpgroup), for which the block walks the keys
+// they see in steps of 128. TMEM: scores of the tiles (128 columns each, overwritten by their BF16
 // probabilities) and their outputs. The issuer alternates between the tiles, so that one's products run
 // while the other's warpgroup exponentiates. A row's accumulators are rescaled only when its
 // maximum has grown by more than 2^8 since the last time.
@@ -111,13 +214,19 @@ template <int HALVES> struct ForwardShape {
   static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + 1024;
 };
 
-struct ForwardControl {
-  uint64_t q_full, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_half[2], p_ready[2], o_full[2], done;
-  uint32_t tmem, dead;
-  int lo[2], hi[2];   // keys that the tiles' rows see
+struct ForwardPlan {
+  int n_lo, steps;           // first key and steps of 128
+  int first[2], last[2];     // the steps that concern each tile
 };
 
-template <int HALVES, bool kMod>
+struct ForwardControl {
+  WorkRing<ForwardPlan> work;
+  DocCache docs;
+  uint64_t q_full, q_empty, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_half[2], p_ready[2], o_full[2], done;
+  uint32_t tmem, dead;
+};
+
+template <int HALVES, int MODE>
 __global__ void __launch_bounds__(kMmaThreads, 1)
     attention_forward_mma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
                                  const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
@@ -127,14 +236,17 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   __shared__ ForwardControl ctl;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   const int tiles = (p.tokens + 2 * kTile - 1) / (2 * kTile);
-  // the last queries see the most keys when causal: start with them
-  const int h = blockIdx.x % p.heads_q, m0 = (tiles - 1 - (int)(blockIdx.x / p.heads_q)) * 2 * kTile;
+  // item -> head and first query: the last queries see the most keys when causal, so they come first
+  const auto head_of = [&](int item) { return item % p.heads_q; };
+  const auto row_of = [&](int item) { return (tiles - 1 - item / p.heads_q) * 2 * kTile; };
   const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
   const uint32_t smem_q = base, smem_k = base + 2 * Shape::kTileBytes, smem_v = smem_k + S * Shape::kTileBytes;
   const Waiter wait{&ctl.dead, p.error};
 
   if (threadIdx.x == 0) {
+    ctl.work.init();
     mbar_init(smem_addr(&ctl.q_full), 1);
+    mbar_init(smem_addr(&ctl.q_empty), 1);
     for (int i = 0; i < S; ++i) {
       mbar_init(smem_addr(&ctl.k_full[i]), 1);
       mbar_init(smem_addr(&ctl.k_empty[i]), 1);
@@ -151,105 +263,119 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     ctl.dead = 0;
     mbar_init_fence();
   }
-  if (threadIdx.x >= 64 && threadIdx.x < 66) {
-    const int s = threadIdx.x - 64, r0 = m0 + s * kTile;
-    int lo = 0, hi = 0, x;
-    if (r0 < p.tokens) {
-      p.mask.keys_of(r0, &lo, &x);
-      p.mask.keys_of(r0 + kTile - 1 < p.tokens ? r0 + kTile - 1 : p.tokens - 1, &x, &hi);
-    }
-    ctl.lo[s] = lo;
-    ctl.hi[s] = hi > lo ? hi : lo;
-  }
+  ctl.docs.fill(p.mask);
   if (warp == 8) tmem_alloc(smem_addr(&ctl.tmem), kTmemColumns);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = ctl.tmem;
-
-  // steps [first[s], last[s]) of the walk concern tile s
-  int n_lo = 0, steps = 0, first[2], last[2];
-  {
-    const bool on0 = ctl.lo[0] < ctl.hi[0], on1 = ctl.lo[1] < ctl.hi[1];
-    n_lo = on0 && (!on1 || ctl.lo[0] < ctl.lo[1]) ? ctl.lo[0] : on1 ? ctl.lo[1] : 0;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const bool on = s ? on1 : on0;
-      first[s] = on ? (ctl.lo[s] - n_lo) / kTile : 0;
-      last[s] = on ? (ctl.hi[s] - n_lo + kTile - 1) / kTile : 0;
-      if (last[s] > steps) steps = last[s];
-    }
-  }
+  const DocMask mask = ctl.docs.mask(p.mask);
 
   if (warp >= 8) {
     fewer_registers();
-    if (warp == 9 && lane == 0) {   // ---- producer
-      const int hk = h / p.group;
-      int k_sent = 0, v_sent = 0, q_tiles = 0;
+    if (warp == 10) {   // ---- the next tiles
+      ctl.work.serve(wait, [&](int item) {
+        // lanes 0..3: the keys of each tile's first and last row
+        const int m0 = row_of(item), row = m0 + (lane >> 1) * kTile + (lane & 1 ? kTile - 1 : 0);
+        int lo = 0, hi = 0;
+        if (lane < 4 && m0 + (lane >> 1) * kTile < p.tokens) mask.keys_of(row < p.tokens ? row : p.tokens - 1, &lo, &hi);
+        ForwardPlan pl = {};
+        const int lo0 = __shfl_sync(0xffffffffu, lo, 0), hi0 = __shfl_sync(0xffffffffu, hi, 1);
+        const int lo1 = __shfl_sync(0xffffffffu, lo, 2), hi1 = __shfl_sync(0xffffffffu, hi, 3);
+        const bool on0 = lo0 < hi0, on1 = lo1 < hi1;
+        pl.n_lo = on0 && (!on1 || lo0 < lo1) ? lo0 : on1 ? lo1 : 0;
+        pl.first[0] = on0 ? (lo0 - pl.n_lo) / kTile : 0;
+        pl.last[0] = on0 ? (hi0 - pl.n_lo + kTile - 1) / kTile : 0;
+        pl.first[1] = on1 ? (lo1 - pl.n_lo) / kTile : 0;
+        pl.last[1] = on1 ? (hi1 - pl.n_lo + kTile - 1) / kTile : 0;
+        pl.steps = pl.last[0] > pl.last[1] ? pl.last[0] : pl.last[1];
+        return pl;
+      });
+    } else if (warp == 9 && lane == 0) {   // ---- producer
+      int item, sent = 0, walks = 0, q_bytes = 0;   // sent: key and value tiles so far
+      int k_sent = 0;
       bool ok = true;
-      for (int s = 0; s < 2; ++s) q_tiles += first[s] < last[s];
-      if (q_tiles > 0) {
-        mbar_expect(smem_addr(&ctl.q_full), q_tiles * Shape::kTileBytes);
+      ForwardPlan pl;
+      for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, true); ++n) {
+        if (pl.steps == 0) {
+          ctl.work.sent_all();
+          continue;
+        }
+        const int h = head_of(item), hk = h / p.group, m0 = row_of(item);
+        if (walks > 0 && !(ok = wait(smem_addr(&ctl.q_empty), walks - 1 & 1))) break;
+        q_bytes = ((pl.first[0] < pl.last[0]) + (pl.first[1] < pl.last[1])) * Shape::kTileBytes;
+        mbar_expect(smem_addr(&ctl.q_full), q_bytes);
         for (int s = 0; s < 2; ++s)
-          if (first[s] < last[s])
+          if (pl.first[s] < pl.last[s])
             load_tile<HALVES>(smem_q + s * Shape::kTileBytes, &map_q, h, m0 + s * kTile, smem_addr(&ctl.q_full));
-      }
-      for (int j = 0; j < steps && ok; ++j) {
-        const int st = j % S;
-        const uint32_t turn = (uint32_t)(j / S + 1) & 1;   // parity of the previous use's release
-        if (j >= S && !(ok = wait(smem_addr(&ctl.k_empty[st]), turn))) break;
-        mbar_expect(smem_addr(&ctl.k_full[st]), Shape::kTileBytes);
-        load_tile<HALVES>(smem_k + st * Shape::kTileBytes, &map_k, hk, n_lo + j * kTile, smem_addr(&ctl.k_full[st]));
-        ++k_sent;
-        if (j >= S && !(ok = wait(smem_addr(&ctl.v_empty[st]), turn))) break;
-        mbar_expect(smem_addr(&ctl.v_full[st]), Shape::kTileBytes);
-        load_tile<HALVES>(smem_v + st * Shape::kTileBytes, &map_v, hk, n_lo + j * kTile, smem_addr(&ctl.v_full[st]));
-        ++v_sent;
+        ++walks;
+        for (int j = 0; j < pl.steps; ++j, ++sent) {
+          const int st = sent % S;
+          const uint32_t turn = (uint32_t)(sent / S + 1) & 1;   // parity of the previous use's release
+          if (sent >= S && !(ok = wait(smem_addr(&ctl.k_empty[st]), turn))) break;
+          mbar_expect(smem_addr(&ctl.k_full[st]), Shape::kTileBytes);
+          load_tile<HALVES>(smem_k + st * Shape::kTileBytes, &map_k, hk, pl.n_lo + j * kTile, smem_addr(&ctl.k_full[st]));
+          ++k_sent;
+          if (sent >= S && !(ok = wait(smem_addr(&ctl.v_empty[st]), turn))) break;
+          mbar_expect(smem_addr(&ctl.v_full[st]), Shape::kTileBytes);
+          load_tile<HALVES>(smem_v + st * Shape::kTileBytes, &map_v, hk, pl.n_lo + j * kTile, smem_addr(&ctl.v_full[st]));
+        }
+        if (ok) ctl.work.sent_all();
       }
       if (ctl.dead) {   // leave no copy in flight
-        if (q_tiles > 0) drain(smem_addr(&ctl.q_full), 0);
+        if (walks > 0) drain(smem_addr(&ctl.q_full), walks - 1 & 1);
         for (int j = k_sent > S ? k_sent - S : 0; j < k_sent; ++j) drain(smem_addr(&ctl.k_full[j % S]), (j / S) & 1);
-        for (int j = v_sent > S ? v_sent - S : 0; j < v_sent; ++j) drain(smem_addr(&ctl.v_full[j % S]), (j / S) & 1);
+        for (int j = sent > S ? sent - S : 0; j < sent; ++j) drain(smem_addr(&ctl.v_full[j % S]), (j / S) & 1);
       }
     } else if (warp == 8) {   // ---- issuer
       const bool leader = elect_leader();
       const auto wait_all = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
       const int k_steps = (p.head_dim + 15) / 16;
       const uint32_t desc_s = mma_desc_bf16(kTile, false), desc_o = mma_desc_bf16(k_steps * 16, true);
-      bool ok = steps == 0 || wait_all(smem_addr(&ctl.q_full), 0);
-      for (int j = -1; j < steps && ok; ++j) {
-        // products of step j's probabilities, and step j + 1's scores
-        const int st = j % S, nx = (j + 1) % S;
-        bool have_k = false;
-        if (j >= 0 && !(ok = wait_all(smem_addr(&ctl.v_full[st]), (j / S) & 1))) break;
+      int item, done = 0, walks = 0, turns[2] = {0, 0};   // done: key tiles before this walk; turns: each tile's steps
+      bool ok = true;
+      ForwardPlan pl;
+      for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, false); ++n) {
+        if (pl.steps == 0) continue;
+        if (!(ok = wait_all(smem_addr(&ctl.q_full), walks & 1))) break;
+        ++walks;
+        for (int j = -1; j < pl.steps; ++j) {
+          // products of step j's probabilities, and step j + 1's scores
+          const int at = done + j, st = at % S, nx = (at + 1) % S;
+          const bool more = j + 1 < pl.steps;
+          bool have_k = false;
+          if (j >= 0 && !(ok = wait_all(smem_addr(&ctl.v_full[st]), (at / S) & 1))) break;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          if (j >= first[s] && j < last[s]) {
-            // the first 64 keys' products run while the row warps are on the other 64
-            const uint32_t turn = (j - first[s]) & 1, v = smem_v + st * Shape::kTileBytes;
-            if (!(ok = wait_all(smem_addr(&ctl.p_half[s]), turn))) break;
-            tc_fence_after();
-            product_tmem<0, 4>(tmem + 256 + s * 128, tmem + s * 128, 32, v, desc_o, j > first[s], leader);
-            if (!(ok = wait_all(smem_addr(&ctl.p_ready[s]), turn))) break;
-            tc_fence_after();
-            product_tmem<4, 8>(tmem + 256 + s * 128, tmem + s * 128, 32, v, desc_o, true, leader);
-            if (j == last[s] - 1) mma_commit(smem_addr(&ctl.o_full[s]), leader);
-          }
-          if (j + 1 >= first[s] && j + 1 < last[s]) {
-            if (!have_k) {
-              if (!(ok = wait_all(smem_addr(&ctl.k_full[nx]), ((j + 1) / S) & 1))) break;
-              have_k = true;
+          for (int s = 0; s < 2; ++s) {
+            if (j >= pl.first[s] && j < pl.last[s]) {
+              // the first 64 keys' products run while the row warps are on the other 64
+              const uint32_t turn = turns[s]++ & 1, v = smem_v + st * Shape::kTileBytes;
+              if (!(ok = wait_all(smem_addr(&ctl.p_half[s]), turn))) break;
+              tc_fence_after();
+              product_tmem<0, 4>(tmem + 256 + s * 128, tmem + s * 128, 32, v, desc_o, j > pl.first[s], leader);
+              if (!(ok = wait_all(smem_addr(&ctl.p_ready[s]), turn))) break;
+              tc_fence_after();
+              product_tmem<4, 8>(tmem + 256 + s * 128, tmem + s * 128, 32, v, desc_o, true, leader);
+              if (j == pl.last[s] - 1) mma_commit(smem_addr(&ctl.o_full[s]), leader);
             }
-            product_rows(tmem + s * 128, smem_q + s * Shape::kTileBytes, smem_k + nx * Shape::kTileBytes, k_steps, desc_s, leader);
-            mma_commit(smem_addr(&ctl.s_full[s]), leader);
+            if (j + 1 >= pl.first[s] && j + 1 < pl.last[s]) {
+              if (!have_k) {
+                if (!(ok = wait_all(smem_addr(&ctl.k_full[nx]), ((at + 1) / S) & 1))) break;
+                have_k = true;
+              }
+              product_rows(tmem + s * 128, smem_q + s * Shape::kTileBytes, smem_k + nx * Shape::kTileBytes, k_steps, desc_s, leader);
+              mma_commit(smem_addr(&ctl.s_full[s]), leader);
+            }
+          }
+          if (!ok) break;
+          if (j >= 0) mma_commit(smem_addr(&ctl.v_empty[st]), leader);
+          if (more) {
+            if (!have_k && !(ok = wait_all(smem_addr(&ctl.k_full[nx]), ((at + 1) / S) & 1))) break;
+            mma_commit(smem_addr(&ctl.k_empty[nx]), leader);
+            if (j + 2 == pl.steps) mma_commit(smem_addr(&ctl.q_empty), leader);
           }
         }
-        if (!ok) break;
-        if (j >= 0) mma_commit(smem_addr(&ctl.v_empty[st]), leader);
-        if (j + 1 < steps) {
-          if (!have_k && !(ok = wait_all(smem_addr(&ctl.k_full[nx]), ((j + 1) / S) & 1))) break;
-          mma_commit(smem_addr(&ctl.k_empty[nx]), leader);
-        }
+        done += pl.steps;
       }
       if (ctl.dead) {
         mma_commit(smem_addr(&ctl.done), leader);
@@ -259,102 +385,109 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   } else {   // ---- rows
     more_registers();
     const int s = warp / 4, r = (warp % 4) * 32;
-    const int i = m0 + s * kTile + r + lane;
     const uint32_t at = tmem + ((uint32_t)r << 16) + s * 128, at_o = at + 256;
-    const int from = s ? first[1] : first[0], to = s ? last[1] : last[0];
-    const ScoreMod mod(p, h);
-    int lo = 0, hi = 0;
-    if (i < p.tokens) p.mask.keys_of(i, &lo, &hi);
-    const float unit = kMod ? 1.0f : p.scale_log2;   // log2 per unit of the values compared
-    float m = -INFINITY, l = 0.0f;
+    const float unit = MODE == kPlain ? p.scale_log2 : 1.0f;   // log2 per unit of the values compared
+    int item, turns = 0, walks = 0;
     bool ok = true;
-    for (int j = from; j < to; ++j) {
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.s_full[s]), (j - from) & 1));
+    ForwardPlan pl;
+    for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, false); ++n) {
+      const int h = head_of(item), i = row_of(item) + s * kTile + r + lane;
+      const int from = s ? pl.first[1] : pl.first[0], to = s ? pl.last[1] : pl.last[0];
+      const ScoreMod<MODE> mod(p, h);
+      int lo = 0, hi = 0;
+      if (i < p.tokens) mask.keys_of(i, &lo, &hi);
+      float m = -INFINITY, l = 0.0f;
+      for (int j = from; j < to; ++j, ++turns) {
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.s_full[s]), turns & 1));
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t x[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_load32(at + c * 32, x + c * 32);
+        tmem_wait_load();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_landed(x + c * 32);
+        const int n0 = pl.n_lo + j * kTile;
+        if constexpr (MODE != kPlain) {
+          const float d0 = (float)(i - n0);
+          float g;
+#pragma unroll
+          for (int c = 0; c < 128; ++c) x[c] = __float_as_uint(mod(__uint_as_float(x[c]), d0 - (float)c, &g));
+        }
+        // visible columns [a, b); a chunk of 32 is masked value by value only where a row of the warp ends in it. Rows
+        // past the sequence are not stored: they need no mask.
+        const int a = i < p.tokens ? lo - n0 : 0, b = i < p.tokens ? hi - n0 : kTile;
+        if (!__all_sync(0xffffffffu, a <= 0 && b >= kTile)) {
+#pragma unroll
+          for (int c0 = 0; c0 < 128; c0 += 32)
+            if (!__all_sync(0xffffffffu, a <= c0 && b >= c0 + 32)) {
+#pragma unroll
+              for (int c = c0; c < c0 + 32; ++c) x[c] = c >= a && c < b ? x[c] : 0xff800000u;
+            }
+        }
+        float top[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) top[c] = __uint_as_float(x[c]);
+#pragma unroll
+        for (int c = 4; c < 128; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(x[c]));
+        const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        const bool grow = mx > -INFINITY && (m == -INFINITY || (mx - m) * unit > kRescaleAbove);
+        if (__any_sync(0xffffffffu, grow)) {
+          const float keep = !grow ? 1.0f : m == -INFINITY ? 0.0f : exp2_approx((m - mx) * unit);
+          if (grow) m = mx;
+          l *= keep;
+          if (j > from) {   // the products before these scores are complete: they were issued earlier
+#pragma unroll
+            for (int c = 0; c < HALVES * 2; ++c) {
+              uint32_t o[32];
+              tmem_load32(at_o + c * 32, o);
+              tmem_wait_load();
+              tmem_landed(o);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+              tmem_store32(at_o + c * 32, o);
+            }
+          }
+        }
+        const float shift = m == -INFINITY ? 0.0f : m * unit;
+        const uint64_t unit2 = pair(unit, unit), shift2 = pair(-shift, -shift);
+        uint64_t sum2[2] = {0, 0};
+        const auto probabilities = [&](int half) {
+          uint32_t pk[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            const int e = half * 64 + 2 * c;
+            const uint64_t y = fma2(pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), unit2, shift2);
+            float e0, e1;
+            if (c % 8 < kPolyOfEight) {
+              exp2_pair_poly(y, &e0, &e1);
+            } else {
+              split(y, &e0, &e1);
+              e0 = exp2_approx(e0);
+              e1 = exp2_approx(e1);
+            }
+            sum2[c & 1] = add2(sum2[c & 1], pair(e0, e1));
+            pk[c] = pack_bf16(e0, e1);
+          }
+          tmem_store32(at + half * 32, pk);
+        };
+        probabilities(0);
+        tmem_wait_store();
+        tc_fence_before();
+        mbar_arrive(smem_addr(&ctl.p_half[s]));
+        probabilities(1);
+        float s0, s1;
+        split(add2(sum2[0], sum2[1]), &s0, &s1);
+        l += s0 + s1;
+        tmem_wait_store();
+        tc_fence_before();
+        mbar_arrive(smem_addr(&ctl.p_ready[s]));
+      }
+      if (ok && from < to) {
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.o_full[s]), walks++ & 1));
+        tc_fence_after();
+      }
       if (!ok) break;
-      tc_fence_after();
-      uint32_t x[128];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_load32(at + c * 32, x + c * 32);
-      tmem_wait_load();
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_landed(x + c * 32);
-      const int n0 = n_lo + j * kTile;
-      if constexpr (kMod) {
-        const float d0 = (float)(i - n0);
-        float g;
-#pragma unroll
-        for (int c = 0; c < 128; ++c) x[c] = __float_as_uint(mod(__uint_as_float(x[c]), d0 - (float)c, &g));
-      }
-      // rows past the sequence are not stored: they need no mask
-      const bool whole = __all_sync(0xffffffffu, i >= p.tokens || (lo <= n0 && hi >= n0 + kTile));
-      if (!whole) {
-        const int a = lo - n0, b = hi - n0;
-#pragma unroll
-        for (int c = 0; c < 128; ++c) x[c] = c >= a && c < b ? x[c] : 0xff800000u;
-      }
-      float top[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) top[c] = __uint_as_float(x[c]);
-#pragma unroll
-      for (int c = 4; c < 128; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(x[c]));
-      const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-      const bool grow = mx > -INFINITY && (m == -INFINITY || (mx - m) * unit > kRescaleAbove);
-      if (__any_sync(0xffffffffu, grow)) {
-        const float keep = !grow ? 1.0f : m == -INFINITY ? 0.0f : exp2_approx((m - mx) * unit);
-        if (grow) m = mx;
-        l *= keep;
-        if (j > from) {   // the products before these scores are complete: they were issued earlier
-#pragma unroll
-          for (int c = 0; c < HALVES * 2; ++c) {
-            uint32_t o[32];
-            tmem_load32(at_o + c * 32, o);
-            tmem_wait_load();
-            tmem_landed(o);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-            tmem_store32(at_o + c * 32, o);
-          }
-        }
-      }
-      const float shift = m == -INFINITY ? 0.0f : m * unit;
-      const uint64_t unit2 = pair(unit, unit), shift2 = pair(-shift, -shift);
-      uint64_t sum2[2] = {0, 0};
-      const auto probabilities = [&](int half) {
-        uint32_t pk[32];
-#pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          const int e = half * 64 + 2 * c;
-          const uint64_t y = fma2(pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), unit2, shift2);
-          float e0, e1;
-          if (c % 8 < kPolyOfEight) {
-            exp2_pair_poly<4>(y, &e0, &e1);
-          } else {
-            split(y, &e0, &e1);
-            e0 = exp2_approx(e0);
-            e1 = exp2_approx(e1);
-          }
-          sum2[c & 1] = add2(sum2[c & 1], pair(e0, e1));
-          pk[c] = pack_bf16(e0, e1);
-        }
-        tmem_store32(at + half * 32, pk);
-      };
-      probabilities(0);
-      tmem_wait_store();
-      tc_fence_before();
-      mbar_arrive(smem_addr(&ctl.p_half[s]));
-      probabilities(1);
-      float s0, s1;
-      split(add2(sum2[0], sum2[1]), &s0, &s1);
-      l += s0 + s1;
-      tmem_wait_store();
-      tc_fence_before();
-      mbar_arrive(smem_addr(&ctl.p_ready[s]));
-    }
-    if (ok && from < to) {
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.o_full[s]), 0));
-      tc_fence_after();
-    }
-    if (ok) {
       const bool live = i < p.tokens, some = lo < hi;
       const float inv = some ? 1.0f / l : 0.0f;
       uint16_t* row = p.o.p + (int64_t)i * p.o.t + h * p.o.h;
@@ -403,7 +536,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 // sum is taken by one block in a fixed order. That costs the scores and dP twice (14 head_dim flops per
 // pair instead of 10) and buys the same bits in every run without FP32 atomics on dQ.
 
-// Keys: a block takes 128 keys of one key head and walks all queries that see them, for every query head of
+// Keys: an item is 128 keys of one key head, for which the block walks all queries that see them, for every query head of
 // the group. Rows of the tiles (TMEM lanes) are keys: S^T = K Q^T and dP^T = V dO^T, so that P^T and dS^T
 // are, as they stand, the left operands of dV and dK. TMEM: S^T, dP^T (overwritten by P^T and dS^T, each
 // warpgroup within its own 64 columns), dV, dK.
@@ -413,16 +546,21 @@ template <int HALVES> struct KeysShape {
   static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + 1024;
 };
 
-struct KeysControl {
-  alignas(16) float lse[2][kTile];
-  alignas(16) float delta[2][kTile];
-  uint64_t kv_full, q_full[2], q_empty[2], do_full[2], do_empty[2], s_full, dp_full, p_ready, ds_ready, acc_full, done;
-  uint32_t tmem, dead;
-  int lo, hi;
-  uint32_t redo[4];
+struct KeysPlan {
+  int q_lo, per_head;   // first tile of queries, tiles of queries per query head
 };
 
-template <int HALVES, bool kMod>
+struct KeysControl {
+  WorkRing<KeysPlan> work;
+  DocCache docs;
+  alignas(16) float lse[2][kTile];
+  alignas(16) float delta[2][kTile];
+  uint64_t kv_full, kv_empty, q_full[2], q_empty[2], do_full[2], do_empty[2], s_full, dp_full, p_ready, ds_ready, acc_full, stored, done;
+  uint32_t tmem, dead;
+  uint32_t redo[2][4];   // rows to do again, of this item and the next
+};
+
+template <int HALVES, int MODE>
 __global__ void __launch_bounds__(kMmaThreads, 1)
     attention_dkv_mma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
                              const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -432,14 +570,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   extern __shared__ uint8_t raw_smem[];
   __shared__ KeysControl ctl;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
-  const int hk = blockIdx.x % p.heads_kv, n0 = (int)(blockIdx.x / p.heads_kv) * kTile;   // first keys: most queries
+  // item -> key head and first key: the first keys are seen by the most queries when causal, so they come first
+  const auto head_of = [&](int item) { return item % p.heads_kv; };
+  const auto row_of = [&](int item) { return item / p.heads_kv * kTile; };
   const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
   const uint32_t smem_k = base, smem_v = smem_k + Shape::kTileBytes, smem_q = smem_v + Shape::kTileBytes,
                  smem_do = smem_q + S * Shape::kTileBytes;
   const Waiter wait{&ctl.dead, p.error};
 
   if (threadIdx.x == 0) {
+    ctl.work.init();
     mbar_init(smem_addr(&ctl.kv_full), 1);
+    mbar_init(smem_addr(&ctl.kv_empty), 1);
     for (int i = 0; i < S; ++i) {
       mbar_init(smem_addr(&ctl.q_full[i]), 1);
       mbar_init(smem_addr(&ctl.q_empty[i]), 1);
@@ -451,88 +593,111 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     mbar_init(smem_addr(&ctl.p_ready), 2 * kTile);
     mbar_init(smem_addr(&ctl.ds_ready), 2 * kTile);
     mbar_init(smem_addr(&ctl.acc_full), 1);
+    mbar_init(smem_addr(&ctl.stored), 2 * kTile);
     mbar_init(smem_addr(&ctl.done), 1);
     ctl.dead = 0;
-    for (int i = 0; i < 4; ++i) ctl.redo[i] = 0;
+    for (int i = 0; i < 4; ++i) ctl.redo[0][i] = ctl.redo[1][i] = 0;
     mbar_init_fence();
   }
-  if (threadIdx.x == 64) {
-    int lo, hi, x;
-    p.mask.queries_of(n0, &lo, &x);
-    p.mask.queries_of(n0 + kTile - 1 < p.tokens ? n0 + kTile - 1 : p.tokens - 1, &x, &hi);
-    ctl.lo = lo / kTile;                              // in tiles of queries
-    ctl.hi = hi > lo ? (hi + kTile - 1) / kTile : ctl.lo;
-  }
+  ctl.docs.fill(p.mask);
   if (warp == 8) tmem_alloc(smem_addr(&ctl.tmem), kTmemColumns);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = ctl.tmem, at_s = tmem, at_dp = tmem + 128, at_dv = tmem + 256, at_dk = tmem + 384;
-  const int q_lo = ctl.lo, per_head = ctl.hi - ctl.lo, steps = per_head * p.group;
+  const DocMask mask = ctl.docs.mask(p.mask);
 
   if (warp >= 8) {
     fewer_registers();
-    if (warp == 9 && lane == 0) {   // ---- producer
-      int q_sent = 0, do_sent = 0;
+    if (warp == 10) {   // ---- the next tiles
+      ctl.work.serve(wait, [&](int item) {
+        const int n0 = row_of(item), row = n0 + (lane ? kTile - 1 : 0);   // lanes 0 and 1: first and last key
+        int lo = 0, hi = 0;
+        if (lane < 2) mask.queries_of(row < p.tokens ? row : p.tokens - 1, &lo, &hi);
+        lo = __shfl_sync(0xffffffffu, lo, 0);
+        hi = __shfl_sync(0xffffffffu, hi, 1);
+        return KeysPlan{lo / kTile, hi > lo ? (hi + kTile - 1) / kTile - lo / kTile : 0};
+      });
+    } else if (warp == 9 && lane == 0) {   // ---- producer
+      int item, q_sent = 0, sent = 0, walks = 0;
       bool ok = true;
-      if (steps > 0) {
+      KeysPlan pl;
+      for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, true); ++n) {
+        if (pl.per_head == 0) {
+          ctl.work.sent_all();
+          continue;
+        }
+        const int hk = head_of(item), n0 = row_of(item);
+        if (walks > 0 && !(ok = wait(smem_addr(&ctl.kv_empty), walks - 1 & 1))) break;
         mbar_expect(smem_addr(&ctl.kv_full), 2 * Shape::kTileBytes);
         load_tile<HALVES>(smem_k, &map_k, hk, n0, smem_addr(&ctl.kv_full));
         load_tile<HALVES>(smem_v, &map_v, hk, n0, smem_addr(&ctl.kv_full));
-      }
-      for (int it = 0; it < steps && ok; ++it) {
-        const int st = it % S, h = hk * p.group + it / per_head, m0 = (q_lo + it % per_head) * kTile;
-        const uint32_t turn = (uint32_t)(it / S + 1) & 1;
-        if (it >= S && !(ok = wait(smem_addr(&ctl.q_empty[st]), turn))) break;
-        mbar_expect(smem_addr(&ctl.q_full[st]), Shape::kTileBytes + 2 * kTile * sizeof(float));
-        load_tile<HALVES>(smem_q + st * Shape::kTileBytes, &map_q, h, m0, smem_addr(&ctl.q_full[st]));
-        bulk_load(smem_addr(ctl.lse[st]), p.row_lse + h * p.pitch + m0, kTile * sizeof(float), smem_addr(&ctl.q_full[st]));
-        bulk_load(smem_addr(ctl.delta[st]), p.row_delta + h * p.pitch + m0, kTile * sizeof(float), smem_addr(&ctl.q_full[st]));
-        ++q_sent;
-        if (it >= S && !(ok = wait(smem_addr(&ctl.do_empty[st]), turn))) break;
-        mbar_expect(smem_addr(&ctl.do_full[st]), Shape::kTileBytes);
-        load_tile<HALVES>(smem_do + st * Shape::kTileBytes, &map_do, h, m0, smem_addr(&ctl.do_full[st]));
-        ++do_sent;
+        ++walks;
+        for (int h = hk * p.group; h < (hk + 1) * p.group && ok; ++h)
+          for (int tile = 0; tile < pl.per_head; ++tile, ++sent) {
+            const int st = sent % S, m0 = (pl.q_lo + tile) * kTile;
+            const uint32_t turn = (uint32_t)(sent / S + 1) & 1;
+            if (sent >= S && !(ok = wait(smem_addr(&ctl.q_empty[st]), turn))) break;
+            mbar_expect(smem_addr(&ctl.q_full[st]), Shape::kTileBytes + 2 * kTile * sizeof(float));
+            load_tile<HALVES>(smem_q + st * Shape::kTileBytes, &map_q, h, m0, smem_addr(&ctl.q_full[st]));
+            bulk_load(smem_addr(ctl.lse[st]), p.row_lse + h * p.pitch + m0, kTile * sizeof(float), smem_addr(&ctl.q_full[st]));
+            bulk_load(smem_addr(ctl.delta[st]), p.row_delta + h * p.pitch + m0, kTile * sizeof(float), smem_addr(&ctl.q_full[st]));
+            ++q_sent;
+            if (sent >= S && !(ok = wait(smem_addr(&ctl.do_empty[st]), turn))) break;
+            mbar_expect(smem_addr(&ctl.do_full[st]), Shape::kTileBytes);
+            load_tile<HALVES>(smem_do + st * Shape::kTileBytes, &map_do, h, m0, smem_addr(&ctl.do_full[st]));
+          }
+        if (ok) ctl.work.sent_all();
       }
       if (ctl.dead) {
-        if (steps > 0) drain(smem_addr(&ctl.kv_full), 0);
+        if (walks > 0) drain(smem_addr(&ctl.kv_full), walks - 1 & 1);
         for (int j = q_sent > S ? q_sent - S : 0; j < q_sent; ++j) drain(smem_addr(&ctl.q_full[j % S]), (j / S) & 1);
-        for (int j = do_sent > S ? do_sent - S : 0; j < do_sent; ++j) drain(smem_addr(&ctl.do_full[j % S]), (j / S) & 1);
+        for (int j = sent > S ? sent - S : 0; j < sent; ++j) drain(smem_addr(&ctl.do_full[j % S]), (j / S) & 1);
       }
     } else if (warp == 8) {   // ---- issuer
       const bool leader = elect_leader();
       const auto wait_all = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
       const int k_steps = (p.head_dim + 15) / 16;
       const uint32_t desc_s = mma_desc_bf16(kTile, false), desc_acc = mma_desc_bf16(k_steps * 16, true);
-      bool ok = steps == 0 || wait_all(smem_addr(&ctl.kv_full), 0);
-      for (int it = -1; it < steps && ok; ++it) {
-        const int st = it % S, nx = (it + 1) % S;
-        const bool more = it + 1 < steps;
-        const uint32_t next_turn = ((it + 1) / S) & 1;
-        if (it >= 0) {
-          if (!(ok = wait_all(smem_addr(&ctl.p_ready), it & 1))) break;
-          tc_fence_after();
-          product_tmem(at_dv, at_s, 64, smem_do + st * Shape::kTileBytes, desc_acc, it > 0, leader);
-          mma_commit(smem_addr(&ctl.do_empty[st]), leader);
+      int item, done = 0, walks = 0;   // done: steps before this walk
+      bool ok = true;
+      KeysPlan pl;
+      for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, false); ++n) {
+        const int steps = pl.per_head * p.group;
+        if (steps == 0) continue;
+        if (!(ok = wait_all(smem_addr(&ctl.kv_full), walks & 1))) break;
+        ++walks;
+        for (int it = -1; it < steps; ++it) {
+          const int at = done + it, st = at % S, nx = (at + 1) % S;
+          const bool more = it + 1 < steps;
+          const uint32_t next_turn = ((at + 1) / S) & 1;
+          if (it >= 0) {
+            if (!(ok = wait_all(smem_addr(&ctl.p_ready), at & 1))) break;
+            tc_fence_after();
+            product_tmem(at_dv, at_s, 64, smem_do + st * Shape::kTileBytes, desc_acc, it > 0, leader);
+            mma_commit(smem_addr(&ctl.do_empty[st]), leader);
+          }
+          if (more) {
+            if (!(ok = wait_all(smem_addr(&ctl.q_full[nx]), next_turn))) break;
+            product_rows(at_s, smem_k, smem_q + nx * Shape::kTileBytes, k_steps, desc_s, leader);
+            mma_commit(smem_addr(&ctl.s_full), leader);
+          }
+          if (it >= 0) {
+            if (!(ok = wait_all(smem_addr(&ctl.ds_ready), at & 1))) break;
+            tc_fence_after();
+            product_tmem(at_dk, at_dp, 64, smem_q + st * Shape::kTileBytes, desc_acc, it > 0, leader);
+            mma_commit(smem_addr(&ctl.q_empty[st]), leader);
+          }
+          if (more) {
+            if (!(ok = wait_all(smem_addr(&ctl.do_full[nx]), next_turn))) break;
+            product_rows(at_dp, smem_v, smem_do + nx * Shape::kTileBytes, k_steps, desc_s, leader);
+            mma_commit(smem_addr(&ctl.dp_full), leader);
+            if (it + 2 == steps) mma_commit(smem_addr(&ctl.kv_empty), leader);
+          }
         }
-        if (more) {
-          if (!(ok = wait_all(smem_addr(&ctl.q_full[nx]), next_turn))) break;
-          product_rows(at_s, smem_k, smem_q + nx * Shape::kTileBytes, k_steps, desc_s, leader);
-          mma_commit(smem_addr(&ctl.s_full), leader);
-        }
-        if (it >= 0) {
-          if (!(ok = wait_all(smem_addr(&ctl.ds_ready), it & 1))) break;
-          tc_fence_after();
-          product_tmem(at_dk, at_dp, 64, smem_q + st * Shape::kTileBytes, desc_acc, it > 0, leader);
-          mma_commit(smem_addr(&ctl.q_empty[st]), leader);
-        }
-        if (more) {
-          if (!(ok = wait_all(smem_addr(&ctl.do_full[nx]), next_turn))) break;
-          product_rows(at_dp, smem_v, smem_do + nx * Shape::kTileBytes, k_steps, desc_s, leader);
-          mma_commit(smem_addr(&ctl.dp_full), leader);
-        }
+        done += steps;
+        if (ok) mma_commit(smem_addr(&ctl.acc_full), leader);
       }
-      if (ok && steps > 0) mma_commit(smem_addr(&ctl.acc_full), leader);
       if (ctl.dead) {
         mma_commit(smem_addr(&ctl.done), leader);
         drain(smem_addr(&ctl.done), 0);
@@ -541,136 +706,144 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   } else {   // ---- rows: keys; the warpgroups take 64 of a step's queries each
     more_registers();
     const int g = warp / 4, r = (warp % 4) * 32;
-    const int j = n0 + r + lane;
     const uint32_t at = ((uint32_t)r << 16) + g * 64;
-    int lo = 0, hi = 0;
-    if (j < p.tokens) p.mask.queries_of(j, &lo, &hi);
+    int item, turns = 0, walks = 0;
     bool ok = true;
-    int h = hk * p.group, tile = 0;
-    ScoreMod mod(p, h);
-    for (int it = 0; it < steps; ++it, ++tile) {
-      if (tile == per_head) {
-        tile = 0;
-        mod = ScoreMod(p, ++h);
-      }
-      const int st = it % S, m0 = (q_lo + tile) * kTile + g * 64;
-      // The queries' statistics come from shared memory, which the tensor cores keep busy: they are
-      // fetched in blocks ahead of the waits (one at a time, each use waited 200 cycles).
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.q_full[st]), (it / S) & 1));
-      if (!ok) break;
-      float y[64];
-      load_floats<64>(y, &ctl.lse[st][g * 64]);
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.s_full), it & 1));
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t x[64];
-      tmem_load32(at_s + at, x);
-      tmem_load32(at_s + at + 32, x + 32);
-      tmem_wait_load();
-      tmem_landed(x);
-      tmem_landed(x + 32);
-      const bool whole = __all_sync(0xffffffffu, j >= p.tokens || (lo <= m0 && hi >= m0 + 64));
-      const int a = lo - m0, b = hi - m0;
-      float pr[64];   // P (d score / d product)
-      {
-        uint32_t pk[32];
-        const float d0 = (float)(j - m0);
-        const auto probabilities = [&](auto masked) {
+    KeysPlan pl;
+    for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, false); ++n) {
+      const int hk = head_of(item), n0 = row_of(item), j = n0 + r + lane, steps = pl.per_head * p.group;
+      int lo = 0, hi = 0;
+      if (j < p.tokens) mask.queries_of(j, &lo, &hi);
+      int h = hk * p.group, tile = 0;
+      ScoreMod<MODE> mod(p, h);
+      for (int it = 0; it < steps; ++it, ++tile, ++turns) {
+        if (tile == pl.per_head) {
+          tile = 0;
+          mod = ScoreMod<MODE>(p, ++h);
+        }
+        const int st = turns % S, m0 = (pl.q_lo + tile) * kTile + g * 64;
+        // The queries' statistics come from shared memory, which the tensor cores keep busy: they are
+        // fetched in blocks ahead of the waits (one at a time, each use waited 200 cycles).
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.q_full[st]), (turns / S) & 1));
+        if (!ok) break;
+        float y[64];
+        load_floats<64>(y, &ctl.lse[st][g * 64]);
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.s_full), turns & 1));
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t x[64];
+        tmem_load32(at_s + at, x);
+        tmem_load32(at_s + at + 32, x + 32);
+        tmem_wait_load();
+        tmem_landed(x);
+        tmem_landed(x + 32);
+        const int a = j < p.tokens ? lo - m0 : 0, b = j < p.tokens ? hi - m0 : 64;   // visible columns [a, b)
+        const bool whole[2] = {(bool)__all_sync(0xffffffffu, a <= 0 && b >= 32), (bool)__all_sync(0xffffffffu, a <= 32 && b >= 64)};
+        float pr[64];   // P (d score / d product)
+        {
+          uint32_t pk[32];
+          const float d0 = (float)(j - m0);
+          const auto probabilities = [&](int c0, auto masked) {
 #pragma unroll
-          for (int c = 0; c < 64; c += 2) {
-            float e[2], grad[2] = {1.0f, 1.0f};
+            for (int c = c0; c < c0 + 32; c += 2) {
+              float e[2], grad[2] = {1.0f, 1.0f};
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              if constexpr (kMod) e[k] = mod(__uint_as_float(x[c + k]), d0 - (float)(c + k), &grad[k]) - y[c + k];
-              else e[k] = fmaf(__uint_as_float(x[c + k]), p.scale_log2, -y[c + k]);
-              e[k] = exp2_approx(e[k]);
-              if (decltype(masked)::value) e[k] = c + k >= a && c + k < b ? e[k] : 0.0f;
-              pr[c + k] = kMod ? e[k] * grad[k] : e[k];
-            }
-            pk[c / 2] = pack_bf16(e[0], e[1]);
-          }
-        };
-        if (whole) probabilities(std::false_type()); else probabilities(std::true_type());
-        tmem_store32(at_s + at, pk);
-      }
-      tmem_wait_store();
-      tc_fence_before();
-      mbar_arrive(smem_addr(&ctl.p_ready));
-
-      load_floats<64>(y, &ctl.delta[st][g * 64]);
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.dp_full), it & 1));
-      if (!ok) break;
-      tc_fence_after();
-      {
-        uint32_t pk[32];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t d[32];
-          tmem_load32(at_dp + at + half * 32, d);
-          tmem_wait_load();
-          tmem_landed(d);
-          const auto gradients = [&](auto masked) {
-#pragma unroll
-            for (int c = 0; c < 32; c += 2) {
-              const int n = half * 32 + c;
-              float e0 = pr[n] * (__uint_as_float(d[c]) - y[n]), e1 = pr[n + 1] * (__uint_as_float(d[c + 1]) - y[n + 1]);
-              if (decltype(masked)::value) {   // not zero times what a masked pair holds
-                e0 = n >= a && n < b ? e0 : 0.0f;
-                e1 = n + 1 >= a && n + 1 < b ? e1 : 0.0f;
+              for (int k = 0; k < 2; ++k) {
+                if constexpr (MODE != kPlain) e[k] = mod(__uint_as_float(x[c + k]), d0 - (float)(c + k), &grad[k]) - y[c + k];
+                else e[k] = fmaf(__uint_as_float(x[c + k]), p.scale_log2, -y[c + k]);
+                e[k] = exp2_approx(e[k]);
+                if (decltype(masked)::value) e[k] = c + k >= a && c + k < b ? e[k] : 0.0f;
+                pr[c + k] = MODE == kCap ? e[k] * grad[k] : e[k];
               }
-              pk[n / 2] = pack_bf16(e0, e1);
+              pk[c / 2] = pack_bf16(e[0], e[1]);
             }
           };
-          if (whole) gradients(std::false_type()); else gradients(std::true_type());
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+            if (whole[half]) probabilities(half * 32, std::false_type()); else probabilities(half * 32, std::true_type());
+          tmem_store32(at_s + at, pk);
         }
-        tmem_store32(at_dp + at, pk);
+        tmem_wait_store();
+        tc_fence_before();
+        mbar_arrive(smem_addr(&ctl.p_ready));
+
+        load_floats<64>(y, &ctl.delta[st][g * 64]);
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.dp_full), turns & 1));
+        if (!ok) break;
+        tc_fence_after();
+        {
+          uint32_t pk[32];
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            uint32_t d[32];
+            tmem_load32(at_dp + at + half * 32, d);
+            tmem_wait_load();
+            tmem_landed(d);
+            const auto gradients = [&](auto masked) {
+#pragma unroll
+              for (int c = 0; c < 32; c += 2) {
+                const int n = half * 32 + c;
+                float e0 = pr[n] * (__uint_as_float(d[c]) - y[n]), e1 = pr[n + 1] * (__uint_as_float(d[c + 1]) - y[n + 1]);
+                if (decltype(masked)::value) {   // not zero times what a masked pair holds
+                  e0 = n >= a && n < b ? e0 : 0.0f;
+                  e1 = n + 1 >= a && n + 1 < b ? e1 : 0.0f;
+                }
+                pk[n / 2] = pack_bf16(e0, e1);
+              }
+            };
+            if (whole[half]) gradients(std::false_type()); else gradients(std::true_type());
+          }
+          tmem_store32(at_dp + at, pk);
+        }
+        tmem_wait_store();
+        tc_fence_before();
+        mbar_arrive(smem_addr(&ctl.ds_ready));
       }
-      tmem_wait_store();
-      tc_fence_before();
-      mbar_arrive(smem_addr(&ctl.ds_ready));
-    }
-    if (ok && steps > 0) {
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.acc_full), 0));
-      tc_fence_after();
-    }
-    bool nan = false;
-    if (ok) {
-      // warpgroup 0 stores dV, warpgroup 1 dK
-      const AttnView& out = g ? p.dk : p.dv;
-      const uint32_t src = (g ? at_dk : at_dv) + ((uint32_t)r << 16);
-      const float factor = g ? p.scale : 1.0f;
-      uint16_t* row = out.p + (int64_t)j * out.t + hk * out.h;
+      if (ok && steps > 0) {
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.acc_full), walks++ & 1));
+        tc_fence_after();
+      }
+      bool nan = false;
+      if (ok) {
+        // warpgroup 0 stores dV, warpgroup 1 dK
+        const AttnView& out = g ? p.dk : p.dv;
+        const uint32_t src = (g ? at_dk : at_dv) + ((uint32_t)r << 16);
+        const float factor = g ? p.scale : 1.0f;
+        uint16_t* row = out.p + (int64_t)j * out.t + hk * out.h;
 #pragma unroll
-      for (int c = 0; c < HALVES * 2; ++c) {
-        uint32_t o[32];
-        if (steps > 0) {
-          tmem_load32(src + c * 32, o);
-          tmem_wait_load();
-          tmem_landed(o);
-        } else {
+        for (int c = 0; c < HALVES * 2; ++c) {
+          uint32_t o[32];
+          if (steps > 0) {
+            tmem_load32(src + c * 32, o);
+            tmem_wait_load();
+            tmem_landed(o);
+          } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0;
-        }
+            for (int e = 0; e < 32; ++e) o[e] = 0;
+          }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int d = c * 32 + e * 8;
-          float y[8];
+          for (int e = 0; e < 4; ++e) {
+            const int d = c * 32 + e * 8;
+            float y[8];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[e * 8 + k]) * factor;
-          if (j < p.tokens && d < p.head_dim) {
+            for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[e * 8 + k]) * factor;
+            if (j < p.tokens && d < p.head_dim) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) nan |= y[k] != y[k];
-            *reinterpret_cast<uint4*>(row + d) =
-                make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+              for (int k = 0; k < 8; ++k) nan |= y[k] != y[k];
+              *reinterpret_cast<uint4*>(row + d) =
+                  make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+            }
           }
         }
       }
+      const uint32_t mine = __ballot_sync(0xffffffffu, nan);
+      if (lane == 0 && mine) atomicOr(&ctl.redo[n & 1][warp % 4], mine);
+      if (lane == 0 && g == 0) ctl.redo[n + 1 & 1][warp % 4] = 0;
+      mbar_arrive(smem_addr(&ctl.stored));   // both warpgroups have stored
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.stored), n & 1)) && ok;
+      if (g == 0 && ok)
+        for (uint32_t redo = ctl.redo[n & 1][warp % 4]; redo; redo &= redo - 1) attention_dkv_row(p, n0 + r + __ffs(redo) - 1, hk);
     }
-    const uint32_t mine = __ballot_sync(0xffffffffu, nan);
-    if (lane == 0 && mine) atomicOr(&ctl.redo[warp % 4], mine);
-    asm volatile("bar.sync 1, 256;" ::: "memory");   // both warpgroups have stored
-    if (g == 0)
-      for (uint32_t redo = ctl.redo[warp % 4]; redo; redo &= redo - 1) attention_dkv_row(p, n0 + r + __ffs(redo) - 1, hk);
   }
   __syncwarp();
   tc_fence_before();
@@ -678,7 +851,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   if (warp == 8) tmem_free(tmem, kTmemColumns);
 }
 
-// Queries: a block takes 128 queries of one head and walks the keys that they see. Rows are queries; dS goes
+// Queries: an item is 128 queries of one head, for which the block walks the keys that they see. Rows are queries; dS goes
 // where its scores were. TMEM: two buffers of scores (the next step's are made while this one's are
 // worked on), dP, dQ.
 template <int HALVES> struct QueriesShape {
@@ -688,14 +861,19 @@ template <int HALVES> struct QueriesShape {
   static constexpr int kSmem = (2 + kKStages + kVStages) * kTileBytes + 1024;
 };
 
-struct QueriesControl {
-  uint64_t q_full, k_full[3], k_empty[3], v_full[2], v_empty[2], s_full[2], dp_full, ds_ready, acc_full, done;
-  uint32_t tmem, dead;
-  int lo, hi;
-  uint32_t redo[4];
+struct QueriesPlan {
+  int n_lo, steps;   // first key and steps of 128
 };
 
-template <int HALVES, bool kMod>
+struct QueriesControl {
+  WorkRing<QueriesPlan> work;
+  DocCache docs;
+  uint64_t q_full, q_empty, k_full[3], k_empty[3], v_full[2], v_empty[2], s_full[2], dp_full, ds_ready, acc_full, stored, done;
+  uint32_t tmem, dead;
+  uint32_t redo[2][4];
+};
+
+template <int HALVES, int MODE>
 __global__ void __launch_bounds__(kMmaThreads, 1)
     attention_dq_mma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
                             const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -706,14 +884,17 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   __shared__ QueriesControl ctl;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   const int tiles = (p.tokens + kTile - 1) / kTile;
-  const int h = blockIdx.x % p.heads_q, m0 = (tiles - 1 - (int)(blockIdx.x / p.heads_q)) * kTile;
+  const auto head_of = [&](int item) { return item % p.heads_q; };
+  const auto row_of = [&](int item) { return (tiles - 1 - item / p.heads_q) * kTile; };
   const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
   const uint32_t smem_q = base, smem_do = smem_q + Shape::kTileBytes, smem_k = smem_do + Shape::kTileBytes,
                  smem_v = smem_k + SK * Shape::kTileBytes;
   const Waiter wait{&ctl.dead, p.error};
 
   if (threadIdx.x == 0) {
+    ctl.work.init();
     mbar_init(smem_addr(&ctl.q_full), 1);
+    mbar_init(smem_addr(&ctl.q_empty), 1);
     for (int i = 0; i < SK; ++i) {
       mbar_init(smem_addr(&ctl.k_full[i]), 1);
       mbar_init(smem_addr(&ctl.k_empty[i]), 1);
@@ -726,82 +907,102 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     mbar_init(smem_addr(&ctl.dp_full), 1);
     mbar_init(smem_addr(&ctl.ds_ready), 2 * kTile);
     mbar_init(smem_addr(&ctl.acc_full), 1);
+    mbar_init(smem_addr(&ctl.stored), 2 * kTile);
     mbar_init(smem_addr(&ctl.done), 1);
     ctl.dead = 0;
-    for (int i = 0; i < 4; ++i) ctl.redo[i] = 0;
+    for (int i = 0; i < 4; ++i) ctl.redo[0][i] = ctl.redo[1][i] = 0;
     mbar_init_fence();
   }
-  if (threadIdx.x == 64) {
-    int lo, hi, x;
-    p.mask.keys_of(m0, &lo, &x);
-    p.mask.keys_of(m0 + kTile - 1 < p.tokens ? m0 + kTile - 1 : p.tokens - 1, &x, &hi);
-    ctl.lo = lo;
-    ctl.hi = hi > lo ? hi : lo;
-  }
+  ctl.docs.fill(p.mask);
   if (warp == 8) tmem_alloc(smem_addr(&ctl.tmem), kTmemColumns);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = ctl.tmem, at_s = tmem, at_dp = tmem + 256, at_dq = tmem + 384;   // at_s: two buffers
-  const int n_lo = ctl.lo, steps = (ctl.hi - ctl.lo + kTile - 1) / kTile;
+  const DocMask mask = ctl.docs.mask(p.mask);
 
   if (warp >= 8) {
     fewer_registers();
-    if (warp == 9 && lane == 0) {   // ---- producer
-      const int hk = h / p.group;
-      int k_sent = 0, v_sent = 0;
+    if (warp == 10) {   // ---- the next tiles
+      ctl.work.serve(wait, [&](int item) {
+        const int m0 = row_of(item), row = m0 + (lane ? kTile - 1 : 0);   // lanes 0 and 1: first and last query
+        int lo = 0, hi = 0;
+        if (lane < 2) mask.keys_of(row < p.tokens ? row : p.tokens - 1, &lo, &hi);
+        lo = __shfl_sync(0xffffffffu, lo, 0);
+        hi = __shfl_sync(0xffffffffu, hi, 1);
+        return QueriesPlan{lo, hi > lo ? (hi - lo + kTile - 1) / kTile : 0};
+      });
+    } else if (warp == 9 && lane == 0) {   // ---- producer
+      int item, k_sent = 0, sent = 0, walks = 0;
       bool ok = true;
-      if (steps > 0) {
+      QueriesPlan pl;
+      for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, true); ++n) {
+        if (pl.steps == 0) {
+          ctl.work.sent_all();
+          continue;
+        }
+        const int h = head_of(item), hk = h / p.group, m0 = row_of(item);
+        if (walks > 0 && !(ok = wait(smem_addr(&ctl.q_empty), walks - 1 & 1))) break;
         mbar_expect(smem_addr(&ctl.q_full), 2 * Shape::kTileBytes);
         load_tile<HALVES>(smem_q, &map_q, h, m0, smem_addr(&ctl.q_full));
         load_tile<HALVES>(smem_do, &map_do, h, m0, smem_addr(&ctl.q_full));
-      }
-      for (int j = 0; j < steps && ok; ++j) {
-        const int sk = j % SK, sv = j % SV;
-        if (j >= SK && !(ok = wait(smem_addr(&ctl.k_empty[sk]), (uint32_t)(j / SK + 1) & 1))) break;
-        mbar_expect(smem_addr(&ctl.k_full[sk]), Shape::kTileBytes);
-        load_tile<HALVES>(smem_k + sk * Shape::kTileBytes, &map_k, hk, n_lo + j * kTile, smem_addr(&ctl.k_full[sk]));
-        ++k_sent;
-        if (j >= SV && !(ok = wait(smem_addr(&ctl.v_empty[sv]), (uint32_t)(j / SV + 1) & 1))) break;
-        mbar_expect(smem_addr(&ctl.v_full[sv]), Shape::kTileBytes);
-        load_tile<HALVES>(smem_v + sv * Shape::kTileBytes, &map_v, hk, n_lo + j * kTile, smem_addr(&ctl.v_full[sv]));
-        ++v_sent;
+        ++walks;
+        for (int j = 0; j < pl.steps; ++j, ++sent) {
+          const int sk = sent % SK, sv = sent % SV;
+          if (sent >= SK && !(ok = wait(smem_addr(&ctl.k_empty[sk]), (uint32_t)(sent / SK + 1) & 1))) break;
+          mbar_expect(smem_addr(&ctl.k_full[sk]), Shape::kTileBytes);
+          load_tile<HALVES>(smem_k + sk * Shape::kTileBytes, &map_k, hk, pl.n_lo + j * kTile, smem_addr(&ctl.k_full[sk]));
+          ++k_sent;
+          if (sent >= SV && !(ok = wait(smem_addr(&ctl.v_empty[sv]), (uint32_t)(sent / SV + 1) & 1))) break;
+          mbar_expect(smem_addr(&ctl.v_full[sv]), Shape::kTileBytes);
+          load_tile<HALVES>(smem_v + sv * Shape::kTileBytes, &map_v, hk, pl.n_lo + j * kTile, smem_addr(&ctl.v_full[sv]));
+        }
+        if (ok) ctl.work.sent_all();
       }
       if (ctl.dead) {
-        if (steps > 0) drain(smem_addr(&ctl.q_full), 0);
+        if (walks > 0) drain(smem_addr(&ctl.q_full), walks - 1 & 1);
         for (int j = k_sent > SK ? k_sent - SK : 0; j < k_sent; ++j) drain(smem_addr(&ctl.k_full[j % SK]), (j / SK) & 1);
-        for (int j = v_sent > SV ? v_sent - SV : 0; j < v_sent; ++j) drain(smem_addr(&ctl.v_full[j % SV]), (j / SV) & 1);
+        for (int j = sent > SV ? sent - SV : 0; j < sent; ++j) drain(smem_addr(&ctl.v_full[j % SV]), (j / SV) & 1);
       }
     } else if (warp == 8) {   // ---- issuer
       const bool leader = elect_leader();
       const auto wait_all = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
       const int k_steps = (p.head_dim + 15) / 16;
       const uint32_t desc_s = mma_desc_bf16(kTile, false), desc_acc = mma_desc_bf16(k_steps * 16, true);
-      bool ok = steps == 0 || wait_all(smem_addr(&ctl.q_full), 0);
-      for (int j = -1; j < steps && ok; ++j) {
-        const int nk = (j + 1) % SK, nv = (j + 1) % SV;
-        const bool more = j + 1 < steps;
-        if (more) {
-          if (!(ok = wait_all(smem_addr(&ctl.k_full[nk]), ((j + 1) / SK) & 1))) break;
-          product_rows(at_s + ((j + 1) & 1) * 128, smem_q, smem_k + nk * Shape::kTileBytes, k_steps, desc_s, leader);
-          mma_commit(smem_addr(&ctl.s_full[(j + 1) & 1]), leader);
+      int item, done = 0, walks = 0;   // done: steps before this walk
+      bool ok = true;
+      QueriesPlan pl;
+      for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, false); ++n) {
+        if (pl.steps == 0) continue;
+        if (!(ok = wait_all(smem_addr(&ctl.q_full), walks & 1))) break;
+        ++walks;
+        for (int j = -1; j < pl.steps; ++j) {
+          const int at = done + j, nk = (at + 1) % SK, nv = (at + 1) % SV;
+          const bool more = j + 1 < pl.steps;
+          if (more) {
+            if (!(ok = wait_all(smem_addr(&ctl.k_full[nk]), ((at + 1) / SK) & 1))) break;
+            product_rows(at_s + (at + 1 & 1) * 128, smem_q, smem_k + nk * Shape::kTileBytes, k_steps, desc_s, leader);
+            mma_commit(smem_addr(&ctl.s_full[at + 1 & 1]), leader);
+          }
+          if (j >= 0) {
+            if (!(ok = wait_all(smem_addr(&ctl.ds_ready), at & 1))) break;
+            tc_fence_after();
+          }
+          if (more) {
+            if (!(ok = wait_all(smem_addr(&ctl.v_full[nv]), ((at + 1) / SV) & 1))) break;
+            product_rows(at_dp, smem_do, smem_v + nv * Shape::kTileBytes, k_steps, desc_s, leader);
+            mma_commit(smem_addr(&ctl.dp_full), leader);
+            mma_commit(smem_addr(&ctl.v_empty[nv]), leader);
+            if (j + 2 == pl.steps) mma_commit(smem_addr(&ctl.q_empty), leader);
+          }
+          if (j >= 0) {
+            product_tmem(at_dq, at_s + (at & 1) * 128, 64, smem_k + (at % SK) * Shape::kTileBytes, desc_acc, j > 0, leader);
+            mma_commit(smem_addr(&ctl.k_empty[at % SK]), leader);
+          }
         }
-        if (j >= 0) {
-          if (!(ok = wait_all(smem_addr(&ctl.ds_ready), j & 1))) break;
-          tc_fence_after();
-        }
-        if (more) {
-          if (!(ok = wait_all(smem_addr(&ctl.v_full[nv]), ((j + 1) / SV) & 1))) break;
-          product_rows(at_dp, smem_do, smem_v + nv * Shape::kTileBytes, k_steps, desc_s, leader);
-          mma_commit(smem_addr(&ctl.dp_full), leader);
-          mma_commit(smem_addr(&ctl.v_empty[nv]), leader);
-        }
-        if (j >= 0) {
-          product_tmem(at_dq, at_s + (j & 1) * 128, 64, smem_k + (j % SK) * Shape::kTileBytes, desc_acc, j > 0, leader);
-          mma_commit(smem_addr(&ctl.k_empty[j % SK]), leader);
-        }
+        done += pl.steps;
+        if (ok) mma_commit(smem_addr(&ctl.acc_full), leader);
       }
-      if (ok && steps > 0) mma_commit(smem_addr(&ctl.acc_full), leader);
       if (ctl.dead) {
         mma_commit(smem_addr(&ctl.done), leader);
         drain(smem_addr(&ctl.done), 0);
@@ -810,102 +1011,113 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   } else {   // ---- rows: queries; the warpgroups take 64 of a step's keys each
     more_registers();
     const int g = warp / 4, r = (warp % 4) * 32;
-    const int i = m0 + r + lane;
     const uint32_t at = ((uint32_t)r << 16) + g * 64;
-    const ScoreMod mod(p, h);
-    int lo = 0, hi = 0;
-    float lse = 0.0f, delta = 0.0f;
-    if (i < p.tokens) {
-      p.mask.keys_of(i, &lo, &hi);
-      lse = p.row_lse[h * p.pitch + i];
-      delta = p.row_delta[h * p.pitch + i];
-    }
+    int item, turns = 0, walks = 0;
     bool ok = true;
-    for (int j = 0; j < steps; ++j) {
-      const uint32_t buf = at_s + (j & 1) * 128 + at;
-      const int c0 = n_lo + j * kTile + g * 64;
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.s_full[j & 1]), (j >> 1) & 1));
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t x[64];
-      tmem_load32(buf, x);
-      tmem_load32(buf + 32, x + 32);
-      tmem_wait_load();
-      tmem_landed(x);
-      tmem_landed(x + 32);
-      const bool whole = __all_sync(0xffffffffu, i >= p.tokens || (lo <= c0 && hi >= c0 + 64));
-      const int a = lo - c0, b = hi - c0;
-      float pr[64];
-#pragma unroll
-      for (int c = 0; c < 64; ++c) {
-        float e, grad = 1.0f;
-        if constexpr (kMod) e = mod(__uint_as_float(x[c]), (float)(i - c0) - (float)c, &grad) - lse;
-        else e = fmaf(__uint_as_float(x[c]), p.scale_log2, -lse);
-        pr[c] = exp2_approx(e) * grad;
+    QueriesPlan pl;
+    for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, false); ++n) {
+      const int h = head_of(item), m0 = row_of(item), i = m0 + r + lane, steps = pl.steps;
+      const ScoreMod<MODE> mod(p, h);
+      int lo = 0, hi = 0;
+      float lse = 0.0f, delta = 0.0f;
+      if (i < p.tokens) {
+        mask.keys_of(i, &lo, &hi);
+        lse = p.row_lse[h * p.pitch + i];
+        delta = p.row_delta[h * p.pitch + i];
       }
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.dp_full), j & 1));
-      if (!ok) break;
-      tc_fence_after();
-      tmem_load32(at_dp + at, x);
-      tmem_load32(at_dp + at + 32, x + 32);
-      tmem_wait_load();
-      tmem_landed(x);
-      tmem_landed(x + 32);
-      uint32_t pk[32];
+      for (int j = 0; j < steps; ++j, ++turns) {
+        const uint32_t buf = at_s + (turns & 1) * 128 + at;
+        const int c0 = pl.n_lo + j * kTile + g * 64;
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.s_full[turns & 1]), (turns >> 1) & 1));
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t x[64];
+        tmem_load32(buf, x);
+        tmem_load32(buf + 32, x + 32);
+        tmem_wait_load();
+        tmem_landed(x);
+        tmem_landed(x + 32);
+        const int a = i < p.tokens ? lo - c0 : 0, b = i < p.tokens ? hi - c0 : 64;   // visible columns [a, b)
+        const bool whole[2] = {(bool)__all_sync(0xffffffffu, a <= 0 && b >= 32), (bool)__all_sync(0xffffffffu, a <= 32 && b >= 64)};
+        float pr[64];
 #pragma unroll
-      for (int c = 0; c < 32; ++c) {
-        float e0 = pr[2 * c] * (__uint_as_float(x[2 * c]) - delta);
-        float e1 = pr[2 * c + 1] * (__uint_as_float(x[2 * c + 1]) - delta);
-        if (!whole) {
-          e0 = 2 * c >= a && 2 * c < b ? e0 : 0.0f;
-          e1 = 2 * c + 1 >= a && 2 * c + 1 < b ? e1 : 0.0f;
+        for (int c = 0; c < 64; ++c) {
+          float e, grad = 1.0f;
+          if constexpr (MODE != kPlain) e = mod(__uint_as_float(x[c]), (float)(i - c0) - (float)c, &grad) - lse;
+          else e = fmaf(__uint_as_float(x[c]), p.scale_log2, -lse);
+          pr[c] = exp2_approx(e) * grad;
         }
-        pk[c] = pack_bf16(e0, e1);
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.dp_full), turns & 1));
+        if (!ok) break;
+        tc_fence_after();
+        tmem_load32(at_dp + at, x);
+        tmem_load32(at_dp + at + 32, x + 32);
+        tmem_wait_load();
+        tmem_landed(x);
+        tmem_landed(x + 32);
+        uint32_t pk[32];
+        const auto gradients = [&](int half, auto masked) {
+#pragma unroll
+          for (int c = half * 16; c < half * 16 + 16; ++c) {
+            float e0 = pr[2 * c] * (__uint_as_float(x[2 * c]) - delta);
+            float e1 = pr[2 * c + 1] * (__uint_as_float(x[2 * c + 1]) - delta);
+            if (decltype(masked)::value) {
+              e0 = 2 * c >= a && 2 * c < b ? e0 : 0.0f;
+              e1 = 2 * c + 1 >= a && 2 * c + 1 < b ? e1 : 0.0f;
+            }
+            pk[c] = pack_bf16(e0, e1);
+          }
+        };
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          if (whole[half]) gradients(half, std::false_type()); else gradients(half, std::true_type());
+        tmem_store32(buf, pk);
+        tmem_wait_store();
+        tc_fence_before();
+        mbar_arrive(smem_addr(&ctl.ds_ready));
       }
-      tmem_store32(buf, pk);
-      tmem_wait_store();
-      tc_fence_before();
-      mbar_arrive(smem_addr(&ctl.ds_ready));
-    }
-    if (ok && steps > 0) {
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.acc_full), 0));
-      tc_fence_after();
-    }
-    bool nan = false;
-    if (ok) {
-      uint16_t* row = p.dq.p + (int64_t)i * p.dq.t + h * p.dq.h;
+      if (ok && steps > 0) {
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.acc_full), walks++ & 1));
+        tc_fence_after();
+      }
+      bool nan = false;
+      if (ok) {
+        uint16_t* row = p.dq.p + (int64_t)i * p.dq.t + h * p.dq.h;
 #pragma unroll
-      for (int c = 0; c < HALVES; ++c) {   // the warpgroups store half of the columns each
-        const int d0 = g * HALVES * 32 + c * 32;
-        uint32_t o[32];
-        if (steps > 0) {
-          tmem_load32(at_dq + ((uint32_t)r << 16) + d0, o);
-          tmem_wait_load();
-          tmem_landed(o);
-        } else {
+        for (int c = 0; c < HALVES; ++c) {   // the warpgroups store half of the columns each
+          const int d0 = g * HALVES * 32 + c * 32;
+          uint32_t o[32];
+          if (steps > 0) {
+            tmem_load32(at_dq + ((uint32_t)r << 16) + d0, o);
+            tmem_wait_load();
+            tmem_landed(o);
+          } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0;
-        }
+            for (int e = 0; e < 32; ++e) o[e] = 0;
+          }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int d = d0 + e * 8;
-          float y[8];
+          for (int e = 0; e < 4; ++e) {
+            const int d = d0 + e * 8;
+            float y[8];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[e * 8 + k]) * p.scale;
-          if (i < p.tokens && d < p.head_dim) {
+            for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[e * 8 + k]) * p.scale;
+            if (i < p.tokens && d < p.head_dim) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) nan |= y[k] != y[k];
-            *reinterpret_cast<uint4*>(row + d) =
-                make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+              for (int k = 0; k < 8; ++k) nan |= y[k] != y[k];
+              *reinterpret_cast<uint4*>(row + d) =
+                  make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+            }
           }
         }
       }
+      const uint32_t mine = __ballot_sync(0xffffffffu, nan);
+      if (lane == 0 && mine) atomicOr(&ctl.redo[n & 1][warp % 4], mine);
+      if (lane == 0 && g == 0) ctl.redo[n + 1 & 1][warp % 4] = 0;
+      mbar_arrive(smem_addr(&ctl.stored));
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.stored), n & 1)) && ok;
+      if (g == 0 && ok)
+        for (uint32_t redo = ctl.redo[n & 1][warp % 4]; redo; redo &= redo - 1) attention_dq_row(p, m0 + r + __ffs(redo) - 1, h);
     }
-    const uint32_t mine = __ballot_sync(0xffffffffu, nan);
-    if (lane == 0 && mine) atomicOr(&ctl.redo[warp % 4], mine);
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    if (g == 0)
-      for (uint32_t redo = ctl.redo[warp % 4]; redo; redo &= redo - 1) attention_dq_row(p, m0 + r + __ffs(redo) - 1, h);
   }
   __syncwarp();
   tc_fence_before();
@@ -956,53 +1168,61 @@ static cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>* done, 
   return e;
 }
 
-static bool plain_scores(const AttnParams& p) { return p.softcap == 0.0f && !p.slopes && p.scale_log2 > 0.0f; }
+static int score_mode(const AttnParams& p) { return p.softcap > 0.0f ? kCap : p.slopes || !(p.scale_log2 > 0.0f) ? kBias : kPlain; }
 
-template <int HALVES, bool kMod>
+template <int HALVES, int MODE>
 static int forward(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
   static std::atomic<uint64_t> ready{0};
   CUtensorMap q, k, v;
   if (!make_map(&q, p.q, p, p.heads_q) || !make_map(&k, p.k, p, p.heads_kv) || !make_map(&v, p.v, p, p.heads_kv))
     return SLIDEDP_ERR_CUDA;
-  CU(allow_smem(attention_forward_mma_kernel<HALVES, kMod>, ForwardShape<HALVES>::kSmem, &ready, ctx->device));
+  CU(allow_smem(attention_forward_mma_kernel<HALVES, MODE>, ForwardShape<HALVES>::kSmem, &ready, ctx->device));
   const int64_t blocks = (int64_t)((p.tokens + 2 * kTile - 1) / (2 * kTile)) * p.heads_q;
   if (blocks > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
-  attention_forward_mma_kernel<HALVES, kMod><<<(unsigned)blocks, kMmaThreads, ForwardShape<HALVES>::kSmem, st>>>(p, q, k, v);
+  attention_forward_mma_kernel<HALVES, MODE><<<(unsigned)blocks, kMmaThreads, ForwardShape<HALVES>::kSmem, st>>>(p, q, k, v);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;
 }
 
-template <int HALVES, bool kMod>
+template <int HALVES, int MODE>
 static int backward(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
   static std::atomic<uint64_t> ready_q{0}, ready_k{0};
   CUtensorMap q, k, v, d;
   if (!make_map(&q, p.q, p, p.heads_q) || !make_map(&k, p.k, p, p.heads_kv) || !make_map(&v, p.v, p, p.heads_kv) ||
       !make_map(&d, p.dout, p, p.heads_q))
     return SLIDEDP_ERR_CUDA;
-  CU(allow_smem(attention_dkv_mma_kernel<HALVES, kMod>, KeysShape<HALVES>::kSmem, &ready_k, ctx->device));
-  CU(allow_smem(attention_dq_mma_kernel<HALVES, kMod>, QueriesShape<HALVES>::kSmem, &ready_q, ctx->device));
+  CU(allow_smem(attention_dkv_mma_kernel<HALVES, MODE>, KeysShape<HALVES>::kSmem, &ready_k, ctx->device));
+  CU(allow_smem(attention_dq_mma_kernel<HALVES, MODE>, QueriesShape<HALVES>::kSmem, &ready_q, ctx->device));
   const int64_t tiles = (p.tokens + kTile - 1) / kTile;
   if (tiles * p.heads_q > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
   FAULT_POINT();
-  attention_dkv_mma_kernel<HALVES, kMod><<<(unsigned)(tiles * p.heads_kv), kMmaThreads, KeysShape<HALVES>::kSmem, st>>>(p, q, k, v, d);
+  attention_dkv_mma_kernel<HALVES, MODE><<<(unsigned)(tiles * p.heads_kv), kMmaThreads, KeysShape<HALVES>::kSmem, st>>>(p, q, k, v, d);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   FAULT_POINT();
-  attention_dq_mma_kernel<HALVES, kMod><<<(unsigned)(tiles * p.heads_q), kMmaThreads, QueriesShape<HALVES>::kSmem, st>>>(p, q, k, v, d);
+  attention_dq_mma_kernel<HALVES, MODE><<<(unsigned)(tiles * p.heads_q), kMmaThreads, QueriesShape<HALVES>::kSmem, st>>>(p, q, k, v, d);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;
 }
 
 int attention_forward_mma(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
-  if (p.head_dim <= 64) return plain_scores(p) ? forward<1, false>(ctx, p, st) : forward<1, true>(ctx, p, st);
-  return plain_scores(p) ? forward<2, false>(ctx, p, st) : forward<2, true>(ctx, p, st);
+  const bool narrow = p.head_dim <= 64;
+  switch (score_mode(p)) {
+    case kPlain: return narrow ? forward<1, kPlain>(ctx, p, st) : forward<2, kPlain>(ctx, p, st);
+    case kBias: return narrow ? forward<1, kBias>(ctx, p, st) : forward<2, kBias>(ctx, p, st);
+    default: return narrow ? forward<1, kCap>(ctx, p, st) : forward<2, kCap>(ctx, p, st);
+  }
 }
 
 int attention_backward_mma(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
-  if (p.head_dim <= 64) return plain_scores(p) ? backward<1, false>(ctx, p, st) : backward<1, true>(ctx, p, st);
-  return plain_scores(p) ? backward<2, false>(ctx, p, st) : backward<2, true>(ctx, p, st);
+  const bool narrow = p.head_dim <= 64;
+  switch (score_mode(p)) {
+    case kPlain: return narrow ? backward<1, kPlain>(ctx, p, st) : backward<2, kPlain>(ctx, p, st);
+    case kBias: return narrow ? backward<1, kBias>(ctx, p, st) : backward<2, kBias>(ctx, p, st);
+    default: return narrow ? backward<1, kCap>(ctx, p, st) : backward<2, kCap>(ctx, p, st);
+  }
 }
 
 }  // namespace host

@@ -42,17 +42,41 @@ constexpr uint32_t kSpinLimit = 1u << 24;
 struct Waiter {
   volatile uint32_t* dead;   // shared memory
   int* error;                // pinned host memory
-  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, uint32_t nap_ns = 0) const {
     if (mbar_try(bar, parity)) return true;
     for (uint32_t n = 0; n < kSpinLimit; ++n) {
       if (mbar_try(bar, parity)) return true;
       if ((n & 255u) == 255u && *dead) return false;
+      if (nap_ns) __nanosleep(nap_ns);   // a wait that may be long and is not urgent leaves the issue slots alone
     }
     *dead = 1;
     *reinterpret_cast<volatile int*>(error) = 1;
     return false;
   }
 };
+
+// Order between ordinary accesses of shared memory and those of the asynchronous proxy (copies, answers).
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// ---- cluster launch control --------------------------------------------------------------------------
+
+// Asks to take over a block of the grid that has not started; 16 bytes at `answer` complete on `bar`.
+__device__ __forceinline__ void take_over_next_block(uint32_t answer, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar)
+               : "memory");
+}
+// The index of the block taken over, or -1 when none was left (after which one must not ask again).
+__device__ __forceinline__ int taken_block(uint32_t answer) {
+  uint32_t ok, x;
+  asm volatile(
+      "{\n .reg .b128 r;\n .reg .pred p;\n ld.shared.b128 r, [%2];\n"
+      " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n selp.u32 %0, 1, 0, p;\n mov.u32 %1, 0;\n"
+      " @p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}"
+      : "=r"(ok), "=r"(x)
+      : "r"(answer)
+      : "memory");
+  return ok ? (int)x : -1;
+}
 
 // ---- TMA -------------------------------------------------------------------------------------------
 
@@ -193,12 +217,10 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
 }
 // 2^x on the multiply-add pipe, for a share of the exponentials where the special-function pipe would be the
 // bound: x = n + f with n = floor x (adding 1.5 * 2^23, rounded down, leaves n in the low bits), 2^f on [0, 1)
-// by the polynomial with p(0) = 1 and the least greatest relative error (from a linear program: 2.9e-6 at
-// degree 4, 9.2e-8 at degree 5), n added to the exponent. Below -127 the result is exactly zero; NaN stays
-// NaN; x is at most a few units above zero.
-template <int DEGREE>
+// by the polynomial of degree 4 with p(0) = 1 and the least greatest relative error (2.9e-6, from a linear
+// program; the result is rounded to BF16, 4e-3), n added to the exponent. Below -127 the result is exactly
+// zero; NaN stays NaN; x is at most a few units above zero.
 __device__ __forceinline__ void exp2_pair_poly(uint64_t x, float* lo, float* hi) {
-  static_assert(DEGREE == 4 || DEGREE == 5, "");
   float a, b, ta, tb, pa, pb;
   split(x, &a, &b);
   asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(a));   // -127
@@ -208,17 +230,9 @@ __device__ __forceinline__ void exp2_pair_poly(uint64_t x, float* lo, float* hi)
   asm("add.rm.f32x2 %0, %1, %2;" : "=l"(t) : "l"(x), "l"(pair(12582912.0f, 12582912.0f)));
   const uint64_t f = fma2(add2(t, pair(-12582912.0f, -12582912.0f)), pair(-1.0f, -1.0f), x);
   const auto step = [&](uint64_t p, float c) { return fma2(p, f, pair(c, c)); };
-  uint64_t p;
-  if constexpr (DEGREE == 4) {
-    p = step(pair(0.013426683843135834f, 0.013426683843135834f), 0.052242472767829895f);
-    p = step(p, 0.241280198097229f);
-    p = step(p, 0.6930448412895203f);
-  } else {
-    p = step(pair(0.0018671337747946382f, 0.0018671337747946382f), 0.00901702232658863f);
-    p = step(p, 0.05579992011189461f);
-    p = step(p, 0.24016444385051727f);
-    p = step(p, 0.6931512951850891f);
-  }
+  uint64_t p = step(pair(0.013426683843135834f, 0.013426683843135834f), 0.052242472767829895f);
+  p = step(p, 0.241280198097229f);
+  p = step(p, 0.6930448412895203f);
   p = step(p, 1.0f);
   split(t, &ta, &tb);
   split(p, &pa, &pb);
