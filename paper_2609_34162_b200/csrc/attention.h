@@ -14,41 +14,45 @@ struct DocMask {
   int docs, tokens, causal;
 
 #ifdef __CUDACC__
-  // Document of token i as [s, e) and its index; false (and an empty range that keeps the order)
-  // when no document holds it. Bounds are clamped to the sequence whatever the array holds.
-  __device__ __forceinline__ bool find(int i, int* s, int* e, int* d) const {
-    if (!cu) { *s = 0; *e = tokens; *d = 0; return true; }
-    int lo = 0, hi = docs + 1;       // first index whose offset is above i
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (cu[mid] <= i) lo = mid + 1; else hi = mid;
+  // First index whose offset is above i, known to lie in [from, to]; 0 and 0 without offsets.
+  __device__ __forceinline__ int above(int i, int from, int to) const {
+    while (from < to) {
+      const int mid = (from + to) >> 1;
+      if (cu[mid] <= i) from = mid + 1; else to = mid;
     }
-    *d = lo - 1;
-    if (lo == 0 || lo == docs + 1) {
-      *s = *e = clamp(cu[lo == 0 ? 0 : docs]);
+    return from;
+  }
+  __device__ __forceinline__ int above(int i) const { return cu ? above(i, 0, docs + 1) : 0; }
+  // The document before that index as [s, e); false (and an empty range that keeps the order) when there is
+  // none. Bounds are clamped to the sequence whatever the array holds.
+  __device__ __forceinline__ bool document(int index, int* s, int* e) const {
+    if (!cu) { *s = 0; *e = tokens; return true; }
+    if (index == 0 || index == docs + 1) {
+      *s = *e = clamp(cu[index == 0 ? 0 : docs]);
       return false;
     }
-    *s = clamp(cu[lo - 1]);
-    *e = clamp(cu[lo]);
+    *s = clamp(cu[index - 1]);
+    *e = clamp(cu[index]);
     return true;
   }
   __device__ __forceinline__ int clamp(int x) const { return x < 0 ? 0 : x > tokens ? tokens : x; }
-  __device__ __forceinline__ int seen_by_all(int s, int e, int d) const {   // end of the prefix
+  __device__ __forceinline__ int seen_by_all(int s, int e, int index) const {   // end of the prefix
     if (!causal) return e;
     if (!prefix) return s;
-    const int n = prefix[d];
+    const int n = prefix[index - 1];
     return n <= 0 ? s : n >= e - s ? e : s + n;
   }
-  __device__ __forceinline__ void keys_of(int i, int* lo, int* hi) const {
-    int e, d;
-    if (!find(i, lo, &e, &d)) { *hi = *lo; return; }
-    const int all = seen_by_all(*lo, e, d);
+  // The keys that query i sees and the queries that see key j, as [lo, hi), from above(i) or above(j).
+  __device__ __forceinline__ void keys_of(int i, int index, int* lo, int* hi) const {
+    int e;
+    if (!document(index, lo, &e)) { *hi = *lo; return; }
+    const int all = seen_by_all(*lo, e, index);
     *hi = i + 1 > all ? i + 1 : all;
   }
-  __device__ __forceinline__ void queries_of(int j, int* lo, int* hi) const {
-    int s, d;
-    if (!find(j, &s, hi, &d)) { *lo = *hi; return; }
-    *lo = j < seen_by_all(s, *hi, d) ? s : j;
+  __device__ __forceinline__ void queries_of(int j, int index, int* lo, int* hi) const {
+    int s;
+    if (!document(index, &s, hi)) { *lo = *hi; return; }
+    *lo = j < seen_by_all(s, *hi, index) ? s : j;
   }
 #endif
 };

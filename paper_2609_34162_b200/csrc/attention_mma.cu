@@ -21,6 +21,7 @@ constexpr int kHalfBytes = kTile * 128;    // 64 BF16 columns of a tile, as TMA 
 // Eight warps of rows and a warpgroup with the issuer and the producer. Launched with 168 registers per
 // thread (65536 / 384); the row warpgroups then take 216 and the third keeps 72: 2 * 216 + 72 = 3 * 168.
 constexpr int kMmaThreads = 384;
+constexpr int kStageBytes = 4096;          // per warp of rows: 32 rows of 64 BF16 columns, on their way out
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
 constexpr int kTmemColumns = 512;
@@ -169,7 +170,7 @@ struct WorkRing {
 };
 
 // The document offsets, when there are not too many, in shared memory: every row looks its document up there.
-constexpr int kDocCache = 128;
+constexpr int kDocCache = 64;
 struct DocCache {
   int32_t cu[kDocCache + 1], prefix[kDocCache];
   __device__ void fill(const DocMask& m) {   // all threads of the block
@@ -187,6 +188,60 @@ struct DocCache {
     return r;
   }
 };
+
+// How the warp's rows, which see columns [a, b), stand to the 32 columns from c0 on.
+enum ChunkMask { kAllSeen, kRowsSeen, kMixed };   // every row all of them; every row all or none of them; some row a part
+__device__ __forceinline__ ChunkMask chunk_mask(int a, int b, int c0) {
+  const bool all = a <= c0 && b >= c0 + 32, none = a >= c0 + 32 || b <= c0;
+  if (__all_sync(0xffffffffu, all)) return kAllSeen;
+  return __all_sync(0xffffffffu, all || none) ? kRowsSeen : kMixed;
+}
+
+template <typename F>
+__device__ __forceinline__ void by_mask(ChunkMask m, F f) {
+  if (m == kAllSeen) f(std::integral_constant<int, kAllSeen>());
+  else if (m == kRowsSeen) f(std::integral_constant<int, kRowsSeen>());
+  else f(std::integral_constant<int, kMixed>());
+}
+
+// Stores 128 rows, a warp its own 32, of a tile whose row of FP32 values lies in the thread's TMEM lane, as BF16: 64 columns
+// at a time through 4 KB of shared memory per warp, from where TMA writes them (16 bytes per thread straight to global
+// memory touched 32 lines per instruction: 3000 cycles a tile). Returns whether the thread saw a NaN.
+__device__ __forceinline__ bool store_columns(uint32_t stage, const CUtensorMap* map, int head, int row0, int column, int head_dim, int tokens,
+                                              uint32_t from, bool any, float factor) {
+  const int lane = threadIdx.x % 32;
+  if (lane == 0) tma_stores_read();   // the last 64 columns have left the stage
+  __syncwarp();
+  bool nan = false;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    uint32_t o[32];
+    if (any) {
+      tmem_load32(from + c * 32, o);
+      tmem_wait_load();
+      tmem_landed(o);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) o[e] = 0;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float v = __uint_as_float(o[e * 8 + 2 * k]) * factor, w = __uint_as_float(o[e * 8 + 2 * k + 1]) * factor;
+        nan |= column + c * 32 + e * 8 < head_dim && !(v == v && w == w);   // columns past the head hold anything
+        y[k] = pack_bf16(v, w);
+      }
+      const uint32_t at = stage + lane * 128 + (((c * 4 + e) ^ (lane & 7)) << 4);   // the 128-byte swizzle
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+    }
+  }
+  fence_async_proxy();
+  __syncwarp();
+  if (lane == 0 && row0 < tokens) tma_store_3d(map, stage, column, head, row0);
+  return nan && row0 + lane < tokens;
+}
 
 template <int N>
 __device__ __forceinline__ void load_floats(float* y, const float* from) {
@@ -211,12 +266,13 @@ __device__ __forceinline__ void load_floats(float* y, const float* from) {
 template <int HALVES> struct ForwardShape {
   static constexpr int kStages = HALVES == 2 ? 2 : 4;
   static constexpr int kTileBytes = HALVES * kHalfBytes;
-  static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + 1024;
+  static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + 8 * kStageBytes;
 };
 
 struct ForwardPlan {
   int n_lo, steps;           // first key and steps of 128
   int first[2], last[2];     // the steps that concern each tile
+  int above[2][2];           // each tile's first and last row in the document offsets
 };
 
 struct ForwardControl {
@@ -229,18 +285,20 @@ struct ForwardControl {
 template <int HALVES, int MODE>
 __global__ void __launch_bounds__(kMmaThreads, 1)
     attention_forward_mma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
-                                 const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+                                 const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                                 const __grid_constant__ CUtensorMap map_o) {
   using Shape = ForwardShape<HALVES>;
   constexpr int S = Shape::kStages;
-  extern __shared__ uint8_t raw_smem[];
+  extern __shared__ __align__(1024) uint8_t raw_smem[];
   __shared__ ForwardControl ctl;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   const int tiles = (p.tokens + 2 * kTile - 1) / (2 * kTile);
   // item -> head and first query: the last queries see the most keys when causal, so they come first
   const auto head_of = [&](int item) { return item % p.heads_q; };
   const auto row_of = [&](int item) { return (tiles - 1 - item / p.heads_q) * 2 * kTile; };
-  const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
-  const uint32_t smem_q = base, smem_k = base + 2 * Shape::kTileBytes, smem_v = smem_k + S * Shape::kTileBytes;
+  const uint32_t base = smem_addr(raw_smem);
+  const uint32_t smem_q = base, smem_k = base + 2 * Shape::kTileBytes, smem_v = smem_k + S * Shape::kTileBytes,
+                 stages = smem_v + S * Shape::kTileBytes;
   const Waiter wait{&ctl.dead, p.error};
 
   if (threadIdx.x == 0) {
@@ -276,10 +334,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     if (warp == 10) {   // ---- the next tiles
       ctl.work.serve(wait, [&](int item) {
         // lanes 0..3: the keys of each tile's first and last row
-        const int m0 = row_of(item), row = m0 + (lane >> 1) * kTile + (lane & 1 ? kTile - 1 : 0);
-        int lo = 0, hi = 0;
-        if (lane < 4 && m0 + (lane >> 1) * kTile < p.tokens) mask.keys_of(row < p.tokens ? row : p.tokens - 1, &lo, &hi);
+        const int m0 = row_of(item), row = min(m0 + (lane >> 1) * kTile + (lane & 1 ? kTile - 1 : 0), p.tokens - 1);
+        int lo = 0, hi = 0, index = 0;
+        if (lane < 4) {
+          index = mask.above(row);
+          if (m0 + (lane >> 1) * kTile < p.tokens) mask.keys_of(row, index, &lo, &hi);
+        }
         ForwardPlan pl = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pl.above[i >> 1][i & 1] = __shfl_sync(0xffffffffu, index, i);
         const int lo0 = __shfl_sync(0xffffffffu, lo, 0), hi0 = __shfl_sync(0xffffffffu, hi, 1);
         const int lo1 = __shfl_sync(0xffffffffu, lo, 2), hi1 = __shfl_sync(0xffffffffu, hi, 3);
         const bool on0 = lo0 < hi0, on1 = lo1 < hi1;
@@ -395,7 +458,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       const int from = s ? pl.first[1] : pl.first[0], to = s ? pl.last[1] : pl.last[0];
       const ScoreMod<MODE> mod(p, h);
       int lo = 0, hi = 0;
-      if (i < p.tokens) mask.keys_of(i, &lo, &hi);
+      if (i < p.tokens) mask.keys_of(i, mask.above(i, s ? pl.above[1][0] : pl.above[0][0], s ? pl.above[1][1] : pl.above[0][1]), &lo, &hi);
       float m = -INFINITY, l = 0.0f;
       for (int j = from; j < to; ++j, ++turns) {
         ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.s_full[s]), turns & 1));
@@ -414,16 +477,21 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 #pragma unroll
           for (int c = 0; c < 128; ++c) x[c] = __float_as_uint(mod(__uint_as_float(x[c]), d0 - (float)c, &g));
         }
-        // visible columns [a, b); a chunk of 32 is masked value by value only where a row of the warp ends in it. Rows
-        // past the sequence are not stored: they need no mask.
+        // Visible columns [a, b), by chunks of 32. Rows past the sequence are not stored: they need no mask.
         const int a = i < p.tokens ? lo - n0 : 0, b = i < p.tokens ? hi - n0 : kTile;
         if (!__all_sync(0xffffffffu, a <= 0 && b >= kTile)) {
 #pragma unroll
-          for (int c0 = 0; c0 < 128; c0 += 32)
-            if (!__all_sync(0xffffffffu, a <= c0 && b >= c0 + 32)) {
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            const ChunkMask seen = chunk_mask(a, b, c0);
+            if (seen == kRowsSeen) {
+              const bool none = a >= c0 + 32 || b <= c0;
+#pragma unroll
+              for (int c = c0; c < c0 + 32; ++c) x[c] = none ? 0xff800000u : x[c];
+            } else if (seen == kMixed) {
 #pragma unroll
               for (int c = c0; c < c0 + 32; ++c) x[c] = c >= a && c < b ? x[c] : 0xff800000u;
             }
+          }
         }
         float top[4];
 #pragma unroll
@@ -490,37 +558,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       if (!ok) break;
       const bool live = i < p.tokens, some = lo < hi;
       const float inv = some ? 1.0f / l : 0.0f;
-      uint16_t* row = p.o.p + (int64_t)i * p.o.t + h * p.o.h;
+      const int row0 = i - lane;
       bool nan = false;
 #pragma unroll
-      for (int c = 0; c < HALVES * 2; ++c) {
-        uint32_t o[32];
-        if (from < to) {
-          tmem_load32(at_o + c * 32, o);
-          tmem_wait_load();
-          tmem_landed(o);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int d = c * 32 + e * 8;
-          float y[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[e * 8 + k]) * inv;
-          if (live && d < p.head_dim) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) nan |= y[k] != y[k];
-            *reinterpret_cast<uint4*>(row + d) =
-                make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-          }
-        }
-      }
+      for (int c = 0; c < HALVES; ++c)
+        nan |= store_columns(stages + warp * kStageBytes, &map_o, h, row0, c * 64, p.head_dim, p.tokens, at_o + c * 64, from < to, inv);
       if (live) p.lse[(int64_t)h * p.tokens + i] = some ? (m * unit + log2f(l)) * (1.0f / kLog2e) : -INFINITY;
-      for (uint32_t redo = __ballot_sync(0xffffffffu, nan); redo; redo &= redo - 1)
-        attention_out_row(p, i - lane + __ffs(redo) - 1, h, false);   // its lse is right: masked scores are dropped
+      uint32_t redo = __ballot_sync(0xffffffffu, nan);
+      if (redo) {
+        if (lane == 0) tma_stores_done();
+        __syncwarp();
+        for (; redo; redo &= redo - 1) attention_out_row(p, row0 + __ffs(redo) - 1, h, false);   // its lse is right: masked scores are dropped
+      }
     }
+    if (lane == 0) tma_stores_done();
   }
   __syncwarp();
   tc_fence_before();
@@ -543,11 +594,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 template <int HALVES> struct KeysShape {
   static constexpr int kStages = 2;
   static constexpr int kTileBytes = HALVES * kHalfBytes;
-  static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + 1024;
+  static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + 8 * kStageBytes;
 };
 
 struct KeysPlan {
   int q_lo, per_head;   // first tile of queries, tiles of queries per query head
+  int above[2];         // the first and last key in the document offsets
 };
 
 struct KeysControl {
@@ -555,27 +607,27 @@ struct KeysControl {
   DocCache docs;
   alignas(16) float lse[2][kTile];
   alignas(16) float delta[2][kTile];
-  uint64_t kv_full, kv_empty, q_full[2], q_empty[2], do_full[2], do_empty[2], s_full, dp_full, p_ready, ds_ready, acc_full, stored, done;
+  uint64_t kv_full, kv_empty, q_full[2], q_empty[2], do_full[2], do_empty[2], s_full, dp_full, p_ready, ds_ready, acc_full, done;
   uint32_t tmem, dead;
-  uint32_t redo[2][4];   // rows to do again, of this item and the next
 };
 
 template <int HALVES, int MODE>
 __global__ void __launch_bounds__(kMmaThreads, 1)
     attention_dkv_mma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
                              const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                             const __grid_constant__ CUtensorMap map_do) {
+                             const __grid_constant__ CUtensorMap map_do, const __grid_constant__ CUtensorMap map_dk,
+                             const __grid_constant__ CUtensorMap map_dv) {
   using Shape = KeysShape<HALVES>;
   constexpr int S = Shape::kStages;
-  extern __shared__ uint8_t raw_smem[];
+  extern __shared__ __align__(1024) uint8_t raw_smem[];
   __shared__ KeysControl ctl;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   // item -> key head and first key: the first keys are seen by the most queries when causal, so they come first
   const auto head_of = [&](int item) { return item % p.heads_kv; };
   const auto row_of = [&](int item) { return item / p.heads_kv * kTile; };
-  const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
+  const uint32_t base = smem_addr(raw_smem);
   const uint32_t smem_k = base, smem_v = smem_k + Shape::kTileBytes, smem_q = smem_v + Shape::kTileBytes,
-                 smem_do = smem_q + S * Shape::kTileBytes;
+                 smem_do = smem_q + S * Shape::kTileBytes, stages = smem_do + S * Shape::kTileBytes;
   const Waiter wait{&ctl.dead, p.error};
 
   if (threadIdx.x == 0) {
@@ -593,10 +645,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     mbar_init(smem_addr(&ctl.p_ready), 2 * kTile);
     mbar_init(smem_addr(&ctl.ds_ready), 2 * kTile);
     mbar_init(smem_addr(&ctl.acc_full), 1);
-    mbar_init(smem_addr(&ctl.stored), 2 * kTile);
     mbar_init(smem_addr(&ctl.done), 1);
     ctl.dead = 0;
-    for (int i = 0; i < 4; ++i) ctl.redo[0][i] = ctl.redo[1][i] = 0;
     mbar_init_fence();
   }
   ctl.docs.fill(p.mask);
@@ -611,12 +661,16 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     fewer_registers();
     if (warp == 10) {   // ---- the next tiles
       ctl.work.serve(wait, [&](int item) {
-        const int n0 = row_of(item), row = n0 + (lane ? kTile - 1 : 0);   // lanes 0 and 1: first and last key
-        int lo = 0, hi = 0;
-        if (lane < 2) mask.queries_of(row < p.tokens ? row : p.tokens - 1, &lo, &hi);
+        const int row = min(row_of(item) + (lane ? kTile - 1 : 0), p.tokens - 1);   // lanes 0 and 1: first and last key
+        int lo = 0, hi = 0, index = 0;
+        if (lane < 2) {
+          index = mask.above(row);
+          mask.queries_of(row, index, &lo, &hi);
+        }
         lo = __shfl_sync(0xffffffffu, lo, 0);
         hi = __shfl_sync(0xffffffffu, hi, 1);
-        return KeysPlan{lo / kTile, hi > lo ? (hi + kTile - 1) / kTile - lo / kTile : 0};
+        return KeysPlan{lo / kTile, hi > lo ? (hi + kTile - 1) / kTile - lo / kTile : 0,
+                        {__shfl_sync(0xffffffffu, index, 0), __shfl_sync(0xffffffffu, index, 1)}};
       });
     } else if (warp == 9 && lane == 0) {   // ---- producer
       int item, q_sent = 0, sent = 0, walks = 0;
@@ -713,7 +767,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, false); ++n) {
       const int hk = head_of(item), n0 = row_of(item), j = n0 + r + lane, steps = pl.per_head * p.group;
       int lo = 0, hi = 0;
-      if (j < p.tokens) mask.queries_of(j, &lo, &hi);
+      if (j < p.tokens) mask.queries_of(j, mask.above(j, pl.above[0], pl.above[1]), &lo, &hi);
       int h = hk * p.group, tile = 0;
       ScoreMod<MODE> mod(p, h);
       for (int it = 0; it < steps; ++it, ++tile, ++turns) {
@@ -738,12 +792,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tmem_landed(x);
         tmem_landed(x + 32);
         const int a = j < p.tokens ? lo - m0 : 0, b = j < p.tokens ? hi - m0 : 64;   // visible columns [a, b)
-        const bool whole[2] = {(bool)__all_sync(0xffffffffu, a <= 0 && b >= 32), (bool)__all_sync(0xffffffffu, a <= 32 && b >= 64)};
+        const ChunkMask seen[2] = {chunk_mask(a, b, 0), chunk_mask(a, b, 32)};
         float pr[64];   // P (d score / d product)
         {
           uint32_t pk[32];
           const float d0 = (float)(j - m0);
           const auto probabilities = [&](int c0, auto masked) {
+            const bool row = b > c0 && a < c0 + 32;   // where a row sees all or nothing of the chunk
 #pragma unroll
             for (int c = c0; c < c0 + 32; c += 2) {
               float e[2], grad[2] = {1.0f, 1.0f};
@@ -752,7 +807,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
                 if constexpr (MODE != kPlain) e[k] = mod(__uint_as_float(x[c + k]), d0 - (float)(c + k), &grad[k]) - y[c + k];
                 else e[k] = fmaf(__uint_as_float(x[c + k]), p.scale_log2, -y[c + k]);
                 e[k] = exp2_approx(e[k]);
-                if (decltype(masked)::value) e[k] = c + k >= a && c + k < b ? e[k] : 0.0f;
+                if (decltype(masked)::value == kMixed) e[k] = c + k >= a && c + k < b ? e[k] : 0.0f;
+                if (decltype(masked)::value == kRowsSeen) e[k] = row ? e[k] : 0.0f;
                 pr[c + k] = MODE == kCap ? e[k] * grad[k] : e[k];
               }
               pk[c / 2] = pack_bf16(e[0], e[1]);
@@ -760,7 +816,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           };
 #pragma unroll
           for (int half = 0; half < 2; ++half)
-            if (whole[half]) probabilities(half * 32, std::false_type()); else probabilities(half * 32, std::true_type());
+            by_mask(seen[half], [&](auto masked) { probabilities(half * 32, masked); });
           tmem_store32(at_s + at, pk);
         }
         tmem_wait_store();
@@ -779,19 +835,23 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
             tmem_load32(at_dp + at + half * 32, d);
             tmem_wait_load();
             tmem_landed(d);
+            const bool row = b > half * 32 && a < half * 32 + 32;
             const auto gradients = [&](auto masked) {
 #pragma unroll
               for (int c = 0; c < 32; c += 2) {
                 const int n = half * 32 + c;
                 float e0 = pr[n] * (__uint_as_float(d[c]) - y[n]), e1 = pr[n + 1] * (__uint_as_float(d[c + 1]) - y[n + 1]);
-                if (decltype(masked)::value) {   // not zero times what a masked pair holds
+                if (decltype(masked)::value == kMixed) {   // not zero times what a masked pair holds
                   e0 = n >= a && n < b ? e0 : 0.0f;
                   e1 = n + 1 >= a && n + 1 < b ? e1 : 0.0f;
+                } else if (decltype(masked)::value == kRowsSeen) {
+                  e0 = row ? e0 : 0.0f;
+                  e1 = row ? e1 : 0.0f;
                 }
                 pk[n / 2] = pack_bf16(e0, e1);
               }
             };
-            if (whole[half]) gradients(std::false_type()); else gradients(std::true_type());
+            by_mask(seen[half], gradients);
           }
           tmem_store32(at_dp + at, pk);
         }
@@ -803,47 +863,23 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.acc_full), walks++ & 1));
         tc_fence_after();
       }
+      if (!ok) break;
+      // warpgroup 0 stores dV, warpgroup 1 dK
+      const int row0 = j - lane;
+      const uint32_t src = (g ? at_dk : at_dv) + ((uint32_t)r << 16);
       bool nan = false;
-      if (ok) {
-        // warpgroup 0 stores dV, warpgroup 1 dK
-        const AttnView& out = g ? p.dk : p.dv;
-        const uint32_t src = (g ? at_dk : at_dv) + ((uint32_t)r << 16);
-        const float factor = g ? p.scale : 1.0f;
-        uint16_t* row = out.p + (int64_t)j * out.t + hk * out.h;
 #pragma unroll
-        for (int c = 0; c < HALVES * 2; ++c) {
-          uint32_t o[32];
-          if (steps > 0) {
-            tmem_load32(src + c * 32, o);
-            tmem_wait_load();
-            tmem_landed(o);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0;
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int d = c * 32 + e * 8;
-            float y[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[e * 8 + k]) * factor;
-            if (j < p.tokens && d < p.head_dim) {
-#pragma unroll
-              for (int k = 0; k < 8; ++k) nan |= y[k] != y[k];
-              *reinterpret_cast<uint4*>(row + d) =
-                  make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-            }
-          }
-        }
+      for (int c = 0; c < HALVES; ++c)
+        nan |= store_columns(stages + warp * kStageBytes, g ? &map_dk : &map_dv, hk, row0, c * 64, p.head_dim, p.tokens, src + c * 64, steps > 0,
+                             g ? p.scale : 1.0f);
+      uint32_t redo = __ballot_sync(0xffffffffu, nan);
+      if (redo) {
+        if (lane == 0) tma_stores_done();
+        __syncwarp();
+        for (; redo; redo &= redo - 1) attention_dkv_row(p, row0 + __ffs(redo) - 1, hk, g == 1, g == 0);
       }
-      const uint32_t mine = __ballot_sync(0xffffffffu, nan);
-      if (lane == 0 && mine) atomicOr(&ctl.redo[n & 1][warp % 4], mine);
-      if (lane == 0 && g == 0) ctl.redo[n + 1 & 1][warp % 4] = 0;
-      mbar_arrive(smem_addr(&ctl.stored));   // both warpgroups have stored
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.stored), n & 1)) && ok;
-      if (g == 0 && ok)
-        for (uint32_t redo = ctl.redo[n & 1][warp % 4]; redo; redo &= redo - 1) attention_dkv_row(p, n0 + r + __ffs(redo) - 1, hk);
     }
+    if (lane == 0) tma_stores_done();
   }
   __syncwarp();
   tc_fence_before();
@@ -856,39 +892,39 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 // worked on), dP, dQ.
 template <int HALVES> struct QueriesShape {
   static constexpr int kKStages = 3;   // the next step's scores need K beside this step's dS K
-  static constexpr int kVStages = 2;
+  static constexpr int kVStages = HALVES == 2 ? 1 : 2;   // the stores' room; V comes back while the rows work on dP
   static constexpr int kTileBytes = HALVES * kHalfBytes;
-  static constexpr int kSmem = (2 + kKStages + kVStages) * kTileBytes + 1024;
+  static constexpr int kSmem = (2 + kKStages + kVStages) * kTileBytes + 8 * kStageBytes;
 };
 
 struct QueriesPlan {
   int n_lo, steps;   // first key and steps of 128
+  int above[2];      // the first and last query in the document offsets
 };
 
 struct QueriesControl {
   WorkRing<QueriesPlan> work;
   DocCache docs;
-  uint64_t q_full, q_empty, k_full[3], k_empty[3], v_full[2], v_empty[2], s_full[2], dp_full, ds_ready, acc_full, stored, done;
+  uint64_t q_full, q_empty, k_full[3], k_empty[3], v_full[2], v_empty[2], s_full[2], dp_full, ds_ready, acc_full, done;
   uint32_t tmem, dead;
-  uint32_t redo[2][4];
 };
 
 template <int HALVES, int MODE>
 __global__ void __launch_bounds__(kMmaThreads, 1)
     attention_dq_mma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
                             const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                            const __grid_constant__ CUtensorMap map_do) {
+                            const __grid_constant__ CUtensorMap map_do, const __grid_constant__ CUtensorMap map_dq) {
   using Shape = QueriesShape<HALVES>;
   constexpr int SK = Shape::kKStages, SV = Shape::kVStages;
-  extern __shared__ uint8_t raw_smem[];
+  extern __shared__ __align__(1024) uint8_t raw_smem[];
   __shared__ QueriesControl ctl;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
   const int tiles = (p.tokens + kTile - 1) / kTile;
   const auto head_of = [&](int item) { return item % p.heads_q; };
   const auto row_of = [&](int item) { return (tiles - 1 - item / p.heads_q) * kTile; };
-  const uint32_t base = (smem_addr(raw_smem) + 1023u) & ~1023u;
+  const uint32_t base = smem_addr(raw_smem);
   const uint32_t smem_q = base, smem_do = smem_q + Shape::kTileBytes, smem_k = smem_do + Shape::kTileBytes,
-                 smem_v = smem_k + SK * Shape::kTileBytes;
+                 smem_v = smem_k + SK * Shape::kTileBytes, stages = smem_v + SV * Shape::kTileBytes;
   const Waiter wait{&ctl.dead, p.error};
 
   if (threadIdx.x == 0) {
@@ -907,10 +943,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     mbar_init(smem_addr(&ctl.dp_full), 1);
     mbar_init(smem_addr(&ctl.ds_ready), 2 * kTile);
     mbar_init(smem_addr(&ctl.acc_full), 1);
-    mbar_init(smem_addr(&ctl.stored), 2 * kTile);
     mbar_init(smem_addr(&ctl.done), 1);
     ctl.dead = 0;
-    for (int i = 0; i < 4; ++i) ctl.redo[0][i] = ctl.redo[1][i] = 0;
     mbar_init_fence();
   }
   ctl.docs.fill(p.mask);
@@ -925,12 +959,16 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     fewer_registers();
     if (warp == 10) {   // ---- the next tiles
       ctl.work.serve(wait, [&](int item) {
-        const int m0 = row_of(item), row = m0 + (lane ? kTile - 1 : 0);   // lanes 0 and 1: first and last query
-        int lo = 0, hi = 0;
-        if (lane < 2) mask.keys_of(row < p.tokens ? row : p.tokens - 1, &lo, &hi);
+        const int row = min(row_of(item) + (lane ? kTile - 1 : 0), p.tokens - 1);   // lanes 0 and 1: first and last query
+        int lo = 0, hi = 0, index = 0;
+        if (lane < 2) {
+          index = mask.above(row);
+          mask.keys_of(row, index, &lo, &hi);
+        }
         lo = __shfl_sync(0xffffffffu, lo, 0);
         hi = __shfl_sync(0xffffffffu, hi, 1);
-        return QueriesPlan{lo, hi > lo ? (hi - lo + kTile - 1) / kTile : 0};
+        return QueriesPlan{lo, hi > lo ? (hi - lo + kTile - 1) / kTile : 0,
+                           {__shfl_sync(0xffffffffu, index, 0), __shfl_sync(0xffffffffu, index, 1)}};
       });
     } else if (warp == 9 && lane == 0) {   // ---- producer
       int item, k_sent = 0, sent = 0, walks = 0;
@@ -1021,7 +1059,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       int lo = 0, hi = 0;
       float lse = 0.0f, delta = 0.0f;
       if (i < p.tokens) {
-        mask.keys_of(i, &lo, &hi);
+        mask.keys_of(i, mask.above(i, pl.above[0], pl.above[1]), &lo, &hi);
         lse = p.row_lse[h * p.pitch + i];
         delta = p.row_delta[h * p.pitch + i];
       }
@@ -1038,7 +1076,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tmem_landed(x);
         tmem_landed(x + 32);
         const int a = i < p.tokens ? lo - c0 : 0, b = i < p.tokens ? hi - c0 : 64;   // visible columns [a, b)
-        const bool whole[2] = {(bool)__all_sync(0xffffffffu, a <= 0 && b >= 32), (bool)__all_sync(0xffffffffu, a <= 32 && b >= 64)};
+        const ChunkMask seen[2] = {chunk_mask(a, b, 0), chunk_mask(a, b, 32)};
         float pr[64];
 #pragma unroll
         for (int c = 0; c < 64; ++c) {
@@ -1057,20 +1095,24 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tmem_landed(x + 32);
         uint32_t pk[32];
         const auto gradients = [&](int half, auto masked) {
+          const bool row = b > half * 32 && a < half * 32 + 32;   // where a row sees all or nothing of the chunk
 #pragma unroll
           for (int c = half * 16; c < half * 16 + 16; ++c) {
             float e0 = pr[2 * c] * (__uint_as_float(x[2 * c]) - delta);
             float e1 = pr[2 * c + 1] * (__uint_as_float(x[2 * c + 1]) - delta);
-            if (decltype(masked)::value) {
+            if (decltype(masked)::value == kMixed) {   // not zero times what a masked pair holds
               e0 = 2 * c >= a && 2 * c < b ? e0 : 0.0f;
               e1 = 2 * c + 1 >= a && 2 * c + 1 < b ? e1 : 0.0f;
+            } else if (decltype(masked)::value == kRowsSeen) {
+              e0 = row ? e0 : 0.0f;
+              e1 = row ? e1 : 0.0f;
             }
             pk[c] = pack_bf16(e0, e1);
           }
         };
 #pragma unroll
         for (int half = 0; half < 2; ++half)
-          if (whole[half]) gradients(half, std::false_type()); else gradients(half, std::true_type());
+          by_mask(seen[half], [&](auto masked) { gradients(half, masked); });
         tmem_store32(buf, pk);
         tmem_wait_store();
         tc_fence_before();
@@ -1080,44 +1122,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.acc_full), walks++ & 1));
         tc_fence_after();
       }
-      bool nan = false;
-      if (ok) {
-        uint16_t* row = p.dq.p + (int64_t)i * p.dq.t + h * p.dq.h;
-#pragma unroll
-        for (int c = 0; c < HALVES; ++c) {   // the warpgroups store half of the columns each
-          const int d0 = g * HALVES * 32 + c * 32;
-          uint32_t o[32];
-          if (steps > 0) {
-            tmem_load32(at_dq + ((uint32_t)r << 16) + d0, o);
-            tmem_wait_load();
-            tmem_landed(o);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0;
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int d = d0 + e * 8;
-            float y[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[e * 8 + k]) * p.scale;
-            if (i < p.tokens && d < p.head_dim) {
-#pragma unroll
-              for (int k = 0; k < 8; ++k) nan |= y[k] != y[k];
-              *reinterpret_cast<uint4*>(row + d) =
-                  make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-            }
-          }
+      if (!ok) break;
+      if (g < HALVES) {   // a warpgroup stores 64 columns
+        const int row0 = i - lane;
+        const bool nan = store_columns(stages + warp * kStageBytes, &map_dq, h, row0, g * 64, p.head_dim, p.tokens,
+                                       at_dq + ((uint32_t)r << 16) + g * 64, steps > 0, p.scale);
+        uint32_t redo = __ballot_sync(0xffffffffu, nan);
+        if (redo) {
+          if (lane == 0) tma_stores_done();
+          __syncwarp();
+          for (; redo; redo &= redo - 1) attention_dq_row(p, row0 + __ffs(redo) - 1, h, g * 64, min(g * 64 + 64, p.head_dim));
         }
       }
-      const uint32_t mine = __ballot_sync(0xffffffffu, nan);
-      if (lane == 0 && mine) atomicOr(&ctl.redo[n & 1][warp % 4], mine);
-      if (lane == 0 && g == 0) ctl.redo[n + 1 & 1][warp % 4] = 0;
-      mbar_arrive(smem_addr(&ctl.stored));
-      ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.stored), n & 1)) && ok;
-      if (g == 0 && ok)
-        for (uint32_t redo = ctl.redo[n & 1][warp % 4]; redo; redo &= redo - 1) attention_dq_row(p, m0 + r + __ffs(redo) - 1, h);
     }
+    if (lane == 0) tma_stores_done();
   }
   __syncwarp();
   tc_fence_before();
@@ -1146,14 +1164,14 @@ static EncodeTiled encode_tiled() {
   return reinterpret_cast<EncodeTiled>(f);
 }
 
-// A view as (value, head, token) with boxes of 64 values of 128 tokens of one head; zeros outside.
-static bool make_map(CUtensorMap* map, const AttnView& v, const AttnParams& p, int heads) {
+// A view as (value, head, token) with boxes of 64 values of `rows` tokens of one head; zeros are read outside.
+static bool make_map(CUtensorMap* map, const AttnView& v, const AttnParams& p, int heads, int rows = kTile) {
   const EncodeTiled encode = encode_tiled();
   if (!encode) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)p.head_dim, (cuuint64_t)heads, (cuuint64_t)p.tokens};
   // the stride of an axis of one entry is not used, but must be valid
   const cuuint64_t strides[2] = {(cuuint64_t)(heads > 1 ? v.h * 2 : p.head_dim * 2), (cuuint64_t)(p.tokens > 1 ? v.t * 2 : p.head_dim * 2)};
-  const cuuint32_t box[3] = {64, 1, (cuuint32_t)kTile}, ones[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, 1, (cuuint32_t)rows}, ones[3] = {1, 1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, v.p, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -1173,13 +1191,14 @@ static int score_mode(const AttnParams& p) { return p.softcap > 0.0f ? kCap : p.
 template <int HALVES, int MODE>
 static int forward(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
   static std::atomic<uint64_t> ready{0};
-  CUtensorMap q, k, v;
-  if (!make_map(&q, p.q, p, p.heads_q) || !make_map(&k, p.k, p, p.heads_kv) || !make_map(&v, p.v, p, p.heads_kv))
+  CUtensorMap q, k, v, o;
+  if (!make_map(&q, p.q, p, p.heads_q) || !make_map(&k, p.k, p, p.heads_kv) || !make_map(&v, p.v, p, p.heads_kv) ||
+      !make_map(&o, p.o, p, p.heads_q, 32))
     return SLIDEDP_ERR_CUDA;
   CU(allow_smem(attention_forward_mma_kernel<HALVES, MODE>, ForwardShape<HALVES>::kSmem, &ready, ctx->device));
   const int64_t blocks = (int64_t)((p.tokens + 2 * kTile - 1) / (2 * kTile)) * p.heads_q;
   if (blocks > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
-  attention_forward_mma_kernel<HALVES, MODE><<<(unsigned)blocks, kMmaThreads, ForwardShape<HALVES>::kSmem, st>>>(p, q, k, v);
+  attention_forward_mma_kernel<HALVES, MODE><<<(unsigned)blocks, kMmaThreads, ForwardShape<HALVES>::kSmem, st>>>(p, q, k, v, o);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;
@@ -1188,20 +1207,21 @@ static int forward(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
 template <int HALVES, int MODE>
 static int backward(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
   static std::atomic<uint64_t> ready_q{0}, ready_k{0};
-  CUtensorMap q, k, v, d;
+  CUtensorMap q, k, v, d, dq, dk, dv;
   if (!make_map(&q, p.q, p, p.heads_q) || !make_map(&k, p.k, p, p.heads_kv) || !make_map(&v, p.v, p, p.heads_kv) ||
-      !make_map(&d, p.dout, p, p.heads_q))
+      !make_map(&d, p.dout, p, p.heads_q) || !make_map(&dq, p.dq, p, p.heads_q, 32) || !make_map(&dk, p.dk, p, p.heads_kv, 32) ||
+      !make_map(&dv, p.dv, p, p.heads_kv, 32))
     return SLIDEDP_ERR_CUDA;
   CU(allow_smem(attention_dkv_mma_kernel<HALVES, MODE>, KeysShape<HALVES>::kSmem, &ready_k, ctx->device));
   CU(allow_smem(attention_dq_mma_kernel<HALVES, MODE>, QueriesShape<HALVES>::kSmem, &ready_q, ctx->device));
   const int64_t tiles = (p.tokens + kTile - 1) / kTile;
   if (tiles * p.heads_q > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
   FAULT_POINT();
-  attention_dkv_mma_kernel<HALVES, MODE><<<(unsigned)(tiles * p.heads_kv), kMmaThreads, KeysShape<HALVES>::kSmem, st>>>(p, q, k, v, d);
+  attention_dkv_mma_kernel<HALVES, MODE><<<(unsigned)(tiles * p.heads_kv), kMmaThreads, KeysShape<HALVES>::kSmem, st>>>(p, q, k, v, d, dk, dv);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   FAULT_POINT();
-  attention_dq_mma_kernel<HALVES, MODE><<<(unsigned)(tiles * p.heads_q), kMmaThreads, QueriesShape<HALVES>::kSmem, st>>>(p, q, k, v, d);
+  attention_dq_mma_kernel<HALVES, MODE><<<(unsigned)(tiles * p.heads_q), kMmaThreads, QueriesShape<HALVES>::kSmem, st>>>(p, q, k, v, d, dq);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;

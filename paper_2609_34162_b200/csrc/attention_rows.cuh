@@ -22,12 +22,12 @@ __device__ __forceinline__ void load_row(const AttnView& v, int t, int h, int n,
 #pragma unroll
   for (int i = 0; i < kMaxPer; ++i) x[i] = lane + i * kLanes < n ? load_bf16(row + lane + i * kLanes) : 0.0f;
 }
-__device__ __forceinline__ void store_row(const AttnView& v, int t, int h, int n, const float* x) {
+__device__ __forceinline__ void store_row(const AttnView& v, int t, int h, int from, int to, const float* x) {
   uint16_t* row = v.p + t * v.t + h * v.h;
   const int lane = threadIdx.x % kLanes;
 #pragma unroll
   for (int i = 0; i < kMaxPer; ++i)
-    if (lane + i * kLanes < n) row[lane + i * kLanes] = (uint16_t)f32_to_bf16_bits(x[i]);
+    if (lane + i * kLanes >= from && lane + i * kLanes < to) row[lane + i * kLanes] = (uint16_t)f32_to_bf16_bits(x[i]);
 }
 __device__ __forceinline__ float dot(const float* a, const float* b) {
   float s = 0.0f;
@@ -56,7 +56,7 @@ static __device__ __noinline__ void attention_out_row(const AttnParams& p, int i
   float q[kMaxPer], o[kMaxPer] = {};
   load_row(p.q, i, h, p.head_dim, q);
   int lo, hi;
-  p.mask.keys_of(i, &lo, &hi);
+  p.mask.keys_of(i, p.mask.above(i), &lo, &hi);
   float m = -INFINITY, l = 0.0f;
   for (int j = lo; j < hi; ++j) {
     float x[kMaxPer], g;
@@ -72,11 +72,12 @@ static __device__ __noinline__ void attention_out_row(const AttnParams& p, int i
   const float inv = lo < hi ? 1.0f / l : 0.0f;
 #pragma unroll
   for (int d = 0; d < kMaxPer; ++d) o[d] *= inv;
-  store_row(p.o, i, h, p.head_dim, o);
+  store_row(p.o, i, h, 0, p.head_dim, o);
   if (with_lse && threadIdx.x % kLanes == 0) p.lse[(int64_t)h * p.tokens + i] = lo < hi ? (m + log2f(l)) / kLog2e : -INFINITY;
 }
 
-static __device__ __noinline__ void attention_dq_row(const AttnParams& p, int i, int h) {
+// dq's values [from, to) are stored.
+static __device__ __noinline__ void attention_dq_row(const AttnParams& p, int i, int h, int from, int to) {
   const int hk = h / p.group;
   const float slope = p.slopes ? p.slopes[h] : 0.0f;
   float q[kMaxPer], go[kMaxPer], dq[kMaxPer] = {};
@@ -84,7 +85,7 @@ static __device__ __noinline__ void attention_dq_row(const AttnParams& p, int i,
   load_row(p.dout, i, h, p.head_dim, go);
   const float lse = p.row_lse[h * p.pitch + i], delta = p.row_delta[h * p.pitch + i];
   int lo, hi;
-  p.mask.keys_of(i, &lo, &hi);
+  p.mask.keys_of(i, p.mask.above(i), &lo, &hi);
   for (int j = lo; j < hi; ++j) {
     float k[kMaxPer], v[kMaxPer], g;
     load_row(p.k, j, hk, p.head_dim, k);
@@ -94,15 +95,15 @@ static __device__ __noinline__ void attention_dq_row(const AttnParams& p, int i,
 #pragma unroll
     for (int d = 0; d < kMaxPer; ++d) dq[d] = fmaf(ds, k[d], dq[d]);
   }
-  store_row(p.dq, i, h, p.head_dim, dq);
+  store_row(p.dq, i, h, from, to, dq);
 }
 
-static __device__ __noinline__ void attention_dkv_row(const AttnParams& p, int j, int hk) {
+static __device__ __noinline__ void attention_dkv_row(const AttnParams& p, int j, int hk, bool with_dk, bool with_dv) {
   float k[kMaxPer], v[kMaxPer], dk[kMaxPer] = {}, dv[kMaxPer] = {};
   load_row(p.k, j, hk, p.head_dim, k);
   load_row(p.v, j, hk, p.head_dim, v);
   int lo, hi;
-  p.mask.queries_of(j, &lo, &hi);
+  p.mask.queries_of(j, p.mask.above(j), &lo, &hi);
   for (int h = hk * p.group; h < (hk + 1) * p.group; ++h) {
     const float slope = p.slopes ? p.slopes[h] : 0.0f;
     for (int i = lo; i < hi; ++i) {
@@ -118,8 +119,8 @@ static __device__ __noinline__ void attention_dkv_row(const AttnParams& p, int j
       }
     }
   }
-  store_row(p.dk, j, hk, p.head_dim, dk);
-  store_row(p.dv, j, hk, p.head_dim, dv);
+  if (with_dk) store_row(p.dk, j, hk, 0, p.head_dim, dk);
+  if (with_dv) store_row(p.dv, j, hk, 0, p.head_dim, dv);
 }
 
 }  // namespace slidedp
