@@ -102,14 +102,13 @@ struct WorkRing {
   uint64_t answered, full[2], empty[2], ask;
   Plan plan[2];
   int item[2];   // -1: no more
-  static constexpr int kReaders = 10;   // warps of rows, the issuer, the producer
   static constexpr uint32_t kNap = 100;
-  __device__ void init() {   // one thread
+  __device__ void init(int readers) {   // one thread; readers: the warps that take items from the ring
     mbar_init(smem_addr(&answered), 1);
     mbar_init(smem_addr(&ask), 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_addr(&full[i]), 1);
-      mbar_init(smem_addr(&empty[i]), kReaders);
+      mbar_init(smem_addr(&empty[i]), readers);
     }
   }
   // The n-th item, for all threads of a reading warp (or for the one thread `alone`).
@@ -132,10 +131,11 @@ struct WorkRing {
     if (alone || threadIdx.x % 32 == 0) mbar_arrive(smem_addr(&empty[slot]));
     return *it >= 0;
   }
-  // The producer, when it has sent for all of an item: only now is the next one taken, while the last steps and the
-  // stores are still to come. (Taken a whole item ahead, the long items of a causal walk ended up two to a block:
+  // The producer, kAhead steps before it has sent for all of an item: only now is the next one taken, while the last steps
+  // and the stores are still to come. (Taken a whole item ahead, the long items of a causal walk ended up two to a block:
   // keys' gradients of one document of 8192 tokens 1035 us.)
-  __device__ __forceinline__ void sent_all() { mbar_arrive(smem_addr(&ask)); }
+  __device__ __forceinline__ void take_next() { mbar_arrive(smem_addr(&ask)); }
+  static constexpr int kAhead = 4;
   // The asking warp: make(item) returns the item's plan (in every lane).
   template <typename F>
   __device__ __forceinline__ void serve(const Waiter& wait, F make) {
@@ -189,19 +189,10 @@ struct DocCache {
   }
 };
 
-// How the warp's rows, which see columns [a, b), stand to the 32 columns from c0 on.
-enum ChunkMask { kAllSeen, kRowsSeen, kMixed };   // every row all of them; every row all or none of them; some row a part
-__device__ __forceinline__ ChunkMask chunk_mask(int a, int b, int c0) {
-  const bool all = a <= c0 && b >= c0 + 32, none = a >= c0 + 32 || b <= c0;
-  if (__all_sync(0xffffffffu, all)) return kAllSeen;
-  return __all_sync(0xffffffffu, all || none) ? kRowsSeen : kMixed;
-}
-
-template <typename F>
-__device__ __forceinline__ void by_mask(ChunkMask m, F f) {
-  if (m == kAllSeen) f(std::integral_constant<int, kAllSeen>());
-  else if (m == kRowsSeen) f(std::integral_constant<int, kRowsSeen>());
-  else f(std::integral_constant<int, kMixed>());
+// The columns [a, b) that a row sees, as bits of the 32 columns from c0 on.
+__device__ __forceinline__ uint32_t seen_bits(int a, int b, int c0) {
+  const auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
+  return below(b - c0) & ~below(a - c0);
 }
 
 // Stores 128 rows, a warp its own 32, of a tile whose row of FP32 values lies in the thread's TMEM lane, as BF16: 64 columns
@@ -259,8 +250,8 @@ __device__ __forceinline__ void load_floats(float* y, const float* from) {
 //
 // An item is 256 queries of one head as two tiles of 128 (one per row warpgroup), for which the block walks the keys
 // they see in steps of 128. TMEM: scores of the tiles (128 columns each, overwritten by their BF16
-// probabilities) and their outputs. The issuer alternates between the tiles, so that one's products run
-// while the other's warpgroup exponentiates. A row's accumulators are rescaled only when its
+// probabilities) and their outputs. The issuer alternates between the tiles, so that one's products
+// run while the other's warpgroup exponentiates. A row's accumulators are rescaled only when its
 // maximum has grown by more than 2^8 since the last time.
 
 template <int HALVES> struct ForwardShape {
@@ -302,7 +293,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const Waiter wait{&ctl.dead, p.error};
 
   if (threadIdx.x == 0) {
-    ctl.work.init();
+    ctl.work.init(10);   // eight of rows, the issuer, the producer
     mbar_init(smem_addr(&ctl.q_full), 1);
     mbar_init(smem_addr(&ctl.q_empty), 1);
     for (int i = 0; i < S; ++i) {
@@ -361,7 +352,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       ForwardPlan pl;
       for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, true); ++n) {
         if (pl.steps == 0) {
-          ctl.work.sent_all();
+          ctl.work.take_next();
           continue;
         }
         const int h = head_of(item), hk = h / p.group, m0 = row_of(item);
@@ -373,6 +364,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
             load_tile<HALVES>(smem_q + s * Shape::kTileBytes, &map_q, h, m0 + s * kTile, smem_addr(&ctl.q_full));
         ++walks;
         for (int j = 0; j < pl.steps; ++j, ++sent) {
+          if (j == max(pl.steps - ctl.work.kAhead, 0)) ctl.work.take_next();
           const int st = sent % S;
           const uint32_t turn = (uint32_t)(sent / S + 1) & 1;   // parity of the previous use's release
           if (sent >= S && !(ok = wait(smem_addr(&ctl.k_empty[st]), turn))) break;
@@ -383,7 +375,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           mbar_expect(smem_addr(&ctl.v_full[st]), Shape::kTileBytes);
           load_tile<HALVES>(smem_v + st * Shape::kTileBytes, &map_v, hk, pl.n_lo + j * kTile, smem_addr(&ctl.v_full[st]));
         }
-        if (ok) ctl.work.sent_all();
       }
       if (ctl.dead) {   // leave no copy in flight
         if (walks > 0) drain(smem_addr(&ctl.q_full), walks - 1 & 1);
@@ -402,6 +393,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         if (pl.steps == 0) continue;
         if (!(ok = wait_all(smem_addr(&ctl.q_full), walks & 1))) break;
         ++walks;
+        // Strictly in turn, so that the tiles stay half a period out of step, one on the tensor cores while the other is on
+        // the special functions. (Serving whichever is ready first let the tiles fall into step: one document of 8192
+        // tokens 540 us instead of 440.)
         for (int j = -1; j < pl.steps; ++j) {
           // products of step j's probabilities, and step j + 1's scores
           const int at = done + j, st = at % S, nx = (at + 1) % S;
@@ -477,20 +471,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 #pragma unroll
           for (int c = 0; c < 128; ++c) x[c] = __float_as_uint(mod(__uint_as_float(x[c]), d0 - (float)c, &g));
         }
-        // Visible columns [a, b), by chunks of 32. Rows past the sequence are not stored: they need no mask.
+        // Visible columns [a, b). Rows past the sequence are not stored: they need no mask.
         const int a = i < p.tokens ? lo - n0 : 0, b = i < p.tokens ? hi - n0 : kTile;
         if (!__all_sync(0xffffffffu, a <= 0 && b >= kTile)) {
 #pragma unroll
           for (int c0 = 0; c0 < 128; c0 += 32) {
-            const ChunkMask seen = chunk_mask(a, b, c0);
-            if (seen == kRowsSeen) {
-              const bool none = a >= c0 + 32 || b <= c0;
+            const uint32_t seen = seen_bits(a, b, c0);
 #pragma unroll
-              for (int c = c0; c < c0 + 32; ++c) x[c] = none ? 0xff800000u : x[c];
-            } else if (seen == kMixed) {
-#pragma unroll
-              for (int c = c0; c < c0 + 32; ++c) x[c] = c >= a && c < b ? x[c] : 0xff800000u;
-            }
+            for (int c = 0; c < 32; ++c) x[c0 + c] = seen >> c & 1 ? x[c0 + c] : 0xff800000u;
           }
         }
         float top[4];
@@ -631,7 +619,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const Waiter wait{&ctl.dead, p.error};
 
   if (threadIdx.x == 0) {
-    ctl.work.init();
+    ctl.work.init(10);   // eight of rows, the issuer, the producer
     mbar_init(smem_addr(&ctl.kv_full), 1);
     mbar_init(smem_addr(&ctl.kv_empty), 1);
     for (int i = 0; i < S; ++i) {
@@ -678,7 +666,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       KeysPlan pl;
       for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, true); ++n) {
         if (pl.per_head == 0) {
-          ctl.work.sent_all();
+          ctl.work.take_next();
           continue;
         }
         const int hk = head_of(item), n0 = row_of(item);
@@ -687,8 +675,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         load_tile<HALVES>(smem_k, &map_k, hk, n0, smem_addr(&ctl.kv_full));
         load_tile<HALVES>(smem_v, &map_v, hk, n0, smem_addr(&ctl.kv_full));
         ++walks;
+        int left = pl.per_head * p.group;
         for (int h = hk * p.group; h < (hk + 1) * p.group && ok; ++h)
-          for (int tile = 0; tile < pl.per_head; ++tile, ++sent) {
+          for (int tile = 0; tile < pl.per_head; ++tile, ++sent, --left) {
+            if (left == min(pl.per_head * p.group, ctl.work.kAhead)) ctl.work.take_next();
             const int st = sent % S, m0 = (pl.q_lo + tile) * kTile;
             const uint32_t turn = (uint32_t)(sent / S + 1) & 1;
             if (sent >= S && !(ok = wait(smem_addr(&ctl.q_empty[st]), turn))) break;
@@ -701,7 +691,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
             mbar_expect(smem_addr(&ctl.do_full[st]), Shape::kTileBytes);
             load_tile<HALVES>(smem_do + st * Shape::kTileBytes, &map_do, h, m0, smem_addr(&ctl.do_full[st]));
           }
-        if (ok) ctl.work.sent_all();
       }
       if (ctl.dead) {
         if (walks > 0) drain(smem_addr(&ctl.kv_full), walks - 1 & 1);
@@ -792,31 +781,28 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tmem_landed(x);
         tmem_landed(x + 32);
         const int a = j < p.tokens ? lo - m0 : 0, b = j < p.tokens ? hi - m0 : 64;   // visible columns [a, b)
-        const ChunkMask seen[2] = {chunk_mask(a, b, 0), chunk_mask(a, b, 32)};
+        const bool whole = __all_sync(0xffffffffu, a <= 0 && b >= 64);
+        const uint32_t seen[2] = {seen_bits(a, b, 0), seen_bits(a, b, 32)};
         float pr[64];   // P (d score / d product)
         {
           uint32_t pk[32];
           const float d0 = (float)(j - m0);
-          const auto probabilities = [&](int c0, auto masked) {
-            const bool row = b > c0 && a < c0 + 32;   // where a row sees all or nothing of the chunk
+          const auto probabilities = [&](auto masked) {
 #pragma unroll
-            for (int c = c0; c < c0 + 32; c += 2) {
+            for (int c = 0; c < 64; c += 2) {
               float e[2], grad[2] = {1.0f, 1.0f};
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
                 if constexpr (MODE != kPlain) e[k] = mod(__uint_as_float(x[c + k]), d0 - (float)(c + k), &grad[k]) - y[c + k];
                 else e[k] = fmaf(__uint_as_float(x[c + k]), p.scale_log2, -y[c + k]);
                 e[k] = exp2_approx(e[k]);
-                if (decltype(masked)::value == kMixed) e[k] = c + k >= a && c + k < b ? e[k] : 0.0f;
-                if (decltype(masked)::value == kRowsSeen) e[k] = row ? e[k] : 0.0f;
+                if (decltype(masked)::value) e[k] = seen[c / 32] >> (c % 32 + k) & 1 ? e[k] : 0.0f;
                 pr[c + k] = MODE == kCap ? e[k] * grad[k] : e[k];
               }
               pk[c / 2] = pack_bf16(e[0], e[1]);
             }
           };
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-            by_mask(seen[half], [&](auto masked) { probabilities(half * 32, masked); });
+          if (whole) probabilities(std::false_type()); else probabilities(std::true_type());
           tmem_store32(at_s + at, pk);
         }
         tmem_wait_store();
@@ -835,23 +821,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
             tmem_load32(at_dp + at + half * 32, d);
             tmem_wait_load();
             tmem_landed(d);
-            const bool row = b > half * 32 && a < half * 32 + 32;
             const auto gradients = [&](auto masked) {
 #pragma unroll
               for (int c = 0; c < 32; c += 2) {
                 const int n = half * 32 + c;
                 float e0 = pr[n] * (__uint_as_float(d[c]) - y[n]), e1 = pr[n + 1] * (__uint_as_float(d[c + 1]) - y[n + 1]);
-                if (decltype(masked)::value == kMixed) {   // not zero times what a masked pair holds
-                  e0 = n >= a && n < b ? e0 : 0.0f;
-                  e1 = n + 1 >= a && n + 1 < b ? e1 : 0.0f;
-                } else if (decltype(masked)::value == kRowsSeen) {
-                  e0 = row ? e0 : 0.0f;
-                  e1 = row ? e1 : 0.0f;
+                if (decltype(masked)::value) {   // not zero times what a masked pair holds
+                  e0 = seen[half] >> c & 1 ? e0 : 0.0f;
+                  e1 = seen[half] >> (c + 1) & 1 ? e1 : 0.0f;
                 }
                 pk[n / 2] = pack_bf16(e0, e1);
               }
             };
-            by_mask(seen[half], gradients);
+            if (whole) gradients(std::false_type()); else gradients(std::true_type());
           }
           tmem_store32(at_dp + at, pk);
         }
@@ -928,7 +910,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const Waiter wait{&ctl.dead, p.error};
 
   if (threadIdx.x == 0) {
-    ctl.work.init();
+    ctl.work.init(10);
     mbar_init(smem_addr(&ctl.q_full), 1);
     mbar_init(smem_addr(&ctl.q_empty), 1);
     for (int i = 0; i < SK; ++i) {
@@ -976,7 +958,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       QueriesPlan pl;
       for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, true); ++n) {
         if (pl.steps == 0) {
-          ctl.work.sent_all();
+          ctl.work.take_next();
           continue;
         }
         const int h = head_of(item), hk = h / p.group, m0 = row_of(item);
@@ -986,6 +968,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         load_tile<HALVES>(smem_do, &map_do, h, m0, smem_addr(&ctl.q_full));
         ++walks;
         for (int j = 0; j < pl.steps; ++j, ++sent) {
+          if (j == max(pl.steps - ctl.work.kAhead, 0)) ctl.work.take_next();
           const int sk = sent % SK, sv = sent % SV;
           if (sent >= SK && !(ok = wait(smem_addr(&ctl.k_empty[sk]), (uint32_t)(sent / SK + 1) & 1))) break;
           mbar_expect(smem_addr(&ctl.k_full[sk]), Shape::kTileBytes);
@@ -995,7 +978,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           mbar_expect(smem_addr(&ctl.v_full[sv]), Shape::kTileBytes);
           load_tile<HALVES>(smem_v + sv * Shape::kTileBytes, &map_v, hk, pl.n_lo + j * kTile, smem_addr(&ctl.v_full[sv]));
         }
-        if (ok) ctl.work.sent_all();
       }
       if (ctl.dead) {
         if (walks > 0) drain(smem_addr(&ctl.q_full), walks - 1 & 1);
@@ -1076,7 +1058,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tmem_landed(x);
         tmem_landed(x + 32);
         const int a = i < p.tokens ? lo - c0 : 0, b = i < p.tokens ? hi - c0 : 64;   // visible columns [a, b)
-        const ChunkMask seen[2] = {chunk_mask(a, b, 0), chunk_mask(a, b, 32)};
+        const bool whole = __all_sync(0xffffffffu, a <= 0 && b >= 64);
+        const uint32_t seen[2] = {seen_bits(a, b, 0), seen_bits(a, b, 32)};
         float pr[64];
 #pragma unroll
         for (int c = 0; c < 64; ++c) {
@@ -1094,25 +1077,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tmem_landed(x);
         tmem_landed(x + 32);
         uint32_t pk[32];
-        const auto gradients = [&](int half, auto masked) {
-          const bool row = b > half * 32 && a < half * 32 + 32;   // where a row sees all or nothing of the chunk
+        const auto gradients = [&](auto masked) {
 #pragma unroll
-          for (int c = half * 16; c < half * 16 + 16; ++c) {
-            float e0 = pr[2 * c] * (__uint_as_float(x[2 * c]) - delta);
-            float e1 = pr[2 * c + 1] * (__uint_as_float(x[2 * c + 1]) - delta);
-            if (decltype(masked)::value == kMixed) {   // not zero times what a masked pair holds
-              e0 = 2 * c >= a && 2 * c < b ? e0 : 0.0f;
-              e1 = 2 * c + 1 >= a && 2 * c + 1 < b ? e1 : 0.0f;
-            } else if (decltype(masked)::value == kRowsSeen) {
-              e0 = row ? e0 : 0.0f;
-              e1 = row ? e1 : 0.0f;
+          for (int c = 0; c < 64; c += 2) {
+            float e0 = pr[c] * (__uint_as_float(x[c]) - delta), e1 = pr[c + 1] * (__uint_as_float(x[c + 1]) - delta);
+            if (decltype(masked)::value) {   // not zero times what a masked pair holds
+              e0 = seen[c / 32] >> (c % 32) & 1 ? e0 : 0.0f;
+              e1 = seen[c / 32] >> (c % 32 + 1) & 1 ? e1 : 0.0f;
             }
-            pk[c] = pack_bf16(e0, e1);
+            pk[c / 2] = pack_bf16(e0, e1);
           }
         };
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-          by_mask(seen[half], [&](auto masked) { gradients(half, masked); });
+        if (whole) gradients(std::false_type()); else gradients(std::true_type());
         tmem_store32(buf, pk);
         tmem_wait_store();
         tc_fence_before();
