@@ -240,19 +240,25 @@ def _refuse(x, what: str, dtype, shape):
     raise ValueError(f"{what} must be contiguous")
 
 
+# The library sees addresses only; these look at what it cannot: type, shape, device and layout. They run once or
+# more per argument of every call, and are written to touch each property of a tensor once.
+
 def _flat(x, what: str, dtype, shape=None) -> int:
-    """Address of a contiguous tensor, after what the library cannot see of an address: its type, shape,
-    device and layout."""
-    if (not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or not x.is_contiguous()
+    """Address of a contiguous tensor."""
+    if (type(x) not in _TENSORS or x.dtype is not dtype or not x.is_cuda or not x.is_contiguous()
             or (shape is not None and x.shape != shape)):
-        _refuse(x, what, dtype, shape)
+        if type(x) in _TENSORS or not isinstance(x, torch.Tensor):
+            _refuse(x, what, dtype, shape)
+        return _flat(x.as_subclass(torch.Tensor), what, dtype, shape)
     return x.data_ptr()
 
 
 def _heads(x, what: str, dtype, shape):
     """Address and strides of a [tokens, heads, head_dim] tensor whose last axis is contiguous."""
-    if not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or x.shape != shape:
-        _refuse(x, what, dtype, shape)
+    if type(x) not in _TENSORS or x.dtype is not dtype or not x.is_cuda or x.shape != shape:
+        if type(x) in _TENSORS or not isinstance(x, torch.Tensor):
+            _refuse(x, what, dtype, shape)
+        return _heads(x.as_subclass(torch.Tensor), what, dtype, shape)
     t, h, d = x.stride()
     if d != 1 and shape[2] > 1:
         raise ValueError(f"the last axis of {what} must be contiguous")
@@ -269,10 +275,21 @@ def _matrix(x, what: str, dtype, shape) -> int:
     return t if shape[0] > 1 else shape[1]
 
 
+_TENSORS = (torch.Tensor, torch.nn.Parameter)
+
+
 def _workspace(x, nbytes: int) -> int:
     if x is None or not x.is_cuda or not x.is_contiguous() or x.numel() * x.element_size() < nbytes:
         raise ValueError(f"workspace must be a contiguous CUDA tensor of at least {nbytes} bytes")
     return x.data_ptr()
+
+
+def _two_sides(q, k):
+    """Shapes of q and k, which must agree in tokens and head_dim."""
+    qs, ks = q.shape, k.shape
+    if len(qs) != 3 or len(ks) != 3 or qs[0] != ks[0] or qs[2] != ks[2]:
+        raise ValueError("q and k must be [tokens, heads, head_dim] with the same tokens and head_dim")
+    return qs, ks
 
 
 class Context:
@@ -471,65 +488,65 @@ class Context:
     # ---- operators of the fine-tuning pass (include/slidedp_ops.h) ----------------------------
 
     @staticmethod
-    def _qk_args(q, k, cos_sin, eps, interleaved):
-        if q.dtype not in _DTYPES:
+    def _qk_args(qs, ks, dtype, cos_sin, eps, interleaved):
+        if dtype not in _DTYPES:
             raise TypeError("q and k must be bfloat16 or float32")
-        if q.dim() != 3 or k.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
-            raise ValueError("q and k must be [tokens, heads, head_dim] with the same tokens and head_dim")
-        T, H, D = q.shape
         rows, rope = cos_sin.shape if cos_sin is not None else (0, 0)
-        return _QkArgs(T, H, k.shape[1], D, rope, bool(interleaved), _DTYPES[q.dtype], rows, eps)
+        return _QkArgs(qs[0], qs[1], ks[1], qs[2], rope, bool(interleaved), _DTYPES[dtype], rows, eps)
 
     @staticmethod
-    def _qk_tables(a, dtype, w_q, w_k, cos_sin, positions):
-        D = (a.head_dim,)
+    def _qk_tables(qs, dtype, w_q, w_k, cos_sin, positions):
+        D = (qs[2],)
         return (None if w_q is None else _flat(w_q, "w_q", dtype, D), None if w_k is None else _flat(w_k, "w_k", dtype, D),
                 None if cos_sin is None else _flat(cos_sin, "cos_sin", torch.float32),
-                None if positions is None else _flat(positions, "positions", torch.int32, (a.tokens,)))
+                None if positions is None else _flat(positions, "positions", torch.int32, (qs[0],)))
 
     def slidedp_qk_norm_rope(self, q, k, w_q, w_k, cos_sin, positions, q_out, k_out, eps: float = 1e-6,
                              interleaved: bool = False, stream=None) -> None:
         """RMS norm of every head of ``q`` and ``k`` ([tokens, heads, head_dim]) and the rotation by
         ``cos_sin`` ([rows, rope_dim]: cosines, then sines; None: no rotation) at ``positions``
         (int32 per token; None: 0, 1, ..)."""
-        a, dt, at = self._qk_args(q, k, cos_sin, eps, interleaved), q.dtype, self._at
-        _pack_heads[4](self._views, 0, *_heads(q, "q", dt, q.shape), *_heads(k, "k", dt, k.shape),
-                       *_heads(q_out, "q_out", dt, q.shape), *_heads(k_out, "k_out", dt, k.shape))
-        self._check(_lib.slidedp_qk_norm_rope(self._h, a, at[0], at[1], *self._qk_tables(a, dt, w_q, w_k, cos_sin, positions),
-                                              at[2], at[3], _stream(stream)))
+        (qs, ks), dt, at = _two_sides(q, k), q.dtype, self._at
+        a = self._qk_args(qs, ks, dt, cos_sin, eps, interleaved)
+        _pack_heads[4](self._views, 0, *_heads(q, "q", dt, qs), *_heads(k, "k", dt, ks), *_heads(q_out, "q_out", dt, qs),
+                       *_heads(k_out, "k_out", dt, ks))
+        rc = _lib.slidedp_qk_norm_rope(self._h, a, at[0], at[1], *self._qk_tables(qs, dt, w_q, w_k, cos_sin, positions),
+                                       at[2], at[3], _stream(stream))
+        if rc:
+            self._check(rc)
 
     def slidedp_qk_norm_rope_workspace(self, q, k) -> int:
         """Bytes of workspace that ``slidedp_qk_norm_rope_backward`` needs for these heads."""
-        return int(_lib.slidedp_qk_norm_rope_workspace(self._qk_args(q, k, None, 0.0, False)))
+        return int(_lib.slidedp_qk_norm_rope_workspace(self._qk_args(*_two_sides(q, k), q.dtype, None, 0.0, False)))
 
     def slidedp_qk_norm_rope_backward(self, q, k, w_q, w_k, cos_sin, positions, dq_out, dk_out, dq, dk, dw_q,
                                       dw_k, workspace, eps: float = 1e-6, interleaved: bool = False,
                                       stream=None) -> None:
         """Gradients ``dq``, ``dk`` and (float32, may be None) ``dw_q``, ``dw_k`` from those of the outputs."""
-        a, dt, at = self._qk_args(q, k, cos_sin, eps, interleaved), q.dtype, self._at
-        D, f32, ws = (a.head_dim,), torch.float32, None
+        (qs, ks), dt, at = _two_sides(q, k), q.dtype, self._at
+        a = self._qk_args(qs, ks, dt, cos_sin, eps, interleaved)
+        D, f32, ws = (qs[2],), torch.float32, None
         if dw_q is not None or dw_k is not None:
             ws = _workspace(workspace, _lib.slidedp_qk_norm_rope_workspace(a))
-        _pack_heads[6](self._views, 0, *_heads(q, "q", dt, q.shape), *_heads(k, "k", dt, k.shape),
-                       *_heads(dq_out, "dq_out", dt, q.shape), *_heads(dk_out, "dk_out", dt, k.shape),
-                       *_heads(dq, "dq", dt, q.shape), *_heads(dk, "dk", dt, k.shape))
-        self._check(_lib.slidedp_qk_norm_rope_backward(
-            self._h, a, at[0], at[1], *self._qk_tables(a, dt, w_q, w_k, cos_sin, positions), at[2], at[3], at[4], at[5],
+        _pack_heads[6](self._views, 0, *_heads(q, "q", dt, qs), *_heads(k, "k", dt, ks), *_heads(dq_out, "dq_out", dt, qs),
+                       *_heads(dk_out, "dk_out", dt, ks), *_heads(dq, "dq", dt, qs), *_heads(dk, "dk", dt, ks))
+        rc = _lib.slidedp_qk_norm_rope_backward(
+            self._h, a, at[0], at[1], *self._qk_tables(qs, dt, w_q, w_k, cos_sin, positions), at[2], at[3], at[4], at[5],
             None if dw_q is None else _flat(dw_q, "dw_q", f32, D), None if dw_k is None else _flat(dw_k, "dw_k", f32, D),
-            ws, _stream(stream)))
+            ws, _stream(stream))
+        if rc:
+            self._check(rc)
 
     @staticmethod
-    def _attn_args(q, k, cu_docs=None, prefix=None, slopes=None, causal=True, scale=None, softcap=0.0):
-        if q.dim() != 3 or k.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
-            raise ValueError("q and k must be [tokens, heads, head_dim] with the same tokens and head_dim")
-        T, H, D = q.shape
+    def _attn_args(qs, ks, cu_docs=None, prefix=None, slopes=None, causal=True, scale=None, softcap=0.0):
+        T, H, D = qs
         docs, cu = 1, None
         if cu_docs is not None:
             cu = _flat(cu_docs, "cu_docs", torch.int32)
             if cu_docs.dim() != 1 or cu_docs.numel() < 1:
                 raise ValueError("cu_docs must hold docs + 1 offsets")
             docs = cu_docs.numel() - 1
-        return _AttnArgs(T, H, k.shape[1], D, bool(causal), docs, 0, cu,
+        return _AttnArgs(T, H, ks[1], D, bool(causal), docs, 0, cu,
                          None if prefix is None else _flat(prefix, "prefix", torch.int32, (docs,)) or None,
                          None if slopes is None else _flat(slopes, "slopes", torch.float32, (H,)),
                          D ** -0.5 if scale is None else scale, softcap)
@@ -539,23 +556,25 @@ class Context:
         """Attention of ``q`` [tokens, heads_q, head_dim] over ``k``, ``v`` [tokens, heads_kv, head_dim] within
         packed documents (``cu_docs``: int32 offsets; None: one document). Fills ``out`` and ``lse``
         [heads_q, tokens]. ``scale`` defaults to head_dim ** -0.5."""
-        a = self._attn_args(q, k, cu_docs, prefix, slopes, causal, scale, softcap)
-        bf, at, qs, ks = torch.bfloat16, self._at, q.shape, k.shape
+        (qs, ks), bf, at = _two_sides(q, k), torch.bfloat16, self._at
+        a = self._attn_args(qs, ks, cu_docs, prefix, slopes, causal, scale, softcap)
         _pack_heads[4](self._views, 0, *_heads(q, "q", bf, qs), *_heads(k, "k", bf, ks), *_heads(v, "v", bf, ks),
                        *_heads(out, "out", bf, qs))
-        self._check(_lib.slidedp_attention(self._h, a, at[0], at[1], at[2], at[3],
-                                           _flat(lse, "lse", torch.float32, (qs[1], qs[0])), _stream(stream)))
+        rc = _lib.slidedp_attention(self._h, a, at[0], at[1], at[2], at[3], _flat(lse, "lse", torch.float32, (qs[1], qs[0])),
+                                    _stream(stream))
+        if rc:
+            self._check(rc)
 
     def slidedp_attention_workspace(self, q, k) -> int:
         """Bytes of workspace that ``slidedp_attention_backward`` needs."""
-        return int(_lib.slidedp_attention_workspace(self._attn_args(q, k)))
+        return int(_lib.slidedp_attention_workspace(self._attn_args(*_two_sides(q, k))))
 
     def slidedp_attention_backward(self, q, k, v, out, lse, d_out, dq, dk, dv, workspace, cu_docs=None, prefix=None,
                                    slopes=None, causal: bool = True, scale: float | None = None,
                                    softcap: float = 0.0, stream=None) -> None:
         """Gradients ``dq``, ``dk``, ``dv`` from ``d_out``, with the forward's ``out`` and ``lse``."""
-        a = self._attn_args(q, k, cu_docs, prefix, slopes, causal, scale, softcap)
-        bf, at, qs, ks = torch.bfloat16, self._at, q.shape, k.shape
+        (qs, ks), bf, at = _two_sides(q, k), torch.bfloat16, self._at
+        a = self._attn_args(qs, ks, cu_docs, prefix, slopes, causal, scale, softcap)
         ws = _workspace(workspace, _lib.slidedp_attention_workspace(a))
         _pack_heads[8](self._views, 0, *_heads(q, "q", bf, qs), *_heads(k, "k", bf, ks), *_heads(v, "v", bf, ks),
                        *_heads(out, "out", bf, qs), *_heads(d_out, "d_out", bf, qs), *_heads(dq, "dq", bf, qs),
