@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(kGeneralThreads) attention_dq_general_kernel(c
 }
 __global__ void __launch_bounds__(kGeneralThreads) attention_dkv_general_kernel(const __grid_constant__ AttnParams p) {
   const int j = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
-  if (j < p.tokens) attention_dkv_row(p, j, blockIdx.y, true, true);
+  if (j < p.tokens) attention_dkv_row(p, j, blockIdx.y, true, true, 0, p.head_dim);
 }
 
 // row_lse[h][i] = lse log2 e, row_delta[h][i] = sum_d dout out, zeros for the rows of the padding: one warp per row.

@@ -21,6 +21,7 @@ constexpr int kHalfBytes = kTile * 128;    // 64 BF16 columns of a tile, as TMA 
 // Eight warps of rows and a warpgroup with the issuer and the producer. Launched with 168 registers per
 // thread (65536 / 384); the row warpgroups then take 216 and the third keeps 72: 2 * 216 + 72 = 3 * 168.
 constexpr int kMmaThreads = 384;
+constexpr int64_t kSplitBelow = 148 * 2;   // see key_split
 constexpr int kStageBytes = 4096;          // per warp of rows: 32 rows of 64 BF16 columns, on their way out
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
@@ -137,10 +138,10 @@ struct WorkRing {
   __device__ __forceinline__ void take_next() { mbar_arrive(smem_addr(&ask)); }
   static constexpr int kAhead = 4;
   // The asking warp: make(item) returns the item's plan (in every lane).
+  // single: the given item only.
   template <typename F>
-  __device__ __forceinline__ void serve(const Waiter& wait, F make) {
+  __device__ __forceinline__ void serve(const Waiter& wait, int now, bool single, F make) {
     const int lane = threadIdx.x % 32;
-    int now = (int)blockIdx.x;
     for (int n = 0;; ++n) {
       const int slot = n & 1;
       if (n >= 2 && !__all_sync(0xffffffffu, wait(smem_addr(&empty[slot]), (n >> 1) + 1 & 1, kNap))) return;
@@ -153,6 +154,10 @@ struct WorkRing {
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_addr(&full[slot]));
       if (now < 0 || !__all_sync(0xffffffffu, wait(smem_addr(&ask), n & 1, kNap))) return;
+      if (single) {
+        now = -1;
+        continue;
+      }
       if (lane == 0) {
         mbar_expect(smem_addr(&answered), 16);
         take_over_next_block(smem_addr(&answer), smem_addr(&answered));
@@ -197,9 +202,11 @@ __device__ __forceinline__ uint32_t seen_bits(int a, int b, int c0) {
 
 // Stores 128 rows, a warp its own 32, of a tile whose row of FP32 values lies in the thread's TMEM lane, as BF16: 64 columns
 // at a time through 4 KB of shared memory per warp, from where TMA writes them (16 bytes per thread straight to global
-// memory touched 32 lines per instruction: 3000 cycles a tile). Returns whether the thread saw a NaN.
+// memory touched 32 lines per instruction: 3000 cycles a tile). get(c, o) fetches columns 32 c .. of the 64. Returns whether
+// the thread saw a NaN.
+template <typename F>
 __device__ __forceinline__ bool store_columns(uint32_t stage, const CUtensorMap* map, int head, int row0, int column, int head_dim, int tokens,
-                                              uint32_t from, bool any, float factor) {
+                                              float factor, F get) {
   const int lane = threadIdx.x % 32;
   if (lane == 0) tma_stores_read();   // the last 64 columns have left the stage
   __syncwarp();
@@ -207,14 +214,7 @@ __device__ __forceinline__ bool store_columns(uint32_t stage, const CUtensorMap*
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
     uint32_t o[32];
-    if (any) {
-      tmem_load32(from + c * 32, o);
-      tmem_wait_load();
-      tmem_landed(o);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 32; ++e) o[e] = 0;
-    }
+    get(c, o);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       uint32_t y[4];
@@ -232,6 +232,18 @@ __device__ __forceinline__ bool store_columns(uint32_t stage, const CUtensorMap*
   __syncwarp();
   if (lane == 0 && row0 < tokens) tma_store_3d(map, stage, column, head, row0);
   return nan && row0 + lane < tokens;
+}
+
+// Columns from TMEM, or zeros where nothing was accumulated.
+__device__ __forceinline__ void tmem_columns(uint32_t from, bool any, uint32_t* o) {
+  if (any) {
+    tmem_load32(from, o);
+    tmem_wait_load();
+    tmem_landed(o);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) o[e] = 0;
+  }
 }
 
 template <int N>
@@ -323,7 +335,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   if (warp >= 8) {
     fewer_registers();
     if (warp == 10) {   // ---- the next tiles
-      ctl.work.serve(wait, [&](int item) {
+      ctl.work.serve(wait, (int)blockIdx.x, false, [&](int item) {
         // lanes 0..3: the keys of each tile's first and last row
         const int m0 = row_of(item), row = min(m0 + (lane >> 1) * kTile + (lane & 1 ? kTile - 1 : 0), p.tokens - 1);
         int lo = 0, hi = 0, index = 0;
@@ -550,7 +562,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       bool nan = false;
 #pragma unroll
       for (int c = 0; c < HALVES; ++c)
-        nan |= store_columns(stages + warp * kStageBytes, &map_o, h, row0, c * 64, p.head_dim, p.tokens, at_o + c * 64, from < to, inv);
+        nan |= store_columns(stages + warp * kStageBytes, &map_o, h, row0, c * 64, p.head_dim, p.tokens, inv,
+                             [&](int k, uint32_t* o) { tmem_columns(at_o + c * 64 + k * 32, from < to, o); });
       if (live) p.lse[(int64_t)h * p.tokens + i] = some ? (m * unit + log2f(l)) * (1.0f / kLog2e) : -INFINITY;
       uint32_t redo = __ballot_sync(0xffffffffu, nan);
       if (redo) {
@@ -578,7 +591,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 // Keys: an item is 128 keys of one key head, for which the block walks all queries that see them, for every query head of
 // the group. Rows of the tiles (TMEM lanes) are keys: S^T = K Q^T and dP^T = V dO^T, so that P^T and dS^T
 // are, as they stand, the left operands of dV and dK. TMEM: S^T, dP^T (overwritten by P^T and dS^T, each
-// warpgroup within its own 64 columns), dV, dK.
+// warpgroup within its own 64 columns), dV, dK. When there are few tiles of keys, a cluster of blocks shares an item, each
+// taking some of the group's query heads, and adds up through distributed shared memory.
 template <int HALVES> struct KeysShape {
   static constexpr int kStages = 2;
   static constexpr int kTileBytes = HALVES * kHalfBytes;
@@ -604,7 +618,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     attention_dkv_mma_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
                              const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                              const __grid_constant__ CUtensorMap map_do, const __grid_constant__ CUtensorMap map_dk,
-                             const __grid_constant__ CUtensorMap map_dv) {
+                             const __grid_constant__ CUtensorMap map_dv, int split) {
   using Shape = KeysShape<HALVES>;
   constexpr int S = Shape::kStages;
   extern __shared__ __align__(1024) uint8_t raw_smem[];
@@ -613,6 +627,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   // item -> key head and first key: the first keys are seen by the most queries when causal, so they come first
   const auto head_of = [&](int item) { return item % p.heads_kv; };
   const auto row_of = [&](int item) { return item / p.heads_kv * kTile; };
+  // the block's share of the group's query heads
+  const int rank = (int)(blockIdx.x % split), h_from = rank * p.group / split, heads = (rank + 1) * p.group / split - h_from;
   const uint32_t base = smem_addr(raw_smem);
   const uint32_t smem_k = base, smem_v = smem_k + Shape::kTileBytes, smem_q = smem_v + Shape::kTileBytes,
                  smem_do = smem_q + S * Shape::kTileBytes, stages = smem_do + S * Shape::kTileBytes;
@@ -648,7 +664,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   if (warp >= 8) {
     fewer_registers();
     if (warp == 10) {   // ---- the next tiles
-      ctl.work.serve(wait, [&](int item) {
+      ctl.work.serve(wait, (int)(blockIdx.x / split), split > 1, [&](int item) {
         const int row = min(row_of(item) + (lane ? kTile - 1 : 0), p.tokens - 1);   // lanes 0 and 1: first and last key
         int lo = 0, hi = 0, index = 0;
         if (lane < 2) {
@@ -675,10 +691,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         load_tile<HALVES>(smem_k, &map_k, hk, n0, smem_addr(&ctl.kv_full));
         load_tile<HALVES>(smem_v, &map_v, hk, n0, smem_addr(&ctl.kv_full));
         ++walks;
-        int left = pl.per_head * p.group;
-        for (int h = hk * p.group; h < (hk + 1) * p.group && ok; ++h)
+        int left = pl.per_head * heads;
+        for (int h = hk * p.group + h_from; left > 0 && ok; ++h)
           for (int tile = 0; tile < pl.per_head; ++tile, ++sent, --left) {
-            if (left == min(pl.per_head * p.group, ctl.work.kAhead)) ctl.work.take_next();
+            if (left == min(pl.per_head * heads, ctl.work.kAhead)) ctl.work.take_next();
             const int st = sent % S, m0 = (pl.q_lo + tile) * kTile;
             const uint32_t turn = (uint32_t)(sent / S + 1) & 1;
             if (sent >= S && !(ok = wait(smem_addr(&ctl.q_empty[st]), turn))) break;
@@ -706,7 +722,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       bool ok = true;
       KeysPlan pl;
       for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, false); ++n) {
-        const int steps = pl.per_head * p.group;
+        const int steps = pl.per_head * heads;
         if (steps == 0) continue;
         if (!(ok = wait_all(smem_addr(&ctl.kv_full), walks & 1))) break;
         ++walks;
@@ -746,18 +762,23 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         drain(smem_addr(&ctl.done), 0);
       }
     }
+    if (split > 1) {   // as below
+      __syncwarp();
+      cluster_sync();
+      cluster_sync();
+    }
   } else {   // ---- rows: keys; the warpgroups take 64 of a step's queries each
     more_registers();
     const int g = warp / 4, r = (warp % 4) * 32;
     const uint32_t at = ((uint32_t)r << 16) + g * 64;
     int item, turns = 0, walks = 0;
-    bool ok = true;
+    bool ok = true, joined = false;
     KeysPlan pl;
     for (int n = 0; ok && ctl.work.next(n, wait, &item, &pl, false); ++n) {
-      const int hk = head_of(item), n0 = row_of(item), j = n0 + r + lane, steps = pl.per_head * p.group;
+      const int hk = head_of(item), n0 = row_of(item), j = n0 + r + lane, steps = pl.per_head * heads;
       int lo = 0, hi = 0;
       if (j < p.tokens) mask.queries_of(j, mask.above(j, pl.above[0], pl.above[1]), &lo, &hi);
-      int h = hk * p.group, tile = 0;
+      int h = hk * p.group + h_from, tile = 0;
       ScoreMod<MODE> mod(p, h);
       for (int it = 0; it < steps; ++it, ++tile, ++turns) {
         if (tile == pl.per_head) {
@@ -846,20 +867,85 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tc_fence_after();
       }
       if (!ok) break;
-      // warpgroup 0 stores dV, warpgroup 1 dK
       const int row0 = j - lane;
-      const uint32_t src = (g ? at_dk : at_dv) + ((uint32_t)r << 16);
-      bool nan = false;
+      const uint32_t lanes = (uint32_t)r << 16;
+      if (split > 1) {
+        // The blocks of the cluster hold the sums over their heads of both outputs, side by side as 2 HALVES 64 columns. Each
+        // block adds up its share of the columns, in the order of the blocks: the others write theirs into its rings, which
+        // are free once everyone's products are done.
+        constexpr int kColumns = 2 * HALVES * 64;
+        const int width = kColumns / split;
+        const auto column = [&](int c) { return (c < HALVES * 64 ? at_dv + c : at_dk + c - HALVES * 64) + lanes; };
+        const auto slot = [&](int from, int c) { return smem_q + (from * width + c) * (kTile * 4) + (r + lane) * 16; };   // [column / 4][row]
+        cluster_sync();
+        for (int to = 0; to < split; ++to) {
+          if (to == rank) continue;
+          const uint32_t there = peer_addr(slot(rank, 0), to);
+          for (int c = g * 32; c < width; c += 64) {
+            uint32_t o[32];
+            tmem_columns(column(to * width + c), steps > 0, o);
 #pragma unroll
-      for (int c = 0; c < HALVES; ++c)
-        nan |= store_columns(stages + warp * kStageBytes, g ? &map_dk : &map_dv, hk, row0, c * 64, p.head_dim, p.tokens, src + c * 64, steps > 0,
-                             g ? p.scale : 1.0f);
-      uint32_t redo = __ballot_sync(0xffffffffu, nan);
-      if (redo) {
-        if (lane == 0) tma_stores_done();
-        __syncwarp();
-        for (; redo; redo &= redo - 1) attention_dkv_row(p, row0 + __ffs(redo) - 1, hk, g == 1, g == 0);
+            for (int e = 0; e < 32; e += 4)
+              asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(there + (c + e) * (kTile * 4)), "r"(o[e]), "r"(o[e + 1]),
+                           "r"(o[e + 2]), "r"(o[e + 3])
+                           : "memory");
+          }
+        }
+        cluster_sync();
+        if (g * 64 < width) {
+          const int first = rank * width + g * 64, d0 = first % (HALVES * 64);
+          const bool is_k = first >= HALVES * 64;
+          const bool nan = store_columns(stages + warp * kStageBytes, is_k ? &map_dk : &map_dv, hk, row0, d0, p.head_dim, p.tokens,
+                                         is_k ? p.scale : 1.0f, [&](int k, uint32_t* o) {
+            float sum[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sum[e] = 0.0f;
+            for (int from = 0; from < split; ++from) {
+              if (from == rank) {
+                tmem_columns(column(first + k * 32), steps > 0, o);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) sum[e] += __uint_as_float(o[e]);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                  float v[4];
+                  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+                               : "r"(slot(from, g * 64 + k * 32 + e)) : "memory");
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) sum[e + i] += v[i];
+                }
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(sum[e]);
+          });
+          uint32_t redo = __ballot_sync(0xffffffffu, nan);
+          if (redo) {
+            if (lane == 0) tma_stores_done();
+            __syncwarp();
+            for (; redo; redo &= redo - 1) attention_dkv_row(p, row0 + __ffs(redo) - 1, hk, is_k, !is_k, d0, min(d0 + 64, p.head_dim));
+          }
+        }
+        joined = true;
+      } else {
+        // warpgroup 0 stores dV, warpgroup 1 dK
+        bool nan = false;
+#pragma unroll
+        for (int c = 0; c < HALVES; ++c)
+          nan |= store_columns(stages + warp * kStageBytes, g ? &map_dk : &map_dv, hk, row0, c * 64, p.head_dim, p.tokens, g ? p.scale : 1.0f,
+                               [&](int k, uint32_t* o) { tmem_columns((g ? at_dk : at_dv) + lanes + c * 64 + k * 32, steps > 0, o); });
+        uint32_t redo = __ballot_sync(0xffffffffu, nan);
+        if (redo) {
+          if (lane == 0) tma_stores_done();
+          __syncwarp();
+          for (; redo; redo &= redo - 1) attention_dkv_row(p, row0 + __ffs(redo) - 1, hk, g == 1, g == 0, 0, p.head_dim);
+        }
       }
+    }
+    if (split > 1 && !joined) {   // gave up: the others still come to the barriers
+      __syncwarp();
+      cluster_sync();
+      cluster_sync();
     }
     if (lane == 0) tma_stores_done();
   }
@@ -940,7 +1026,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   if (warp >= 8) {
     fewer_registers();
     if (warp == 10) {   // ---- the next tiles
-      ctl.work.serve(wait, [&](int item) {
+      ctl.work.serve(wait, (int)blockIdx.x, false, [&](int item) {
         const int row = min(row_of(item) + (lane ? kTile - 1 : 0), p.tokens - 1);   // lanes 0 and 1: first and last query
         int lo = 0, hi = 0, index = 0;
         if (lane < 2) {
@@ -1101,8 +1187,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       if (!ok) break;
       if (g < HALVES) {   // a warpgroup stores 64 columns
         const int row0 = i - lane;
-        const bool nan = store_columns(stages + warp * kStageBytes, &map_dq, h, row0, g * 64, p.head_dim, p.tokens,
-                                       at_dq + ((uint32_t)r << 16) + g * 64, steps > 0, p.scale);
+        const bool nan = store_columns(stages + warp * kStageBytes, &map_dq, h, row0, g * 64, p.head_dim, p.tokens, p.scale, [&](int k, uint32_t* o) {
+          tmem_columns(at_dq + ((uint32_t)r << 16) + g * 64 + k * 32, steps > 0, o);
+        });
         uint32_t redo = __ballot_sync(0xffffffffu, nan);
         if (redo) {
           if (lane == 0) tma_stores_done();
@@ -1162,6 +1249,14 @@ static cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>* done, 
   return e;
 }
 
+// Blocks that share a tile of keys, by query heads: as many as the group has, up to what the tile's columns can be cut
+// into, while tiles are fewer than a few per SM.
+static int key_split(int64_t tiles, int group, int halves) {
+  int n = 1;
+  while (n < 2 * halves && n * 2 <= group && tiles * n < kSplitBelow) n *= 2;
+  return n;
+}
+
 static int score_mode(const AttnParams& p) { return p.softcap > 0.0f ? kCap : p.slopes || !(p.scale_log2 > 0.0f) ? kBias : kPlain; }
 
 template <int HALVES, int MODE>
@@ -1192,8 +1287,20 @@ static int backward(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
   CU(allow_smem(attention_dq_mma_kernel<HALVES, MODE>, QueriesShape<HALVES>::kSmem, &ready_q, ctx->device));
   const int64_t tiles = (p.tokens + kTile - 1) / kTile;
   if (tiles * p.heads_q > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
+  const int split = key_split(tiles * p.heads_kv, p.group, HALVES);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * p.heads_kv * split));
+  cfg.blockDim = dim3(kMmaThreads);
+  cfg.dynamicSmemBytes = KeysShape<HALVES>::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)split;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = split > 1 ? 1 : 0;
   FAULT_POINT();
-  attention_dkv_mma_kernel<HALVES, MODE><<<(unsigned)(tiles * p.heads_kv), kMmaThreads, KeysShape<HALVES>::kSmem, st>>>(p, q, k, v, d, dk, dv);
+  (void)cudaLaunchKernelEx(&cfg, attention_dkv_mma_kernel<HALVES, MODE>, p, q, k, v, d, dk, dv, split);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   FAULT_POINT();

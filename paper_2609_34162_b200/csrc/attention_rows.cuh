@@ -98,7 +98,8 @@ static __device__ __noinline__ void attention_dq_row(const AttnParams& p, int i,
   store_row(p.dq, i, h, from, to, dq);
 }
 
-static __device__ __noinline__ void attention_dkv_row(const AttnParams& p, int j, int hk, bool with_dk, bool with_dv) {
+// Values [from, to) of dk, of dv, or of both are stored.
+static __device__ __noinline__ void attention_dkv_row(const AttnParams& p, int j, int hk, bool with_dk, bool with_dv, int from, int to) {
   float k[kMaxPer], v[kMaxPer], dk[kMaxPer] = {}, dv[kMaxPer] = {};
   load_row(p.k, j, hk, p.head_dim, k);
   load_row(p.v, j, hk, p.head_dim, v);
@@ -119,8 +120,8 @@ static __device__ __noinline__ void attention_dkv_row(const AttnParams& p, int j
       }
     }
   }
-  if (with_dk) store_row(p.dk, j, hk, 0, p.head_dim, dk);
-  if (with_dv) store_row(p.dv, j, hk, 0, p.head_dim, dv);
+  if (with_dk) store_row(p.dk, j, hk, from, to, dk);
+  if (with_dv) store_row(p.dv, j, hk, from, to, dv);
 }
 
 }  // namespace slidedp

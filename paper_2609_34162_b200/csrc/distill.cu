@@ -262,15 +262,10 @@ __device__ __forceinline__ SoftSum join_block(SoftSum mine, SoftSum* warps, floa
 
 // Sums travel between the blocks of a cluster as asynchronous stores into the receiver's `part`, which count
 // towards its barrier: nobody waits for more than the sums.
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ void send_sums(const SoftSum& v, DistillShared& sh, int rank, int size) {
   if (threadIdx.x == 0) mbar_expect(smem_addr(&sh.exchanged), size * sizeof(float4));
   if ((int)threadIdx.x >= size) return;
-  uint32_t to, at;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(&sh.part[rank])), "r"(threadIdx.x));
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(&sh.exchanged)), "r"(threadIdx.x));
+  const uint32_t to = peer_addr(smem_addr(&sh.part[rank]), threadIdx.x), at = peer_addr(smem_addr(&sh.exchanged), threadIdx.x);
   asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to), "f"(v.m),
                "f"(v.s0), "f"(v.s1), "f"(0.0f), "r"(at)
                : "memory");

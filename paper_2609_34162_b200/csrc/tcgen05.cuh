@@ -58,6 +58,19 @@ struct Waiter {
 // Order between ordinary accesses of shared memory and those of the asynchronous proxy (copies, answers).
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// ---- clusters -------------------------------------------------------------------------------------------
+
+// All threads of all blocks of the cluster; shared-memory accesses before it are seen after it.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
+}
+// The address, in the shared memory of block `rank` of the cluster, of what lies at `addr` in one's own.
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
+  uint32_t to;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(addr), "r"(rank));
+  return to;
+}
+
 // ---- cluster launch control --------------------------------------------------------------------------
 
 // Asks to take over a block of the grid that has not started; 16 bytes at `answer` complete on `bar`.
