@@ -21,7 +21,7 @@ constexpr int kHalfBytes = kTile * 128;    // 64 BF16 columns of a tile, as TMA 
 // Eight warps of rows and a warpgroup with the issuer and the producer. Launched with 168 registers per
 // thread (65536 / 384); the row warpgroups then take 216 and the third keeps 72: 2 * 216 + 72 = 3 * 168.
 constexpr int kMmaThreads = 384;
-constexpr int64_t kSplitBelow = 148 * 2;   // see key_split
+constexpr int64_t kSMs = 148;
 constexpr int kStageBytes = 4096;          // per warp of rows: 32 rows of 64 BF16 columns, on their way out
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
@@ -66,27 +66,58 @@ __device__ __forceinline__ void product_tmem(uint32_t d, uint32_t a, uint32_t se
 // chains of special functions from overlapping (9000 cycles a step where these take a third).
 enum ScoreMode { kPlain = 0, kBias = 1, kCap = 2 };   // kBias also takes scales that are not positive; kCap has the bias as well
 
-// Scores in units of log2 e, and the factor of d score / d (scale product).
+// Scores in units of log2 e, and the factor of d score / d (scale product), two neighbouring columns at a time.
 template <int MODE>
 struct ScoreMod {
-  float scale;   // of the product; with a cap, of 2 log2(e) (scale / cap) product
+  static constexpr float kSmall = 0.7f;   // where tanh is a polynomial
+  float scale;   // of the product; with a cap, the product's scale over the cap
   float cap;     // cap log2 e
   float slope;   // log2 units per position
   __device__ ScoreMod(const AttnParams& p, int h) {
-    scale = MODE == kCap ? p.scale_log2 * 2.0f / p.softcap : p.scale_log2;
+    scale = MODE == kCap ? p.scale / p.softcap : p.scale_log2;
     cap = p.softcap * kLog2e;
     slope = p.slopes ? -p.slopes[h] * kLog2e : 0.0f;
   }
-  // distance: query minus key
-  __device__ __forceinline__ float operator()(float raw, float distance, float* grad) const {
-    *grad = 1.0f;
+  // Whether the polynomial serves the warp's columns: capped models keep most scores well below the cap.
+  template <int N>
+  __device__ __forceinline__ bool small(const uint32_t* x) const {
+    if constexpr (MODE != kCap) return true;
+    float top[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < N; ++c) top[c & 3] = fmaxf(top[c & 3], fabsf(__uint_as_float(x[c])));
+    const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * fabsf(scale);
+    return __all_sync(0xffffffffu, m <= kSmall);
+  }
+  // distance: query minus key of the first column; the second's is one less (columns are keys) or one more.
+  template <bool SMALL>
+  __device__ __forceinline__ void operator()(float r0, float r1, float distance0, float distance1, float* s, float* grad) const {
+    grad[0] = grad[1] = 1.0f;
+    float th[2];
     if constexpr (MODE == kCap) {
-      // tanh y = 1 - 2 / (1 + exp 2y): absolute error near 2^-23, and 1 and -1 at the ends
-      const float th = fmaf(-2.0f, rcp_approx(1.0f + exp2_approx(raw * scale)), 1.0f);
-      *grad = fmaf(-th, th, 1.0f);
-      return fmaf(slope, fabsf(distance), cap * th);
+      uint64_t y = mul2(pair(r0, r1), pair(scale, scale)), t;
+      if constexpr (SMALL) {
+        // tanh y = y + y^3 q(y^2): the odd polynomial of degree 9 with the least greatest error for |y| <= 0.7 (1.4e-7, from
+        // a linear program), on the multiply-add pipe: the special functions of the other form, three of them with the
+        // exponential, would take longer than the tile's products
+        const uint64_t z = mul2(y, y);
+        const auto step = [&](uint64_t q, float c) { return fma2(q, z, pair(c, c)); };
+        uint64_t q = step(pair(0.01359964907169342f, 0.01359964907169342f), -0.05067462846636772f);
+        q = step(q, 0.1327691525220871f);
+        q = step(q, -0.3333006501197815f);
+        t = fma2(mul2(q, z), y, y);
+      } else {
+        // tanh y = 1 - 2 / (1 + exp 2y): absolute error near 2^-23, and 1 and -1 at the ends
+        float e0, e1;
+        split(mul2(y, pair(2.0f * kLog2e, 2.0f * kLog2e)), &e0, &e1);
+        t = fma2(pair(rcp_approx(1.0f + exp2_approx(e0)), rcp_approx(1.0f + exp2_approx(e1))), pair(-2.0f, -2.0f), pair(1.0f, 1.0f));
+      }
+      split(t, &th[0], &th[1]);
+      split(fma2(mul2(t, t), pair(-1.0f, -1.0f), pair(1.0f, 1.0f)), &grad[0], &grad[1]);
+      s[0] = fmaf(cap, th[0], slope * fabsf(distance0));
+      s[1] = fmaf(cap, th[1], slope * fabsf(distance1));
     } else {
-      return fmaf(slope, fabsf(distance), raw * scale);
+      s[0] = fmaf(r0, scale, slope * fabsf(distance0));
+      s[1] = fmaf(r1, scale, slope * fabsf(distance1));
     }
   }
 };
@@ -479,9 +510,16 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         const int n0 = pl.n_lo + j * kTile;
         if constexpr (MODE != kPlain) {
           const float d0 = (float)(i - n0);
-          float g;
+          const auto scores = [&](auto small) {
 #pragma unroll
-          for (int c = 0; c < 128; ++c) x[c] = __float_as_uint(mod(__uint_as_float(x[c]), d0 - (float)c, &g));
+            for (int c = 0; c < 128; c += 2) {
+              float y[2], g[2];
+              mod.template operator()<decltype(small)::value>(__uint_as_float(x[c]), __uint_as_float(x[c + 1]), d0 - (float)c, d0 - (float)(c + 1), y, g);
+              x[c] = __float_as_uint(y[0]);
+              x[c + 1] = __float_as_uint(y[1]);
+            }
+          };
+          if (mod.template small<128>(x)) scores(std::true_type()); else if constexpr (MODE == kCap) scores(std::false_type());
         }
         // Visible columns [a, b). Rows past the sequence are not stored: they need no mask.
         const int a = i < p.tokens ? lo - n0 : 0, b = i < p.tokens ? hi - n0 : kTile;
@@ -808,22 +846,26 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         {
           uint32_t pk[32];
           const float d0 = (float)(j - m0);
-          const auto probabilities = [&](auto masked) {
+          const auto probabilities = [&](auto masked, auto small) {
 #pragma unroll
             for (int c = 0; c < 64; c += 2) {
               float e[2], grad[2] = {1.0f, 1.0f};
+              if constexpr (MODE != kPlain)
+                mod.template operator()<decltype(small)::value>(__uint_as_float(x[c]), __uint_as_float(x[c + 1]), d0 - (float)c, d0 - (float)(c + 1), e, grad);
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                if constexpr (MODE != kPlain) e[k] = mod(__uint_as_float(x[c + k]), d0 - (float)(c + k), &grad[k]) - y[c + k];
-                else e[k] = fmaf(__uint_as_float(x[c + k]), p.scale_log2, -y[c + k]);
-                e[k] = exp2_approx(e[k]);
+                e[k] = exp2_approx(MODE != kPlain ? e[k] - y[c + k] : fmaf(__uint_as_float(x[c + k]), p.scale_log2, -y[c + k]));
                 if (decltype(masked)::value) e[k] = seen[c / 32] >> (c % 32 + k) & 1 ? e[k] : 0.0f;
                 pr[c + k] = MODE == kCap ? e[k] * grad[k] : e[k];
               }
               pk[c / 2] = pack_bf16(e[0], e[1]);
             }
           };
-          if (whole) probabilities(std::false_type()); else probabilities(std::true_type());
+          if (mod.template small<64>(x)) {
+            if (whole) probabilities(std::false_type(), std::true_type()); else probabilities(std::true_type(), std::true_type());
+          } else if constexpr (MODE == kCap) {
+            probabilities(std::true_type(), std::false_type());
+          }
           tmem_store32(at_s + at, pk);
         }
         tmem_wait_store();
@@ -1147,13 +1189,21 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         const bool whole = __all_sync(0xffffffffu, a <= 0 && b >= 64);
         const uint32_t seen[2] = {seen_bits(a, b, 0), seen_bits(a, b, 32)};
         float pr[64];
+        const float d0 = (float)(i - c0);
+        const auto probabilities = [&](auto small) {
 #pragma unroll
-        for (int c = 0; c < 64; ++c) {
-          float e, grad = 1.0f;
-          if constexpr (MODE != kPlain) e = mod(__uint_as_float(x[c]), (float)(i - c0) - (float)c, &grad) - lse;
-          else e = fmaf(__uint_as_float(x[c]), p.scale_log2, -lse);
-          pr[c] = exp2_approx(e) * grad;
-        }
+          for (int c = 0; c < 64; c += 2) {
+            float e[2], grad[2] = {1.0f, 1.0f};
+            if constexpr (MODE != kPlain)
+              mod.template operator()<decltype(small)::value>(__uint_as_float(x[c]), __uint_as_float(x[c + 1]), d0 - (float)c, d0 - (float)(c + 1), e, grad);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              pr[c + k] = exp2_approx(MODE != kPlain ? e[k] - lse : fmaf(__uint_as_float(x[c + k]), p.scale_log2, -lse));
+              if (MODE == kCap) pr[c + k] *= grad[k];
+            }
+          }
+        };
+        if (mod.template small<64>(x)) probabilities(std::true_type()); else if constexpr (MODE == kCap) probabilities(std::false_type());
         ok = __all_sync(0xffffffffu, wait(smem_addr(&ctl.dp_full), turns & 1));
         if (!ok) break;
         tc_fence_after();
@@ -1249,11 +1299,12 @@ static cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>* done, 
   return e;
 }
 
-// Blocks that share a tile of keys, by query heads: as many as the group has, up to what the tile's columns can be cut
-// into, while tiles are fewer than a few per SM.
+// Blocks that share a tile of keys, by query heads: two below two tiles per SM, four while two each would leave SMs
+// idle (a tile's columns can be cut no finer than into 64). Keys' gradients in us, by 1 / 2 / 4 blocks: 128 tiles (2048
+// tokens, causal) 125 / 76 / 108, 256 (4096, not causal) 421 / 320 / 381, 512 (8192, packed) 191 / 224 / -.
 static int key_split(int64_t tiles, int group, int halves) {
   int n = 1;
-  while (n < 2 * halves && n * 2 <= group && tiles * n < kSplitBelow) n *= 2;
+  while (n < 2 * halves && n * 2 <= group && tiles * n < (n == 1 ? 2 * kSMs : kSMs)) n *= 2;
   return n;
 }
 
