@@ -19,7 +19,13 @@ constexpr int kMaxEntries = 512;        // teacher entries per row
 constexpr int kDistillThreads = 256;
 constexpr int kDistillWarps = kDistillThreads / 32;
 constexpr int kDistillMaxCluster = 8;
-constexpr int kDistillUnroll = 4;       // 16-byte chunks per thread and turn; the next turn's are on their way
+// 16-byte chunks per thread and turn; the next turn's are on their way. A step's long slices of a row take four (70
+// registers, three blocks per SM); short ones two, five blocks per SM, so that more rows cover each other's exchange of
+// sums. Steps of BF16 logits with four / two: 8192 x 8000 135 / 105 us, 4096 x 32768 130 / 119, 4096 x 49152 180 / 173,
+// 4096 x 65536 224 / 231, 4096 x 131072 446 / 473.
+constexpr int kDistillUnroll = 4, kDistillUnrollShort = 2;
+constexpr int64_t kShortSliceBytes = 112 * 1024;
+constexpr int distill_min_blocks(int unroll) { return unroll == kDistillUnroll ? 0 : 5; }   // 0: as the compiler likes
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -339,11 +345,11 @@ __device__ __forceinline__ void write_values(const Row<T>& row, T* dz, int64_t c
   for (int e = 0; e < Logit<T>::kPer; ++e)
     if (first + e >= 0 && first + e < row.vocab) Logit<T>::store(dz + first + e, g[e]);
 }
-// Walks a slice's whole chunks, kDistillUnroll per thread and turn, with the next turn's loads issued before this
+// Walks a slice's whole chunks, U per thread and turn, with the next turn's loads issued before this
 // turn's work: work(first chunk, chunks, how many of them exist); the others hold -inf.
-template <typename T, typename L, typename W>
+template <typename T, int U, typename L, typename W>
 __device__ __forceinline__ void stream_chunks(int n, L load, W work) {
-  constexpr int U = kDistillUnroll, kStep = kDistillThreads * U;
+  constexpr int kStep = kDistillThreads * U;
   uint4 a[U], b[U];
   const auto fetch = [&](int i0, uint4* to) {
 #pragma unroll
@@ -362,15 +368,15 @@ __device__ __forceinline__ void stream_chunks(int n, L load, W work) {
   }
 }
 // The gradient of a slice's whole chunks.
-template <typename T, bool kTwo>
+template <typename T, bool kTwo, int U>
 __device__ __forceinline__ void write_slice(const Slice<T>& s, T* dz, float m, const GradFactors& f) {
   const bool same_grid = (reinterpret_cast<uintptr_t>(dz) & 15u) == (reinterpret_cast<uintptr_t>(s.row.z) & 15u);
   uint4* out = reinterpret_cast<uint4*>(dz + s.row.first(s.mid_lo));
   const auto load = [&](int i) { return ld_stream(s.mid + i); };
   if (same_grid) {
-    stream_chunks<T>(s.n, load, [&](int i0, const uint4* a, int n) {
+    stream_chunks<T, U>(s.n, load, [&](int i0, const uint4* a, int n) {
 #pragma unroll
-      for (int u = 0; u < kDistillUnroll; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int i = i0 + u * kDistillThreads;
         if (i >= n) continue;
         float g[Logit<T>::kPer];
@@ -421,8 +427,8 @@ __device__ __forceinline__ GradFactors factors(const DistillParams& p, float g, 
 
 // Loss, and for a step the gradient in the same kernel: a row per block, or per cluster of blocks. kTwo: the softmax at
 // temperature 1 is needed beside the one at tau (label term, tau != 1).
-template <typename T, bool kTwo, bool kGradient>
-__global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(const __grid_constant__ DistillParams p, int cluster) {
+template <typename T, bool kTwo, bool kGradient, int U>
+__global__ void __launch_bounds__(kDistillThreads, distill_min_blocks(U)) distill_row_kernel(const __grid_constant__ DistillParams p, int cluster) {
   extern __shared__ uint4 dynamic[];
   __shared__ DistillShared sh;
   __shared__ uint32_t dead;
@@ -440,8 +446,8 @@ __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(const __gr
   bool some = false;
   if (kGradient || s.rank == 0) some = fetch_entries<T>(p, s.r, s.row.z, en);
   SoftSum mine = {-INFINITY, 0.0f, 0.0f};
-  stream_chunks<T>(s.n, [&](int i) { return kGradient ? s.mid[i] : ld_stream(s.mid + i); },
-                   [&](int, const uint4* a, int) { accumulate<T, kTwo, kDistillUnroll>(mine, a, k0, k1); });
+  stream_chunks<T, U>(s.n, [&](int i) { return kGradient ? s.mid[i] : ld_stream(s.mid + i); },
+                   [&](int, const uint4* a, int) { accumulate<T, kTwo, U>(mine, a, k0, k1); });
   s.edges([&](int, int64_t c) {
     const uint4 a = s.row.load(c);
     accumulate<T, kTwo, 1>(mine, &a, k0, k1);
@@ -468,7 +474,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(const __gr
     float a0, a1;
     const GradFactors f = factors<kTwo>(p, p.row_grad ? p.row_grad[s.r] : 1.0f, some, en.id[en.count] >= 0, l0, l1, &a0, &a1);
     T* dz = static_cast<T*>(p.dz) + s.r * p.dz_stride;
-    write_slice<T, kTwo>(s, dz, m, f);
+    write_slice<T, kTwo, U>(s, dz, m, f);
     s.edges([&](int, int64_t c) { write_values<T, kTwo>(s.row, dz, c, s.row.load(c), m, f); });
     __syncthreads();   // the stores above come before those at the entries
     write_entries<T, kTwo>(s, dz, en, m, f, a0, a1);
@@ -487,7 +493,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_gradient_kernel(const
   float a0, a1;
   const GradFactors f = factors<kTwo>(p, p.row_grad ? p.row_grad[s.r] : 1.0f, some, en.id[en.count] >= 0, l0, l1, &a0, &a1);
   T* dz = static_cast<T*>(p.dz) + s.r * p.dz_stride;
-  write_slice<T, kTwo>(s, dz, 0.0f, f);
+  write_slice<T, kTwo, kDistillUnroll>(s, dz, 0.0f, f);
   s.edges([&](int, int64_t c) { write_values<T, kTwo>(s.row, dz, c, s.row.load(c), 0.0f, f); });
   if (threadIdx.x < 32) {
     float unused = 0.0f;
@@ -595,10 +601,12 @@ int run_distill(slidedp_ctx* ctx, const slidedp_distill_args* a, int mode, const
 #define SLIDEDP_KERNEL(KERNEL, ...) \
   (f32 ? (two ? run(KERNEL<float, true __VA_ARGS__>) : run(KERNEL<float, false __VA_ARGS__>)) \
        : (two ? run(KERNEL<uint16_t, true __VA_ARGS__>) : run(KERNEL<uint16_t, false __VA_ARGS__>)))
-#define SLIDEDP_ALSO(x) , x
-  const cudaError_t e = mode == kForward    ? SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(false))
+#define SLIDEDP_ALSO(x, u) , x, u
+  const bool is_short = p.chunks_per_block * 16 <= kShortSliceBytes;
+  const cudaError_t e = mode == kForward    ? SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(false, kDistillUnroll))
                         : mode == kBackward ? SLIDEDP_KERNEL(distill_gradient_kernel)
-                                            : SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(true));
+                        : is_short          ? SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(true, kDistillUnrollShort))
+                                            : SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(true, kDistillUnroll));
 #undef SLIDEDP_ALSO
 #undef SLIDEDP_KERNEL
   if (e != cudaSuccess) return cuda_fail(ctx, e);
