@@ -11,6 +11,10 @@
  * Calls on one context may go to different streams, but workspaces must not be shared by calls
  * that can overlap.
  *
+ * The attention and distillation kernels wait on copies and on blocks of their own launch; every
+ * such wait is bounded. If one runs out, the results of that call are not complete and the next
+ * operator call on the context returns SLIDEDP_ERR_TIMEOUT (once).
+ *
  * BF16 and FP32 tensors need the alignment of their element only; 16-byte aligned bases and
  * strides are faster. All sums, norms and softmax statistics are FP32 and each output is rounded
  * once. Sizes of zero are no-ops.

@@ -298,6 +298,8 @@ __device__ __forceinline__ void load_floats(float* y, const float* from) {
 // probabilities) and their outputs. The issuer alternates between the tiles, so that one's products
 // run while the other's warpgroup exponentiates. A row's accumulators are rescaled only when its
 // maximum has grown by more than 2^8 since the last time.
+// One causal document of 8192 tokens, 32 + 8 heads of 128: 437 us, 1.26 PFLOP/s of the visible pairs, tensor pipe 64 %
+// active; what bounds it is the chain scores, softmax, products of a tile, of which two are in flight.
 
 template <int HALVES> struct ForwardShape {
   static constexpr int kStages = HALVES == 2 ? 2 : 4;
@@ -633,6 +635,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 // are, as they stand, the left operands of dV and dK. TMEM: S^T, dP^T (overwritten by P^T and dS^T, each
 // warpgroup within its own 64 columns), dV, dK. When there are few tiles of keys, a cluster of blocks shares an item, each
 // taking some of the group's query heads, and adds up through distributed shared memory.
+// The same document: 868 us, 1.27 PFLOP/s of its 8 head_dim flops per pair, tensor pipe 60 % active: the rows' work on P and
+// dS stands between the products of one step, and TMEM has no room for a second pair of S^T and dP^T.
 template <int HALVES> struct KeysShape {
   static constexpr int kStages = 2;
   static constexpr int kTileBytes = HALVES * kHalfBytes;
@@ -1001,7 +1005,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 
 // Queries: an item is 128 queries of one head, for which the block walks the keys that they see. Rows are queries; dS goes
 // where its scores were. TMEM: two buffers of scores (the next step's are made while this one's are
-// worked on), dP, dQ.
+// worked on), dP, dQ. The same document: 567 us, 1.46 PFLOP/s of its 6 head_dim flops per pair, tensor pipe 72 % active.
 template <int HALVES> struct QueriesShape {
   static constexpr int kKStages = 3;   // the next step's scores need K beside this step's dS K
   static constexpr int kVStages = HALVES == 2 ? 1 : 2;   // the stores' room; V comes back while the rows work on dP
