@@ -27,6 +27,7 @@ __global__ void __launch_bounds__(kGeneralThreads) attention_dkv_general_kernel(
 // row_lse[h][i] = lse log2 e, row_delta[h][i] = sum_d dout out, zeros for the rows of the padding: one warp per row.
 // Bound: HBM, one read of out and dout.
 __global__ void __launch_bounds__(kGeneralThreads) attention_rows_kernel(const __grid_constant__ AttnParams p) {
+  allow_next_kernel();   // the tensor-core kernel after it waits for its results itself
   const int64_t i = (int64_t)blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
   const int h = blockIdx.y;
   if (i >= p.pitch) return;
@@ -48,6 +49,7 @@ __global__ void __launch_bounds__(kGeneralThreads) attention_rows_kernel(const _
 // head per group of lanes. 8192 tokens, 32 heads of 128: 28 us against 48 of the kernel above.
 template <int L>
 __global__ void __launch_bounds__(kGeneralThreads) attention_rows_wide_kernel(const __grid_constant__ AttnParams p) {
+  allow_next_kernel();   // the tensor-core kernel after it waits for its results itself
   constexpr int kGroups = kGeneralThreads / L, U = 4;
   const int group = threadIdx.x / L, d = threadIdx.x % L * 8, h = blockIdx.y;
   const int64_t first = (int64_t)blockIdx.x * kGroups * U + group;

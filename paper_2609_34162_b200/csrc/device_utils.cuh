@@ -70,5 +70,7 @@ __device__ __forceinline__ void st_stream(void* p, uint4 v) {
 __device__ __forceinline__ void wait_for_previous_kernel() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
+// Lets a kernel launched that way start as soon as every block of this one has come here or ended.
+__device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 }  // namespace slidedp
