@@ -1,0 +1,115 @@
+// _marshal: the part of the Python binding that runs several times per argument of every operator call. It looks at
+// what the library cannot see of a tensor (type, device, shape, layout) and puts its address and strides where the C ABI
+// wants them. A tensor that is not as it should be goes to the binding's own Python functions, which say what is wrong with
+// it or accept it (subclasses of Tensor). One token through the norm operator, 8 tensors: 10.8 us a call with these checks
+// in Python, 9.6 in C through the tensors' Python attributes, 6.5 as here.
+#include <torch/csrc/Dtype.h>
+#include <torch/csrc/autograd/python_variable.h>
+#include <c10/cuda/CUDAStream.h>
+
+static PyObject *careful_flat, *careful_heads; // set by setup()
+
+typedef struct { // slidedp_heads
+  uint64_t data;
+  int64_t stride_token, stride_head;
+} heads_view;
+
+// Whether x is a Tensor or Parameter of this dtype and shape (a tuple, or None) on a GPU.
+static bool plain(PyObject* x, PyObject* dtype, PyObject* shape) {
+  if (!THPVariable_CheckExact(x) || !THPDtype_Check(dtype)) return false;
+  const at::Tensor& t = THPVariable_Unpack(x);
+  if (t.scalar_type() != reinterpret_cast<THPDtype*>(dtype)->scalar_type || !t.is_cuda()) return false;
+  if (shape == Py_None) return true;
+  if (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != t.dim()) return false;
+  for (int64_t i = 0; i < t.dim(); ++i) {
+    if (PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i)) == t.size(i)) continue;
+    PyErr_Clear();
+    return false;
+  }
+  return true;
+}
+
+// flat(x, what, dtype, shape or None): address of a contiguous tensor
+static PyObject* flat(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 3 && n != 4) return PyErr_Format(PyExc_TypeError, "flat takes 3 or 4 arguments");
+  PyObject *x = args[0], *shape = n == 4 ? args[3] : Py_None;
+  if (plain(x, args[2], shape) && THPVariable_Unpack(x).is_contiguous()) return PyLong_FromVoidPtr(THPVariable_Unpack(x).data_ptr());
+  return PyObject_CallFunctionObjArgs(careful_flat, x, args[1], args[2], shape, NULL);
+}
+
+static bool view_of(PyObject* x, PyObject* what, PyObject* dtype, PyObject* shape, heads_view* v) {
+  if (plain(x, dtype, shape)) {
+    const at::Tensor& t = THPVariable_Unpack(x);
+    if (t.dim() == 3 && t.stride(2) == 1) {
+      *v = heads_view{reinterpret_cast<uint64_t>(t.data_ptr()), t.stride(0), t.stride(1)};
+      return true;
+    }
+  }
+  PyObject* r = PyObject_CallFunctionObjArgs(careful_heads, x, what, dtype, shape, NULL);
+  if (!r) return false;
+  unsigned long long data;
+  long long a, b;
+  const bool got = PyArg_ParseTuple(r, "KLL", &data, &a, &b);
+  Py_DECREF(r);
+  if (got) *v = heads_view{data, a, b};
+  return got;
+}
+
+// heads(at, dtype, shape, x0, what0, x1, what1, ..): the tensors' views, one after the other from address `at` on
+static PyObject* heads(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n < 3 || n % 2 == 0) return PyErr_Format(PyExc_TypeError, "heads takes an address, a dtype, a shape and pairs");
+  heads_view* out = static_cast<heads_view*>(PyLong_AsVoidPtr(args[0]));
+  if (PyErr_Occurred()) return NULL;
+  for (Py_ssize_t i = 3; i < n; i += 2)
+    if (!view_of(args[i], args[i + 1], args[1], args[2], out++)) return NULL;
+  Py_RETURN_NONE;
+}
+
+// block(): address of this thread's argument block, free for use until its next call
+static PyObject* block(PyObject*, PyObject*) {
+  static thread_local uint64_t bytes[64];
+  return PyLong_FromVoidPtr(bytes);
+}
+
+// current_stream(): the handle of torch's current stream on the current device
+static PyObject* current_stream(PyObject*, PyObject*) { return PyLong_FromVoidPtr(c10::cuda::getCurrentCUDAStream().stream()); }
+
+// setup(function for flat, function for heads)
+static PyObject* setup(PyObject*, PyObject* args) {
+  PyObject *f, *h;
+  if (!PyArg_ParseTuple(args, "OO", &f, &h)) return NULL;
+  Py_INCREF(f);
+  Py_INCREF(h);
+  Py_XSETREF(careful_flat, f);
+  Py_XSETREF(careful_heads, h);
+  Py_RETURN_NONE;
+}
+
+// No C++ exception leaves a function called by the interpreter.
+template <typename F>
+static PyObject* guarded(F f) {
+  try {
+    return f();
+  } catch (const std::exception& e) {
+    return PyErr_Format(PyExc_RuntimeError, "%s", e.what());
+  }
+}
+static PyObject* py_flat(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&] { return flat(self, args, n); });
+}
+static PyObject* py_heads(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&] { return heads(self, args, n); });
+}
+static PyObject* py_current_stream(PyObject* self, PyObject* none) {
+  return guarded([&] { return current_stream(self, none); });
+}
+
+static PyMethodDef methods[] = {{"flat", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_flat)), METH_FASTCALL, NULL},
+                                {"heads", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_heads)), METH_FASTCALL, NULL},
+                                {"block", block, METH_NOARGS, NULL},
+                                {"current_stream", py_current_stream, METH_NOARGS, NULL},
+                                {"setup", setup, METH_VARARGS, NULL},
+                                {NULL, NULL, 0, NULL}};
+static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
+
+PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module); }

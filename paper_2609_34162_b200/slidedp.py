@@ -22,6 +22,11 @@ if not os.path.exists(LIB_PATH):
         f"{LIB_PATH} is missing: build it with `python -m paper_2609_34162_b200.build` "
         "(nvcc, sm_100a). libslidedp has no CPU fallback.")
 
+try:
+    from . import _marshal
+except ImportError as e:
+    raise ImportError("the binding's _marshal module is missing: build it with `python -m paper_2609_34162_b200.build`") from e
+
 _lib = ctypes.CDLL(LIB_PATH)
 
 MAX_RANKS = 16
@@ -174,20 +179,20 @@ class _DistillArgs(ctypes.Structure):
                 ("temperature", ctypes.c_double), ("w_teacher", ctypes.c_double), ("w_label", ctypes.c_double)]
 
 
-_qp, _ap, _dp = (ctypes.POINTER(t) for t in (_QkArgs, _AttnArgs, _DistillArgs))
-_HEADS = 24                                     # sizeof(slidedp_heads): address and two strides
-_pack_heads = {n: struct.Struct("@" + "Qqq" * n).pack_into for n in (4, 6, 8)}
-# views are passed as addresses of the context's argument block (_HEADS bytes each)
+# A call's views (slidedp_heads: an address and two strides, _V bytes each) are written to the calling thread's argument block
+# and passed as addresses there; the scalar arguments go as the bytes of their struct (a ctypes object costs three times that).
+_V = 24
+_qk_bytes, _attn_bytes, _distill_bytes = (struct.Struct(f).pack for f in ("@qiiiiiiqd", "@qiiiiiiPPPdd", "@qqiiqqddd"))
 for _name, _res, _args in (
-        ("slidedp_qk_norm_rope", ctypes.c_int, [_vp, _qp] + [_vp] * 9),
-        ("slidedp_qk_norm_rope_backward", ctypes.c_int, [_vp, _qp] + [_vp] * 14),
-        ("slidedp_qk_norm_rope_workspace", ctypes.c_size_t, [_qp]),
-        ("slidedp_attention", ctypes.c_int, [_vp, _ap] + [_vp] * 6),
-        ("slidedp_attention_backward", ctypes.c_int, [_vp, _ap] + [_vp] * 11),
-        ("slidedp_attention_workspace", ctypes.c_size_t, [_ap]),
-        ("slidedp_distill_loss", ctypes.c_int, [_vp, _dp] + [_vp] * 7),
-        ("slidedp_distill_loss_backward", ctypes.c_int, [_vp, _dp] + [_vp] * 8),
-        ("slidedp_distill_step", ctypes.c_int, [_vp, _dp] + [_vp] * 9)):
+        ("slidedp_qk_norm_rope", ctypes.c_int, [_vp, _vp] + [_vp] * 9),
+        ("slidedp_qk_norm_rope_backward", ctypes.c_int, [_vp, _vp] + [_vp] * 14),
+        ("slidedp_qk_norm_rope_workspace", ctypes.c_size_t, [_vp]),
+        ("slidedp_attention", ctypes.c_int, [_vp, _vp] + [_vp] * 6),
+        ("slidedp_attention_backward", ctypes.c_int, [_vp, _vp] + [_vp] * 11),
+        ("slidedp_attention_workspace", ctypes.c_size_t, [_vp]),
+        ("slidedp_distill_loss", ctypes.c_int, [_vp, _vp] + [_vp] * 7),
+        ("slidedp_distill_loss_backward", ctypes.c_int, [_vp, _vp] + [_vp] * 8),
+        ("slidedp_distill_step", ctypes.c_int, [_vp, _vp] + [_vp] * 9)):
     getattr(_lib, _name).restype, getattr(_lib, _name).argtypes = _res, _args
 
 
@@ -222,8 +227,8 @@ def _grad_array(grads):
 
 
 def _stream(stream) -> int:
-    if stream is None:       # the current stream's handle, without building a Stream object around it
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    if stream is None:
+        return _marshal.current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -240,25 +245,27 @@ def _refuse(x, what: str, dtype, shape):
     raise ValueError(f"{what} must be contiguous")
 
 
-# The library sees addresses only; these look at what it cannot: type, shape, device and layout. They run once or
-# more per argument of every call, and are written to touch each property of a tensor once.
+# The library sees addresses only; these look at what it cannot: type, shape, device and layout. _marshal has their fast
+# paths and calls them for tensors that need a second look.
 
-def _flat(x, what: str, dtype, shape=None) -> int:
+def _as_tensor(x):
+    return x.as_subclass(torch.Tensor) if isinstance(x, torch.Tensor) else x
+
+
+def _careful_flat(x, what: str, dtype, shape=None) -> int:
     """Address of a contiguous tensor."""
-    if (type(x) not in _TENSORS or x.dtype is not dtype or not x.is_cuda or not x.is_contiguous()
+    x = _as_tensor(x)
+    if (not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or not x.is_contiguous()
             or (shape is not None and x.shape != shape)):
-        if type(x) in _TENSORS or not isinstance(x, torch.Tensor):
-            _refuse(x, what, dtype, shape)
-        return _flat(x.as_subclass(torch.Tensor), what, dtype, shape)
+        _refuse(x, what, dtype, shape)
     return x.data_ptr()
 
 
-def _heads(x, what: str, dtype, shape):
+def _careful_heads(x, what: str, dtype, shape):
     """Address and strides of a [tokens, heads, head_dim] tensor whose last axis is contiguous."""
-    if type(x) not in _TENSORS or x.dtype is not dtype or not x.is_cuda or x.shape != shape:
-        if type(x) in _TENSORS or not isinstance(x, torch.Tensor):
-            _refuse(x, what, dtype, shape)
-        return _heads(x.as_subclass(torch.Tensor), what, dtype, shape)
+    x = _as_tensor(x)
+    if not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or x.shape != shape:
+        _refuse(x, what, dtype, shape)
     t, h, d = x.stride()
     if d != 1 and shape[2] > 1:
         raise ValueError(f"the last axis of {what} must be contiguous")
@@ -275,7 +282,8 @@ def _matrix(x, what: str, dtype, shape) -> int:
     return t if shape[0] > 1 else shape[1]
 
 
-_TENSORS = (torch.Tensor, torch.nn.Parameter)
+_marshal.setup(_careful_flat, _careful_heads)
+_flat, _heads, _block = _marshal.flat, _marshal.heads, _marshal.block
 
 
 def _workspace(x, nbytes: int) -> int:
@@ -302,9 +310,6 @@ class Context:
             self._h = _vp()
             raise SlideDPError(rc)
         self.device = device
-        self._views = ctypes.create_string_buffer(8 * _HEADS)      # slidedp_heads of the call being made
-        at = ctypes.addressof(self._views)
-        self._at = [at + i * _HEADS for i in range(8)]
 
     def _check(self, rc: int):
         if rc != OK:
@@ -492,7 +497,7 @@ class Context:
         if dtype not in _DTYPES:
             raise TypeError("q and k must be bfloat16 or float32")
         rows, rope = cos_sin.shape if cos_sin is not None else (0, 0)
-        return _QkArgs(qs[0], qs[1], ks[1], qs[2], rope, bool(interleaved), _DTYPES[dtype], rows, eps)
+        return _qk_bytes(qs[0], qs[1], ks[1], qs[2], rope, bool(interleaved), _DTYPES[dtype], rows, eps)
 
     @staticmethod
     def _qk_tables(qs, dtype, w_q, w_k, cos_sin, positions):
@@ -506,12 +511,12 @@ class Context:
         """RMS norm of every head of ``q`` and ``k`` ([tokens, heads, head_dim]) and the rotation by
         ``cos_sin`` ([rows, rope_dim]: cosines, then sines; None: no rotation) at ``positions``
         (int32 per token; None: 0, 1, ..)."""
-        (qs, ks), dt, at = _two_sides(q, k), q.dtype, self._at
-        a = self._qk_args(qs, ks, dt, cos_sin, eps, interleaved)
-        _pack_heads[4](self._views, 0, *_heads(q, "q", dt, qs), *_heads(k, "k", dt, ks), *_heads(q_out, "q_out", dt, qs),
-                       *_heads(k_out, "k_out", dt, ks))
-        rc = _lib.slidedp_qk_norm_rope(self._h, a, at[0], at[1], *self._qk_tables(qs, dt, w_q, w_k, cos_sin, positions),
-                                       at[2], at[3], _stream(stream))
+        (qs, ks), dt, at = _two_sides(q, k), q.dtype, _block()
+        _heads(at, dt, qs, q, "q", q_out, "q_out")
+        _heads(at + 2 * _V, dt, ks, k, "k", k_out, "k_out")
+        rc = _lib.slidedp_qk_norm_rope(self._h, self._qk_args(qs, ks, dt, cos_sin, eps, interleaved), at, at + 2 * _V,
+                                       *self._qk_tables(qs, dt, w_q, w_k, cos_sin, positions), at + _V, at + 3 * _V,
+                                       _stream(stream))
         if rc:
             self._check(rc)
 
@@ -523,15 +528,16 @@ class Context:
                                       dw_k, workspace, eps: float = 1e-6, interleaved: bool = False,
                                       stream=None) -> None:
         """Gradients ``dq``, ``dk`` and (float32, may be None) ``dw_q``, ``dw_k`` from those of the outputs."""
-        (qs, ks), dt, at = _two_sides(q, k), q.dtype, self._at
+        (qs, ks), dt, at = _two_sides(q, k), q.dtype, _block()
         a = self._qk_args(qs, ks, dt, cos_sin, eps, interleaved)
         D, f32, ws = (qs[2],), torch.float32, None
         if dw_q is not None or dw_k is not None:
             ws = _workspace(workspace, _lib.slidedp_qk_norm_rope_workspace(a))
-        _pack_heads[6](self._views, 0, *_heads(q, "q", dt, qs), *_heads(k, "k", dt, ks), *_heads(dq_out, "dq_out", dt, qs),
-                       *_heads(dk_out, "dk_out", dt, ks), *_heads(dq, "dq", dt, qs), *_heads(dk, "dk", dt, ks))
+        _heads(at, dt, qs, q, "q", dq_out, "dq_out", dq, "dq")
+        ak = at + 3 * _V
+        _heads(ak, dt, ks, k, "k", dk_out, "dk_out", dk, "dk")
         rc = _lib.slidedp_qk_norm_rope_backward(
-            self._h, a, at[0], at[1], *self._qk_tables(qs, dt, w_q, w_k, cos_sin, positions), at[2], at[3], at[4], at[5],
+            self._h, a, at, ak, *self._qk_tables(qs, dt, w_q, w_k, cos_sin, positions), at + _V, ak + _V, at + 2 * _V, ak + 2 * _V,
             None if dw_q is None else _flat(dw_q, "dw_q", f32, D), None if dw_k is None else _flat(dw_k, "dw_k", f32, D),
             ws, _stream(stream))
         if rc:
@@ -540,27 +546,27 @@ class Context:
     @staticmethod
     def _attn_args(qs, ks, cu_docs=None, prefix=None, slopes=None, causal=True, scale=None, softcap=0.0):
         T, H, D = qs
-        docs, cu = 1, None
+        docs, cu = 1, 0
         if cu_docs is not None:
             cu = _flat(cu_docs, "cu_docs", torch.int32)
             if cu_docs.dim() != 1 or cu_docs.numel() < 1:
                 raise ValueError("cu_docs must hold docs + 1 offsets")
             docs = cu_docs.numel() - 1
-        return _AttnArgs(T, H, ks[1], D, bool(causal), docs, 0, cu,
-                         None if prefix is None else _flat(prefix, "prefix", torch.int32, (docs,)) or None,
-                         None if slopes is None else _flat(slopes, "slopes", torch.float32, (H,)),
-                         D ** -0.5 if scale is None else scale, softcap)
+        return _attn_bytes(T, H, ks[1], D, bool(causal), docs, 0, cu,
+                           0 if prefix is None else _flat(prefix, "prefix", torch.int32, (docs,)),
+                           0 if slopes is None else _flat(slopes, "slopes", torch.float32, (H,)),
+                           D ** -0.5 if scale is None else scale, softcap)
 
     def slidedp_attention(self, q, k, v, out, lse, cu_docs=None, prefix=None, slopes=None, causal: bool = True,
                           scale: float | None = None, softcap: float = 0.0, stream=None) -> None:
         """Attention of ``q`` [tokens, heads_q, head_dim] over ``k``, ``v`` [tokens, heads_kv, head_dim] within
         packed documents (``cu_docs``: int32 offsets; None: one document). Fills ``out`` and ``lse``
         [heads_q, tokens]. ``scale`` defaults to head_dim ** -0.5."""
-        (qs, ks), bf, at = _two_sides(q, k), torch.bfloat16, self._at
+        (qs, ks), bf, at = _two_sides(q, k), torch.bfloat16, _block()
         a = self._attn_args(qs, ks, cu_docs, prefix, slopes, causal, scale, softcap)
-        _pack_heads[4](self._views, 0, *_heads(q, "q", bf, qs), *_heads(k, "k", bf, ks), *_heads(v, "v", bf, ks),
-                       *_heads(out, "out", bf, qs))
-        rc = _lib.slidedp_attention(self._h, a, at[0], at[1], at[2], at[3], _flat(lse, "lse", torch.float32, (qs[1], qs[0])),
+        _heads(at, bf, qs, q, "q", out, "out")
+        _heads(at + 2 * _V, bf, ks, k, "k", v, "v")
+        rc = _lib.slidedp_attention(self._h, a, at, at + 2 * _V, at + 3 * _V, at + _V, _flat(lse, "lse", torch.float32, (qs[1], qs[0])),
                                     _stream(stream))
         if rc:
             self._check(rc)
@@ -573,15 +579,17 @@ class Context:
                                    slopes=None, causal: bool = True, scale: float | None = None,
                                    softcap: float = 0.0, stream=None) -> None:
         """Gradients ``dq``, ``dk``, ``dv`` from ``d_out``, with the forward's ``out`` and ``lse``."""
-        (qs, ks), bf, at = _two_sides(q, k), torch.bfloat16, self._at
+        (qs, ks), bf, at = _two_sides(q, k), torch.bfloat16, _block()
         a = self._attn_args(qs, ks, cu_docs, prefix, slopes, causal, scale, softcap)
         ws = _workspace(workspace, _lib.slidedp_attention_workspace(a))
-        _pack_heads[8](self._views, 0, *_heads(q, "q", bf, qs), *_heads(k, "k", bf, ks), *_heads(v, "v", bf, ks),
-                       *_heads(out, "out", bf, qs), *_heads(d_out, "d_out", bf, qs), *_heads(dq, "dq", bf, qs),
-                       *_heads(dk, "dk", bf, ks), *_heads(dv, "dv", bf, ks))
-        self._check(_lib.slidedp_attention_backward(
-            self._h, a, at[0], at[1], at[2], at[3], _flat(lse, "lse", torch.float32, (qs[1], qs[0])), at[4], at[5], at[6],
-            at[7], ws, _stream(stream)))
+        _heads(at, bf, qs, q, "q", out, "out", d_out, "d_out", dq, "dq")
+        ak = at + 4 * _V
+        _heads(ak, bf, ks, k, "k", v, "v", dk, "dk", dv, "dv")
+        rc = _lib.slidedp_attention_backward(
+            self._h, a, at, ak, ak + _V, at + _V, _flat(lse, "lse", torch.float32, (qs[1], qs[0])), at + 2 * _V, at + 3 * _V,
+            ak + 2 * _V, ak + 3 * _V, ws, _stream(stream))
+        if rc:
+            self._check(rc)
 
     @staticmethod
     def _distill_call(logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits, temperature, w_teacher,
@@ -593,8 +601,8 @@ class Context:
         dt, shape, f32, i32 = logits.dtype, logits.shape, torch.float32, torch.int32
         rows, vocab = shape
         entries = teacher_ids.shape[-1]
-        a = _DistillArgs(rows, vocab, entries, _DTYPES[dt], _matrix(logits, "logits", dt, shape),
-                         0 if d_logits is None else _matrix(d_logits, "d_logits", dt, shape), temperature, w_teacher, w_label)
+        a = _distill_bytes(rows, vocab, entries, _DTYPES[dt], _matrix(logits, "logits", dt, shape),
+                           0 if d_logits is None else _matrix(d_logits, "d_logits", dt, shape), temperature, w_teacher, w_label)
         return (a, (logits.data_ptr(), _flat(teacher_ids, "teacher_ids", i32, (rows, entries)),
                     _flat(teacher_logits, "teacher_logits", f32, (rows, entries)),
                     None if labels is None else _flat(labels, "labels", i32, (rows,))),
@@ -606,8 +614,9 @@ class Context:
         stored entries (int32 ids, float32 logits, both [rows, entries]) and int32 ``labels`` (may be None)."""
         a, ins, l, _ = self._distill_call(logits, teacher_ids, teacher_logits, labels, lse, None, None, temperature,
                                           w_teacher, w_label)
-        self._check(_lib.slidedp_distill_loss(self._h, a, *ins, _flat(loss, "loss", torch.float32, (a.rows,)), l,
-                                              _stream(stream)))
+        rc = _lib.slidedp_distill_loss(self._h, a, *ins, _flat(loss, "loss", torch.float32, logits.shape[:1]), l, _stream(stream))
+        if rc:
+            self._check(rc)
 
     def slidedp_distill_loss_backward(self, logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits,
                                       temperature: float = 1.0, w_teacher: float = 1.0, w_label: float = 0.0,
@@ -624,7 +633,7 @@ class Context:
         """``loss``, ``lse`` and ``d_logits`` in one pass over the logits."""
         a, ins, l, g = self._distill_call(logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits,
                                           temperature, w_teacher, w_label)
-        self._check(_lib.slidedp_distill_step(self._h, a, *ins, g, _flat(loss, "loss", torch.float32, (a.rows,)), l,
+        self._check(_lib.slidedp_distill_step(self._h, a, *ins, g, _flat(loss, "loss", torch.float32, logits.shape[:1]), l,
                                               d_logits.data_ptr(), _stream(stream)))
 
 
