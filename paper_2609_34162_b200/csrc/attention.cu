@@ -12,14 +12,17 @@ constexpr int kGeneralThreads = 128;
 // aligned, which TMA cannot address.
 
 __global__ void __launch_bounds__(kGeneralThreads) attention_forward_general_kernel(const __grid_constant__ AttnParams p) {
+  start_after_previous_kernel();
   const int i = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
   if (i < p.tokens) attention_out_row(p, i, blockIdx.y, true);
 }
 __global__ void __launch_bounds__(kGeneralThreads) attention_dq_general_kernel(const __grid_constant__ AttnParams p) {
+  start_after_previous_kernel();
   const int i = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
   if (i < p.tokens) attention_dq_row(p, i, blockIdx.y, 0, p.head_dim);
 }
 __global__ void __launch_bounds__(kGeneralThreads) attention_dkv_general_kernel(const __grid_constant__ AttnParams p) {
+  start_after_previous_kernel();
   const int j = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
   if (j < p.tokens) attention_dkv_row(p, j, blockIdx.y, true, true, 0, p.head_dim);
 }
@@ -27,7 +30,7 @@ __global__ void __launch_bounds__(kGeneralThreads) attention_dkv_general_kernel(
 // row_lse[h][i] = lse log2 e, row_delta[h][i] = sum_d dout out, zeros for the rows of the padding: one warp per row.
 // Bound: HBM, one read of out and dout.
 __global__ void __launch_bounds__(kGeneralThreads) attention_rows_kernel(const __grid_constant__ AttnParams p) {
-  allow_next_kernel();   // the tensor-core kernel after it waits for its results itself
+  start_after_previous_kernel();
   const int64_t i = (int64_t)blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
   const int h = blockIdx.y;
   if (i >= p.pitch) return;
@@ -49,7 +52,7 @@ __global__ void __launch_bounds__(kGeneralThreads) attention_rows_kernel(const _
 // head per group of lanes. 8192 tokens, 32 heads of 128: 28 us against 48 of the kernel above.
 template <int L>
 __global__ void __launch_bounds__(kGeneralThreads) attention_rows_wide_kernel(const __grid_constant__ AttnParams p) {
-  allow_next_kernel();   // the tensor-core kernel after it waits for its results itself
+  start_after_previous_kernel();
   constexpr int kGroups = kGeneralThreads / L, U = 4;
   const int group = threadIdx.x / L, d = threadIdx.x % L * 8, h = blockIdx.y;
   const int64_t first = (int64_t)blockIdx.x * kGroups * U + group;
@@ -160,7 +163,7 @@ int slidedp_attention(slidedp_ctx* ctx, const slidedp_attn_args* a, const slided
       tma_view(v, p.tokens, p.heads_kv) && tma_view(out, p.tokens, p.heads_q))
     return attention_forward_mma(ctx, p, st);
   FAULT_POINT();
-  attention_forward_general_kernel<<<dim3(general_blocks(p.tokens), p.heads_q), kGeneralThreads, 0, st>>>(p);
+  launch_after(attention_forward_general_kernel, dim3(general_blocks(p.tokens), p.heads_q), kGeneralThreads, 0, 1, st, p);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;
@@ -200,11 +203,11 @@ int slidedp_attention_backward(slidedp_ctx* ctx, const slidedp_attn_args* a, con
     const int lanes = p.head_dim <= 64 ? 8 : p.head_dim <= 128 ? 16 : 32;
     const int64_t per_block = (int64_t)kGeneralThreads / lanes * 4;
     const dim3 grid((unsigned)((p.pitch + per_block - 1) / per_block), p.heads_q);
-    if (lanes == 8) attention_rows_wide_kernel<8><<<grid, kGeneralThreads, 0, st>>>(p);
-    else if (lanes == 16) attention_rows_wide_kernel<16><<<grid, kGeneralThreads, 0, st>>>(p);
-    else attention_rows_wide_kernel<32><<<grid, kGeneralThreads, 0, st>>>(p);
+    if (lanes == 8) launch_after(attention_rows_wide_kernel<8>, grid, kGeneralThreads, 0, 1, st, p);
+    else if (lanes == 16) launch_after(attention_rows_wide_kernel<16>, grid, kGeneralThreads, 0, 1, st, p);
+    else launch_after(attention_rows_wide_kernel<32>, grid, kGeneralThreads, 0, 1, st, p);
   } else {
-    attention_rows_kernel<<<dim3(general_blocks(p.pitch), p.heads_q), kGeneralThreads, 0, st>>>(p);
+    launch_after(attention_rows_kernel, dim3(general_blocks(p.pitch), p.heads_q), kGeneralThreads, 0, 1, st, p);
   }
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
@@ -213,11 +216,11 @@ int slidedp_attention_backward(slidedp_ctx* ctx, const slidedp_attn_args* a, con
       tma_view(dk, p.tokens, p.heads_kv) && tma_view(dv, p.tokens, p.heads_kv))
     return attention_backward_mma(ctx, p, st);
   FAULT_POINT();
-  attention_dq_general_kernel<<<dim3(general_blocks(p.tokens), p.heads_q), kGeneralThreads, 0, st>>>(p);
+  launch_after(attention_dq_general_kernel, dim3(general_blocks(p.tokens), p.heads_q), kGeneralThreads, 0, 1, st, p);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   FAULT_POINT();
-  attention_dkv_general_kernel<<<dim3(general_blocks(p.tokens), p.heads_kv), kGeneralThreads, 0, st>>>(p);
+  launch_after(attention_dkv_general_kernel, dim3(general_blocks(p.tokens), p.heads_kv), kGeneralThreads, 0, 1, st, p);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;

@@ -359,6 +359,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     ctl.dead = 0;
     mbar_init_fence();
   }
+  wait_for_previous_kernel();   // (letting the next kernel in early cost more than it gave: prefixes and caps 67 -> 74 us)
   ctl.docs.fill(p.mask);
   if (warp == 8) tmem_alloc(smem_addr(&ctl.tmem), kTmemColumns);
   tc_fence_before();
@@ -697,11 +698,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     ctl.dead = 0;
     mbar_init_fence();
   }
+  wait_for_previous_kernel();
+  allow_next_kernel();   // the queries' kernel, which needs what was there before this one
   ctl.docs.fill(p.mask);
   if (warp == 8) tmem_alloc(smem_addr(&ctl.tmem), kTmemColumns);
   tc_fence_before();
-  wait_for_previous_kernel();   // the rows' statistics
-  allow_next_kernel();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = ctl.tmem, at_s = tmem, at_dp = tmem + 128, at_dv = tmem + 256, at_dk = tmem + 384;
@@ -1329,7 +1330,7 @@ static int forward(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
   CU(allow_smem(attention_forward_mma_kernel<HALVES, MODE>, ForwardShape<HALVES>::kSmem, &ready, ctx->device));
   const int64_t blocks = (int64_t)((p.tokens + 2 * kTile - 1) / (2 * kTile)) * p.heads_q;
   if (blocks > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
-  attention_forward_mma_kernel<HALVES, MODE><<<(unsigned)blocks, kMmaThreads, ForwardShape<HALVES>::kSmem, st>>>(p, q, k, v, o);
+  launch_after(attention_forward_mma_kernel<HALVES, MODE>, (unsigned)blocks, kMmaThreads, ForwardShape<HALVES>::kSmem, 1, st, p, q, k, v, o);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;
@@ -1348,31 +1349,17 @@ static int backward(slidedp_ctx* ctx, const AttnParams& p, cudaStream_t st) {
   const int64_t tiles = (p.tokens + kTile - 1) / kTile;
   if (tiles * p.heads_q > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
   const int split = key_split(tiles * p.heads_kv, p.group, HALVES);
-  // The keys' kernel is set up while the one with the rows' statistics ends. The queries' kernel needs nothing of the keys'
-  // kernel and may start once all blocks of that have (it has then passed its own wait), on SMs that run out of tiles; its
-  // blocks end after it. Backward pass of 4099 tokens with prefixes 148 -> 121 us, of 1000 tokens, 8 heads 43 -> 29.
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)split;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(kMmaThreads);
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.gridDim = dim3((unsigned)(tiles * p.heads_kv * split));
-  cfg.dynamicSmemBytes = KeysShape<HALVES>::kSmem;
-  cfg.numAttrs = split > 1 ? 2 : 1;
+  // The queries' kernel needs nothing of the keys' kernel and may start once all blocks of that have passed their wait, on SMs
+  // that run out of tiles; its blocks end after it. Backward pass of 4099 tokens with prefixes 148 -> 121 us, of 1000
+  // tokens, 8 heads 43 -> 29.
   FAULT_POINT();
-  (void)cudaLaunchKernelEx(&cfg, attention_dkv_mma_kernel<HALVES, MODE>, p, q, k, v, d, dk, dv, split);
+  launch_after(attention_dkv_mma_kernel<HALVES, MODE>, (unsigned)(tiles * p.heads_kv * split), kMmaThreads, KeysShape<HALVES>::kSmem, split, st,
+               p, q, k, v, d, dk, dv, split);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
-  cfg.gridDim = dim3((unsigned)(tiles * p.heads_q));
-  cfg.dynamicSmemBytes = QueriesShape<HALVES>::kSmem;
-  cfg.numAttrs = 1;
   FAULT_POINT();
-  (void)cudaLaunchKernelEx(&cfg, attention_dq_mma_kernel<HALVES, MODE>, p, q, k, v, d, dq);
+  launch_after(attention_dq_mma_kernel<HALVES, MODE>, (unsigned)(tiles * p.heads_q), kMmaThreads, QueriesShape<HALVES>::kSmem, 1, st, p, q, k, v, d,
+               dq);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;

@@ -72,5 +72,10 @@ __device__ __forceinline__ void wait_for_previous_kernel() {
 }
 // Lets a kernel launched that way start as soon as every block of this one has come here or ended.
 __device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// For kernels that have nothing to do before their first access to memory.
+__device__ __forceinline__ void start_after_previous_kernel() {
+  allow_next_kernel();
+  wait_for_previous_kernel();
+}
 
 }  // namespace slidedp

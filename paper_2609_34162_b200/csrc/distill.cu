@@ -432,6 +432,7 @@ __global__ void __launch_bounds__(kDistillThreads, distill_min_blocks(U)) distil
   extern __shared__ uint4 dynamic[];
   __shared__ DistillShared sh;
   __shared__ uint32_t dead;
+  allow_next_kernel();
   if (cluster > 1) {
     if (threadIdx.x == 0) {
       mbar_init(smem_addr(&sh.exchanged), 1);
@@ -440,6 +441,7 @@ __global__ void __launch_bounds__(kDistillThreads, distill_min_blocks(U)) distil
     }
     cluster_sync();
   }
+  wait_for_previous_kernel();
   const Slice<T> s(p, cluster, blockIdx.x % cluster, blockIdx.x / cluster);
   const Entries en(dynamic, p.entries);
   const float k0 = p.inv_tau * kLog2e, k1 = kLog2e;
@@ -485,6 +487,7 @@ __global__ void __launch_bounds__(kDistillThreads, distill_min_blocks(U)) distil
 // Gradient from the saved lse: blocks of a row share nothing.
 template <typename T, bool kTwo>
 __global__ void __launch_bounds__(kDistillThreads) distill_gradient_kernel(const __grid_constant__ DistillParams p, int parts) {
+  start_after_previous_kernel();
   extern __shared__ uint4 dynamic[];
   const Slice<T> s(p, parts, blockIdx.x % parts, blockIdx.x / parts);
   const Entries en(dynamic, p.entries);
@@ -518,22 +521,6 @@ int check_distill(const slidedp_distill_args* a) {
       !is_finite(a->w_label))
     return SLIDEDP_ERR_INVALID_ARG;
   return SLIDEDP_OK;
-}
-
-template <typename K>
-cudaError_t launch_distill(K kernel, const DistillParams& p, unsigned parts, bool clustered, size_t smem, cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)p.rows * parts);
-  cfg.blockDim = dim3(kDistillThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = parts;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = clustered && parts > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, p, (int)parts);
 }
 
 // Blocks per row: one when the rows fill the device; when they do not, a row is cut, down to 8 KB. A step also cuts
@@ -597,19 +584,20 @@ int run_distill(slidedp_ctx* ctx, const slidedp_distill_args* a, int mode, const
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());
   const size_t smem = Entries::bytes(a->entries);
   FAULT_POINT();
-  const auto run = [&](auto kernel) { return launch_distill(kernel, p, cluster, mode != kBackward, smem, st); };
+  const auto run = [&](auto kernel) {
+    launch_after(kernel, (unsigned)(p.rows * cluster), kDistillThreads, smem, mode == kBackward ? 1 : cluster, st, p, (int)cluster);
+  };
 #define SLIDEDP_KERNEL(KERNEL, ...) \
   (f32 ? (two ? run(KERNEL<float, true __VA_ARGS__>) : run(KERNEL<float, false __VA_ARGS__>)) \
        : (two ? run(KERNEL<uint16_t, true __VA_ARGS__>) : run(KERNEL<uint16_t, false __VA_ARGS__>)))
 #define SLIDEDP_ALSO(x, u) , x, u
   const bool is_short = p.chunks_per_block * 16 <= kShortSliceBytes;
-  const cudaError_t e = mode == kForward    ? SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(false, kDistillUnroll))
-                        : mode == kBackward ? SLIDEDP_KERNEL(distill_gradient_kernel)
-                        : is_short          ? SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(true, kDistillUnrollShort))
-                                            : SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(true, kDistillUnroll));
+  if (mode == kForward) SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(false, kDistillUnroll));
+  else if (mode == kBackward) SLIDEDP_KERNEL(distill_gradient_kernel);
+  else if (is_short) SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(true, kDistillUnrollShort));
+  else SLIDEDP_KERNEL(distill_row_kernel, SLIDEDP_ALSO(true, kDistillUnroll));
 #undef SLIDEDP_ALSO
 #undef SLIDEDP_KERNEL
-  if (e != cudaSuccess) return cuda_fail(ctx, e);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;

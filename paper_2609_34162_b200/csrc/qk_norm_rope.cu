@@ -317,6 +317,7 @@ __global__ void __launch_bounds__(kQkThreads, BACK ? kQkBackwardPerSM : kQkForwa
       ahead.advance(by_t, by_c, chunks);
     }
   };
+  start_after_previous_kernel();
 #pragma unroll
   for (int k = 0; k < kStages - 1; ++k) fetch(k);
 
@@ -435,6 +436,7 @@ __global__ void __launch_bounds__(kQkThreads, BACK ? kQkBackwardPerSM : kQkForwa
 
 template <typename T>
 __global__ void __launch_bounds__(kQkThreads) qk_pairs_kernel(const __grid_constant__ QkParams p) {
+  start_after_previous_kernel();
   constexpr int U = kQkHeads, VW = 1, N = 2, L = 32, GPL = kQkPairs;
   const int lane = threadIdx.x % L;
   const uint32_t task = blockIdx.x * (kQkThreads / L) + threadIdx.x / L;
@@ -495,6 +497,7 @@ __global__ void __launch_bounds__(kQkThreads) qk_pairs_kernel(const __grid_const
 // In FP64: it serves the heads of a few values, where dx is a small difference (one value: u (1 - xh^2), about eps of u).
 template <typename T>
 __global__ void __launch_bounds__(kQkThreads) qk_pairs_backward_kernel(const __grid_constant__ QkParams p) {
+  start_after_previous_kernel();
   constexpr int VW = 1, N = 2, L = 32, GPL = kQkPairs, kTasks = kQkThreads / L;
   using A = double;
   __shared__ float part[kTasks][L * GPL * N + 1];
@@ -597,18 +600,19 @@ __global__ void __launch_bounds__(kQkThreads) qk_pairs_backward_kernel(const __g
 __global__ void __launch_bounds__(1024) qk_weight_grad_kernel(const float* partials, int head_dim, int blocks_q,
                                                               int blocks, float* dw_q, float* dw_k) {
   __shared__ float part[32][33];
-  const int side = blockIdx.y, d = blockIdx.x * 32 + threadIdx.x;
+  start_after_previous_kernel();
+  const int column = threadIdx.x % 32, row = threadIdx.x / 32, side = blockIdx.y, d = blockIdx.x * 32 + column;
   float* dw = side ? dw_k : dw_q;
   const int lo = side ? blocks_q : 0, hi = side ? blocks : blocks_q;
   float s = 0.0f;
   if (d < head_dim)
-    for (int b = lo + (int)threadIdx.y; b < hi; b += 32) s += partials[(int64_t)b * head_dim + d];
-  part[threadIdx.y][threadIdx.x] = s;
+    for (int b = lo + row; b < hi; b += 32) s += partials[(int64_t)b * head_dim + d];
+  part[row][column] = s;
   __syncthreads();
-  if (threadIdx.y == 0 && d < head_dim && dw) {
+  if (row == 0 && d < head_dim && dw) {
     float t = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) t += part[i][threadIdx.x];
+    for (int i = 0; i < 32; ++i) t += part[i][column];
     dw[d] = t;
   }
 }
@@ -733,11 +737,11 @@ void split_grid(const slidedp_qk_args* a, int64_t blocks, QkPlan* plan) {
 template <typename T, int VW, bool BACK, bool INTER>
 void launch_heads(const QkPlan& plan, cudaStream_t st) {
   switch (plan.lanes) {
-    case 4: qk_heads_kernel<T, VW, 4, BACK, INTER><<<plan.grid, kQkThreads, 0, st>>>(plan.p); break;
-    case 8: qk_heads_kernel<T, VW, 8, BACK, INTER><<<plan.grid, kQkThreads, 0, st>>>(plan.p); break;
-    case 16: qk_heads_kernel<T, VW, 16, BACK, INTER><<<plan.grid, kQkThreads, 0, st>>>(plan.p); break;
+    case 4: launch_after(qk_heads_kernel<T, VW, 4, BACK, INTER>, plan.grid, kQkThreads, 0, 1, st, plan.p); break;
+    case 8: launch_after(qk_heads_kernel<T, VW, 8, BACK, INTER>, plan.grid, kQkThreads, 0, 1, st, plan.p); break;
+    case 16: launch_after(qk_heads_kernel<T, VW, 16, BACK, INTER>, plan.grid, kQkThreads, 0, 1, st, plan.p); break;
     default:   // 2 * VW * 32 values: more than a head has when VW is 8
-      if constexpr (VW == 4) qk_heads_kernel<T, VW, 32, BACK, INTER><<<plan.grid, kQkThreads, 0, st>>>(plan.p);
+      if constexpr (VW == 4) launch_after(qk_heads_kernel<T, VW, 32, BACK, INTER>, plan.grid, kQkThreads, 0, 1, st, plan.p);
   }
 }
 template <bool BACK, bool INTER>
@@ -777,8 +781,8 @@ int slidedp_qk_norm_rope(slidedp_ctx* ctx, const slidedp_qk_args* a, const slide
   } else {
     const int64_t per_block = kQkThreads / 32;
     const unsigned grid = (unsigned)((a->tokens * plan.p.chunks + per_block - 1) / per_block);
-    if (a->dtype == SLIDEDP_F32) qk_pairs_kernel<float><<<grid, kQkThreads, 0, st>>>(plan.p);
-    else qk_pairs_kernel<uint16_t><<<grid, kQkThreads, 0, st>>>(plan.p);
+    if (a->dtype == SLIDEDP_F32) launch_after(qk_pairs_kernel<float>, grid, kQkThreads, 0, 1, st, plan.p);
+    else launch_after(qk_pairs_kernel<uint16_t>, grid, kQkThreads, 0, 1, st, plan.p);
   }
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
@@ -818,14 +822,14 @@ int slidedp_qk_norm_rope_backward(slidedp_ctx* ctx, const slidedp_qk_args* a, co
   plan.p.partials = (dw_q || dw_k) ? static_cast<float*>(workspace) : nullptr;
   FAULT_POINT();
   if (plan.vec > 1) launch_heads<true>(a, plan, st);
-  else if (a->dtype == SLIDEDP_F32) qk_pairs_backward_kernel<float><<<plan.grid, kQkThreads, 0, st>>>(plan.p);
-  else qk_pairs_backward_kernel<uint16_t><<<plan.grid, kQkThreads, 0, st>>>(plan.p);
+  else if (a->dtype == SLIDEDP_F32) launch_after(qk_pairs_backward_kernel<float>, plan.grid, kQkThreads, 0, 1, st, plan.p);
+  else launch_after(qk_pairs_backward_kernel<uint16_t>, plan.grid, kQkThreads, 0, 1, st, plan.p);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   if (plan.p.partials) {
     FAULT_POINT();
-    qk_weight_grad_kernel<<<dim3((a->head_dim + 31) / 32, 2), dim3(32, 32), 0, st>>>(
-        plan.p.partials, a->head_dim, plan.p.blocks_q, (int)plan.grid, dw_q, dw_k);
+    launch_after(qk_weight_grad_kernel, dim3((a->head_dim + 31) / 32, 2), 1024, 0, 1, st, plan.p.partials, a->head_dim, plan.p.blocks_q,
+                 (int)plan.grid, dw_q, dw_k);
     ctx->launches += 1;
     CU_AFTER_LAUNCH();
   }
