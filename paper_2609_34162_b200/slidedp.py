@@ -183,6 +183,8 @@ class _DistillArgs(ctypes.Structure):
 # and passed as addresses there; the scalar arguments go as the bytes of their struct (a ctypes object costs three times that).
 _V = 24
 _qk_bytes, _attn_bytes, _distill_bytes = (struct.Struct(f).pack for f in ("@qiiiiiiqd", "@qiiiiiiPPPdd", "@qqiiqqddd"))
+for _args, _pack in ((_QkArgs, _qk_bytes), (_AttnArgs, _attn_bytes), (_DistillArgs, _distill_bytes)):
+    assert len(_pack(*[0] * len(_args._fields_))) == ctypes.sizeof(_args)
 for _name, _res, _args in (
         ("slidedp_qk_norm_rope", ctypes.c_int, [_vp, _vp] + [_vp] * 9),
         ("slidedp_qk_norm_rope_backward", ctypes.c_int, [_vp, _vp] + [_vp] * 14),
