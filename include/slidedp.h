@@ -123,9 +123,14 @@ SLIDEDP_API int slidedp_destroy(slidedp_ctx* ctx);
  * nth guarded CUDA runtime call (or kernel launch) that the context issues from now on is not
  * issued at all and is reported as failed with cudaErrorUnknown, so that every error path above
  * can be exercised; nth <= 0 switches the hook off. The countdown stops at the failure.
+ *
+ * slidedp_test_wait_polls is another one: waits inside the kernels of slidedp_ops.h that the context launches from now on
+ * give up after `polls` polls (0: at once) instead of the seconds' worth that they allow, so that healthy launches run out
+ * of them and return; polls < 0 restores the limit.
  */
 SLIDEDP_API int slidedp_set_wait_seconds(slidedp_ctx* ctx, double seconds);
 SLIDEDP_API int slidedp_test_fail_nth_call(slidedp_ctx* ctx, int64_t nth);
+SLIDEDP_API int slidedp_test_wait_polls(slidedp_ctx* ctx, int64_t polls);
 SLIDEDP_API const char* slidedp_strerror(int status);
 SLIDEDP_API int slidedp_last_cuda_error(const slidedp_ctx* ctx);
 

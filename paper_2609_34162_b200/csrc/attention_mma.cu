@@ -33,12 +33,6 @@ constexpr uint32_t kRowStep = 16 * 128 >> 4;   // and of 16 contracted rows
 constexpr int kPolyOfEight = 2;
 constexpr float kRescaleAbove = 8.0f;      // log2: how far a row's maximum may run ahead of its scale
 
-// Waits that outlive the early exit: for copies and products of this thread still in flight.
-__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
-  for (uint32_t n = 0; n < kSpinLimit; ++n)
-    if (mbar_try(bar, parity)) return;
-}
-
 template <int HALVES>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int head, int row, uint32_t bar) {
 #pragma unroll
@@ -337,7 +331,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t base = smem_addr(raw_smem);
   const uint32_t smem_q = base, smem_k = base + 2 * Shape::kTileBytes, smem_v = smem_k + S * Shape::kTileBytes,
                  stages = smem_v + S * Shape::kTileBytes;
-  const Waiter wait{&ctl.dead, p.error};
+  const Waiter wait{&ctl.dead, p.error, kWaitPolls};
 
   if (threadIdx.x == 0) {
     ctl.work.init(10);   // eight of rows, the issuer, the producer
@@ -677,7 +671,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t base = smem_addr(raw_smem);
   const uint32_t smem_k = base, smem_v = smem_k + Shape::kTileBytes, smem_q = smem_v + Shape::kTileBytes,
                  smem_do = smem_q + S * Shape::kTileBytes, stages = smem_do + S * Shape::kTileBytes;
-  const Waiter wait{&ctl.dead, p.error};
+  const Waiter wait{&ctl.dead, p.error, kWaitPolls};
 
   if (threadIdx.x == 0) {
     ctl.work.init(10);   // eight of rows, the issuer, the producer
@@ -1044,7 +1038,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t base = smem_addr(raw_smem);
   const uint32_t smem_q = base, smem_do = smem_q + Shape::kTileBytes, smem_k = smem_do + Shape::kTileBytes,
                  smem_v = smem_k + SK * Shape::kTileBytes, stages = smem_v + SV * Shape::kTileBytes;
-  const Waiter wait{&ctl.dead, p.error};
+  const Waiter wait{&ctl.dead, p.error, kWaitPolls};
 
   if (threadIdx.x == 0) {
     ctl.work.init(10);

@@ -44,6 +44,12 @@ int slidedp_test_fail_nth_call(slidedp_ctx* ctx, int64_t nth) {
   return SLIDEDP_OK;
 }
 
+int slidedp_test_wait_polls(slidedp_ctx* ctx, int64_t polls) {
+  if (!ctx) return SLIDEDP_ERR_INVALID_ARG;
+  ctx->wait_polls = polls < 0 || polls > (int64_t)kWaitPolls ? kWaitPolls : (uint32_t)polls;
+  return SLIDEDP_OK;
+}
+
 int slidedp_create(slidedp_ctx** out, int device, size_t gpu_budget_bytes) {
   if (!out) return SLIDEDP_ERR_INVALID_ARG;
   *out = nullptr;

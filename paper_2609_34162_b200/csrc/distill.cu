@@ -45,6 +45,7 @@ struct DistillParams {
   int64_t chunks_per_block;  // 16-byte chunks of a row that one block of its cluster takes
   float inv_tau, tau, w_teacher, w_label;
   int* error;              // pinned host word that a wait which runs out sets
+  uint32_t polls;          // and how long it polls
 };
 
 template <typename T> struct Logit;
@@ -276,7 +277,7 @@ __device__ __forceinline__ void send_sums(const SoftSum& v, DistillShared& sh, i
                "f"(v.s0), "f"(v.s1), "f"(0.0f), "r"(at)
                : "memory");
 }
-// The cluster's sums in every thread.
+// The cluster's sums in every thread; whether they came in time, which the block's warps may see differently.
 template <bool kTwo>
 __device__ __forceinline__ bool receive_sums(SoftSum* all, DistillShared& sh, int size, float k0, float k1, const Waiter& wait) {
   const int i = threadIdx.x % 8;
@@ -460,10 +461,10 @@ __global__ void __launch_bounds__(kDistillThreads, distill_min_blocks(U)) distil
   float q_log_q = 0.0f, q_sum = 0.0f;
   if ((kGradient || s.rank == 0) && threadIdx.x < 32) teacher_softmax(p, en, &q_log_q, &q_sum);
   bool ok = true;
-  if (cluster > 1) ok = receive_sums<kTwo>(&mine, sh, s.size, k0, k1, Waiter{&dead, p.error});
+  if (cluster > 1) ok = receive_sums<kTwo>(&mine, sh, s.size, k0, k1, Waiter{&dead, p.error, p.polls});
   __syncwarp();
   const float m = finite_shift(mine.m), l0 = log2f(mine.s0), l1 = kTwo ? log2f(mine.s1) : l0;
-  if (s.rank == 0 && threadIdx.x < 32) {
+  if (ok && s.rank == 0 && threadIdx.x < 32) {
     float cross = 0.0f;
     for (int k = threadIdx.x; k < en.count; k += 32)
       if (en.q[k] != 0.0f) cross += en.q[k] * ((en.z[k] - m) * p.inv_tau);
@@ -472,16 +473,21 @@ __global__ void __launch_bounds__(kDistillThreads, distill_min_blocks(U)) distil
     cross = warp_sum(cross);
     if (threadIdx.x == 0) write_loss(p, s.r, en.id[en.count] >= 0, q_log_q, q_sum, cross, en.z[en.count] - m, m, l0, l1);
   }
-  if (kGradient && ok) {
+  if constexpr (kGradient) {
     float a0, a1;
     const GradFactors f = factors<kTwo>(p, p.row_grad ? p.row_grad[s.r] : 1.0f, some, en.id[en.count] >= 0, l0, l1, &a0, &a1);
     T* dz = static_cast<T*>(p.dz) + s.r * p.dz_stride;
-    write_slice<T, kTwo, U>(s, dz, m, f);
-    s.edges([&](int, int64_t c) { write_values<T, kTwo>(s.row, dz, c, s.row.load(c), m, f); });
-    __syncthreads();   // the stores above come before those at the entries
-    write_entries<T, kTwo>(s, dz, en, m, f, a0, a1);
+    if (ok) {
+      write_slice<T, kTwo, U>(s, dz, m, f);
+      s.edges([&](int, int64_t c) { write_values<T, kTwo>(s.row, dz, c, s.row.load(c), m, f); });
+    }
+    __syncthreads();   // the stores above come before those at the entries; all warps, whatever they were told
+    if (ok) write_entries<T, kTwo>(s, dz, en, m, f, a0, a1);
   }
-  if (cluster > 1) cluster_sync();   // nobody leaves while sums may still be sent to it
+  if (cluster > 1) {   // nobody leaves while sums may still be sent to it
+    cluster_sync();
+    if (!ok) drain(smem_addr(&sh.exchanged), 0);
+  }
 }
 
 // Gradient from the saved lse: blocks of a row share nothing.
@@ -574,6 +580,7 @@ int run_distill(slidedp_ctx* ctx, const slidedp_distill_args* a, int mode, const
   const unsigned cluster = blocks_per_row(mode, a->rows, chunks * 16);
   p.chunks_per_block = (chunks + cluster - 1) / cluster;
   p.error = ctx->kernel_error;
+  p.polls = ctx->wait_polls;
   if ((int64_t)a->rows * cluster > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
   const bool two = p.labels && a->temperature != 1.0;
   const bool f32 = a->dtype == SLIDEDP_F32;

@@ -52,6 +52,7 @@ struct slidedp_ctx {
   double* host_scalars = nullptr;   // pinned mirror
   bool norm_issued = false;
   int* kernel_error = nullptr;      // pinned: set by a kernel whose bounded wait ran out
+  uint32_t wait_polls = slidedp::kWaitPolls;   // bound of those waits (slidedp_test_wait_polls)
   cudaEvent_t scalar_event = nullptr;
   // host-resident streaming
   cudaStream_t s_in = nullptr, s_compute = nullptr, s_out = nullptr;

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "device_utils.cuh"
+#include "types.h"
 
 namespace slidedp {
 
@@ -35,17 +36,15 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 
-// Every wait inside a kernel ends: after kSpinLimit polls (each of them suspends the thread for a
-// while, so this is seconds where microseconds are expected) it sets the block's `dead` word, which ends
-// every other wait of the block early, and the error word that the host reads. A caller that gets
-// false stops issuing work and leaves.
-constexpr uint32_t kSpinLimit = 1u << 24;
+// Every wait inside a kernel ends: after `polls` polls (kWaitPolls, but for tests) it sets the block's `dead` word, which
+// ends every other wait of the block early, and the error word that the host reads. A caller that gets
+// false stops issuing work and leaves. Threads that wait for the same thing may get different answers.
 struct Waiter {
   volatile uint32_t* dead;   // shared memory
   int* error;                // pinned host memory
+  uint32_t polls;
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, uint32_t nap_ns = 0) const {
-    if (mbar_try(bar, parity)) return true;
-    for (uint32_t n = 0; n < kSpinLimit; ++n) {
+    for (uint32_t n = 0; n < polls; ++n) {
       if (mbar_try(bar, parity)) return true;
       if ((n & 255u) == 255u && *dead) return false;
       if (nap_ns) __nanosleep(nap_ns);   // a wait that may be long and is not urgent leaves the issue slots alone
@@ -55,6 +54,11 @@ struct Waiter {
     return false;
   }
 };
+// Waits, also after such an early exit, for what this thread has started and must not leave in flight: copies, products.
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
+  for (uint32_t n = 0; n < kWaitPolls; ++n)
+    if (mbar_try(bar, parity)) return;
+}
 
 // Order between ordinary accesses of shared memory and those of the asynchronous proxy (copies, answers).
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }

@@ -7,6 +7,10 @@ namespace slidedp {
 
 constexpr int kMaxRanks = 16;
 
+// How often a wait inside a kernel polls before it gives up: each poll suspends the thread for a while, so this is
+// seconds where microseconds are expected.
+constexpr uint32_t kWaitPolls = 1u << 24;
+
 struct GradPtrs {
   const uint16_t* p[kMaxRanks];
 };

@@ -146,6 +146,8 @@ _lib.slidedp_set_wait_seconds.restype = ctypes.c_int
 _lib.slidedp_set_wait_seconds.argtypes = [_vp, ctypes.c_double]
 _lib.slidedp_test_fail_nth_call.restype = ctypes.c_int
 _lib.slidedp_test_fail_nth_call.argtypes = [_vp, ctypes.c_int64]
+_lib.slidedp_test_wait_polls.restype = ctypes.c_int
+_lib.slidedp_test_wait_polls.argtypes = [_vp, ctypes.c_int64]
 
 
 class _Rates(ctypes.Structure):
@@ -348,6 +350,9 @@ class Context:
 
     def slidedp_test_fail_nth_call(self, nth: int) -> None:
         self._check(_lib.slidedp_test_fail_nth_call(self._h, nth))
+
+    def slidedp_test_wait_polls(self, polls: int) -> None:
+        self._check(_lib.slidedp_test_wait_polls(self._h, polls))
 
     def slidedp_last_cuda_error(self) -> int:
         return int(_lib.slidedp_last_cuda_error(self._h))

@@ -1,0 +1,56 @@
+"""Waits inside the operators' kernels that run out: the kernel returns, the next call says SLIDEDP_ERR_TIMEOUT once, and the
+context works as before. The waits are made to run out by a short limit on healthy launches; nothing hangs or fails on the GPU."""
+import pytest
+import torch
+
+from test_operators_gpu import BF16, F32, ctx, distill_inputs, gen, randn, sd  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+POLLS = [0, 1, 2, 3, 5, 9, 20]     # 0: every wait gives up; others: some do, and not the same ones in every warp
+
+
+def out_of_patience(ctx, sd, polls, call, check):
+    """Runs `call` with the limit, then without: an operator call reports a wait that ran out, once, and does nothing then."""
+    ctx.slidedp_test_wait_polls(polls)
+    try:
+        call()
+        torch.cuda.synchronize()
+    finally:
+        ctx.slidedp_test_wait_polls(-1)
+    reported = False
+    try:
+        call()
+    except sd.SlideDPError as e:
+        assert e.status == sd.ERR_TIMEOUT
+        reported = True
+    if polls == 0:
+        assert reported
+    call()
+    torch.cuda.synchronize()
+    check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,vocab", [(3, 40000), (8, 131072)])
+def test_distill_waits_that_run_out(ctx, sd, dtype, rows, vocab):
+    z, ids, t, labels, gr = distill_inputs(rows, vocab, 12, dtype, seed=5)
+    loss, lse, dz = torch.empty(rows, device="cuda"), torch.empty(2, rows, device="cuda"), torch.empty_like(z)
+    kw = dict(temperature=1.5, w_teacher=0.7, w_label=0.3)
+    step = lambda: ctx.slidedp_distill_step(z, ids, t, labels, gr, loss, lse, dz, **kw)   # noqa: E731
+    forward = lambda: ctx.slidedp_distill_loss(z, ids, t, labels, loss, lse, **kw)         # noqa: E731
+    cases = []
+    for call, n in ((step, 3), (forward, 2)):      # the two add up in other orders: each is compared with itself
+        call()
+        cases.append((call, [x.clone() for x in (loss, lse, dz)[:n]]))
+
+    def same(want):
+        def check():
+            for a, b in zip((loss, lse, dz), want):
+                assert torch.equal(a, b)
+        return check
+    for polls in POLLS:
+        for call, want in cases:
+            for x in (loss, lse, dz):
+                x.fill_(7.0)
+            out_of_patience(ctx, sd, polls, call, same(want))
