@@ -154,6 +154,7 @@ int slidedp_attention(slidedp_ctx* ctx, const slidedp_attn_args* a, const slided
     return SLIDEDP_ERR_INVALID_ARG;
   AttnParams p = make_params(a, q, k, v, out, lse);
   p.error = ctx->kernel_error;
+  p.polls = ctx->wait_polls;
   const int rc = check_kernel_error(ctx);
   if (rc != SLIDEDP_OK) return rc;
   DeviceGuard guard(ctx->device);
@@ -191,6 +192,7 @@ int slidedp_attention_backward(slidedp_ctx* ctx, const slidedp_attn_args* a, con
   p.dk = view(dk);
   p.dv = view(dv);
   p.error = ctx->kernel_error;
+  p.polls = ctx->wait_polls;
   const int rc = check_kernel_error(ctx);
   if (rc != SLIDEDP_OK) return rc;
   p.row_lse = static_cast<float*>(workspace);

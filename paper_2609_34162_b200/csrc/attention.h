@@ -69,6 +69,7 @@ struct AttnParams {
   float* row_delta;    // backward: sum_d dout * out, likewise
   int64_t pitch;
   int* error;          // pinned host word that a wait which runs out sets
+  uint32_t polls;      // and how long it polls
   const float* slopes;
   DocMask mask;
   int tokens, heads_q, heads_kv, group, head_dim;

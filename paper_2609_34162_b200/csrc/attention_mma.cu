@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t base = smem_addr(raw_smem);
   const uint32_t smem_q = base, smem_k = base + 2 * Shape::kTileBytes, smem_v = smem_k + S * Shape::kTileBytes,
                  stages = smem_v + S * Shape::kTileBytes;
-  const Waiter wait{&ctl.dead, p.error, kWaitPolls};
+  const Waiter wait{&ctl.dead, p.error, p.polls};
 
   if (threadIdx.x == 0) {
     ctl.work.init(10);   // eight of rows, the issuer, the producer
@@ -418,11 +418,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           load_tile<HALVES>(smem_v + st * Shape::kTileBytes, &map_v, hk, pl.n_lo + j * kTile, smem_addr(&ctl.v_full[st]));
         }
       }
-      if (ctl.dead) {   // leave no copy in flight
-        if (walks > 0) drain(smem_addr(&ctl.q_full), walks - 1 & 1);
-        for (int j = k_sent > S ? k_sent - S : 0; j < k_sent; ++j) drain(smem_addr(&ctl.k_full[j % S]), (j / S) & 1);
-        for (int j = sent > S ? sent - S : 0; j < sent; ++j) drain(smem_addr(&ctl.v_full[j % S]), (j / S) & 1);
-      }
+      // leave no copy in flight (whatever `dead` says now: another warp may give up later, and then nobody waits for them)
+      if (walks > 0) drain(smem_addr(&ctl.q_full), walks - 1 & 1);
+      for (int j = k_sent > S ? k_sent - S : 0; j < k_sent; ++j) drain(smem_addr(&ctl.k_full[j % S]), (j / S) & 1);
+      for (int j = sent > S ? sent - S : 0; j < sent; ++j) drain(smem_addr(&ctl.v_full[j % S]), (j / S) & 1);
     } else if (warp == 8) {   // ---- issuer
       const bool leader = elect_leader();
       const auto wait_all = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
@@ -476,10 +475,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         }
         done += pl.steps;
       }
-      if (ctl.dead) {
-        mma_commit(smem_addr(&ctl.done), leader);
-        drain(smem_addr(&ctl.done), 0);
-      }
+      mma_commit(smem_addr(&ctl.done), leader);   // nor a product
+      drain(smem_addr(&ctl.done), 0);
     }
   } else {   // ---- rows
     more_registers();
@@ -671,7 +668,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t base = smem_addr(raw_smem);
   const uint32_t smem_k = base, smem_v = smem_k + Shape::kTileBytes, smem_q = smem_v + Shape::kTileBytes,
                  smem_do = smem_q + S * Shape::kTileBytes, stages = smem_do + S * Shape::kTileBytes;
-  const Waiter wait{&ctl.dead, p.error, kWaitPolls};
+  const Waiter wait{&ctl.dead, p.error, p.polls};
 
   if (threadIdx.x == 0) {
     ctl.work.init(10);   // eight of rows, the issuer, the producer
@@ -749,11 +746,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
             load_tile<HALVES>(smem_do + st * Shape::kTileBytes, &map_do, h, m0, smem_addr(&ctl.do_full[st]));
           }
       }
-      if (ctl.dead) {
-        if (walks > 0) drain(smem_addr(&ctl.kv_full), walks - 1 & 1);
-        for (int j = q_sent > S ? q_sent - S : 0; j < q_sent; ++j) drain(smem_addr(&ctl.q_full[j % S]), (j / S) & 1);
-        for (int j = sent > S ? sent - S : 0; j < sent; ++j) drain(smem_addr(&ctl.do_full[j % S]), (j / S) & 1);
-      }
+      if (walks > 0) drain(smem_addr(&ctl.kv_full), walks - 1 & 1);
+      for (int j = q_sent > S ? q_sent - S : 0; j < q_sent; ++j) drain(smem_addr(&ctl.q_full[j % S]), (j / S) & 1);
+      for (int j = sent > S ? sent - S : 0; j < sent; ++j) drain(smem_addr(&ctl.do_full[j % S]), (j / S) & 1);
     } else if (warp == 8) {   // ---- issuer
       const bool leader = elect_leader();
       const auto wait_all = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
@@ -798,10 +793,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         done += steps;
         if (ok) mma_commit(smem_addr(&ctl.acc_full), leader);
       }
-      if (ctl.dead) {
-        mma_commit(smem_addr(&ctl.done), leader);
-        drain(smem_addr(&ctl.done), 0);
-      }
+      mma_commit(smem_addr(&ctl.done), leader);   // nor a product
+      drain(smem_addr(&ctl.done), 0);
     }
     if (split > 1) {   // as below
       __syncwarp();
@@ -1038,7 +1031,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t base = smem_addr(raw_smem);
   const uint32_t smem_q = base, smem_do = smem_q + Shape::kTileBytes, smem_k = smem_do + Shape::kTileBytes,
                  smem_v = smem_k + SK * Shape::kTileBytes, stages = smem_v + SV * Shape::kTileBytes;
-  const Waiter wait{&ctl.dead, p.error, kWaitPolls};
+  const Waiter wait{&ctl.dead, p.error, p.polls};
 
   if (threadIdx.x == 0) {
     ctl.work.init(10);
@@ -1110,11 +1103,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           load_tile<HALVES>(smem_v + sv * Shape::kTileBytes, &map_v, hk, pl.n_lo + j * kTile, smem_addr(&ctl.v_full[sv]));
         }
       }
-      if (ctl.dead) {
-        if (walks > 0) drain(smem_addr(&ctl.q_full), walks - 1 & 1);
-        for (int j = k_sent > SK ? k_sent - SK : 0; j < k_sent; ++j) drain(smem_addr(&ctl.k_full[j % SK]), (j / SK) & 1);
-        for (int j = sent > SV ? sent - SV : 0; j < sent; ++j) drain(smem_addr(&ctl.v_full[j % SV]), (j / SV) & 1);
-      }
+      if (walks > 0) drain(smem_addr(&ctl.q_full), walks - 1 & 1);
+      for (int j = k_sent > SK ? k_sent - SK : 0; j < k_sent; ++j) drain(smem_addr(&ctl.k_full[j % SK]), (j / SK) & 1);
+      for (int j = sent > SV ? sent - SV : 0; j < sent; ++j) drain(smem_addr(&ctl.v_full[j % SV]), (j / SV) & 1);
     } else if (warp == 8) {   // ---- issuer
       const bool leader = elect_leader();
       const auto wait_all = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
@@ -1154,10 +1145,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         done += pl.steps;
         if (ok) mma_commit(smem_addr(&ctl.acc_full), leader);
       }
-      if (ctl.dead) {
-        mma_commit(smem_addr(&ctl.done), leader);
-        drain(smem_addr(&ctl.done), 0);
-      }
+      mma_commit(smem_addr(&ctl.done), leader);   // nor a product
+      drain(smem_addr(&ctl.done), 0);
     }
   } else {   // ---- rows: queries; the warpgroups take 64 of a step's keys each
     more_registers();

@@ -54,3 +54,28 @@ def test_distill_waits_that_run_out(ctx, sd, dtype, rows, vocab):
             for x in (loss, lse, dz):
                 x.fill_(7.0)
             out_of_patience(ctx, sd, polls, call, same(want))
+
+
+@pytest.mark.parametrize("T,Hq,Hk,D,cu", [(900, 16, 4, 128, [0, 300, 310, 900]), (700, 32, 32, 64, [0, 700]), (200, 8, 1, 128, None)])
+def test_attention_waits_that_run_out(ctx, sd, T, Hq, Hk, D, cu):
+    g = gen(T)
+    q, k, v, do = (randn(g, T, h, D, dtype=BF16) for h in (Hq, Hk, Hk, Hq))
+    cu = None if cu is None else torch.tensor(cu, dtype=torch.int32, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(Hq, T, device="cuda")
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    ws = torch.empty(ctx.slidedp_attention_workspace(q, k), dtype=torch.uint8, device="cuda")
+    forward = lambda: ctx.slidedp_attention(q, k, v, out, lse, cu_docs=cu)                                        # noqa: E731
+    backward = lambda: ctx.slidedp_attention_backward(q, k, v, *saved, do, dq, dk, dv, ws, cu_docs=cu)            # noqa: E731
+    forward()
+    saved = [out.clone(), lse.clone()]
+    backward()
+    want = [x.clone() for x in (dq, dk, dv)]
+
+    def same(got, want):
+        def check():
+            for a, b in zip(got, want):
+                assert torch.equal(a, b)
+        return check
+    for polls in POLLS + [50, 200]:
+        out_of_patience(ctx, sd, polls, forward, same((out, lse), saved))
+        out_of_patience(ctx, sd, polls, backward, same((dq, dk, dv), want))
