@@ -93,7 +93,8 @@ typedef struct {
 /* Creates a context on `device`. gpu_budget_bytes caps what slidedp_stream_step may allocate
  * for its slots (0 = no cap). Allocates the norm workspace (a few MB) and three streams. */
 SLIDEDP_API int slidedp_create(slidedp_ctx** out, int device, size_t gpu_budget_bytes);
-/* Waits (bounded) for the context's own streams, frees everything. NULL is a no-op. */
+/* Waits (bounded) for the context's own streams, frees everything. NULL is a no-op. SLIDEDP_ERR_TIMEOUT also tells of a
+ * wait inside an operator's kernel that ran out and that no call has reported (slidedp_ops.h). */
 SLIDEDP_API int slidedp_destroy(slidedp_ctx* ctx);
 
 /* ---- failure handling ------------------------------------------------------------------
@@ -151,7 +152,8 @@ SLIDEDP_API size_t slidedp_state_bytes(int64_t n);
  * slidedp_grad_norm_finish folds the tile sums in a fixed order and leaves, in device
  * memory owned by the context, sumsq, norm = sqrt(sumsq) and
  * coef = max_norm > 0 ? min(1, max_norm / (norm + 1e-6)) : 1. If host_norm / host_coef is
- * non-NULL the call also waits (bounded) for the stream and returns the values.
+ * non-NULL the call also waits (bounded) for the stream and returns the values; if a wait inside an operator's kernel has
+ * run out by then (slidedp_ops.h) it still returns them, with the status SLIDEDP_ERR_TIMEOUT.
  */
 SLIDEDP_API int slidedp_grad_norm(slidedp_ctx* ctx, const void* const* grads_bf16 /* host array of R device ptrs */,
                       int R, int64_t n, double inv_R, int first_chunk, void* cuda_stream);

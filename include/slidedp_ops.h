@@ -12,8 +12,11 @@
  * that can overlap.
  *
  * The attention and distillation kernels wait on copies and on blocks of their own launch; every
- * such wait is bounded. If one runs out, the results of that call are not complete and the next
- * operator call on the context returns SLIDEDP_ERR_TIMEOUT (once).
+ * such wait is bounded. If one runs out, the results of that call are not complete, and the first of these calls on the
+ * context to start after that returns SLIDEDP_ERR_TIMEOUT, once, and does nothing else: any operator of this header; a
+ * slidedp_grad_norm_finish or slidedp_grad_norm_finish_from that fetches its results (they are fetched all the same); or
+ * slidedp_destroy (which still destroys). A call's own kernels have only been queued when it returns: to know that a step's
+ * gradients are complete before they are used, fetch the norm, which waits for the kernels queued before it.
  *
  * BF16 and FP32 tensors need the alignment of their element only; 16-byte aligned bases and
  * strides are faster. All sums, norms and softmax statistics are FP32 and each output is rounded

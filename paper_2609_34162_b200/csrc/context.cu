@@ -118,6 +118,7 @@ int slidedp_destroy(slidedp_ctx* ctx) {
   for (ChunkEvents& c : ctx->timing) { kill(c.k_start); kill(c.k_end); }
   for (slidedp::host::IpcMapping& m : ctx->ipc) cudaIpcCloseMemHandle(m.base);
   ctx->ipc.clear();
+  if (rc == SLIDEDP_OK) rc = check_kernel_error(ctx);   // nobody else will tell
   if (ctx->slots) cudaFree(ctx->slots);
   if (ctx->partials) cudaFree(ctx->partials);
   if (ctx->scalars) cudaFree(ctx->scalars);

@@ -90,6 +90,12 @@ struct DeviceGuard {
 
 int cuda_fail(slidedp_ctx* ctx, cudaError_t e);
 
+// Whether a wait inside an earlier kernel of the context ran out; told to one caller.
+inline int check_kernel_error(slidedp_ctx* ctx) {
+  if (!ctx->kernel_error || __atomic_load_n(ctx->kernel_error, __ATOMIC_RELAXED) == 0) return SLIDEDP_OK;
+  return __atomic_exchange_n(ctx->kernel_error, 0, __ATOMIC_RELAXED) ? SLIDEDP_ERR_TIMEOUT : SLIDEDP_OK;
+}
+
 // True when the host-side fault injection of `ctx` says that the next guarded call must fail.
 inline bool injected_failure(slidedp_ctx* ctx) {
   return ctx && ctx->fail_countdown > 0 && --ctx->fail_countdown == 0;

@@ -47,13 +47,5 @@ void launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem
   (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);   // the caller asks for the error
 }
 
-// A wait inside an earlier kernel of the context ran out.
-inline int check_kernel_error(slidedp_ctx* ctx) {
-  volatile int* e = ctx->kernel_error;
-  if (*e == 0) return SLIDEDP_OK;
-  *e = 0;
-  return SLIDEDP_ERR_TIMEOUT;
-}
-
 }  // namespace host
 }  // namespace slidedp

@@ -770,6 +770,7 @@ int slidedp_qk_norm_rope(slidedp_ctx* ctx, const slidedp_qk_args* a, const slide
   const void* w[2] = {w_q, w_k};
   QkPlan plan;
   int rc = plan_qk(a, in, nullptr, out, w, cos_sin, positions, &plan);
+  if (rc == SLIDEDP_OK) rc = check_kernel_error(ctx);
   if (rc != SLIDEDP_OK) return rc;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());
@@ -809,6 +810,7 @@ int slidedp_qk_norm_rope_backward(slidedp_ctx* ctx, const slidedp_qk_args* a, co
   QkPlan plan;
   const bool work = a->tokens > 0 && a->heads_q + a->heads_k > 0;
   int rc = work ? plan_qk(a, in, dy, out, w, cos_sin, positions, &plan) : SLIDEDP_OK;
+  if (rc == SLIDEDP_OK) rc = check_kernel_error(ctx);
   if (rc != SLIDEDP_OK) return rc;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());

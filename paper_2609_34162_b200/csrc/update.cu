@@ -202,6 +202,7 @@ int slidedp_grad_norm_finish(slidedp_ctx* ctx, double max_norm, double* host_nor
     if (rc != SLIDEDP_OK) return rc;
     if (host_norm) *host_norm = ctx->host_scalars[1];
     if (host_coef) *host_coef = ctx->host_scalars[2];
+    return check_kernel_error(ctx);   // the gradients that the norm is of may come from an operator that gave up
   }
   return SLIDEDP_OK;
 }
@@ -244,6 +245,7 @@ int slidedp_grad_norm_finish_from(slidedp_ctx* ctx, const double* tile_sums, int
     if (rc != SLIDEDP_OK) return rc;
     if (host_norm) *host_norm = ctx->host_scalars[1];
     if (host_coef) *host_coef = ctx->host_scalars[2];
+    return check_kernel_error(ctx);   // the gradients that the norm is of may come from an operator that gave up
   }
   return SLIDEDP_OK;
 }

@@ -79,3 +79,52 @@ def test_attention_waits_that_run_out(ctx, sd, T, Hq, Hk, D, cu):
     for polls in POLLS + [50, 200]:
         out_of_patience(ctx, sd, polls, forward, same((out, lse), saved))
         out_of_patience(ctx, sd, polls, backward, same((dq, dk, dv), want))
+
+
+def give_up(ctx):
+    """Leaves a wait that ran out behind, unreported."""
+    q = randn(gen(1), 200, 2, 64, dtype=BF16)
+    ctx.slidedp_test_wait_polls(0)
+    ctx.slidedp_attention(q, q, q, torch.empty_like(q), torch.empty(2, 200, device="cuda"))
+    ctx.slidedp_test_wait_polls(-1)
+    torch.cuda.synchronize()
+
+
+def test_every_operator_and_the_norm_report_a_wait_that_ran_out(sd):
+    T, H, D = 40, 2, 64
+    q = randn(gen(2), T, H, D, dtype=BF16)
+    out, out2, lse = torch.empty_like(q), torch.empty_like(q), torch.empty(H, T, device="cuda")
+    dw, n = torch.empty(2, D, device="cuda"), q.numel()
+    z, ids, t = randn(gen(3), 3, 500), torch.zeros(3, 2, dtype=torch.int32, device="cuda"), randn(gen(4), 3, 2)
+    loss, l2 = torch.empty(3, device="cuda"), torch.empty(2, 3, device="cuda")
+    tiles = torch.empty(1, dtype=torch.float64, device="cuda")
+    ctx = sd.slidedp_create(0, 0)
+    ws = torch.empty(max(ctx.slidedp_attention_workspace(q, q), ctx.slidedp_qk_norm_rope_workspace(q, q)), dtype=torch.uint8, device="cuda")
+    ctx.slidedp_attention(q, q, q, out, lse)
+    ctx.slidedp_grad_norm([q], n, 1.0, True)
+    ctx.slidedp_grad_norm_tiles([q], n, 1.0, tiles)
+    want = ctx.slidedp_grad_norm_finish(1.0, fetch=True)
+    calls = [lambda: ctx.slidedp_attention(q, q, q, out2, lse),
+             lambda: ctx.slidedp_attention_backward(q, q, q, out, lse, q, out2, out2.clone(), out2.clone(), ws),
+             lambda: ctx.slidedp_qk_norm_rope(q, q, None, None, None, None, out2, out2.clone()),
+             lambda: ctx.slidedp_qk_norm_rope_backward(q, q, None, None, None, None, q, q, out2, out2.clone(), *dw, ws),
+             lambda: ctx.slidedp_distill_loss(z, ids, t, None, loss, l2),
+             lambda: ctx.slidedp_distill_loss_backward(z, ids, t, None, l2, None, z.clone()),
+             lambda: ctx.slidedp_distill_step(z, ids, t, None, None, loss, l2, z.clone()),
+             lambda: ctx.slidedp_grad_norm_finish(1.0, fetch=True),
+             lambda: ctx.slidedp_grad_norm_finish_from(tiles, 1, 1.0, fetch=True)]
+    for call in calls:
+        for _ in range(2):
+            give_up(ctx)
+            ctx.slidedp_grad_norm_finish(1.0)              # without waiting there is nothing to tell yet
+            with pytest.raises(sd.SlideDPError) as e:
+                call()
+            assert e.value.status == sd.ERR_TIMEOUT
+            call()
+    torch.cuda.synchronize()
+    assert ctx.slidedp_grad_norm_finish(1.0, fetch=True) == want
+    give_up(ctx)
+    with pytest.raises(sd.SlideDPError) as e:
+        ctx.slidedp_destroy()
+    assert e.value.status == sd.ERR_TIMEOUT
+    ctx.slidedp_destroy()                                 # it is gone
