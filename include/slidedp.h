@@ -29,7 +29,8 @@
  *    default stream). Device-resident calls only enqueue work on that stream and return.
  *  - master / m / v are updated in place; gradients are read-only; param_bf16_out must
  *    not overlap any other argument.
- *  - A context is not thread-safe: use one per host thread, or serialise the calls on it. All
+ *  - A context is not thread-safe: use one per host thread, or serialise the calls on it (the operators of slidedp_ops.h
+ *    are the exception, among themselves). All
  *    device pointers passed with a context must live on that context's device.
  */
 #ifndef SLIDEDP_H

@@ -8,8 +8,8 @@
  * Conventions are those of slidedp.h: every call returns SLIDEDP_OK or a negative status and only
  * enqueues work on cuda_stream; the caller owns every buffer, workspaces included; nothing is kept
  * between calls. Results are bit-reproducible: no call adds floating-point numbers with atomics.
- * Calls on one context may go to different streams, but workspaces must not be shared by calls
- * that can overlap.
+ * Calls of this header on one context may go to different streams and come from different threads, also at once (but not
+ * beside other calls on that context); workspaces must not be shared by calls that can overlap.
  *
  * The attention and distillation kernels wait on copies and on blocks of their own launch; every
  * such wait is bounded. If one runs out, the results of that call are not complete, and the first of these calls on the

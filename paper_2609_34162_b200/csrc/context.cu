@@ -29,8 +29,8 @@ size_t slidedp_state_bytes(int64_t n) {
   return n < 0 ? 0 : (size_t)n * (2 + 2 + 4 + 4 + 4);
 }
 
-int slidedp_last_cuda_error(const slidedp_ctx* ctx) { return ctx ? ctx->last_cuda : 0; }
-int64_t slidedp_kernel_launches(const slidedp_ctx* ctx) { return ctx ? ctx->launches : 0; }
+int slidedp_last_cuda_error(const slidedp_ctx* ctx) { return ctx ? ctx->last_cuda.load() : 0; }
+int64_t slidedp_kernel_launches(const slidedp_ctx* ctx) { return ctx ? ctx->launches.load() : 0; }
 
 int slidedp_set_wait_seconds(slidedp_ctx* ctx, double seconds) {
   if (!ctx || !(seconds > 0.0) || seconds > 86400.0) return SLIDEDP_ERR_INVALID_ARG;

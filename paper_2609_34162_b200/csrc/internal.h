@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <vector>
 
 #include "types.h"
@@ -38,12 +39,13 @@ struct IpcMapping {
 struct slidedp_ctx {
   int device = 0;
   size_t budget = 0;
-  int last_cuda = 0;
-  int64_t launches = 0;
+  // atomic: operators (slidedp_ops.h) may be called from several threads at once
+  std::atomic<int> last_cuda{0};
+  std::atomic<int64_t> launches{0};
   double wait_seconds = slidedp::host::kDefaultWaitSeconds;   // slidedp_set_wait_seconds
   // host-side fault injection (slidedp_test_fail_nth_call): the countdown-th guarded runtime
   // call from now is not issued and reports cudaErrorUnknown; <= 0: off
-  int64_t fail_countdown = 0;
+  std::atomic<int64_t> fail_countdown{0};
   // norm workspace
   double* partials = nullptr;
   int64_t partials_cap = 0;
@@ -52,7 +54,7 @@ struct slidedp_ctx {
   double* host_scalars = nullptr;   // pinned mirror
   bool norm_issued = false;
   int* kernel_error = nullptr;      // pinned: set by a kernel whose bounded wait ran out
-  uint32_t wait_polls = slidedp::kWaitPolls;   // bound of those waits (slidedp_test_wait_polls)
+  std::atomic<uint32_t> wait_polls{slidedp::kWaitPolls};   // bound of those waits (slidedp_test_wait_polls)
   cudaEvent_t scalar_event = nullptr;
   // host-resident streaming
   cudaStream_t s_in = nullptr, s_compute = nullptr, s_out = nullptr;
@@ -98,7 +100,10 @@ inline int check_kernel_error(slidedp_ctx* ctx) {
 
 // True when the host-side fault injection of `ctx` says that the next guarded call must fail.
 inline bool injected_failure(slidedp_ctx* ctx) {
-  return ctx && ctx->fail_countdown > 0 && --ctx->fail_countdown == 0;
+  if (!ctx) return false;
+  int64_t left = ctx->fail_countdown.load(std::memory_order_relaxed);
+  while (left > 0 && !ctx->fail_countdown.compare_exchange_weak(left, left - 1)) {}
+  return left == 1;
 }
 
 // Returns SLIDEDP_ERR_CUDA (recording the error in ctx) when a runtime call fails. Under fault

@@ -1,5 +1,7 @@
 """Waits inside the operators' kernels that run out: the kernel returns, the next call says SLIDEDP_ERR_TIMEOUT once, and the
 context works as before. The waits are made to run out by a short limit on healthy launches; nothing hangs or fails on the GPU."""
+import threading
+
 import pytest
 import torch
 
@@ -128,3 +130,34 @@ def test_every_operator_and_the_norm_report_a_wait_that_ran_out(sd):
         ctx.slidedp_destroy()
     assert e.value.status == sd.ERR_TIMEOUT
     ctx.slidedp_destroy()                                 # it is gone
+
+
+def test_threads_on_a_context_count_and_fail_exactly(sd):
+    """Several threads in one context's operators: no launch is lost from the count, and an injected failure happens once."""
+    ctx, threads, calls = sd.slidedp_create(0, 0), 8, 1500
+    failed, statuses = [], []
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            x = randn(gen(i), 1, 2, 8)
+            y = torch.empty_like(x)
+            for _ in range(calls):
+                try:
+                    ctx.slidedp_qk_norm_rope(x, x, None, None, None, None, y, y)
+                except sd.SlideDPError as e:
+                    failed.append(i)
+                    statuses.append(e.status)
+            torch.cuda.current_stream().synchronize()
+    try:
+        for nth in (0, threads * calls // 2):
+            before = ctx.slidedp_kernel_launches()
+            ctx.slidedp_test_fail_nth_call(nth)
+            ts = [threading.Thread(target=work, args=(i,)) for i in range(threads)]
+            for t in ts:
+                t.start()
+            for t in ts:
+                t.join()
+            assert statuses == ([sd.ERR_CUDA] if nth else [])
+            assert ctx.slidedp_kernel_launches() - before == threads * calls - len(failed)
+    finally:
+        ctx.slidedp_destroy()
