@@ -220,28 +220,26 @@ __device__ __forceinline__ float exp2_approx(float x) {   // 2 ulp; 0 for -inf
   return y;
 }
 // 2^x on the multiply-add pipe, for a share of the exponentials where the special-function pipe would be the
-// bound: x = n + f with n = floor x (adding 1.5 * 2^23, rounded down, leaves n in the low bits), 2^f on [0, 1)
-// by the polynomial of degree 4 with p(0) = 1 and the least greatest relative error (2.9e-6, from a linear
-// program; the result is rounded to BF16, 4e-3), n added to the exponent. Below -127 the result is exactly
-// zero; NaN stays NaN; x is at most a few units above zero.
+// bound: x = n + f with n = floor x, 2^f on [0, 1) by the polynomial of degree 4 with p(0) = 1 and the least greatest
+// relative error (2.9e-6, from a linear program; the result is rounded to BF16, 4e-3), times 2^n. Adding 1.5 * 2^23 + 127,
+// rounded down, leaves n + 127 in the low bits: shifted up, the bits of 2^n. A product, not a sum of exponents: that turned a
+// NaN into the largest finite value. Below -126 the result is exactly zero; NaN stays NaN; x is at most a few units above zero.
 __device__ __forceinline__ void exp2_pair_poly(uint64_t x, float* lo, float* hi) {
-  float a, b, ta, tb, pa, pb;
+  float a, b, ta, tb;
   split(x, &a, &b);
   asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(a));   // -127
   asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(b));
   x = pair(a, b);
   uint64_t t;
-  asm("add.rm.f32x2 %0, %1, %2;" : "=l"(t) : "l"(x), "l"(pair(12582912.0f, 12582912.0f)));
-  const uint64_t f = fma2(add2(t, pair(-12582912.0f, -12582912.0f)), pair(-1.0f, -1.0f), x);
+  asm("add.rm.f32x2 %0, %1, %2;" : "=l"(t) : "l"(x), "l"(pair(12583039.0f, 12583039.0f)));
+  const uint64_t f = fma2(add2(t, pair(-12583039.0f, -12583039.0f)), pair(-1.0f, -1.0f), x);
   const auto step = [&](uint64_t p, float c) { return fma2(p, f, pair(c, c)); };
   uint64_t p = step(pair(0.013426683843135834f, 0.013426683843135834f), 0.052242472767829895f);
   p = step(p, 0.241280198097229f);
   p = step(p, 0.6930448412895203f);
   p = step(p, 1.0f);
   split(t, &ta, &tb);
-  split(p, &pa, &pb);
-  *lo = __int_as_float(__float_as_int(pa) + (__float_as_int(ta) << 23));
-  *hi = __int_as_float(__float_as_int(pb) + (__float_as_int(tb) << 23));
+  split(mul2(p, pair(__int_as_float(__float_as_int(ta) << 23), __int_as_float(__float_as_int(tb) << 23))), lo, hi);
 }
 __device__ __forceinline__ float rcp_approx(float x) {    // 1 ulp
   float y;

@@ -1,0 +1,68 @@
+"""NaN and infinities in what a row of attention sees and in what it does not see: the first must show, the second must not,
+and neither may cost more than a multiple of an ordinary pass."""
+import math
+
+import pytest
+import torch
+
+import operators_ref as ref
+from test_operators_gpu import BF16, F32, assert_close, ctx, gen, randn, sd, tolerance  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(T, Hq, Hk, D, seed):
+    g = gen(seed)
+    return [randn(g, T, h, D, dtype=BF16) for h in (Hq, Hk, Hk, Hq)]
+
+
+def forward(ctx, q, k, v, **kw):
+    out, lse = torch.empty_like(q), torch.empty(q.shape[1], q.shape[0], device="cuda")
+    ctx.slidedp_attention(q, k, v, out, lse, **kw)
+    return out, lse
+
+
+MODES = [dict(), dict(slopes=True), dict(softcap=20.0), dict(softcap=0.5, slopes=True)]
+
+
+def keywords(mode, heads):
+    kw = dict(mode)
+    if kw.get("slopes"):
+        kw["slopes"] = 2.0 ** -torch.arange(1, heads + 1, device="cuda").float()
+    return kw
+
+
+@pytest.mark.parametrize("D", [64, 128, 20])
+@pytest.mark.parametrize("mode", MODES, ids=["plain", "bias", "cap", "cap_bias"])
+def test_a_nan_key_shows_in_every_row_that_sees_it(ctx, D, mode):
+    T, Hq, Hk = 300, 4, 2
+    q, k, v, _ = inputs(T, Hq, Hk, D, seed=D)
+    kw = keywords(mode, Hq)
+    want = ref.attention(q, k, v, D ** -0.5, ref.visible(T, None, None, True, "cuda"), kw.get("softcap", 0.0), kw.get("slopes"))
+    for j in [*range(18), 127, 128, 130, 133, 143, 257, 299]:
+        for value, also_v in ((math.nan, False), (math.nan, True)):
+            k2, v2 = k.clone(), v.clone()
+            k2[j, 1, 3] = value
+            if also_v:
+                v2[j, 1] = value
+            out, lse = forward(ctx, q, k2, v2, **kw)
+            assert out[j:, 2:].isnan().all() and lse[2:, j:].isnan().all(), j
+            tol = tolerance(want["out"], BF16, want["out_bound"])
+            assert_close("rows before it", out[:j], want["out"][:j], tol[:j])
+            assert_close("the other heads", out[:, :2], want["out"][:, :2], tol[:, :2])
+            rest = lse.clone()
+            rest[2:, j:] = want["lse"][2:, j:].float()
+            assert_close("lse", rest, want["lse"], 2e-5 + 2e-6 * want["lse"].abs())
+
+
+@pytest.mark.parametrize("D", [64, 128, 20])
+@pytest.mark.parametrize("mode", MODES, ids=["plain", "bias", "cap", "cap_bias"])
+def test_a_nan_query_is_nan_whatever_it_sees(ctx, D, mode):
+    T, H = 270, 2
+    q, k, v, _ = inputs(T, H, H, D, seed=D + 1)
+    for i in [0, 1, 2, 5, 131, 269]:
+        q2 = q.clone()
+        q2[i, 1] = math.nan
+        out, lse = forward(ctx, q2, k, v, **keywords(mode, H))
+        assert out[i, 1].isnan().all() and lse[1, i].isnan(), i
+        assert int(out.isnan().any(-1).sum()) == 1 and int(lse.isnan().sum()) == 1, i
