@@ -63,7 +63,8 @@ static __device__ __noinline__ void attention_out_row(const AttnParams& p, int i
     load_row(p.k, j, hk, p.head_dim, x);
     const float s = score(p, dot(q, x), slope, i - j, &g);
     load_row(p.v, j, hk, p.head_dim, x);
-    const float top = fmaxf(m, s), keep = exp2f(m - top), e = exp2f(s - top);
+    const float top = fmaxf(m, s), shift = top == -INFINITY ? 0.0f : top;   // scores of -inf weigh nothing, also when they come first
+    const float keep = exp2f(m - shift), e = exp2f(s - shift);
     m = top;
     l = l * keep + e;
 #pragma unroll

@@ -66,3 +66,22 @@ def test_a_nan_query_is_nan_whatever_it_sees(ctx, D, mode):
         out, lse = forward(ctx, q2, k, v, **keywords(mode, H))
         assert out[i, 1].isnan().all() and lse[1, i].isnan(), i
         assert int(out.isnan().any(-1).sum()) == 1 and int(lse.isnan().sum()) == 1, i
+
+
+@pytest.mark.parametrize("D", [64, 128, 20])
+def test_a_key_with_a_score_of_minus_infinity_weighs_nothing(ctx, D):
+    """As if it were not there, wherever it lies; a row with nothing else is 0 / 0."""
+    T, H = 200, 2
+    q, k, v, _ = inputs(T, H, H, D, seed=D + 2)
+    q[:, :, 0] = 1.0
+    seen = ref.visible(T, None, None, True, "cuda")
+    for js in ([0], [0, 1, 2], [5], [128], [199], [0, 127, 128, 150]):
+        k2, ok = k.clone(), seen.clone()
+        k2[js, :, 0] = -math.inf
+        ok[:, js] = False
+        want = ref.attention(q, k, v, D ** -0.5, ok)
+        out, lse = forward(ctx, q, k2, v)
+        some = ok.any(1)
+        assert_close("out", out[some], want["out"][some], tolerance(want["out"], BF16, want["out_bound"])[some])
+        assert out[~some].isnan().all() and torch.all(lse[:, ~some] == -math.inf)
+        assert_close("lse", lse[:, some], want["lse"][:, some], 2e-5 + 2e-6 * want["lse"][:, some].abs())
