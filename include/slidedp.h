@@ -127,7 +127,7 @@ SLIDEDP_API int slidedp_destroy(slidedp_ctx* ctx);
  * can be exercised; nth <= 0 switches the hook off. The countdown stops at the failure.
  *
  * slidedp_test_wait_polls is another one: waits inside the kernels of slidedp_ops.h that the context launches from now on
- * give up after `polls` polls (0: at once) instead of the seconds' worth that they allow, so that healthy launches run out
+ * give up after `polls` polls (0: at once) instead of the minute's worth that they allow, so that healthy launches run out
  * of them and return; polls < 0 restores the limit.
  */
 SLIDEDP_API int slidedp_set_wait_seconds(slidedp_ctx* ctx, double seconds);

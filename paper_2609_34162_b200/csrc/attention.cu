@@ -14,17 +14,17 @@ constexpr int kGeneralThreads = 128;
 __global__ void __launch_bounds__(kGeneralThreads) attention_forward_general_kernel(const __grid_constant__ AttnParams p) {
   start_after_previous_kernel();
   const int i = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
-  if (i < p.tokens) attention_out_row(p, i, blockIdx.y, true);
+  if (i < p.tokens) attention_out_row<false>(p, i, blockIdx.y, true);
 }
 __global__ void __launch_bounds__(kGeneralThreads) attention_dq_general_kernel(const __grid_constant__ AttnParams p) {
   start_after_previous_kernel();
   const int i = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
-  if (i < p.tokens) attention_dq_row(p, i, blockIdx.y, 0, p.head_dim);
+  if (i < p.tokens) attention_dq_row<false>(p, i, blockIdx.y, 0, p.head_dim);
 }
 __global__ void __launch_bounds__(kGeneralThreads) attention_dkv_general_kernel(const __grid_constant__ AttnParams p) {
   start_after_previous_kernel();
   const int j = blockIdx.x * (kGeneralThreads / kLanes) + threadIdx.x / kLanes;
-  if (j < p.tokens) attention_dkv_row(p, j, blockIdx.y, true, true, 0, p.head_dim);
+  if (j < p.tokens) attention_dkv_row<false>(p, j, blockIdx.y, true, true, 0, p.head_dim);
 }
 
 // row_lse[h][i] = lse log2 e, row_delta[h][i] = sum_d dout out, zeros for the rows of the padding: one warp per row.

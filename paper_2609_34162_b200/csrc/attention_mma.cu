@@ -599,11 +599,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         nan |= store_columns(stages + warp * kStageBytes, &map_o, h, row0, c * 64, p.head_dim, p.tokens, inv,
                              [&](int k, uint32_t* o) { tmem_columns(at_o + c * 64 + k * 32, from < to, o); });
       if (live) p.lse[(int64_t)h * p.tokens + i] = some ? (m * unit + log2f(l)) * (1.0f / kLog2e) : -INFINITY;
-      uint32_t redo = __ballot_sync(0xffffffffu, nan);
+      // a row with a NaN among its own scores (l is NaN), or with nothing above -inf, is NaN
+      uint32_t redo = __ballot_sync(0xffffffffu, nan && (l > 0.0f || !some));
       if (redo) {
         if (lane == 0) tma_stores_done();
         __syncwarp();
-        for (; redo; redo &= redo - 1) attention_out_row(p, row0 + __ffs(redo) - 1, h, false);   // its lse is right: masked scores are dropped
+        redo = spoiled_out_rows(p, redo, row0, h, lo, hi);
+        for (; redo; redo &= redo - 1) attention_out_row<true>(p, row0 + __ffs(redo) - 1, h, false);   // its lse is right: masked scores are dropped
       }
     }
     if (lane == 0) tma_stores_done();
@@ -961,7 +963,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           if (redo) {
             if (lane == 0) tma_stores_done();
             __syncwarp();
-            for (; redo; redo &= redo - 1) attention_dkv_row(p, row0 + __ffs(redo) - 1, hk, is_k, !is_k, d0, min(d0 + 64, p.head_dim));
+            const int d1 = min(d0 + 64, p.head_dim);
+            redo = spoiled_key_rows(p, redo, row0, hk, lo, hi, !is_k, d0, d1);
+            for (; redo; redo &= redo - 1) attention_dkv_row<true>(p, row0 + __ffs(redo) - 1, hk, is_k, !is_k, d0, d1);
           }
         }
         joined = true;
@@ -976,7 +980,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         if (redo) {
           if (lane == 0) tma_stores_done();
           __syncwarp();
-          for (; redo; redo &= redo - 1) attention_dkv_row(p, row0 + __ffs(redo) - 1, hk, g == 1, g == 0, 0, p.head_dim);
+          redo = spoiled_key_rows(p, redo, row0, hk, lo, hi, g == 0, 0, p.head_dim);
+          for (; redo; redo &= redo - 1) attention_dkv_row<true>(p, row0 + __ffs(redo) - 1, hk, g == 1, g == 0, 0, p.head_dim);
         }
       }
     }
@@ -1232,11 +1237,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         const bool nan = store_columns(stages + warp * kStageBytes, &map_dq, h, row0, g * 64, p.head_dim, p.tokens, p.scale, [&](int k, uint32_t* o) {
           tmem_columns(at_dq + ((uint32_t)r << 16) + g * 64 + k * 32, steps > 0, o);
         });
-        uint32_t redo = __ballot_sync(0xffffffffu, nan);
+        // a NaN among the row's scores shows in lse, one in dout or in the values it sees in delta: then the row is NaN
+        uint32_t redo = __ballot_sync(0xffffffffu, nan && ((finite(lse) && finite(delta)) || lo >= hi));
         if (redo) {
           if (lane == 0) tma_stores_done();
           __syncwarp();
-          for (; redo; redo &= redo - 1) attention_dq_row(p, row0 + __ffs(redo) - 1, h, g * 64, min(g * 64 + 64, p.head_dim));
+          for (; redo; redo &= redo - 1) attention_dq_row<true>(p, row0 + __ffs(redo) - 1, h, g * 64, min(g * 64 + 64, p.head_dim));
         }
       }
     }

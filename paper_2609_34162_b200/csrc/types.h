@@ -7,8 +7,8 @@ namespace slidedp {
 
 constexpr int kMaxRanks = 16;
 
-// How often a wait inside a kernel polls before it gives up: each poll suspends the thread for a while, so this is
-// seconds where microseconds are expected.
+// How often a wait inside a kernel polls before it gives up: a poll suspends the thread for up to 4 us, so this is about a
+// minute where microseconds are expected.
 constexpr uint32_t kWaitPolls = 1u << 24;
 
 struct GradPtrs {

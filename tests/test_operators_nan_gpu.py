@@ -85,3 +85,64 @@ def test_a_key_with_a_score_of_minus_infinity_weighs_nothing(ctx, D):
         assert_close("out", out[some], want["out"][some], tolerance(want["out"], BF16, want["out_bound"])[some])
         assert out[~some].isnan().all() and torch.all(lse[:, ~some] == -math.inf)
         assert_close("lse", lse[:, some], want["lse"][:, some], 2e-5 + 2e-6 * want["lse"][:, some].abs())
+
+
+def backward(ctx, q, k, v, out, lse, do, **kw):
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    ws = torch.empty(ctx.slidedp_attention_workspace(q, k), dtype=torch.uint8, device="cuda")
+    ctx.slidedp_attention_backward(q, k, v, out, lse, do, dq, dk, dv, ws, **kw)
+    return dict(dq=dq, dk=dk, dv=dv)
+
+
+def timed(f):
+    best = math.inf
+    for _ in range(3):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        r = f()
+        b.record()
+        b.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return r, best
+
+
+@pytest.mark.parametrize("Hq,Hk,D", [(8, 2, 128), (8, 2, 64), (3, 3, 96)])
+@pytest.mark.parametrize("where", ["k", "v", "q", "do", "token"])
+def test_one_nan_in_a_long_document(ctx, Hq, Hk, D, where):
+    """At token t, in the first document of two: what it must and must not reach, and what it may cost."""
+    T, cu, t, G, c = 2600, [0, 2500, 2600], 40, Hq // Hk, 3
+    q, k, v, do = inputs(T, Hq, Hk, D, seed=7)
+    kw = dict(cu_docs=torch.tensor(cu, dtype=torch.int32, device="cuda"))
+    want = ref.attention(q, k, v, D ** -0.5, ref.visible(T, cu, None, True, "cuda"), 0.0, None, do)
+    (out, lse), clean_f = timed(lambda: forward(ctx, q, k, v, **kw))
+    grads, clean_b = timed(lambda: backward(ctx, q, k, v, out, lse, do, **kw))
+    for n, x in (("k", k), ("v", v), ("q", q), ("do", do)):
+        if where == n:
+            x[t, 0, c] = math.nan            # head 0, and as a key head the queries' heads 0 .. G - 1
+        elif where == "token":
+            x[t] = math.nan
+    (out, lse), nan_f = timed(lambda: forward(ctx, q, k, v, **kw))
+    got, nan_b = timed(lambda: backward(ctx, q, k, v, out, lse, do, **kw))
+    ctx.slidedp_qk_norm_rope(q, k, None, None, None, None, q.clone(), k.clone())     # would tell of a wait that ran out
+    got["out"] = out
+    nans = {n: torch.zeros_like(x, dtype=torch.bool) for n, x in got.items()}
+    doc, late, early = slice(0, 2500), slice(t, 2500), slice(0, t + 1)
+    if where == "k":         # every later query's scores
+        nans["out"][late, :G] = nans["dq"][late, :G] = nans["dk"][doc, 0] = nans["dv"][doc, 0] = True
+    elif where == "v":       # one column of the outputs, and with it delta
+        nans["out"][late, :G, c] = nans["dq"][late, :G] = nans["dk"][doc, 0] = True
+    elif where == "q":       # one row
+        nans["out"][t, 0] = nans["dq"][t, 0] = nans["dk"][early, 0] = nans["dv"][early, 0] = True
+    elif where == "do":
+        nans["dq"][t, 0] = nans["dk"][early, 0] = nans["dv"][early, 0, c] = True
+    else:
+        nans["out"][late] = nans["dq"][late] = nans["dk"][doc] = nans["dv"][doc] = True
+    assert torch.equal(lse.isnan(), nans["out"].all(-1).T)
+    for n, x in got.items():
+        assert torch.equal(x.isnan(), nans[n]), n
+        tol = tolerance(want[n], BF16, want[n + "_bound"])
+        keep = ~nans[n]
+        assert_close(n, x[keep], want[n][keep], tol[keep])
+    # rows whose NaN is their own are left as they are; redoing them cost over a thousand times an ordinary pass
+    assert nan_f < 10 * clean_f + 1.0
+    assert nan_b < (10 if where in ("k", "v", "token") else 1000) * clean_b + 1.0
