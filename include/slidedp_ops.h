@@ -140,7 +140,8 @@ SLIDEDP_API size_t slidedp_attention_workspace(const slidedp_attn_args* args);
  * logsumexp(z) of every row (zeros there if w_label is 0 or labels NULL: the term is off).
  *
  * Gradient: d_logits[r] = row_grad[r] * d loss[r] / d z, with row_grad: rows floats (nullable: ones).
- * slidedp_distill_loss_backward takes the forward's lse; slidedp_distill_step computes loss, lse and
+ * slidedp_distill_loss_backward takes the forward's lse (probabilities from it have the relative error of its rounding, up to
+ * 8e-6; rows with an lse beyond 128, where that would be more, are summed again); slidedp_distill_step computes loss, lse and
  * gradient in one call that reads the logits once. d_logits may be the logits themselves (same
  * address and stride).
  */

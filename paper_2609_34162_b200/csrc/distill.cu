@@ -300,11 +300,12 @@ struct Slice {
   Row<T> row;
   int64_t lo, hi, mid_lo;
   const uint4* mid;
-  __device__ Slice(const DistillParams& p, int size_, int rank_, int64_t r_)
+  __device__ Slice(const DistillParams& p, int size_, int rank_, int64_t r_) : Slice(p, size_, rank_, r_, p.chunks_per_block) {}
+  __device__ Slice(const DistillParams& p, int size_, int rank_, int64_t r_, int64_t per_block)
       : rank(rank_), size(size_), r(r_), row(static_cast<const T*>(p.z) + r * p.z_stride, p.vocab) {
     const int64_t chunks = (p.vocab + row.head + Logit<T>::kPer - 1) / Logit<T>::kPer;
-    lo = rank * p.chunks_per_block;
-    hi = lo + p.chunks_per_block < chunks ? lo + p.chunks_per_block : chunks;
+    lo = rank * per_block;
+    hi = lo + per_block < chunks ? lo + per_block : chunks;
     if (lo > hi) lo = hi;
     mid_lo = lo < hi && !row.whole(lo) ? lo + 1 : lo;
     n = (int)((hi > mid_lo && !row.whole(hi - 1) ? hi - 1 : hi) - mid_lo);
@@ -490,26 +491,59 @@ __global__ void __launch_bounds__(kDistillThreads, distill_min_blocks(U)) distil
   }
 }
 
-// Gradient from the saved lse: blocks of a row share nothing.
+// Sums of a whole row by one block, for rows whose saved lse is too far from zero.
+template <typename T, bool kTwo>
+static __device__ __noinline__ SoftSum row_sums(const DistillParams& p, int64_t r, SoftSum* warps) {
+  const float k0 = p.inv_tau * kLog2e, k1 = kLog2e;
+  const Slice<T> s(p, 1, 0, r, p.vocab);   // no row has more chunks than values
+  SoftSum mine = {-INFINITY, 0.0f, 0.0f};
+  stream_chunks<T, 1>(s.n, [&](int i) { return s.mid[i]; }, [&](int, const uint4* a, int) { accumulate<T, kTwo, 1>(mine, a, k0, k1); });
+  s.edges([&](int, int64_t c) {
+    const uint4 a = s.row.load(c);
+    accumulate<T, kTwo, 1>(mine, &a, k0, k1);
+  });
+  __syncwarp();
+  bool unused = false;
+  return join_block<kTwo>(mine, warps, k0, k1, &unused);
+}
+
+// Gradient from the saved lse: blocks of a row share nothing. p = exp(z / tau - lse) has the relative error of lse's own
+// rounding, |lse| 2^-25, and of differences of that size: (z - m) / tau - rest, with m where the exponent is zero, rounds no
+// larger terms. Where that could be above 2 kFarLse 2^-25 = 8e-6, or lse has lost the sum altogether (a row of the type's
+// lowest value: -3e38 + log vocab), or there is a NaN, the blocks of the row take its sums again instead.
+constexpr float kFarLse = 128.0f;
 template <typename T, bool kTwo>
 __global__ void __launch_bounds__(kDistillThreads) distill_gradient_kernel(const __grid_constant__ DistillParams p, int parts) {
   start_after_previous_kernel();
   extern __shared__ uint4 dynamic[];
+  __shared__ alignas(16) SoftSum warps[kDistillWarps];
   const Slice<T> s(p, parts, blockIdx.x % parts, blockIdx.x / parts);
   const Entries en(dynamic, p.entries);
-  const float l0 = p.lse[s.r] * kLog2e, l1 = p.labels ? p.lse[p.rows + s.r] * kLog2e : l0;
+  const float lse0 = p.lse[s.r], lse1 = kTwo ? p.lse[p.rows + s.r] : lse0;
   const bool some = __syncthreads_or(fetch_entries<T>(p, s.r, s.row.z, en));
+  float m, l0, l1;
+  if (fabsf(lse0) <= kFarLse && fabsf(lse1) <= kFarLse) {
+    m = kTwo ? lse1 : lse0 * p.tau;
+    l0 = fmaf(-m, p.inv_tau, lse0) * kLog2e;
+    l1 = kTwo ? 0.0f : l0;
+  } else {
+    const SoftSum all = row_sums<T, kTwo>(p, s.r, warps);
+    m = finite_shift(all.m);
+    l0 = log2f(all.s0);
+    l1 = kTwo ? log2f(all.s1) : l0;
+    if (parts > 1) cluster_sync();   // the same lse, so all blocks of the row are here: nobody writes what another still reads
+  }
   float a0, a1;
   const GradFactors f = factors<kTwo>(p, p.row_grad ? p.row_grad[s.r] : 1.0f, some, en.id[en.count] >= 0, l0, l1, &a0, &a1);
   T* dz = static_cast<T*>(p.dz) + s.r * p.dz_stride;
-  write_slice<T, kTwo, kDistillUnroll>(s, dz, 0.0f, f);
-  s.edges([&](int, int64_t c) { write_values<T, kTwo>(s.row, dz, c, s.row.load(c), 0.0f, f); });
+  write_slice<T, kTwo, kDistillUnroll>(s, dz, m, f);
+  s.edges([&](int, int64_t c) { write_values<T, kTwo>(s.row, dz, c, s.row.load(c), m, f); });
   if (threadIdx.x < 32) {
     float unused = 0.0f;
     teacher_softmax(p, en, &unused, &unused);
   }
   __syncthreads();
-  write_entries<T, kTwo>(s, dz, en, 0.0f, f, a0, a1);
+  write_entries<T, kTwo>(s, dz, en, m, f, a0, a1);
 }
 
 }  // namespace slidedp
@@ -592,7 +626,7 @@ int run_distill(slidedp_ctx* ctx, const slidedp_distill_args* a, int mode, const
   const size_t smem = Entries::bytes(a->entries);
   FAULT_POINT();
   const auto run = [&](auto kernel) {
-    launch_after(kernel, (unsigned)(p.rows * cluster), kDistillThreads, smem, mode == kBackward ? 1 : cluster, st, p, (int)cluster);
+    launch_after(kernel, (unsigned)(p.rows * cluster), kDistillThreads, smem, cluster, st, p, (int)cluster);
   };
 #define SLIDEDP_KERNEL(KERNEL, ...) \
   (f32 ? (two ? run(KERNEL<float, true __VA_ARGS__>) : run(KERNEL<float, false __VA_ARGS__>)) \

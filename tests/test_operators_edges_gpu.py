@@ -12,7 +12,7 @@ import pytest
 import torch
 
 import operators_ref as ref
-from test_operators_gpu import BF16, F32, attn_case, ctx, gen, randn, sd, tolerance, assert_close  # noqa: F401
+from test_operators_gpu import BF16, F32, attn_case, ctx, distill_inputs, gen, randn, sd, tolerance, assert_close  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -260,3 +260,42 @@ def test_tensor_checks(ctx):
                 dict(lse=torch.empty(T, H, device="cuda").T), dict(q=q[0])):
         with pytest.raises(ValueError):
             call(**bad)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tau,wl", [(2.0, 0.5), (0.5, 0.5), (1.0, 0.5), (2.0, 0.0), (100.0, 0.5), (0.03, 0.25)])
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("V", [3001, 70000])
+def test_distill_backward_of_masked_and_far_off_rows(ctx, dtype, tau, wl, in_place, V):
+    """The gradient from the saved lse: rows whose lse is large, or beyond FP32, or says nothing of the row's sum."""
+    N = 9
+    z, ids, t, labels, gr = distill_inputs(N, V, 6, dtype, seed=29)
+    z[0, 100:] = -math.inf
+    z[1, 50:] = torch.finfo(dtype).min
+    z[2] -= 20000.0
+    z[3] = torch.finfo(dtype).min
+    z[4] += 700.0
+    z[5] = 3.0
+    z[6] -= 127.0
+    z[7, 2000] = 250.0
+    z[8, 7:] = torch.finfo(dtype).min
+    ids[:, :] = torch.arange(6, device="cuda", dtype=torch.int32)
+    labels[:] = 3
+    labels[5] = -1
+    t[5, :] = -math.inf
+    kw = dict(temperature=tau, w_teacher=0.5, w_label=wl)
+    loss, lse = torch.empty(N, device="cuda"), torch.empty(2, N, device="cuda")
+    _, _, want = ref.distill(z.cpu(), ids.cpu(), t.cpu(), labels.cpu(), tau, 0.5, wl, gr.cpu())
+    # a row of one value throughout is a uniform distribution, which the reference's own log p = z / tau - lse does not resolve
+    want[3] = gr[3].double().cpu() * (0.5 * tau + wl) / V
+    for k in range(6):
+        q = torch.softmax(t[3].double().cpu() / tau, 0)[k]
+        want[3, k] -= float(gr[3]) * 0.5 * tau * float(q)
+    want[3, 3] -= float(gr[3]) * wl
+    ctx.slidedp_distill_loss(z, ids, t, labels, loss, lse, **kw)
+    dz = z if in_place else torch.empty_like(z)
+    ctx.slidedp_distill_loss_backward(z, ids, t, labels, lse, gr, dz, **kw)
+    # as for the step, and for rows near zero 2^-24 of lse's size (at most 128) for the two roundings of it
+    gmax = float(gr.abs().max()) * (0.5 * tau + wl)
+    tol = (2.0 ** -8 * want.abs() if dtype == BF16 else 1e-5 * want.abs()) + (4e-6 + 128 * 2.0 ** -24) * gmax + 1e-30
+    assert_close("gradient", dz.cpu(), want, tol)
