@@ -20,7 +20,8 @@
  *
  * BF16 and FP32 tensors need the alignment of their element only; 16-byte aligned bases and
  * strides are faster. All sums, norms and softmax statistics are FP32 and each output is rounded
- * once. Sizes of zero are no-ops.
+ * once. Sizes of zero are no-ops. Factors given as doubles (scale, softcap, temperature, weights, eps) are used as FP32:
+ * ones that FP32 makes infinite, or makes zero where they must be positive, are refused.
  */
 #ifndef SLIDEDP_OPS_H
 #define SLIDEDP_OPS_H

@@ -97,7 +97,9 @@ int check_attn(const slidedp_attn_args* a) {
       a->heads_q % a->heads_kv != 0 || a->head_dim < 1 || a->head_dim > kMaxHeadDim || (a->causal != 0 && a->causal != 1) ||
       a->docs < 0 || a->docs > kMaxTokens || (!a->cu_docs && (a->docs != 1 || a->prefix)))
     return SLIDEDP_ERR_INVALID_ARG;
-  if (!is_finite(a->scale) || !(a->softcap >= 0.0) || !is_finite(a->softcap)) return SLIDEDP_ERR_INVALID_ARG;
+  if (!fits_f32(a->scale * 1.4426950408889634) || !(a->softcap == 0.0 || (positive_f32(a->softcap) && fits_f32(a->softcap * 1.4426950408889634) &&
+                                                                           fits_f32(a->scale / a->softcap))))
+    return SLIDEDP_ERR_INVALID_ARG;
   const uintptr_t small = reinterpret_cast<uintptr_t>(a->cu_docs) | reinterpret_cast<uintptr_t>(a->prefix) |
                           reinterpret_cast<uintptr_t>(a->slopes);
   return small % 4 == 0 ? SLIDEDP_OK : SLIDEDP_ERR_INVALID_ARG;

@@ -557,8 +557,8 @@ int check_distill(const slidedp_distill_args* a) {
   if (!a || a->rows < 0 || a->rows > kMaxTokens || a->vocab < 1 || a->vocab > (1ll << 30) || a->entries < 0 ||
       a->entries > kMaxEntries || (a->dtype != SLIDEDP_BF16 && a->dtype != SLIDEDP_F32) || a->logits_stride < 0)
     return SLIDEDP_ERR_INVALID_ARG;
-  if (!(a->temperature > 0.0) || !is_finite(a->temperature) || !is_finite(1.0 / a->temperature) || !is_finite(a->w_teacher) ||
-      !is_finite(a->w_label))
+  if (!positive_f32(a->temperature) || !positive_f32(1.0 / a->temperature) || !fits_f32(1.4426950408889634 / a->temperature) ||
+      !fits_f32(a->w_teacher * a->temperature * a->temperature) || !fits_f32(a->w_teacher) || !fits_f32(a->w_label))
     return SLIDEDP_ERR_INVALID_ARG;
   return SLIDEDP_OK;
 }

@@ -24,6 +24,10 @@ inline bool heads_aligned(const slidedp_heads* v, int64_t elem_bytes, int64_t by
          (heads <= 1 || v->stride_head * elem_bytes % bytes == 0);
 }
 inline bool is_finite(double x) { return x - x == 0.0; }
+// The kernels compute with FP32 factors: a number that FP32 turns into infinity, or a positive one that it turns into zero,
+// would silently be another.
+inline bool fits_f32(double x) { return is_finite((double)(float)x); }
+inline bool positive_f32(double x) { return fits_f32(x) && (float)x > 0.0f; }
 
 // Launches a kernel of the operators, in clusters of `cluster` blocks if that is above one. It may be set up while the
 // kernel before it in the stream ends: every block of it waits for that kernel before its first access to memory (where it

@@ -631,7 +631,7 @@ int check_qk(const slidedp_qk_args* a) {
   if (a->tokens * (a->heads_q > a->heads_k ? a->heads_q : a->heads_k) > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
   if (a->rope_dim < 0 || a->rope_dim > a->head_dim || a->rope_dim % 2 != 0 || a->table_rows < 0 ||
       (a->interleaved != 0 && a->interleaved != 1) || (a->dtype != SLIDEDP_BF16 && a->dtype != SLIDEDP_F32) ||
-      !(a->eps >= 0.0) || !is_finite(a->eps))
+      !(a->eps >= 0.0) || !fits_f32(a->eps) || (a->eps > 0.0 && !positive_f32(a->eps)))
     return SLIDEDP_ERR_INVALID_ARG;
   return SLIDEDP_OK;
 }

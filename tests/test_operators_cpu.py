@@ -85,3 +85,17 @@ def test_workspaces_and_refused_arguments(sd):
     assert lib.slidedp_distill_loss(None, None, *[None] * 7) == sd.ERR_INVALID_ARG
     assert lib.slidedp_distill_loss_backward(None, None, *[None] * 8) == sd.ERR_INVALID_ARG
     assert lib.slidedp_distill_step(None, None, *[None] * 9) == sd.ERR_INVALID_ARG
+
+
+def test_factors_that_fp32_does_not_hold_are_refused(sd):
+    """They would otherwise be used as zero (a cap that is silently off) or infinity."""
+    lib = sd._lib
+    ok = dict(tokens=5, heads_q=4, heads_kv=2, head_dim=64, causal=1, docs=1, scale=1.0, softcap=0.0)
+    at = lambda **kw: lib.slidedp_attention_workspace(ctypes.byref(sd._AttnArgs(**{**ok, **kw})))  # noqa: E731
+    for good in (dict(scale=1e30), dict(scale=-1e-30), dict(softcap=1e-20), dict(softcap=1e30), dict(scale=1e-300)):
+        assert at(**good) > 0, good
+    for bad in (dict(scale=1e39), dict(scale=-3.3e38), dict(softcap=1e-46), dict(softcap=1e39), dict(softcap=1e300), dict(scale=1e20, softcap=1e-20)):
+        assert at(**bad) == 0, bad
+    ok = dict(tokens=5, heads_q=4, heads_k=2, head_dim=64, rope_dim=64, interleaved=0, dtype=0, table_rows=9, eps=1e-6)
+    qk = lambda **kw: lib.slidedp_qk_norm_rope_workspace(ctypes.byref(sd._QkArgs(**{**ok, **kw})))  # noqa: E731
+    assert qk(eps=0.0) > 0 and qk(eps=1e-40) > 0 and qk(eps=1e39) == 0 and qk(eps=1e-50) == 0

@@ -299,3 +299,15 @@ def test_distill_backward_of_masked_and_far_off_rows(ctx, dtype, tau, wl, in_pla
     gmax = float(gr.abs().max()) * (0.5 * tau + wl)
     tol = (2.0 ** -8 * want.abs() if dtype == BF16 else 1e-5 * want.abs()) + (4e-6 + 128 * 2.0 ** -24) * gmax + 1e-30
     assert_close("gradient", dz.cpu(), want, tol)
+
+
+def test_distill_factors_that_fp32_does_not_hold_are_refused(ctx, sd):
+    z, ids, t, labels, _ = distill_inputs(3, 50, 4, F32, seed=1)
+    loss, lse = torch.full((3,), 7.0, device="cuda"), torch.full((2, 3), 7.0, device="cuda")
+    for bad in (dict(temperature=1e-39), dict(temperature=1e39), dict(temperature=1e-46), dict(w_teacher=1e39), dict(w_label=-1e39),
+                dict(temperature=1e15, w_teacher=1e15)):
+        with pytest.raises(sd.SlideDPError) as e:
+            ctx.slidedp_distill_loss(z, ids, t, labels, loss, lse, **bad)
+        assert e.value.status == sd.ERR_INVALID_ARG, bad
+    assert torch.all(loss == 7.0) and torch.all(lse == 7.0)
+    ctx.slidedp_distill_loss(z, ids, t, labels, loss, lse, temperature=1e-30)
