@@ -101,14 +101,21 @@ struct ScoreMod {
         q = step(q, 0.1327691525220871f);
         q = step(q, -0.3333006501197815f);
         t = fma2(mul2(q, z), y, y);
+        split(t, &th[0], &th[1]);
+        split(fma2(mul2(t, t), pair(-1.0f, -1.0f), pair(1.0f, 1.0f)), &grad[0], &grad[1]);
       } else {
-        // tanh y = 1 - 2 / (1 + exp 2y): absolute error near 2^-23, and 1 and -1 at the ends
-        float e0, e1;
+        // With r = 1 / (1 + exp 2|y|): tanh |y| = 1 - 2 r, absolute error near 2^-23, and 1 at the end; the derivative is
+        // 4 r (1 - r), which keeps its digits there (1 - tanh^2 does not: a quarter of it is lost at y = 8)
+        float e0, e1, y0, y1;
         split(mul2(y, pair(2.0f * kLog2e, 2.0f * kLog2e)), &e0, &e1);
-        t = fma2(pair(rcp_approx(1.0f + exp2_approx(e0)), rcp_approx(1.0f + exp2_approx(e1))), pair(-2.0f, -2.0f), pair(1.0f, 1.0f));
+        const float r0 = rcp_approx(1.0f + exp2_approx(fabsf(e0))), r1 = rcp_approx(1.0f + exp2_approx(fabsf(e1)));
+        t = pair(r0, r1);
+        split(y, &y0, &y1);
+        split(fma2(t, pair(-2.0f, -2.0f), pair(1.0f, 1.0f)), &th[0], &th[1]);
+        th[0] = copysignf(th[0], y0);
+        th[1] = copysignf(th[1], y1);
+        split(fma2(mul2(t, pair(-4.0f, -4.0f)), t, mul2(t, pair(4.0f, 4.0f))), &grad[0], &grad[1]);
       }
-      split(t, &th[0], &th[1]);
-      split(fma2(mul2(t, t), pair(-1.0f, -1.0f), pair(1.0f, 1.0f)), &grad[0], &grad[1]);
       s[0] = fmaf(cap, th[0], slope * fabsf(distance0));
       s[1] = fmaf(cap, th[1], slope * fabsf(distance1));
     } else {

@@ -44,9 +44,9 @@ __device__ __forceinline__ float score(const AttnParams& p, float raw, float slo
   float s = raw * p.scale;
   *grad = 1.0f;
   if (p.softcap > 0.0f) {
-    const float th = tanhf(s / p.softcap);
-    s = p.softcap * th;
-    *grad = 1.0f - th * th;
+    const float y = s / p.softcap, r = 1.0f / (1.0f + expf(2.0f * fabsf(y)));
+    s = p.softcap * tanhf(y);
+    *grad = 4.0f * r * (1.0f - r);   // 1 - tanh^2, without the difference that cancels when the score is near the cap
   }
   return (s - slope * (float)abs(distance)) * kLog2e;
 }

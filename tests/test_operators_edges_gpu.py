@@ -311,3 +311,19 @@ def test_distill_factors_that_fp32_does_not_hold_are_refused(ctx, sd):
         assert e.value.status == sd.ERR_INVALID_ARG, bad
     assert torch.all(loss == 7.0) and torch.all(lse == 7.0)
     ctx.slidedp_distill_loss(z, ids, t, labels, loss, lse, temperature=1e-30)
+
+
+@pytest.mark.parametrize("D", [64, 128, 132])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_gradients_of_scores_near_the_cap(ctx, D, sign):
+    """Scores six to nine times the cap, whose derivative (1e-5 to 1e-7) is what the gradients of q and k consist of."""
+    T, H, cap = 300, 2, 1.0
+    g = gen(D)
+    q = torch.full((T, H, D), sign, dtype=BF16, device="cuda")
+    k = (1 + 0.1 * randn(g, T, 1, 1).clamp(-1.5, 1.5) + 0.01 * randn(g, T, 1, D)).to(BF16)
+    v, do = randn(g, T, 1, D, dtype=BF16), randn(g, T, H, D, dtype=BF16)
+    scale = 7.4 / D
+    got = attention_pass(ctx, q, k, v, do, scale=scale, softcap=cap)
+    want = ref.attention(q, k, v, scale, ref.visible(T, None, None, True, "cuda"), cap, None, do)
+    for n in ("out", "dq", "dk", "dv"):
+        assert_close(n, got[n], want[n], tolerance(want[n], BF16, want[n + "_bound"]))
