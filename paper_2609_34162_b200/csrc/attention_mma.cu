@@ -214,9 +214,9 @@ struct DocCache {
   int32_t cu[kDocCache + 1], prefix[kDocCache];
   __device__ void fill(const DocMask& m) {   // all threads of the block
     if (!m.cu || m.docs > kDocCache) return;
-    for (int i = threadIdx.x; i <= m.docs; i += blockDim.x) cu[i] = m.cu[i];
+    for (int i = threadIdx.x; i <= m.docs; i += blockDim.x) cu[i] = __ldcg(m.cu + i);
     if (m.prefix)
-      for (int i = threadIdx.x; i < m.docs; i += blockDim.x) prefix[i] = m.prefix[i];
+      for (int i = threadIdx.x; i < m.docs; i += blockDim.x) prefix[i] = __ldcg(m.prefix + i);
   }
   __device__ DocMask mask(const DocMask& m) const {
     DocMask r = m;
@@ -1008,6 +1008,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 // Queries: an item is 128 queries of one head, for which the block walks the keys that they see. Rows are queries; dS goes
 // where its scores were. TMEM: two buffers of scores (the next step's are made while this one's are
 // worked on), dP, dQ. The same document: 567 us, 1.46 PFLOP/s of its 6 head_dim flops per pair, tensor pipe 72 % active.
+//
+// It starts without a wait of its own, beside the keys' kernel. All that it reads was there before that kernel: a block of that
+// lets it start only after its own wait has returned, that is when the kernels before it are complete and their writes are in
+// L2, and from L2 this one reads, by TMA or with loads that pass L1 by (the statistics, offsets that fit the cache; of a longer
+// list of offsets L1 holds nothing older than this kernel's start). It writes dQ only, which no kernel reads that may still
+// run, as no output may lie over an input; and its blocks end after the keys' kernel has.
 template <int HALVES> struct QueriesShape {
   static constexpr int kKStages = 3;   // the next step's scores need K beside this step's dS K
   static constexpr int kVStages = HALVES == 2 ? 1 : 2;   // the stores' room; V comes back while the rows work on dP
@@ -1174,8 +1180,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       float lse = 0.0f, delta = 0.0f;
       if (i < p.tokens) {
         mask.keys_of(i, mask.above(i, pl.above[0], pl.above[1]), &lo, &hi);
-        lse = p.row_lse[h * p.pitch + i];
-        delta = p.row_delta[h * p.pitch + i];
+        lse = __ldcg(p.row_lse + h * p.pitch + i);
+        delta = __ldcg(p.row_delta + h * p.pitch + i);
       }
       for (int j = 0; j < steps; ++j, ++turns) {
         const uint32_t buf = at_s + (turns & 1) * 128 + at;
