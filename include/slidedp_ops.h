@@ -59,7 +59,7 @@ typedef struct {
  * Backward: dq, dk are the gradients of q and k, dw_q and dw_k (device, head_dim floats each,
  * nullable) those of the weights, from the gradients dq_out, dk_out of the outputs. The forward's
  * inputs are needed, its outputs are not. y may be x and dq may be dq_out (same address and
- * strides). workspace: device, slidedp_qk_norm_rope_workspace bytes, 16-byte aligned.
+ * strides; the same address with other strides is refused), but outputs may not overlap otherwise. workspace: device, slidedp_qk_norm_rope_workspace bytes, 16-byte aligned.
  */
 typedef struct {
   int64_t tokens;
@@ -101,6 +101,9 @@ SLIDEDP_API size_t slidedp_qk_norm_rope_workspace(const slidedp_qk_args* args);
  * Backward: the gradients of q, k and v from d_out (the gradient of out), with the forward's out
  * and lse. The slopes are constants and have none. workspace: device,
  * slidedp_attention_workspace bytes, 16-byte aligned.
+ *
+ * In both directions no output may overlap an input or another output: the kernels read inputs, also of other rows and heads,
+ * while they write (in the backward pass two of them at a time). Views that start at the same address are refused.
  */
 typedef struct {
   int64_t tokens;
@@ -144,7 +147,7 @@ SLIDEDP_API size_t slidedp_attention_workspace(const slidedp_attn_args* args);
  * slidedp_distill_loss_backward takes the forward's lse (probabilities from it have the relative error of its rounding, up to
  * 8e-6; rows with an lse beyond 128, where that would be more, are summed again); slidedp_distill_step computes loss, lse and
  * gradient in one call that reads the logits once. d_logits may be the logits themselves (same
- * address and stride).
+ * address and stride; the same address with another stride is refused).
  */
 typedef struct {
   int64_t rows, vocab;

@@ -139,6 +139,10 @@ bool tma_view(const slidedp_heads* v, int64_t tokens, int heads) {
          (heads <= 1 || v->stride_head > 0) && v->stride_token < (1ll << 38) && v->stride_head < (1ll << 38);
 }
 
+// Whether two views start at the same place: outputs that lie over what other blocks still read are refused where that is
+// plain to see.
+bool same_start(const slidedp_heads* a, const slidedp_heads* b) { return a->data == b->data; }
+
 unsigned general_blocks(int64_t rows) {
   return (unsigned)((rows + kGeneralThreads / kLanes - 1) / (kGeneralThreads / kLanes));
 }
@@ -152,7 +156,7 @@ int slidedp_attention(slidedp_ctx* ctx, const slidedp_attn_args* a, const slided
   if (!ctx || check_attn(a) != SLIDEDP_OK) return SLIDEDP_ERR_INVALID_ARG;
   if (a->tokens == 0) return SLIDEDP_OK;
   if (!heads_ok(q, 2) || !heads_ok(k, 2) || !heads_ok(v, 2) || !heads_ok(out, 2) || !lse ||
-      reinterpret_cast<uintptr_t>(lse) % 4 != 0)
+      reinterpret_cast<uintptr_t>(lse) % 4 != 0 || same_start(out, q) || same_start(out, k) || same_start(out, v))
     return SLIDEDP_ERR_INVALID_ARG;
   AttnParams p = make_params(a, q, k, v, out, lse);
   p.error = ctx->kernel_error;
@@ -188,6 +192,13 @@ int slidedp_attention_backward(slidedp_ctx* ctx, const slidedp_attn_args* a, con
       !workspace)
     return SLIDEDP_ERR_INVALID_ARG;
   if (!aligned16(workspace)) return SLIDEDP_ERR_MISALIGNED;
+  const slidedp_heads *ins[] = {q, k, v, d_out}, *outs[] = {dq, dk, dv};
+  for (int i = 0; i < 3; ++i) {
+    for (const slidedp_heads* in : ins)
+      if (same_start(outs[i], in)) return SLIDEDP_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (same_start(outs[i], outs[j])) return SLIDEDP_ERR_INVALID_ARG;
+  }
   AttnParams p = make_params(a, q, k, v, out, lse);
   p.dout = view(d_out);
   p.dq = view(dq);

@@ -588,7 +588,7 @@ int run_distill(slidedp_ctx* ctx, const slidedp_distill_args* a, int mode, const
   const auto bad = [](const void* q, int64_t align) { return !q || reinterpret_cast<uintptr_t>(q) % (uintptr_t)align != 0; };
   if (bad(logits, elem) || bad(lse, 4) || (a->entries > 0 && (bad(ids, 4) || bad(t, 4)))) return SLIDEDP_ERR_INVALID_ARG;
   if (mode != kBackward && bad(loss, 4)) return SLIDEDP_ERR_INVALID_ARG;
-  if (mode != kForward && (bad(dz, elem) || (a->rows > 1 && a->d_logits_stride < a->vocab))) return SLIDEDP_ERR_INVALID_ARG;
+  if (mode != kForward && (bad(dz, elem) || (a->rows > 1 && (a->d_logits_stride < a->vocab || (dz == logits && a->d_logits_stride != a->logits_stride))))) return SLIDEDP_ERR_INVALID_ARG;
   if (labels && reinterpret_cast<uintptr_t>(labels) % 4 != 0) return SLIDEDP_ERR_INVALID_ARG;
   if (row_grad && reinterpret_cast<uintptr_t>(row_grad) % 4 != 0) return SLIDEDP_ERR_INVALID_ARG;
 

@@ -673,6 +673,10 @@ int plan_qk(const slidedp_qk_args* a, const slidedp_heads* const in[2], const sl
     if (!heads_ok(in[s], elem) || !heads_ok(out[s], elem) || (dy && !heads_ok(dy[s], elem)))
       return SLIDEDP_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(w[s]) % (uintptr_t)elem != 0) return SLIDEDP_ERR_INVALID_ARG;
+    for (const slidedp_heads* over : {in[s], dy ? dy[s] : in[s]})   // in place, but not with other strides
+      if (out[s]->data == over->data && ((a->tokens > 1 && out[s]->stride_token != over->stride_token) ||
+                                         (heads[s] > 1 && out[s]->stride_head != over->stride_head)))
+        return SLIDEDP_ERR_INVALID_ARG;
     p.side[s].x = in[s]->data;
     p.side[s].x_t = in[s]->stride_token;
     p.side[s].x_h = in[s]->stride_head;

@@ -327,3 +327,42 @@ def test_gradients_of_scores_near_the_cap(ctx, D, sign):
     want = ref.attention(q, k, v, scale, ref.visible(T, None, None, True, "cuda"), cap, None, do)
     for n in ("out", "dq", "dk", "dv"):
         assert_close(n, got[n], want[n], tolerance(want[n], BF16, want[n + "_bound"]))
+
+
+def test_outputs_over_inputs_are_refused(ctx, sd):
+    T, H, D = 140, 2, 64
+    q, k, v, do = (randn(gen(i), T, H, D, dtype=BF16) for i in range(4))
+    out, dq, dk, dv = (torch.full_like(q, 3.0) for _ in range(4))
+    lse = torch.empty(H, T, device="cuda")
+    ws = torch.empty(ctx.slidedp_attention_workspace(q, k), dtype=torch.uint8, device="cuda")
+
+    def refused(call, **kw):
+        with pytest.raises(sd.SlideDPError) as e:
+            call(**kw)
+        assert e.value.status == sd.ERR_INVALID_ARG, kw
+    before = [x.clone() for x in (q, k, v, do, out)]
+    args = dict(q=q, k=k, v=v, out=out, lse=lse)
+    for x in (q, k, v):
+        refused(ctx.slidedp_attention, **{**args, "out": x})
+    args.update(d_out=do, dq=dq, dk=dk, dv=dv, workspace=ws)
+    for o in ("dq", "dk", "dv"):
+        for x in (q, k, v, do):
+            refused(ctx.slidedp_attention_backward, **{**args, o: x})
+    for bad in (dict(dk=dq), dict(dv=dk), dict(dv=dq)):
+        refused(ctx.slidedp_attention_backward, **{**args, **bad})
+    # in place with other strides
+    x = torch.full((T * H * D * 2,), 2.0, device="cuda")
+    a, b = x[:T * H * D].view(T, H, D), x.view(T, 2 * H, D)[:, :H]
+    y = torch.empty_like(a)
+    refused(ctx.slidedp_qk_norm_rope, q=a, k=a, w_q=None, w_k=None, cos_sin=None, positions=None, q_out=b, k_out=y)
+    refused(ctx.slidedp_qk_norm_rope_backward, q=y, k=y, w_q=None, w_k=None, cos_sin=None, positions=None, dq_out=a, dk_out=a,
+            dq=y.clone(), dk=b, dw_q=None, dw_k=None, workspace=None)
+    z = x.view(T, -1)
+    ids, t, loss, l2 = torch.zeros(T, 1, dtype=torch.int32, device="cuda"), torch.zeros(T, 1, device="cuda"), torch.empty(T, device="cuda"), torch.empty(2, T, device="cuda")
+    V = z.shape[1] // 2
+    refused(ctx.slidedp_distill_step, logits=z[:, :V], teacher_ids=ids, teacher_logits=t, labels=None, row_grad=None, loss=loss, lse=l2,
+            d_logits=x[:T * V].view(T, V))
+    torch.cuda.synchronize()
+    for now, then in zip((q, k, v, do, out), before):
+        assert torch.equal(now, then)
+    assert torch.all(x == 2.0)
