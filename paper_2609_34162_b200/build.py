@@ -5,6 +5,7 @@ Usage: python -m paper_2609_34162_b200.build [--force] [--verbose]
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 import sys
 import sysconfig
@@ -14,7 +15,6 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libslidedp.so")
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")     # the binding's own part in C++, for this interpreter and torch
-MARSHAL = os.path.join(PKG, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = [os.path.join(CSRC, f) for f in ("common.cu", "context.cu", "update.cu", "stream.cu",
                                            "model.cu", "ipc.cu", "qk_norm_rope.cu", "distill.cu",
                                            "attention.cu", "attention_mma.cu")]
@@ -32,20 +32,28 @@ def nvcc() -> str:
     return "nvcc"
 
 
+def marshal_name() -> str:
+    """The module's name: it is compiled against this torch's headers, and another torch must not load it."""
+    import torch
+    return "_marshal_torch_" + re.sub(r"\W", "_", torch.__version__)
+
+
 def build_marshal(force: bool = False) -> str:
-    if force or not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL) < os.path.getmtime(MARSHAL_SOURCE):
+    name = marshal_name()
+    path = os.path.join(PKG, name + sysconfig.get_config_var("EXT_SUFFIX"))
+    if force or not os.path.exists(path) or os.path.getmtime(path) < os.path.getmtime(MARSHAL_SOURCE):
         import torch
         torch_dir = os.path.dirname(torch.__file__)
-        tmp = MARSHAL + ".tmp.%d" % os.getpid()
+        tmp = path + ".tmp.%d" % os.getpid()
         include = [sysconfig.get_paths()["include"], os.path.join(torch_dir, "include"),
                    os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
                    os.path.join(os.path.dirname(os.path.dirname(nvcc())), "include")]
         subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
-                        f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
+                        f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", f"-DMARSHAL_NAME={name}"]
                        + [f"-I{d}" for d in include] + ["-o", tmp, MARSHAL_SOURCE, "-L" + os.path.join(torch_dir, "lib"),
                        "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"], check=True)
-        os.replace(tmp, MARSHAL)
-    return MARSHAL
+        os.replace(tmp, path)
+    return path
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -1,4 +1,4 @@
-// _marshal: the part of the Python binding that runs several times per argument of every operator call. It looks at
+// _marshal_torch_<version>: the part of the Python binding that runs several times per argument of every operator call. It looks at
 // what the library cannot see of a tensor (type, device, shape, layout) and puts its address and strides where the C ABI
 // wants them. A tensor that is not as it should be goes to the binding's own Python functions, which say what is wrong with
 // it or accept it (subclasses of Tensor). One token through the norm operator, 8 tensors: 10.8 us a call with these checks
@@ -110,6 +110,10 @@ static PyMethodDef methods[] = {{"flat", reinterpret_cast<PyCFunction>(reinterpr
                                 {"current_stream", py_current_stream, METH_NOARGS, NULL},
                                 {"setup", setup, METH_VARARGS, NULL},
                                 {NULL, NULL, 0, NULL}};
-static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
+#define MARSHAL_TEXT2(x) #x
+#define MARSHAL_TEXT(x) MARSHAL_TEXT2(x)
+#define MARSHAL_INIT2(x) PyInit_##x
+#define MARSHAL_INIT(x) MARSHAL_INIT2(x)
+static PyModuleDef module = {PyModuleDef_HEAD_INIT, MARSHAL_TEXT(MARSHAL_NAME), NULL, -1, methods, NULL, NULL, NULL, NULL};
 
-PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC MARSHAL_INIT(MARSHAL_NAME)(void) { return PyModule_Create(&module); }

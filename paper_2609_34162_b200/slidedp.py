@@ -8,11 +8,14 @@ fallback: if the shared library is missing the import of this module fails.
 from __future__ import annotations
 
 import ctypes
+import importlib
 import os
 import struct
 from dataclasses import dataclass
 
 import torch
+
+from .build import marshal_name
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libslidedp.so")
@@ -22,10 +25,11 @@ if not os.path.exists(LIB_PATH):
         f"{LIB_PATH} is missing: build it with `python -m paper_2609_34162_b200.build` "
         "(nvcc, sm_100a). libslidedp has no CPU fallback.")
 
+# The operators of the fine-tuning pass need the binding's C++ module; the paper's path does without it.
 try:
-    from . import _marshal
+    _marshal, _marshal_error = importlib.import_module("." + marshal_name(), __package__), None
 except ImportError as e:
-    raise ImportError("the binding's _marshal module is missing: build it with `python -m paper_2609_34162_b200.build`") from e
+    _marshal, _marshal_error = None, e
 
 _lib = ctypes.CDLL(LIB_PATH)
 
@@ -232,7 +236,7 @@ def _grad_array(grads):
 
 def _stream(stream) -> int:
     if stream is None:
-        return _marshal.current_stream()
+        return torch.cuda.current_stream().cuda_stream if _marshal is None else _marshal.current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -286,8 +290,15 @@ def _matrix(x, what: str, dtype, shape) -> int:
     return t if shape[0] > 1 else shape[1]
 
 
-_marshal.setup(_careful_flat, _careful_heads)
-_flat, _heads, _block = _marshal.flat, _marshal.heads, _marshal.block
+def _no_marshal(*_):
+    raise ImportError("the operators need the binding's C++ module, built for this torch: `python -m paper_2609_34162_b200.build`") from _marshal_error
+
+
+if _marshal is None:
+    _flat = _heads = _block = _no_marshal
+else:
+    _marshal.setup(_careful_flat, _careful_heads)
+    _flat, _heads, _block = _marshal.flat, _marshal.heads, _marshal.block
 
 
 def _workspace(x, nbytes: int) -> int:

@@ -99,3 +99,30 @@ def test_factors_that_fp32_does_not_hold_are_refused(sd):
     ok = dict(tokens=5, heads_q=4, heads_k=2, head_dim=64, rope_dim=64, interleaved=0, dtype=0, table_rows=9, eps=1e-6)
     qk = lambda **kw: lib.slidedp_qk_norm_rope_workspace(ctypes.byref(sd._QkArgs(**{**ok, **kw})))  # noqa: E731
     assert qk(eps=0.0) > 0 and qk(eps=1e-40) > 0 and qk(eps=1e39) == 0 and qk(eps=1e-50) == 0
+
+
+def test_the_paper_path_does_without_the_operators_module():
+    """Without _marshal (not built, or built for another torch) the binding imports; the operators say what is missing."""
+    import os
+    import subprocess
+    import sys
+    code = (
+        "import sys\n"
+        "class Block:\n"
+        "    def find_spec(self, name, path=None, target=None):\n"
+        "        if '_marshal' in name: raise ImportError('blocked ' + name)\n"
+        "sys.meta_path.insert(0, Block())\n"
+        "import paper_2609_34162_b200.slidedp as sd, torch\n"
+        "assert sd.slidedp_state_bytes(1) == 16 and sd._marshal is None\n"
+        "c = sd.Context.__new__(sd.Context); c._h = sd._vp(); c.device = 0\n"
+        "x = torch.zeros(1, 1, 8)\n"
+        "try: c.slidedp_qk_norm_rope(x, x, None, None, None, None, x, x)\n"
+        "except ImportError as e: assert 'paper_2609_34162_b200.build' in str(e) and 'blocked' in str(e.__cause__)\n"
+        "else: raise SystemExit('no ImportError')\n")
+    r = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+
+
+def test_the_operators_module_is_of_this_torch(sd):
+    import re
+    assert sd._marshal.__name__.endswith("._marshal_torch_" + re.sub(r"\W", "_", torch.__version__))
