@@ -8,17 +8,18 @@
 #include <c10/cuda/CUDAStream.h>
 
 static PyObject *careful_flat, *careful_heads; // set by setup()
+static thread_local int device = 0;            // of the call whose argument block was asked for last
 
 typedef struct { // slidedp_heads
   uint64_t data;
   int64_t stride_token, stride_head;
 } heads_view;
 
-// Whether x is a Tensor or Parameter of this dtype and shape (a tuple, or None) on a GPU.
+// Whether x is a Tensor or Parameter of this dtype and shape (a tuple, or None) on the call's GPU.
 static bool plain(PyObject* x, PyObject* dtype, PyObject* shape) {
   if (!THPVariable_CheckExact(x) || !THPDtype_Check(dtype)) return false;
   const at::Tensor& t = THPVariable_Unpack(x);
-  if (t.scalar_type() != reinterpret_cast<THPDtype*>(dtype)->scalar_type || !t.is_cuda()) return false;
+  if (t.scalar_type() != reinterpret_cast<THPDtype*>(dtype)->scalar_type || !t.is_cuda() || t.get_device() != device) return false;
   if (shape == Py_None) return true;
   if (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != t.dim()) return false;
   for (int64_t i = 0; i < t.dim(); ++i) {
@@ -65,14 +66,24 @@ static PyObject* heads(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-// block(): address of this thread's argument block, free for use until its next call
-static PyObject* block(PyObject*, PyObject*) {
+// block(device): address of this thread's argument block, free for use until its next call; tensors are to be on that GPU
+static PyObject* block(PyObject*, PyObject* on) {
   static thread_local uint64_t bytes[64];
+  const long d = PyLong_AsLong(on);
+  if (d == -1 && PyErr_Occurred()) return NULL;
+  device = (int)d;
   return PyLong_FromVoidPtr(bytes);
 }
 
-// current_stream(): the handle of torch's current stream on the current device
-static PyObject* current_stream(PyObject*, PyObject*) { return PyLong_FromVoidPtr(c10::cuda::getCurrentCUDAStream().stream()); }
+// device(): the one given to block
+static PyObject* expected_device(PyObject*, PyObject*) { return PyLong_FromLong(device); }
+
+// current_stream(device): the handle of torch's current stream there; -1: on the current device
+static PyObject* current_stream(PyObject*, PyObject* on) {
+  const long d = PyLong_AsLong(on);
+  if (d == -1 && PyErr_Occurred()) return NULL;
+  return PyLong_FromVoidPtr(c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)d).stream());
+}
 
 // setup(function for flat, function for heads)
 static PyObject* setup(PyObject*, PyObject* args) {
@@ -100,14 +111,15 @@ static PyObject* py_flat(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 static PyObject* py_heads(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   return guarded([&] { return heads(self, args, n); });
 }
-static PyObject* py_current_stream(PyObject* self, PyObject* none) {
-  return guarded([&] { return current_stream(self, none); });
+static PyObject* py_current_stream(PyObject* self, PyObject* on) {
+  return guarded([&] { return current_stream(self, on); });
 }
 
 static PyMethodDef methods[] = {{"flat", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_flat)), METH_FASTCALL, NULL},
                                 {"heads", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_heads)), METH_FASTCALL, NULL},
-                                {"block", block, METH_NOARGS, NULL},
-                                {"current_stream", py_current_stream, METH_NOARGS, NULL},
+                                {"block", block, METH_O, NULL},
+                                {"device", expected_device, METH_NOARGS, NULL},
+                                {"current_stream", py_current_stream, METH_O, NULL},
                                 {"setup", setup, METH_VARARGS, NULL},
                                 {NULL, NULL, 0, NULL}};
 #define MARSHAL_TEXT2(x) #x

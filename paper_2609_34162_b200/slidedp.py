@@ -234,9 +234,10 @@ def _grad_array(grads):
     return (ctypes.c_void_p * len(grads))(*[_ptr(g) for g in grads])
 
 
-def _stream(stream) -> int:
+def _stream(stream, device: int = -1) -> int:
+    """The handle of a stream; None: torch's current one, on `device` (-1: the current device)."""
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream if _marshal is None else _marshal.current_stream()
+        return torch.cuda.current_stream().cuda_stream if _marshal is None else _marshal.current_stream(device)
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -250,6 +251,8 @@ def _refuse(x, what: str, dtype, shape):
         raise TypeError(f"{what} must be a CUDA tensor of {dtype}")
     if shape is not None and tuple(x.shape) != tuple(shape):
         raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(x.shape)}")
+    if x.get_device() != _marshal.device():
+        raise ValueError(f"{what} must be on the context's device cuda:{_marshal.device()}, not {x.device}")
     raise ValueError(f"{what} must be contiguous")
 
 
@@ -264,7 +267,7 @@ def _careful_flat(x, what: str, dtype, shape=None) -> int:
     """Address of a contiguous tensor."""
     x = _as_tensor(x)
     if (not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or not x.is_contiguous()
-            or (shape is not None and x.shape != shape)):
+            or x.get_device() != _marshal.device() or (shape is not None and x.shape != shape)):
         _refuse(x, what, dtype, shape)
     return x.data_ptr()
 
@@ -272,7 +275,8 @@ def _careful_flat(x, what: str, dtype, shape=None) -> int:
 def _careful_heads(x, what: str, dtype, shape):
     """Address and strides of a [tokens, heads, head_dim] tensor whose last axis is contiguous."""
     x = _as_tensor(x)
-    if not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or x.shape != shape:
+    if (not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or x.shape != shape
+            or x.get_device() != _marshal.device()):
         _refuse(x, what, dtype, shape)
     t, h, d = x.stride()
     if d != 1 and shape[2] > 1:
@@ -282,7 +286,8 @@ def _careful_heads(x, what: str, dtype, shape):
 
 def _matrix(x, what: str, dtype, shape) -> int:
     """Row stride of a [rows, columns] tensor whose last axis is contiguous."""
-    if not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or x.shape != shape:
+    if (not isinstance(x, torch.Tensor) or x.dtype is not dtype or not x.is_cuda or x.shape != shape
+            or x.get_device() != _marshal.device()):
         _refuse(x, what, dtype, shape)
     t, c = x.stride()
     if c != 1 and shape[1] > 1:
@@ -302,8 +307,9 @@ else:
 
 
 def _workspace(x, nbytes: int) -> int:
-    if x is None or not x.is_cuda or not x.is_contiguous() or x.numel() * x.element_size() < nbytes:
-        raise ValueError(f"workspace must be a contiguous CUDA tensor of at least {nbytes} bytes")
+    if (x is None or not x.is_cuda or not x.is_contiguous() or x.numel() * x.element_size() < nbytes
+            or x.get_device() != _marshal.device()):
+        raise ValueError(f"workspace must be a contiguous tensor of at least {nbytes} bytes on cuda:{_marshal.device()}")
     return x.data_ptr()
 
 
@@ -529,12 +535,12 @@ class Context:
         """RMS norm of every head of ``q`` and ``k`` ([tokens, heads, head_dim]) and the rotation by
         ``cos_sin`` ([rows, rope_dim]: cosines, then sines; None: no rotation) at ``positions``
         (int32 per token; None: 0, 1, ..)."""
-        (qs, ks), dt, at = _two_sides(q, k), q.dtype, _block()
+        (qs, ks), dt, at = _two_sides(q, k), q.dtype, _block(self.device)
         _heads(at, dt, qs, q, "q", q_out, "q_out")
         _heads(at + 2 * _V, dt, ks, k, "k", k_out, "k_out")
         rc = _lib.slidedp_qk_norm_rope(self._h, self._qk_args(qs, ks, dt, cos_sin, eps, interleaved), at, at + 2 * _V,
                                        *self._qk_tables(qs, dt, w_q, w_k, cos_sin, positions), at + _V, at + 3 * _V,
-                                       _stream(stream))
+                                       _stream(stream, self.device))
         if rc:
             self._check(rc)
 
@@ -546,7 +552,7 @@ class Context:
                                       dw_k, workspace, eps: float = 1e-6, interleaved: bool = False,
                                       stream=None) -> None:
         """Gradients ``dq``, ``dk`` and (float32, may be None) ``dw_q``, ``dw_k`` from those of the outputs."""
-        (qs, ks), dt, at = _two_sides(q, k), q.dtype, _block()
+        (qs, ks), dt, at = _two_sides(q, k), q.dtype, _block(self.device)
         a = self._qk_args(qs, ks, dt, cos_sin, eps, interleaved)
         D, f32, ws = (qs[2],), torch.float32, None
         if dw_q is not None or dw_k is not None:
@@ -557,7 +563,7 @@ class Context:
         rc = _lib.slidedp_qk_norm_rope_backward(
             self._h, a, at, ak, *self._qk_tables(qs, dt, w_q, w_k, cos_sin, positions), at + _V, ak + _V, at + 2 * _V, ak + 2 * _V,
             None if dw_q is None else _flat(dw_q, "dw_q", f32, D), None if dw_k is None else _flat(dw_k, "dw_k", f32, D),
-            ws, _stream(stream))
+            ws, _stream(stream, self.device))
         if rc:
             self._check(rc)
 
@@ -580,12 +586,12 @@ class Context:
         """Attention of ``q`` [tokens, heads_q, head_dim] over ``k``, ``v`` [tokens, heads_kv, head_dim] within
         packed documents (``cu_docs``: int32 offsets; None: one document). Fills ``out`` and ``lse``
         [heads_q, tokens]. ``scale`` defaults to head_dim ** -0.5."""
-        (qs, ks), bf, at = _two_sides(q, k), torch.bfloat16, _block()
+        (qs, ks), bf, at = _two_sides(q, k), torch.bfloat16, _block(self.device)
         a = self._attn_args(qs, ks, cu_docs, prefix, slopes, causal, scale, softcap)
         _heads(at, bf, qs, q, "q", out, "out")
         _heads(at + 2 * _V, bf, ks, k, "k", v, "v")
         rc = _lib.slidedp_attention(self._h, a, at, at + 2 * _V, at + 3 * _V, at + _V, _flat(lse, "lse", torch.float32, (qs[1], qs[0])),
-                                    _stream(stream))
+                                    _stream(stream, self.device))
         if rc:
             self._check(rc)
 
@@ -597,7 +603,7 @@ class Context:
                                    slopes=None, causal: bool = True, scale: float | None = None,
                                    softcap: float = 0.0, stream=None) -> None:
         """Gradients ``dq``, ``dk``, ``dv`` from ``d_out``, with the forward's ``out`` and ``lse``."""
-        (qs, ks), bf, at = _two_sides(q, k), torch.bfloat16, _block()
+        (qs, ks), bf, at = _two_sides(q, k), torch.bfloat16, _block(self.device)
         a = self._attn_args(qs, ks, cu_docs, prefix, slopes, causal, scale, softcap)
         ws = _workspace(workspace, _lib.slidedp_attention_workspace(a))
         _heads(at, bf, qs, q, "q", out, "out", d_out, "d_out", dq, "dq")
@@ -605,17 +611,17 @@ class Context:
         _heads(ak, bf, ks, k, "k", v, "v", dk, "dk", dv, "dv")
         rc = _lib.slidedp_attention_backward(
             self._h, a, at, ak, ak + _V, at + _V, _flat(lse, "lse", torch.float32, (qs[1], qs[0])), at + 2 * _V, at + 3 * _V,
-            ak + 2 * _V, ak + 3 * _V, ws, _stream(stream))
+            ak + 2 * _V, ak + 3 * _V, ws, _stream(stream, self.device))
         if rc:
             self._check(rc)
 
-    @staticmethod
-    def _distill_call(logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits, temperature, w_teacher,
+    def _distill_call(self, logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits, temperature, w_teacher,
                       w_label):
         """The arguments that the three calls share: slidedp_distill_args and the addresses of the inputs, of
         lse and of the row gradients."""
         if logits.dtype not in _DTYPES or logits.dim() != 2:
             raise TypeError("logits must be [rows, vocab] of bfloat16 or float32")
+        _block(self.device)
         dt, shape, f32, i32 = logits.dtype, logits.shape, torch.float32, torch.int32
         rows, vocab = shape
         entries = teacher_ids.shape[-1]
@@ -632,7 +638,7 @@ class Context:
         stored entries (int32 ids, float32 logits, both [rows, entries]) and int32 ``labels`` (may be None)."""
         a, ins, l, _ = self._distill_call(logits, teacher_ids, teacher_logits, labels, lse, None, None, temperature,
                                           w_teacher, w_label)
-        rc = _lib.slidedp_distill_loss(self._h, a, *ins, _flat(loss, "loss", torch.float32, logits.shape[:1]), l, _stream(stream))
+        rc = _lib.slidedp_distill_loss(self._h, a, *ins, _flat(loss, "loss", torch.float32, logits.shape[:1]), l, _stream(stream, self.device))
         if rc:
             self._check(rc)
 
@@ -643,7 +649,7 @@ class Context:
         ``lse``. ``d_logits`` may be ``logits``."""
         a, ins, l, g = self._distill_call(logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits,
                                           temperature, w_teacher, w_label)
-        self._check(_lib.slidedp_distill_loss_backward(self._h, a, *ins, l, g, d_logits.data_ptr(), _stream(stream)))
+        self._check(_lib.slidedp_distill_loss_backward(self._h, a, *ins, l, g, d_logits.data_ptr(), _stream(stream, self.device)))
 
     def slidedp_distill_step(self, logits, teacher_ids, teacher_logits, labels, row_grad, loss, lse, d_logits,
                              temperature: float = 1.0, w_teacher: float = 1.0, w_label: float = 0.0,
@@ -652,7 +658,7 @@ class Context:
         a, ins, l, g = self._distill_call(logits, teacher_ids, teacher_logits, labels, lse, row_grad, d_logits,
                                           temperature, w_teacher, w_label)
         self._check(_lib.slidedp_distill_step(self._h, a, *ins, g, _flat(loss, "loss", torch.float32, logits.shape[:1]), l,
-                                              d_logits.data_ptr(), _stream(stream)))
+                                              d_logits.data_ptr(), _stream(stream, self.device)))
 
 
 def slidedp_model_stream_step(n_total: int, R: int, chunk_elems: int, nbuf: int, h2d_gbs: float,

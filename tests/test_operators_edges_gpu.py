@@ -366,3 +366,39 @@ def test_outputs_over_inputs_are_refused(ctx, sd):
     for now, then in zip((q, k, v, do, out), before):
         assert torch.equal(now, then)
     assert torch.all(x == 2.0)
+
+
+def test_tensors_of_another_gpu_are_refused(sd):
+    """The library would hand their addresses to kernels on the context's GPU. With one GPU at hand it is the context that is
+    told another number; the checks come before the library, which still has the first."""
+    T, H, D = 20, 2, 64
+    q = randn(gen(7), T, H, D, dtype=BF16)
+    a, b, lse = torch.full_like(q, 3.0), torch.full_like(q, 3.0), torch.full((H, T), 3.0, device="cuda")
+    z, ids, t = randn(gen(3), 3, 500), torch.zeros(3, 2, dtype=torch.int32, device="cuda"), randn(gen(4), 3, 2)
+    loss, l2, dz = torch.full((3,), 3.0, device="cuda"), torch.full((2, 3), 3.0, device="cuda"), torch.full_like(z, 3.0)
+    with sd.slidedp_create(0, 0) as ctx:
+        ws = torch.empty(max(ctx.slidedp_attention_workspace(q, q), ctx.slidedp_qk_norm_rope_workspace(q, q)), dtype=torch.uint8, device="cuda")
+        before = ctx.slidedp_kernel_launches()
+        ctx.device = 1
+        for call in (lambda: ctx.slidedp_attention(q, q, q, a, lse),
+                     lambda: ctx.slidedp_attention_backward(q, q, q, q, lse, q, a, b, b, ws),
+                     lambda: ctx.slidedp_qk_norm_rope(q, q, None, None, None, None, a, b),
+                     lambda: ctx.slidedp_qk_norm_rope_backward(q, q, None, None, None, None, q, q, a, b, None, None, None),
+                     lambda: ctx.slidedp_distill_loss(z, ids, t, None, loss, l2),
+                     lambda: ctx.slidedp_distill_loss_backward(z, ids, t, None, l2, None, dz),
+                     lambda: ctx.slidedp_distill_step(z, ids, t, None, None, loss, l2, dz)):
+            with pytest.raises(ValueError, match="cuda:1"):
+                call()
+        assert ctx.slidedp_kernel_launches() == before
+        ctx.device = 0
+        ctx.slidedp_attention(q, q, q, a, lse)
+    torch.cuda.synchronize()
+    for x in (b, loss, l2, dz):
+        assert torch.all(x == 3.0)
+
+
+def test_the_default_stream_is_torchs_current_one_on_the_contexts_device(ctx, sd):
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        assert sd._stream(None, ctx.device) == side.cuda_stream == sd._stream(None)
+    assert sd._stream(None, ctx.device) == torch.cuda.current_stream().cuda_stream
