@@ -126,3 +126,25 @@ def test_the_paper_path_does_without_the_operators_module():
 def test_the_operators_module_is_of_this_torch(sd):
     import re
     assert sd._marshal.__name__.endswith("._marshal_torch_" + re.sub(r"\W", "_", torch.__version__))
+
+
+def test_the_headers_are_c(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "use.c"
+    src.write_text('#include "slidedp_ops.h"\n'
+                   "int main(void) {\n"
+                   "  slidedp_heads h = {0, 0, 0};\n"
+                   "  slidedp_qk_args q = {0, 1, 1, 8, 0, 0, SLIDEDP_F32, 0, 0.0};\n"
+                   "  slidedp_attn_args a = {0, 1, 1, 8, 1, 1, 0, 0, 0, 0, 1.0, 0.0};\n"
+                   "  slidedp_distill_args d = {0, 1, 0, SLIDEDP_BF16, 1, 1, 1.0, 1.0, 0.0};\n"
+                   "  return slidedp_qk_norm_rope(0, &q, &h, &h, 0, 0, 0, 0, &h, &h, 0) != SLIDEDP_ERR_INVALID_ARG ||\n"
+                   "         slidedp_attention(0, &a, &h, &h, &h, &h, 0, 0) != SLIDEDP_ERR_INVALID_ARG ||\n"
+                   "         slidedp_distill_loss(0, &d, 0, 0, 0, 0, 0, 0, 0) != SLIDEDP_ERR_INVALID_ARG ||\n"
+                   "         slidedp_qk_norm_rope_workspace(&q) == 0 || slidedp_attention_workspace(&a) != 0;\n}\n")
+    pkg = os.path.join(root, "paper_2609_34162_b200")
+    exe = tmp_path / "use"
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Wextra", "-pedantic", "-Werror", "-I", os.path.join(root, "include"), str(src), "-o", str(exe),
+                    "-L", pkg, "-lslidedp", f"-Wl,-rpath,{pkg}"], check=True)
+    subprocess.run([str(exe)], check=True)
