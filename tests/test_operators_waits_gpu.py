@@ -161,3 +161,20 @@ def test_threads_on_a_context_count_and_fail_exactly(sd):
             assert ctx.slidedp_kernel_launches() - before == threads * calls - len(failed)
     finally:
         ctx.slidedp_destroy()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_distilled_rows_whose_sums_did_not_come_are_nan(ctx, sd, dtype):
+    """Not something that could pass for a result."""
+    rows, vocab = 3, 40000       # cut over a cluster
+    z, ids, t, labels, gr = distill_inputs(rows, vocab, 12, dtype, seed=6)
+    loss, lse, dz = torch.zeros(rows, device="cuda"), torch.zeros(2, rows, device="cuda"), torch.zeros_like(z)
+    for two in (0.0, 0.3):
+        ctx.slidedp_test_wait_polls(0)
+        ctx.slidedp_distill_step(z, ids, t, labels, None, loss, lse, dz, temperature=1.5, w_teacher=0.7, w_label=two)
+        torch.cuda.synchronize()
+        ctx.slidedp_test_wait_polls(-1)
+        has = ((ids >= 0) & (ids < vocab)).any(1) | ((labels >= 0) & (labels < vocab) if two else False)
+        assert has.any() and loss[has].isnan().all() and lse[0].isnan().all() and dz[has].isnan().all()
+        with pytest.raises(sd.SlideDPError):
+            ctx.slidedp_distill_loss(z, ids, t, labels, loss, lse)
