@@ -11,8 +11,8 @@
  * Calls of this header on one context may go to different streams and come from different threads, also at once (but not
  * beside other calls on that context); workspaces must not be shared by calls that can overlap.
  *
- * The attention and distillation kernels wait on copies and on blocks of their own launch; every
- * such wait is bounded. If one runs out, the results of that call are not complete, and the first of these calls on the
+ * The attention and distillation kernels wait on copies and on blocks of their own launch; every such wait is bounded (about
+ * a minute). If one runs out, the results of that call are not complete, and the first of these calls on the
  * context to start after that returns SLIDEDP_ERR_TIMEOUT, once, and does nothing else: any operator of this header; a
  * slidedp_grad_norm_finish or slidedp_grad_norm_finish_from that fetches its results (they are fetched all the same); or
  * slidedp_destroy (which still destroys). A call's own kernels have only been queued when it returns: to know that a step's
@@ -20,7 +20,7 @@
  *
  * BF16 and FP32 tensors need the alignment of their element only; 16-byte aligned bases and
  * strides are faster. All sums, norms and softmax statistics are FP32 and each output is rounded
- * once. Sizes of zero are no-ops. Factors given as doubles (scale, softcap, temperature, weights, eps) are used as FP32:
+ * once (attention multiplies some intermediates as BF16: see there). Sizes of zero are no-ops. Factors given as doubles (scale, softcap, temperature, weights, eps) are used as FP32:
  * ones that FP32 makes infinite, or makes zero where they must be positive, are refused.
  */
 #ifndef SLIDEDP_OPS_H
@@ -97,6 +97,19 @@ SLIDEDP_API size_t slidedp_qk_norm_rope_workspace(const slidedp_qk_args* args);
  * every document sees nothing: out = 0, lse = -inf, and its gradients are 0. Offsets are
  * clamped to [0, tokens]; results for descending ones are undefined but nothing is accessed
  * outside the tensors. head_dim 1..256.
+ *
+ * What a query does not see does not touch its results, whatever it holds: NaN and infinities in other documents, in later
+ * keys, in padding. What it sees and is NaN makes its out and lse NaN.
+ *
+ * With head_dim a multiple of 8 up to 128 and 16-byte aligned views the products run on the tensor cores, with BF16 operands:
+ * the probabilities exp(s - max) for out and those of the backward pass for dv, and the gradients of the scores for dq and dk, are
+ * rounded to BF16 (each by at most 2^-8 of itself); their sums, the scores, lse, maxima and accumulators are FP32. The backward
+ * pass takes the rows' sums of out * d_out from the BF16 `out`. Against arithmetic in 64 bits, with the output's own rounding
+ * (0.0017 in the 2-norm), out is off by 0.0020 and the gradients by 0.0024 to 0.0027. A quarter of the forward pass's exponentials
+ * are a polynomial (relative error 3e-6). With softcap, tanh is a polynomial where all scores of 32 neighbouring rows and a tile of
+ * keys, masked ones included, are below 0.7 of the cap, and made of an exponential elsewhere: both are accurate to FP32's 2^-23,
+ * but the last bits of a row may depend on which it was. Other views and head sizes compute in FP32 throughout, one warp per
+ * row (2048 tokens, 8 heads of 256: 4.2 ms forward, 12.4 ms backward; of 128 on the tensor cores 33 and 41 us).
  *
  * Backward: the gradients of q, k and v from d_out (the gradient of out), with the forward's out
  * and lse. The slopes are constants and have none. workspace: device,

@@ -1314,7 +1314,9 @@ static cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>* done, 
 // Blocks that share a tile of keys, by query heads: two below two tiles per SM, four where all of those then
 // take a quarter of the SMs (a tile's columns can be cut no finer than into 64). Backward pass in us, by 1 / 2 / 4 blocks: 6
 // tiles - / 28 / 24, 64 (1024 tokens, causal) - / 45 / 60, 160 (2500) 220 / 194 / -, 256 (4096) 454 / 465 / -, not causal
-// 564 / 585 / -, 264 (4099 in seven documents, capped) 311 / 243 / -, 512 (8192) 191 / 224 / - for the keys alone.
+// 564 / 585 / -, 264 (4099 in seven documents, capped) 311 / 243 / -, 512 (8192) 191 / 224 / - for the keys alone. What decides
+// between one and two near 256 tiles is how uneven the tiles' walks are, which the host does not know (the offsets are on the
+// device): the rule gives 2 to 4 % to even walks in order not to lose 22 % to uneven ones.
 static int key_split(int64_t tiles, int group, int halves) {
   int n = 1;
   while (n < 2 * halves && n * 2 <= group && tiles * n < (n == 1 ? 2 * kSMs : kSMs / 4)) n *= 2;

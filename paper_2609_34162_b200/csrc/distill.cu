@@ -5,8 +5,10 @@
 //   dz = g (w_t tau (p - q) + w_l (p1 - onehot)),   p1 the softmax at temperature 1.
 // Bound: HBM. The logits are all that is large: forward reads them once, backward reads them and writes the
 // gradient. The step (both) reads a row twice in one kernel, the second time from L2, so that it moves what
-// backward alone does. Measured on 4096 x 131072 BF16 logits: 465 us, 4.6 TB/s of one read and one write, 14
-// instructions and two exponentials per logit. Keeping the row on chip instead, in the shared memory or the
+// backward alone does. Measured on 4096 x 131072 BF16 logits: 445 us, 4.8 TB/s of one read and one write, 14
+// instructions and two exponentials per logit. No unit is saturated there (issue 60 %, special functions 52 %, DRAM 51 % of the
+// time): the warps wait for loads and for each other, as a block has no loads under way while its row starts and while the row's
+// sums are exchanged. Keeping the row on chip instead, in the shared memory or the
 // registers of a cluster of eight blocks, measured 481 to 860 us: the exchange of a row's sums costs each of the
 // eight what 5000 of its own logits do, and too few rows fit to cover that.
 #include "ops_internal.h"
@@ -566,7 +568,7 @@ int check_distill(const slidedp_distill_args* a) {
 
 // Blocks per row: one when the rows fill the device; when they do not, a row is cut, down to 8 KB. A step also cuts
 // rows so that those being worked on (three blocks per SM) stay in L2 for their second reading: 4096 rows of
-// 131072 BF16 logits, in 1 / 2 / 4 blocks each, 493 / 465 / 511 us.
+// 131072 BF16 logits, in 1 / 2 / 4 blocks each, 493 / 465 / 511 us (two blocks now 445).
 constexpr int64_t kMinSliceBytes = 8 * 1024;
 constexpr int64_t kEnoughBlocks = 148 * 4;
 constexpr int64_t kWorkedOn = 148 * 3;
