@@ -253,7 +253,7 @@ __device__ __forceinline__ void nan_columns(const AttnView& v, int t, int h, int
 }
 __device__ __forceinline__ uint32_t any_left(const uint32_t* words) { return (words[0] | words[1]) | (words[2] | words[3]); }
 
-// Outputs whose scores gave a sum above zero: a NaN in a column comes from a value that is not finite in that column of v.
+// Outputs whose scores gave a sum above zero: they are NaN in the columns where a value that they see is.
 static __device__ __noinline__ uint32_t spoiled_out_rows(const AttnParams& p, uint32_t redo, int row0, int h, int lo, int hi) {
   const int hk = h / p.group;
   uint32_t left[kWords] = {};
@@ -269,53 +269,63 @@ static __device__ __noinline__ uint32_t spoiled_out_rows(const AttnParams& p, ui
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int w = 0; w < kWords; ++w) bad |= finite(x[u][w]) ? 0u : 1u << u;
+      for (int w = 0; w < kWords; ++w) bad |= x[u][w] == x[u][w] ? 0u : 1u << u;
     bad = __reduce_or_sync(0xffffffffu, bad);
     if (!bad) continue;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int w = 0; w < kWords; ++w) {
-        const uint32_t columns = __ballot_sync(0xffffffffu, !finite(x[u][w]));
+        const uint32_t columns = __ballot_sync(0xffffffffu, x[u][w] != x[u][w]);
         if (min(j + u, to - 1) >= lo && min(j + u, to - 1) < hi) left[w] &= ~columns;
       }
   }
   return __ballot_sync(0xffffffffu, any_left(left) != 0);
 }
 
-// Gradients of keys (or, of_v, of values): a visible query whose lse is not finite makes the whole row of both NaN (its
-// scores hold NaN), one whose delta is not finite the whole row of dk (dP - delta); in a column of dv it takes a value that is
-// not finite in that column of dout, which also shows in delta. A value that is not finite in the key's own k or v shows in
-// the statistics of every query that sees it.
+// Gradients of keys (or, of_v, of values). A visible query whose lse is not finite makes the whole row of both NaN, as its
+// scores hold NaN. One with a NaN in dout has it in its delta, which makes the whole row of dk NaN, and in a column of dv. One whose
+// delta is infinite adds infinities of the sign of -delta q to dk: NaN in the columns where two differ. What is not finite in
+// the key's own k or v shows in the statistics of every query that sees it.
 static __device__ __noinline__ uint32_t spoiled_key_rows(const AttnParams& p, uint32_t redo, int row0, int hk, int lo, int hi, bool of_v,
                                                          int from, int to) {
   const int lane = threadIdx.x % kLanes;
-  uint32_t left[kWords] = {redo >> lane & 1};
-  if (of_v)
-    for (uint32_t r = redo; r; r &= r - 1) nan_columns(p.dv, row0 + __ffs(r) - 1, hk, __ffs(r) - 1, from, to, left);
+  uint32_t left[kWords] = {}, up[kWords] = {}, down[kWords] = {};
+  for (uint32_t r = redo; r; r &= r - 1) nan_columns(of_v ? p.dv : p.dk, row0 + __ffs(r) - 1, hk, __ffs(r) - 1, from, to, left);
   if (!any_left(left)) lo = hi = 0;
   const int first = __reduce_min_sync(0xffffffffu, lo < hi ? lo : p.tokens) & ~(kLanes * 4 - 1), last = __reduce_max_sync(0xffffffffu, hi);
   for (int h = hk * p.group; h < (hk + 1) * p.group; ++h)
     for (int i0 = first; i0 < last && __any_sync(0xffffffffu, any_left(left)); i0 += kLanes * 4) {   // the pitch is a multiple of 128
-      const float4 l = *reinterpret_cast<const float4*>(p.row_lse + h * p.pitch + i0 + lane * 4);
-      const float4 d = *reinterpret_cast<const float4*>(p.row_delta + h * p.pitch + i0 + lane * 4);
-      const float ls[4] = {l.x, l.y, l.z, l.w}, ds[4] = {d.x, d.y, d.z, d.w};
+      const float4 l4 = *reinterpret_cast<const float4*>(p.row_lse + h * p.pitch + i0 + lane * 4);
+      const float4 d4 = *reinterpret_cast<const float4*>(p.row_delta + h * p.pitch + i0 + lane * 4);
+      const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, ds[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t bad_l = __ballot_sync(0xffffffffu, !finite(ls[e])), bad_d = __ballot_sync(0xffffffffu, !finite(ds[e]));
-        for (uint32_t rest = bad_l | bad_d; rest && __any_sync(0xffffffffu, any_left(left)); rest &= rest - 1) {
+        const uint32_t nans = __ballot_sync(0xffffffffu, !finite(ls[e]) || (!of_v && ds[e] != ds[e]));   // of the whole row
+        const uint32_t some = __ballot_sync(0xffffffffu, !finite(ds[e]));
+        for (uint32_t rest = nans | some; rest && __any_sync(0xffffffffu, any_left(left)); rest &= rest - 1) {
           const int at = __ffs(rest) - 1, i = i0 + at * 4 + e;
           const bool seen = i >= lo && i < hi;
           if (!__any_sync(0xffffffffu, seen)) continue;
-          if (!of_v || bad_l >> at & 1) {
+          if (nans >> at & 1) {
             if (seen) left[0] = left[1] = left[2] = left[3] = 0;
-          } else {
-            float x[kMaxPer];
-            load_row(p.dout, i, h, p.head_dim, x);
+            continue;
+          }
+          float x[kMaxPer];
+          load_row(of_v ? p.dout : p.q, i, h, p.head_dim, x);
+          const float sign = __shfl_sync(0xffffffffu, ds[e], at);
 #pragma unroll
-            for (int w = 0; w < kWords; ++w) {
-              const uint32_t columns = __ballot_sync(0xffffffffu, !finite(x[w]));
+          for (int w = 0; w < kWords; ++w) {
+            if (of_v) {
+              const uint32_t columns = __ballot_sync(0xffffffffu, x[w] != x[w]);
               if (seen) left[w] &= ~columns;
+            } else {   // zero times infinity counts as both
+              const uint32_t plus = __ballot_sync(0xffffffffu, !(x[w] * sign < 0.0f)), minus = __ballot_sync(0xffffffffu, !(x[w] * sign > 0.0f));
+              if (seen) {
+                up[w] |= plus;
+                down[w] |= minus;
+                left[w] &= ~(up[w] & down[w]);
+              }
             }
           }
         }

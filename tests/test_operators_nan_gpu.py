@@ -1,6 +1,7 @@
 """NaN and infinities in what a row of attention sees and in what it does not see: the first must show, the second must not,
 and neither may cost more than a multiple of an ordinary pass."""
 import math
+import random
 
 import pytest
 import torch
@@ -146,3 +147,59 @@ def test_one_nan_in_a_long_document(ctx, Hq, Hk, D, where):
     # rows whose NaN is their own are left as they are; redoing them cost over a thousand times an ordinary pass
     assert nan_f < 10 * clean_f + 1.0
     assert nan_b < (10 if where in ("k", "v", "token") else 1000) * clean_b + 1.0
+
+
+def apart(x):
+    """The same values one element off alignment, where one warp walks the pairs that it sees and nothing else."""
+    y = torch.empty(x.numel() + 1, dtype=x.dtype, device="cuda")[1:].view(x.shape)
+    return y.copy_(x)
+
+
+@pytest.mark.parametrize("seed", range(80))
+def test_nan_and_infinities_are_where_the_visible_pairs_put_them(ctx, seed):
+    """Random documents with NaN and infinities strewn in: which results are NaN, infinite or finite, as in the general kernels,
+    and the finite ones as the definition has them without the strewn values (no row that is finite sees any)."""
+    r = random.Random(seed)
+    T, Hk, G, D = r.choice([1, 5, 130, 257, 300, 500, 700]), r.choice([1, 2, 3]), r.choice([1, 2, 4]), r.choice([8, 40, 64, 96, 128])
+    docs = r.randint(0, 6)
+    cu = sorted(r.randint(0, T) for _ in range(docs + 1)) if r.random() < 0.8 else None
+    prefix = [r.randint(-2, T // 2) for _ in range(docs)] if cu is not None and docs and r.random() < 0.4 else None
+    tens = lambda x: None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    kw = dict(causal=r.random() < 0.7, softcap=r.choice([0.0, 0.0, 5.0]), scale=r.choice([None, None, 0.3, -0.1]), cu_docs=tens(cu),
+              prefix=tens(prefix))
+    if r.random() < 0.3:
+        kw["slopes"] = 2.0 ** -torch.arange(1, Hk * G + 1, device="cuda").float()
+    clean = inputs(T, Hk * G, Hk, D, seed)
+    ins = [x.clone() for x in clean]
+    for _ in range(r.choice([1, 1, 2, 6])):
+        x, value, t, part = r.choice(ins), r.choice([math.nan, math.nan, math.inf, -math.inf]), r.randrange(T), r.random()
+        h = r.randrange(x.shape[1])
+        if part < 0.5:
+            x[t, h, r.randrange(D)] = value
+        elif part < 0.8:
+            x[t, h] = value
+        else:
+            x[t] = value
+
+    def both(ins, place):
+        q, k, v, do = map(place, ins)
+        out, lse = place(torch.zeros_like(q)), torch.empty(q.shape[1], T, device="cuda")
+        res = dict(out=out, dq=place(torch.zeros_like(q)), dk=place(torch.zeros_like(k)), dv=place(torch.zeros_like(v)))
+        ws = torch.empty(ctx.slidedp_attention_workspace(q, k), dtype=torch.uint8, device="cuda")
+        ctx.slidedp_attention(q, k, v, out, lse, **kw)
+        ctx.slidedp_attention_backward(q, k, v, out, lse, do, res["dq"], res["dk"], res["dv"], ws, **kw)
+        return {**res, "lse": lse.T}
+    got, general = both(ins, lambda x: x), both(ins, apart)
+    scale = D ** -0.5 if kw["scale"] is None else kw["scale"]
+    want = ref.attention(*clean[:3], scale, ref.visible(T, cu, prefix, kw["causal"], "cuda"), kw["softcap"], kw.get("slopes"), clean[3])
+    for n, x in got.items():
+        y = general[n]
+        assert torch.equal(x.isnan(), y.isnan()), f"{n}: NaN"
+        assert torch.equal(x.isinf(), y.isinf()) and torch.equal(x[x.isinf()], y[x.isinf()]), f"{n}: infinities"
+        if n != "lse":
+            tol = tolerance(want[n], BF16, want[n + "_bound"])
+            # a score of -inf takes its key out of a row, a score gradient of a row that is NaN its query out of a sum: only rows
+            # and keys of heads without any strewn value are as in the clean definition
+            if not any((~a.isfinite()).any() for a in ins[:3]):
+                keep = x.isfinite()
+                assert_close(n, x[keep], want[n][keep], tol[keep])
