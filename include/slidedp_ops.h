@@ -20,8 +20,9 @@
  *
  * BF16 and FP32 tensors need the alignment of their element only; 16-byte aligned bases and
  * strides are faster. All sums, norms and softmax statistics are FP32 and each output is rounded
- * once (attention multiplies some intermediates as BF16: see there). Sizes of zero are no-ops. Factors given as doubles (scale, softcap, temperature, weights, eps) are used as FP32:
- * ones that FP32 makes infinite, or makes zero where they must be positive, are refused.
+ * once (attention multiplies some intermediates as BF16: see there). Sizes of zero are no-ops. Factors given as doubles
+ * (scale, softcap, temperature, weights, eps) are used as FP32: ones that FP32 makes infinite, or makes zero where they must
+ * be positive, are refused.
  */
 #ifndef SLIDEDP_OPS_H
 #define SLIDEDP_OPS_H
@@ -59,7 +60,8 @@ typedef struct {
  * Backward: dq, dk are the gradients of q and k, dw_q and dw_k (device, head_dim floats each,
  * nullable) those of the weights, from the gradients dq_out, dk_out of the outputs. The forward's
  * inputs are needed, its outputs are not. y may be x and dq may be dq_out (same address and
- * strides; the same address with other strides is refused), but outputs may not overlap otherwise. workspace: device, slidedp_qk_norm_rope_workspace bytes, 16-byte aligned.
+ * strides; the same address with other strides is refused), but outputs may not overlap otherwise.
+ * workspace: device, slidedp_qk_norm_rope_workspace bytes, 16-byte aligned.
  */
 typedef struct {
   int64_t tokens;
