@@ -1,9 +1,10 @@
 /*
  * slidedp_ops.h -- operators of the fine-tuning pass that produces the gradients of slidedp.h:
- * the query / key norms with the position rotation, attention over packed documents, and
- * distillation from a teacher's top logits, each with its gradient. (Not part of the paper, whose
- * Sec. 3.1 takes the layers' forward and backward pass as given; its workloads, Sec. 4.1, are the
- * decoder layers these operators belong to.)
+ * the token embedding, the norms around a block with its gate and residual, the query / key norms
+ * with the position rotation, attention over packed documents, distillation from a teacher's top
+ * logits and the clipped policy loss, each with its gradient, and clipping by the norm over many
+ * gradient tensors. (Not part of the paper, whose Sec. 3.1 takes the layers' forward and backward
+ * pass as given; its workloads, Sec. 4.1, are the decoder layers these operators belong to.)
  *
  * Conventions are those of slidedp.h: every call returns SLIDEDP_OK or a negative status and only
  * enqueues work on cuda_stream; the caller owns every buffer, workspaces included; nothing is kept
@@ -183,6 +184,140 @@ SLIDEDP_API int slidedp_distill_step(slidedp_ctx* ctx, const slidedp_distill_arg
                          const int32_t* teacher_ids, const float* teacher_logits, const int32_t* labels,
                          const float* row_grad, float* loss, float* lse, void* d_logits,
                          void* cuda_stream);
+
+/* ---- token embedding -------------------------------------------------------------------------
+ *
+ * A device matrix whose last axis is contiguous: element (r, c) is data[r * stride + c], the stride in
+ * elements and not negative. Rows of an output do not overlap. */
+typedef struct {
+  void* data;
+  int64_t stride;
+} slidedp_rows;
+
+/*   out[t] = scale * table[ids[t]]                          table: [vocab, hidden], out: [tokens, hidden] of `dtype`
+ *   d_table[v] = scale * sum of d_out[t] over the t with ids[t] = v     d_out of `dtype`, d_table of `grad_dtype`
+ * ids: device, one int32 per token. A token whose id lies outside [0, vocab) is absent (padding): its row of out is zeros,
+ * its row of d_out is not read. accumulate = 0 writes all of d_table, zeros for ids that no token has; 1 adds to what
+ * d_table holds, and touches only the rows of ids that occur. The sum over a row's tokens is FP32 in an order that depends on
+ * the ids alone, scaled and (with what was there) rounded once. d_table may not overlap d_out, nor out the table.
+ * tokens and vocab up to 2^30, hidden up to 2^20.
+ * workspace: device, slidedp_embedding_workspace bytes, 16-byte aligned.
+ */
+typedef struct {
+  int64_t tokens, vocab, hidden;
+  int32_t dtype, grad_dtype; /* slidedp_dtype */
+  int32_t accumulate;
+  int32_t reserved;
+  double scale;
+} slidedp_embedding_args;
+
+SLIDEDP_API int slidedp_embedding(slidedp_ctx* ctx, const slidedp_embedding_args* args, const slidedp_rows* table, const int32_t* ids,
+                      const slidedp_rows* out, void* cuda_stream);
+SLIDEDP_API int slidedp_embedding_backward(slidedp_ctx* ctx, const slidedp_embedding_args* args, const int32_t* ids,
+                               const slidedp_rows* d_out, const slidedp_rows* d_table, void* workspace, void* cuda_stream);
+/* 0 for arguments that the call would refuse. */
+SLIDEDP_API size_t slidedp_embedding_workspace(const slidedp_embedding_args* args);
+
+/* ---- the norms around a block, its gate and its residual ---------------------------------------
+ *
+ * For each token, with x the residual stream, y the block's output (attention or feed-forward), rms(v) =
+ * v * rsqrt(mean(v^2) + eps):
+ *   n = post_norm ? rms(y) * w_post : y
+ *   x' = x + residual_scale * g * n             g = gate, sigmoid(gate) with gate_sigmoid = 1, or 1 without a gate
+ *   h = rms(x') * w_pre                          the next block's input, if pre_norm
+ * All are [tokens, hidden] of `dtype` (BF16 or FP32), w_post and w_pre (nullable: ones) hidden values of it. gate: none
+ * (gate_kind 0), hidden values for all tokens (1), or [tokens, hidden] (2). h is taken from the FP32 x', not from the rounded
+ * one. has_y = 0: there is no block before (x' = x is not written, h alone is; post_norm and gate_kind are then 0 and
+ * pre_norm is 1). hidden 1..16384; tokens up to 2^30.
+ *
+ * Backward: from the gradients dx_out of x' (NULL: zeros) and dh of h, the gradients dx, dy, dgate (2: [tokens, hidden] of
+ * `dtype`; 1: hidden floats), dw_post and dw_pre (hidden floats each); dgate, dw_post and dw_pre may be NULL. The forward's
+ * inputs are needed, its outputs are not.
+ *
+ * An output may be an input of the same form (same address and stride: x' = x, dx = dx_out, dy = y, ..): each row is read
+ * before it is written. The same address with another stride is refused, as are two outputs at one address; outputs may not
+ * overlap otherwise. workspace: device, slidedp_block_norm_workspace bytes, 16-byte aligned; needed where dw_post, dw_pre or
+ * the dgate of a gate for all tokens is wanted.
+ */
+typedef struct {
+  int64_t tokens, hidden;
+  int32_t dtype; /* slidedp_dtype */
+  int32_t has_y, post_norm, pre_norm;
+  int32_t gate_kind, gate_sigmoid;
+  double residual_scale, eps;
+} slidedp_block_norm_args;
+
+SLIDEDP_API int slidedp_block_norm(slidedp_ctx* ctx, const slidedp_block_norm_args* args, const slidedp_rows* x, const slidedp_rows* y,
+                       const void* w_post, const slidedp_rows* gate, const void* w_pre, const slidedp_rows* x_out,
+                       const slidedp_rows* h_out, void* cuda_stream);
+SLIDEDP_API int slidedp_block_norm_backward(slidedp_ctx* ctx, const slidedp_block_norm_args* args, const slidedp_rows* x,
+                                const slidedp_rows* y, const void* w_post, const slidedp_rows* gate, const void* w_pre,
+                                const slidedp_rows* dx_out, const slidedp_rows* dh_out, const slidedp_rows* dx,
+                                const slidedp_rows* dy, const slidedp_rows* dgate, float* dw_post, float* dw_pre,
+                                void* workspace, void* cuda_stream);
+/* 0 for arguments that the call would refuse. */
+SLIDEDP_API size_t slidedp_block_norm_workspace(const slidedp_block_norm_args* args);
+
+/* ---- clipped policy loss ------------------------------------------------------------------------
+ *
+ * For each row (a sampled token) with the policy's logits z[0..vocab), the token y = labels[row], the log-probability
+ * that it was sampled with (old_logp), a reference model's (ref_logp) and its advantage A:
+ *   logp = log softmax(z / temperature)[y],  ratio = exp(logp - old_logp),  k = ref_logp - logp
+ *   loss = -min(ratio A, clamp(ratio, 1 - clip_low, 1 + clip_high) A) + kl_weight (exp(k) - k - 1)
+ * A row whose label lies outside [0, vocab) is absent (prompt, padding): its loss, logp and gradient are 0 and its logits are
+ * not read. old_logp NULL: logp itself (the first step on fresh samples: ratio 1, with its gradient). ref_logp NULL: no
+ * second term. advantage NULL: no first term; a row with A = 0 has none either, whatever its ratio. So with all three NULL the
+ * call computes log-probabilities (loss may then be NULL too). logits: [rows, vocab] of `dtype`, logits_stride elements from row
+ * to row; labels: rows int32; old_logp, ref_logp, advantage, loss, logp: rows floats. clip_low and clip_high are not negative
+ * (clip_low may exceed 1).
+ *
+ * Gradient: d_logits[r] = row_grad[r] * d loss[r] / d z, with row_grad: rows floats (nullable: ones). A ratio on the edge of the
+ * clipped range counts as inside. slidedp_policy_loss_backward takes the forward's logp;
+ * slidedp_policy_step computes loss, logp and gradient in one call. d_logits may be the logits themselves (same address and
+ * stride; the same address with another stride is refused). Rows whose gradient is zero throughout (absent, clipped without a
+ * second term, row_grad 0) are zeros whatever their logits hold; in others NaN and +inf among the logits make the row NaN.
+ */
+typedef struct {
+  int64_t rows, vocab;
+  int32_t dtype; /* slidedp_dtype of logits and d_logits */
+  int32_t reserved;
+  int64_t logits_stride, d_logits_stride;
+  double temperature, clip_low, clip_high, kl_weight;
+} slidedp_policy_args;
+
+SLIDEDP_API int slidedp_policy_loss(slidedp_ctx* ctx, const slidedp_policy_args* args, const void* logits, const int32_t* labels,
+                        const float* old_logp, const float* ref_logp, const float* advantage, float* loss, float* logp,
+                        void* cuda_stream);
+SLIDEDP_API int slidedp_policy_loss_backward(slidedp_ctx* ctx, const slidedp_policy_args* args, const void* logits,
+                                 const int32_t* labels, const float* old_logp, const float* ref_logp, const float* advantage,
+                                 const float* logp, const float* row_grad, void* d_logits, void* cuda_stream);
+SLIDEDP_API int slidedp_policy_step(slidedp_ctx* ctx, const slidedp_policy_args* args, const void* logits, const int32_t* labels,
+                        const float* old_logp, const float* ref_logp, const float* advantage, const float* row_grad,
+                        float* loss, float* logp, void* d_logits, void* cuda_stream);
+
+/* ---- clipping by the norm over many tensors -------------------------------------------------------
+ *
+ * S = sum over all tensors of (scale * x)^2, norm = sqrt(S), coef = min(1, max_norm / (norm + 1e-6)) or 1 where max_norm <= 0,
+ *   out = x * (scale * coef)          (the factor is formed in double and used as FP32)
+ * result: device, four doubles: S, norm, coef, and 1.0 if the norm is inf or NaN, 0.0 otherwise, as slidedp_grad_norm_finish has
+ * them. So accumulated FP32 gradients of any number of tensors become the clipped BF16 gradients that
+ * slidedp_reduce_adamw_chunk takes (with max_norm 0 there). grads, outs: host arrays of `count` tensors each, read before the
+ * call returns; outs[i] has grads[i].count elements of either type and may be grads[i] itself (same address and type); outs NULL:
+ * only result is written. Tensors need the alignment of their element; they may be empty. A factor of 1 in place writes nothing.
+ * With max_norm > 0 a NaN norm makes coef and with it every output NaN, an infinite one makes coef 0. The sums are FP64 in an order that the tensors' sizes alone decide.
+ * workspace: device, slidedp_clip_grad_norm_workspace bytes, 16-byte aligned.
+ */
+typedef struct {
+  void* data;
+  int64_t count;
+  int32_t dtype; /* slidedp_dtype */
+  int32_t reserved;
+} slidedp_tensor;
+
+SLIDEDP_API int slidedp_clip_grad_norm(slidedp_ctx* ctx, const slidedp_tensor* grads, const slidedp_tensor* outs, int32_t count,
+                           double scale, double max_norm, double* result, void* workspace, void* cuda_stream);
+/* 0 for tensors that the call would refuse. */
+SLIDEDP_API size_t slidedp_clip_grad_norm_workspace(const slidedp_tensor* grads, int32_t count);
 
 #ifdef __cplusplus
 }

@@ -17,11 +17,13 @@ LIB = os.path.join(PKG, "libslidedp.so")
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")     # the binding's own part in C++, for this interpreter and torch
 SOURCES = [os.path.join(CSRC, f) for f in ("common.cu", "context.cu", "update.cu", "stream.cu",
                                            "model.cu", "ipc.cu", "qk_norm_rope.cu", "distill.cu",
-                                           "attention.cu", "attention_mma.cu")]
+                                           "attention.cu", "attention_mma.cu", "embedding.cu",
+                                           "block_norm.cu", "policy.cu", "clip.cu")]
 DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in ("kernels.cuh", "cast_kernel.cuh",
                                                      "device_utils.cuh", "types.h", "internal.h",
                                                      "ops_internal.h", "attention.h",
-                                                     "attention_rows.cuh", "tcgen05.cuh")]
+                                                     "attention_rows.cuh", "tcgen05.cuh",
+                                                     "logit_rows.cuh", "rows.cuh")]
 DEPENDS += [os.path.join(ROOT, "include", f) for f in ("slidedp.h", "slidedp_ops.h")]
 
 

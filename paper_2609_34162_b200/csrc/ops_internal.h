@@ -1,6 +1,9 @@
 // Declarations shared by the translation units of the fine-tuning operators (not installed).
 #pragma once
 
+#include <initializer_list>
+#include <utility>
+
 #include "internal.h"
 #include "slidedp_ops.h"
 
@@ -28,6 +31,26 @@ inline bool is_finite(double x) { return x - x == 0.0; }
 // would silently be another.
 inline bool fits_f32(double x) { return is_finite((double)(float)x); }
 inline bool positive_f32(double x) { return fits_f32(x) && (float)x > 0.0f; }
+
+inline bool rows_ok(const slidedp_rows* r, int elem, int64_t rows, int64_t columns, bool output) {
+  return r && r->data && r->stride >= 0 && reinterpret_cast<uintptr_t>(r->data) % elem == 0 && (!output || rows <= 1 || r->stride >= columns);
+}
+inline int elem_bytes(int32_t dtype) { return dtype == SLIDEDP_F32 ? 4 : 2; }
+
+// Values per thread and row that all tensors' alignment allows.
+inline int vector_width(int64_t hidden, int elem, std::initializer_list<std::pair<const slidedp_rows*, int>> all) {
+  const auto fits = [&](int v) {
+    if (hidden % v != 0) return false;
+    for (const auto& r : all) {
+      if (!r.first) continue;
+      const int64_t bytes = v * r.second < 16 ? v * r.second : 16;
+      if (reinterpret_cast<uintptr_t>(r.first->data) % bytes != 0 || r.first->stride * r.second % bytes != 0) return false;
+    }
+    return true;
+  };
+  if (fits(16 / elem)) return 16 / elem;
+  return elem == 2 && fits(2) ? 2 : 1;
+}
 
 // Launches a kernel of the operators, in clusters of `cluster` blocks if that is above one. It may be set up while the
 // kernel before it in the stream ends: every block of it waits for that kernel before its first access to memory (where it

@@ -185,11 +185,35 @@ class _DistillArgs(ctypes.Structure):
                 ("temperature", ctypes.c_double), ("w_teacher", ctypes.c_double), ("w_label", ctypes.c_double)]
 
 
+class _EmbeddingArgs(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("vocab", ctypes.c_int64), ("hidden", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("accumulate", ctypes.c_int32), ("reserved", ctypes.c_int32), ("scale", ctypes.c_double)]
+
+
+class _BlockNormArgs(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("hidden", ctypes.c_int64), ("dtype", ctypes.c_int32), ("has_y", ctypes.c_int32),
+                ("post_norm", ctypes.c_int32), ("pre_norm", ctypes.c_int32), ("gate_kind", ctypes.c_int32), ("gate_sigmoid", ctypes.c_int32),
+                ("residual_scale", ctypes.c_double), ("eps", ctypes.c_double)]
+
+
+class _PolicyArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("logits_stride", ctypes.c_int64), ("d_logits_stride", ctypes.c_int64), ("temperature", ctypes.c_double),
+                ("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double), ("kl_weight", ctypes.c_double)]
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 # A call's views (slidedp_heads: an address and two strides, _V bytes each) are written to the calling thread's argument block
 # and passed as addresses there; the scalar arguments go as the bytes of their struct (a ctypes object costs three times that).
-_V = 24
+# slidedp_rows (an address and a stride) take _R bytes.
+_V, _R = 24, 16
 _qk_bytes, _attn_bytes, _distill_bytes = (struct.Struct(f).pack for f in ("@qiiiiiiqd", "@qiiiiiiPPPdd", "@qqiiqqddd"))
-for _args, _pack in ((_QkArgs, _qk_bytes), (_AttnArgs, _attn_bytes), (_DistillArgs, _distill_bytes)):
+_embedding_bytes, _block_norm_bytes, _policy_bytes = (struct.Struct(f).pack for f in ("@qqqiiiid", "@qqiiiiiidd", "@qqiiqqdddd"))
+for _args, _pack in ((_QkArgs, _qk_bytes), (_AttnArgs, _attn_bytes), (_DistillArgs, _distill_bytes), (_EmbeddingArgs, _embedding_bytes),
+                     (_BlockNormArgs, _block_norm_bytes), (_PolicyArgs, _policy_bytes)):
     assert len(_pack(*[0] * len(_args._fields_))) == ctypes.sizeof(_args)
 for _name, _res, _args in (
         ("slidedp_qk_norm_rope", ctypes.c_int, [_vp, _vp] + [_vp] * 9),
@@ -200,7 +224,18 @@ for _name, _res, _args in (
         ("slidedp_attention_workspace", ctypes.c_size_t, [_vp]),
         ("slidedp_distill_loss", ctypes.c_int, [_vp, _vp] + [_vp] * 7),
         ("slidedp_distill_loss_backward", ctypes.c_int, [_vp, _vp] + [_vp] * 8),
-        ("slidedp_distill_step", ctypes.c_int, [_vp, _vp] + [_vp] * 9)):
+        ("slidedp_distill_step", ctypes.c_int, [_vp, _vp] + [_vp] * 9),
+        ("slidedp_embedding", ctypes.c_int, [_vp, _vp] + [_vp] * 4),
+        ("slidedp_embedding_backward", ctypes.c_int, [_vp, _vp] + [_vp] * 5),
+        ("slidedp_embedding_workspace", ctypes.c_size_t, [_vp]),
+        ("slidedp_block_norm", ctypes.c_int, [_vp, _vp] + [_vp] * 8),
+        ("slidedp_block_norm_backward", ctypes.c_int, [_vp, _vp] + [_vp] * 14),
+        ("slidedp_block_norm_workspace", ctypes.c_size_t, [_vp]),
+        ("slidedp_policy_loss", ctypes.c_int, [_vp, _vp] + [_vp] * 8),
+        ("slidedp_policy_loss_backward", ctypes.c_int, [_vp, _vp] + [_vp] * 9),
+        ("slidedp_policy_step", ctypes.c_int, [_vp, _vp] + [_vp] * 10),
+        ("slidedp_clip_grad_norm", ctypes.c_int, [_vp, _vp, _vp, ctypes.c_int32, ctypes.c_double, ctypes.c_double] + [_vp] * 3),
+        ("slidedp_clip_grad_norm_workspace", ctypes.c_size_t, [_vp, ctypes.c_int32])):
     getattr(_lib, _name).restype, getattr(_lib, _name).argtypes = _res, _args
 
 
@@ -295,15 +330,30 @@ def _matrix(x, what: str, dtype, shape) -> int:
     return t if shape[0] > 1 else shape[1]
 
 
+def _careful_rows(x, what: str, dtype, shape):
+    """Address and row stride of a [rows, columns] tensor whose last axis is contiguous."""
+    x = _as_tensor(x)
+    return (0 if not isinstance(x, torch.Tensor) else x.data_ptr()), _matrix(x, what, dtype, shape)
+
+
+def _careful_tensor(x, what: str):
+    """Address, size and type of one of many tensors."""
+    x = _as_tensor(x)
+    dtype = x.dtype if isinstance(x, torch.Tensor) else None
+    if dtype not in _DTYPES:
+        raise TypeError(f"{what} must be CUDA tensors of bfloat16 or float32")
+    return _careful_flat(x, what, dtype), x.numel(), _DTYPES[dtype]
+
+
 def _no_marshal(*_):
     raise ImportError("the operators need the binding's C++ module, built for this torch: `python -m paper_2609_34162_b200.build`") from _marshal_error
 
 
 if _marshal is None:
-    _flat = _heads = _block = _no_marshal
+    _flat = _heads = _rows = _tensors = _block = _no_marshal
 else:
-    _marshal.setup(_careful_flat, _careful_heads)
-    _flat, _heads, _block = _marshal.flat, _marshal.heads, _marshal.block
+    _marshal.setup(_careful_flat, _careful_heads, _careful_rows, _careful_tensor)
+    _flat, _heads, _rows, _tensors, _block = _marshal.flat, _marshal.heads, _marshal.rows, _marshal.tensors, _marshal.block
 
 
 def _workspace(x, nbytes: int) -> int:
@@ -659,6 +709,171 @@ class Context:
                                           temperature, w_teacher, w_label)
         self._check(_lib.slidedp_distill_step(self._h, a, *ins, g, _flat(loss, "loss", torch.float32, logits.shape[:1]), l,
                                               d_logits.data_ptr(), _stream(stream, self.device)))
+
+    @staticmethod
+    def _embedding_args(tokens, table, table_dtype_of, grad_dtype, scale, accumulate):
+        shape, dt = table.shape, table_dtype_of.dtype
+        if len(shape) != 2 or dt not in _DTYPES or grad_dtype not in _DTYPES:
+            raise TypeError("the table and its rows must be matrices of bfloat16 or float32")
+        return _embedding_bytes(tokens, shape[0], shape[1], _DTYPES[dt], _DTYPES[grad_dtype], bool(accumulate), 0, scale)
+
+    def slidedp_embedding(self, table, ids, out, scale: float = 1.0, stream=None) -> None:
+        """``out`` [tokens, hidden] = ``scale`` times the rows of ``table`` [vocab, hidden] that the int32 ``ids`` [tokens] name;
+        zeros for ids outside the table."""
+        at, dt, shape, T = _block(self.device), table.dtype, table.shape, len(ids)
+        a = self._embedding_args(T, table, table, dt, scale, False)
+        _rows(at, dt, shape, table, "table")
+        _rows(at + _R, dt, (T, shape[1]), out, "out")
+        rc = _lib.slidedp_embedding(self._h, a, at, _flat(ids, "ids", torch.int32, (T,)), at + _R, _stream(stream, self.device))
+        if rc:
+            self._check(rc)
+
+    def slidedp_embedding_workspace(self, d_out, d_table) -> int:
+        """Bytes of workspace that ``slidedp_embedding_backward`` needs."""
+        return int(_lib.slidedp_embedding_workspace(self._embedding_args(len(d_out), d_table, d_out, d_table.dtype, 1.0, False)))
+
+    def slidedp_embedding_backward(self, ids, d_out, d_table, workspace, scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
+        """``d_table`` [vocab, hidden] (either type): the gradient of the table from that of the rows, ``d_out`` [tokens, hidden].
+        ``accumulate`` adds to what it holds, and touches only the rows that have tokens."""
+        at, shape, T = _block(self.device), d_table.shape, len(ids)
+        a = self._embedding_args(T, d_table, d_out, d_table.dtype, scale, accumulate)
+        _rows(at, d_out.dtype, (T, shape[1]), d_out, "d_out")
+        _rows(at + _R, d_table.dtype, shape, d_table, "d_table")
+        rc = _lib.slidedp_embedding_backward(self._h, a, _flat(ids, "ids", torch.int32, (T,)), at, at + _R,
+                                             _workspace(workspace, _lib.slidedp_embedding_workspace(a)), _stream(stream, self.device))
+        if rc:
+            self._check(rc)
+
+    @staticmethod
+    def _block_norm_args(x, has_y, post_norm, pre_norm, gate, gate_sigmoid, residual_scale, eps):
+        shape, dt = x.shape, x.dtype
+        if dt not in _DTYPES or len(shape) != 2:
+            raise TypeError("x must be [tokens, hidden] of bfloat16 or float32")
+        return _block_norm_bytes(shape[0], shape[1], _DTYPES[dt], has_y, bool(post_norm), pre_norm,
+                                 0 if gate is None else gate.dim(), bool(gate_sigmoid) and gate is not None, residual_scale, eps)
+
+    @staticmethod
+    def _block_norm_inputs(at, x, y, w_post, gate, w_pre):
+        """The views of x, y and the gate at ``at``, and the weights' addresses."""
+        dt, shape = x.dtype, x.shape
+        H = (shape[1],)
+        if gate is not None and gate.dim() == 1:
+            _rows(at, dt, shape, x, "x", y, "y")
+            _rows(at + 2 * _R, dt, (1, H[0]), gate[None], "gate")
+        else:
+            _rows(at, dt, shape, x, "x", y, "y", gate, "gate")
+        return (None if w_post is None else _flat(w_post, "w_post", dt, H), None if w_pre is None else _flat(w_pre, "w_pre", dt, H))
+
+    def slidedp_block_norm(self, x, y, w_post, gate, w_pre, x_out, h_out, residual_scale: float = 1.0, eps: float = 1e-6,
+                           post_norm: bool = True, gate_sigmoid: bool = False, stream=None) -> None:
+        """``x_out`` = ``x`` + ``residual_scale`` * gate * n with n the RMS norm of the block's output ``y`` times ``w_post``
+        (``post_norm`` False: ``y`` itself), and the next block's input ``h_out`` = RMS norm of ``x_out`` times ``w_pre``
+        (``h_out`` None: not wanted). All [tokens, hidden]; ``gate``: None, [hidden] or [tokens, hidden], through a sigmoid with
+        ``gate_sigmoid``. ``y`` and ``x_out`` None: the first norm, of ``x`` alone."""
+        at, has_y = _block(self.device), y is not None
+        a = self._block_norm_args(x, has_y, post_norm and has_y, h_out is not None, gate, gate_sigmoid, residual_scale, eps)
+        w_post, w_pre = self._block_norm_inputs(at, x, y, w_post, gate, w_pre)
+        _rows(at + 3 * _R, x.dtype, x.shape, x_out, "x_out", h_out, "h_out")
+        rc = _lib.slidedp_block_norm(self._h, a, at, at + _R, w_post, at + 2 * _R, w_pre, at + 3 * _R, at + 4 * _R, _stream(stream, self.device))
+        if rc:
+            self._check(rc)
+
+    def slidedp_block_norm_workspace(self, x) -> int:
+        """Bytes of workspace that ``slidedp_block_norm_backward`` needs for rows like ``x``."""
+        return int(_lib.slidedp_block_norm_workspace(self._block_norm_args(x, True, True, True, None, False, 1.0, 0.0)))
+
+    def slidedp_block_norm_backward(self, x, y, w_post, gate, w_pre, dx_out, dh_out, dx, dy, dgate, dw_post, dw_pre, workspace,
+                                    residual_scale: float = 1.0, eps: float = 1e-6, post_norm: bool = True, gate_sigmoid: bool = False,
+                                    stream=None) -> None:
+        """Gradients ``dx``, ``dy``, ``dgate`` (float32 [hidden] for a gate of that shape), ``dw_post`` and ``dw_pre`` (float32) from
+        ``dx_out`` (None: zeros) and ``dh_out`` (None: the forward had no ``h_out``). The last three may be None."""
+        at, dt, shape, f32, has_y = _block(self.device), x.dtype, x.shape, torch.float32, y is not None
+        H = (shape[1],)
+        a = self._block_norm_args(x, has_y, post_norm and has_y, dh_out is not None, gate, gate_sigmoid, residual_scale, eps)
+        vector = gate is not None and gate.dim() == 1
+        ws = None
+        if dw_post is not None or dw_pre is not None or (vector and dgate is not None):
+            ws = _workspace(workspace, _lib.slidedp_block_norm_workspace(a))
+        w_post, w_pre = self._block_norm_inputs(at, x, y, w_post, gate, w_pre)
+        _rows(at + 3 * _R, dt, shape, dx_out, "dx_out", dh_out, "dh_out", dx, "dx", dy, "dy")
+        if vector and dgate is not None:
+            _rows(at + 7 * _R, f32, (1, H[0]), dgate[None], "dgate")
+        else:
+            _rows(at + 7 * _R, dt, shape, dgate, "dgate")
+        rc = _lib.slidedp_block_norm_backward(
+            self._h, a, at, at + _R, w_post, at + 2 * _R, w_pre, *(at + i * _R for i in range(3, 8)),
+            None if dw_post is None else _flat(dw_post, "dw_post", f32, H), None if dw_pre is None else _flat(dw_pre, "dw_pre", f32, H), ws,
+            _stream(stream, self.device))
+        if rc:
+            self._check(rc)
+
+    def _policy_call(self, logits, labels, old_logp, ref_logp, advantage, d_logits, temperature, clip_low, clip_high, kl_weight):
+        """slidedp_policy_args and the inputs' addresses."""
+        if logits.dtype not in _DTYPES or logits.dim() != 2:
+            raise TypeError("logits must be [rows, vocab] of bfloat16 or float32")
+        _block(self.device)
+        dt, shape, f32 = logits.dtype, logits.shape, torch.float32
+        rows, each = shape[0], shape[:1]
+        a = _policy_bytes(rows, shape[1], _DTYPES[dt], 0, _matrix(logits, "logits", dt, shape),
+                          0 if d_logits is None else _matrix(d_logits, "d_logits", dt, shape), temperature, clip_low, clip_high, kl_weight)
+        return a, (logits.data_ptr(), _flat(labels, "labels", torch.int32, each),
+                   None if old_logp is None else _flat(old_logp, "old_logp", f32, each),
+                   None if ref_logp is None else _flat(ref_logp, "ref_logp", f32, each),
+                   None if advantage is None else _flat(advantage, "advantage", f32, each))
+
+    def slidedp_policy_loss(self, logits, labels, old_logp, ref_logp, advantage, loss, logp, temperature: float = 1.0, clip_low: float = 0.2,
+                            clip_high: float = 0.2, kl_weight: float = 0.0, stream=None) -> None:
+        """Per row the clipped policy ``loss`` and the log-probability ``logp`` of the int32 ``labels`` under ``logits`` [rows,
+        vocab]; all other arguments float32 per row. With ``old_logp``, ``ref_logp``, ``advantage`` and ``loss`` None: the
+        log-probabilities alone."""
+        a, ins = self._policy_call(logits, labels, old_logp, ref_logp, advantage, None, temperature, clip_low, clip_high, kl_weight)
+        f32, each = torch.float32, logits.shape[:1]
+        rc = _lib.slidedp_policy_loss(self._h, a, *ins, None if loss is None else _flat(loss, "loss", f32, each), _flat(logp, "logp", f32, each),
+                                      _stream(stream, self.device))
+        if rc:
+            self._check(rc)
+
+    def slidedp_policy_loss_backward(self, logits, labels, old_logp, ref_logp, advantage, logp, row_grad, d_logits, temperature: float = 1.0,
+                                     clip_low: float = 0.2, clip_high: float = 0.2, kl_weight: float = 0.0, stream=None) -> None:
+        """``d_logits`` = ``row_grad`` (float32 per row; None: ones) times the loss's gradient, with the forward's ``logp``.
+        ``d_logits`` may be ``logits``."""
+        a, ins = self._policy_call(logits, labels, old_logp, ref_logp, advantage, d_logits, temperature, clip_low, clip_high, kl_weight)
+        f32, each = torch.float32, logits.shape[:1]
+        rc = _lib.slidedp_policy_loss_backward(self._h, a, *ins, _flat(logp, "logp", f32, each),
+                                               None if row_grad is None else _flat(row_grad, "row_grad", f32, each), d_logits.data_ptr(),
+                                               _stream(stream, self.device))
+        if rc:
+            self._check(rc)
+
+    def slidedp_policy_step(self, logits, labels, old_logp, ref_logp, advantage, row_grad, loss, logp, d_logits, temperature: float = 1.0,
+                            clip_low: float = 0.2, clip_high: float = 0.2, kl_weight: float = 0.0, stream=None) -> None:
+        """``loss``, ``logp`` and ``d_logits`` in one pass over the logits."""
+        a, ins = self._policy_call(logits, labels, old_logp, ref_logp, advantage, d_logits, temperature, clip_low, clip_high, kl_weight)
+        f32, each = torch.float32, logits.shape[:1]
+        rc = _lib.slidedp_policy_step(self._h, a, *ins, None if row_grad is None else _flat(row_grad, "row_grad", f32, each),
+                                      None if loss is None else _flat(loss, "loss", f32, each), _flat(logp, "logp", f32, each),
+                                      d_logits.data_ptr(), _stream(stream, self.device))
+        if rc:
+            self._check(rc)
+
+    def slidedp_clip_grad_norm_workspace(self, grads) -> int:
+        """Bytes of workspace that ``slidedp_clip_grad_norm`` needs for these tensors."""
+        _block(self.device)
+        return int(_lib.slidedp_clip_grad_norm_workspace(_tensors(grads, "grads"), len(grads)))
+
+    def slidedp_clip_grad_norm(self, grads, outs, max_norm: float, result, workspace, scale: float = 1.0, stream=None) -> None:
+        """``outs`` (may be ``grads``; None: the norm alone) = the tensors of ``grads`` times ``scale`` times the coefficient
+        min(1, max_norm / (norm + 1e-6)), with the norm over all of them; bfloat16 or float32 each, contiguous. ``result``: four float64
+        (sum of squares, norm, coefficient, 1.0 if the norm is not finite)."""
+        _block(self.device)
+        n, g = len(grads), _tensors(grads, "grads")
+        o = None if outs is None else g if outs is grads else _tensors(outs, "outs")
+        if outs is not None and len(outs) != n:
+            raise ValueError("outs must hold as many tensors as grads")
+        rc = _lib.slidedp_clip_grad_norm(self._h, g, o, n, scale, max_norm, _flat(result, "result", torch.float64, (4,)),
+                                         _workspace(workspace, _lib.slidedp_clip_grad_norm_workspace(g, n)), _stream(stream, self.device))
+        if rc:
+            self._check(rc)
 
 
 def slidedp_model_stream_step(n_total: int, R: int, chunk_elems: int, nbuf: int, h2d_gbs: float,
