@@ -8,6 +8,7 @@
 // gradients in registers. One partial row of sums per block, added in a fixed order by a second kernel.
 #include "ops_internal.h"
 #include "rows.cuh"
+#include "tcgen05.cuh"
 
 #include <type_traits>
 
@@ -29,7 +30,7 @@ struct BlockNormParams {
   float alpha, eps, inv_hidden;
 };
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }
+__device__ __forceinline__ float sigmoid(float x) { return rcp_approx(1.0f + __expf(-x)); }
 
 // Sums of up to two values over the block; each call uses the other half of `sh`, so that one barrier is enough.
 struct BlockSums {
@@ -251,9 +252,438 @@ __global__ void __launch_bounds__(kThreads) block_norm_backward_kernel(const __g
   }
 }
 
-// Adds the blocks' partial rows: 32 columns per block, eight parts of the blocks, joined in order. What the columns of the first
+// ---- rows in shared memory ---------------------------------------------------------------------------------
+// Rows are copied in bulk into a ring ahead of their use, so that what is under way costs no registers. A thread has 16 columns of
+// every row: 16-byte vectors where rows are aligned to them, else single columns, neighbours with neighbouring threads. The factors
+// of y r and of x' r' lie behind the ring in FP32. Two values per instruction. Measured before (rows in registers, no copies ahead):
+// 8192 x 4096 BF16 with both norms, forward 96 us, backward 166; now see the table of the widths below.
+
+__device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
+__device__ __forceinline__ float sum_of(uint64_t v) {
+  float a, b;
+  split(v, &a, &b);
+  return a + b;
+}
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t v) {
+  float a, b;
+  split(v, &a, &b);
+  return pair(sigmoid(a), sigmoid(b));
+}
+
+constexpr int kCols = 16;              // per thread
+constexpr int kPairs = kCols / 2;
+
+// A thread's columns: vectors blockDim vectors apart, or single ones blockDim apart. Columns behind the row are zeros: vectors have
+// zeros behind their rows in shared memory, for single columns it is asked.
+template <typename T, bool kVector>
+struct Columns {
+  static constexpr int V = kVector ? 16 / (int)sizeof(T) : 1, K = kCols / V;
+  static __device__ __forceinline__ int first(int k) { return (k * blockDim.x + threadIdx.x) * V; }
+  static __device__ __forceinline__ void load(const char* row, int hidden, uint64_t* v) {
+    float one[2];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = first(k);
+      if constexpr (kVector) {
+        const uint4 a = *reinterpret_cast<const uint4*>(row + c * sizeof(T));
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[k * 4 + e] = pair(bf16_lo(w[e]), bf16_hi(w[e]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) v[k * 2 + e] = pair(__uint_as_float(w[2 * e]), __uint_as_float(w[2 * e + 1]));
+        }
+      } else {
+        one[k % 2] = 0.0f;
+        if (c < hidden) {
+          if constexpr (sizeof(T) == 2) one[k % 2] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[c] << 16);
+          else one[k % 2] = reinterpret_cast<const float*>(row)[c];
+        }
+        if (k % 2) v[k / 2] = pair(one[0], one[1]);
+      }
+    }
+  }
+  // Factors lie as threads read them: the fours of a thread's values blockDim fours apart (behind one another in a thread's own order,
+  // vectors of eight would meet in the same banks: 94.7 -> FOURS us backward).
+  static __device__ __forceinline__ int place(int value) { return (value / 4 * blockDim.x + threadIdx.x) * 4 + value % 4; }
+  static __device__ __forceinline__ void load_factors(const float* w, uint64_t* v) {
+#pragma unroll
+    for (int j = 0; j < kCols / 4; ++j) {
+      const float4 a = *reinterpret_cast<const float4*>(w + place(4 * j));
+      v[2 * j] = pair(a.x, a.y);
+      v[2 * j + 1] = pair(a.z, a.w);
+    }
+  }
+  static __device__ __forceinline__ void store(T* row, int hidden, const uint64_t* v) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = first(k);
+      float f[V];
+      if constexpr (kVector) {
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) split(v[k * V / 2 + e], &f[2 * e], &f[2 * e + 1]);
+      } else {
+        float lo, hi;
+        split(v[k / 2], &lo, &hi);
+        f[0] = k % 2 ? hi : lo;
+      }
+      if (c < hidden) store_values<V>(row + c, f);
+    }
+  }
+  static __device__ __forceinline__ void store_f32(float* row, int hidden, const uint64_t* v) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = first(k);
+      if (c >= hidden) continue;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float lo, hi;
+        split(v[(k * V + e) / 2], &lo, &hi);
+        row[c + e] = (k * V + e) % 2 ? hi : lo;
+      }
+    }
+  }
+  // f(column, place of its factors) for every column of the thread
+  template <typename F>
+  static __device__ __forceinline__ void each(F f) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int e = 0; e < V; ++e) f(first(k) + e, place(k * V + e));
+  }
+};
+
+// Sums over the block of up to 16 warps, as block_sums; the second of two values is folded onto the upper lanes, and every thread
+// adds the warps' sums itself.
+template <int kWarps>
+__device__ __forceinline__ float2 ring_sums(float a, float b, float2 (*part)[kWarps], int& turn) {
+  const bool upper = threadIdx.x & 16;
+  float v = (upper ? b : a) + __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  turn ^= 1;
+  if (threadIdx.x % 16 == 0) reinterpret_cast<float*>(&part[turn][threadIdx.x / 32])[threadIdx.x / 16 % 2] = v;
+  __syncthreads();
+  uint64_t s = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; w += 2) {
+    const float4 x = *reinterpret_cast<const float4*>(&part[turn][w]);
+    s = add2(s, add2(pair(x.x, x.y), pair(x.z, x.w)));
+  }
+  float2 r;
+  split(s, &r.x, &r.y);
+  return r;
+}
+
+constexpr int kMaxNormStages = 4;
+constexpr int kMaxNormInputs = 5;
+enum NormInput { kInX, kInY, kInGate, kInDx, kInDh };
+
+struct NormFeed {
+  const char* src[kMaxNormInputs];
+  int64_t stride[kMaxNormInputs];    // bytes
+  int slot[kMaxNormInputs];          // the row's place in a stage
+  int inputs, stages;
+  uint32_t row_bytes, slot_bytes;    // a slot has room for the row wherever in its first 16 bytes it begins
+};
+struct NormRingParams {
+  BlockNormParams n;
+  NormFeed feed;
+  int* error;
+  uint32_t polls;
+};
+struct NormRing {
+  uint64_t full[kMaxNormStages];
+  uint32_t dead;
+};
+
+// The ring from the side of one thread; row number i of the block goes to stage i % stages. Thread 0 copies. A wait that runs out
+// makes it stop copying, and the block goes on with what there is to its end: the call has failed, and says so.
+template <bool kVector>
+struct NormRows {
+  const NormRingParams& p;
+  NormRing& ring;
+  char* smem;
+  int64_t count;                 // rows of this block
+  int64_t issued = 0, ready = 0;
+  int stage = 0;                 // of the present row
+  uint32_t parity = 0;
+  bool ok = true;
+  __device__ NormRows(const NormRingParams& p_, NormRing& ring_, void* smem_) : p(p_), ring(ring_), smem(static_cast<char*>(smem_)) {
+    count = p.n.tokens > blockIdx.x ? (p.n.tokens - 1 - blockIdx.x) / gridDim.x + 1 : 0;
+  }
+  __device__ __forceinline__ char* slot(int s, int input) const { return smem + (s * p.feed.inputs + p.feed.slot[input]) * p.feed.slot_bytes; }
+  // Rows that are not aligned are copied from the 16 bytes that hold their first value to those that hold their last, and lie in
+  // their slot as they lie in memory. What else those hold belongs to the rows next to them; before the first row and behind the last
+  // nothing is read, but value by value up to the next 16 bytes.
+  __device__ __forceinline__ void issue_next() {   // thread 0
+    if (!ok || issued >= count) return;
+    const int s = (int)(issued % p.feed.stages);
+    const int64_t row = blockIdx.x + issued * gridDim.x;
+    const uint32_t bar = smem_addr(&ring.full[s]);
+    if constexpr (kVector) {
+      mbar_expect(bar, p.feed.inputs * p.feed.row_bytes);
+#pragma unroll
+      for (int i = 0; i < kMaxNormInputs; ++i)
+        if (p.feed.src[i]) bulk_load(smem_addr(slot(s, i)), p.feed.src[i] + row * p.feed.stride[i], p.feed.row_bytes, bar);
+    } else {
+      uint32_t bytes = 0;
+#pragma unroll 1
+      for (int turn = 0; turn < 2; ++turn) {       // how much it is, then the copies
+        if (turn == 1) mbar_expect(bar, bytes);
+#pragma unroll 1
+        for (int i = 0; i < kMaxNormInputs; ++i) {
+          if (!p.feed.src[i]) continue;
+          const uintptr_t from = reinterpret_cast<uintptr_t>(p.feed.src[i] + row * p.feed.stride[i]), to = from + p.feed.row_bytes;
+          const uintptr_t first = reinterpret_cast<uintptr_t>(p.feed.src[i]), last = first + (p.n.tokens - 1) * p.feed.stride[i] + p.feed.row_bytes;
+          const uintptr_t grid = from & ~(uintptr_t)15, lo = grid < first ? (from + 15) & ~(uintptr_t)15 : grid;
+          const uintptr_t hi = ((to + 15) & ~(uintptr_t)15) > last ? to & ~(uintptr_t)15 : (to + 15) & ~(uintptr_t)15;
+          const bool some = hi > lo;
+          if (turn == 1) {
+            if (some) bulk_load(smem_addr(slot(s, i)) + (uint32_t)(lo - grid), reinterpret_cast<const void*>(lo), (uint32_t)(hi - lo), bar);
+            continue;
+          }
+          if (some) bytes += (uint32_t)(hi - lo);
+          const uintptr_t end = some ? lo : to, begin = some ? hi : to;      // what is left: [from, end) and [begin, to)
+          for (uintptr_t a = from; a < end; a += 2) *reinterpret_cast<uint16_t*>(slot(s, i) + (a - grid)) = *reinterpret_cast<const uint16_t*>(a);
+          for (uintptr_t a = begin; a < to; a += 2) *reinterpret_cast<uint16_t*>(slot(s, i) + (a - grid)) = *reinterpret_cast<const uint16_t*>(a);
+        }
+      }
+    }
+    ++issued;
+  }
+  __device__ __forceinline__ void wait() {
+    ok &= Waiter{&ring.dead, p.error, p.polls}(smem_addr(&ring.full[stage]), parity);
+    if (ok) ++ready;
+  }
+  __device__ __forceinline__ void next() {
+    if (++stage == p.feed.stages) stage = 0, parity ^= 1;
+  }
+  __device__ __forceinline__ const char* at(int input, int64_t row) const {
+    const char* to = slot(stage, input);
+    if constexpr (!kVector) to += reinterpret_cast<uintptr_t>(p.feed.src[input] + row * p.feed.stride[input]) & 15u;
+    return to;
+  }
+  // Zeros behind the rows, once: copies do not reach them.
+  __device__ __forceinline__ void clear_padding() const {
+    if (!kVector) return;
+    const uint32_t words = (p.feed.slot_bytes - p.feed.row_bytes) / 4;
+    for (int i = 0; i < p.feed.stages * p.feed.inputs; ++i)
+      for (uint32_t w = threadIdx.x; w < words; w += blockDim.x) reinterpret_cast<uint32_t*>(smem + i * p.feed.slot_bytes + p.feed.row_bytes)[w] = 0;
+  }
+  __device__ __forceinline__ float* factors() const { return reinterpret_cast<float*>(smem + p.feed.stages * p.feed.inputs * p.feed.slot_bytes); }
+  __device__ __forceinline__ void finish() {       // thread 0: no copy is left under way
+    for (int64_t i = ready; i < issued; ++i) drain(smem_addr(&ring.full[i % p.feed.stages]), i / p.feed.stages & 1);
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ float weight(const void* w, int c) {
+  float v = 1.0f;
+  if (w) load_values<1>(static_cast<const T*>(w) + c, &v);
+  return v;
+}
+
+// The start that both kernels share: barriers, the first rows, the factors a g w_post (without a token's g) and w_pre.
+template <typename T, bool kVector, bool kToken, int kWarps>
+__device__ __forceinline__ void start_ring(const BlockNormParams& p, NormRows<kVector>& rows, float2 (*part)[kWarps]) {
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kMaxNormStages; ++s) mbar_init(smem_addr(&rows.ring.full[s]), 1);
+    rows.ring.dead = 0;
+    mbar_init_fence();
+  }
+  rows.clear_padding();
+  if (threadIdx.x < 2 * kWarps) part[threadIdx.x / kWarps][threadIdx.x % kWarps] = make_float2(0.0f, 0.0f);
+  __syncthreads();
+  wait_for_previous_kernel();
+  if (threadIdx.x == 0)
+    for (int s = 0; s < rows.p.feed.stages; ++s) rows.issue_next();
+  float *post = rows.factors(), *pre = post + blockDim.x * kCols;
+  Columns<T, kVector>::each([&](int c, int at) {
+    post[at] = pre[at] = 0.0f;
+    if (c >= p.hidden) return;
+    float f = p.alpha * weight<T>(p.w_post, c);
+    if (!kToken && p.gate_kind) {
+      const float g = weight<T>(p.gate.p, c);
+      f *= p.sigmoid ? sigmoid(g) : g;
+    }
+    post[at] = f;
+    pre[at] = weight<T>(p.w_pre, c);
+  });
+}
+
+// kToken: the gate is each token's. kFull: there are a block's output, both norms and, backward, both gradients; known when it is
+// compiled, which leaves out the moves of values between branches (8192 x 4096, forward and backward: 53.6 + 108.5 us -> KFULL).
+template <typename T, bool kVector, bool kToken, bool kFull, int kThreads, int kBlocks>
+__global__ void __launch_bounds__(kThreads, kBlocks) block_norm_ring_kernel(const __grid_constant__ NormRingParams rp) {
+  extern __shared__ uint4 dynamic[];
+  __shared__ NormRing ring;
+  __shared__ alignas(16) float2 part[2][kThreads / 32];
+  allow_next_kernel();
+  typedef Columns<T, kVector> C;
+  const BlockNormParams& p = rp.n;
+  NormRows<kVector> rows(rp, ring, dynamic);
+  start_ring<T, kVector, kToken>(p, rows, part);
+  const bool has_y = kFull || p.has_y, norm_y = kFull || p.post, norm_x = kFull || p.pre;
+  const float *post = rows.factors(), *pre = post + blockDim.x * kCols;
+  int turn = 0;
+  for (int64_t i = 0; i < rows.count; ++i, rows.next()) {
+    const int64_t row = blockIdx.x + i * gridDim.x;
+    rows.wait();
+    uint64_t x[kPairs], y[kPairs], f[kPairs];
+    C::load(rows.at(kInX, row), p.hidden, x);
+    float r = 1.0f;
+    if (has_y) {
+      C::load(rows.at(kInY, row), p.hidden, y);
+      C::load_factors(post, f);
+      if (kToken) {
+        uint64_t g[kPairs];
+        C::load(rows.at(kInGate, row), p.hidden, g);
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) f[e] = mul2(f[e], p.sigmoid ? sigmoid2(g[e]) : g[e]);
+      }
+      if (norm_y) {
+        uint64_t s = 0;
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) s = fma2(y[e], y[e], s);
+        r = rsqrtf(ring_sums(sum_of(s), 0.0f, part, turn).x * p.inv_hidden + p.eps);
+        if (threadIdx.x == 0) rows.issue_next();      // all threads have the row
+      }
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) x[e] = fma2(mul2(f[e], both(r)), y[e], x[e]);
+      C::store(static_cast<T*>(p.x_out.p) + row * p.x_out.stride, p.hidden, x);
+    }
+    if (norm_x) {
+      uint64_t s = 0;
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) s = fma2(x[e], x[e], s);
+      const float r2 = rsqrtf(ring_sums(sum_of(s), 0.0f, part, turn).x * p.inv_hidden + p.eps);
+      if (!norm_y && threadIdx.x == 0) rows.issue_next();
+      C::load_factors(pre, f);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) x[e] = mul2(mul2(f[e], both(r2)), x[e]);
+      C::store(static_cast<T*>(p.h_out.p) + row * p.h_out.stride, p.hidden, x);
+    } else if (!norm_y) {
+      __syncthreads();
+      if (threadIdx.x == 0) rows.issue_next();
+    }
+  }
+  if (threadIdx.x == 0) rows.finish();
+}
+
+template <typename T, bool kVector, bool kToken, bool kFull, int kThreads, int kBlocks>
+__global__ void __launch_bounds__(kThreads, kBlocks) block_norm_backward_ring_kernel(const __grid_constant__ NormRingParams rp) {
+  extern __shared__ uint4 dynamic[];
+  __shared__ NormRing ring;
+  __shared__ alignas(16) float2 part[2][kThreads / 32];
+  allow_next_kernel();
+  typedef Columns<T, kVector> C;
+  const BlockNormParams& p = rp.n;
+  NormRows<kVector> rows(rp, ring, dynamic);
+  start_ring<T, kVector, kToken>(p, rows, part);
+  const bool has_y = kFull || p.has_y, norm_y = kFull || p.post, norm_x = kFull || p.pre;
+  const float *post = rows.factors(), *pre = post + blockDim.x * kCols;
+  uint64_t sum_post[kPairs] = {}, sum_pre[kPairs] = {};
+  int turn = 0;
+  for (int64_t i = 0; i < rows.count; ++i, rows.next()) {
+    const int64_t row = blockIdx.x + i * gridDim.x;
+    rows.wait();
+    uint64_t x[kPairs], y[kPairs], g[kPairs], h[kPairs], f[kPairs];     // y: times r
+    float r = 1.0f, r2 = 0.0f, m = 0.0f;
+    if (has_y) {
+      C::load(rows.at(kInY, row), p.hidden, y);
+      if (norm_y) {
+        uint64_t s = 0;
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) s = fma2(y[e], y[e], s);
+        r = rsqrtf(ring_sums(sum_of(s), 0.0f, part, turn).x * p.inv_hidden + p.eps);
+      }
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) y[e] = mul2(y[e], both(r));
+      if (kToken) {
+        C::load(rows.at(kInGate, row), p.hidden, g);
+        if (p.sigmoid) {
+#pragma unroll
+          for (int e = 0; e < kPairs; ++e) g[e] = sigmoid2(g[e]);
+        }
+      }
+    }
+    if (norm_x) {
+      C::load(rows.at(kInX, row), p.hidden, x);
+      if (has_y) {
+        C::load_factors(post, f);
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) x[e] = fma2(kToken ? mul2(f[e], g[e]) : f[e], y[e], x[e]);
+      }
+      C::load(rows.at(kInDh, row), p.hidden, h);
+      C::load_factors(pre, f);
+      uint64_t ss = 0, ux = 0;
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) {
+        ss = fma2(x[e], x[e], ss);
+        ux = fma2(mul2(h[e], f[e]), x[e], ux);
+      }
+      const float2 s = ring_sums(sum_of(ss), sum_of(ux), part, turn);
+      r2 = rsqrtf(s.x * p.inv_hidden + p.eps);
+      m = -s.y * r2 * p.inv_hidden;
+    }
+    uint64_t d[kPairs] = {};
+    if (kFull || p.dx_out.p) C::load(rows.at(kInDx, row), p.hidden, d);
+    if (norm_x) {
+      C::load_factors(pre, f);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) {
+        const uint64_t xh = mul2(x[e], both(r2));
+        sum_pre[e] = fma2(h[e], xh, sum_pre[e]);
+        d[e] = fma2(both(r2), fma2(xh, both(m), mul2(h[e], f[e])), d[e]);
+      }
+    }
+    C::store(static_cast<T*>(p.dx.p) + row * p.dx.stride, p.hidden, d);
+    uint64_t dot = 0;
+    if (has_y) {
+      C::load_factors(post, f);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) {
+        x[e] = mul2(f[e], d[e]);                   // v, or v / g
+        d[e] = mul2(d[e], both(p.alpha));
+        if (kToken) {
+          const uint64_t v = mul2(x[e], g[e]);     // and x: dgate = v / g y r g'
+          sum_post[e] = fma2(mul2(d[e], g[e]), y[e], sum_post[e]);
+          dot = fma2(v, y[e], dot);
+          f[e] = mul2(x[e], y[e]);
+          if (p.sigmoid) f[e] = mul2(f[e], mul2(g[e], fma2(g[e], both(-1.0f), both(1.0f))));
+          x[e] = v;
+        } else {
+          sum_post[e] = fma2(d[e], y[e], sum_post[e]);
+          dot = fma2(x[e], y[e], dot);
+        }
+      }
+      if (kToken && p.dgate.p) C::store(static_cast<T*>(p.dgate.p) + row * p.dgate.stride, p.hidden, f);
+    }
+    if (norm_y) {
+      m = -ring_sums(sum_of(dot), 0.0f, part, turn).x * p.inv_hidden;
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) x[e] = mul2(both(r), fma2(y[e], both(m), x[e]));
+    } else {
+      __syncthreads();
+    }
+    if (threadIdx.x == 0) rows.issue_next();       // all threads have read the row
+    if (has_y) C::store(static_cast<T*>(p.dy.p) + row * p.dy.stride, p.hidden, x);
+  }
+  if (threadIdx.x == 0) rows.finish();
+  if (p.partial) {
+    float* at = p.partial + (int64_t)blockIdx.x * 2 * p.hidden;
+    C::store_f32(at, p.hidden, sum_post);
+    C::store_f32(at + p.hidden, p.hidden, sum_pre);
+  }
+}
+
+// ---- weights' gradients --------------------------------------------------------------------------------------
+
+// Adds the blocks' partial rows: 32 columns per block, 32 parts of the blocks, joined in order. What the columns of the first
 // sum stand for: sum a d y r, times g for w_post and times w_post g' for a gate for all tokens.
-constexpr int kNormSumParts = 8;
+constexpr int kNormSumParts = 32;
 template <typename T>
 __global__ void __launch_bounds__(32 * kNormSumParts) block_norm_sum_kernel(const __grid_constant__ BlockNormParams p, int blocks) {
   start_after_previous_kernel();
@@ -310,9 +740,10 @@ unsigned norm_threads(const slidedp_block_norm_args* a) {
   const int64_t n = (a->hidden + values_per_thread(a) - 1) / values_per_thread(a);
   return (unsigned)((n + 31) / 32 * 32);
 }
-// Blocks that stay: about 20 warps per SM, and no more than 16 blocks.
-int64_t norm_blocks(const slidedp_block_norm_args* a) {
-  const int64_t per_sm = 640 / norm_threads(a), most = 148 * (per_sm < 1 ? 1 : per_sm > 16 ? 16 : per_sm);
+// Blocks that stay, of which each has a row of partial sums: at most 16 per SM, or the second kernel becomes long.
+constexpr int kMaxNormBlocks = 16;
+int64_t norm_blocks(const slidedp_block_norm_args* a, int per_sm) {
+  const int64_t most = 148 * (per_sm < 1 ? 1 : per_sm > kMaxNormBlocks ? kMaxNormBlocks : per_sm);
   return a->tokens < most ? a->tokens : most;
 }
 
@@ -369,6 +800,75 @@ void pick_norm_kernel(const slidedp_block_norm_args* a, int v, F run) {
   else width(float(), N16(), std::integral_constant<int, 4>());
 }
 
+// Blocks that hold their rows in shared memory: threads, blocks per SM, stages of the ring. The kernels are compiled for up to 256,
+// 320 or 512 threads, and the blocks per SM that leave a thread 80 registers forward and 100 to 128 backward.
+struct RingPlan {
+  bool use, vector;
+  int threads, blocks, stages;
+  size_t smem, slot;
+};
+constexpr int ring_blocks(bool backward, int threads) { return threads > 256 ? (threads > 320 || backward ? 1 : 2) : backward ? 2 : 3; }
+constexpr int ring_class(int threads) { return threads <= 256 ? 256 : threads <= 320 ? 320 : 512; }
+constexpr int kNormSmem = 222 * 1024;      // of an SM's 227 KB, less what each block has besides
+
+RingPlan ring_plan(const slidedp_block_norm_args* a, bool vector, int inputs, bool backward) {
+  RingPlan r = {};
+  if (a->hidden > 512 * kCols) return r;
+  const int64_t row = a->hidden * elem_bytes(a->dtype);
+  r.vector = vector;
+  r.threads = (int)((a->hidden + kCols * 32 - 1) / (kCols * 32) * 32);
+  r.slot = vector ? r.threads * kCols * elem_bytes(a->dtype) : (row + 15) / 16 * 16 + 16;
+  const int cls = ring_class(r.threads), most = ring_blocks(backward, cls) * cls / r.threads;
+  for (r.blocks = most < kMaxNormBlocks ? most : kMaxNormBlocks; r.blocks >= 1; --r.blocks)
+    for (r.stages = kMaxNormStages; r.stages >= (r.blocks > 1 ? 2 : 1); --r.stages) {
+      r.smem = r.stages * inputs * r.slot + r.threads * kCols * 8;
+      if (r.blocks * (r.smem + 2048) <= kNormSmem) {
+        r.use = true;
+        return r;
+      }
+    }
+  return r;
+}
+NormRingParams ring_params(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const BlockNormParams& n, const RingPlan& plan) {
+  NormRingParams r = {};
+  r.n = n;
+  const NormView* in[kMaxNormInputs] = {&n.x, &n.y, &n.gate, &n.dx_out, &n.dh};
+  const int elem = elem_bytes(a->dtype);
+  for (int i = 0; i < kMaxNormInputs; ++i) {
+    if (i == kInGate && a->gate_kind != 2) continue;
+    r.feed.src[i] = static_cast<const char*>(in[i]->p);
+    r.feed.stride[i] = in[i]->stride * elem;
+    r.feed.slot[i] = r.feed.inputs;
+    r.feed.inputs += in[i]->p != nullptr;
+  }
+  r.feed.stages = plan.stages;
+  r.feed.row_bytes = (uint32_t)(a->hidden * elem);
+  r.feed.slot_bytes = (uint32_t)plan.slot;
+  r.error = ctx->kernel_error;
+  r.polls = ctx->wait_polls;
+  return r;
+}
+// run(T, vector, token, full, threads, blocks) as template arguments.
+template <bool kBackward, typename F>
+void pick_ring_kernel(const slidedp_block_norm_args* a, const RingPlan& plan, bool full, F run) {
+  typedef std::true_type Yes;
+  typedef std::false_type No;
+  const auto threads = [&](auto type, auto vector, auto token, auto whole) {
+    const auto with = [&](auto t) { run(type, vector, token, whole, t, std::integral_constant<int, ring_blocks(kBackward, t)>()); };
+    switch (ring_class(plan.threads)) {
+      case 256: return with(std::integral_constant<int, 256>());
+      case 320: return with(std::integral_constant<int, 320>());
+      default: return with(std::integral_constant<int, 512>());
+    }
+  };
+  const auto forms = [&](auto type, auto token) {
+    if (!plan.vector) return threads(type, No(), token, No());
+    full ? threads(type, Yes(), token, Yes()) : threads(type, Yes(), token, No());
+  };
+  const auto gates = [&](auto type) { a->gate_kind == 2 ? forms(type, Yes()) : forms(type, No()); };
+  a->dtype == SLIDEDP_BF16 ? gates(uint16_t()) : gates(float());
+}
+
 }  // namespace
 
 extern "C" {
@@ -403,12 +903,28 @@ int slidedp_block_norm(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const
   if (rc != SLIDEDP_OK) return rc;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const RingPlan plan = ring_plan(a, v * elem == 16, 1 + (y != nullptr) + (a->gate_kind == 2), false);
+  cudaError_t attribute = cudaSuccess;
   FAULT_POINT();
-  pick_norm_kernel(a, v, [&](auto type, auto vec, auto n, auto threads) {
-    typedef decltype(type) T_;
-    const auto run = [&](auto kernel) { launch_after(kernel, dim3((unsigned)norm_blocks(a)), norm_threads(a), 0, 1, static_cast<cudaStream_t>(cuda_stream), p); };
-    a->gate_kind == 2 ? run(block_norm_kernel<T_, vec, n, true, threads>) : run(block_norm_kernel<T_, vec, n, false, threads>);
-  });
+  if (plan.use) {
+    const NormRingParams r = ring_params(ctx, a, p, plan);
+    pick_ring_kernel<false>(a, plan, y && a->post_norm && a->pre_norm, [&](auto type, auto vector, auto token, auto full, auto threads, auto per_sm) {
+      typedef decltype(type) T_;
+      const auto run = [&](auto kernel) {
+        attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem);
+        if (attribute == cudaSuccess) launch_after(kernel, dim3((unsigned)norm_blocks(a, plan.blocks)), plan.threads, plan.smem, 1, st, r);
+      };
+      run(block_norm_ring_kernel<T_, vector, token, full, threads, per_sm>);
+    });
+  } else {
+    pick_norm_kernel(a, v, [&](auto type, auto vec, auto n, auto threads) {
+      typedef decltype(type) T_;
+      const auto run = [&](auto kernel) { launch_after(kernel, dim3((unsigned)norm_blocks(a, 640 / norm_threads(a))), norm_threads(a), 0, 1, st, p); };
+      a->gate_kind == 2 ? run(block_norm_kernel<T_, vec, n, true, threads>) : run(block_norm_kernel<T_, vec, n, false, threads>);
+    });
+  }
+  if (attribute != cudaSuccess) return cuda_fail(ctx, attribute);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;
@@ -416,7 +932,7 @@ int slidedp_block_norm(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const
 
 size_t slidedp_block_norm_workspace(const slidedp_block_norm_args* a) {
   if (check_norm(a) != SLIDEDP_OK) return 0;
-  return (size_t)(norm_blocks(a) * 2 * a->hidden) * sizeof(float) + 16;
+  return (size_t)(norm_blocks(a, kMaxNormBlocks) * 2 * a->hidden) * sizeof(float) + 16;
 }
 
 int slidedp_block_norm_backward(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const slidedp_rows* x, const slidedp_rows* y,
@@ -469,17 +985,33 @@ int slidedp_block_norm_backward(slidedp_ctx* ctx, const slidedp_block_norm_args*
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const unsigned blocks = (unsigned)norm_blocks(a);
+  unsigned blocks = 0;
   if (T > 0) {
     const slidedp_rows wp = {const_cast<void*>(w_post), 0}, wq = {const_cast<void*>(w_pre), 0};
     const int v = vector_width(H, elem, {{x, elem}, {y, elem}, {gate, elem}, {dx_out, elem}, {dh_out, elem}, {dx, elem}, {dy, elem}, {dgate, elem},
                                          {&wp, elem}, {&wq, elem}});
+    const RingPlan plan = ring_plan(a, v * elem == 16, 1 + (y != nullptr) + (a->gate_kind == 2) + (dx_out != nullptr) + a->pre_norm, true);
+    cudaError_t attribute = cudaSuccess;
+    blocks = (unsigned)norm_blocks(a, plan.use ? plan.blocks : (int)(640 / norm_threads(a)));
     FAULT_POINT();
-    pick_norm_kernel(a, v, [&](auto type, auto vec, auto n, auto threads) {
-      typedef decltype(type) T_;
-      const auto run = [&](auto kernel) { launch_after(kernel, dim3(blocks), norm_threads(a), 0, 1, st, p); };
-      a->gate_kind == 2 ? run(block_norm_backward_kernel<T_, vec, n, true, threads>) : run(block_norm_backward_kernel<T_, vec, n, false, threads>);
-    });
+    if (plan.use) {
+      const NormRingParams r = ring_params(ctx, a, p, plan);
+      pick_ring_kernel<true>(a, plan, y && a->post_norm && a->pre_norm && dx_out, [&](auto type, auto vector, auto token, auto full, auto threads, auto per_sm) {
+        typedef decltype(type) T_;
+        const auto run = [&](auto kernel) {
+          attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem);
+          if (attribute == cudaSuccess) launch_after(kernel, dim3(blocks), plan.threads, plan.smem, 1, st, r);
+        };
+        run(block_norm_backward_ring_kernel<T_, vector, token, full, threads, per_sm>);
+      });
+    } else {
+      pick_norm_kernel(a, v, [&](auto type, auto vec, auto n, auto threads) {
+        typedef decltype(type) T_;
+        const auto run = [&](auto kernel) { launch_after(kernel, dim3(blocks), norm_threads(a), 0, 1, st, p); };
+        a->gate_kind == 2 ? run(block_norm_backward_kernel<T_, vec, n, true, threads>) : run(block_norm_backward_kernel<T_, vec, n, false, threads>);
+      });
+    }
+    if (attribute != cudaSuccess) return cuda_fail(ctx, attribute);
     ctx->launches += 1;
     CU_AFTER_LAUNCH();
   }
