@@ -11,6 +11,8 @@ namespace slidedp {
 
 constexpr int kPolicyThreads = 256;
 constexpr int kPolicyWarps = kPolicyThreads / 32;
+constexpr int kPolicyMaxCluster = 8;
+constexpr int kPolicyUnroll = 4;
 
 struct PolicyParams {
   const void* z;
@@ -20,146 +22,478 @@ struct PolicyParams {
   const float* saved_logp;
   float *loss, *logp;
   int64_t rows, vocab, z_stride, dz_stride;
+  int64_t chunks_per_block;  // 16-byte chunks of a row that one block of its cluster takes
+  int* error;                // pinned host word that a wait which runs out sets
+  uint32_t polls;            // and how long it polls
   float inv_tau;
   double low, high, kl, inv_tau64;
 };
-
-// What a row's log-probability makes of it: its loss, and the factor f of dz = f (onehot - p). In FP64: the ratio is compared
-// with the edges of the clipped range, and one thread per row does it.
-struct RowTerms {
-  double loss;
-  float f;
-};
-__device__ __forceinline__ RowTerms row_terms(const PolicyParams& p, int64_t r, double logp) {
-  double loss = 0.0, slope = 0.0;
-  const double a = p.advantage ? (double)p.advantage[r] : 0.0;
-  if (a != 0.0) {
-    const double ratio = p.old_logp ? exp(logp - (double)p.old_logp[r]) : 1.0;
-    const bool inside = a > 0.0 ? ratio <= p.high : ratio >= p.low;
-    const double clipped = ratio > p.high ? p.high : ratio < p.low ? p.low : ratio;
-    loss = -(inside || ratio != ratio || a != a ? ratio : clipped) * a;
-    if (inside || ratio != ratio || a != a) slope = -a * ratio;
-  }
-  if (p.ref_logp) {
-    const double k = (double)p.ref_logp[r] - logp, e = exp(k);
-    loss += p.kl * (e - k - 1.0);
-    slope += p.kl * (1.0 - e);
-  }
-  const double g = p.row_grad ? (double)p.row_grad[r] : 1.0;
-  return RowTerms{loss, g == 0.0 ? 0.0f : (float)(g * slope * p.inv_tau64)};
-}
 
 __device__ __forceinline__ int row_label(const PolicyParams& p, int64_t r) {
   const int y = p.labels[r];
   return y >= 0 && y < p.vocab ? y : -1;
 }
 
-struct PolicyShared {
-  SoftSum warp[kPolicyWarps];
-  double loss, logp;
-  float f;
-};
-
-// Gradient of a chunk of a row: f (onehot - p) with p = exp2(k (z - base) + offset); nothing outside the row is written.
+// Gradient of a chunk of a row: f (onehot - p) with p = exp2(k (z - base) + offset); differences before they are scaled, so that logits
+// far from zero cost no digits. Nothing outside the row is written.
 struct PolicyGrad {
   float k, base, offset, f, at_label;
   int label;
 };
 template <typename T>
-__device__ __forceinline__ void policy_chunk(const Row<T>& row, T* dz, int64_t c, uint4 a, const PolicyGrad& g) {
+__device__ __forceinline__ void policy_values(uint4 a, const PolicyGrad& g, float* out) {
   constexpr int P = Logit<T>::kPer;
   uint64_t v[P / 2];
-  float out[P];
   Logit<T>::unpack(a, v);
-  const uint64_t minus = pair(-g.base, -g.base);
+  const uint64_t minus = pair(-g.base, -g.base), factor = pair(-g.f, -g.f);
 #pragma unroll
-  for (int e = 0; e < P / 2; ++e) {
-    float lo, hi;
-    split(fma2(add2(v[e], minus), pair(g.k, g.k), pair(g.offset, g.offset)), &lo, &hi);
-    out[2 * e] = -g.f * exp2_approx(lo);
-    out[2 * e + 1] = -g.f * exp2_approx(hi);
-  }
+  for (int e = 0; e < P / 2; ++e)
+    split(mul2(exp2_pair(fma2(add2(v[e], minus), pair(g.k, g.k), pair(g.offset, g.offset))), factor), &out[2 * e], &out[2 * e + 1]);
+}
+// The label is the chunk's value number `at`, if that is one of them.
+template <typename T>
+__device__ __forceinline__ void put_label(float* out, int64_t at, float v) {
+#pragma unroll
+  for (int e = 0; e < Logit<T>::kPer; ++e) out[e] = at == e ? v : out[e];
+}
+// Value by value: partial chunks, and rows whose gradient lies on another address grid.
+template <typename T>
+__device__ __forceinline__ void store_chunk(const Row<T>& row, T* dz, int64_t c, const float* out) {
   const int64_t first = row.first(c);
-  if (g.label >= first && g.label < first + P) out[g.label - first] = g.at_label;
-  const bool same_grid = ((reinterpret_cast<uintptr_t>(dz) ^ reinterpret_cast<uintptr_t>(row.z)) & 15u) == 0;
-  if (same_grid && first >= 0 && first + P <= row.vocab) {
-    st_stream(dz + first, Logit<T>::pack(out));
-  } else {
 #pragma unroll
-    for (int e = 0; e < P; ++e)
-      if (first + e >= 0 && first + e < row.vocab) Logit<T>::store(dz + first + e, out[e]);
+  for (int e = 0; e < Logit<T>::kPer; ++e)
+    if (first + e >= 0 && first + e < row.vocab) Logit<T>::store(dz + first + e, out[e]);
+}
+template <typename T>
+__device__ __forceinline__ void policy_chunk(const Row<T>& row, T* dz, bool same_grid, int64_t c, uint4 a, const PolicyGrad& g) {
+  float out[Logit<T>::kPer];
+  policy_values<T>(a, g, out);
+  const int64_t at = g.label - row.first(c);
+  if (at >= 0 && at < Logit<T>::kPer) put_label<T>(out, at, g.at_label);
+  if (same_grid && row.whole(c)) st_stream(dz + row.first(c), Logit<T>::pack(out));
+  else store_chunk<T>(row, dz, c, out);
+}
+template <typename T>
+__device__ __forceinline__ void zero_chunks(const Row<T>& row, T* dz, bool same_grid, int64_t from, int64_t to, int first, int step) {
+  const float zeros[Logit<T>::kPer] = {};
+  for (int64_t c = from + first; c < to; c += step) {
+    if (same_grid && row.whole(c)) st_stream(dz + row.first(c), make_uint4(0, 0, 0, 0));
+    else store_chunk<T>(row, dz, c, zeros);
+  }
+}
+template <typename T>
+__device__ __forceinline__ bool on_same_grid(const T* a, const T* b) {
+  return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
+}
+
+// What the gradient needs of a row, from its maximum (or any shift) and its sum; and its loss. One warp: the exponentials that hang on the
+// log-probability are taken by three lanes at once. In FP64: the ratio is compared with the edges of the clipped range.
+struct RowResult {
+  float offset, f, at_label;
+};
+__device__ __forceinline__ RowResult finish_row(const PolicyParams& p, int64_t r, double logp, double log_sum, bool write) {
+  const int lane = threadIdx.x % 32;
+  const double a = p.advantage ? (double)p.advantage[r] : 0.0, g = p.row_grad ? (double)p.row_grad[r] : 1.0;
+  const double k = p.ref_logp ? (double)p.ref_logp[r] - logp : 0.0;
+  const double e = exp(lane == 0 ? (p.old_logp && a != 0.0 ? logp - (double)p.old_logp[r] : 0.0) : lane == 1 ? k : logp);
+  const double ratio = __shfl_sync(0xffffffffu, e, 0), to_ref = __shfl_sync(0xffffffffu, e, 1), prob = __shfl_sync(0xffffffffu, e, 2);
+  double loss = 0.0, slope = 0.0;
+  if (a != 0.0) {
+    const bool inside = !(a > 0.0 ? ratio > p.high : ratio < p.low) || a != a;
+    loss = -(inside ? ratio : a > 0.0 ? p.high : p.low) * a;
+    if (inside) slope = -a * ratio;
+  }
+  if (p.ref_logp) {
+    loss += p.kl * (to_ref - k - 1.0);
+    slope += p.kl * (1.0 - to_ref);
+  }
+  if (write && lane == 0) {
+    if (p.loss) p.loss[r] = (float)loss;
+    p.logp[r] = (float)logp;
+  }
+  RowResult t;
+  t.f = g == 0.0 ? 0.0f : (float)(g * slope * p.inv_tau64);
+  t.at_label = t.f * (float)(1.0 - prob);
+  t.offset = (float)(-log_sum * 1.4426950408889634);
+  return t;
+}
+
+// ---- a block, or a cluster of them, per row ----------------------------------------------------------------
+
+struct PolicyShared {
+  SoftSum warp[kPolicyWarps];
+  alignas(8) float2 part[kPolicyMaxCluster];   // maximum and sum of each block of the cluster
+  RowResult row;
+};
+
+// kForward: log-probability and loss; kGradient: the gradient, without kForward from the saved log-probability. The blocks of a cluster
+// share a row's chunks, and exchange their sums through distributed shared memory.
+template <typename T, bool kForward, bool kGradient>
+__global__ void __launch_bounds__(kPolicyThreads) policy_row_kernel(const __grid_constant__ PolicyParams p, int cluster) {
+  start_after_previous_kernel();
+  __shared__ PolicyShared sh;
+  const int64_t r = blockIdx.x / cluster;
+  const int rank = blockIdx.x % cluster;
+  const T* z = static_cast<const T*>(p.z) + r * p.z_stride;
+  T* dz = static_cast<T*>(p.dz) + r * p.dz_stride;
+  const Row<T> row(z, p.vocab);
+  const int64_t chunks = (p.vocab + row.head + Logit<T>::kPer - 1) / Logit<T>::kPer;
+  const int64_t from = rank * p.chunks_per_block < chunks ? rank * p.chunks_per_block : chunks;
+  const int64_t to = from + p.chunks_per_block < chunks ? from + p.chunks_per_block : chunks;
+  const int label = row_label(p, r);
+  const bool same_grid = on_same_grid<T>(z, dz);
+  if (label < 0) {      // all blocks of the cluster alike
+    if (kForward && rank == 0 && threadIdx.x == 0) {
+      if (p.loss) p.loss[r] = 0.0f;
+      p.logp[r] = 0.0f;
+    }
+    if (kGradient) zero_chunks<T>(row, dz, same_grid, from, to, threadIdx.x, kPolicyThreads);
+    return;
+  }
+  const float at = Logit<T>::load(z + label);
+  PolicyGrad g;
+  g.k = p.inv_tau * kLog2e;
+  g.label = label;
+  g.base = at;
+  constexpr int U = kPolicyUnroll;
+  if (kForward) {
+    SoftSum mine = {-INFINITY, 0.0f, 0.0f};
+    for (int64_t c = from + threadIdx.x; c < to; c += kPolicyThreads * U) {
+      uint4 a[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t i = c + u * kPolicyThreads;
+        a[u] = Logit<T>::lowest();
+        if (i < to) a[u] = kGradient && row.whole(i) ? *reinterpret_cast<const uint4*>(z + row.first(i)) : row.load(i);
+      }
+      accumulate<T, false, U>(mine, a, g.k, g.k);
+    }
+    mine = join_lanes<32, false>(mine, g.k, g.k);
+    if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32] = mine;
+    __syncthreads();
+    mine = join_lanes<kPolicyWarps, false>(sh.warp[threadIdx.x % kPolicyWarps], g.k, g.k);
+    if (cluster > 1) {
+      if ((int)threadIdx.x < cluster && (kGradient || threadIdx.x == 0)) {
+        const uint32_t there = peer_addr(smem_addr(&sh.part[rank]), threadIdx.x);
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(mine.m), "f"(mine.s0) : "memory");
+      }
+      cluster_sync();
+      const int i = threadIdx.x % kPolicyMaxCluster;
+      mine = SoftSum{-INFINITY, 0.0f, 0.0f};
+      if (i < cluster && (kGradient || rank == 0)) mine.m = sh.part[i].x, mine.s0 = sh.part[i].y;
+      mine = join_lanes<kPolicyMaxCluster, false>(mine, g.k, g.k);
+    }
+    g.base = finite_shift(mine.m);
+    if ((kGradient || rank == 0) && threadIdx.x < 32) {
+      const double log_sum = log((double)mine.s0);
+      const RowResult t = finish_row(p, r, ((double)at - (double)g.base) * p.inv_tau64 - log_sum, log_sum, rank == 0);
+      if (threadIdx.x == 0) sh.row = t;
+    }
+  } else if (threadIdx.x < 32) {
+    const double logp = p.saved_logp[r];
+    const RowResult t = finish_row(p, r, logp, -logp, false);
+    if (threadIdx.x == 0) sh.row = t;
+  }
+  if (kGradient) {
+    // without kForward nothing has been read of the row but `at`, which no block may change before all have it
+    if (!kForward && cluster > 1) cluster_sync(); else __syncthreads();
+    g.f = sh.row.f;
+    g.offset = sh.row.offset;
+    g.at_label = sh.row.at_label;
+    if (g.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, from, to, threadIdx.x, kPolicyThreads);
+    for (int64_t c = from + threadIdx.x; c < to; c += kPolicyThreads * U) {
+      uint4 a[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c + u * kPolicyThreads < to) a[u] = row.load(c + u * kPolicyThreads);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c + u * kPolicyThreads < to) policy_chunk<T>(row, dz, same_grid, c + u * kPolicyThreads, a[u], g);
+    }
   }
 }
 
-// A block per row. kForward: log-probability and loss; kGradient: the gradient, from the saved log-probability without kForward.
-template <typename T, bool kForward, bool kGradient>
-__global__ void __launch_bounds__(kPolicyThreads) policy_row_kernel(const __grid_constant__ PolicyParams p) {
+// Both for short rows: a block holds its row in registers, U chunks a thread.
+template <typename T, int U>
+__global__ void __launch_bounds__(kPolicyThreads) policy_held_kernel(const __grid_constant__ PolicyParams p) {
   start_after_previous_kernel();
   __shared__ PolicyShared sh;
   const int64_t r = blockIdx.x;
   const T* z = static_cast<const T*>(p.z) + r * p.z_stride;
   T* dz = static_cast<T*>(p.dz) + r * p.dz_stride;
   const Row<T> row(z, p.vocab);
-  const int64_t chunks = (p.vocab + row.head + Logit<T>::kPer - 1) / Logit<T>::kPer;
+  const int chunks = (int)((p.vocab + row.head + Logit<T>::kPer - 1) / Logit<T>::kPer);
   const int label = row_label(p, r);
-  const float at = label >= 0 ? Logit<T>::load(z + label) : 0.0f;
+  const bool same_grid = on_same_grid<T>(z, dz);
+  if (label < 0) {
+    if (threadIdx.x == 0) {
+      if (p.loss) p.loss[r] = 0.0f;
+      p.logp[r] = 0.0f;
+    }
+    return zero_chunks<T>(row, dz, same_grid, 0, chunks, threadIdx.x, kPolicyThreads);
+  }
+  const float at = Logit<T>::load(z + label);
   PolicyGrad g;
   g.k = p.inv_tau * kLog2e;
   g.label = label;
-  g.f = 0.0f;
-  if (kForward) {
-    if (label < 0) {
-      if (threadIdx.x == 0) {
-        if (p.loss) p.loss[r] = 0.0f;
-        p.logp[r] = 0.0f;
-      }
-    } else {
+  uint4 a[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int c = threadIdx.x + u * kPolicyThreads;
+    a[u] = c < chunks ? row.load(c) : Logit<T>::lowest();
+  }
+  SoftSum mine = {-INFINITY, 0.0f, 0.0f};
+  accumulate<T, false, U>(mine, a, g.k, g.k);
+  mine = join_lanes<32, false>(mine, g.k, g.k);
+  if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32] = mine;
+  __syncthreads();
+  mine = join_lanes<kPolicyWarps, false>(sh.warp[threadIdx.x % kPolicyWarps], g.k, g.k);
+  g.base = finite_shift(mine.m);
+  if (threadIdx.x < 32) {
+    const double log_sum = log((double)mine.s0);
+    const RowResult t = finish_row(p, r, ((double)at - (double)g.base) * p.inv_tau64 - log_sum, log_sum, true);
+    if (threadIdx.x == 0) sh.row = t;
+  }
+  __syncthreads();
+  g.f = sh.row.f;
+  g.offset = sh.row.offset;
+  g.at_label = sh.row.at_label;
+  if (g.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, 0, chunks, threadIdx.x, kPolicyThreads);
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (threadIdx.x + u * kPolicyThreads < chunks) policy_chunk<T>(row, dz, same_grid, threadIdx.x + u * kPolicyThreads, a[u], g);
+}
+
+// ---- rows in shared memory -----------------------------------------------------------------------------------
+// Both for long rows: blocks, or clusters that share a row, stay, one per SM. A producer copies slice after slice into a ring of
+// slots; the sums' warps go through a row as it comes, the gradient's warps follow one row behind them and give the slots back. So
+// the next rows are under way while a row's sums are exchanged and made into its loss, by a warp of its own, and every logit is
+// read once. A slice is at most as long as leaves part of the ring for the row after it.
+
+constexpr int kRingWarps = 8;                       // of each of the two groups
+constexpr int kRingGroup = kRingWarps * 32;
+constexpr int kRingThreads = 2 * kRingGroup + 64;   // and the producer's and the rows' warps
+constexpr int kSlotChunks = 1024;                   // 16 KB
+constexpr int kSlotUnroll = kSlotChunks / kRingGroup;
+constexpr int kSlots = 13;
+// Rows between the first and the last that any block of a cluster has to do with: a block's sums are at most kSlots rows before its
+// gradients, which wait for the other blocks' sums, which are at most kSlots rows before those blocks' gradients.
+constexpr int kRowSlots = 32;
+static_assert(kRowSlots > 2 * kSlots + 2, "rows that are still looked at would be overwritten");
+
+struct PolicyRing {
+  alignas(16) float4 part[kRowSlots][kPolicyMaxCluster];   // maximum, sum, the label's logit where it is known
+  alignas(16) float4 row[kRowSlots];                       // base, offset, factor, value at the label
+  alignas(16) SoftSum warp[2][kRingWarps];
+  uint64_t full[kSlots], empty[kSlots];
+  uint64_t summed[kRowSlots], known[kRowSlots];
+  uint32_t dead;
+};
+
+// One block's part of a row: chunks [lo, hi), of which [mid, mid + n) are whole.
+template <typename T>
+struct RingSlice {
+  Row<T> row;
+  int64_t lo, hi, mid;
+  int n;
+  __device__ __forceinline__ RingSlice(const PolicyParams& p, int64_t r, int rank) : row(static_cast<const T*>(p.z) + r * p.z_stride, p.vocab) {
+    const int64_t chunks = (p.vocab + row.head + Logit<T>::kPer - 1) / Logit<T>::kPer;
+    lo = rank * p.chunks_per_block;
+    hi = lo + p.chunks_per_block < chunks ? lo + p.chunks_per_block : chunks;
+    if (lo > hi) lo = hi;
+    mid = lo < hi && !row.whole(lo) ? lo + 1 : lo;
+    n = (int)((hi > mid && !row.whole(hi - 1) ? hi - 1 : hi) - mid);
+  }
+  // f(chunk) for the partial chunks, each by one thread of a group
+  template <typename F>
+  __device__ __forceinline__ void edges(int thread, F f) const {
+    if (thread == 32 && mid > lo) f(lo);
+    if (thread == 64 && mid + n < hi) f(hi - 1);
+  }
+};
+// The place in a ring of N that comes round: its index and the parity of its phase.
+template <int N>
+struct Place {
+  int i = 0;
+  uint32_t parity = 0;
+  __device__ __forceinline__ void next() {
+    if (++i == N) i = 0, parity ^= 1;
+  }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __grid_constant__ PolicyParams p, int cluster) {
+  extern __shared__ uint4 slots[];
+  __shared__ PolicyRing ring;
+  allow_next_kernel();
+  const int rank = blockIdx.x % cluster, first = blockIdx.x / cluster, step = gridDim.x / cluster;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(smem_addr(&ring.full[i]), 1);
+      mbar_init(smem_addr(&ring.empty[i]), kRingWarps);
+    }
+    for (int i = 0; i < kRowSlots; ++i) {
+      mbar_init(smem_addr(&ring.summed[i]), cluster);
+      mbar_init(smem_addr(&ring.known[i]), 1);
+    }
+    ring.dead = 0;
+    mbar_init_fence();
+  }
+  if (cluster > 1) cluster_sync(); else __syncthreads();
+  wait_for_previous_kernel();
+  const Waiter wait{&ring.dead, p.error, p.polls};
+  const float k = p.inv_tau * kLog2e;
+  Place<kSlots> slot;
+  Place<kRowSlots> at;
+  int next_label = first < p.rows ? row_label(p, first) : -1;
+  const auto label_of = [&](int64_t r) {      // the next row's is fetched ahead
+    const int y = next_label;
+    if (r + step < p.rows) next_label = row_label(p, r + step);
+    return y;
+  };
+  bool ok = true;
+  if (warp < kRingWarps) {                    // the sums
+    int turn = 0;
+    for (int64_t r = first; r < p.rows; r += step) {
+      const int label = label_of(r);
+      if (label < 0) continue;
+      const RingSlice<T> s(p, r, rank);
+      // read before any block may write this row's gradient to the same memory
+      float mark = 0.0f;
+      const int64_t label_chunk = (label + s.row.head) / Logit<T>::kPer;
+      const bool owner = label_chunk >= s.lo && label_chunk < s.hi;
+      if (threadIdx.x == 0 && owner) mark = Logit<T>::load(s.row.z + label);
       SoftSum mine = {-INFINITY, 0.0f, 0.0f};
-      for (int64_t c = threadIdx.x; c < chunks; c += kPolicyThreads) {
-        const uint4 a = row.load(c);
-        accumulate<T, false, 1>(mine, &a, g.k, g.k);
+      s.edges(threadIdx.x, [&](int64_t c) {
+        const uint4 a = s.row.load(c);
+        accumulate<T, false, 1>(mine, &a, k, k);
+      });
+      __syncwarp();
+      for (int i0 = 0; i0 < s.n; i0 += kSlotChunks, slot.next()) {
+        // after a wait that ran out no more of them, but this row's barrier, where all warps learn of it
+        if (ok) ok = __all_sync(0xffffffffu, wait(smem_addr(&ring.full[slot.i]), slot.parity));
+        uint4 a[kSlotUnroll];
+#pragma unroll
+        for (int u = 0; u < kSlotUnroll; ++u) {
+          const int i = threadIdx.x + u * kRingGroup;
+          a[u] = i0 + i < s.n ? slots[slot.i * kSlotChunks + i] : Logit<T>::lowest();
+        }
+        accumulate<T, false, kSlotUnroll>(mine, a, k, k);
       }
-      mine = join_lanes<32, false>(mine, g.k, g.k);
-      if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32] = mine;
-      __syncthreads();
-      mine = join_lanes<kPolicyWarps, false>(sh.warp[threadIdx.x % kPolicyWarps], g.k, g.k);
-      g.base = finite_shift(mine.m);
-      if (threadIdx.x == 0) {
-        const double logp = ((double)at - (double)g.base) * p.inv_tau64 - log((double)mine.s0);
-        const RowTerms t = row_terms(p, r, logp);
-        if (p.loss) p.loss[r] = (float)t.loss;
-        p.logp[r] = (float)logp;
-        sh.logp = logp;
-        sh.f = t.f;
+      mine = join_lanes<32, false>(mine, k, k);
+      if (lane == 0) ring.warp[turn][warp] = mine;
+      uint32_t all_ok;
+      asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
+                   : "=r"(all_ok)
+                   : "r"((uint32_t)ok), "n"(kRingGroup)
+                   : "memory");
+      if (!all_ok) break;                     // all of them, at the same barrier
+      if (warp == 0) {
+        mine = join_lanes<kRingWarps, false>(ring.warp[turn][lane % kRingWarps], k, k);
+        mark = __shfl_sync(0xffffffffu, mark, 0);
+        if (lane < cluster) {
+          const uint32_t to = peer_addr(smem_addr(&ring.part[at.i][rank]), lane);
+          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(mine.m), "f"(mine.s0), "f"(mark), "f"(0.0f) : "memory");
+          mbar_arrive_cluster(peer_addr(smem_addr(&ring.summed[at.i]), lane));
+        }
       }
-      g.offset = -log2f(mine.s0);
+      turn ^= 1;
+      at.next();
     }
-  } else if (label >= 0) {
-    g.base = at;
-    if (threadIdx.x == 0) {
-      const double logp = p.saved_logp[r];
-      sh.logp = logp;
-      sh.f = row_terms(p, r, logp).f;
+  } else if (warp < 2 * kRingWarps) {         // the gradients
+    const int thread = threadIdx.x - kRingGroup;
+    for (int64_t r = first; ok && r < p.rows; r += step) {
+      const int label = label_of(r);
+      const RingSlice<T> s(p, r, rank);
+      T* dz = static_cast<T*>(p.dz) + r * p.dz_stride;
+      const bool same_grid = on_same_grid<T>(s.row.z, dz);
+      if (label < 0) {
+        zero_chunks<T>(s.row, dz, same_grid, s.lo, s.hi, thread, kRingGroup);
+        continue;
+      }
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ring.known[at.i]), at.parity));
+      if (!ok) break;
+      const float4 t = ring.row[at.i];
+      const PolicyGrad g = {k, t.x, t.y, t.z, t.w, label};
+      at.next();
+      const bool zero = g.f == 0.0f;
+      if (zero) zero_chunks<T>(s.row, dz, same_grid, s.lo, s.hi, thread, kRingGroup);
+      else s.edges(thread, [&](int64_t c) { policy_chunk<T>(s.row, dz, same_grid, c, s.row.load(c), g); });
+      const int64_t hot = (label + s.row.head) / Logit<T>::kPer - s.mid;       // the label's chunk and its place there
+      const int hot_at = (label + s.row.head) % Logit<T>::kPer;
+      T* out = dz + s.row.first(s.mid);
+      for (int i0 = 0; i0 < s.n; i0 += kSlotChunks, slot.next()) {
+        // it is: its sums are known
+        ok = __all_sync(0xffffffffu, ok && wait(smem_addr(&ring.full[slot.i]), slot.parity));
+        if (!ok) break;
+        uint4 a[kSlotUnroll];
+#pragma unroll
+        for (int u = 0; u < kSlotUnroll; ++u) a[u] = slots[slot.i * kSlotChunks + thread + u * kRingGroup];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&ring.empty[slot.i]));
+        if (zero) continue;
+#pragma unroll
+        for (int u = 0; u < kSlotUnroll; ++u) {
+          const int i = i0 + thread + u * kRingGroup;
+          if (i >= s.n) continue;
+          float v[Logit<T>::kPer];
+          policy_values<T>(a[u], g, v);
+          if (i == hot) put_label<T>(v, hot_at, g.at_label);
+          if (same_grid) st_stream(out + (int64_t)i * Logit<T>::kPer, Logit<T>::pack(v));
+          else store_chunk<T>(s.row, dz, s.mid + i, v);
+        }
+      }
     }
-    g.offset = p.saved_logp[r] * kLog2e;
+  } else if (warp == 2 * kRingWarps) {        // the copies
+    int64_t issued = 0;
+    if (lane == 0) {
+      for (int64_t r = first; ok && r < p.rows; r += step) {
+        if (label_of(r) < 0) continue;
+        const RingSlice<T> s(p, r, rank);
+        const uint4* from = reinterpret_cast<const uint4*>(s.row.z + s.row.first(s.mid));
+        for (int i0 = 0; ok && i0 < s.n; i0 += kSlotChunks, slot.next(), ++issued) {
+          if (issued >= kSlots) ok = wait(smem_addr(&ring.empty[slot.i]), slot.parity ^ 1);
+          if (!ok) break;
+          const uint32_t bytes = (uint32_t)min(s.n - i0, kSlotChunks) * 16, bar = smem_addr(&ring.full[slot.i]);
+          mbar_expect(bar, bytes);
+          bulk_load(smem_addr(&slots[slot.i * kSlotChunks]), from + i0, bytes, bar);
+        }
+      }
+      // none may be left under way, whoever gave up
+      for (int64_t i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i) drain(smem_addr(&ring.full[i % kSlots]), i / kSlots & 1);
+    }
+  } else {                                    // the rows: their sums to what the gradient needs
+    for (int64_t r = first; ok && r < p.rows; r += step) {
+      const int label = label_of(r);
+      if (label < 0) {
+        if (rank == 0 && lane == 0) {
+          if (p.loss) p.loss[r] = 0.0f;
+          p.logp[r] = 0.0f;
+        }
+        continue;
+      }
+      ok = __all_sync(0xffffffffu, wait.wait<true>(smem_addr(&ring.summed[at.i]), at.parity));
+      if (!ok) break;
+      SoftSum all = {-INFINITY, 0.0f, 0.0f};
+      const float4 v = lane % kPolicyMaxCluster < cluster ? ring.part[at.i][lane % kPolicyMaxCluster] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+      all.m = v.x;
+      all.s0 = v.y;
+      all = join_lanes<kPolicyMaxCluster, false>(all, k, k);
+      const RingSlice<T> s(p, r, rank);
+      const int owner = (int)((label + s.row.head) / Logit<T>::kPer / p.chunks_per_block);
+      const float mark = __shfl_sync(0xffffffffu, v.z, owner), base = finite_shift(all.m);
+      const double log_sum = log((double)all.s0);
+      const RowResult t = finish_row(p, r, ((double)mark - (double)base) * p.inv_tau64 - log_sum, log_sum, rank == 0);
+      if (lane == 0) {
+        ring.row[at.i] = make_float4(base, t.offset, t.f, t.at_label);
+        mbar_arrive(smem_addr(&ring.known[at.i]));
+      }
+      at.next();
+    }
   }
-  if (kGradient) {
-    __syncthreads();
-    if (label >= 0) {
-      g.f = sh.f;
-      g.at_label = g.f * -(float)expm1(sh.logp);
-    }
-    if (g.f == 0.0f) {
-      for (int64_t c = threadIdx.x; c < chunks; c += kPolicyThreads) {
-        g.label = -1;
-        g.k = g.base = 0.0f;
-        g.offset = -INFINITY;
-        policy_chunk<T>(row, dz, c, make_uint4(0, 0, 0, 0), g);
-      }
-    } else {
-      for (int64_t c = threadIdx.x; c < chunks; c += kPolicyThreads) policy_chunk<T>(row, dz, c, row.load(c), g);
-    }
-  }
+  __syncwarp();
+  if (cluster > 1) cluster_sync();            // nobody leaves while sums are still stored to it
 }
 
 }  // namespace slidedp
@@ -169,7 +503,41 @@ using namespace slidedp::host;
 
 namespace {
 
+constexpr int kSms = 148;
+constexpr int64_t kHeldChunks = 8 * kPolicyThreads;          // rows up to 32 KB are held in registers
+constexpr int64_t kMaxSliceChunks = 8 * kSlotChunks + 512;   // of the ring's 13 slots
+constexpr int64_t kMinSliceChunks = 512;
+constexpr int64_t kEnoughBlocks = kSms * 4;
+
 enum PolicyMode { kPolicyForward, kPolicyBackward, kPolicyStep };
+
+// How many clusters of the ring's kernel run at once: blocks that stay must all be of the first round. Asked once per type and size.
+template <typename K>
+cudaError_t resident_clusters(K kernel, bool f32, int cluster, size_t smem, int* out) {
+  static std::atomic<int> known[2][kPolicyMaxCluster + 1];
+  *out = known[f32][cluster];
+  if (*out > 0) return cudaSuccess;
+  if (cluster == 1) {
+    *out = kSms;
+  } else {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = cluster;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kSms / cluster * cluster);
+    cfg.blockDim = dim3(kRingThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(out, kernel, &cfg);
+    if (e != cudaSuccess) return e;
+    if (*out < 1) return cudaErrorLaunchOutOfResources;
+    if (*out > kSms / cluster) *out = kSms / cluster;
+  }
+  known[f32][cluster] = *out;
+  return cudaSuccess;
+}
 
 int check_policy(const slidedp_policy_args* a) {
   if (!a || a->rows < 0 || a->rows > kMaxTokens || a->vocab < 1 || a->vocab > (1ll << 30) || (a->dtype != SLIDEDP_BF16 && a->dtype != SLIDEDP_F32) ||
@@ -216,12 +584,44 @@ int run_policy(slidedp_ctx* ctx, const slidedp_policy_args* a, PolicyMode mode, 
   if (rc != SLIDEDP_OK) return rc;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());
-  FAULT_POINT();
-  const auto run = [&](auto kernel) { launch_after(kernel, dim3((unsigned)a->rows), kPolicyThreads, 0, 1, st, p); };
+  cudaStream_t stream = st;
+  const int64_t chunks = (a->vocab * elem + 15) / 16 + 1;   // an unaligned row touches one more
+  p.error = ctx->kernel_error;
+  p.polls = ctx->wait_polls;
   const bool f32 = a->dtype == SLIDEDP_F32;
-  if (mode == kPolicyForward) f32 ? run(policy_row_kernel<float, true, false>) : run(policy_row_kernel<uint16_t, true, false>);
-  else if (mode == kPolicyBackward) f32 ? run(policy_row_kernel<float, false, true>) : run(policy_row_kernel<uint16_t, false, true>);
-  else f32 ? run(policy_row_kernel<float, true, true>) : run(policy_row_kernel<uint16_t, true, true>);
+  FAULT_POINT();
+  cudaError_t failed = cudaSuccess;
+  if (mode == kPolicyStep && chunks <= kHeldChunks) {
+    const auto run = [&](auto kernel) { launch_after(kernel, dim3((unsigned)a->rows), kPolicyThreads, 0, 1, stream, p); };
+    const auto held = [&](auto type) {
+      typedef decltype(type) T;
+      chunks <= 2 * kPolicyThreads ? run(policy_held_kernel<T, 2>) : chunks <= 4 * kPolicyThreads ? run(policy_held_kernel<T, 4>) : run(policy_held_kernel<T, 8>);
+    };
+    f32 ? held(float()) : held(uint16_t());
+  } else if (mode == kPolicyStep && chunks <= kPolicyMaxCluster * kMaxSliceChunks) {
+    int cluster = 1;
+    while (cluster < kPolicyMaxCluster && (chunks > cluster * kMaxSliceChunks || (a->rows * cluster < kSms && chunks > cluster * kSlotChunks))) cluster *= 2;
+    p.chunks_per_block = (chunks + cluster - 1) / cluster;
+    const size_t smem = kSlots * kSlotChunks * 16;
+    const auto run = [&](auto kernel) {
+      failed = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      int most = 0;
+      if (failed == cudaSuccess) failed = resident_clusters(kernel, f32, cluster, smem, &most);
+      const int64_t clusters = a->rows < most ? a->rows : most;
+      if (failed == cudaSuccess) launch_after(kernel, dim3((unsigned)(clusters * cluster)), kRingThreads, smem, cluster, stream, p, cluster);
+    };
+    f32 ? run(policy_ring_kernel<float>) : run(policy_ring_kernel<uint16_t>);
+  } else {
+    int cluster = 1;
+    while (cluster < kPolicyMaxCluster && a->rows * cluster < kEnoughBlocks && chunks >= 2 * kMinSliceChunks * cluster) cluster *= 2;
+    p.chunks_per_block = (chunks + cluster - 1) / cluster;
+    if (a->rows * cluster > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
+    const auto run = [&](auto kernel) { launch_after(kernel, dim3((unsigned)(a->rows * cluster)), kPolicyThreads, 0, cluster, stream, p, cluster); };
+    if (mode == kPolicyForward) f32 ? run(policy_row_kernel<float, true, false>) : run(policy_row_kernel<uint16_t, true, false>);
+    else if (mode == kPolicyBackward) f32 ? run(policy_row_kernel<float, false, true>) : run(policy_row_kernel<uint16_t, false, true>);
+    else f32 ? run(policy_row_kernel<float, true, true>) : run(policy_row_kernel<uint16_t, true, true>);
+  }
+  if (failed != cudaSuccess) return cuda_fail(ctx, failed);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   return SLIDEDP_OK;
