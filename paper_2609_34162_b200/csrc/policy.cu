@@ -34,10 +34,101 @@ __device__ __forceinline__ int row_label(const PolicyParams& p, int64_t r) {
   return y >= 0 && y < p.vocab ? y : -1;
 }
 
-// Gradient of a chunk of a row: f (onehot - p) with p = exp2(k (z - base) + offset); differences before they are scaled, so that logits
-// far from zero cost no digits. Nothing outside the row is written.
+// ---- a row's sum and its probabilities ------------------------------------------------------------------------
+// With k = log2 e / temperature in FP32 and a shift c in FP32, exp2(fma(z, k, -c)) has one rounding, of the exponent: logits far from
+// zero cost no digits as long as the same c goes into what is made of the sum. c = k m, rounded, for the greatest logit m so far.
+// Far from zero, where that rounding is no longer small, a logit's difference from m is taken first and then scaled.
+
+struct PolicySum {
+  float m, s;
+};
+// rounded on its own, wherever it is used: no part of a fused multiply-add
+__device__ __forceinline__ float shift_of(float m, float k) { return m == -INFINITY ? 0.0f : __fmul_rn(m, k); }
+__device__ __forceinline__ bool is_far(float c) { return !(fabsf(c) < 1048576.0f); }
+// What the shift of a sum lacks of k m.
+__device__ __forceinline__ float shift_error(float m, float k) {
+  const float c = shift_of(m, k);
+  return is_far(c) ? 0.0f : -fmaf(m, k, -c);
+}
+// The factor that takes a sum shifted for m to one shifted for the greater `to`.
+__device__ __forceinline__ float rescale(float m, float to, float k) {
+  if (m == to) return 1.0f;
+  return m == -INFINITY ? 0.0f : exp2_approx((m - to) * k + (shift_error(m, k) - shift_error(to, k)));
+}
+template <int LANES>
+__device__ __forceinline__ PolicySum join_sums(PolicySum a, float k) {
+  float m = a.m;   // never NaN: a NaN logit shows in the sum
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  a.s *= rescale(a.m, m, k);
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+  a.m = m;
+  return a;
+}
+template <typename T, int N>
+__device__ __forceinline__ float largest_of(const uint4* a) {
+  if constexpr (sizeof(T) == 2) {
+    uint4 m = a[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) {
+      m.x = Logit<T>::max2(m.x, a[i].x); m.y = Logit<T>::max2(m.y, a[i].y);
+      m.z = Logit<T>::max2(m.z, a[i].z); m.w = Logit<T>::max2(m.w, a[i].w);
+    }
+    return Logit<T>::largest(m);
+  } else {
+    float m = Logit<T>::largest(a[0]);
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = fmaxf(m, Logit<T>::largest(a[i]));
+    return m;
+  }
+}
+// Adds N chunks to a thread's sum.
+template <typename T, int N>
+__device__ __forceinline__ void add_chunks(PolicySum& mine, const uint4* a, float k) {
+  constexpr int P = Logit<T>::kPer;
+  const float top = fmaxf(mine.m, largest_of<T, N>(a));
+  mine.s *= rescale(mine.m, top, k);
+  mine.m = top;
+  const float c = shift_of(top, k);
+  uint64_t s0 = 0, s1 = 0;
+  const uint64_t kk = pair(k, k), minus = pair(-c, -c);
+  if (!is_far(c)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint64_t v[P / 2];
+      Logit<T>::unpack(a[i], v);
+#pragma unroll
+      for (int e = 0; e < P / 2; ++e) {
+        const uint64_t x = exp2_pair(fma2(v[e], kk, minus));
+        if (e % 2) s1 = add2(s1, x); else s0 = add2(s0, x);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint64_t v[P / 2];
+      Logit<T>::unpack(a[i], v);
+#pragma unroll
+      for (int e = 0; e < P / 2; ++e) {
+        s0 = add2(s0, exp2_pair(mul2(add2(v[e], pair(-top, -top)), kk)));
+      }
+    }
+  }
+  float x, y;
+  split(add2(s0, s1), &x, &y);
+  mine.s += x + y;
+}
+
+// What a row's gradient f (onehot - p) needs: p = exp2(k z - shift) * scale, or far from zero exp2(k (z - shift) + offset) * scale; `factor`
+// is -f scale. A gradient that is zero throughout is told by f.
+struct RowTerms {
+  float shift, offset, factor, at_label, f;
+  int far;
+};
 struct PolicyGrad {
-  float k, base, offset, f, at_label;
+  float k;
+  RowTerms t;
   int label;
 };
 template <typename T>
@@ -45,10 +136,18 @@ __device__ __forceinline__ void policy_values(uint4 a, const PolicyGrad& g, floa
   constexpr int P = Logit<T>::kPer;
   uint64_t v[P / 2];
   Logit<T>::unpack(a, v);
-  const uint64_t minus = pair(-g.base, -g.base), factor = pair(-g.f, -g.f);
+  const uint64_t factor = pair(g.t.factor, g.t.factor), kk = pair(g.k, g.k), minus = pair(-g.t.shift, -g.t.shift);
+#pragma unroll
+  for (int e = 0; e < P / 2; ++e) split(mul2(exp2_pair(fma2(v[e], kk, minus)), factor), &out[2 * e], &out[2 * e + 1]);
+}
+template <typename T>
+__device__ __forceinline__ void policy_values_far(uint4 a, float k, const RowTerms& t, float* out) {
+  constexpr int P = Logit<T>::kPer;
+  uint64_t v[P / 2];
+  Logit<T>::unpack(a, v);
 #pragma unroll
   for (int e = 0; e < P / 2; ++e)
-    split(mul2(exp2_pair(fma2(add2(v[e], minus), pair(g.k, g.k), pair(g.offset, g.offset))), factor), &out[2 * e], &out[2 * e + 1]);
+    split(mul2(exp2_pair(fma2(add2(v[e], pair(-t.shift, -t.shift)), pair(k, k), pair(t.offset, t.offset))), pair(t.factor, t.factor)), &out[2 * e], &out[2 * e + 1]);
 }
 // The label is the chunk's value number `at`, if that is one of them.
 template <typename T>
@@ -67,9 +166,10 @@ __device__ __forceinline__ void store_chunk(const Row<T>& row, T* dz, int64_t c,
 template <typename T>
 __device__ __forceinline__ void policy_chunk(const Row<T>& row, T* dz, bool same_grid, int64_t c, uint4 a, const PolicyGrad& g) {
   float out[Logit<T>::kPer];
-  policy_values<T>(a, g, out);
+  if (g.t.far) policy_values_far<T>(a, g.k, g.t, out);
+  else policy_values<T>(a, g, out);
   const int64_t at = g.label - row.first(c);
-  if (at >= 0 && at < Logit<T>::kPer) put_label<T>(out, at, g.at_label);
+  if (at >= 0 && at < Logit<T>::kPer) put_label<T>(out, at, g.t.at_label);
   if (same_grid && row.whole(c)) st_stream(dz + row.first(c), Logit<T>::pack(out));
   else store_chunk<T>(row, dz, c, out);
 }
@@ -86,12 +186,9 @@ __device__ __forceinline__ bool on_same_grid(const T* a, const T* b) {
   return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
 }
 
-// What the gradient needs of a row, from its maximum (or any shift) and its sum; and its loss. One warp: the exponentials that hang on the
-// log-probability are taken by three lanes at once. In FP64: the ratio is compared with the edges of the clipped range.
-struct RowResult {
-  float offset, f, at_label;
-};
-__device__ __forceinline__ RowResult finish_row(const PolicyParams& p, int64_t r, double logp, double log_sum, bool write) {
+// A row's loss, and the rest of its terms, by one warp: the exponentials that hang on the log-probability are taken by three lanes at
+// once. In FP64: the ratio is compared with the edges of the clipped range.
+__device__ __forceinline__ void finish_row(const PolicyParams& p, int64_t r, double logp, double scale, bool write, RowTerms* t) {
   const int lane = threadIdx.x % 32;
   const double a = p.advantage ? (double)p.advantage[r] : 0.0, g = p.row_grad ? (double)p.row_grad[r] : 1.0;
   const double k = p.ref_logp ? (double)p.ref_logp[r] - logp : 0.0;
@@ -111,19 +208,40 @@ __device__ __forceinline__ RowResult finish_row(const PolicyParams& p, int64_t r
     if (p.loss) p.loss[r] = (float)loss;
     p.logp[r] = (float)logp;
   }
-  RowResult t;
-  t.f = g == 0.0 ? 0.0f : (float)(g * slope * p.inv_tau64);
-  t.at_label = t.f * (float)(1.0 - prob);
-  t.offset = (float)(-log_sum * 1.4426950408889634);
+  const double f = g == 0.0 ? 0.0 : g * slope * p.inv_tau64;
+  t->factor = (float)(-f * scale);
+  t->at_label = (float)(f * (1.0 - prob));
+  t->f = (float)f;
+}
+// From the sum, and the label's logit.
+__device__ __forceinline__ RowTerms finish_sum(const PolicyParams& p, int64_t r, PolicySum all, float mark, float k, bool write) {
+  const float c = shift_of(all.m, k);
+  const double log_sum = log((double)all.s);
+  RowTerms t;
+  t.far = is_far(c);
+  t.shift = t.far ? all.m : c;
+  t.offset = 0.0f;
+  const double logp = t.far ? ((double)mark - (double)all.m) * p.inv_tau64 : ((double)k * (double)mark - (double)c) * 0.6931471805599453;
+  finish_row(p, r, logp - log_sum, 1.0 / (double)all.s, write, &t);
+  return t;
+}
+// From the saved log-probability: the shift is the row's log2 sum, or far from zero the label's logit.
+__device__ __forceinline__ RowTerms finish_saved(const PolicyParams& p, int64_t r, float mark, float k) {
+  const double logp = p.saved_logp[r], log2_p = logp * 1.4426950408889634, exact = (double)k * (double)mark - log2_p;
+  RowTerms t;
+  t.far = is_far((float)exact) || is_far(mark * k);
+  t.shift = t.far ? mark : (float)exact;
+  t.offset = (float)log2_p;
+  finish_row(p, r, logp, t.far ? 1.0 : exp2((double)t.shift - exact), false, &t);
   return t;
 }
 
 // ---- a block, or a cluster of them, per row ----------------------------------------------------------------
 
 struct PolicyShared {
-  SoftSum warp[kPolicyWarps];
+  RowTerms row;
+  PolicySum warp[kPolicyWarps];
   alignas(8) float2 part[kPolicyMaxCluster];   // maximum and sum of each block of the cluster
-  RowResult row;
 };
 
 // kForward: log-probability and loss; kGradient: the gradient, without kForward from the saved log-probability. The blocks of a cluster
@@ -151,13 +269,10 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_row_kernel(const __grid
     return;
   }
   const float at = Logit<T>::load(z + label);
-  PolicyGrad g;
-  g.k = p.inv_tau * kLog2e;
-  g.label = label;
-  g.base = at;
+  const float k = p.inv_tau * kLog2e;
   constexpr int U = kPolicyUnroll;
   if (kForward) {
-    SoftSum mine = {-INFINITY, 0.0f, 0.0f};
+    PolicySum mine = {-INFINITY, 0.0f};
     for (int64_t c = from + threadIdx.x; c < to; c += kPolicyThreads * U) {
       uint4 a[U];
 #pragma unroll
@@ -166,41 +281,37 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_row_kernel(const __grid
         a[u] = Logit<T>::lowest();
         if (i < to) a[u] = kGradient && row.whole(i) ? *reinterpret_cast<const uint4*>(z + row.first(i)) : row.load(i);
       }
-      accumulate<T, false, U>(mine, a, g.k, g.k);
+      add_chunks<T, U>(mine, a, k);
     }
-    mine = join_lanes<32, false>(mine, g.k, g.k);
+    mine = join_sums<32>(mine, k);
     if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32] = mine;
     __syncthreads();
-    mine = join_lanes<kPolicyWarps, false>(sh.warp[threadIdx.x % kPolicyWarps], g.k, g.k);
+    mine = join_sums<kPolicyWarps>(sh.warp[threadIdx.x % kPolicyWarps], k);
     if (cluster > 1) {
       if ((int)threadIdx.x < cluster && (kGradient || threadIdx.x == 0)) {
         const uint32_t there = peer_addr(smem_addr(&sh.part[rank]), threadIdx.x);
-        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(mine.m), "f"(mine.s0) : "memory");
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(mine.m), "f"(mine.s) : "memory");
       }
       cluster_sync();
       const int i = threadIdx.x % kPolicyMaxCluster;
-      mine = SoftSum{-INFINITY, 0.0f, 0.0f};
-      if (i < cluster && (kGradient || rank == 0)) mine.m = sh.part[i].x, mine.s0 = sh.part[i].y;
-      mine = join_lanes<kPolicyMaxCluster, false>(mine, g.k, g.k);
+      mine = PolicySum{-INFINITY, 0.0f};
+      if (i < cluster && (kGradient || rank == 0)) mine = PolicySum{sh.part[i].x, sh.part[i].y};
+      mine = join_sums<kPolicyMaxCluster>(mine, k);
     }
-    g.base = finite_shift(mine.m);
     if ((kGradient || rank == 0) && threadIdx.x < 32) {
-      const double log_sum = log((double)mine.s0);
-      const RowResult t = finish_row(p, r, ((double)at - (double)g.base) * p.inv_tau64 - log_sum, log_sum, rank == 0);
+      const RowTerms t = finish_sum(p, r, mine, at, k, rank == 0);
       if (threadIdx.x == 0) sh.row = t;
     }
   } else if (threadIdx.x < 32) {
-    const double logp = p.saved_logp[r];
-    const RowResult t = finish_row(p, r, logp, -logp, false);
+    const RowTerms t = finish_saved(p, r, at, k);
     if (threadIdx.x == 0) sh.row = t;
   }
   if (kGradient) {
     // without kForward nothing has been read of the row but `at`, which no block may change before all have it
     if (!kForward && cluster > 1) cluster_sync(); else __syncthreads();
-    g.f = sh.row.f;
-    g.offset = sh.row.offset;
-    g.at_label = sh.row.at_label;
-    if (g.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, from, to, threadIdx.x, kPolicyThreads);
+    const RowTerms t = sh.row;
+    if (t.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, from, to, threadIdx.x, kPolicyThreads);
+    const PolicyGrad g = {k, t, label};
     for (int64_t c = from + threadIdx.x; c < to; c += kPolicyThreads * U) {
       uint4 a[U];
 #pragma unroll
@@ -232,33 +343,27 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_held_kernel(const __gri
     }
     return zero_chunks<T>(row, dz, same_grid, 0, chunks, threadIdx.x, kPolicyThreads);
   }
-  const float at = Logit<T>::load(z + label);
-  PolicyGrad g;
-  g.k = p.inv_tau * kLog2e;
-  g.label = label;
+  const float at = Logit<T>::load(z + label), k = p.inv_tau * kLog2e;
   uint4 a[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int c = threadIdx.x + u * kPolicyThreads;
     a[u] = c < chunks ? row.load(c) : Logit<T>::lowest();
   }
-  SoftSum mine = {-INFINITY, 0.0f, 0.0f};
-  accumulate<T, false, U>(mine, a, g.k, g.k);
-  mine = join_lanes<32, false>(mine, g.k, g.k);
+  PolicySum mine = {-INFINITY, 0.0f};
+  add_chunks<T, U>(mine, a, k);
+  mine = join_sums<32>(mine, k);
   if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32] = mine;
   __syncthreads();
-  mine = join_lanes<kPolicyWarps, false>(sh.warp[threadIdx.x % kPolicyWarps], g.k, g.k);
-  g.base = finite_shift(mine.m);
+  mine = join_sums<kPolicyWarps>(sh.warp[threadIdx.x % kPolicyWarps], k);
   if (threadIdx.x < 32) {
-    const double log_sum = log((double)mine.s0);
-    const RowResult t = finish_row(p, r, ((double)at - (double)g.base) * p.inv_tau64 - log_sum, log_sum, true);
+    const RowTerms t = finish_sum(p, r, mine, at, k, true);
     if (threadIdx.x == 0) sh.row = t;
   }
   __syncthreads();
-  g.f = sh.row.f;
-  g.offset = sh.row.offset;
-  g.at_label = sh.row.at_label;
-  if (g.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, 0, chunks, threadIdx.x, kPolicyThreads);
+  const RowTerms t = sh.row;
+  if (t.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, 0, chunks, threadIdx.x, kPolicyThreads);
+  const PolicyGrad g = {k, t, label};
 #pragma unroll
   for (int u = 0; u < U; ++u)
     if (threadIdx.x + u * kPolicyThreads < chunks) policy_chunk<T>(row, dz, same_grid, threadIdx.x + u * kPolicyThreads, a[u], g);
@@ -283,8 +388,8 @@ static_assert(kRowSlots > 2 * kSlots + 2, "rows that are still looked at would b
 
 struct PolicyRing {
   alignas(16) float4 part[kRowSlots][kPolicyMaxCluster];   // maximum, sum, the label's logit where it is known
-  alignas(16) float4 row[kRowSlots];                       // base, offset, factor, value at the label
-  alignas(16) SoftSum warp[2][kRingWarps];
+  RowTerms row[kRowSlots];
+  alignas(16) PolicySum warp[2][kRingWarps];
   uint64_t full[kSlots], empty[kSlots];
   uint64_t summed[kRowSlots], known[kRowSlots];
   uint32_t dead;
@@ -364,24 +469,27 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
       const int64_t label_chunk = (label + s.row.head) / Logit<T>::kPer;
       const bool owner = label_chunk >= s.lo && label_chunk < s.hi;
       if (threadIdx.x == 0 && owner) mark = Logit<T>::load(s.row.z + label);
-      SoftSum mine = {-INFINITY, 0.0f, 0.0f};
+      PolicySum mine = {-INFINITY, 0.0f};
       s.edges(threadIdx.x, [&](int64_t c) {
         const uint4 a = s.row.load(c);
-        accumulate<T, false, 1>(mine, &a, k, k);
+        add_chunks<T, 1>(mine, &a, k);
       });
       __syncwarp();
       for (int i0 = 0; i0 < s.n; i0 += kSlotChunks, slot.next()) {
         // after a wait that ran out no more of them, but this row's barrier, where all warps learn of it
         if (ok) ok = __all_sync(0xffffffffu, wait(smem_addr(&ring.full[slot.i]), slot.parity));
         uint4 a[kSlotUnroll];
+        const uint4* from = slots + slot.i * kSlotChunks + threadIdx.x;
 #pragma unroll
-        for (int u = 0; u < kSlotUnroll; ++u) {
-          const int i = threadIdx.x + u * kRingGroup;
-          a[u] = i0 + i < s.n ? slots[slot.i * kSlotChunks + i] : Logit<T>::lowest();
+        for (int u = 0; u < kSlotUnroll; ++u) a[u] = from[u * kRingGroup];
+        if (i0 + kSlotChunks > s.n) {
+#pragma unroll
+          for (int u = 0; u < kSlotUnroll; ++u)
+            if (i0 + (int)threadIdx.x + u * kRingGroup >= s.n) a[u] = Logit<T>::lowest();
         }
-        accumulate<T, false, kSlotUnroll>(mine, a, k, k);
+        add_chunks<T, kSlotUnroll>(mine, a, k);
       }
-      mine = join_lanes<32, false>(mine, k, k);
+      mine = join_sums<32>(mine, k);
       if (lane == 0) ring.warp[turn][warp] = mine;
       uint32_t all_ok;
       asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
@@ -390,11 +498,11 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
                    : "memory");
       if (!all_ok) break;                     // all of them, at the same barrier
       if (warp == 0) {
-        mine = join_lanes<kRingWarps, false>(ring.warp[turn][lane % kRingWarps], k, k);
+        mine = join_sums<kRingWarps>(ring.warp[turn][lane % kRingWarps], k);
         mark = __shfl_sync(0xffffffffu, mark, 0);
         if (lane < cluster) {
           const uint32_t to = peer_addr(smem_addr(&ring.part[at.i][rank]), lane);
-          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(mine.m), "f"(mine.s0), "f"(mark), "f"(0.0f) : "memory");
+          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(mine.m), "f"(mine.s), "f"(mark), "f"(0.0f) : "memory");
           mbar_arrive_cluster(peer_addr(smem_addr(&ring.summed[at.i]), lane));
         }
       }
@@ -414,34 +522,36 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
       }
       ok = __all_sync(0xffffffffu, wait(smem_addr(&ring.known[at.i]), at.parity));
       if (!ok) break;
-      const float4 t = ring.row[at.i];
-      const PolicyGrad g = {k, t.x, t.y, t.z, t.w, label};
+      const RowTerms t = ring.row[at.i];
+      const PolicyGrad g = {k, t, label};
       at.next();
-      const bool zero = g.f == 0.0f;
+      const bool zero = t.f == 0.0f, usual = same_grid && !t.far;
       if (zero) zero_chunks<T>(s.row, dz, same_grid, s.lo, s.hi, thread, kRingGroup);
       else s.edges(thread, [&](int64_t c) { policy_chunk<T>(s.row, dz, same_grid, c, s.row.load(c), g); });
-      const int64_t hot = (label + s.row.head) / Logit<T>::kPer - s.mid;       // the label's chunk and its place there
-      const int hot_at = (label + s.row.head) % Logit<T>::kPer;
-      T* out = dz + s.row.first(s.mid);
+      const int64_t hot = (label + s.row.head) / Logit<T>::kPer - s.mid;       // the label's chunk
+      uint4* out = reinterpret_cast<uint4*>(dz + s.row.first(s.mid)) + thread;     // used where it is aligned
       for (int i0 = 0; i0 < s.n; i0 += kSlotChunks, slot.next()) {
         // it is: its sums are known
         ok = __all_sync(0xffffffffu, ok && wait(smem_addr(&ring.full[slot.i]), slot.parity));
         if (!ok) break;
         uint4 a[kSlotUnroll];
+        const uint4* from = slots + slot.i * kSlotChunks + thread;
 #pragma unroll
-        for (int u = 0; u < kSlotUnroll; ++u) a[u] = slots[slot.i * kSlotChunks + thread + u * kRingGroup];
+        for (int u = 0; u < kSlotUnroll; ++u) a[u] = from[u * kRingGroup];
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_addr(&ring.empty[slot.i]));
         if (zero) continue;
+        float v[Logit<T>::kPer];
+        if (usual && i0 + kSlotChunks <= s.n && !(hot >= i0 && hot < i0 + kSlotChunks)) {
 #pragma unroll
-        for (int u = 0; u < kSlotUnroll; ++u) {
-          const int i = i0 + thread + u * kRingGroup;
-          if (i >= s.n) continue;
-          float v[Logit<T>::kPer];
-          policy_values<T>(a[u], g, v);
-          if (i == hot) put_label<T>(v, hot_at, g.at_label);
-          if (same_grid) st_stream(out + (int64_t)i * Logit<T>::kPer, Logit<T>::pack(v));
-          else store_chunk<T>(s.row, dz, s.mid + i, v);
+          for (int u = 0; u < kSlotUnroll; ++u) {
+            policy_values<T>(a[u], g, v);
+            st_stream(out + i0 + u * kRingGroup, Logit<T>::pack(v));
+          }
+        } else {
+#pragma unroll
+          for (int u = 0; u < kSlotUnroll; ++u)
+            if (i0 + thread + u * kRingGroup < s.n) policy_chunk<T>(s.row, dz, same_grid, s.mid + i0 + thread + u * kRingGroup, a[u], g);
         }
       }
     }
@@ -475,18 +585,13 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
       }
       ok = __all_sync(0xffffffffu, wait.wait<true>(smem_addr(&ring.summed[at.i]), at.parity));
       if (!ok) break;
-      SoftSum all = {-INFINITY, 0.0f, 0.0f};
       const float4 v = lane % kPolicyMaxCluster < cluster ? ring.part[at.i][lane % kPolicyMaxCluster] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
-      all.m = v.x;
-      all.s0 = v.y;
-      all = join_lanes<kPolicyMaxCluster, false>(all, k, k);
-      const RingSlice<T> s(p, r, rank);
-      const int owner = (int)((label + s.row.head) / Logit<T>::kPer / p.chunks_per_block);
-      const float mark = __shfl_sync(0xffffffffu, v.z, owner), base = finite_shift(all.m);
-      const double log_sum = log((double)all.s0);
-      const RowResult t = finish_row(p, r, ((double)mark - (double)base) * p.inv_tau64 - log_sum, log_sum, rank == 0);
+      const PolicySum all = join_sums<kPolicyMaxCluster>(PolicySum{v.x, v.y}, k);
+      const int head = Row<T>(static_cast<const T*>(p.z) + r * p.z_stride, p.vocab).head;
+      const int owner = (int)((uint32_t)(label + head) / Logit<T>::kPer / (uint32_t)p.chunks_per_block);
+      const RowTerms t = finish_sum(p, r, all, __shfl_sync(0xffffffffu, v.z, owner), k, rank == 0);
       if (lane == 0) {
-        ring.row[at.i] = make_float4(base, t.offset, t.f, t.at_label);
+        ring.row[at.i] = t;
         mbar_arrive(smem_addr(&ring.known[at.i]));
       }
       at.next();

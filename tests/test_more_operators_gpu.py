@@ -361,9 +361,9 @@ def test_policy_terms_left_out(ctx, dtype):
     a = policy_inputs(64, 777, dtype, seed=8)
     for names in (("old",), ("ref",), ("adv",), ("g",), ("old", "ref"), ("old", "adv"), ("old", "ref", "adv", "g")):
         policy_case(ctx, {**a, **dict.fromkeys(names)}, kl=0.1)
-    lp = torch.empty(64, device="cuda")
+    lp, want, loss = (torch.empty(64, device="cuda") for _ in range(3))
     ctx.slidedp_policy_loss(a["z"], a["labels"], None, None, None, None, lp)
-    _, want, _ = policy_case(ctx, a)
+    ctx.slidedp_policy_loss(a["z"], a["labels"], a["old"], a["ref"], a["adv"], loss, want)
     assert torch.equal(lp, want)
 
 
@@ -540,3 +540,22 @@ def test_clip_is_the_norm_of_the_flat_path(ctx):
     ws = torch.empty(ctx.slidedp_clip_grad_norm_workspace(parts), dtype=torch.uint8, device="cuda")
     ctx.slidedp_clip_grad_norm(parts, None, 0.1, result, ws, scale=0.5)
     assert abs(result[1].item() - norm) <= 1e-12 * norm and abs(result[2].item() - coef) <= 1e-12 * coef
+
+
+@pytest.mark.parametrize("V", [9, 1000, 20000, 70000])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_policy_rows_of_the_lowest_value(ctx, V, dtype):
+    """All logits masked with the type's lowest value: as likely as each other. Some of them: not at all. Very large ones beside them."""
+    a = policy_inputs(8, V, dtype, absent=0.0)
+    lowest = torch.finfo(dtype).min
+    z = a["z"].clone()
+    z[0], z[1], z[2] = lowest, lowest, -lowest
+    z[1, ::2] = -math.inf
+    z[2, 1::3] = 1.0
+    z[3], z[3, 5:8] = 1e30, 2e30
+    z[4], z[4, 2] = lowest, 0.0
+    a["z"], a["labels"] = z, torch.tensor([3, 5, 0, 6, 2, 1, 2, 3], dtype=torch.int32, device="cuda")
+    lp = torch.log_softmax(z.double(), 1).gather(1, a["labels"].long()[:, None])[:, 0]
+    a["old"], a["ref"] = (lp + 0.1).float(), (lp - 0.3).float()
+    for tau in (1.0, 0.6):
+        policy_case(ctx, a, tau=tau, kl=0.05 if tau == 1.0 else 0.0)
