@@ -25,8 +25,8 @@ struct PolicyParams {
   int64_t chunks_per_block;  // 16-byte chunks of a row that one block of its cluster takes
   int* error;                // pinned host word that a wait which runs out sets
   uint32_t polls;            // and how long it polls
-  float inv_tau;
-  double low, high, kl, inv_tau64;
+  float inv_tau, low, high, kl;
+  double inv_tau64;
 };
 
 __device__ __forceinline__ int row_label(const PolicyParams& p, int64_t r) {
@@ -125,20 +125,32 @@ __device__ __forceinline__ void add_chunks(PolicySum& mine, const uint4* a, floa
 struct RowTerms {
   float shift, offset, factor, at_label, f;
   int far;
+  float loss, logp;
 };
 struct PolicyGrad {
   float k;
   RowTerms t;
   int label;
 };
-template <typename T>
+// Of BF16 logits every kPoly-th pair takes the polynomial exponential (relative error 3e-6, of a value that is rounded to BF16): two
+// exponentials per logit are more than the special-function units give at the rate of the memory.
+template <typename T, int kPoly = 0>
 __device__ __forceinline__ void policy_values(uint4 a, const PolicyGrad& g, float* out) {
   constexpr int P = Logit<T>::kPer;
   uint64_t v[P / 2];
   Logit<T>::unpack(a, v);
   const uint64_t factor = pair(g.t.factor, g.t.factor), kk = pair(g.k, g.k), minus = pair(-g.t.shift, -g.t.shift);
 #pragma unroll
-  for (int e = 0; e < P / 2; ++e) split(mul2(exp2_pair(fma2(v[e], kk, minus)), factor), &out[2 * e], &out[2 * e + 1]);
+  for (int e = 0; e < P / 2; ++e) {
+    const uint64_t x = fma2(v[e], kk, minus);
+    float lo, hi;
+    if constexpr (sizeof(T) == 2 && kPoly > 0) {
+      if (e % kPoly == 0) exp2_pair_poly(x, &lo, &hi); else split(exp2_pair(x), &lo, &hi);
+    } else {
+      split(exp2_pair(x), &lo, &hi);
+    }
+    split(mul2(pair(lo, hi), factor), &out[2 * e], &out[2 * e + 1]);
+  }
 }
 template <typename T>
 __device__ __forceinline__ void policy_values_far(uint4 a, float k, const RowTerms& t, float* out) {
@@ -186,53 +198,68 @@ __device__ __forceinline__ bool on_same_grid(const T* a, const T* b) {
   return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
 }
 
+// A row's own numbers, which can be fetched before its sum is known.
+struct RowInput {
+  float advantage, old_logp, ref_logp, grad;
+};
+__device__ __forceinline__ RowInput row_input(const PolicyParams& p, int64_t r) {
+  return RowInput{p.advantage ? p.advantage[r] : 0.0f, p.old_logp ? p.old_logp[r] : 0.0f, p.ref_logp ? p.ref_logp[r] : 0.0f, p.row_grad ? p.row_grad[r] : 1.0f};
+}
+// ln s to 2^-24: the exponent's part in FP64, FP32 for the part in [1, 2).
+__device__ __forceinline__ double log_of(float s) {
+  if (!(s >= 1.1754944e-38f && s <= 3.4028235e38f)) return (double)logf(s);
+  const int bits = __float_as_int(s);
+  return (double)((bits >> 23) - 127) * 0.6931471805599453 + (double)logf(__int_as_float((bits & 0x007fffff) | 0x3f800000));
+}
 // A row's loss, and the rest of its terms, by one warp: the exponentials that hang on the log-probability are taken by three lanes at
-// once. In FP64: the ratio is compared with the edges of the clipped range.
-__device__ __forceinline__ void finish_row(const PolicyParams& p, int64_t r, double logp, double scale, bool write, RowTerms* t) {
+// once. The log-probability comes in FP64, its differences from the old and the reference's one are formed in FP64.
+__device__ __forceinline__ void finish_row(const PolicyParams& p, const RowInput& in, double logp, float scale, RowTerms* t) {
   const int lane = threadIdx.x % 32;
-  const double a = p.advantage ? (double)p.advantage[r] : 0.0, g = p.row_grad ? (double)p.row_grad[r] : 1.0;
-  const double k = p.ref_logp ? (double)p.ref_logp[r] - logp : 0.0;
-  const double e = exp(lane == 0 ? (p.old_logp && a != 0.0 ? logp - (double)p.old_logp[r] : 0.0) : lane == 1 ? k : logp);
-  const double ratio = __shfl_sync(0xffffffffu, e, 0), to_ref = __shfl_sync(0xffffffffu, e, 1), prob = __shfl_sync(0xffffffffu, e, 2);
-  double loss = 0.0, slope = 0.0;
-  if (a != 0.0) {
-    const bool inside = !(a > 0.0 ? ratio > p.high : ratio < p.low) || a != a;
-    loss = -(inside ? ratio : a > 0.0 ? p.high : p.low) * a;
+  const float a = in.advantage, k = p.ref_logp ? (float)((double)in.ref_logp - logp) : 0.0f;
+  const float x = lane == 0 ? (p.old_logp && a != 0.0f ? (float)(logp - (double)in.old_logp) : 0.0f) : lane == 1 ? k : (float)logp;
+  const float ratio = __shfl_sync(0xffffffffu, expf(x), 0), less_one = expm1f(x);
+  const float to_ref = __shfl_sync(0xffffffffu, less_one, 1), prob = __shfl_sync(0xffffffffu, less_one, 2);     // less one
+  float loss = 0.0f, slope = 0.0f;
+  if (a != 0.0f) {
+    const bool inside = !(a > 0.0f ? ratio > p.high : ratio < p.low) || a != a;
+    loss = -(inside ? ratio : a > 0.0f ? p.high : p.low) * a;
     if (inside) slope = -a * ratio;
   }
   if (p.ref_logp) {
-    loss += p.kl * (to_ref - k - 1.0);
-    slope += p.kl * (1.0 - to_ref);
+    loss = fmaf(p.kl, to_ref - k, loss);
+    slope = fmaf(-p.kl, to_ref, slope);
   }
-  if (write && lane == 0) {
-    if (p.loss) p.loss[r] = (float)loss;
-    p.logp[r] = (float)logp;
-  }
-  const double f = g == 0.0 ? 0.0 : g * slope * p.inv_tau64;
-  t->factor = (float)(-f * scale);
-  t->at_label = (float)(f * (1.0 - prob));
-  t->f = (float)f;
+  t->loss = loss;
+  t->logp = (float)logp;
+  const float f = in.grad == 0.0f ? 0.0f : in.grad * slope * p.inv_tau;
+  t->factor = -f * scale;
+  t->at_label = -f * prob;
+  t->f = f;
 }
 // From the sum, and the label's logit.
-__device__ __forceinline__ RowTerms finish_sum(const PolicyParams& p, int64_t r, PolicySum all, float mark, float k, bool write) {
+__device__ __forceinline__ RowTerms finish_sum(const PolicyParams& p, const RowInput& in, PolicySum all, float mark, float k) {
   const float c = shift_of(all.m, k);
-  const double log_sum = log((double)all.s);
+  const double log_sum = log_of(all.s);
   RowTerms t;
   t.far = is_far(c);
   t.shift = t.far ? all.m : c;
   t.offset = 0.0f;
   const double logp = t.far ? ((double)mark - (double)all.m) * p.inv_tau64 : ((double)k * (double)mark - (double)c) * 0.6931471805599453;
-  finish_row(p, r, logp - log_sum, 1.0 / (double)all.s, write, &t);
+  finish_row(p, in, logp - log_sum, 1.0f / all.s, &t);
   return t;
 }
+__device__ __forceinline__ void write_loss(const PolicyParams& p, int64_t r, const RowTerms& t) {
+  if (p.loss) p.loss[r] = t.loss;
+  p.logp[r] = t.logp;
+}
 // From the saved log-probability: the shift is the row's log2 sum, or far from zero the label's logit.
-__device__ __forceinline__ RowTerms finish_saved(const PolicyParams& p, int64_t r, float mark, float k) {
+__device__ __forceinline__ RowTerms finish_saved(const PolicyParams& p, int64_t r, const RowInput& in, float mark, float k) {
   const double logp = p.saved_logp[r], log2_p = logp * 1.4426950408889634, exact = (double)k * (double)mark - log2_p;
   RowTerms t;
   t.far = is_far((float)exact) || is_far(mark * k);
   t.shift = t.far ? mark : (float)exact;
   t.offset = (float)log2_p;
-  finish_row(p, r, logp, t.far ? 1.0 : exp2((double)t.shift - exact), false, &t);
+  finish_row(p, in, logp, t.far ? 1.0f : exp2f((float)((double)t.shift - exact)), &t);
   return t;
 }
 
@@ -247,7 +274,7 @@ struct PolicyShared {
 // kForward: log-probability and loss; kGradient: the gradient, without kForward from the saved log-probability. The blocks of a cluster
 // share a row's chunks, and exchange their sums through distributed shared memory.
 template <typename T, bool kForward, bool kGradient>
-__global__ void __launch_bounds__(kPolicyThreads) policy_row_kernel(const __grid_constant__ PolicyParams p, int cluster) {
+__global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __grid_constant__ PolicyParams p, int cluster) {
   start_after_previous_kernel();
   __shared__ PolicyShared sh;
   const int64_t r = blockIdx.x / cluster;
@@ -270,6 +297,8 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_row_kernel(const __grid
   }
   const float at = Logit<T>::load(z + label);
   const float k = p.inv_tau * kLog2e;
+  RowInput in = {};
+  if (threadIdx.x < 32) in = row_input(p, r);
   constexpr int U = kPolicyUnroll;
   if (kForward) {
     PolicySum mine = {-INFINITY, 0.0f};
@@ -299,11 +328,14 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_row_kernel(const __grid
       mine = join_sums<kPolicyMaxCluster>(mine, k);
     }
     if ((kGradient || rank == 0) && threadIdx.x < 32) {
-      const RowTerms t = finish_sum(p, r, mine, at, k, rank == 0);
-      if (threadIdx.x == 0) sh.row = t;
+      const RowTerms t = finish_sum(p, in, mine, at, k);
+      if (threadIdx.x == 0) {
+        sh.row = t;
+        if (rank == 0) write_loss(p, r, t);
+      }
     }
   } else if (threadIdx.x < 32) {
-    const RowTerms t = finish_saved(p, r, at, k);
+    const RowTerms t = finish_saved(p, r, in, at, k);
     if (threadIdx.x == 0) sh.row = t;
   }
   if (kGradient) {
@@ -344,6 +376,8 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_held_kernel(const __gri
     return zero_chunks<T>(row, dz, same_grid, 0, chunks, threadIdx.x, kPolicyThreads);
   }
   const float at = Logit<T>::load(z + label), k = p.inv_tau * kLog2e;
+  RowInput in = {};
+  if (threadIdx.x < 32) in = row_input(p, r);
   uint4 a[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -357,8 +391,11 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_held_kernel(const __gri
   __syncthreads();
   mine = join_sums<kPolicyWarps>(sh.warp[threadIdx.x % kPolicyWarps], k);
   if (threadIdx.x < 32) {
-    const RowTerms t = finish_sum(p, r, mine, at, k, true);
-    if (threadIdx.x == 0) sh.row = t;
+    const RowTerms t = finish_sum(p, in, mine, at, k);
+    if (threadIdx.x == 0) {
+      sh.row = t;
+      write_loss(p, r, t);
+    }
   }
   __syncthreads();
   const RowTerms t = sh.row;
@@ -378,20 +415,22 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_held_kernel(const __gri
 constexpr int kRingWarps = 8;                       // of each of the two groups
 constexpr int kRingGroup = kRingWarps * 32;
 constexpr int kRingThreads = 2 * kRingGroup + 64;   // and the producer's and the rows' warps
-constexpr int kSlotChunks = 1024;                   // 16 KB
-constexpr int kSlotUnroll = kSlotChunks / kRingGroup;
-constexpr int kSlots = 13;
+constexpr int kSlotUnroll = 4;
+constexpr int kSlotChunks = kRingGroup * kSlotUnroll;
+constexpr int kSlots = 208 * 1024 / (kSlotChunks * 16);
+constexpr int kGradPoly = 0;
 // Rows between the first and the last that any block of a cluster has to do with: a block's sums are at most kSlots rows before its
 // gradients, which wait for the other blocks' sums, which are at most kSlots rows before those blocks' gradients.
 constexpr int kRowSlots = 32;
 static_assert(kRowSlots > 2 * kSlots + 2, "rows that are still looked at would be overwritten");
 
 struct PolicyRing {
-  alignas(16) float4 part[kRowSlots][kPolicyMaxCluster];   // maximum, sum, the label's logit where it is known
+  alignas(16) float4 part[kRowSlots][kPolicyMaxCluster];   // maximum, sum, the label's logit where it is known, the sums' number
   RowTerms row[kRowSlots];
   alignas(16) PolicySum warp[2][kRingWarps];
   uint64_t full[kSlots], empty[kSlots];
   uint64_t summed[kRowSlots], known[kRowSlots];
+  int sent[kPolicyMaxCluster];                             // the number after that of the last sums that each block sent
   uint32_t dead;
 };
 
@@ -439,36 +478,37 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
       mbar_init(smem_addr(&ring.empty[i]), kRingWarps);
     }
     for (int i = 0; i < kRowSlots; ++i) {
-      mbar_init(smem_addr(&ring.summed[i]), cluster);
+      mbar_init(smem_addr(&ring.summed[i]), 1);
       mbar_init(smem_addr(&ring.known[i]), 1);
     }
     ring.dead = 0;
     mbar_init_fence();
   }
+  if (threadIdx.x < kRowSlots * kPolicyMaxCluster) ring.part[threadIdx.x / kPolicyMaxCluster][threadIdx.x % kPolicyMaxCluster].w = 0.0f;
   if (cluster > 1) cluster_sync(); else __syncthreads();
   wait_for_previous_kernel();
   const Waiter wait{&ring.dead, p.error, p.polls};
   const float k = p.inv_tau * kLog2e;
   Place<kSlots> slot;
   Place<kRowSlots> at;
-  int next_label = first < p.rows ? row_label(p, first) : -1;
-  const auto label_of = [&](int64_t r) {      // the next row's is fetched ahead
-    const int y = next_label;
-    if (r + step < p.rows) next_label = row_label(p, r + step);
-    return y;
+  int label1 = first < p.rows ? p.labels[first] : -1, label2 = first + step < p.rows ? p.labels[first + step] : -1;
+  const auto label_of = [&](int64_t r) {      // fetched two rows ahead
+    const int y = label1;
+    label1 = label2;
+    if (r + 2 * (int64_t)step < p.rows) label2 = p.labels[r + 2 * (int64_t)step];
+    return y >= 0 && y < p.vocab ? y : -1;
   };
   bool ok = true;
   if (warp < kRingWarps) {                    // the sums
-    int turn = 0;
+    int turn = 0, sent = 1;
     for (int64_t r = first; r < p.rows; r += step) {
       const int label = label_of(r);
       if (label < 0) continue;
       const RingSlice<T> s(p, r, rank);
-      // read before any block may write this row's gradient to the same memory
+      // the label's logit comes from the block that has it, before any block may write this row's gradient to the same memory
       float mark = 0.0f;
-      const int64_t label_chunk = (label + s.row.head) / Logit<T>::kPer;
-      const bool owner = label_chunk >= s.lo && label_chunk < s.hi;
-      if (threadIdx.x == 0 && owner) mark = Logit<T>::load(s.row.z + label);
+      const int64_t hot = (label + s.row.head) / Logit<T>::kPer;
+      if (warp == 0 && (hot == s.lo || hot == s.hi - 1)) mark = Logit<T>::load(s.row.z + label);
       PolicySum mine = {-INFINITY, 0.0f};
       s.edges(threadIdx.x, [&](int64_t c) {
         const uint4 a = s.row.load(c);
@@ -487,27 +527,42 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
           for (int u = 0; u < kSlotUnroll; ++u)
             if (i0 + (int)threadIdx.x + u * kRingGroup >= s.n) a[u] = Logit<T>::lowest();
         }
+        if (warp == 0 && hot >= s.mid + i0 && hot < s.mid + i0 + kSlotChunks && hot < s.mid + s.n)
+          mark = Logit<T>::load(reinterpret_cast<const T*>(slots + slot.i * kSlotChunks) + (label - s.row.first(s.mid + i0)));
         add_chunks<T, kSlotUnroll>(mine, a, k);
       }
       mine = join_sums<32>(mine, k);
       if (lane == 0) ring.warp[turn][warp] = mine;
       uint32_t all_ok;
-      asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
+      __syncwarp();                           // lanes that took different ways meet before the barrier
+      asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n barrier.cta.red.and.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
                    : "=r"(all_ok)
                    : "r"((uint32_t)ok), "n"(kRingGroup)
                    : "memory");
       if (!all_ok) break;                     // all of them, at the same barrier
       if (warp == 0) {
-        mine = join_sums<kRingWarps>(ring.warp[turn][lane % kRingWarps], k);
-        mark = __shfl_sync(0xffffffffu, mark, 0);
-        if (lane < cluster) {
-          const uint32_t to = peer_addr(smem_addr(&ring.part[at.i][rank]), lane);
-          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(mine.m), "f"(mine.s), "f"(mark), "f"(0.0f) : "memory");
-          mbar_arrive_cluster(peer_addr(smem_addr(&ring.summed[at.i]), lane));
+        mine = join_sums<16>(lane % 16 < kRingWarps ? ring.warp[turn][lane % 16] : PolicySum{-INFINITY, 0.0f}, k);
+        const uint32_t bar = smem_addr(&ring.summed[at.i]);
+        if (cluster == 1) {                   // asynchronous stores are for clusters: in a launch without them they are an illegal instruction
+          if (lane == 0) {
+            ring.part[at.i][0] = make_float4(mine.m, mine.s, mark, 0.0f);
+            mbar_arrive(bar);
+          }
+        } else if (lane < cluster) {          // stores and an arrival that others see would wait 2500 cycles for the order between them
+          const uint32_t to = peer_addr(smem_addr(&ring.part[at.i][rank]), lane), there = peer_addr(bar, lane);
+          if (lane == 0) mbar_expect(bar, cluster * sizeof(float4));
+          asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to), "f"(mine.m),
+                       "f"(mine.s), "f"(mark), "f"(__int_as_float(sent)), "r"(there)
+                       : "memory");
         }
+        ++sent;
       }
       turn ^= 1;
       at.next();
+    }
+    if (warp == 0 && cluster > 1 && lane < cluster) {        // told to all, should one of them have given up
+      const uint32_t to = peer_addr(smem_addr(&ring.sent[rank]), lane);
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(sent) : "memory");
     }
   } else if (warp < 2 * kRingWarps) {         // the gradients
     const int thread = threadIdx.x - kRingGroup;
@@ -531,9 +586,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
       const int64_t hot = (label + s.row.head) / Logit<T>::kPer - s.mid;       // the label's chunk
       uint4* out = reinterpret_cast<uint4*>(dz + s.row.first(s.mid)) + thread;     // used where it is aligned
       for (int i0 = 0; i0 < s.n; i0 += kSlotChunks, slot.next()) {
-        // it is: its sums are known
-        ok = __all_sync(0xffffffffu, ok && wait(smem_addr(&ring.full[slot.i]), slot.parity));
-        if (!ok) break;
+        // the slot is full: what is known of the row was known after its sums
         uint4 a[kSlotUnroll];
         const uint4* from = slots + slot.i * kSlotChunks + thread;
 #pragma unroll
@@ -545,7 +598,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
         if (usual && i0 + kSlotChunks <= s.n && !(hot >= i0 && hot < i0 + kSlotChunks)) {
 #pragma unroll
           for (int u = 0; u < kSlotUnroll; ++u) {
-            policy_values<T>(a[u], g, v);
+            policy_values<T, kGradPoly>(a[u], g, v);
             st_stream(out + i0 + u * kRingGroup, Logit<T>::pack(v));
           }
         } else {
@@ -583,22 +636,32 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
         }
         continue;
       }
-      ok = __all_sync(0xffffffffu, wait.wait<true>(smem_addr(&ring.summed[at.i]), at.parity));
+      const RowInput in = row_input(p, r);
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&ring.summed[at.i]), at.parity));
       if (!ok) break;
       const float4 v = lane % kPolicyMaxCluster < cluster ? ring.part[at.i][lane % kPolicyMaxCluster] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
       const PolicySum all = join_sums<kPolicyMaxCluster>(PolicySum{v.x, v.y}, k);
       const int head = Row<T>(static_cast<const T*>(p.z) + r * p.z_stride, p.vocab).head;
       const int owner = (int)((uint32_t)(label + head) / Logit<T>::kPer / (uint32_t)p.chunks_per_block);
-      const RowTerms t = finish_sum(p, r, all, __shfl_sync(0xffffffffu, v.z, owner), k, rank == 0);
+      const RowTerms t = finish_sum(p, in, all, __shfl_sync(0xffffffffu, v.z, owner), k);
       if (lane == 0) {
         ring.row[at.i] = t;
         mbar_arrive(smem_addr(&ring.known[at.i]));
+        if (rank == 0) write_loss(p, r, t);
       }
       at.next();
     }
   }
   __syncwarp();
-  if (cluster > 1) cluster_sync();            // nobody leaves while sums are still stored to it
+  if (cluster == 1) return;
+  cluster_sync();
+  // Sums that were waited for have come. Where a wait ran out, nobody sends any more, but some may still be on their way here.
+  if (ring.dead && warp == 0 && lane < cluster) {
+    for (int n = max(1, ring.sent[lane] - kRowSlots); n < ring.sent[lane]; ++n) {
+      const volatile float4* to = &ring.part[(n - 1) % kRowSlots][lane];
+      for (uint32_t polls = 0; __float_as_int(to->w) != n && polls < (1u << 20); ++polls) __nanosleep(100);
+    }
+  }
 }
 
 }  // namespace slidedp
@@ -610,7 +673,7 @@ namespace {
 
 constexpr int kSms = 148;
 constexpr int64_t kHeldChunks = 8 * kPolicyThreads;          // rows up to 32 KB are held in registers
-constexpr int64_t kMaxSliceChunks = 8 * kSlotChunks + 512;   // of the ring's 13 slots
+constexpr int64_t kMaxSliceChunks = 8704;                    // of the ring's 13312
 constexpr int64_t kMinSliceChunks = 512;
 constexpr int64_t kEnoughBlocks = kSms * 4;
 
@@ -682,9 +745,9 @@ int run_policy(slidedp_ctx* ctx, const slidedp_policy_args* a, PolicyMode mode, 
   p.dz_stride = a->d_logits_stride;
   p.inv_tau = (float)(1.0 / a->temperature);
   p.inv_tau64 = 1.0 / a->temperature;
-  p.low = 1.0 - a->clip_low;
-  p.high = 1.0 + a->clip_high;
-  p.kl = a->kl_weight;
+  p.low = (float)(1.0 - a->clip_low);
+  p.high = (float)(1.0 + a->clip_high);
+  p.kl = (float)a->kl_weight;
   const int rc = check_kernel_error(ctx);
   if (rc != SLIDEDP_OK) return rc;
   DeviceGuard guard(ctx->device);
@@ -705,7 +768,7 @@ int run_policy(slidedp_ctx* ctx, const slidedp_policy_args* a, PolicyMode mode, 
     f32 ? held(float()) : held(uint16_t());
   } else if (mode == kPolicyStep && chunks <= kPolicyMaxCluster * kMaxSliceChunks) {
     int cluster = 1;
-    while (cluster < kPolicyMaxCluster && (chunks > cluster * kMaxSliceChunks || (a->rows * cluster < kSms && chunks > cluster * kSlotChunks))) cluster *= 2;
+    while (cluster < kPolicyMaxCluster && (chunks > cluster * kMaxSliceChunks || (a->rows * cluster < kSms && chunks > cluster * 1024))) cluster *= 2;
     p.chunks_per_block = (chunks + cluster - 1) / cluster;
     const size_t smem = kSlots * kSlotChunks * 16;
     const auto run = [&](auto kernel) {

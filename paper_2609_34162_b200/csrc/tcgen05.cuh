@@ -36,20 +36,6 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 
-// The same for barriers that other blocks of the cluster arrive at, and their arrival, which their stores come before.
-__device__ __forceinline__ bool mbar_try_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_there) {   // an address in the cluster's shared memory
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_there) : "memory");
-}
-
 // Every wait inside a kernel ends: after `polls` polls (kWaitPolls, but for tests) it sets the block's `dead` word, which
 // ends every other wait of the block early, and the error word that the host reads. A caller that gets
 // false stops issuing work and leaves. Threads that wait for the same thing may get different answers.
@@ -57,10 +43,9 @@ struct Waiter {
   volatile uint32_t* dead;   // shared memory
   int* error;                // pinned host memory
   uint32_t polls;
-  template <bool kCluster = false>
-  __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, uint32_t nap_ns = 0) const {
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, uint32_t nap_ns = 0) const {
     for (uint32_t n = 0; n < polls; ++n) {
-      if (kCluster ? mbar_try_cluster(bar, parity) : mbar_try(bar, parity)) return true;
+      if (mbar_try(bar, parity)) return true;
       if ((n & 255u) == 255u && *dead) return false;
       if (nap_ns) __nanosleep(nap_ns);   // a wait that may be long and is not urgent leaves the issue slots alone
     }
@@ -68,7 +53,6 @@ struct Waiter {
     *reinterpret_cast<volatile int*>(error) = 1;
     return false;
   }
-  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, uint32_t nap_ns = 0) const { return wait(bar, parity, nap_ns); }
 };
 // Waits, also after such an early exit, for what this thread has started and must not leave in flight: copies, products.
 __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
