@@ -1,10 +1,11 @@
 // libslidedp: token embedding with scaling, and the table's gradient by sorted tokens. See include/slidedp_ops.h for the contract.
 //
 // out[t] = s table[id t];  d_table[v] = s sum of d_out[t] over id t = v.  Bound: HBM.
-// The gradient is two kernels. The first sorts the tokens by id, stably, so that each id's tokens stand together in their
-// order. The second cuts the sorted list into pieces of equal length, however often an id occurs, and sums each piece's rows; an id
-// whose tokens lie in several pieces has a partial sum per piece, added in the pieces' order by the block that comes last. No
-// floating-point atomics: the order of every sum follows from the ids alone.
+// The gradient is three kernels. The first sorts the tokens by id, stably, so that each id's tokens stand together in their
+// order; meanwhile the SMs that it leaves idle clear part of the table. The second cuts the sorted list into pieces and sums their
+// rows, and clears what is left; the tokens of an id that has many are cut where the pieces are, however often it occurs, and have a
+// partial sum per piece, which the third adds in the pieces' order. No atomics, no waiting for other blocks: the order of every sum
+// follows from the ids alone.
 #include "ops_internal.h"
 #include "rows.cuh"
 #include "tcgen05.cuh"
@@ -26,30 +27,45 @@ struct EmbedParams {
   float scale;
 };
 
-// Bound: HBM, each row read once and written once. One vector of four tokens' rows per thread.
+// A thread's values of a row: K vectors of V, blockDim vectors apart, so that narrow ones (rows that are not aligned) come in numbers.
+template <int V> constexpr int vectors_per_thread = V == 1 ? 4 : V == 2 ? 2 : 1;
+
+// Bound: HBM, each row read once and written once. K vectors of four tokens' rows per thread.
 template <typename T, int V>
 __global__ void __launch_bounds__(kEmbedThreads) embedding_kernel(const __grid_constant__ EmbedParams p) {
   start_after_previous_kernel();
   typedef typename Raw<T, V>::type R;
+  constexpr int K = vectors_per_thread<V>;
   const int64_t t0 = (int64_t)(blockIdx.x / p.chunks) * kEmbedTokens;
-  const int64_t col = ((int64_t)(blockIdx.x % p.chunks) * blockDim.x + threadIdx.x) * V;
-  if (col >= p.hidden) return;
+  const int64_t first = (int64_t)(blockIdx.x % p.chunks) * K * blockDim.x + threadIdx.x;
   int id[kEmbedTokens];
-  R a[kEmbedTokens];
+  R a[kEmbedTokens][K];
 #pragma unroll
-  for (int k = 0; k < kEmbedTokens; ++k) id[k] = t0 + k < p.tokens ? p.ids[t0 + k] : -1;
+  for (int t = 0; t < kEmbedTokens; ++t) id[t] = t0 + t < p.tokens ? p.ids[t0 + t] : -1;
 #pragma unroll
-  for (int k = 0; k < kEmbedTokens; ++k)
-    if (id[k] >= 0 && id[k] < p.vocab) a[k] = __ldg(reinterpret_cast<const R*>(static_cast<const T*>(p.table) + id[k] * p.table_stride + col));
+  for (int t = 0; t < kEmbedTokens; ++t) {
+    if (id[t] < 0 || id[t] >= p.vocab) continue;
+    const T* row = static_cast<const T*>(p.table) + id[t] * p.table_stride;
 #pragma unroll
-  for (int k = 0; k < kEmbedTokens; ++k) {
-    if (t0 + k >= p.tokens) return;
-    float v[V];
-    const bool has = id[k] >= 0 && id[k] < p.vocab;
-    if (has) to_floats<T, V>(a[k], v);
+    for (int k = 0; k < K; ++k) {
+      const int64_t col = (first + k * blockDim.x) * V;
+      if (col < p.hidden) a[t][k] = __ldg(reinterpret_cast<const R*>(row + col));
+    }
+  }
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = has ? v[e] * p.scale : 0.0f;
-    store_values<V>(static_cast<T*>(p.out) + (t0 + k) * p.out_stride + col, v);
+  for (int t = 0; t < kEmbedTokens; ++t) {
+    if (t0 + t >= p.tokens) return;
+    const bool has = id[t] >= 0 && id[t] < p.vocab;
+    T* row = static_cast<T*>(p.out) + (t0 + t) * p.out_stride;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t col = (first + k * blockDim.x) * V;
+      float v[V] = {};
+      if (has && col < p.hidden) to_floats<T, V>(a[t][k], v);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] = has ? v[e] * p.scale : 0.0f;
+      if (col < p.hidden) store_values<V>(row + col, v);
+    }
   }
 }
 
@@ -64,15 +80,18 @@ constexpr int kMaxSortCluster = 8;
 
 struct SortParams {
   const int32_t* ids;
-  uint32_t *key[2], *pos[2];     // sorted ids (vocab: absent) and their tokens, the result in [passes % 2]
+  uint2* item[2];                // ids (vocab: absent) and their tokens, sorted in [passes % 2]
   uint32_t* used;                // a bit per row of the table
-  int32_t* arrived;              // counters of the blocks that have a part of an id's sum
-  int64_t used_words, arrived_words;
-  int32_t tokens, vocab, per_block;
+  int64_t used_words;
+  int32_t tokens, vocab, per_block, per_lane;
   int passes, digit;
+  char* clear;                   // rows [0, clear_rows) of the table, each `clear_vectors` of clear_width bytes
+  int64_t clear_stride;
+  uint32_t clear_rows, clear_vectors;
+  int clear_width;
 };
 struct SortShared {
-  uint32_t count[kSortWarps][kBins];   // of one turn, per warp; then where its first one goes
+  uint32_t count[kSortWarps][kBins];   // of one turn, per warp; then where in the turn's tokens of that digit its first one stands
   uint32_t total[kBins];               // of this block
   uint32_t next[kBins];                // where the next of each digit goes
   uint32_t warp[kSortWarps];
@@ -80,43 +99,113 @@ struct SortShared {
 
 // Sorts by digits of up to nine bits, the lowest first, in one cluster whatever the number of tokens: each block has a contiguous
 // part of the list. A pass counts the digits, exchanges the counts through distributed shared memory, and moves the tokens in
-// turns of 4096: a warp finds equal digits among its lanes, and the counts per warp give every token its place. Bound: latency
-// of its steps (8192 tokens, two passes: 4 MB of shared-memory counters go through their zeroing, counting and sums).
+// turns of 4096: a warp finds equal digits among its lanes, and the counts per warp give every token its place. A block whose part is
+// one turn finds the places first and has its counts from them. Bound: latency of its steps, a handful of barriers and trips to
+// L2 per pass.
+__device__ __forceinline__ void clear_rows(const SortParams& p, uint32_t block, uint32_t blocks) {
+  const uint32_t all = p.clear_rows * p.clear_vectors;
+  for (uint32_t i = block * kSortThreads + threadIdx.x; i < all; i += blocks * kSortThreads) {
+    char* to = p.clear + (int64_t)(i / p.clear_vectors) * p.clear_stride + (int64_t)(i % p.clear_vectors) * p.clear_width;
+    if (p.clear_width == 16) st_stream(to, make_uint4(0, 0, 0, 0));
+    else if (p.clear_width == 4) __stcs(reinterpret_cast<uint32_t*>(to), 0u);
+    else __stcs(reinterpret_cast<uint16_t*>(to), (uint16_t)0);
+  }
+}
 __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_constant__ SortParams p, int cluster) {
   extern __shared__ uint4 dynamic[];
   SortShared& sh = *reinterpret_cast<SortShared*>(dynamic);
   start_after_previous_kernel();
+  if ((int)blockIdx.x >= cluster) return clear_rows(p, blockIdx.x - cluster, gridDim.x - cluster);   // whole clusters of them
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, rank = blockIdx.x;
   const int from = min((int64_t)rank * p.per_block, (int64_t)p.tokens), to = min((int64_t)from + p.per_block, (int64_t)p.tokens);
-  for (int64_t i = (int64_t)rank * kSortThreads + tid; i < p.used_words; i += (int64_t)cluster * kSortThreads) p.used[i] = 0;
-  for (int64_t i = (int64_t)rank * kSortThreads + tid; i < p.arrived_words; i += (int64_t)cluster * kSortThreads) p.arrived[i] = 0;
+  const bool one_turn = p.per_block <= kSortThreads * kSortItems;
   const uint32_t mask = (1u << p.digit) - 1;
   const int bins = 1 << p.digit;
-  for (int pass = 0; pass < p.passes; ++pass) {
-    const int shift = pass * p.digit, dst = (pass + 1) & 1;
-    const auto key_at = [&](int i) -> uint32_t {
-      if (pass > 0) return __ldcg(p.key[pass & 1] + i);
-      const int id = p.ids[i];
-      return id >= 0 && id < p.vocab ? id : p.vocab;
-    };
-    for (int b = tid; b < bins; b += kSortThreads) sh.total[b] = 0;
+  uint2 item[kSortItems];        // of this turn: id and token
+  uint32_t place[kSortItems];    // among the warp's tokens of the same digit
+  int source = 0, shift = 0;
+  const auto fetch = [&](int i0) {
+    const int first = i0 + warp * 32 * p.per_lane + lane;
+#pragma unroll
+    for (int j = 0; j < kSortItems; ++j) {
+      const int i = first + 32 * j;
+      if (j >= p.per_lane || i >= to) continue;
+      if (shift > 0) {
+        item[j] = __ldcg(p.item[source] + i);
+      } else {
+        const int id = p.ids[i];
+        item[j] = make_uint2(id >= 0 && id < p.vocab ? id : p.vocab, i);
+      }
+    }
+  };
+  // places of a turn's tokens, and the turn's number of each digit in one thread per digit
+  const auto rank_turn = [&](int i0) -> uint32_t {
+    for (int b = tid; b < kSortWarps * bins / 4; b += kSortThreads)
+      reinterpret_cast<uint4*>(sh.count[b * 4 / bins])[(b * 4 % bins) / 4] = make_uint4(0, 0, 0, 0);
     __syncthreads();
-    for (int i0 = from; i0 < to; i0 += kSortThreads) {
-      const int i = i0 + tid;
-      const uint32_t d = i < to ? key_at(i) >> shift & mask : kBins;
+    const int first = i0 + warp * 32 * p.per_lane + lane;
+#pragma unroll
+    for (int j = 0; j < kSortItems; ++j) {
+      if (j >= p.per_lane) break;
+      const bool on = first + 32 * j < to;
+      const uint32_t d = on ? item[j].x >> shift & mask : kBins;
       const uint32_t same = __match_any_sync(0xffffffffu, d);
-      if (d < (uint32_t)bins && lane == __ffs(same) - 1) atomicAdd(&sh.total[d], __popc(same));
+      const uint32_t prior = on ? sh.count[warp][d] : 0;
+      __syncwarp();
+      if (on && lane == __ffs(same) - 1) sh.count[warp][d] = prior + __popc(same);
+      __syncwarp();
+      place[j] = prior + __popc(same & ((1u << lane) - 1));
+    }
+    __syncthreads();
+    uint32_t sum = 0;
+    if (tid < bins) {
+      uint32_t c[kSortWarps];
+#pragma unroll
+      for (int w = 0; w < kSortWarps; ++w) c[w] = sh.count[w][tid];
+#pragma unroll
+      for (int w = 0; w < kSortWarps; ++w) {
+        sh.count[w][tid] = sum;
+        sum += c[w];
+      }
+    }
+    return sum;
+  };
+  for (int64_t i = (int64_t)rank * kSortThreads + tid; i < p.used_words; i += (int64_t)cluster * kSortThreads) p.used[i] = 0;
+  for (int pass = 0; pass < p.passes; ++pass, shift += p.digit, source = pass & 1) {
+    if (one_turn) {
+      fetch(from);
+      const uint32_t sum = rank_turn(from);
+      if (tid < bins) sh.total[tid] = sum;
+    } else {
+      for (int b = tid; b < bins; b += kSortThreads) sh.total[b] = 0;
+      __syncthreads();
+      for (int i0 = from; i0 < to; i0 += kSortThreads * kSortItems) {
+        fetch(i0);
+        const int first = i0 + warp * 32 * p.per_lane + lane;
+#pragma unroll
+        for (int j = 0; j < kSortItems; ++j) {
+          if (j >= p.per_lane) break;
+          const uint32_t d = first + 32 * j < to ? item[j].x >> shift & mask : kBins;
+          const uint32_t same = __match_any_sync(0xffffffffu, d);
+          if (d < (uint32_t)bins && lane == __ffs(same) - 1) atomicAdd(&sh.total[d], __popc(same));
+        }
+      }
     }
     if (cluster > 1) cluster_sync(); else __syncthreads();
     // exclusive sums over the digits, and within a digit over the blocks
     uint32_t before = 0, all = 0;
     if (tid < bins) {
-      for (int r = 0; r < cluster; ++r) {
-        uint32_t c;
-        if (cluster > 1) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(peer_addr(smem_addr(&sh.total[tid]), r)));
-        else c = sh.total[tid];
-        if (r < rank) before += c;
-        all += c;
+      uint32_t c[kMaxSortCluster] = {};
+#pragma unroll
+      for (int r = 0; r < kMaxSortCluster; ++r) {
+        if (r >= cluster) break;
+        if (cluster > 1) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c[r]) : "r"(peer_addr(smem_addr(&sh.total[tid]), r)));
+        else c[r] = sh.total[tid];
+      }
+#pragma unroll
+      for (int r = 0; r < kMaxSortCluster; ++r) {
+        if (r < rank) before += c[r];
+        all += c[r];
       }
     }
     uint32_t sum = all;
@@ -127,51 +216,31 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
     }
     if (lane == 31) sh.warp[warp] = sum;
     __syncthreads();
-    uint32_t ahead = 0;
-    for (int w = 0; w < warp; ++w) ahead += sh.warp[w];
-    if (tid < bins) sh.next[tid] = ahead + sum - all + before;
+    if (tid < bins) {
+      uint32_t ahead = 0;
+      for (int w = 0; w < warp; ++w) ahead += sh.warp[w];
+      sh.next[tid] = ahead + sum - all + before;
+    }
+    __syncthreads();
     for (int i0 = from; i0 < to; i0 += kSortThreads * kSortItems) {
-      for (int b = tid; b < kSortWarps * bins; b += kSortThreads) sh.count[b / bins][b % bins] = 0;
-      __syncthreads();
-      uint32_t k[kSortItems], place[kSortItems];
-      const int first = i0 + warp * 32 * kSortItems + lane;
-#pragma unroll
-      for (int j = 0; j < kSortItems; ++j) k[j] = first + 32 * j < to ? key_at(first + 32 * j) : 0;
-#pragma unroll
-      for (int j = 0; j < kSortItems; ++j) {
-        const bool on = first + 32 * j < to;
-        const uint32_t d = on ? k[j] >> shift & mask : kBins;
-        const uint32_t same = __match_any_sync(0xffffffffu, d);
-        const uint32_t prior = on ? sh.count[warp][d] : 0;
-        __syncwarp();
-        if (on && lane == __ffs(same) - 1) sh.count[warp][d] = prior + __popc(same);
-        __syncwarp();
-        place[j] = prior + __popc(same & ((1u << lane) - 1));
+      uint32_t turn = 0;
+      if (!one_turn) {
+        fetch(i0);
+        turn = rank_turn(i0);
+        __syncthreads();
       }
-      __syncthreads();
-      for (int b = tid; b < bins; b += kSortThreads) {
-        uint32_t at = sh.next[b];
-        for (int w = 0; w < kSortWarps; ++w) {
-          const uint32_t c = sh.count[w][b];
-          sh.count[w][b] = at;
-          at += c;
-        }
-        sh.next[b] = at;
-      }
-      __syncthreads();
+      const int first = i0 + warp * 32 * p.per_lane + lane;
 #pragma unroll
       for (int j = 0; j < kSortItems; ++j) {
-        const int i = first + 32 * j;
-        if (i >= to) continue;
-        const uint32_t at = sh.count[warp][k[j] >> shift & mask] + place[j];
-        p.key[dst][at] = k[j];
-        p.pos[dst][at] = pass > 0 ? __ldcg(p.pos[pass & 1] + i) : i;
-        if (pass == p.passes - 1 && k[j] < (uint32_t)p.vocab) atomicOr(&p.used[k[j] / 32], 1u << k[j] % 32);
+        if (j >= p.per_lane || first + 32 * j >= to) continue;
+        const uint32_t d = item[j].x >> shift & mask;
+        p.item[(pass + 1) & 1][sh.next[d] + sh.count[warp][d] + place[j]] = item[j];
+        if (pass == p.passes - 1 && item[j].x < (uint32_t)p.vocab) atomicOr(&p.used[item[j].x / 32], 1u << item[j].x % 32);
       }
       __syncthreads();
+      if (!one_turn && tid < bins) sh.next[tid] += turn;
     }
     // what the others have written is read in the next pass, and nobody clears counts that are still being read
-    __threadfence();
     if (cluster > 1) cluster_sync(); else __syncthreads();
   }
 }
@@ -179,9 +248,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
 // ---- sums ---------------------------------------------------------------------------------------------------
 
 struct EmbedGradParams {
-  const uint32_t *key, *pos;     // sorted
+  const uint2* item;             // sorted: id and token
   const uint32_t* used;
-  int32_t* arrived;              // [pieces][chunks]
   float* partial;                // [pieces][2][hidden]: of an id that began before the piece, of one that goes on behind it
   const void* d_out;
   void* d_table;
@@ -189,37 +257,85 @@ struct EmbedGradParams {
   int64_t vocab, hidden;
   int32_t tokens, piece, pieces, chunks;
   int accumulate;
+  int32_t first_clear;           // the first word of `used` whose rows are to be cleared here
   float scale;
 };
 
 constexpr int kMaxPiece = 128;
+constexpr int kLongRun = 32;     // ids with more tokens are cut where pieces are; the others belong to the piece where they begin
 constexpr int kClearRows = 32;   // rows of the table that a block of the second kind looks after: a word of `used`
 
-// The first of [lo, hi) in the sorted keys that is not below `key`, by all lanes of a warp.
-__device__ __forceinline__ int first_not_below(const uint32_t* keys, int lo, int hi, uint32_t key) {
-  const int lane = threadIdx.x % 32;
+// By all lanes of a warp: where the run of `id` begins that ends before `end`, and where the one ends that begins at `begin`. Most are
+// shorter than 32; the others are found by looking at 32 places at a time.
+__device__ __forceinline__ int run_begin(const uint2* item, int end, uint32_t id) {
+  const int lane = threadIdx.x % 32, near = end - 1 - lane;
+  const uint32_t other = __ballot_sync(0xffffffffu, near < 0 || item[near].x != id);
+  if (other) return end - __ffs(other) + 1;
+  int lo = 0, hi = end - 32;                       // the first of [lo, hi] that is not below: item[hi] is the id's
   while (lo < hi) {
     const int step = (hi - lo + 31) / 32, i = lo + lane * step;
-    const uint32_t below = __ballot_sync(0xffffffffu, i < hi && keys[i] < key);
-    const int n = __popc(below);      // probes below come first
+    const int n = __popc(__ballot_sync(0xffffffffu, i < hi && item[i].x < id));
     if (n == 0) return lo;
-    const int l = lo + (n - 1) * step + 1, h = min(hi, lo + n * step);
-    lo = l;
-    hi = h;
+    lo += (n - 1) * step + 1;
+    hi = min(hi, lo - 1 + step);
+  }
+  return lo;
+}
+__device__ __forceinline__ int run_end(const uint2* item, int begin, int tokens, uint32_t id) {
+  const int lane = threadIdx.x % 32, near = begin + lane;
+  const uint32_t other = __ballot_sync(0xffffffffu, near >= tokens || item[near].x != id);
+  if (other) return begin + __ffs(other) - 1;
+  int lo = begin + 32, hi = tokens;                // the first of [lo, hi] that is above
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+    const int n = __popc(__ballot_sync(0xffffffffu, i < hi && item[i].x <= id));
+    if (n == 0) return lo;
+    lo += (n - 1) * step + 1;
+    hi = min(hi, lo - 1 + step);
   }
   return lo;
 }
 
-// The first `pieces * chunks` blocks sum pieces; the others write the zeros of rows that no token has.
+// A thread's columns of a row: K vectors of V, blockDim vectors apart.
+template <int V>
+struct GradColumns {
+  static constexpr int K = vectors_per_thread<V>, N = K * V;
+  int64_t first, hidden;
+  __device__ __forceinline__ GradColumns(int chunk, int64_t hidden_) : first((int64_t)chunk * K * blockDim.x + threadIdx.x), hidden(hidden_) {}
+  __device__ __forceinline__ int64_t at(int k) const { return (first + k * blockDim.x) * V; }
+  __device__ __forceinline__ bool on(int k) const { return at(k) < hidden; }
+  // the sum, scaled and added to what is there, to a row of the table
+  template <typename G>
+  __device__ __forceinline__ void write(G* row, const float* sum, float scale, bool accumulate) const {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (!on(k)) continue;
+      float v[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] = sum[k * V + e] * scale;
+      if (accumulate) {
+        float old[V];
+        load_values<V>(row + at(k), old);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] += old[e];
+      }
+      store_values<V>(row + at(k), v);
+    }
+  }
+};
+
+// The first `pieces * chunks` blocks sum pieces; the others write the zeros of rows that no token has. A thread has four rows under way
+// while it adds the four before them.
 template <typename T, typename G, int V>
 __global__ void __launch_bounds__(kEmbedThreads) embedding_sum_kernel(const __grid_constant__ EmbedGradParams p) {
   start_after_previous_kernel();
   typedef typename Raw<T, V>::type R;
-  __shared__ uint32_t key[kMaxPiece + 2], pos[kMaxPiece];
-  __shared__ int last;
+  typedef GradColumns<V> C;
+  constexpr int U = 4, W = kLongRun;
+  __shared__ uint32_t key[kMaxPiece + 2 * W], pos[kMaxPiece + 2 * W];     // of the piece and 32 tokens on either side
   G* table = static_cast<G*>(p.d_table);
   if (blockIdx.x >= (unsigned)(p.pieces * p.chunks)) {
-    const int64_t w = blockIdx.x - p.pieces * p.chunks;
+    const int64_t w = p.first_clear + (int64_t)(blockIdx.x - p.pieces * p.chunks);
     const uint32_t used = p.used[w];
     const float zero[V] = {};
     for (int r = 0; r < kClearRows && w * kClearRows + r < p.vocab; ++r)
@@ -227,81 +343,135 @@ __global__ void __launch_bounds__(kEmbedThreads) embedding_sum_kernel(const __gr
         for (int64_t c = threadIdx.x * V; c < p.hidden; c += blockDim.x * V) store_values<V>(table + (w * kClearRows + r) * p.d_table_stride + c, zero);
     return;
   }
-  const int piece = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
-  const int from = piece * p.piece, n = min(p.piece, p.tokens - from);
-  for (int i = threadIdx.x; i < n + 2; i += blockDim.x) {     // one on either side
-    const int at = from + i - 1;
-    key[i] = at >= 0 && at < p.tokens ? p.key[at] : 0xffffffffu;
-    if (i >= 1 && i <= n) pos[i - 1] = p.pos[at];
+  const int piece = blockIdx.x / p.chunks, from = piece * p.piece, n = min(p.piece, p.tokens - from), lane = threadIdx.x % 32;
+  const uint32_t absent = (uint32_t)p.vocab;
+  for (int i = threadIdx.x; i < n + 2 * W; i += blockDim.x) {
+    const int at = from + i - W;
+    const uint2 it = at >= 0 && at < p.tokens ? p.item[at] : make_uint2(0xffffffffu, 0);
+    key[i] = it.x;
+    pos[i] = it.y;
   }
   __syncthreads();
-  const int64_t col = ((int64_t)chunk * blockDim.x + threadIdx.x) * V;
-  const bool on = col < p.hidden;
-  const T* src = static_cast<const T*>(p.d_out) + (on ? col : 0);
-  constexpr int U = 8;
-  R a[U];
-  float sum[V] = {};
-  int begin = 0;                       // of the present id within the piece
-  for (int i0 = 0; i0 < n && key[i0 + 1] < (uint32_t)p.vocab; i0 += U) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (on && i0 + u < n && key[i0 + u + 1] < (uint32_t)p.vocab) a[u] = __ldcs(reinterpret_cast<const R*>(src + pos[i0 + u] * p.d_out_stride));
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + u;
-      if (i >= n || key[i + 1] >= (uint32_t)p.vocab) break;
-      const uint32_t id = key[i + 1];
-      float v[V] = {};
-      if (on) to_floats<T, V>(a[u], v);
-#pragma unroll
-      for (int e = 0; e < V; ++e) sum[e] += v[e];
-      const bool ends = i + 1 == n;
-      if (!ends && key[i + 2] == id) continue;
-      const bool before = begin == 0 && key[0] == id, behind = ends && key[i + 2] == id;
-      bool write = true;
-      if (before || behind) {
-        const int first = before ? first_not_below(p.key, 0, from, id) / p.piece : piece;
-        const int final = behind ? (first_not_below(p.key, from + n, p.tokens, id + 1) - 1) / p.piece : piece;
-        if (on) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) p.partial[((int64_t)piece * 2 + (before ? 0 : 1)) * p.hidden + col + e] = sum[e];
-        }
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) last = atomicAdd(&p.arrived[(int64_t)first * p.chunks + chunk], 1) == final - first;
-        __syncthreads();
-        write = last;
-        if (write) {
-          __threadfence();
-          // in its first piece the id's part is in the second place, in the others in the first
-          if (on) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-              const float* at = p.partial + (int64_t)first * 2 * p.hidden + col + e;
-              float s = __ldcg(at + p.hidden);
-              for (int k = 1; k <= final - first; ++k) s += __ldcg(at + (int64_t)k * 2 * p.hidden);
-              sum[e] = s;
-            }
-          }
-        }
-      }
-      if (write && on) {
-        G* to = table + id * p.d_table_stride + col;
-#pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] *= p.scale;
-        if (p.accumulate) {
-          float old[V];
-          load_values<V>(to, old);
-#pragma unroll
-          for (int e = 0; e < V; ++e) sum[e] += old[e];
-        }
-        store_values<V>(to, sum);
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) sum[e] = 0.0f;
-      begin = i + 1;
+  // places are counted in the window: the piece is [W, end)
+  int end = W + n;
+  const uint32_t head = key[W], tail = key[end - 1];
+  if (head >= absent) return;
+  const auto same_before = [&](int at, uint32_t id) {   // up to W of them
+    const uint32_t other = __ballot_sync(0xffffffffu, key[at - 1 - lane] != id);
+    return other ? __ffs(other) - 1 : W;
+  };
+  const auto same_from = [&](int at, uint32_t id) {
+    const uint32_t other = __ballot_sync(0xffffffffu, key[at + lane] != id);
+    return other ? __ffs(other) - 1 : W;
+  };
+  int i = W, cut_head = -1;                              // where the part of a run that is cut before the piece ends
+  bool cut_tail = false;
+  const int before = same_before(W, head);
+  if (before > 0) {
+    const int here = same_from(W, head);
+    if (before + here > W) {
+      cut_head = W;
+      while (cut_head < end && key[cut_head] == head) ++cut_head;
+    } else {
+      i += here;                                         // the piece before has them
     }
   }
+  const int behind = tail < absent && !(cut_head == end) ? same_from(end, tail) : 0;
+  if (behind > 0 && i < end) {
+    const int here = min(same_before(end, tail), n);     // more than W of them: a long run
+    cut_tail = here + behind > W;
+    if (!cut_tail) end += behind;
+  }
+  const C cols((int)(blockIdx.x % p.chunks), p.hidden);
+  const T* src = static_cast<const T*>(p.d_out);
+  R buffer[2][U][C::K];
+  const auto fetch = [&](R (&a)[U][C::K], int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i0 + u >= end || key[i0 + u] >= absent) break;
+      const T* row = src + pos[i0 + u] * p.d_out_stride;
+#pragma unroll
+      for (int k = 0; k < C::K; ++k)
+        if (cols.on(k)) a[u][k] = __ldcs(reinterpret_cast<const R*>(row + cols.at(k)));
+    }
+  };
+  float sum[C::N] = {};
+  const auto add = [&](const R (&a)[U][C::K], int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = i0 + u;
+      if (at >= end || key[at] >= absent) break;
+      const uint32_t id = key[at];
+#pragma unroll
+      for (int k = 0; k < C::K; ++k) {
+        float v[V] = {};
+        if (cols.on(k)) to_floats<T, V>(a[u][k], v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[k * V + e] += v[e];
+      }
+      if (at + 1 < end && key[at + 1] == id) continue;
+      const bool began = at + 1 == cut_head, goes_on = cut_tail && at + 1 == end;
+      if (began || goes_on) {
+        float* mine = p.partial + ((int64_t)piece * 2 + (began ? 0 : 1)) * p.hidden;
+#pragma unroll
+        for (int k = 0; k < C::K; ++k)
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            if (cols.on(k)) mine[cols.at(k) + e] = sum[k * V + e];
+      } else {
+        cols.write(table + id * p.d_table_stride, sum, p.scale, p.accumulate);
+      }
+#pragma unroll
+      for (int e = 0; e < C::N; ++e) sum[e] = 0.0f;
+    }
+  };
+  fetch(buffer[0], i);
+  for (; i < end; i += 2 * U) {
+    fetch(buffer[1], i + U);
+    add(buffer[0], i);
+    fetch(buffer[0], i + 2 * U);
+    add(buffer[1], i + U);
+  }
+}
+
+// Adds the parts of the run that begins in a piece, is longer than kLongRun and goes on behind the piece, if there is one: in its first
+// piece its part is in the second place, in the others in the first.
+template <typename G, int V>
+__global__ void __launch_bounds__(kEmbedThreads) embedding_join_kernel(const __grid_constant__ EmbedGradParams p) {
+  start_after_previous_kernel();
+  typedef GradColumns<V> C;
+  const int piece = blockIdx.x / p.chunks, from = piece * p.piece, end = from + p.piece;
+  if (end >= p.tokens) return;
+  const uint32_t id = p.item[end - 1].x;
+  if (id >= (uint32_t)p.vocab || p.item[end].x != id) return;
+  const int begin = run_begin(p.item, end, id);
+  if (begin < from) return;
+  const int behind = run_end(p.item, end, p.tokens, id);
+  if (behind - begin <= kLongRun) return;
+  const int parts = (behind - 1) / p.piece - piece;    // in later pieces
+  const C cols((int)(blockIdx.x % p.chunks), p.hidden);
+  const float* at = p.partial + ((int64_t)piece * 2 + 1) * p.hidden;
+  float sum[C::N];
+#pragma unroll
+  for (int k = 0; k < C::K; ++k)
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[k * V + e] = cols.on(k) ? at[cols.at(k) + e] : 0.0f;
+  at += p.hidden;
+  constexpr int B = 8;                                 // parts under way
+  for (int q = 0; q < parts; q += B) {
+    float part[B][C::N];
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int k = 0; k < C::K; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) part[b][k * V + e] = q + b < parts && cols.on(k) ? at[(int64_t)(q + b) * 2 * p.hidden + cols.at(k) + e] : 0.0f;
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int e = 0; e < C::N; ++e) sum[e] += part[b][e];
+  }
+  cols.write(static_cast<G*>(p.d_table) + id * p.d_table_stride, sum, p.scale, p.accumulate);
 }
 
 }  // namespace slidedp
@@ -312,6 +482,9 @@ using namespace slidedp::host;
 namespace {
 
 constexpr int64_t kMaxHidden = 1 << 20;
+// What the SMs beside the sort clear of the table: about as much as they can in its time. 148 blocks of 1024 threads in all.
+constexpr int64_t kClearBytes = 64 << 20;
+constexpr int kClearBlocks = 148;
 
 int check_embedding(const slidedp_embedding_args* a) {
   const auto type = [](int32_t t) { return t == SLIDEDP_BF16 || t == SLIDEDP_F32; };
@@ -326,58 +499,63 @@ struct Split {
   int chunks;
 };
 Split split_row(int64_t hidden, int v) {
-  const int64_t vectors = (hidden + v - 1) / v;
-  const unsigned threads = vectors >= kEmbedThreads ? kEmbedThreads : (unsigned)((vectors + 31) / 32 * 32);
-  return Split{threads, (int)((vectors + threads - 1) / threads)};
+  const int64_t per = v == 1 ? vectors_per_thread<1> : v == 2 ? vectors_per_thread<2> : 1, vectors = (hidden + v - 1) / v;
+  const int64_t wanted = (vectors + per - 1) / per;
+  const unsigned threads = wanted >= kEmbedThreads ? kEmbedThreads : (unsigned)((wanted + 31) / 32 * 32);
+  return Split{threads, (int)((wanted + threads - 1) / threads)};
 }
 
 // Tokens per piece: short ones where there are few tokens, so that they fill the SMs; the partial sums are at most 2 / piece of the
 // tokens' rows in FP32.
 int piece_length(int64_t tokens) { return tokens <= 16384 ? 16 : tokens <= 131072 ? 32 : kMaxPiece; }
 
-// The workspace: sorted keys and tokens twice, the used rows' bits, counters, partial sums.
+// The workspace: ids and tokens twice, the used rows' bits, partial sums.
 struct Layout {
-  int64_t keys, used_words, arrived_words, pieces, bytes;
-  int64_t used_at, arrived_at, partial_at;
+  int64_t items, used_words, pieces, bytes;
+  int64_t used_at, partial_at;
 };
 Layout layout(const slidedp_embedding_args* a) {
   Layout l;
   const int piece = piece_length(a->tokens);
   const auto up = [](int64_t b) { return (b + 15) / 16 * 16; };
-  l.keys = up(a->tokens * 4);
+  l.items = up(a->tokens * 8);
   l.pieces = (a->tokens + piece - 1) / piece;
   l.used_words = (a->vocab + 31) / 32;
-  l.arrived_words = l.pieces * split_row(a->hidden, 1).chunks;
-  l.used_at = 4 * l.keys;
-  l.arrived_at = l.used_at + up(l.used_words * 4);
-  l.partial_at = l.arrived_at + up(l.arrived_words * 4);
+  l.used_at = 2 * l.items;
+  l.partial_at = l.used_at + up(l.used_words * 4);
   l.bytes = l.partial_at + l.pieces * 2 * a->hidden * 4;
   return l;
 }
 
-int sort_tokens(slidedp_ctx* ctx, const slidedp_embedding_args* a, const int32_t* ids, const Layout& l, char* ws, int* result, cudaStream_t st) {
+int sort_tokens(slidedp_ctx* ctx, const slidedp_embedding_args* a, const int32_t* ids, const Layout& l, const slidedp_rows* d_table,
+                int64_t clear_rows, char* ws, int* result, cudaStream_t st) {
   SortParams p = {};
   p.ids = ids;
-  for (int i = 0; i < 2; ++i) {
-    p.key[i] = reinterpret_cast<uint32_t*>(ws + i * l.keys);
-    p.pos[i] = reinterpret_cast<uint32_t*>(ws + (2 + i) * l.keys);
-  }
+  for (int i = 0; i < 2; ++i) p.item[i] = reinterpret_cast<uint2*>(ws + i * l.items);
   p.used = reinterpret_cast<uint32_t*>(ws + l.used_at);
-  p.arrived = reinterpret_cast<int32_t*>(ws + l.arrived_at);
   p.used_words = l.used_words;
-  p.arrived_words = l.arrived_words;
   p.tokens = (int32_t)a->tokens;
   p.vocab = (int32_t)a->vocab;
   int bits = 1;
   while (a->vocab >> bits) ++bits;       // the absent ones' key is vocab
   p.passes = (bits + kMaxDigit - 1) / kMaxDigit;
   p.digit = (bits + p.passes - 1) / p.passes;
+  if (p.digit < 2) p.digit = 2;          // counters are cleared by fours
   int cluster = 1;
   while (cluster < kMaxSortCluster && a->tokens > (int64_t)cluster * kSortThreads) cluster *= 2;
   p.per_block = (int32_t)((a->tokens + cluster - 1) / cluster);
+  p.per_lane = p.per_block >= kSortThreads * kSortItems ? kSortItems : (p.per_block + kSortThreads - 1) / kSortThreads;
+  const int64_t elem = elem_bytes(a->grad_dtype);
+  const uintptr_t shape = reinterpret_cast<uintptr_t>(d_table->data) | (uintptr_t)(d_table->stride * elem) | (uintptr_t)(a->hidden * elem);
+  p.clear = static_cast<char*>(d_table->data);
+  p.clear_stride = d_table->stride * elem;
+  p.clear_width = shape % 16 == 0 ? 16 : shape % 4 == 0 ? 4 : 2;
+  p.clear_vectors = (uint32_t)(a->hidden * elem / p.clear_width);
+  p.clear_rows = (uint32_t)clear_rows;
+  const int others = clear_rows > 0 ? (kClearBlocks - cluster) / cluster * cluster : 0;
   CU(cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortShared)));
   FAULT_POINT();
-  launch_after(sort_tokens_kernel, dim3(cluster), kSortThreads, sizeof(SortShared), cluster, st, p, cluster);
+  launch_after(sort_tokens_kernel, dim3(cluster + others), kSortThreads, sizeof(SortShared), cluster, st, p, cluster);
   ctx->launches += 1;
   CU_AFTER_LAUNCH();
   *result = p.passes & 1;
@@ -433,7 +611,11 @@ int slidedp_embedding_backward(slidedp_ctx* ctx, const slidedp_embedding_args* a
   const int v = vector_width(a->hidden, elem, {{d_out, elem}, {d_table, grad}});
   const Split s = split_row(a->hidden, v);
   const Layout l = layout(a);
-  const int64_t sums = l.pieces * s.chunks, blocks = sums + (a->accumulate ? 0 : l.used_words);
+  // whole words of `used`, as many as are cleared while the tokens are sorted
+  int64_t clear_words = a->accumulate ? 0 : kClearBytes / (a->hidden * grad) / kClearRows;
+  if (clear_words > l.used_words) clear_words = l.used_words;
+  const int64_t clear_rows = clear_words * kClearRows < a->vocab ? clear_words * kClearRows : a->vocab;
+  const int64_t sums = l.pieces * s.chunks, blocks = sums + (a->accumulate ? 0 : l.used_words - clear_words);
   if (blocks > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
   int rc = check_kernel_error(ctx);
   if (rc != SLIDEDP_OK) return rc;
@@ -442,13 +624,11 @@ int slidedp_embedding_backward(slidedp_ctx* ctx, const slidedp_embedding_args* a
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   char* ws = static_cast<char*>(workspace);
   int sorted;
-  rc = sort_tokens(ctx, a, ids, l, ws, &sorted, st);
+  rc = sort_tokens(ctx, a, ids, l, d_table, clear_rows, ws, &sorted, st);
   if (rc != SLIDEDP_OK) return rc;
   EmbedGradParams p = {};
-  p.key = reinterpret_cast<uint32_t*>(ws + sorted * l.keys);
-  p.pos = reinterpret_cast<uint32_t*>(ws + (2 + sorted) * l.keys);
+  p.item = reinterpret_cast<const uint2*>(ws + sorted * l.items);
   p.used = reinterpret_cast<uint32_t*>(ws + l.used_at);
-  p.arrived = reinterpret_cast<int32_t*>(ws + l.arrived_at);
   p.partial = reinterpret_cast<float*>(ws + l.partial_at);
   p.d_out = d_out->data;
   p.d_table = d_table->data;
@@ -462,18 +642,29 @@ int slidedp_embedding_backward(slidedp_ctx* ctx, const slidedp_embedding_args* a
   p.chunks = s.chunks;
   p.accumulate = a->accumulate;
   p.scale = (float)a->scale;
-  FAULT_POINT();
-  const auto run = [&](auto kernel) { launch_after(kernel, dim3((unsigned)blocks), s.threads, 0, 1, st, p); };
-  if (elem == 4) {
-    if (grad == 4) v == 4 ? run(embedding_sum_kernel<float, float, 4>) : run(embedding_sum_kernel<float, float, 1>);
-    else v == 4 ? run(embedding_sum_kernel<float, uint16_t, 4>) : run(embedding_sum_kernel<float, uint16_t, 1>);
-  } else if (grad == 4) {
-    v == 8 ? run(embedding_sum_kernel<uint16_t, float, 8>) : v == 2 ? run(embedding_sum_kernel<uint16_t, float, 2>) : run(embedding_sum_kernel<uint16_t, float, 1>);
-  } else {
-    v == 8 ? run(embedding_sum_kernel<uint16_t, uint16_t, 8>) : v == 2 ? run(embedding_sum_kernel<uint16_t, uint16_t, 2>) : run(embedding_sum_kernel<uint16_t, uint16_t, 1>);
+  p.first_clear = (int32_t)clear_words;
+  if (blocks > 0) {
+    FAULT_POINT();
+    const auto run = [&](auto kernel) { launch_after(kernel, dim3((unsigned)blocks), s.threads, 0, 1, st, p); };
+    if (elem == 4) {
+      if (grad == 4) v == 4 ? run(embedding_sum_kernel<float, float, 4>) : run(embedding_sum_kernel<float, float, 1>);
+      else v == 4 ? run(embedding_sum_kernel<float, uint16_t, 4>) : run(embedding_sum_kernel<float, uint16_t, 1>);
+    } else if (grad == 4) {
+      v == 8 ? run(embedding_sum_kernel<uint16_t, float, 8>) : v == 2 ? run(embedding_sum_kernel<uint16_t, float, 2>) : run(embedding_sum_kernel<uint16_t, float, 1>);
+    } else {
+      v == 8 ? run(embedding_sum_kernel<uint16_t, uint16_t, 8>) : v == 2 ? run(embedding_sum_kernel<uint16_t, uint16_t, 2>) : run(embedding_sum_kernel<uint16_t, uint16_t, 1>);
+    }
+    ctx->launches += 1;
+    CU_AFTER_LAUNCH();
   }
-  ctx->launches += 1;
-  CU_AFTER_LAUNCH();
+  if (a->tokens > kLongRun && l.pieces > 1) {
+    FAULT_POINT();
+    const auto join = [&](auto kernel) { launch_after(kernel, dim3((unsigned)sums), s.threads, 0, 1, st, p); };
+    if (grad == 4) v == 8 ? join(embedding_join_kernel<float, 8>) : v == 4 ? join(embedding_join_kernel<float, 4>) : v == 2 ? join(embedding_join_kernel<float, 2>) : join(embedding_join_kernel<float, 1>);
+    else v == 8 ? join(embedding_join_kernel<uint16_t, 8>) : v == 4 ? join(embedding_join_kernel<uint16_t, 4>) : v == 2 ? join(embedding_join_kernel<uint16_t, 2>) : join(embedding_join_kernel<uint16_t, 1>);
+    ctx->launches += 1;
+    CU_AFTER_LAUNCH();
+  }
   return SLIDEDP_OK;
 }
 
