@@ -82,6 +82,7 @@ struct SortParams {
   const int32_t* ids;
   uint2* item[2];                // ids (vocab: absent) and their tokens, sorted in [passes % 2]
   uint32_t* used;                // a bit per row of the table
+  int32_t* cut;                  // how many runs are cut
   int64_t used_words;
   int32_t tokens, vocab, per_block, per_lane;
   int passes, digit;
@@ -95,13 +96,14 @@ struct SortShared {
   uint32_t total[kBins];               // of this block
   uint32_t next[kBins];                // where the next of each digit goes
   uint32_t warp[kSortWarps];
+  uint2 moved[kSortThreads * kSortItems];   // this block's part of the list between two passes, if it is one turn
 };
 
 // Sorts by digits of up to nine bits, the lowest first, in one cluster whatever the number of tokens: each block has a contiguous
 // part of the list. A pass counts the digits, exchanges the counts through distributed shared memory, and moves the tokens in
-// turns of 4096: a warp finds equal digits among its lanes, and the counts per warp give every token its place. A block whose part is
-// one turn finds the places first and has its counts from them. Bound: latency of its steps, a handful of barriers and trips to
-// L2 per pass.
+// turns of 4096: a warp finds equal digits among its lanes, and the counts per warp give every token its place. Blocks whose part is
+// one turn find the places first and have their counts from them, and pass tokens on through each other's shared memory. Bound:
+// latency of its steps, a barrier of the cluster being 1 us: 32749 tokens, two passes, SORT_US us.
 __device__ __forceinline__ void clear_rows(const SortParams& p, uint32_t block, uint32_t blocks) {
   const uint32_t all = p.clear_rows * p.clear_vectors;
   for (uint32_t i = block * kSortThreads + threadIdx.x; i < all; i += blocks * kSortThreads) {
@@ -131,7 +133,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
       const int i = first + 32 * j;
       if (j >= p.per_lane || i >= to) continue;
       if (shift > 0) {
-        item[j] = __ldcg(p.item[source] + i);
+        item[j] = one_turn ? sh.moved[i - from] : __ldcg(p.item[source] + i);
       } else {
         const int id = p.ids[i];
         item[j] = make_uint2(id >= 0 && id < p.vocab ? id : p.vocab, i);
@@ -144,17 +146,20 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
       reinterpret_cast<uint4*>(sh.count[b * 4 / bins])[(b * 4 % bins) / 4] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     const int first = i0 + warp * 32 * p.per_lane + lane;
+    uint32_t same[kSortItems];
+#pragma unroll
+    for (int j = 0; j < kSortItems; ++j)
+      if (j < p.per_lane) same[j] = __match_any_sync(0xffffffffu, first + 32 * j < to ? item[j].x >> shift & mask : kBins);
 #pragma unroll
     for (int j = 0; j < kSortItems; ++j) {
       if (j >= p.per_lane) break;
       const bool on = first + 32 * j < to;
-      const uint32_t d = on ? item[j].x >> shift & mask : kBins;
-      const uint32_t same = __match_any_sync(0xffffffffu, d);
+      const uint32_t d = item[j].x >> shift & mask;
       const uint32_t prior = on ? sh.count[warp][d] : 0;
       __syncwarp();
-      if (on && lane == __ffs(same) - 1) sh.count[warp][d] = prior + __popc(same);
+      if (on && lane == __ffs(same[j]) - 1) sh.count[warp][d] = prior + __popc(same[j]);
       __syncwarp();
-      place[j] = prior + __popc(same & ((1u << lane) - 1));
+      place[j] = prior + __popc(same[j] & ((1u << lane) - 1));
     }
     __syncthreads();
     uint32_t sum = 0;
@@ -170,6 +175,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
     }
     return sum;
   };
+  if (rank == 0 && tid == 0) *p.cut = 0;
   for (int64_t i = (int64_t)rank * kSortThreads + tid; i < p.used_words; i += (int64_t)cluster * kSortThreads) p.used[i] = 0;
   for (int pass = 0; pass < p.passes; ++pass, shift += p.digit, source = pass & 1) {
     if (one_turn) {
@@ -233,16 +239,28 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
 #pragma unroll
       for (int j = 0; j < kSortItems; ++j) {
         if (j >= p.per_lane || first + 32 * j >= to) continue;
-        const uint32_t d = item[j].x >> shift & mask;
-        p.item[(pass + 1) & 1][sh.next[d] + sh.count[warp][d] + place[j]] = item[j];
-        if (pass == p.passes - 1 && item[j].x < (uint32_t)p.vocab) atomicOr(&p.used[item[j].x / 32], 1u << item[j].x % 32);
+        const uint32_t d = item[j].x >> shift & mask, at = sh.next[d] + sh.count[warp][d] + place[j];
+        if (!one_turn || pass == p.passes - 1) {
+          p.item[(pass + 1) & 1][at] = item[j];
+        } else if (cluster > 1) {
+          const uint32_t there = peer_addr(smem_addr(&sh.moved[at % (uint32_t)p.per_block]), at / (uint32_t)p.per_block);
+          asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(there), "r"(item[j].x), "r"(item[j].y) : "memory");
+        } else {
+          sh.moved[at] = item[j];
+        }
       }
       __syncthreads();
       if (!one_turn && tid < bins) sh.next[tid] += turn;
     }
-    // what the others have written is read in the next pass, and nobody clears counts that are still being read
+    // what the others have written is read in the next pass, and nobody clears counts that are still being read, or leaves
     if (cluster > 1) cluster_sync(); else __syncthreads();
   }
+  // the rows that are used, by the first token of each
+  if (p.used_words > 0)
+    for (int i = from + tid; i < to; i += kSortThreads) {
+      const uint32_t id = __ldcg(p.item[source] + i).x;
+      if (id < (uint32_t)p.vocab && (i == 0 || __ldcg(p.item[source] + i - 1).x != id)) atomicOr(&p.used[id / 32], 1u << id % 32);
+    }
 }
 
 // ---- sums ---------------------------------------------------------------------------------------------------
@@ -250,6 +268,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const __grid_
 struct EmbedGradParams {
   const uint2* item;             // sorted: id and token
   const uint32_t* used;
+  int32_t* cut;                  // how many runs are cut, then the pieces where they begin, in any order
   float* partial;                // [pieces][2][hidden]: of an id that began before the piece, of one that goes on behind it
   const void* d_out;
   void* d_table;
@@ -265,22 +284,8 @@ constexpr int kMaxPiece = 128;
 constexpr int kLongRun = 32;     // ids with more tokens are cut where pieces are; the others belong to the piece where they begin
 constexpr int kClearRows = 32;   // rows of the table that a block of the second kind looks after: a word of `used`
 
-// By all lanes of a warp: where the run of `id` begins that ends before `end`, and where the one ends that begins at `begin`. Most are
-// shorter than 32; the others are found by looking at 32 places at a time.
-__device__ __forceinline__ int run_begin(const uint2* item, int end, uint32_t id) {
-  const int lane = threadIdx.x % 32, near = end - 1 - lane;
-  const uint32_t other = __ballot_sync(0xffffffffu, near < 0 || item[near].x != id);
-  if (other) return end - __ffs(other) + 1;
-  int lo = 0, hi = end - 32;                       // the first of [lo, hi] that is not below: item[hi] is the id's
-  while (lo < hi) {
-    const int step = (hi - lo + 31) / 32, i = lo + lane * step;
-    const int n = __popc(__ballot_sync(0xffffffffu, i < hi && item[i].x < id));
-    if (n == 0) return lo;
-    lo += (n - 1) * step + 1;
-    hi = min(hi, lo - 1 + step);
-  }
-  return lo;
-}
+// By all lanes of a warp: where the run of `id` ends that has `begin`. Most end within 32 places; the others are found by looking at 32
+// places at a time.
 __device__ __forceinline__ int run_end(const uint2* item, int begin, int tokens, uint32_t id) {
   const int lane = threadIdx.x % 32, near = begin + lane;
   const uint32_t other = __ballot_sync(0xffffffffu, near >= tokens || item[near].x != id);
@@ -296,33 +301,26 @@ __device__ __forceinline__ int run_end(const uint2* item, int begin, int tokens,
   return lo;
 }
 
-// A thread's columns of a row: K vectors of V, blockDim vectors apart.
-template <int V>
-struct GradColumns {
-  static constexpr int K = vectors_per_thread<V>, N = K * V;
-  int64_t first, hidden;
-  __device__ __forceinline__ GradColumns(int chunk, int64_t hidden_) : first((int64_t)chunk * K * blockDim.x + threadIdx.x), hidden(hidden_) {}
-  __device__ __forceinline__ int64_t at(int k) const { return (first + k * blockDim.x) * V; }
-  __device__ __forceinline__ bool on(int k) const { return at(k) < hidden; }
-  // the sum, scaled and added to what is there, to a row of the table
-  template <typename G>
-  __device__ __forceinline__ void write(G* row, const float* sum, float scale, bool accumulate) const {
+// A thread's columns of a row are K vectors of V, `step` vectors apart from `first` on. Their sums, scaled and added to what is there, to a
+// row of the table.
+template <typename G, int V>
+__device__ __forceinline__ void write_columns(G* row, int64_t first, int step, int64_t hidden, const float* sum, float scale, bool accumulate) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (!on(k)) continue;
-      float v[V];
+  for (int k = 0; k < vectors_per_thread<V>; ++k) {
+    const int64_t col = (first + k * step) * V;
+    if (col >= hidden) continue;
+    float v[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = sum[k * V + e] * scale;
-      if (accumulate) {
-        float old[V];
-        load_values<V>(row + at(k), old);
+    for (int e = 0; e < V; ++e) v[e] = sum[k * V + e] * scale;
+    if (accumulate) {
+      float old[V];
+      load_values<V>(row + col, old);
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] += old[e];
-      }
-      store_values<V>(row + at(k), v);
+      for (int e = 0; e < V; ++e) v[e] += old[e];
     }
+    store_values<V>(row + col, v);
   }
-};
+}
 
 // The first `pieces * chunks` blocks sum pieces; the others write the zeros of rows that no token has. A thread has four rows under way
 // while it adds the four before them.
@@ -330,8 +328,7 @@ template <typename T, typename G, int V>
 __global__ void __launch_bounds__(kEmbedThreads) embedding_sum_kernel(const __grid_constant__ EmbedGradParams p) {
   start_after_previous_kernel();
   typedef typename Raw<T, V>::type R;
-  typedef GradColumns<V> C;
-  constexpr int U = 4, W = kLongRun;
+  constexpr int K = vectors_per_thread<V>, N = K * V, U = 4, W = kLongRun;
   __shared__ uint32_t key[kMaxPiece + 2 * W], pos[kMaxPiece + 2 * W];     // of the piece and 32 tokens on either side
   G* table = static_cast<G*>(p.d_table);
   if (blockIdx.x >= (unsigned)(p.pieces * p.chunks)) {
@@ -382,47 +379,49 @@ __global__ void __launch_bounds__(kEmbedThreads) embedding_sum_kernel(const __gr
     cut_tail = here + behind > W;
     if (!cut_tail) end += behind;
   }
-  const C cols((int)(blockIdx.x % p.chunks), p.hidden);
+  const int64_t first = (int64_t)(blockIdx.x % p.chunks) * K * blockDim.x + threadIdx.x;
+  const auto col = [&](int k) { return (first + k * blockDim.x) * V; };
   const T* src = static_cast<const T*>(p.d_out);
-  R buffer[2][U][C::K];
-  const auto fetch = [&](R (&a)[U][C::K], int i0) {
+  R buffer[2][U][K];
+  const auto fetch = [&](R (&a)[U][K], int i0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i0 + u >= end || key[i0 + u] >= absent) break;
       const T* row = src + pos[i0 + u] * p.d_out_stride;
 #pragma unroll
-      for (int k = 0; k < C::K; ++k)
-        if (cols.on(k)) a[u][k] = __ldcs(reinterpret_cast<const R*>(row + cols.at(k)));
+      for (int k = 0; k < K; ++k)
+        if (col(k) < p.hidden) a[u][k] = __ldcs(reinterpret_cast<const R*>(row + col(k)));
     }
   };
-  float sum[C::N] = {};
-  const auto add = [&](const R (&a)[U][C::K], int i0) {
+  float sum[N] = {};
+  const auto add = [&](const R (&a)[U][K], int i0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = i0 + u;
       if (at >= end || key[at] >= absent) break;
       const uint32_t id = key[at];
 #pragma unroll
-      for (int k = 0; k < C::K; ++k) {
+      for (int k = 0; k < K; ++k) {
         float v[V] = {};
-        if (cols.on(k)) to_floats<T, V>(a[u][k], v);
+        if (col(k) < p.hidden) to_floats<T, V>(a[u][k], v);
 #pragma unroll
         for (int e = 0; e < V; ++e) sum[k * V + e] += v[e];
       }
       if (at + 1 < end && key[at + 1] == id) continue;
       const bool began = at + 1 == cut_head, goes_on = cut_tail && at + 1 == end;
+      if (goes_on && blockIdx.x % p.chunks == 0 && threadIdx.x == 0) p.cut[1 + atomicAdd(p.cut, 1)] = piece;
       if (began || goes_on) {
         float* mine = p.partial + ((int64_t)piece * 2 + (began ? 0 : 1)) * p.hidden;
 #pragma unroll
-        for (int k = 0; k < C::K; ++k)
+        for (int k = 0; k < K; ++k)
 #pragma unroll
           for (int e = 0; e < V; ++e)
-            if (cols.on(k)) mine[cols.at(k) + e] = sum[k * V + e];
+            if (col(k) < p.hidden) mine[col(k) + e] = sum[k * V + e];
       } else {
-        cols.write(table + id * p.d_table_stride, sum, p.scale, p.accumulate);
+        write_columns<G, V>(table + id * p.d_table_stride, first, blockDim.x, p.hidden, sum, p.scale, p.accumulate);
       }
 #pragma unroll
-      for (int e = 0; e < C::N; ++e) sum[e] = 0.0f;
+      for (int e = 0; e < N; ++e) sum[e] = 0.0f;
     }
   };
   fetch(buffer[0], i);
@@ -434,44 +433,50 @@ __global__ void __launch_bounds__(kEmbedThreads) embedding_sum_kernel(const __gr
   }
 }
 
-// Adds the parts of the run that begins in a piece, is longer than kLongRun and goes on behind the piece, if there is one: in its first
-// piece its part is in the second place, in the others in the first.
+// Adds the parts of the runs that are cut: in its first piece a run's part is in the second place, in the others in the first. A block has
+// the columns of one of its warps; the warps share the parts, and the first adds up what they have.
 template <typename G, int V>
-__global__ void __launch_bounds__(kEmbedThreads) embedding_join_kernel(const __grid_constant__ EmbedGradParams p) {
+__global__ void __launch_bounds__(kEmbedThreads) embedding_join_kernel(const __grid_constant__ EmbedGradParams p, int chunks) {
   start_after_previous_kernel();
-  typedef GradColumns<V> C;
-  const int piece = blockIdx.x / p.chunks, from = piece * p.piece, end = from + p.piece;
-  if (end >= p.tokens) return;
-  const uint32_t id = p.item[end - 1].x;
-  if (id >= (uint32_t)p.vocab || p.item[end].x != id) return;
-  const int begin = run_begin(p.item, end, id);
-  if (begin < from) return;
-  const int behind = run_end(p.item, end, p.tokens, id);
-  if (behind - begin <= kLongRun) return;
-  const int parts = (behind - 1) / p.piece - piece;    // in later pieces
-  const C cols((int)(blockIdx.x % p.chunks), p.hidden);
-  const float* at = p.partial + ((int64_t)piece * 2 + 1) * p.hidden;
-  float sum[C::N];
+  constexpr int K = vectors_per_thread<V>, N = K * V, kWarps = kEmbedThreads / 32;
+  __shared__ float sums[kWarps][N][32];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  for (int work = blockIdx.x; work < p.cut[0] * chunks; work += gridDim.x) {
+    const int piece = p.cut[1 + work / chunks], end = (piece + 1) * p.piece;
+    const uint32_t id = p.item[end - 1].x;
+    const int parts = (run_end(p.item, end, p.tokens, id) - 1) / p.piece - piece + 1, each = (parts + kWarps - 1) / kWarps;
+    const int64_t first = (int64_t)(work % chunks) * K * 32 + lane;
+    const auto col = [&](int k) { return (first + k * 32) * V; };
+    float sum[N] = {};
+    constexpr int B = 8;                                 // parts under way
+    const int stop = min(parts, (warp + 1) * each);
+    for (int q = warp * each; q < stop; q += B) {
+      float part[B][N];
 #pragma unroll
-  for (int k = 0; k < C::K; ++k)
+      for (int b = 0; b < B; ++b) {
+        const float* at = p.partial + ((int64_t)(piece + q + b) * 2 + (q + b == 0)) * p.hidden;
 #pragma unroll
-    for (int e = 0; e < V; ++e) sum[k * V + e] = cols.on(k) ? at[cols.at(k) + e] : 0.0f;
-  at += p.hidden;
-  constexpr int B = 8;                                 // parts under way
-  for (int q = 0; q < parts; q += B) {
-    float part[B][C::N];
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int b = 0; b < B; ++b)
+          for (int e = 0; e < V; ++e) part[b][k * V + e] = q + b < stop && col(k) < p.hidden ? at[col(k) + e] : 0.0f;
+      }
 #pragma unroll
-      for (int k = 0; k < C::K; ++k)
+      for (int b = 0; b < B; ++b)
 #pragma unroll
-        for (int e = 0; e < V; ++e) part[b][k * V + e] = q + b < parts && cols.on(k) ? at[(int64_t)(q + b) * 2 * p.hidden + cols.at(k) + e] : 0.0f;
+        for (int e = 0; e < N; ++e) sum[e] += part[b][e];
+    }
 #pragma unroll
-    for (int b = 0; b < B; ++b)
+    for (int e = 0; e < N; ++e) sums[warp][e][lane] = sum[e];
+    __syncthreads();
+    if (warp == 0) {
 #pragma unroll
-      for (int e = 0; e < C::N; ++e) sum[e] += part[b][e];
+      for (int w = 1; w < kWarps; ++w)
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] += sums[w][e][lane];
+      write_columns<G, V>(static_cast<G*>(p.d_table) + id * p.d_table_stride, first, 32, p.hidden, sum, p.scale, p.accumulate);
+    }
+    __syncthreads();
   }
-  cols.write(static_cast<G*>(p.d_table) + id * p.d_table_stride, sum, p.scale, p.accumulate);
 }
 
 }  // namespace slidedp
@@ -484,7 +489,7 @@ namespace {
 constexpr int64_t kMaxHidden = 1 << 20;
 // What the SMs beside the sort clear of the table: about as much as they can in its time. 148 blocks of 1024 threads in all.
 constexpr int64_t kClearBytes = 64 << 20;
-constexpr int kClearBlocks = 148;
+constexpr int kSms = 148, kClearBlocks = kSms;
 
 int check_embedding(const slidedp_embedding_args* a) {
   const auto type = [](int32_t t) { return t == SLIDEDP_BF16 || t == SLIDEDP_F32; };
@@ -505,35 +510,42 @@ Split split_row(int64_t hidden, int v) {
   return Split{threads, (int)((wanted + threads - 1) / threads)};
 }
 
-// Tokens per piece: short ones where there are few tokens, so that they fill the SMs; the partial sums are at most 2 / piece of the
+// Tokens per piece: as many as make the pieces' blocks one round of the device, 16 to 128. The partial sums are at most 2 / piece of the
 // tokens' rows in FP32.
-int piece_length(int64_t tokens) { return tokens <= 16384 ? 16 : tokens <= 131072 ? 32 : kMaxPiece; }
+int piece_length(const slidedp_embedding_args* a) {
+  const int64_t blocks = a->tokens * split_row(a->hidden, 16 / elem_bytes(a->dtype)).chunks;
+  int p = 16;
+  while (p < kMaxPiece && blocks > (int64_t)p * kSms * 8) p *= 2;
+  return p;
+}
 
-// The workspace: ids and tokens twice, the used rows' bits, partial sums.
+// The workspace: ids and tokens twice, the used rows' bits, the pieces where runs are cut, partial sums.
 struct Layout {
   int64_t items, used_words, pieces, bytes;
-  int64_t used_at, partial_at;
+  int64_t used_at, cut_at, partial_at;
 };
 Layout layout(const slidedp_embedding_args* a) {
   Layout l;
-  const int piece = piece_length(a->tokens);
+  const int piece = piece_length(a);
   const auto up = [](int64_t b) { return (b + 15) / 16 * 16; };
   l.items = up(a->tokens * 8);
   l.pieces = (a->tokens + piece - 1) / piece;
   l.used_words = (a->vocab + 31) / 32;
   l.used_at = 2 * l.items;
-  l.partial_at = l.used_at + up(l.used_words * 4);
+  l.cut_at = l.used_at + up(l.used_words * 4);
+  l.partial_at = l.cut_at + up((l.pieces + 1) * 4);
   l.bytes = l.partial_at + l.pieces * 2 * a->hidden * 4;
   return l;
 }
 
 int sort_tokens(slidedp_ctx* ctx, const slidedp_embedding_args* a, const int32_t* ids, const Layout& l, const slidedp_rows* d_table,
-                int64_t clear_rows, char* ws, int* result, cudaStream_t st) {
+                int64_t clear_rows, bool all_cleared, char* ws, int* result, cudaStream_t st) {
   SortParams p = {};
   p.ids = ids;
   for (int i = 0; i < 2; ++i) p.item[i] = reinterpret_cast<uint2*>(ws + i * l.items);
   p.used = reinterpret_cast<uint32_t*>(ws + l.used_at);
-  p.used_words = l.used_words;
+  p.used_words = all_cleared ? 0 : l.used_words;
+  p.cut = reinterpret_cast<int32_t*>(ws + l.cut_at);
   p.tokens = (int32_t)a->tokens;
   p.vocab = (int32_t)a->vocab;
   int bits = 1;
@@ -624,12 +636,13 @@ int slidedp_embedding_backward(slidedp_ctx* ctx, const slidedp_embedding_args* a
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   char* ws = static_cast<char*>(workspace);
   int sorted;
-  rc = sort_tokens(ctx, a, ids, l, d_table, clear_rows, ws, &sorted, st);
+  rc = sort_tokens(ctx, a, ids, l, d_table, clear_rows, a->accumulate || clear_words == l.used_words, ws, &sorted, st);
   if (rc != SLIDEDP_OK) return rc;
   EmbedGradParams p = {};
   p.item = reinterpret_cast<const uint2*>(ws + sorted * l.items);
   p.used = reinterpret_cast<uint32_t*>(ws + l.used_at);
   p.partial = reinterpret_cast<float*>(ws + l.partial_at);
+  p.cut = reinterpret_cast<int32_t*>(ws + l.cut_at);
   p.d_out = d_out->data;
   p.d_table = d_table->data;
   p.d_out_stride = d_out->stride;
@@ -637,7 +650,7 @@ int slidedp_embedding_backward(slidedp_ctx* ctx, const slidedp_embedding_args* a
   p.vocab = a->vocab;
   p.hidden = a->hidden;
   p.tokens = (int32_t)a->tokens;
-  p.piece = piece_length(a->tokens);
+  p.piece = piece_length(a);
   p.pieces = (int32_t)l.pieces;
   p.chunks = s.chunks;
   p.accumulate = a->accumulate;
@@ -659,7 +672,9 @@ int slidedp_embedding_backward(slidedp_ctx* ctx, const slidedp_embedding_args* a
   }
   if (a->tokens > kLongRun && l.pieces > 1) {
     FAULT_POINT();
-    const auto join = [&](auto kernel) { launch_after(kernel, dim3((unsigned)sums), s.threads, 0, 1, st, p); };
+    const int64_t columns = 32 * v * (v == 1 ? vectors_per_thread<1> : v == 2 ? vectors_per_thread<2> : 1), chunks = (a->hidden + columns - 1) / columns;
+    const int64_t most = a->tokens / (kLongRun + 1) * chunks, joins = most < kSms * 8 ? most : kSms * 8;
+    const auto join = [&](auto kernel) { launch_after(kernel, dim3((unsigned)joins), kEmbedThreads, 0, 1, st, p, (int)chunks); };
     if (grad == 4) v == 8 ? join(embedding_join_kernel<float, 8>) : v == 4 ? join(embedding_join_kernel<float, 4>) : v == 2 ? join(embedding_join_kernel<float, 2>) : join(embedding_join_kernel<float, 1>);
     else v == 8 ? join(embedding_join_kernel<uint16_t, 8>) : v == 4 ? join(embedding_join_kernel<uint16_t, 4>) : v == 2 ? join(embedding_join_kernel<uint16_t, 2>) : join(embedding_join_kernel<uint16_t, 1>);
     ctx->launches += 1;
