@@ -330,6 +330,8 @@ __global__ void __launch_bounds__(kEmbedThreads) embedding_sum_kernel(const __gr
   typedef typename Raw<T, V>::type R;
   constexpr int K = vectors_per_thread<V>, N = K * V, U = 4, W = kLongRun;
   __shared__ uint32_t key[kMaxPiece + 2 * W], pos[kMaxPiece + 2 * W];     // of the piece and 32 tokens on either side
+  __shared__ int64_t offset[kMaxPiece + 2 * W];
+  __shared__ uint8_t what[kMaxPiece + 2 * W];
   G* table = static_cast<G*>(p.d_table);
   if (blockIdx.x >= (unsigned)(p.pieces * p.chunks)) {
     const int64_t w = p.first_clear + (int64_t)(blockIdx.x - p.pieces * p.chunks);
@@ -349,10 +351,18 @@ __global__ void __launch_bounds__(kEmbedThreads) embedding_sum_kernel(const __gr
     pos[i] = it.y;
   }
   __syncthreads();
-  // places are counted in the window: the piece is [W, end)
+  // places are counted in the window: the piece is [W, end), less absent tokens, which come last
   int end = W + n;
-  const uint32_t head = key[W], tail = key[end - 1];
+  const uint32_t head = key[W];
   if (head >= absent) return;
+  for (int at = W; at < W + n; at += 32) {
+    const uint32_t none = __ballot_sync(0xffffffffu, at + lane < W + n && key[at + lane] >= absent);
+    if (none) {
+      end = at + __ffs(none) - 1;
+      break;
+    }
+  }
+  const uint32_t tail = key[end - 1];
   const auto same_before = [&](int at, uint32_t id) {   // up to W of them
     const uint32_t other = __ballot_sync(0xffffffffu, key[at - 1 - lane] != id);
     return other ? __ffs(other) - 1 : W;
@@ -361,36 +371,39 @@ __global__ void __launch_bounds__(kEmbedThreads) embedding_sum_kernel(const __gr
     const uint32_t other = __ballot_sync(0xffffffffu, key[at + lane] != id);
     return other ? __ffs(other) - 1 : W;
   };
-  int i = W, cut_head = -1;                              // where the part of a run that is cut before the piece ends
-  bool cut_tail = false;
+  int i = W;
+  bool cut_head = false, cut_tail = false;               // the part of the first run belongs to one that is cut before; of the last, behind
   const int before = same_before(W, head);
   if (before > 0) {
     const int here = same_from(W, head);
-    if (before + here > W) {
-      cut_head = W;
-      while (cut_head < end && key[cut_head] == head) ++cut_head;
-    } else {
-      i += here;                                         // the piece before has them
-    }
+    cut_head = before + here > W;
+    if (!cut_head) i += here;                            // the piece before has them
   }
-  const int behind = tail < absent && !(cut_head == end) ? same_from(end, tail) : 0;
+  const int behind = cut_head && tail == head ? 0 : same_from(end, tail);
   if (behind > 0 && i < end) {
     const int here = min(same_before(end, tail), n);     // more than W of them: a long run
     cut_tail = here + behind > W;
     if (!cut_tail) end += behind;
   }
+  if (i >= end) return;
+  // where each token's row is, and what is to be done after it: nothing yet, the run's sum to the table, or to one of the two places
+  for (int at = i + threadIdx.x; at < end; at += blockDim.x) {
+    const bool last = at + 1 == end || key[at + 1] != key[at];
+    offset[at] = pos[at] * p.d_out_stride;
+    what[at] = !last ? 0 : cut_head && key[at] == head ? 2 : cut_tail && at + 1 == end ? 3 : 1;
+  }
+  __syncthreads();
   const int64_t first = (int64_t)(blockIdx.x % p.chunks) * K * blockDim.x + threadIdx.x;
   const auto col = [&](int k) { return (first + k * blockDim.x) * V; };
   const T* src = static_cast<const T*>(p.d_out);
   R buffer[2][U][K];
-  const auto fetch = [&](R (&a)[U][K], int i0) {
+  const auto fetch = [&](R (&a)[U][K], int i0) {          // behind the end the last one again
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i0 + u >= end || key[i0 + u] >= absent) break;
-      const T* row = src + pos[i0 + u] * p.d_out_stride;
+      const T* row = src + offset[min(i0 + u, end - 1)];
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (col(k) < p.hidden) a[u][k] = __ldcs(reinterpret_cast<const R*>(row + col(k)));
+        if (col(k) < p.hidden) a[u][k] = __ldg(reinterpret_cast<const R*>(row + col(k)));
     }
   };
   float sum[N] = {};
@@ -398,8 +411,7 @@ __global__ void __launch_bounds__(kEmbedThreads) embedding_sum_kernel(const __gr
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = i0 + u;
-      if (at >= end || key[at] >= absent) break;
-      const uint32_t id = key[at];
+      if (at >= end) break;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         float v[V] = {};
@@ -407,18 +419,18 @@ __global__ void __launch_bounds__(kEmbedThreads) embedding_sum_kernel(const __gr
 #pragma unroll
         for (int e = 0; e < V; ++e) sum[k * V + e] += v[e];
       }
-      if (at + 1 < end && key[at + 1] == id) continue;
-      const bool began = at + 1 == cut_head, goes_on = cut_tail && at + 1 == end;
-      if (goes_on && blockIdx.x % p.chunks == 0 && threadIdx.x == 0) p.cut[1 + atomicAdd(p.cut, 1)] = piece;
-      if (began || goes_on) {
-        float* mine = p.partial + ((int64_t)piece * 2 + (began ? 0 : 1)) * p.hidden;
+      const int todo = what[at];
+      if (todo == 0) continue;
+      if (todo == 1) {
+        write_columns<G, V>(table + key[at] * p.d_table_stride, first, blockDim.x, p.hidden, sum, p.scale, p.accumulate);
+      } else {
+        if (todo == 3 && blockIdx.x % p.chunks == 0 && threadIdx.x == 0) p.cut[1 + atomicAdd(p.cut, 1)] = piece;
+        float* mine = p.partial + ((int64_t)piece * 2 + (todo - 2)) * p.hidden;
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
           for (int e = 0; e < V; ++e)
             if (col(k) < p.hidden) mine[col(k) + e] = sum[k * V + e];
-      } else {
-        write_columns<G, V>(table + id * p.d_table_stride, first, blockDim.x, p.hidden, sum, p.scale, p.accumulate);
       }
 #pragma unroll
       for (int e = 0; e < N; ++e) sum[e] = 0.0f;
