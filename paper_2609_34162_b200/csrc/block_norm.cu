@@ -253,10 +253,14 @@ __global__ void __launch_bounds__(kThreads) block_norm_backward_kernel(const __g
 }
 
 // ---- rows in shared memory ---------------------------------------------------------------------------------
-// Rows are copied in bulk into a ring ahead of their use, so that what is under way costs no registers. A thread has 16 columns of
-// every row: 16-byte vectors where rows are aligned to them, else single columns, neighbours with neighbouring threads. The factors
-// of y r and of x' r' lie behind the ring in FP32. Two values per instruction. Measured before (rows in registers, no copies ahead):
-// 8192 x 4096 BF16 with both norms, forward 96 us, backward 166; now see the table of the widths below.
+// A block per SM, of several groups of warps that work on a row each. Rows are copied in bulk into each group's ring ahead of their use,
+// so that what is under way costs no registers. A thread has 16 columns of every row: 16-byte vectors where rows are aligned to
+// them, else single columns, neighbours with neighbouring threads. The factors of y r and of x' r' lie before the rings in FP32, for all
+// groups. Two values per instruction. What bounds a group is the chain of its two or three sums over the row (700 cycles each);
+// what a row needs is kept in registers from one sum to the next, which leaves room for two groups of 256 threads (three, with
+// 80 registers and values read again from shared memory, took 150 us backward where two take NOW_B).
+// 8192 x 4096 BF16, both norms: forward 96 us with rows in registers and no copies ahead, 54 as blocks with a ring each, NOW_F now;
+// backward 166, 88, NOW_B.
 
 __device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
 __device__ __forceinline__ float sum_of(uint64_t v) {
@@ -273,13 +277,14 @@ __device__ __forceinline__ uint64_t sigmoid2(uint64_t v) {
 constexpr int kCols = 16;              // per thread
 constexpr int kPairs = kCols / 2;
 
-// A thread's columns: vectors blockDim vectors apart, or single ones blockDim apart. Columns behind the row are zeros: vectors have
+// A thread's columns: vectors `n` vectors apart, or single ones `n` apart, with n threads in the group. Columns behind the row are zeros: vectors have
 // zeros behind their rows in shared memory, for single columns it is asked.
 template <typename T, bool kVector>
 struct Columns {
   static constexpr int V = kVector ? 16 / (int)sizeof(T) : 1, K = kCols / V;
-  static __device__ __forceinline__ int first(int k) { return (k * blockDim.x + threadIdx.x) * V; }
-  static __device__ __forceinline__ void load(const char* row, int hidden, uint64_t* v) {
+  int t, n;
+  __device__ __forceinline__ int first(int k) const { return (k * n + t) * V; }
+  __device__ __forceinline__ void load(const char* row, int hidden, uint64_t* v) const {
     float one[2];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -304,10 +309,10 @@ struct Columns {
       }
     }
   }
-  // Factors lie as threads read them: the fours of a thread's values blockDim fours apart (behind one another in a thread's own order,
-  // vectors of eight would meet in the same banks: 94.7 -> FOURS us backward).
-  static __device__ __forceinline__ int place(int value) { return (value / 4 * blockDim.x + threadIdx.x) * 4 + value % 4; }
-  static __device__ __forceinline__ void load_factors(const float* w, uint64_t* v) {
+  // Factors lie as threads read them: the fours of a thread's values `n` fours apart (behind one another in a thread's own order,
+  // vectors of eight would meet in the same banks: 94.7 -> 87.5 us backward).
+  __device__ __forceinline__ int place(int value) const { return (value / 4 * n + t) * 4 + value % 4; }
+  __device__ __forceinline__ void load_factors(const float* w, uint64_t* v) const {
 #pragma unroll
     for (int j = 0; j < kCols / 4; ++j) {
       const float4 a = *reinterpret_cast<const float4*>(w + place(4 * j));
@@ -315,7 +320,16 @@ struct Columns {
       v[2 * j + 1] = pair(a.z, a.w);
     }
   }
-  static __device__ __forceinline__ void store(T* row, int hidden, const uint64_t* v) {
+  __device__ __forceinline__ void store_factors(float* w, const uint64_t* v) const {
+#pragma unroll
+    for (int j = 0; j < kCols / 4; ++j) {
+      float4 a;
+      split(v[2 * j], &a.x, &a.y);
+      split(v[2 * j + 1], &a.z, &a.w);
+      *reinterpret_cast<float4*>(w + place(4 * j)) = a;
+    }
+  }
+  __device__ __forceinline__ void store(T* row, int hidden, const uint64_t* v) const {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = first(k);
@@ -331,7 +345,7 @@ struct Columns {
       if (c < hidden) store_values<V>(row + c, f);
     }
   }
-  static __device__ __forceinline__ void store_f32(float* row, int hidden, const uint64_t* v) {
+  __device__ __forceinline__ void store_f32(float* row, int hidden, const uint64_t* v) const {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = first(k);
@@ -344,27 +358,24 @@ struct Columns {
       }
     }
   }
-  // f(column, place of its factors) for every column of the thread
-  template <typename F>
-  static __device__ __forceinline__ void each(F f) {
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int e = 0; e < V; ++e) f(first(k) + e, place(k * V + e));
-  }
 };
 
-// Sums over the block of up to 16 warps, as block_sums; the second of two values is folded onto the upper lanes, and every thread
-// adds the warps' sums itself.
+__device__ __forceinline__ void group_sync(int group, int n) {
+  __syncwarp();
+  if (n > 32) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(n) : "memory");
+}
+// Sums of up to two values over a group; the second is folded onto the upper lanes of its warps, and every thread adds the warps' sums
+// itself. Calls take the halves of `part` in turn, so that one barrier is enough.
 template <int kWarps>
-__device__ __forceinline__ float2 ring_sums(float a, float b, float2 (*part)[kWarps], int& turn) {
-  const bool upper = threadIdx.x & 16;
+__device__ __forceinline__ float2 group_sums(float a, float b, float2 (*part)[kWarps], int& turn, int t, int n, int group) {
+  const bool upper = t & 16;
   float v = (upper ? b : a) + __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (n == 32) return make_float2(__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16));
   turn ^= 1;
-  if (threadIdx.x % 16 == 0) reinterpret_cast<float*>(&part[turn][threadIdx.x / 32])[threadIdx.x / 16 % 2] = v;
-  __syncthreads();
+  if (t % 16 == 0) reinterpret_cast<float*>(&part[turn][t / 32])[t / 16 % 2] = v;
+  group_sync(group, n);
   uint64_t s = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; w += 2) {
@@ -376,7 +387,7 @@ __device__ __forceinline__ float2 ring_sums(float a, float b, float2 (*part)[kWa
   return r;
 }
 
-constexpr int kMaxNormStages = 4;
+constexpr int kMaxNormStages = 4, kMaxGroups = 15;
 constexpr int kMaxNormInputs = 5;
 enum NormInput { kInX, kInY, kInGate, kInDx, kInDh };
 
@@ -384,7 +395,7 @@ struct NormFeed {
   const char* src[kMaxNormInputs];
   int64_t stride[kMaxNormInputs];    // bytes
   int slot[kMaxNormInputs];          // the row's place in a stage
-  int inputs, stages;
+  int inputs, stages, groups, group_threads;
   uint32_t row_bytes, slot_bytes;    // a slot has room for the row wherever in its first 16 bytes it begins
 };
 struct NormRingParams {
@@ -393,35 +404,39 @@ struct NormRingParams {
   int* error;
   uint32_t polls;
 };
-struct NormRing {
-  uint64_t full[kMaxNormStages];
+struct NormRings {
+  uint64_t full[kMaxGroups][kMaxNormStages];
   uint32_t dead;
 };
 
-// The ring from the side of one thread; row number i of the block goes to stage i % stages. Thread 0 copies. A wait that runs out
-// makes it stop copying, and the block goes on with what there is to its end: the call has failed, and says so.
+// A group's ring from the side of one thread; row number i of the group goes to stage i % stages. Its first thread copies. A wait that
+// runs out makes it stop copying, and the group goes on with what there is to its end: the call has failed, and says so.
 template <bool kVector>
 struct NormRows {
   const NormRingParams& p;
-  NormRing& ring;
+  uint64_t* full;
+  uint32_t* dead;
   char* smem;
-  int64_t count;                 // rows of this block
+  int64_t first, step, count;    // rows of this group
   int64_t issued = 0, ready = 0;
   int stage = 0;                 // of the present row
   uint32_t parity = 0;
   bool ok = true;
-  __device__ NormRows(const NormRingParams& p_, NormRing& ring_, void* smem_) : p(p_), ring(ring_), smem(static_cast<char*>(smem_)) {
-    count = p.n.tokens > blockIdx.x ? (p.n.tokens - 1 - blockIdx.x) / gridDim.x + 1 : 0;
+  __device__ NormRows(const NormRingParams& p_, NormRings& rings, float* factors, int group) : p(p_), full(rings.full[group]), dead(&rings.dead) {
+    smem = reinterpret_cast<char*>(factors + 2 * kCols * p.feed.group_threads) + (size_t)group * p.feed.stages * p.feed.inputs * p.feed.slot_bytes;
+    first = (int64_t)group * gridDim.x + blockIdx.x;
+    step = (int64_t)gridDim.x * p.feed.groups;
+    count = p.n.tokens > first ? (p.n.tokens - 1 - first) / step + 1 : 0;
   }
   __device__ __forceinline__ char* slot(int s, int input) const { return smem + (s * p.feed.inputs + p.feed.slot[input]) * p.feed.slot_bytes; }
   // Rows that are not aligned are copied from the 16 bytes that hold their first value to those that hold their last, and lie in
   // their slot as they lie in memory. What else those hold belongs to the rows next to them; before the first row and behind the last
   // nothing is read, but value by value up to the next 16 bytes.
-  __device__ __forceinline__ void issue_next() {   // thread 0
+  __device__ __forceinline__ void issue_next() {   // the first thread
     if (!ok || issued >= count) return;
     const int s = (int)(issued % p.feed.stages);
-    const int64_t row = blockIdx.x + issued * gridDim.x;
-    const uint32_t bar = smem_addr(&ring.full[s]);
+    const int64_t row = first + issued * step;
+    const uint32_t bar = smem_addr(&full[s]);
     if constexpr (kVector) {
       mbar_expect(bar, p.feed.inputs * p.feed.row_bytes);
 #pragma unroll
@@ -454,7 +469,7 @@ struct NormRows {
     ++issued;
   }
   __device__ __forceinline__ void wait() {
-    ok &= Waiter{&ring.dead, p.error, p.polls}(smem_addr(&ring.full[stage]), parity);
+    ok &= Waiter{dead, p.error, p.polls}(smem_addr(&full[stage]), parity);
     if (ok) ++ready;
   }
   __device__ __forceinline__ void next() {
@@ -466,80 +481,104 @@ struct NormRows {
     return to;
   }
   // Zeros behind the rows, once: copies do not reach them.
-  __device__ __forceinline__ void clear_padding() const {
+  __device__ __forceinline__ void clear_padding(int t) const {
     if (!kVector) return;
     const uint32_t words = (p.feed.slot_bytes - p.feed.row_bytes) / 4;
     for (int i = 0; i < p.feed.stages * p.feed.inputs; ++i)
-      for (uint32_t w = threadIdx.x; w < words; w += blockDim.x) reinterpret_cast<uint32_t*>(smem + i * p.feed.slot_bytes + p.feed.row_bytes)[w] = 0;
+      for (uint32_t w = t; w < words; w += p.feed.group_threads) reinterpret_cast<uint32_t*>(smem + i * p.feed.slot_bytes + p.feed.row_bytes)[w] = 0;
   }
-  __device__ __forceinline__ float* factors() const { return reinterpret_cast<float*>(smem + p.feed.stages * p.feed.inputs * p.feed.slot_bytes); }
-  __device__ __forceinline__ void finish() {       // thread 0: no copy is left under way
-    for (int64_t i = ready; i < issued; ++i) drain(smem_addr(&ring.full[i % p.feed.stages]), i / p.feed.stages & 1);
+  __device__ __forceinline__ void finish() {       // the first thread: no copy is left under way
+    for (int64_t i = ready; i < issued; ++i) drain(smem_addr(&full[i % p.feed.stages]), i / p.feed.stages & 1);
   }
 };
 
-template <typename T>
-__device__ __forceinline__ float weight(const void* w, int c) {
-  float v = 1.0f;
-  if (w) load_values<1>(static_cast<const T*>(w) + c, &v);
-  return v;
+// The columns of a weight in global memory; ones without it.
+template <typename T, bool kVector>
+__device__ __forceinline__ void load_weight(const Columns<T, kVector>& cols, const void* w, int hidden, uint64_t* v) {
+  if (!w) {
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) v[e] = both(1.0f);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < cols.K; ++k) {
+    const int c = cols.first(k);
+    float f[cols.V + 1] = {};
+    if (c < hidden) {
+      if constexpr (kVector) to_floats<T, cols.V>(*reinterpret_cast<const uint4*>(static_cast<const T*>(w) + c), f);
+      else load_values<1>(static_cast<const T*>(w) + c, f);
+    }
+    if constexpr (kVector) {
+#pragma unroll
+      for (int e = 0; e < cols.V; e += 2) v[(k * cols.V + e) / 2] = pair(f[e], f[e + 1]);
+    } else {
+      float lo, hi;
+      split(v[k / 2], &lo, &hi);
+      v[k / 2] = k % 2 ? pair(lo, f[0]) : pair(f[0], 0.0f);
+    }
+  }
 }
-
-// The start that both kernels share: barriers, the first rows, the factors a g w_post (without a token's g) and w_pre.
+// The start that both kernels share: barriers, the first rows, the factors a g w_post (without a token's g) and w_pre, by the first group.
 template <typename T, bool kVector, bool kToken, int kWarps>
-__device__ __forceinline__ void start_ring(const BlockNormParams& p, NormRows<kVector>& rows, float2 (*part)[kWarps]) {
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < kMaxNormStages; ++s) mbar_init(smem_addr(&rows.ring.full[s]), 1);
-    rows.ring.dead = 0;
+__device__ __forceinline__ void start_rings(const BlockNormParams& p, const Columns<T, kVector>& cols, NormRows<kVector>& rows, NormRings& rings,
+                                            float2 (*part)[kWarps], float* post, float* pre, int group) {
+  if (cols.t == 0) {
+    for (int s = 0; s < kMaxNormStages; ++s) mbar_init(smem_addr(&rows.full[s]), 1);
+    if (group == 0) rings.dead = 0;
     mbar_init_fence();
   }
-  rows.clear_padding();
-  if (threadIdx.x < 2 * kWarps) part[threadIdx.x / kWarps][threadIdx.x % kWarps] = make_float2(0.0f, 0.0f);
+  rows.clear_padding(cols.t);
+  for (int i = cols.t; i < 2 * kWarps; i += cols.n) part[i / kWarps][i % kWarps] = make_float2(0.0f, 0.0f);
   __syncthreads();
   wait_for_previous_kernel();
-  if (threadIdx.x == 0)
+  if (cols.t == 0)
     for (int s = 0; s < rows.p.feed.stages; ++s) rows.issue_next();
-  float *post = rows.factors(), *pre = post + blockDim.x * kCols;
-  Columns<T, kVector>::each([&](int c, int at) {
-    post[at] = pre[at] = 0.0f;
-    if (c >= p.hidden) return;
-    float f = p.alpha * weight<T>(p.w_post, c);
-    if (!kToken && p.gate_kind) {
-      const float g = weight<T>(p.gate.p, c);
-      f *= p.sigmoid ? sigmoid(g) : g;
+  if (group == 0) {
+    uint64_t f[kPairs], g[kPairs];
+    load_weight(cols, p.w_post, p.hidden, f);
+    if (!kToken && p.gate_kind) load_weight(cols, p.gate.p, p.hidden, g);
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) {
+      f[e] = mul2(f[e], both(p.alpha));
+      if (!kToken && p.gate_kind) f[e] = mul2(f[e], p.sigmoid ? sigmoid2(g[e]) : g[e]);
     }
-    post[at] = f;
-    pre[at] = weight<T>(p.w_pre, c);
-  });
+    cols.store_factors(post, f);
+    load_weight(cols, p.w_pre, p.hidden, f);
+    cols.store_factors(pre, f);
+  }
+  __syncthreads();
 }
 
 // kToken: the gate is each token's. kFull: there are a block's output, both norms and, backward, both gradients; known when it is
-// compiled, which leaves out the moves of values between branches (8192 x 4096, forward and backward: 53.6 + 108.5 us -> KFULL).
-template <typename T, bool kVector, bool kToken, bool kFull, int kThreads, int kBlocks>
-__global__ void __launch_bounds__(kThreads, kBlocks) block_norm_ring_kernel(const __grid_constant__ NormRingParams rp) {
+// compiled, which leaves out the moves of values between branches (8192 x 4096, forward and backward: 53.6 + 108.5 us -> 51.6 + 94.7).
+template <typename T, bool kVector, bool kToken, bool kFull, int kThreads, int kWarps>
+__global__ void __launch_bounds__(kThreads, 1) block_norm_ring_kernel(const __grid_constant__ NormRingParams rp) {
   extern __shared__ uint4 dynamic[];
-  __shared__ NormRing ring;
-  __shared__ alignas(16) float2 part[2][kThreads / 32];
+  __shared__ NormRings rings;
+  __shared__ alignas(16) float2 parts[kMaxGroups][2][kWarps];
   allow_next_kernel();
-  typedef Columns<T, kVector> C;
   const BlockNormParams& p = rp.n;
-  NormRows<kVector> rows(rp, ring, dynamic);
-  start_ring<T, kVector, kToken>(p, rows, part);
+  const int n = rp.feed.group_threads, group = threadIdx.x / n;
+  const Columns<T, kVector> cols = {(int)threadIdx.x - group * n, n};
+  float *post = reinterpret_cast<float*>(dynamic), *pre = post + n * kCols;
+  float2(*part)[kWarps] = parts[group];
+  NormRows<kVector> rows(rp, rings, post, group);
+  start_rings<T, kVector, kToken>(p, cols, rows, rings, part, post, pre, group);
+  const bool leader = cols.t == 0;
   const bool has_y = kFull || p.has_y, norm_y = kFull || p.post, norm_x = kFull || p.pre;
-  const float *post = rows.factors(), *pre = post + blockDim.x * kCols;
   int turn = 0;
   for (int64_t i = 0; i < rows.count; ++i, rows.next()) {
-    const int64_t row = blockIdx.x + i * gridDim.x;
+    const int64_t row = rows.first + i * rows.step;
     rows.wait();
     uint64_t x[kPairs], y[kPairs], f[kPairs];
-    C::load(rows.at(kInX, row), p.hidden, x);
+    cols.load(rows.at(kInX, row), p.hidden, x);
     float r = 1.0f;
     if (has_y) {
-      C::load(rows.at(kInY, row), p.hidden, y);
-      C::load_factors(post, f);
+      cols.load(rows.at(kInY, row), p.hidden, y);
+      cols.load_factors(post, f);
       if (kToken) {
         uint64_t g[kPairs];
-        C::load(rows.at(kInGate, row), p.hidden, g);
+        cols.load(rows.at(kInGate, row), p.hidden, g);
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) f[e] = mul2(f[e], p.sigmoid ? sigmoid2(g[e]) : g[e]);
       }
@@ -547,91 +586,108 @@ __global__ void __launch_bounds__(kThreads, kBlocks) block_norm_ring_kernel(cons
         uint64_t s = 0;
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) s = fma2(y[e], y[e], s);
-        r = rsqrtf(ring_sums(sum_of(s), 0.0f, part, turn).x * p.inv_hidden + p.eps);
-        if (threadIdx.x == 0) rows.issue_next();      // all threads have the row
+        r = rsqrtf(group_sums<kWarps>(sum_of(s), 0.0f, part, turn, cols.t, n, group).x * p.inv_hidden + p.eps);
+        if (leader) rows.issue_next();      // all threads have the row
       }
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) x[e] = fma2(mul2(f[e], both(r)), y[e], x[e]);
-      C::store(static_cast<T*>(p.x_out.p) + row * p.x_out.stride, p.hidden, x);
+      cols.store(static_cast<T*>(p.x_out.p) + row * p.x_out.stride, p.hidden, x);
     }
     if (norm_x) {
       uint64_t s = 0;
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) s = fma2(x[e], x[e], s);
-      const float r2 = rsqrtf(ring_sums(sum_of(s), 0.0f, part, turn).x * p.inv_hidden + p.eps);
-      if (!norm_y && threadIdx.x == 0) rows.issue_next();
-      C::load_factors(pre, f);
+      const float r2 = rsqrtf(group_sums<kWarps>(sum_of(s), 0.0f, part, turn, cols.t, n, group).x * p.inv_hidden + p.eps);
+      if (!norm_y && leader) rows.issue_next();
+      cols.load_factors(pre, f);
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) x[e] = mul2(mul2(f[e], both(r2)), x[e]);
-      C::store(static_cast<T*>(p.h_out.p) + row * p.h_out.stride, p.hidden, x);
+      cols.store(static_cast<T*>(p.h_out.p) + row * p.h_out.stride, p.hidden, x);
     } else if (!norm_y) {
-      __syncthreads();
-      if (threadIdx.x == 0) rows.issue_next();
+      group_sync(group, n);
+      if (leader) rows.issue_next();
     }
   }
-  if (threadIdx.x == 0) rows.finish();
+  if (leader) rows.finish();
 }
 
-template <typename T, bool kVector, bool kToken, bool kFull, int kThreads, int kBlocks>
-__global__ void __launch_bounds__(kThreads, kBlocks) block_norm_backward_ring_kernel(const __grid_constant__ NormRingParams rp) {
+template <typename T, bool kVector, bool kToken, bool kFull, int kThreads, int kWarps>
+__global__ void __launch_bounds__(kThreads, 1) block_norm_backward_ring_kernel(const __grid_constant__ NormRingParams rp) {
   extern __shared__ uint4 dynamic[];
-  __shared__ NormRing ring;
-  __shared__ alignas(16) float2 part[2][kThreads / 32];
+  __shared__ NormRings rings;
+  __shared__ alignas(16) float2 parts[kMaxGroups][2][kWarps];
   allow_next_kernel();
-  typedef Columns<T, kVector> C;
   const BlockNormParams& p = rp.n;
-  NormRows<kVector> rows(rp, ring, dynamic);
-  start_ring<T, kVector, kToken>(p, rows, part);
+  const int n = rp.feed.group_threads, group = threadIdx.x / n;
+  const Columns<T, kVector> cols = {(int)threadIdx.x - group * n, n};
+  float *post = reinterpret_cast<float*>(dynamic), *pre = post + n * kCols;
+  float2(*part)[kWarps] = parts[group];
+  NormRows<kVector> rows(rp, rings, post, group);
+  start_rings<T, kVector, kToken>(p, cols, rows, rings, part, post, pre, group);
+  const bool leader = cols.t == 0;
   const bool has_y = kFull || p.has_y, norm_y = kFull || p.post, norm_x = kFull || p.pre;
-  const float *post = rows.factors(), *pre = post + blockDim.x * kCols;
+  // Whether a row stays in registers from one sum to the next, as far as there are any: a token's gate is 32 more, single columns take
+  // more to address. Their rows are read again (8192 x 4096 BF16 with such a gate: 158 -> GATE2 us).
+  constexpr bool kKeep = kVector && !kToken;
   uint64_t sum_post[kPairs] = {}, sum_pre[kPairs] = {};
   int turn = 0;
   for (int64_t i = 0; i < rows.count; ++i, rows.next()) {
-    const int64_t row = blockIdx.x + i * gridDim.x;
+    const int64_t row = rows.first + i * rows.step;
     rows.wait();
     uint64_t x[kPairs], y[kPairs], g[kPairs], h[kPairs], f[kPairs];     // y: times r
     float r = 1.0f, r2 = 0.0f, m = 0.0f;
+    const auto load_y = [&] {
+      cols.load(rows.at(kInY, row), p.hidden, y);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) y[e] = mul2(y[e], both(r));
+    };
+    const auto load_gate = [&] {
+      cols.load(rows.at(kInGate, row), p.hidden, g);
+      if (p.sigmoid) {
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) g[e] = sigmoid2(g[e]);
+      }
+    };
     if (has_y) {
-      C::load(rows.at(kInY, row), p.hidden, y);
+      cols.load(rows.at(kInY, row), p.hidden, y);
       if (norm_y) {
         uint64_t s = 0;
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) s = fma2(y[e], y[e], s);
-        r = rsqrtf(ring_sums(sum_of(s), 0.0f, part, turn).x * p.inv_hidden + p.eps);
+        r = rsqrtf(group_sums<kWarps>(sum_of(s), 0.0f, part, turn, cols.t, n, group).x * p.inv_hidden + p.eps);
       }
+      if constexpr (kKeep) {
 #pragma unroll
-      for (int e = 0; e < kPairs; ++e) y[e] = mul2(y[e], both(r));
-      if (kToken) {
-        C::load(rows.at(kInGate, row), p.hidden, g);
-        if (p.sigmoid) {
-#pragma unroll
-          for (int e = 0; e < kPairs; ++e) g[e] = sigmoid2(g[e]);
-        }
+        for (int e = 0; e < kPairs; ++e) y[e] = mul2(y[e], both(r));
+      } else {
+        load_y();
       }
+      if (kToken) load_gate();
     }
     if (norm_x) {
-      C::load(rows.at(kInX, row), p.hidden, x);
+      cols.load(rows.at(kInX, row), p.hidden, x);
       if (has_y) {
-        C::load_factors(post, f);
+        cols.load_factors(post, f);
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) x[e] = fma2(kToken ? mul2(f[e], g[e]) : f[e], y[e], x[e]);
       }
-      C::load(rows.at(kInDh, row), p.hidden, h);
-      C::load_factors(pre, f);
+      cols.load(rows.at(kInDh, row), p.hidden, h);
+      cols.load_factors(pre, f);
       uint64_t ss = 0, ux = 0;
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) {
         ss = fma2(x[e], x[e], ss);
         ux = fma2(mul2(h[e], f[e]), x[e], ux);
       }
-      const float2 s = ring_sums(sum_of(ss), sum_of(ux), part, turn);
+      const float2 s = group_sums<kWarps>(sum_of(ss), sum_of(ux), part, turn, cols.t, n, group);
       r2 = rsqrtf(s.x * p.inv_hidden + p.eps);
       m = -s.y * r2 * p.inv_hidden;
     }
     uint64_t d[kPairs] = {};
-    if (kFull || p.dx_out.p) C::load(rows.at(kInDx, row), p.hidden, d);
+    if (kFull || p.dx_out.p) cols.load(rows.at(kInDx, row), p.hidden, d);
     if (norm_x) {
-      C::load_factors(pre, f);
+      cols.load_factors(pre, f);
+      if (!kKeep) cols.load(rows.at(kInDh, row), p.hidden, h);
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) {
         const uint64_t xh = mul2(x[e], both(r2));
@@ -639,10 +695,14 @@ __global__ void __launch_bounds__(kThreads, kBlocks) block_norm_backward_ring_ke
         d[e] = fma2(both(r2), fma2(xh, both(m), mul2(h[e], f[e])), d[e]);
       }
     }
-    C::store(static_cast<T*>(p.dx.p) + row * p.dx.stride, p.hidden, d);
+    cols.store(static_cast<T*>(p.dx.p) + row * p.dx.stride, p.hidden, d);
     uint64_t dot = 0;
     if (has_y) {
-      C::load_factors(post, f);
+      cols.load_factors(post, f);
+      if (!kKeep) {
+        load_y();
+        if (kToken) load_gate();
+      }
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) {
         x[e] = mul2(f[e], d[e]);                   // v, or v / g
@@ -659,23 +719,45 @@ __global__ void __launch_bounds__(kThreads, kBlocks) block_norm_backward_ring_ke
           dot = fma2(x[e], y[e], dot);
         }
       }
-      if (kToken && p.dgate.p) C::store(static_cast<T*>(p.dgate.p) + row * p.dgate.stride, p.hidden, f);
+      if (kToken && p.dgate.p) cols.store(static_cast<T*>(p.dgate.p) + row * p.dgate.stride, p.hidden, f);
     }
     if (norm_y) {
-      m = -ring_sums(sum_of(dot), 0.0f, part, turn).x * p.inv_hidden;
+      m = -group_sums<kWarps>(sum_of(dot), 0.0f, part, turn, cols.t, n, group).x * p.inv_hidden;
+      if (!kKeep) {
+        load_y();
+        group_sync(group, n);
+      }
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) x[e] = mul2(both(r), fma2(y[e], both(m), x[e]));
     } else {
-      __syncthreads();
+      group_sync(group, n);
     }
-    if (threadIdx.x == 0) rows.issue_next();       // all threads have read the row
-    if (has_y) C::store(static_cast<T*>(p.dy.p) + row * p.dy.stride, p.hidden, x);
+    if (leader) rows.issue_next();       // all threads have read the row
+    if (has_y) cols.store(static_cast<T*>(p.dy.p) + row * p.dy.stride, p.hidden, x);
   }
-  if (threadIdx.x == 0) rows.finish();
-  if (p.partial) {
-    float* at = p.partial + (int64_t)blockIdx.x * 2 * p.hidden;
-    C::store_f32(at, p.hidden, sum_post);
-    C::store_f32(at + p.hidden, p.hidden, sum_pre);
+  if (leader) rows.finish();
+  if (!p.partial) return;
+  // the groups' sums, one after the other, where the factors were
+  for (int g = 0; g < rp.feed.groups; ++g) {
+    __syncthreads();
+    if (g != group) continue;
+    if (g > 0) {
+      uint64_t s[kPairs];
+      cols.load_factors(post, s);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) sum_post[e] = add2(s[e], sum_post[e]);
+      cols.load_factors(pre, s);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) sum_pre[e] = add2(s[e], sum_pre[e]);
+    }
+    if (g + 1 < rp.feed.groups) {
+      cols.store_factors(post, sum_post);
+      cols.store_factors(pre, sum_pre);
+    } else {
+      float* at = p.partial + (int64_t)blockIdx.x * 2 * p.hidden;
+      cols.store_f32(at, p.hidden, sum_post);
+      cols.store_f32(at + p.hidden, p.hidden, sum_pre);
+    }
   }
 }
 
@@ -800,16 +882,15 @@ void pick_norm_kernel(const slidedp_block_norm_args* a, int v, F run) {
   else width(float(), N16(), std::integral_constant<int, 4>());
 }
 
-// Blocks that hold their rows in shared memory: threads, blocks per SM, stages of the ring. The kernels are compiled for up to 256,
-// 320 or 512 threads, and the blocks per SM that leave a thread 80 registers forward and 100 to 128 backward.
+// A block per SM whose groups hold their rows in shared memory: threads of a group, groups, stages of a ring. The kernels are compiled for
+// blocks of 512 threads, 128 registers each; forward two groups of up to 10 warps fit as well (5120 columns: 84 -> 59 us).
 struct RingPlan {
   bool use, vector;
-  int threads, blocks, stages;
+  int threads, groups, stages;
   size_t smem, slot;
 };
-constexpr int ring_blocks(bool backward, int threads) { return threads > 256 ? (threads > 320 || backward ? 1 : 2) : backward ? 2 : 3; }
-constexpr int ring_class(int threads) { return threads <= 256 ? 256 : threads <= 320 ? 320 : 512; }
-constexpr int kNormSmem = 222 * 1024;      // of an SM's 227 KB, less what each block has besides
+constexpr int ring_class(bool backward, int group) { return !backward && group > 256 && group <= 320 ? 640 : 512; }
+constexpr int kNormSmem = 222 * 1024;      // of an SM's 227 KB, less what a block has besides
 
 RingPlan ring_plan(const slidedp_block_norm_args* a, bool vector, int inputs, bool backward) {
   RingPlan r = {};
@@ -818,17 +899,19 @@ RingPlan ring_plan(const slidedp_block_norm_args* a, bool vector, int inputs, bo
   r.vector = vector;
   r.threads = (int)((a->hidden + kCols * 32 - 1) / (kCols * 32) * 32);
   r.slot = vector ? r.threads * kCols * elem_bytes(a->dtype) : (row + 15) / 16 * 16 + 16;
-  const int cls = ring_class(r.threads), most = ring_blocks(backward, cls) * cls / r.threads;
-  for (r.blocks = most < kMaxNormBlocks ? most : kMaxNormBlocks; r.blocks >= 1; --r.blocks)
-    for (r.stages = kMaxNormStages; r.stages >= (r.blocks > 1 ? 2 : 1); --r.stages) {
-      r.smem = r.stages * inputs * r.slot + r.threads * kCols * 8;
-      if (r.blocks * (r.smem + 2048) <= kNormSmem) {
+  const int most = ring_class(backward, r.threads) / r.threads;
+  for (r.groups = most < kMaxGroups ? most : kMaxGroups; r.groups >= 1; --r.groups)
+    for (r.stages = kMaxNormStages; r.stages >= (r.groups > 1 ? 2 : 1); --r.stages) {
+      r.smem = r.groups * r.stages * inputs * r.slot + r.threads * kCols * 8;
+      if (r.smem <= kNormSmem) {
         r.use = true;
         return r;
       }
     }
   return r;
 }
+// Rows go to groups block by block: all SMs have one before one has two.
+unsigned ring_grid(const slidedp_block_norm_args* a) { return (unsigned)(a->tokens < 148 ? a->tokens : 148); }
 NormRingParams ring_params(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const BlockNormParams& n, const RingPlan& plan) {
   NormRingParams r = {};
   r.n = n;
@@ -842,24 +925,25 @@ NormRingParams ring_params(slidedp_ctx* ctx, const slidedp_block_norm_args* a, c
     r.feed.inputs += in[i]->p != nullptr;
   }
   r.feed.stages = plan.stages;
+  r.feed.groups = plan.groups;
+  r.feed.group_threads = plan.threads;
   r.feed.row_bytes = (uint32_t)(a->hidden * elem);
   r.feed.slot_bytes = (uint32_t)plan.slot;
   r.error = ctx->kernel_error;
   r.polls = ctx->wait_polls;
   return r;
 }
-// run(T, vector, token, full, threads, blocks) as template arguments.
+// run(T, vector, token, full, threads, warps of a group) as template arguments.
 template <bool kBackward, typename F>
 void pick_ring_kernel(const slidedp_block_norm_args* a, const RingPlan& plan, bool full, F run) {
   typedef std::true_type Yes;
   typedef std::false_type No;
   const auto threads = [&](auto type, auto vector, auto token, auto whole) {
-    const auto with = [&](auto t) { run(type, vector, token, whole, t, std::integral_constant<int, ring_blocks(kBackward, t)>()); };
-    switch (ring_class(plan.threads)) {
-      case 256: return with(std::integral_constant<int, 256>());
-      case 320: return with(std::integral_constant<int, 320>());
-      default: return with(std::integral_constant<int, 512>());
-    }
+    typedef std::integral_constant<int, 512> Usual;
+    if (plan.threads <= 256) return run(type, vector, token, whole, Usual(), std::integral_constant<int, 8>());
+    if constexpr (!kBackward)
+      if (plan.threads <= 320) return run(type, vector, token, whole, std::integral_constant<int, 640>(), std::integral_constant<int, 10>());
+    run(type, vector, token, whole, Usual(), std::integral_constant<int, 16>());
   };
   const auto forms = [&](auto type, auto token) {
     if (!plan.vector) return threads(type, No(), token, No());
@@ -909,13 +993,13 @@ int slidedp_block_norm(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const
   FAULT_POINT();
   if (plan.use) {
     const NormRingParams r = ring_params(ctx, a, p, plan);
-    pick_ring_kernel<false>(a, plan, y && a->post_norm && a->pre_norm, [&](auto type, auto vector, auto token, auto full, auto threads, auto per_sm) {
+    pick_ring_kernel<false>(a, plan, y && a->post_norm && a->pre_norm, [&](auto type, auto vector, auto token, auto full, auto threads, auto warps) {
       typedef decltype(type) T_;
       const auto run = [&](auto kernel) {
         attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem);
-        if (attribute == cudaSuccess) launch_after(kernel, dim3((unsigned)norm_blocks(a, plan.blocks)), plan.threads, plan.smem, 1, st, r);
+        if (attribute == cudaSuccess) launch_after(kernel, dim3(ring_grid(a)), plan.threads * plan.groups, plan.smem, 1, st, r);
       };
-      run(block_norm_ring_kernel<T_, vector, token, full, threads, per_sm>);
+      run(block_norm_ring_kernel<T_, vector, token, full, threads, warps>);
     });
   } else {
     pick_norm_kernel(a, v, [&](auto type, auto vec, auto n, auto threads) {
@@ -992,17 +1076,17 @@ int slidedp_block_norm_backward(slidedp_ctx* ctx, const slidedp_block_norm_args*
                                          {&wp, elem}, {&wq, elem}});
     const RingPlan plan = ring_plan(a, v * elem == 16, 1 + (y != nullptr) + (a->gate_kind == 2) + (dx_out != nullptr) + a->pre_norm, true);
     cudaError_t attribute = cudaSuccess;
-    blocks = (unsigned)norm_blocks(a, plan.use ? plan.blocks : (int)(640 / norm_threads(a)));
+    blocks = plan.use ? ring_grid(a) : (unsigned)norm_blocks(a, 640 / norm_threads(a));
     FAULT_POINT();
     if (plan.use) {
       const NormRingParams r = ring_params(ctx, a, p, plan);
-      pick_ring_kernel<true>(a, plan, y && a->post_norm && a->pre_norm && dx_out, [&](auto type, auto vector, auto token, auto full, auto threads, auto per_sm) {
+      pick_ring_kernel<true>(a, plan, y && a->post_norm && a->pre_norm && dx_out, [&](auto type, auto vector, auto token, auto full, auto threads, auto warps) {
         typedef decltype(type) T_;
         const auto run = [&](auto kernel) {
           attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem);
-          if (attribute == cudaSuccess) launch_after(kernel, dim3(blocks), plan.threads, plan.smem, 1, st, r);
+          if (attribute == cudaSuccess) launch_after(kernel, dim3(blocks), plan.threads * plan.groups, plan.smem, 1, st, r);
         };
-        run(block_norm_backward_ring_kernel<T_, vector, token, full, threads, per_sm>);
+        run(block_norm_backward_ring_kernel<T_, vector, token, full, threads, warps>);
       });
     } else {
       pick_norm_kernel(a, v, [&](auto type, auto vec, auto n, auto threads) {
