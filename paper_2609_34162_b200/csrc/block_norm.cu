@@ -361,6 +361,7 @@ struct Columns {
 };
 
 __device__ __forceinline__ void group_sync(int group, int n) {
+  if (n == (int)blockDim.x) return __syncthreads();      // the only group: a barrier known when it is compiled
   __syncwarp();
   if (n > 32) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(n) : "memory");
 }
@@ -889,7 +890,7 @@ struct RingPlan {
   int threads, groups, stages;
   size_t smem, slot;
 };
-constexpr int ring_class(bool backward, int group) { return !backward && group > 256 && group <= 320 ? 640 : 512; }
+constexpr int ring_class(bool backward, int group) { return group > 256 && group <= 320 ? (backward ? 320 : 640) : 512; }
 constexpr int kNormSmem = 222 * 1024;      // of an SM's 227 KB, less what a block has besides
 
 RingPlan ring_plan(const slidedp_block_norm_args* a, bool vector, int inputs, bool backward) {
@@ -941,8 +942,7 @@ void pick_ring_kernel(const slidedp_block_norm_args* a, const RingPlan& plan, bo
   const auto threads = [&](auto type, auto vector, auto token, auto whole) {
     typedef std::integral_constant<int, 512> Usual;
     if (plan.threads <= 256) return run(type, vector, token, whole, Usual(), std::integral_constant<int, 8>());
-    if constexpr (!kBackward)
-      if (plan.threads <= 320) return run(type, vector, token, whole, std::integral_constant<int, 640>(), std::integral_constant<int, 10>());
+    if (plan.threads <= 320) return run(type, vector, token, whole, std::integral_constant<int, kBackward ? 320 : 640>(), std::integral_constant<int, 10>());
     run(type, vector, token, whole, Usual(), std::integral_constant<int, 16>());
   };
   const auto forms = [&](auto type, auto token) {
