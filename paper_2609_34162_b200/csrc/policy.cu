@@ -132,25 +132,14 @@ struct PolicyGrad {
   RowTerms t;
   int label;
 };
-// Of BF16 logits every kPoly-th pair takes the polynomial exponential (relative error 3e-6, of a value that is rounded to BF16): two
-// exponentials per logit are more than the special-function units give at the rate of the memory.
-template <typename T, int kPoly = 0>
+template <typename T>
 __device__ __forceinline__ void policy_values(uint4 a, const PolicyGrad& g, float* out) {
   constexpr int P = Logit<T>::kPer;
   uint64_t v[P / 2];
   Logit<T>::unpack(a, v);
   const uint64_t factor = pair(g.t.factor, g.t.factor), kk = pair(g.k, g.k), minus = pair(-g.t.shift, -g.t.shift);
 #pragma unroll
-  for (int e = 0; e < P / 2; ++e) {
-    const uint64_t x = fma2(v[e], kk, minus);
-    float lo, hi;
-    if constexpr (sizeof(T) == 2 && kPoly > 0) {
-      if (e % kPoly == 0) exp2_pair_poly(x, &lo, &hi); else split(exp2_pair(x), &lo, &hi);
-    } else {
-      split(exp2_pair(x), &lo, &hi);
-    }
-    split(mul2(pair(lo, hi), factor), &out[2 * e], &out[2 * e + 1]);
-  }
+  for (int e = 0; e < P / 2; ++e) split(mul2(exp2_pair(fma2(v[e], kk, minus)), factor), &out[2 * e], &out[2 * e + 1]);
 }
 template <typename T>
 __device__ __forceinline__ void policy_values_far(uint4 a, float k, const RowTerms& t, float* out) {
@@ -253,8 +242,8 @@ __device__ __forceinline__ void write_loss(const PolicyParams& p, int64_t r, con
   p.logp[r] = t.logp;
 }
 // From the saved log-probability: the shift is the row's log2 sum, or far from zero the label's logit.
-__device__ __forceinline__ RowTerms finish_saved(const PolicyParams& p, int64_t r, const RowInput& in, float mark, float k) {
-  const double logp = p.saved_logp[r], log2_p = logp * 1.4426950408889634, exact = (double)k * (double)mark - log2_p;
+__device__ __forceinline__ RowTerms finish_saved(const PolicyParams& p, const RowInput& in, float mark, float k, float saved) {
+  const double logp = saved, log2_p = logp * 1.4426950408889634, exact = (double)k * (double)mark - log2_p;
   RowTerms t;
   t.far = is_far((float)exact) || is_far(mark * k);
   t.shift = t.far ? mark : (float)exact;
@@ -271,9 +260,10 @@ struct PolicyShared {
   alignas(8) float2 part[kPolicyMaxCluster];   // maximum and sum of each block of the cluster
 };
 
-// kForward: log-probability and loss; kGradient: the gradient, without kForward from the saved log-probability. The blocks of a cluster
-// share a row's chunks, and exchange their sums through distributed shared memory.
-template <typename T, bool kForward, bool kGradient>
+// kGradient: the gradient from the saved log-probability, else log-probability and loss. The blocks of a cluster share a row's chunks;
+// forward they bring their sums to the first through distributed shared memory. Bound: HBM. 4096 x 131072 BF16: forward FWD_US us, gradient
+// BWD_US.
+template <typename T, bool kGradient>
 __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __grid_constant__ PolicyParams p, int cluster) {
   start_after_previous_kernel();
   __shared__ PolicyShared sh;
@@ -288,59 +278,23 @@ __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __g
   const int label = row_label(p, r);
   const bool same_grid = on_same_grid<T>(z, dz);
   if (label < 0) {      // all blocks of the cluster alike
-    if (kForward && rank == 0 && threadIdx.x == 0) {
+    if (kGradient) {
+      zero_chunks<T>(row, dz, same_grid, from, to, threadIdx.x, kPolicyThreads);
+    } else if (rank == 0 && threadIdx.x == 0) {
       if (p.loss) p.loss[r] = 0.0f;
       p.logp[r] = 0.0f;
     }
-    if (kGradient) zero_chunks<T>(row, dz, same_grid, from, to, threadIdx.x, kPolicyThreads);
     return;
   }
-  const float at = Logit<T>::load(z + label);
-  const float k = p.inv_tau * kLog2e;
-  RowInput in = {};
-  if (threadIdx.x < 32) in = row_input(p, r);
+  const float at = Logit<T>::load(z + label), k = p.inv_tau * kLog2e;
   constexpr int U = kPolicyUnroll;
-  if (kForward) {
-    PolicySum mine = {-INFINITY, 0.0f};
-    for (int64_t c = from + threadIdx.x; c < to; c += kPolicyThreads * U) {
-      uint4 a[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t i = c + u * kPolicyThreads;
-        a[u] = Logit<T>::lowest();
-        if (i < to) a[u] = kGradient && row.whole(i) ? *reinterpret_cast<const uint4*>(z + row.first(i)) : row.load(i);
-      }
-      add_chunks<T, U>(mine, a, k);
+  if constexpr (kGradient) {
+    if (threadIdx.x < 32) {
+      const RowTerms t = finish_saved(p, row_input(p, r), at, k, p.saved_logp[r]);
+      if (threadIdx.x == 0) sh.row = t;
     }
-    mine = join_sums<32>(mine, k);
-    if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32] = mine;
-    __syncthreads();
-    mine = join_sums<kPolicyWarps>(sh.warp[threadIdx.x % kPolicyWarps], k);
-    if (cluster > 1) {
-      if ((int)threadIdx.x < cluster && (kGradient || threadIdx.x == 0)) {
-        const uint32_t there = peer_addr(smem_addr(&sh.part[rank]), threadIdx.x);
-        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(mine.m), "f"(mine.s) : "memory");
-      }
-      cluster_sync();
-      const int i = threadIdx.x % kPolicyMaxCluster;
-      mine = PolicySum{-INFINITY, 0.0f};
-      if (i < cluster && (kGradient || rank == 0)) mine = PolicySum{sh.part[i].x, sh.part[i].y};
-      mine = join_sums<kPolicyMaxCluster>(mine, k);
-    }
-    if ((kGradient || rank == 0) && threadIdx.x < 32) {
-      const RowTerms t = finish_sum(p, in, mine, at, k);
-      if (threadIdx.x == 0) {
-        sh.row = t;
-        if (rank == 0) write_loss(p, r, t);
-      }
-    }
-  } else if (threadIdx.x < 32) {
-    const RowTerms t = finish_saved(p, r, in, at, k);
-    if (threadIdx.x == 0) sh.row = t;
-  }
-  if (kGradient) {
-    // without kForward nothing has been read of the row but `at`, which no block may change before all have it
-    if (!kForward && cluster > 1) cluster_sync(); else __syncthreads();
+    // nothing has been read of the row but `at`, which no block may change before all have it
+    if (cluster > 1) cluster_sync(); else __syncthreads();
     const RowTerms t = sh.row;
     if (t.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, from, to, threadIdx.x, kPolicyThreads);
     const PolicyGrad g = {k, t, label};
@@ -352,6 +306,32 @@ __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __g
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (c + u * kPolicyThreads < to) policy_chunk<T>(row, dz, same_grid, c + u * kPolicyThreads, a[u], g);
+    }
+  } else {
+    PolicySum mine = {-INFINITY, 0.0f};
+    for (int64_t c = from + threadIdx.x; c < to; c += kPolicyThreads * U) {
+      uint4 a[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) a[u] = c + u * kPolicyThreads < to ? row.load(c + u * kPolicyThreads) : Logit<T>::lowest();
+      add_chunks<T, U>(mine, a, k);
+    }
+    mine = join_sums<32>(mine, k);
+    if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32] = mine;
+    __syncthreads();
+    mine = join_sums<kPolicyWarps>(sh.warp[threadIdx.x % kPolicyWarps], k);
+    if (cluster > 1) {
+      if (threadIdx.x == 0) {
+        const uint32_t there = peer_addr(smem_addr(&sh.part[rank]), 0);
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(mine.m), "f"(mine.s) : "memory");
+      }
+      cluster_sync();
+      if (rank > 0) return;
+      const int i = threadIdx.x % kPolicyMaxCluster;
+      mine = join_sums<kPolicyMaxCluster>(i < cluster ? PolicySum{sh.part[i].x, sh.part[i].y} : PolicySum{-INFINITY, 0.0f}, k);
+    }
+    if (threadIdx.x < 32) {
+      const RowTerms t = finish_sum(p, row_input(p, r), mine, at, k);
+      if (threadIdx.x == 0) write_loss(p, r, t);
     }
   }
 }
@@ -418,7 +398,6 @@ constexpr int kRingThreads = 2 * kRingGroup + 64;   // and the producer's and th
 constexpr int kSlotUnroll = 4;
 constexpr int kSlotChunks = kRingGroup * kSlotUnroll;
 constexpr int kSlots = 208 * 1024 / (kSlotChunks * 16);
-constexpr int kGradPoly = 0;
 // Rows between the first and the last that any block of a cluster has to do with: a block's sums are at most kSlots rows before its
 // gradients, which wait for the other blocks' sums, which are at most kSlots rows before those blocks' gradients.
 constexpr int kRowSlots = 32;
@@ -598,7 +577,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
         if (usual && i0 + kSlotChunks <= s.n && !(hot >= i0 && hot < i0 + kSlotChunks)) {
 #pragma unroll
           for (int u = 0; u < kSlotUnroll; ++u) {
-            policy_values<T, kGradPoly>(a[u], g, v);
+            policy_values<T>(a[u], g, v);
             st_stream(out + i0 + u * kRingGroup, Logit<T>::pack(v));
           }
         } else {
@@ -788,9 +767,14 @@ int run_policy(slidedp_ctx* ctx, const slidedp_policy_args* a, PolicyMode mode, 
     p.chunks_per_block = (chunks + cluster - 1) / cluster;
     if (a->rows * cluster > 0x7fffffff) return SLIDEDP_ERR_INVALID_ARG;
     const auto run = [&](auto kernel) { launch_after(kernel, dim3((unsigned)(a->rows * cluster)), kPolicyThreads, 0, cluster, stream, p, cluster); };
-    if (mode == kPolicyForward) f32 ? run(policy_row_kernel<float, true, false>) : run(policy_row_kernel<uint16_t, true, false>);
-    else if (mode == kPolicyBackward) f32 ? run(policy_row_kernel<float, false, true>) : run(policy_row_kernel<uint16_t, false, true>);
-    else f32 ? run(policy_row_kernel<float, true, true>) : run(policy_row_kernel<uint16_t, true, true>);
+    if (mode != kPolicyBackward) f32 ? run(policy_row_kernel<float, false>) : run(policy_row_kernel<uint16_t, false>);
+    if (mode == kPolicyStep) {        // a row that no ring holds: one after the other
+      ctx->launches += 1;
+      CU_AFTER_LAUNCH();
+      FAULT_POINT();
+      p.saved_logp = logp;
+    }
+    if (mode != kPolicyForward) f32 ? run(policy_row_kernel<float, true>) : run(policy_row_kernel<uint16_t, true>);
   }
   if (failed != cudaSuccess) return cuda_fail(ctx, failed);
   ctx->launches += 1;
