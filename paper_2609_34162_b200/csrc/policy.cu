@@ -336,12 +336,18 @@ __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __g
   }
 }
 
-// Both for short rows: a block holds its row in registers, U chunks a thread.
-template <typename T, int U>
-__global__ void __launch_bounds__(kPolicyThreads) policy_held_kernel(const __grid_constant__ PolicyParams p) {
+// Both for short rows: kRow threads hold a row in registers, U chunks each; a warp, eight of them per block, or a block. Against the ring
+// below, which is for rows longer than these: 8192 x 8000 BF16 55 us (a block of 256) and 117, 4096 x 32768 HELD_US (of 512) and 117;
+// a warp for 8192 x 1000: WARP_US, where a block takes 28.
+template <typename T, int U, int kRow>
+__global__ void __launch_bounds__(kRow < 256 ? 256 : kRow) policy_held_kernel(const __grid_constant__ PolicyParams p) {
   start_after_previous_kernel();
-  __shared__ PolicyShared sh;
-  const int64_t r = blockIdx.x;
+  __shared__ RowTerms shared_terms;
+  __shared__ PolicySum warps[16];
+  constexpr int kRows = kRow < 256 ? 256 / kRow : 1, kWarps = kRow / 32;
+  const int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / kRow;
+  const int thread = threadIdx.x % kRow;
+  if (r >= p.rows) return;
   const T* z = static_cast<const T*>(p.z) + r * p.z_stride;
   T* dz = static_cast<T*>(p.dz) + r * p.dz_stride;
   const Row<T> row(z, p.vocab);
@@ -349,41 +355,47 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_held_kernel(const __gri
   const int label = row_label(p, r);
   const bool same_grid = on_same_grid<T>(z, dz);
   if (label < 0) {
-    if (threadIdx.x == 0) {
+    if (thread == 0) {
       if (p.loss) p.loss[r] = 0.0f;
       p.logp[r] = 0.0f;
     }
-    return zero_chunks<T>(row, dz, same_grid, 0, chunks, threadIdx.x, kPolicyThreads);
+    return zero_chunks<T>(row, dz, same_grid, 0, chunks, thread, kRow);
   }
   const float at = Logit<T>::load(z + label), k = p.inv_tau * kLog2e;
   RowInput in = {};
-  if (threadIdx.x < 32) in = row_input(p, r);
+  if (thread < 32) in = row_input(p, r);
   uint4 a[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int c = threadIdx.x + u * kPolicyThreads;
+    const int c = thread + u * kRow;
     a[u] = c < chunks ? row.load(c) : Logit<T>::lowest();
   }
   PolicySum mine = {-INFINITY, 0.0f};
   add_chunks<T, U>(mine, a, k);
   mine = join_sums<32>(mine, k);
-  if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32] = mine;
-  __syncthreads();
-  mine = join_sums<kPolicyWarps>(sh.warp[threadIdx.x % kPolicyWarps], k);
-  if (threadIdx.x < 32) {
-    const RowTerms t = finish_sum(p, in, mine, at, k);
-    if (threadIdx.x == 0) {
-      sh.row = t;
-      write_loss(p, r, t);
+  RowTerms t;
+  if constexpr (kWarps == 1) {
+    t = finish_sum(p, in, mine, at, k);      // all lanes read the row before one writes it: they have met in the sums
+    if (thread == 0) write_loss(p, r, t);
+  } else {
+    if (thread % 32 == 0) warps[thread / 32] = mine;
+    __syncthreads();
+    if (thread < 32) {
+      mine = join_sums<kWarps>(warps[thread % kWarps], k);
+      t = finish_sum(p, in, mine, at, k);
+      if (thread == 0) {
+        shared_terms = t;
+        write_loss(p, r, t);
+      }
     }
+    __syncthreads();
+    t = shared_terms;
   }
-  __syncthreads();
-  const RowTerms t = sh.row;
-  if (t.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, 0, chunks, threadIdx.x, kPolicyThreads);
+  if (t.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, 0, chunks, thread, kRow);
   const PolicyGrad g = {k, t, label};
 #pragma unroll
   for (int u = 0; u < U; ++u)
-    if (threadIdx.x + u * kPolicyThreads < chunks) policy_chunk<T>(row, dz, same_grid, threadIdx.x + u * kPolicyThreads, a[u], g);
+    if (thread + u * kRow < chunks) policy_chunk<T>(row, dz, same_grid, thread + u * kRow, a[u], g);
 }
 
 // ---- rows in shared memory -----------------------------------------------------------------------------------
@@ -651,7 +663,7 @@ using namespace slidedp::host;
 namespace {
 
 constexpr int kSms = 148;
-constexpr int64_t kHeldChunks = 8 * kPolicyThreads;          // rows up to 32 KB are held in registers
+constexpr int64_t kHeldChunks = 8 * 512;                 // rows up to 64 KB are held in registers
 constexpr int64_t kMaxSliceChunks = 8704;                    // of the ring's 13312
 constexpr int64_t kMinSliceChunks = 512;
 constexpr int64_t kEnoughBlocks = kSms * 4, kRound = kSms * 5;
@@ -732,17 +744,29 @@ int run_policy(slidedp_ctx* ctx, const slidedp_policy_args* a, PolicyMode mode, 
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return cuda_fail(ctx, cudaGetLastError());
   cudaStream_t stream = st;
-  const int64_t chunks = (a->vocab * elem + 15) / 16 + 1;   // an unaligned row touches one more
+  const bool aligned = !odd(logits, 16) && (a->rows == 1 || a->logits_stride * elem % 16 == 0);
+  const int64_t chunks = (a->vocab * elem + 15) / 16 + !aligned;   // an unaligned row touches one more
   p.error = ctx->kernel_error;
   p.polls = ctx->wait_polls;
   const bool f32 = a->dtype == SLIDEDP_F32;
   FAULT_POINT();
   cudaError_t failed = cudaSuccess;
   if (mode == kPolicyStep && chunks <= kHeldChunks) {
-    const auto run = [&](auto kernel) { launch_after(kernel, dim3((unsigned)a->rows), kPolicyThreads, 0, 1, stream, p); };
+    const auto run = [&](auto kernel, int row) {
+      const int64_t rows = row < 256 ? 256 / row : 1;
+      launch_after(kernel, dim3((unsigned)((a->rows + rows - 1) / rows)), row < 256 ? 256 : row, 0, 1, stream, p);
+    };
     const auto held = [&](auto type) {
       typedef decltype(type) T;
-      chunks <= 2 * kPolicyThreads ? run(policy_held_kernel<T, 2>) : chunks <= 4 * kPolicyThreads ? run(policy_held_kernel<T, 4>) : run(policy_held_kernel<T, 8>);
+      if (chunks <= 4 * 32) run(policy_held_kernel<T, 4, 32>, 32);
+      else if (chunks <= 8 * 32) run(policy_held_kernel<T, 8, 32>, 32);
+      else if (chunks <= 16 * 32) run(policy_held_kernel<T, 16, 32>, 32);
+      else if (chunks <= 3 * 256) run(policy_held_kernel<T, 3, 256>, 256);
+      else if (chunks <= 4 * 256) run(policy_held_kernel<T, 4, 256>, 256);
+      else if (chunks <= 6 * 256) run(policy_held_kernel<T, 6, 256>, 256);
+      else if (chunks <= 8 * 256) run(policy_held_kernel<T, 8, 256>, 256);
+      else if (chunks <= 6 * 512) run(policy_held_kernel<T, 6, 512>, 512);
+      else run(policy_held_kernel<T, 8, 512>, 512);
     };
     f32 ? held(float()) : held(uint16_t());
   } else if (mode == kPolicyStep && chunks <= kPolicyMaxCluster * kMaxSliceChunks) {

@@ -559,3 +559,15 @@ def test_policy_rows_of_the_lowest_value(ctx, V, dtype):
     a["old"], a["ref"] = (lp + 0.1).float(), (lp - 0.3).float()
     for tau in (1.0, 0.6):
         policy_case(ctx, a, tau=tau, kl=0.05 if tau == 1.0 else 0.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_policy_rows_at_the_limits_of_their_kernels(ctx, dtype):
+    """Rows that just fit what a warp, a block or the ring holds, and rows one chunk longer, aligned and not."""
+    per = 16 // dtype.itemsize
+    for chunks in (128, 256, 512, 768, 1024, 1536, 2048, 3072, 4096, 8704):
+        for V in (chunks * per, chunks * per + 1):
+            a = policy_inputs(3, V, dtype, seed=chunks)
+            policy_case(ctx, a)
+            if chunks in (128, 2048, 4096):
+                policy_case(ctx, a, layout=(1, 1))
