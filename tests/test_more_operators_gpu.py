@@ -565,7 +565,7 @@ def test_policy_rows_of_the_lowest_value(ctx, V, dtype):
 def test_policy_rows_at_the_limits_of_their_kernels(ctx, dtype):
     """Rows that just fit what a warp, a block or the ring holds, and rows one chunk longer, aligned and not."""
     per = 16 // dtype.itemsize
-    for chunks in (128, 256, 512, 768, 1024, 1536, 2048, 3072, 4096, 8704):
+    for chunks in (128, 256, 512, 768, 1024, 1536, 2048, 2560, 4096, 8704):
         for V in (chunks * per, chunks * per + 1):
             a = policy_inputs(3, V, dtype, seed=chunks)
             policy_case(ctx, a)
