@@ -12,7 +12,7 @@
  * Calls of this header on one context may go to different streams and come from different threads, also at once (but not
  * beside other calls on that context); workspaces must not be shared by calls that can overlap.
  *
- * The attention and distillation kernels wait on copies and on blocks of their own launch; every such wait is bounded (about
+ * The attention, distillation, block-norm and policy-step kernels wait on copies and on blocks of their own launch; every such wait is bounded (about
  * a minute). If one runs out, the results of that call are not complete, and the first of these calls on the
  * context to start after that returns SLIDEDP_ERR_TIMEOUT, once, and does nothing else: any operator of this header; a
  * slidedp_grad_norm_finish or slidedp_grad_norm_finish_from that fetches its results (they are fetched all the same); or
@@ -198,8 +198,8 @@ typedef struct {
  *   d_table[v] = scale * sum of d_out[t] over the t with ids[t] = v     d_out of `dtype`, d_table of `grad_dtype`
  * ids: device, one int32 per token. A token whose id lies outside [0, vocab) is absent (padding): its row of out is zeros,
  * its row of d_out is not read. accumulate = 0 writes all of d_table, zeros for ids that no token has; 1 adds to what
- * d_table holds, and touches only the rows of ids that occur. The sum over a row's tokens is FP32 in an order that depends on
- * the ids alone, scaled and (with what was there) rounded once. d_table may not overlap d_out, nor out the table.
+ * d_table holds, and touches only the rows of ids that occur. The sum over a row's tokens is FP32 in an order that follows
+ * from the ids and the sizes, scaled and (with what was there) rounded once. d_table may not overlap d_out, nor out the table.
  * tokens and vocab up to 2^30, hidden up to 2^20.
  * workspace: device, slidedp_embedding_workspace bytes, 16-byte aligned.
  */
@@ -237,7 +237,9 @@ SLIDEDP_API size_t slidedp_embedding_workspace(const slidedp_embedding_args* arg
  * An output may be an input of the same form (same address and stride: x' = x, dx = dx_out, dy = y, ..): each row is read
  * before it is written. The same address with another stride is refused, as are two outputs at one address; outputs may not
  * overlap otherwise. workspace: device, slidedp_block_norm_workspace bytes, 16-byte aligned; needed where dw_post, dw_pre or
- * the dgate of a gate for all tokens is wanted.
+ * the dgate of a gate for all tokens is wanted. The squares are added up in FP32: a row whose sum passes its range is
+ * normalised to zeros, and eps = 0 makes a row of zeros NaN. Fastest up to 8192 columns (a gradient of FP32 rows with a gate
+ * [tokens, hidden]: 7680).
  */
 typedef struct {
   int64_t tokens, hidden;
@@ -274,7 +276,8 @@ SLIDEDP_API size_t slidedp_block_norm_workspace(const slidedp_block_norm_args* a
  * Gradient: d_logits[r] = row_grad[r] * d loss[r] / d z, with row_grad: rows floats (nullable: ones). A ratio on the edge of the
  * clipped range counts as inside. slidedp_policy_loss_backward takes the forward's logp;
  * slidedp_policy_step computes loss, logp and gradient in one call. d_logits may be the logits themselves (same address and
- * stride; the same address with another stride is refused). Rows whose gradient is zero throughout (absent, clipped without a
+ * stride; the same address with another stride is refused) and may not overlap them otherwise. A kl_weight of 0 is no second
+ * term, whatever ref_logp holds. Rows whose gradient is zero throughout (absent, clipped without a
  * second term, row_grad 0) are zeros whatever their logits hold; in others NaN and +inf among the logits make the row NaN.
  */
 typedef struct {
@@ -304,7 +307,8 @@ SLIDEDP_API int slidedp_policy_step(slidedp_ctx* ctx, const slidedp_policy_args*
  * slidedp_reduce_adamw_chunk takes (with max_norm 0 there). grads, outs: host arrays of `count` tensors each, read before the
  * call returns; outs[i] has grads[i].count elements of either type and may be grads[i] itself (same address and type); outs NULL:
  * only result is written. Tensors need the alignment of their element; they may be empty. A factor of 1 in place writes nothing.
- * With max_norm > 0 a NaN norm makes coef and with it every output NaN, an infinite one makes coef 0. The sums are FP64 in an order that the tensors' sizes alone decide.
+ * With max_norm > 0 a NaN norm makes coef and with it every output NaN, an infinite one makes coef 0. The sums are FP64 in an order that the tensors' sizes and alignment decide. No tensor of
+ * outs may overlap another one, or a tensor of grads other than its own.
  * workspace: device, slidedp_clip_grad_norm_workspace bytes, 16-byte aligned.
  */
 typedef struct {

@@ -3,9 +3,9 @@
 // n = y r w_post, x' = x + a g n, h = x' r' w_pre with r = rsqrt(mean y^2 + eps), r' = rsqrt(mean x'^2 + eps). Backward:
 //   u = dh w_pre, d = dx' + r' (u - x' r'^2 mean(u x')), dx = d
 //   v = a d g w_post, dy = r (v - y r mean(v y r)), dgate = a d n g', dw_pre = sum dh x' r', dw_post = sum a d g y r
-// Bound: HBM; every tensor is read or written once. A row is held in the registers of one block, 16 values per thread, its sums are
-// joined through shared memory; blocks stay and take every (number of blocks)th row, with the weights and the sums of their
-// gradients in registers. One partial row of sums per block, added in a fixed order by a second kernel.
+// Bound: HBM; every tensor is read or written once, and x' is computed anew backward rather than kept. Blocks stay, one per SM, and take
+// row after row, with the sums of the weights' gradients; each has one partial row of them, which a second kernel adds in
+// a fixed order. Rows of up to 8192 columns are copied into shared memory ahead of their use, wider ones are read as they are needed.
 #include "ops_internal.h"
 #include "rows.cuh"
 #include "tcgen05.cuh"
@@ -56,6 +56,14 @@ __device__ __forceinline__ float2 block_sums(float a, float b, BlockSums& sh, in
   return v;
 }
 
+// ---- wide rows ----------------------------------------------------------------------------------------------
+// Rows that the rings below have no room for: more than 8192 columns, or FP32 ones close to that with a token's gate. A block of up to
+// 1024 threads takes a row, 16 values per thread.
+
+constexpr int kWideThreads = 1024, kWideValues = 16;
+
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 // A thread's N values of a row: vectors of V, blockDim vectors apart.
 template <typename T, int V, int N>
 struct Values {
@@ -74,6 +82,44 @@ struct Values {
     for (int k = 0; k < N / V; ++k) to_floats<T, V>(a[k], v + k * V);
   }
 };
+template <typename T, int V>
+__device__ __forceinline__ void get_vector(const void* row, int64_t at, float* v) {
+  to_floats<T, V>(*reinterpret_cast<const typename Raw<T, V>::type*>(static_cast<const T*>(row) + at), v);
+}
+// The factor a g w_post of y r of one vector, and the gate.
+template <typename T, int V, bool kToken>
+__device__ __forceinline__ void wide_factor(const BlockNormParams& p, int64_t row, int col, float* f, float* g) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) f[e] = 1.0f;
+  if (p.w_post) get_vector<T, V>(p.w_post, col, f);
+#pragma unroll
+  for (int e = 0; e < V; ++e) f[e] *= p.alpha;
+  if (!kToken && !p.gate_kind) return;
+  get_vector<T, V>(p.gate.p, kToken ? row * p.gate.stride + col : col, g);
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    if (p.sigmoid) g[e] = sigmoid(g[e]);
+    f[e] *= g[e];
+  }
+}
+// What is read of a row, to L2.
+template <typename T, bool kToken>
+__device__ __forceinline__ void fetch_row(const BlockNormParams& p, int64_t row) {
+  if (row >= p.tokens) return;
+  const int step = 128 / (int)sizeof(T), last = p.hidden - 1;
+  for (int c = threadIdx.x * step; c < p.hidden + step; c += blockDim.x * step) {
+    const int col = c < last ? c : last;
+    const auto line = [&](const NormView& v) {
+      if (v.p) prefetch_l2(static_cast<const T*>(v.p) + row * v.stride + col);
+    };
+    line(p.x);
+    line(p.y);
+    line(p.dx_out);
+    line(p.dh);
+    if (kToken) line(p.gate);
+  }
+}
+
 template <typename T, int V, int N>
 __device__ __forceinline__ void store_row(void* p, int64_t at, int hidden, const float* v) {
 #pragma unroll
@@ -94,11 +140,13 @@ __device__ __forceinline__ void weights(const void* w, int hidden, float* v) {
   }
 }
 
-// kToken: the gate is [tokens, hidden].
-template <typename T, int V, int N, bool kToken, int kThreads>
-__global__ void __launch_bounds__(kThreads) block_norm_kernel(const __grid_constant__ BlockNormParams p) {
+// kToken: the gate is [tokens, hidden]. Each thread has its columns to itself, with the weights in registers, so rows may be written
+// where they were read. 2048 x 16384 BF16, both norms: 53 us (61 without fetching the next row to L2).
+template <typename T, int V, bool kToken>
+__global__ void __launch_bounds__(kWideThreads) block_norm_kernel(const __grid_constant__ BlockNormParams p) {
   start_after_previous_kernel();
   __shared__ BlockSums sh;
+  constexpr int N = kWideValues;
   int turn = 0;
   float w_post[N], w_pre[N];
   weights<T, V, N>(p.w_post, p.hidden, w_post);
@@ -110,6 +158,7 @@ __global__ void __launch_bounds__(kThreads) block_norm_kernel(const __grid_const
     for (int i = 0; i < N; ++i) w_post[i] *= p.sigmoid ? sigmoid(g[i]) : g[i];
   }
   for (int64_t row = blockIdx.x; row < p.tokens; row += gridDim.x) {
+    fetch_row<T, kToken>(p, row + gridDim.x);
     Values<T, V, N> raw, raw_y, raw_g;
     raw.load(p.x.p, row * p.x.stride, p.hidden);
     if (p.has_y) raw_y.load(p.y.p, row * p.y.stride, p.hidden);
@@ -147,108 +196,121 @@ __global__ void __launch_bounds__(kThreads) block_norm_kernel(const __grid_const
   }
 }
 
-template <typename T, int V, int N, bool kToken, int kThreads>
-__global__ void __launch_bounds__(kThreads) block_norm_backward_kernel(const __grid_constant__ BlockNormParams p) {
+// A row's values are read where a sum asks for them, by then from L2, into which each row is fetched while the one before it is
+// computed: x' and y stay in registers, all of the row and the weights would not (64 for each of 1024 threads), and the sums of the
+// weights' gradients lie in shared memory. 2048 x 16384 BF16, both norms: 170 us; with everything in registers, spilled, 934.
+template <typename T, int V, bool kToken>
+__global__ void __launch_bounds__(kWideThreads) block_norm_backward_kernel(const __grid_constant__ BlockNormParams p) {
+  extern __shared__ uint4 dynamic[];
   start_after_previous_kernel();
   __shared__ BlockSums sh;
+  constexpr int N = kWideValues, K = N / V;
   int turn = 0;
-  Values<T, V, N> raw_w_post, raw_w_pre, raw_gate;
-  if (p.w_post) raw_w_post.load(p.w_post, 0, p.hidden);
-  if (p.w_pre) raw_w_pre.load(p.w_pre, 0, p.hidden);
-  if (!kToken && p.gate_kind) raw_gate.load(p.gate.p, 0, p.hidden);
-  float sum_post[N] = {}, sum_pre[N] = {};
+  const int n = blockDim.x, t = threadIdx.x;
+  float *sum_post = reinterpret_cast<float*>(dynamic) + t, *sum_pre = sum_post + N * n;     // value i at i n
+  if (p.partial) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum_post[i * n] = sum_pre[i * n] = 0.0f;
+  }
+  fetch_row<T, kToken>(p, blockIdx.x);
   for (int64_t row = blockIdx.x; row < p.tokens; row += gridDim.x) {
-    Values<T, V, N> rx, ry, rg, rd, rh;
-    rx.load(p.x.p, row * p.x.stride, p.hidden);
-    if (p.has_y) ry.load(p.y.p, row * p.y.stride, p.hidden);
-    if (kToken) rg.load(p.gate.p, row * p.gate.stride, p.hidden);
-    if (p.dx_out.p) rd.load(p.dx_out.p, row * p.dx_out.stride, p.hidden);
-    if (p.pre) rh.load(p.dh.p, row * p.dh.stride, p.hidden);
-    float y[N], f[N], g[N], x[N], r = 1.0f;      // y r, the factor a g w_post of it, the gate
-    rx.get(x);
+    fetch_row<T, kToken>(p, row + gridDim.x);
+    Values<T, V, N> raw_y;
+    float r = 1.0f, r2 = 0.0f, m = 0.0f, x[N];       // x', then v
     if (p.has_y) {
-      ry.get(y);
+      raw_y.load(p.y.p, row * p.y.stride, p.hidden);
       if (p.post) {
-        float s = 0.0f;
+        float s = 0.0f, y[N];
+        raw_y.get(y);
 #pragma unroll
         for (int i = 0; i < N; ++i) s = fmaf(y[i], y[i], s);
         r = rsqrtf(block_sums(s, 0.0f, sh, turn).x * p.inv_hidden + p.eps);
       }
-#pragma unroll
-      for (int i = 0; i < N; ++i) f[i] = p.alpha;
-      if (p.w_post) {
-        raw_w_post.get(f);
-#pragma unroll
-        for (int i = 0; i < N; ++i) f[i] *= p.alpha;
-      }
-      if (kToken) rg.get(g);
-      else if (p.gate_kind) raw_gate.get(g);
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if (kToken || p.gate_kind) {
-          if (p.sigmoid) g[i] = sigmoid(g[i]);
-          f[i] *= g[i];
-        }
-        y[i] *= r;
-        x[i] = fmaf(f[i], y[i], x[i]);
-      }
     }
-    float d[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) d[i] = 0.0f;
-    if (p.dx_out.p) rd.get(d);
     if (p.pre) {
-      float h[N], u[N], ss = 0.0f, ux = 0.0f;
-      rh.get(h);
+      float ss = 0.0f, ux = 0.0f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) u[i] = 1.0f;
-      if (p.w_pre) raw_w_pre.get(u);
+      for (int k = 0; k < K; ++k) {
+        const int col = (k * n + t) * V;
+        float *xk = x + k * V, f[V], g[V], y[V], h[V], w[V];
+        if (col >= p.hidden) continue;
+        get_vector<T, V>(p.x.p, row * p.x.stride + col, xk);
+        if (p.has_y) {
+          wide_factor<T, V, kToken>(p, row, col, f, g);
+          to_floats<T, V>(raw_y.a[k], y);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        u[i] *= h[i];
-        ss = fmaf(x[i], x[i], ss);
-        ux = fmaf(u[i], x[i], ux);
+          for (int e = 0; e < V; ++e) xk[e] = fmaf(f[e], y[e] * r, xk[e]);
+        }
+        get_vector<T, V>(p.dh.p, row * p.dh.stride + col, h);
+        if (p.w_pre) get_vector<T, V>(p.w_pre, col, w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          ss = fmaf(xk[e], xk[e], ss);
+          ux = fmaf(p.w_pre ? h[e] * w[e] : h[e], xk[e], ux);
+        }
       }
       const float2 s = block_sums(ss, ux, sh, turn);
-      const float r2 = rsqrtf(s.x * p.inv_hidden + p.eps), m = s.y * r2 * p.inv_hidden;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float xh = x[i] * r2;
-        sum_pre[i] = fmaf(h[i], xh, sum_pre[i]);
-        d[i] = fmaf(r2, fmaf(-xh, m, u[i]), d[i]);
-      }
+      r2 = rsqrtf(s.x * p.inv_hidden + p.eps);
+      m = s.y * r2 * p.inv_hidden;
     }
-    store_row<T, V, N>(p.dx.p, row * p.dx.stride, p.hidden, d);
-    if (p.has_y) {
-      float dot = 0.0f;
+    float dot = 0.0f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float ad = p.alpha * d[i];
-        sum_post[i] = fmaf(kToken ? ad * g[i] : ad, y[i], sum_post[i]);
-        f[i] *= d[i];                          // now v
-        dot = fmaf(f[i], y[i], dot);
+    for (int k = 0; k < K; ++k) {
+      const int col = (k * n + t) * V;
+      if (col >= p.hidden) continue;
+      float *v = x + k * V, d[V] = {}, f[V], g[V], y[V], h[V], w[V];
+      if (p.dx_out.p) get_vector<T, V>(p.dx_out.p, row * p.dx_out.stride + col, d);
+      if (p.pre) {
+        get_vector<T, V>(p.dh.p, row * p.dh.stride + col, h);
+        if (p.w_pre) get_vector<T, V>(p.w_pre, col, w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float xh = v[e] * r2;
+          if (p.partial) sum_pre[(k * V + e) * n] += h[e] * xh;
+          d[e] = fmaf(r2, fmaf(-xh, m, p.w_pre ? h[e] * w[e] : h[e]), d[e]);
+        }
       }
-      if (kToken && p.dgate.p) {               // a d n g', n = y r w_post
-        float w[N];
+      if (p.has_y) {
+        wide_factor<T, V, kToken>(p, row, col, f, g);                       // before this vector of dx or dgate may take its place
+        if (kToken && p.dgate.p && p.w_post) get_vector<T, V>(p.w_post, col, w);
+        to_floats<T, V>(raw_y.a[k], y);
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = 1.0f;
-        if (p.w_post) raw_w_post.get(w);
-#pragma unroll
-        for (int i = 0; i < N; ++i) w[i] *= p.alpha * d[i] * y[i] * (p.sigmoid ? g[i] * (1.0f - g[i]) : 1.0f);
-        store_row<T, V, N>(p.dgate.p, row * p.dgate.stride, p.hidden, w);
+        for (int e = 0; e < V; ++e) {
+          y[e] *= r;
+          const float ad = p.alpha * d[e];
+          if (p.partial) sum_post[(k * V + e) * n] += (kToken ? ad * g[e] : ad) * y[e];
+          v[e] = f[e] * d[e];
+          dot = fmaf(v[e], y[e], dot);
+          if (kToken) g[e] = ad * y[e] * (p.w_post ? w[e] : 1.0f) * (p.sigmoid ? g[e] * (1.0f - g[e]) : 1.0f);   // a d n g'
+        }
+        if (kToken && p.dgate.p) store_values<V>(static_cast<T*>(p.dgate.p) + row * p.dgate.stride + col, g);
       }
+      store_values<V>(static_cast<T*>(p.dx.p) + row * p.dx.stride + col, d);
+    }
+    if (!p.has_y) continue;
+    if (p.post) m = block_sums(dot, 0.0f, sh, turn).x * p.inv_hidden;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int col = (k * n + t) * V;
+      if (col >= p.hidden) continue;
+      float* v = x + k * V;
       if (p.post) {
-        const float m = block_sums(dot, 0.0f, sh, turn).x * p.inv_hidden;
+        float y[V];
+        to_floats<T, V>(raw_y.a[k], y);
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = r * fmaf(-y[i], m, f[i]);
+        for (int e = 0; e < V; ++e) v[e] = r * fmaf(-(y[e] * r), m, v[e]);
       }
-      store_row<T, V, N>(p.dy.p, row * p.dy.stride, p.hidden, f);
+      store_values<V>(static_cast<T*>(p.dy.p) + row * p.dy.stride + col, v);
     }
   }
-  if (p.partial) {
-    float* at = p.partial + (int64_t)blockIdx.x * 2 * p.hidden;
-    store_row<float, V, N>(at, 0, p.hidden, sum_post);
-    store_row<float, V, N>(at, p.hidden, p.hidden, sum_pre);
+  if (!p.partial) return;
+  float* at = p.partial + (int64_t)blockIdx.x * 2 * p.hidden;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int col = (i / V * n + t) * V + i % V;
+    if (col >= p.hidden) continue;
+    at[col] = sum_post[i * n];
+    at[p.hidden + col] = sum_pre[i * n];
   }
 }
 
@@ -258,9 +320,9 @@ __global__ void __launch_bounds__(kThreads) block_norm_backward_kernel(const __g
 // them, else single columns, neighbours with neighbouring threads. The factors of y r and of x' r' lie before the rings in FP32, for all
 // groups. Two values per instruction. What bounds a group is the chain of its two or three sums over the row (700 cycles each);
 // what a row needs is kept in registers from one sum to the next, which leaves room for two groups of 256 threads (three, with
-// 80 registers and values read again from shared memory, took 150 us backward where two take NOW_B).
-// 8192 x 4096 BF16, both norms: forward 96 us with rows in registers and no copies ahead, 54 as blocks with a ring each, NOW_F now;
-// backward 166, 88, NOW_B.
+// 80 registers and values read again from shared memory, took 150 us backward where two take 87).
+// 8192 x 4096 BF16, both norms: forward 96 us with rows in registers and no copies ahead, 54 as blocks with a ring each, 51 now
+// (268 MB at 5.2 TB/s); backward 166, 95, 87.
 
 __device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
 __device__ __forceinline__ float sum_of(uint64_t v) {
@@ -373,7 +435,10 @@ __device__ __forceinline__ float2 group_sums(float a, float b, float2 (*part)[kW
   float v = (upper ? b : a) + __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if (n == 32) return make_float2(__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16));
+  if (n == 32) {
+    __syncwarp();        // all lanes have read what is copied over next
+    return make_float2(__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16));
+  }
   turn ^= 1;
   if (t % 16 == 0) reinterpret_cast<float*>(&part[turn][t / 32])[t / 16 % 2] = v;
   group_sync(group, n);
@@ -628,7 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_backward_ring_kernel(c
   const bool leader = cols.t == 0;
   const bool has_y = kFull || p.has_y, norm_y = kFull || p.post, norm_x = kFull || p.pre;
   // Whether a row stays in registers from one sum to the next, as far as there are any: a token's gate is 32 more, single columns take
-  // more to address. Their rows are read again (8192 x 4096 BF16 with such a gate: 158 -> GATE2 us).
+  // more to address. Their rows are read again (8192 x 4096 BF16 with such a gate: 158 -> 124 us).
   constexpr bool kKeep = kVector && !kToken;
   uint64_t sum_post[kPairs] = {}, sum_pre[kPairs] = {};
   int turn = 0;
@@ -817,18 +882,12 @@ int check_norm(const slidedp_block_norm_args* a) {
   return SLIDEDP_OK;
 }
 
-// Values per thread: 16, or 8 where that is as many registers; longer FP32 rows would need more threads than a block has.
-int values_per_thread(const slidedp_block_norm_args* a) { return a->dtype == SLIDEDP_F32 && a->hidden <= 4096 ? 8 : 16; }
-unsigned norm_threads(const slidedp_block_norm_args* a) {
-  const int64_t n = (a->hidden + values_per_thread(a) - 1) / values_per_thread(a);
-  return (unsigned)((n + 31) / 32 * 32);
-}
-// Blocks that stay, of which each has a row of partial sums: at most 16 per SM, or the second kernel becomes long.
-constexpr int kMaxNormBlocks = 16;
-int64_t norm_blocks(const slidedp_block_norm_args* a, int per_sm) {
-  const int64_t most = 148 * (per_sm < 1 ? 1 : per_sm > kMaxNormBlocks ? kMaxNormBlocks : per_sm);
-  return a->tokens < most ? a->tokens : most;
-}
+unsigned wide_threads(const slidedp_block_norm_args* a) { return (unsigned)((a->hidden + kWideValues * 32 - 1) / (kWideValues * 32) * 32); }
+// Blocks that stay, of which each has a row of partial sums: one per SM, or two wide rows' ones with up to half the threads (2048 x 8192
+// FP32 with a token's gate, backward: 242 -> 174 us).
+constexpr int kSms = 148;
+int64_t norm_blocks(const slidedp_block_norm_args* a, int per_sm) { return a->tokens < kSms * per_sm ? a->tokens : kSms * per_sm; }
+int wide_per_sm(const slidedp_block_norm_args* a) { return wide_threads(a) <= kWideThreads / 2 ? 2 : 1; }
 
 // Whether the outputs may be where they are: not two of them at one address, none at an input's with another stride.
 bool places_ok(std::initializer_list<const slidedp_rows*> outs, std::initializer_list<const slidedp_rows*> ins, int64_t rows) {
@@ -861,26 +920,13 @@ BlockNormParams norm_params(const slidedp_block_norm_args* a) {
   return p;
 }
 
-// run(T, V, N, threads) as template arguments
+// run(T, V) as template arguments
 template <typename F>
-void pick_norm_kernel(const slidedp_block_norm_args* a, int v, F run) {
-  typedef std::integral_constant<int, 8> N8;
-  typedef std::integral_constant<int, 16> N16;
-  const bool wide = norm_threads(a) > 512;
-  const auto width = [&](auto type, auto n, auto full) {
-    typedef std::integral_constant<int, 512> Up512;
-    typedef std::integral_constant<int, 1024> Up1024;
-    typedef std::integral_constant<int, 1> One;
-    typedef std::integral_constant<int, 2> Two;
-    const auto threads = [&](auto vector) { wide ? run(type, vector, n, Up1024()) : run(type, vector, n, Up512()); };
-    if (v == full) return threads(full);
-    if constexpr (sizeof(type) == 2)
-      if (v == 2) return threads(Two());
-    threads(One());
-  };
-  if (a->dtype == SLIDEDP_BF16) width(uint16_t(), N16(), std::integral_constant<int, 8>());
-  else if (values_per_thread(a) == 8) width(float(), N8(), std::integral_constant<int, 4>());
-  else width(float(), N16(), std::integral_constant<int, 4>());
+void pick_wide_kernel(const slidedp_block_norm_args* a, int v, F run) {
+  typedef std::integral_constant<int, 1> One;
+  if (a->dtype == SLIDEDP_F32) v == 4 ? run(float(), std::integral_constant<int, 4>()) : run(float(), One());
+  else if (v == 8) run(uint16_t(), std::integral_constant<int, 8>());
+  else v == 2 ? run(uint16_t(), std::integral_constant<int, 2>()) : run(uint16_t(), One());
 }
 
 // A block per SM whose groups hold their rows in shared memory: threads of a group, groups, stages of a ring. The kernels are compiled for
@@ -911,8 +957,6 @@ RingPlan ring_plan(const slidedp_block_norm_args* a, bool vector, int inputs, bo
     }
   return r;
 }
-// Rows go to groups block by block: all SMs have one before one has two.
-unsigned ring_grid(const slidedp_block_norm_args* a) { return (unsigned)(a->tokens < 148 ? a->tokens : 148); }
 NormRingParams ring_params(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const BlockNormParams& n, const RingPlan& plan) {
   NormRingParams r = {};
   r.n = n;
@@ -990,6 +1034,7 @@ int slidedp_block_norm(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const RingPlan plan = ring_plan(a, v * elem == 16, 1 + (y != nullptr) + (a->gate_kind == 2), false);
   cudaError_t attribute = cudaSuccess;
+  const unsigned blocks = (unsigned)norm_blocks(a, plan.use ? 1 : wide_per_sm(a));      // rows go to groups block by block: all SMs have one before one has two
   FAULT_POINT();
   if (plan.use) {
     const NormRingParams r = ring_params(ctx, a, p, plan);
@@ -997,15 +1042,15 @@ int slidedp_block_norm(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const
       typedef decltype(type) T_;
       const auto run = [&](auto kernel) {
         attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem);
-        if (attribute == cudaSuccess) launch_after(kernel, dim3(ring_grid(a)), plan.threads * plan.groups, plan.smem, 1, st, r);
+        if (attribute == cudaSuccess) launch_after(kernel, dim3(blocks), plan.threads * plan.groups, plan.smem, 1, st, r);
       };
       run(block_norm_ring_kernel<T_, vector, token, full, threads, warps>);
     });
   } else {
-    pick_norm_kernel(a, v, [&](auto type, auto vec, auto n, auto threads) {
+    pick_wide_kernel(a, v, [&](auto type, auto vec) {
       typedef decltype(type) T_;
-      const auto run = [&](auto kernel) { launch_after(kernel, dim3((unsigned)norm_blocks(a, 640 / norm_threads(a))), norm_threads(a), 0, 1, st, p); };
-      a->gate_kind == 2 ? run(block_norm_kernel<T_, vec, n, true, threads>) : run(block_norm_kernel<T_, vec, n, false, threads>);
+      const auto run = [&](auto kernel) { launch_after(kernel, dim3(blocks), wide_threads(a), 0, 1, st, p); };
+      a->gate_kind == 2 ? run(block_norm_kernel<T_, vec, true>) : run(block_norm_kernel<T_, vec, false>);
     });
   }
   if (attribute != cudaSuccess) return cuda_fail(ctx, attribute);
@@ -1016,7 +1061,7 @@ int slidedp_block_norm(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const
 
 size_t slidedp_block_norm_workspace(const slidedp_block_norm_args* a) {
   if (check_norm(a) != SLIDEDP_OK) return 0;
-  return (size_t)(norm_blocks(a, kMaxNormBlocks) * 2 * a->hidden) * sizeof(float) + 16;
+  return (size_t)(norm_blocks(a, 2) * 2 * a->hidden) * sizeof(float) + 16;
 }
 
 int slidedp_block_norm_backward(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const slidedp_rows* x, const slidedp_rows* y,
@@ -1076,7 +1121,7 @@ int slidedp_block_norm_backward(slidedp_ctx* ctx, const slidedp_block_norm_args*
                                          {&wp, elem}, {&wq, elem}});
     const RingPlan plan = ring_plan(a, v * elem == 16, 1 + (y != nullptr) + (a->gate_kind == 2) + (dx_out != nullptr) + a->pre_norm, true);
     cudaError_t attribute = cudaSuccess;
-    blocks = plan.use ? ring_grid(a) : (unsigned)norm_blocks(a, 640 / norm_threads(a));
+    blocks = (unsigned)norm_blocks(a, plan.use ? 1 : wide_per_sm(a));
     FAULT_POINT();
     if (plan.use) {
       const NormRingParams r = ring_params(ctx, a, p, plan);
@@ -1089,10 +1134,14 @@ int slidedp_block_norm_backward(slidedp_ctx* ctx, const slidedp_block_norm_args*
         run(block_norm_backward_ring_kernel<T_, vector, token, full, threads, warps>);
       });
     } else {
-      pick_norm_kernel(a, v, [&](auto type, auto vec, auto n, auto threads) {
+      pick_wide_kernel(a, v, [&](auto type, auto vec) {
         typedef decltype(type) T_;
-        const auto run = [&](auto kernel) { launch_after(kernel, dim3(blocks), norm_threads(a), 0, 1, st, p); };
-        a->gate_kind == 2 ? run(block_norm_backward_kernel<T_, vec, n, true, threads>) : run(block_norm_backward_kernel<T_, vec, n, false, threads>);
+        const size_t smem = sums ? (size_t)wide_threads(a) * kWideValues * 2 * sizeof(float) : 0;
+        const auto run = [&](auto kernel) {
+          attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideThreads * kWideValues * 2 * (int)sizeof(float));
+          if (attribute == cudaSuccess) launch_after(kernel, dim3(blocks), wide_threads(a), smem, 1, st, p);
+        };
+        a->gate_kind == 2 ? run(block_norm_backward_kernel<T_, vec, true>) : run(block_norm_backward_kernel<T_, vec, false>);
       });
     }
     if (attribute != cudaSuccess) return cuda_fail(ctx, attribute);

@@ -270,6 +270,35 @@ def test_block_norm_in_place(ctx, dtype):
     assert torch.equal(a, dx) and torch.equal(b, dy)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_block_norm_of_wide_rows(ctx, dtype):
+    """Rows that do not fit a ring: several for each block, every form, and written where they were read."""
+    norm_case(ctx, 310, 8200, dtype)
+    norm_case(ctx, 310, 8200, dtype, gate=1, sigmoid=True)
+    norm_case(ctx, 310, 8193, dtype, gate=2, sigmoid=True, layout=(3, 1))
+    norm_case(ctx, 601, 8190, dtype, gate=2, sigmoid=True)          # of these FP32 rows two blocks per SM
+    norm_case(ctx, 150, 9002, dtype, gate=2, pre=False, weights=False)
+    norm_case(ctx, 150, 9002, dtype, gate=1, post=False, layout=(2, 0))
+    norm_case(ctx, 150, 9000, dtype, with_y=False, post=False, dx_out=False)
+    norm_case(ctx, 150, 9000, dtype, sums=False, weights=False)
+    norm_case(ctx, 150, 9000, dtype, post=False, pre=False)
+    g = gen(8)
+    T, H = 320, 8704
+    x, y, gx, gh, gate = (randn(g, T, H, dtype=dtype) for _ in range(5))
+    w = [randn(g, H, dtype=dtype) for _ in range(2)]
+    x2, h, dx, dy, dgate = (torch.empty_like(x) for _ in range(5))
+    ctx.slidedp_block_norm(x, y, w[0], gate, w[1], x2, h)
+    a, b = x.clone(), y.clone()
+    ctx.slidedp_block_norm(a, b, w[0], gate, w[1], a, b)
+    assert torch.equal(a, x2) and torch.equal(b, h)
+    ctx.slidedp_block_norm_backward(x, y, w[0], gate, w[1], gx, gh, dx, dy, dgate, None, None, None)
+    for places in ((0, 1, 2), (1, 2, 0), (3, 4, 1), (2, 3, 4), (4, 0, 3)):
+        ins = [t.clone() for t in (x, y, gate, gx, gh)]
+        p, q, r = (ins[i] for i in places)
+        ctx.slidedp_block_norm_backward(ins[0], ins[1], w[0], ins[2], w[1], ins[3], ins[4], p, q, r, None, None, None)
+        assert torch.equal(p, dx) and torch.equal(q, dy) and torch.equal(r, dgate)
+
+
 def test_block_norm_rows_do_not_touch_each_other(ctx):
     g = gen(6)
     T, H = 400, 512
