@@ -12,8 +12,8 @@
  * Calls of this header on one context may go to different streams and come from different threads, also at once (but not
  * beside other calls on that context); workspaces must not be shared by calls that can overlap.
  *
- * The attention, distillation, block-norm and policy-step kernels wait on copies and on blocks of their own launch; every such wait is bounded (about
- * a minute). If one runs out, the results of that call are not complete, and the first of these calls on the
+ * The attention, distillation, block-norm and policy-step kernels wait on copies and on blocks of their own launch; every
+ * such wait is bounded (about a minute). If one runs out, the results of that call are not complete, and the first of these calls on the
  * context to start after that returns SLIDEDP_ERR_TIMEOUT, once, and does nothing else: any operator of this header; a
  * slidedp_grad_norm_finish or slidedp_grad_norm_finish_from that fetches its results (they are fetched all the same); or
  * slidedp_destroy (which still destroys). A call's own kernels have only been queued when it returns: to know that a step's
@@ -277,8 +277,8 @@ SLIDEDP_API size_t slidedp_block_norm_workspace(const slidedp_block_norm_args* a
  * clipped range counts as inside. slidedp_policy_loss_backward takes the forward's logp;
  * slidedp_policy_step computes loss, logp and gradient in one call. d_logits may be the logits themselves (same address and
  * stride; the same address with another stride is refused) and may not overlap them otherwise. A kl_weight of 0 is no second
- * term, whatever ref_logp holds. Rows whose gradient is zero throughout (absent, clipped without a
- * second term, row_grad 0) are zeros whatever their logits hold; in others NaN and +inf among the logits make the row NaN.
+ * term, whatever ref_logp holds. Rows whose gradient is zero throughout (absent, clipped without a second term, row_grad 0)
+ * are zeros whatever their logits hold; in others NaN and +inf among the logits make the row NaN.
  */
 typedef struct {
   int64_t rows, vocab;
@@ -307,8 +307,9 @@ SLIDEDP_API int slidedp_policy_step(slidedp_ctx* ctx, const slidedp_policy_args*
  * slidedp_reduce_adamw_chunk takes (with max_norm 0 there). grads, outs: host arrays of `count` tensors each, read before the
  * call returns; outs[i] has grads[i].count elements of either type and may be grads[i] itself (same address and type); outs NULL:
  * only result is written. Tensors need the alignment of their element; they may be empty. A factor of 1 in place writes nothing.
- * With max_norm > 0 a NaN norm makes coef and with it every output NaN, an infinite one makes coef 0. The sums are FP64 in an order that the tensors' sizes and alignment decide. No tensor of
- * outs may overlap another one, or a tensor of grads other than its own.
+ * With max_norm > 0 a NaN norm makes coef and with it every output NaN, an infinite one makes coef 0. The sums are FP64 in an
+ * order that the tensors' sizes and alignment decide. No tensor of outs may overlap another one, or a tensor of grads other than
+ * its own.
  * workspace: device, slidedp_clip_grad_norm_workspace bytes, 16-byte aligned.
  */
 typedef struct {
