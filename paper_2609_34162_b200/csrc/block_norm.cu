@@ -321,8 +321,8 @@ __global__ void __launch_bounds__(kWideThreads) block_norm_backward_kernel(const
 // groups. Two values per instruction. What bounds a group is the chain of its two or three sums over the row (700 cycles each);
 // what a row needs is kept in registers from one sum to the next, which leaves room for two groups of 256 threads (three, with
 // 80 registers and values read again from shared memory, took 150 us backward where two take 87).
-// 8192 x 4096 BF16, both norms: forward 96 us with rows in registers and no copies ahead, 54 as blocks with a ring each, 51 now
-// (268 MB at 5.2 TB/s); backward 166, 95, 87.
+// 8192 x 4096 BF16, both norms: forward 96 us with rows in registers and no copies ahead, 54 as blocks with a ring each, 46 now
+// (268 MB at 5.8 TB/s); backward 166, 95, 87.
 
 __device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
 __device__ __forceinline__ float sum_of(uint64_t v) {
@@ -453,6 +453,16 @@ __device__ __forceinline__ float2 group_sums(float a, float b, float2 (*part)[kW
   return r;
 }
 
+// A thread's share of a row's sum of squares.
+template <typename T, bool kVector>
+__device__ __forceinline__ float sum_squares(const Columns<T, kVector>& cols, const char* row, int hidden) {
+  uint64_t v[kPairs], s = 0;
+  cols.load(row, hidden, v);
+#pragma unroll
+  for (int e = 0; e < kPairs; ++e) s = fma2(v[e], v[e], s);
+  return sum_of(s);
+}
+
 constexpr int kMaxNormStages = 4, kMaxGroups = 15;
 constexpr int kMaxNormInputs = 5;
 enum NormInput { kInX, kInY, kInGate, kInDx, kInDh };
@@ -534,15 +544,16 @@ struct NormRows {
     }
     ++issued;
   }
-  __device__ __forceinline__ void wait() {
-    ok &= Waiter{dead, p.error, p.polls}(smem_addr(&full[stage]), parity);
+  __device__ __forceinline__ void wait(bool following = false) {      // for the present row, or the one after it
+    const bool wraps = following && stage + 1 == p.feed.stages;
+    ok &= Waiter{dead, p.error, p.polls}(smem_addr(&full[wraps ? 0 : stage + following]), parity ^ (uint32_t)wraps);
     if (ok) ++ready;
   }
   __device__ __forceinline__ void next() {
     if (++stage == p.feed.stages) stage = 0, parity ^= 1;
   }
-  __device__ __forceinline__ const char* at(int input, int64_t row) const {
-    const char* to = slot(stage, input);
+  __device__ __forceinline__ const char* at(int input, int64_t row, bool following = false) const {
+    const char* to = slot(following && stage + 1 == p.feed.stages ? 0 : stage + following, input);
     if constexpr (!kVector) to += reinterpret_cast<uintptr_t>(p.feed.src[input] + row * p.feed.stride[input]) & 15u;
     return to;
   }
@@ -633,12 +644,20 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_ring_kernel(const __gr
   const bool leader = cols.t == 0;
   const bool has_y = kFull || p.has_y, norm_y = kFull || p.post, norm_x = kFull || p.pre;
   int turn = 0;
+  // A row's first sum is taken with the last one of the row before it, which makes the chain one sum shorter (8192 x 4096 BF16: 51.5
+  // -> 45.9 us) but gives the row's place back later: with a token's gate, which leaves fewer rows under way, 79.9 -> 87.5 us for 5120.
+  const bool ahead = !kToken && norm_y && norm_x && rp.feed.stages > 1;
+  const auto squares = [&](int64_t row, bool following) { return sum_squares(cols, rows.at(kInY, row, following), p.hidden); };
+  float r = 1.0f;
+  if (ahead && rows.count > 0) {
+    rows.wait();
+    r = rsqrtf(group_sums<kWarps>(squares(rows.first, false), 0.0f, part, turn, cols.t, n, group).x * p.inv_hidden + p.eps);
+  }
   for (int64_t i = 0; i < rows.count; ++i, rows.next()) {
     const int64_t row = rows.first + i * rows.step;
-    rows.wait();
+    if (!ahead) rows.wait();
     uint64_t x[kPairs], y[kPairs], f[kPairs];
     cols.load(rows.at(kInX, row), p.hidden, x);
-    float r = 1.0f;
     if (has_y) {
       cols.load(rows.at(kInY, row), p.hidden, y);
       cols.load_factors(post, f);
@@ -648,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_ring_kernel(const __gr
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) f[e] = mul2(f[e], p.sigmoid ? sigmoid2(g[e]) : g[e]);
       }
-      if (norm_y) {
+      if (norm_y && !ahead) {
         uint64_t s = 0;
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) s = fma2(y[e], y[e], s);
@@ -663,8 +682,15 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_ring_kernel(const __gr
       uint64_t s = 0;
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) s = fma2(x[e], x[e], s);
-      const float r2 = rsqrtf(group_sums<kWarps>(sum_of(s), 0.0f, part, turn, cols.t, n, group).x * p.inv_hidden + p.eps);
-      if (!norm_y && leader) rows.issue_next();
+      float next = 0.0f;
+      if (ahead && i + 1 < rows.count) {
+        rows.wait(true);
+        next = squares(row + rows.step, true);
+      }
+      const float2 both_sums = group_sums<kWarps>(sum_of(s), next, part, turn, cols.t, n, group);
+      const float r2 = rsqrtf(both_sums.x * p.inv_hidden + p.eps);
+      if (ahead) r = rsqrtf(both_sums.y * p.inv_hidden + p.eps);
+      if ((ahead || !norm_y) && leader) rows.issue_next();
       cols.load_factors(pre, f);
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) x[e] = mul2(mul2(f[e], both(r2)), x[e]);
@@ -697,11 +723,20 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_backward_ring_kernel(c
   constexpr bool kKeep = kVector && !kToken;
   uint64_t sum_post[kPairs] = {}, sum_pre[kPairs] = {};
   int turn = 0;
+  // A row's first sum with the last one of the row before, as forward, where there are registers for it: 8192 x 5120 BF16 132 -> 127 us, with
+  // a token's gate 214 -> 190, 4096 x 5120 FP32 85 -> 91; but 8192 x 4096 with its two groups 87 -> 96.
+  const bool ahead = kThreads < 512 && norm_y && rp.feed.stages > 1;
+  const auto squares = [&](int64_t row, bool following) { return sum_squares(cols, rows.at(kInY, row, following), p.hidden); };
+  float r = 1.0f;
+  if (ahead && rows.count > 0) {
+    rows.wait();
+    r = rsqrtf(group_sums<kWarps>(squares(rows.first, false), 0.0f, part, turn, cols.t, n, group).x * p.inv_hidden + p.eps);
+  }
   for (int64_t i = 0; i < rows.count; ++i, rows.next()) {
     const int64_t row = rows.first + i * rows.step;
-    rows.wait();
+    if (!ahead) rows.wait();
     uint64_t x[kPairs], y[kPairs], g[kPairs], h[kPairs], f[kPairs];     // y: times r
-    float r = 1.0f, r2 = 0.0f, m = 0.0f;
+    float r2 = 0.0f, m = 0.0f;
     const auto load_y = [&] {
       cols.load(rows.at(kInY, row), p.hidden, y);
 #pragma unroll
@@ -716,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_backward_ring_kernel(c
     };
     if (has_y) {
       cols.load(rows.at(kInY, row), p.hidden, y);
-      if (norm_y) {
+      if (norm_y && !ahead) {
         uint64_t s = 0;
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) s = fma2(y[e], y[e], s);
@@ -788,13 +823,20 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_backward_ring_kernel(c
       if (kToken && p.dgate.p) cols.store(static_cast<T*>(p.dgate.p) + row * p.dgate.stride, p.hidden, f);
     }
     if (norm_y) {
-      m = -group_sums<kWarps>(sum_of(dot), 0.0f, part, turn, cols.t, n, group).x * p.inv_hidden;
+      float next = 0.0f;
+      if (ahead && i + 1 < rows.count) {
+        rows.wait(true);
+        next = squares(row + rows.step, true);
+      }
+      const float2 both_sums = group_sums<kWarps>(sum_of(dot), next, part, turn, cols.t, n, group);
+      m = -both_sums.x * p.inv_hidden;
       if (!kKeep) {
         load_y();
         group_sync(group, n);
       }
 #pragma unroll
       for (int e = 0; e < kPairs; ++e) x[e] = mul2(both(r), fma2(y[e], both(m), x[e]));
+      if (ahead) r = rsqrtf(both_sums.y * p.inv_hidden + p.eps);
     } else {
       group_sync(group, n);
     }
