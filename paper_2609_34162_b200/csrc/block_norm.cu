@@ -317,12 +317,13 @@ __global__ void __launch_bounds__(kWideThreads) block_norm_backward_kernel(const
 // ---- rows in shared memory ---------------------------------------------------------------------------------
 // A block per SM, of several groups of warps that work on a row each. Rows are copied in bulk into each group's ring ahead of their use,
 // so that what is under way costs no registers. A thread has 16 columns of every row: 16-byte vectors where rows are aligned to
-// them, else single columns, neighbours with neighbouring threads. The factors of y r and of x' r' lie before the rings in FP32, for all
+// them, else pairs or single ones, neighbours with neighbouring threads (8192 x 4098 BF16, both norms, 89 and 248 us in pairs, 134 and 373
+// one by one; 8192 x 4097 110 and 359). The factors of y r and of x' r' lie before the rings in FP32, for all
 // groups. Two values per instruction. What bounds a group is the chain of its two or three sums over the row (700 cycles each);
 // what a row needs is kept in registers from one sum to the next, which leaves room for two groups of 256 threads (three, with
 // 80 registers and values read again from shared memory, took 150 us backward where two take 87).
-// 8192 x 4096 BF16, both norms: forward 96 us with rows in registers and no copies ahead, 54 as blocks with a ring each, 46 now
-// (268 MB at 5.8 TB/s); backward 166, 95, 87.
+// 8192 x 4096 BF16, both norms: forward 96 us with rows in registers and no copies ahead, 54 as blocks with a ring each, 47 now
+// (268 MB at 5.7 TB/s); backward 166, 95, 85.
 
 __device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
 __device__ __forceinline__ float sum_of(uint64_t v) {
@@ -339,20 +340,24 @@ __device__ __forceinline__ uint64_t sigmoid2(uint64_t v) {
 constexpr int kCols = 16;              // per thread
 constexpr int kPairs = kCols / 2;
 
-// A thread's columns: vectors `n` vectors apart, or single ones `n` apart, with n threads in the group. Columns behind the row are zeros: vectors have
-// zeros behind their rows in shared memory, for single columns it is asked.
-template <typename T, bool kVector>
+// A thread's columns: its warp's are behind one another, K times 32 vectors of V, of which each lane has one, so that their distances
+// are known when this is compiled (with the group's vectors behind one another they took 16 registers for single columns: 452 bytes spilled). Columns behind the row
+// are zeros: whole vectors have zeros behind their rows in shared memory, for shorter ones it is asked.
+template <typename T, int V_>
 struct Columns {
-  static constexpr int V = kVector ? 16 / (int)sizeof(T) : 1, K = kCols / V;
-  int t, n;
-  __device__ __forceinline__ int first(int k) const { return (k * n + t) * V; }
+  static constexpr int V = V_, K = kCols / V, kStep = 32 * V;
+  static constexpr bool kVector = V * sizeof(T) == 16;
+  int t, n;          // thread of the group, and how many it has
+  __device__ __forceinline__ int first() const { return t / 32 * (32 * kCols) + t % 32 * V; }
   __device__ __forceinline__ void load(const char* row, int hidden, uint64_t* v) const {
+    const char* at = row + first() * sizeof(T);
+    const int left = hidden - first();
     float one[2];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = first(k);
+      const char* p = at + k * kStep * sizeof(T);
       if constexpr (kVector) {
-        const uint4 a = *reinterpret_cast<const uint4*>(row + c * sizeof(T));
+        const uint4 a = *reinterpret_cast<const uint4*>(p);
         const uint32_t w[4] = {a.x, a.y, a.z, a.w};
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -361,63 +366,73 @@ struct Columns {
 #pragma unroll
           for (int e = 0; e < 2; ++e) v[k * 2 + e] = pair(__uint_as_float(w[2 * e]), __uint_as_float(w[2 * e + 1]));
         }
+      } else if constexpr (V == 2) {
+        const uint32_t a = k * kStep < left ? *reinterpret_cast<const uint32_t*>(p) : 0;
+        v[k] = pair(bf16_lo(a), bf16_hi(a));
       } else {
         one[k % 2] = 0.0f;
-        if (c < hidden) {
-          if constexpr (sizeof(T) == 2) one[k % 2] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[c] << 16);
-          else one[k % 2] = reinterpret_cast<const float*>(row)[c];
+        if (k * kStep < left) {
+          if constexpr (sizeof(T) == 2) one[k % 2] = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
+          else one[k % 2] = *reinterpret_cast<const float*>(p);
         }
         if (k % 2) v[k / 2] = pair(one[0], one[1]);
       }
     }
   }
-  // Factors lie as threads read them: the fours of a thread's values `n` fours apart (behind one another in a thread's own order,
+  // Factors lie as threads read them: the fours of a thread's values 32 fours apart (behind one another in a thread's own order,
   // vectors of eight would meet in the same banks: 94.7 -> 87.5 us backward).
-  __device__ __forceinline__ int place(int value) const { return (value / 4 * n + t) * 4 + value % 4; }
+  __device__ __forceinline__ int place() const { return t / 32 * (32 * kCols) + t % 32 * 4; }
   __device__ __forceinline__ void load_factors(const float* w, uint64_t* v) const {
+    const float* at = w + place();
 #pragma unroll
     for (int j = 0; j < kCols / 4; ++j) {
-      const float4 a = *reinterpret_cast<const float4*>(w + place(4 * j));
+      const float4 a = *reinterpret_cast<const float4*>(at + j * 128);
       v[2 * j] = pair(a.x, a.y);
       v[2 * j + 1] = pair(a.z, a.w);
     }
   }
   __device__ __forceinline__ void store_factors(float* w, const uint64_t* v) const {
+    float* at = w + place();
 #pragma unroll
     for (int j = 0; j < kCols / 4; ++j) {
       float4 a;
       split(v[2 * j], &a.x, &a.y);
       split(v[2 * j + 1], &a.z, &a.w);
-      *reinterpret_cast<float4*>(w + place(4 * j)) = a;
+      *reinterpret_cast<float4*>(at + j * 128) = a;
     }
   }
-  __device__ __forceinline__ void store(T* row, int hidden, const uint64_t* v) const {
+  // Vector number k.
+  __device__ __forceinline__ void get(const uint64_t* v, int k, float* f) const {
+    if constexpr (V > 1) {
+#pragma unroll
+      for (int e = 0; e < V / 2; ++e) split(v[k * V / 2 + e], &f[2 * e], &f[2 * e + 1]);
+    } else {
+      float lo, hi;
+      split(v[k / 2], &lo, &hi);
+      f[0] = k % 2 ? hi : lo;
+    }
+  }
+  template <typename O>
+  __device__ __forceinline__ void store(O* row, int hidden, const uint64_t* v) const {
+    O* at = row + first();
+    const int left = hidden - first();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = first(k);
       float f[V];
-      if constexpr (kVector) {
-#pragma unroll
-        for (int e = 0; e < V / 2; ++e) split(v[k * V / 2 + e], &f[2 * e], &f[2 * e + 1]);
-      } else {
-        float lo, hi;
-        split(v[k / 2], &lo, &hi);
-        f[0] = k % 2 ? hi : lo;
-      }
-      if (c < hidden) store_values<V>(row + c, f);
+      get(v, k, f);
+      if (k * kStep < left) store_values<V>(at + k * kStep, f);
     }
   }
   __device__ __forceinline__ void store_f32(float* row, int hidden, const uint64_t* v) const {
+    float* at = row + first();
+    const int left = hidden - first();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = first(k);
-      if (c >= hidden) continue;
+      float f[V];
+      get(v, k, f);
+      if (k * kStep >= left) continue;
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        float lo, hi;
-        split(v[(k * V + e) / 2], &lo, &hi);
-        row[c + e] = (k * V + e) % 2 ? hi : lo;
-      }
+      for (int e = 0; e < V; ++e) at[k * kStep + e] = f[e];
     }
   }
 };
@@ -454,8 +469,8 @@ __device__ __forceinline__ float2 group_sums(float a, float b, float2 (*part)[kW
 }
 
 // A thread's share of a row's sum of squares.
-template <typename T, bool kVector>
-__device__ __forceinline__ float sum_squares(const Columns<T, kVector>& cols, const char* row, int hidden) {
+template <typename T, int V>
+__device__ __forceinline__ float sum_squares(const Columns<T, V>& cols, const char* row, int hidden) {
   uint64_t v[kPairs], s = 0;
   cols.load(row, hidden, v);
 #pragma unroll
@@ -570,8 +585,8 @@ struct NormRows {
 };
 
 // The columns of a weight in global memory; ones without it.
-template <typename T, bool kVector>
-__device__ __forceinline__ void load_weight(const Columns<T, kVector>& cols, const void* w, int hidden, uint64_t* v) {
+template <typename T, int V>
+__device__ __forceinline__ void load_weight(const Columns<T, V>& cols, const void* w, int hidden, uint64_t* v) {
   if (!w) {
 #pragma unroll
     for (int e = 0; e < kPairs; ++e) v[e] = both(1.0f);
@@ -579,13 +594,12 @@ __device__ __forceinline__ void load_weight(const Columns<T, kVector>& cols, con
   }
 #pragma unroll
   for (int k = 0; k < cols.K; ++k) {
-    const int c = cols.first(k);
-    float f[cols.V + 1] = {};
+    const int c = cols.first() + k * cols.kStep;
+    float f[V + 1] = {};
     if (c < hidden) {
-      if constexpr (kVector) to_floats<T, cols.V>(*reinterpret_cast<const uint4*>(static_cast<const T*>(w) + c), f);
-      else load_values<1>(static_cast<const T*>(w) + c, f);
+      to_floats<T, V>(*reinterpret_cast<const typename Raw<T, V>::type*>(static_cast<const T*>(w) + c), f);
     }
-    if constexpr (kVector) {
+    if constexpr (V > 1) {
 #pragma unroll
       for (int e = 0; e < cols.V; e += 2) v[(k * cols.V + e) / 2] = pair(f[e], f[e + 1]);
     } else {
@@ -596,8 +610,8 @@ __device__ __forceinline__ void load_weight(const Columns<T, kVector>& cols, con
   }
 }
 // The start that both kernels share: barriers, the first rows, the factors a g w_post (without a token's g) and w_pre, by the first group.
-template <typename T, bool kVector, bool kToken, int kWarps>
-__device__ __forceinline__ void start_rings(const BlockNormParams& p, const Columns<T, kVector>& cols, NormRows<kVector>& rows, NormRings& rings,
+template <typename T, int V, bool kToken, int kWarps>
+__device__ __forceinline__ void start_rings(const BlockNormParams& p, const Columns<T, V>& cols, NormRows<Columns<T, V>::kVector>& rows, NormRings& rings,
                                             float2 (*part)[kWarps], float* post, float* pre, int group) {
   if (cols.t == 0) {
     for (int s = 0; s < kMaxNormStages; ++s) mbar_init(smem_addr(&rows.full[s]), 1);
@@ -626,9 +640,11 @@ __device__ __forceinline__ void start_rings(const BlockNormParams& p, const Colu
   __syncthreads();
 }
 
-// kToken: the gate is each token's. kFull: there are a block's output, both norms and, backward, both gradients; known when it is
-// compiled, which leaves out the moves of values between branches (8192 x 4096, forward and backward: 53.6 + 108.5 us -> 51.6 + 94.7).
-template <typename T, bool kVector, bool kToken, bool kFull, int kThreads, int kWarps>
+// kToken: the gate is each token's. kForm: 1, there are a block's output, both norms and, backward, both gradients; 2, the same without the
+// norm of the block's output; 0, anything. Known when it is compiled, they leave out the moves of values between branches (8192 x 4096,
+// forward and backward: the first 53.6 + 108.5 us -> 51.6 + 94.7, the second backward 82 -> 77,
+// with a token's gate 135 -> 95).
+template <typename T, int V, bool kToken, int kForm, int kThreads, int kWarps>
 __global__ void __launch_bounds__(kThreads, 1) block_norm_ring_kernel(const __grid_constant__ NormRingParams rp) {
   extern __shared__ uint4 dynamic[];
   __shared__ NormRings rings;
@@ -636,13 +652,14 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_ring_kernel(const __gr
   allow_next_kernel();
   const BlockNormParams& p = rp.n;
   const int n = rp.feed.group_threads, group = threadIdx.x / n;
-  const Columns<T, kVector> cols = {(int)threadIdx.x - group * n, n};
+  constexpr bool kVector = Columns<T, V>::kVector;
+  const Columns<T, V> cols = {(int)threadIdx.x - group * n, n};
   float *post = reinterpret_cast<float*>(dynamic), *pre = post + n * kCols;
   float2(*part)[kWarps] = parts[group];
   NormRows<kVector> rows(rp, rings, post, group);
-  start_rings<T, kVector, kToken>(p, cols, rows, rings, part, post, pre, group);
+  start_rings<T, V, kToken>(p, cols, rows, rings, part, post, pre, group);
   const bool leader = cols.t == 0;
-  const bool has_y = kFull || p.has_y, norm_y = kFull || p.post, norm_x = kFull || p.pre;
+  const bool has_y = kForm != 0 || p.has_y, norm_y = kForm == 1 || (kForm == 0 && p.post), norm_x = kForm != 0 || p.pre;
   int turn = 0;
   // A row's first sum is taken with the last one of the row before it, which makes the chain one sum shorter (8192 x 4096 BF16: 51.5
   // -> 45.9 us) but gives the row's place back later: with a token's gate, which leaves fewer rows under way, 79.9 -> 87.5 us for 5120.
@@ -703,7 +720,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_ring_kernel(const __gr
   if (leader) rows.finish();
 }
 
-template <typename T, bool kVector, bool kToken, bool kFull, int kThreads, int kWarps>
+template <typename T, int V, bool kToken, int kForm, int kThreads, int kWarps>
 __global__ void __launch_bounds__(kThreads, 1) block_norm_backward_ring_kernel(const __grid_constant__ NormRingParams rp) {
   extern __shared__ uint4 dynamic[];
   __shared__ NormRings rings;
@@ -711,13 +728,14 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_backward_ring_kernel(c
   allow_next_kernel();
   const BlockNormParams& p = rp.n;
   const int n = rp.feed.group_threads, group = threadIdx.x / n;
-  const Columns<T, kVector> cols = {(int)threadIdx.x - group * n, n};
+  constexpr bool kVector = Columns<T, V>::kVector;
+  const Columns<T, V> cols = {(int)threadIdx.x - group * n, n};
   float *post = reinterpret_cast<float*>(dynamic), *pre = post + n * kCols;
   float2(*part)[kWarps] = parts[group];
   NormRows<kVector> rows(rp, rings, post, group);
-  start_rings<T, kVector, kToken>(p, cols, rows, rings, part, post, pre, group);
+  start_rings<T, V, kToken>(p, cols, rows, rings, part, post, pre, group);
   const bool leader = cols.t == 0;
-  const bool has_y = kFull || p.has_y, norm_y = kFull || p.post, norm_x = kFull || p.pre;
+  const bool has_y = kForm != 0 || p.has_y, norm_y = kForm == 1 || (kForm == 0 && p.post), norm_x = kForm != 0 || p.pre;
   // Whether a row stays in registers from one sum to the next, as far as there are any: a token's gate is 32 more, single columns take
   // more to address. Their rows are read again (8192 x 4096 BF16 with such a gate: 158 -> 124 us).
   constexpr bool kKeep = kVector && !kToken;
@@ -785,7 +803,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_backward_ring_kernel(c
       m = -s.y * r2 * p.inv_hidden;
     }
     uint64_t d[kPairs] = {};
-    if (kFull || p.dx_out.p) cols.load(rows.at(kInDx, row), p.hidden, d);
+    if (kForm != 0 || p.dx_out.p) cols.load(rows.at(kInDx, row), p.hidden, d);
     if (norm_x) {
       cols.load_factors(pre, f);
       if (!kKeep) cols.load(rows.at(kInDh, row), p.hidden, h);
@@ -1020,9 +1038,9 @@ NormRingParams ring_params(slidedp_ctx* ctx, const slidedp_block_norm_args* a, c
   r.polls = ctx->wait_polls;
   return r;
 }
-// run(T, vector, token, full, threads, warps of a group) as template arguments.
+// run(T, V, token, form, threads, warps of a group) as template arguments.
 template <bool kBackward, typename F>
-void pick_ring_kernel(const slidedp_block_norm_args* a, const RingPlan& plan, bool full, F run) {
+void pick_ring_kernel(const slidedp_block_norm_args* a, const RingPlan& plan, int v, int form, F run) {
   typedef std::true_type Yes;
   typedef std::false_type No;
   const auto threads = [&](auto type, auto vector, auto token, auto whole) {
@@ -1032,8 +1050,14 @@ void pick_ring_kernel(const slidedp_block_norm_args* a, const RingPlan& plan, bo
     run(type, vector, token, whole, Usual(), std::integral_constant<int, 16>());
   };
   const auto forms = [&](auto type, auto token) {
-    if (!plan.vector) return threads(type, No(), token, No());
-    full ? threads(type, Yes(), token, Yes()) : threads(type, Yes(), token, No());
+    typedef std::integral_constant<int, 1> One;
+    typedef std::integral_constant<int, 16 / (int)sizeof(type)> Whole;
+    typedef std::integral_constant<int, 0> Any;
+    typedef std::integral_constant<int, 2> Two;
+    if (plan.vector) return form == 1 ? threads(type, Whole(), token, One()) : form == 2 ? threads(type, Whole(), token, Two()) : threads(type, Whole(), token, Any());
+    if constexpr (sizeof(type) == 2)
+      if (v == 2) return threads(type, Two(), token, Any());
+    threads(type, One(), token, Any());
   };
   const auto gates = [&](auto type) { a->gate_kind == 2 ? forms(type, Yes()) : forms(type, No()); };
   a->dtype == SLIDEDP_BF16 ? gates(uint16_t()) : gates(float());
@@ -1080,13 +1104,13 @@ int slidedp_block_norm(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const
   FAULT_POINT();
   if (plan.use) {
     const NormRingParams r = ring_params(ctx, a, p, plan);
-    pick_ring_kernel<false>(a, plan, y && a->post_norm && a->pre_norm, [&](auto type, auto vector, auto token, auto full, auto threads, auto warps) {
+    pick_ring_kernel<false>(a, plan, v, y && a->pre_norm ? (a->post_norm ? 1 : 2) : 0, [&](auto type, auto vector, auto token, auto form, auto threads, auto warps) {
       typedef decltype(type) T_;
       const auto run = [&](auto kernel) {
         attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem);
         if (attribute == cudaSuccess) launch_after(kernel, dim3(blocks), plan.threads * plan.groups, plan.smem, 1, st, r);
       };
-      run(block_norm_ring_kernel<T_, vector, token, full, threads, warps>);
+      run(block_norm_ring_kernel<T_, vector, token, form, threads, warps>);
     });
   } else {
     pick_wide_kernel(a, v, [&](auto type, auto vec) {
@@ -1167,13 +1191,13 @@ int slidedp_block_norm_backward(slidedp_ctx* ctx, const slidedp_block_norm_args*
     FAULT_POINT();
     if (plan.use) {
       const NormRingParams r = ring_params(ctx, a, p, plan);
-      pick_ring_kernel<true>(a, plan, y && a->post_norm && a->pre_norm && dx_out, [&](auto type, auto vector, auto token, auto full, auto threads, auto warps) {
+      pick_ring_kernel<true>(a, plan, v, y && a->pre_norm && dx_out ? (a->post_norm ? 1 : 2) : 0, [&](auto type, auto vector, auto token, auto form, auto threads, auto warps) {
         typedef decltype(type) T_;
         const auto run = [&](auto kernel) {
           attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem);
           if (attribute == cudaSuccess) launch_after(kernel, dim3(blocks), plan.threads * plan.groups, plan.smem, 1, st, r);
         };
-        run(block_norm_backward_ring_kernel<T_, vector, token, full, threads, warps>);
+        run(block_norm_backward_ring_kernel<T_, vector, token, form, threads, warps>);
       });
     } else {
       pick_wide_kernel(a, v, [&](auto type, auto vec) {
