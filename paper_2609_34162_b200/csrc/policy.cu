@@ -287,6 +287,9 @@ __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __g
     }
     return;
   }
+  // forward, a block's sums go to the first block's shared memory: that block must have started, which is asked for here and waited
+  // for where they are ready
+  if (!kGradient && cluster > 1) cluster_arrive();
   const float at = Logit<T>::load(z + label), k = p.inv_tau * kLog2e;
   constexpr int U = kPolicyUnroll;
   if constexpr (kGradient) {
@@ -321,6 +324,7 @@ __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __g
     __syncthreads();
     mine = join_sums<kPolicyWarps>(sh.warp[threadIdx.x % kPolicyWarps], k);
     if (cluster > 1) {
+      cluster_wait();
       if (threadIdx.x == 0) {
         const uint32_t there = peer_addr(smem_addr(&sh.part[rank]), 0);
         asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(mine.m), "f"(mine.s) : "memory");
