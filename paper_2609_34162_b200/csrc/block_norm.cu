@@ -904,6 +904,12 @@ __global__ void __launch_bounds__(32 * kNormSumParts) block_norm_sum_kernel(cons
   __syncthreads();
   if (slice > 0 || col >= p.hidden) return;
   for (int i = 1; i < kNormSumParts; ++i) s += part[i][lane];
+  if (blocks == 0) {                  // no tokens: zeros, whatever the weight and the gate hold
+    if (which == 1 && p.dw_pre) p.dw_pre[col] = 0.0f;
+    if (which == 0 && p.dw_post) p.dw_post[col] = 0.0f;
+    if (which == 0 && p.dgate_sum) p.dgate_sum[col] = 0.0f;
+    return;
+  }
   if (which == 1) {
     if (p.dw_pre) p.dw_pre[col] = s;
     return;
@@ -1156,7 +1162,7 @@ int slidedp_block_norm_backward(slidedp_ctx* ctx, const slidedp_block_norm_args*
                  (dx_out && !rows_ok(dx_out, elem, T, H, false)) || !rows_ok(dx, elem, T, H, true) || (dgate && !rows_ok(dgate, elem, T, H, true)) ||
                  !places_ok({dx, dy, dgate}, {x, y, a->gate_kind == 2 ? gate : nullptr, dx_out, dh_out}, T))) ||
       !weight_ok(w_post, elem) || !weight_ok(w_pre, elem) || !weight_ok(dw_post, 4) || !weight_ok(dw_pre, 4) || !weight_ok(dgate_sum, 4) ||
-      (sums && !workspace))
+      (sums && (!workspace || (a->gate_kind == 1 && !rows_ok(gate, elem, 1, H, false)))))
     return SLIDEDP_ERR_INVALID_ARG;
   if (sums && !aligned16(workspace)) return SLIDEDP_ERR_MISALIGNED;
   if (T == 0 && !sums) return SLIDEDP_OK;

@@ -1,4 +1,6 @@
 """Block norms and policy loss where their kernels change over, exchange between blocks or are called side by side."""
+import math
+
 import pytest
 import torch
 
@@ -25,3 +27,16 @@ def test_policy_forward_of_rows_that_blocks_share(ctx, dtype, N, V):
         lp = torch.full((N,), 9.0, device="cuda")
         ctx.slidedp_policy_loss(a["z"], a["labels"], None, None, None, None, lp)
         assert_close("logp", lp, want, 5e-6 + 2.0 ** -22 * want.abs())
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_block_norm_sums_without_tokens_are_zeros_whatever_the_gate_holds(ctx, dtype, sigmoid):
+    H = 70
+    x = torch.empty(0, H, dtype=dtype, device="cuda")
+    ws = torch.empty(ctx.slidedp_block_norm_workspace(x), dtype=torch.uint8, device="cuda")
+    for bad in (math.inf, math.nan):
+        w, gate = torch.full((H,), bad, dtype=dtype, device="cuda"), torch.full((H,), bad, dtype=dtype, device="cuda")
+        sums = [torch.full((H,), 5.0, device="cuda") for _ in range(3)]
+        ctx.slidedp_block_norm_backward(x, x, w, gate, w, x, x, x, x, *sums, ws, gate_sigmoid=sigmoid)
+        assert not any(s.any() for s in sums)
