@@ -1003,7 +1003,9 @@ struct RingPlan {
   size_t smem, slot;
 };
 constexpr int ring_class(bool backward, int group) { return group > 256 && group <= 320 ? (backward ? 320 : 640) : 512; }
-constexpr int kNormSmem = 222 * 1024;      // of an SM's 227 KB, less what a block has besides
+// Of an SM's 227 KB, less what a block has besides. Kernels are allowed all of it: the limit belongs to the kernel, which calls with
+// other plans launch from other threads at the same time.
+constexpr int kNormSmem = 222 * 1024;
 
 RingPlan ring_plan(const slidedp_block_norm_args* a, bool vector, int inputs, bool backward) {
   RingPlan r = {};
@@ -1113,7 +1115,7 @@ int slidedp_block_norm(slidedp_ctx* ctx, const slidedp_block_norm_args* a, const
     pick_ring_kernel<false>(a, plan, v, y && a->pre_norm ? (a->post_norm ? 1 : 2) : 0, [&](auto type, auto vector, auto token, auto form, auto threads, auto warps) {
       typedef decltype(type) T_;
       const auto run = [&](auto kernel) {
-        attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem);
+        attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormSmem);
         if (attribute == cudaSuccess) launch_after(kernel, dim3(blocks), plan.threads * plan.groups, plan.smem, 1, st, r);
       };
       run(block_norm_ring_kernel<T_, vector, token, form, threads, warps>);
@@ -1200,7 +1202,7 @@ int slidedp_block_norm_backward(slidedp_ctx* ctx, const slidedp_block_norm_args*
       pick_ring_kernel<true>(a, plan, v, y && a->pre_norm && dx_out ? (a->post_norm ? 1 : 2) : 0, [&](auto type, auto vector, auto token, auto form, auto threads, auto warps) {
         typedef decltype(type) T_;
         const auto run = [&](auto kernel) {
-          attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem);
+          attribute = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormSmem);
           if (attribute == cudaSuccess) launch_after(kernel, dim3(blocks), plan.threads * plan.groups, plan.smem, 1, st, r);
         };
         run(block_norm_backward_ring_kernel<T_, vector, token, form, threads, warps>);
