@@ -55,6 +55,7 @@ struct slidedp_ctx {
   bool norm_issued = false;
   int* kernel_error = nullptr;      // pinned: set by a kernel whose bounded wait ran out
   std::atomic<uint32_t> wait_polls{slidedp::kWaitPolls};   // bound of those waits (slidedp_test_wait_polls)
+  std::atomic<int> policy_clusters[2][9] = {};   // clusters of each size that run at once (policy.cu), by type; 0: not asked yet
   cudaEvent_t scalar_event = nullptr;
   // host-resident streaming
   cudaStream_t s_in = nullptr, s_compute = nullptr, s_out = nullptr;

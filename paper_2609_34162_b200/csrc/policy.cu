@@ -677,11 +677,13 @@ constexpr int64_t kEnoughBlocks = kSms * 4, kRound = kSms * 5;
 
 enum PolicyMode { kPolicyForward, kPolicyBackward, kPolicyStep };
 
-// How many clusters of the ring's kernel run at once: blocks that stay must all be of the first round. Asked once per type and size.
+// How many clusters of the ring's kernel run at once: blocks that stay must all be of the first round. Asked once per context, that is
+// device, type and size.
 template <typename K>
-cudaError_t resident_clusters(K kernel, bool f32, int cluster, size_t smem, int* out) {
-  static std::atomic<int> known[2][kPolicyMaxCluster + 1];
-  *out = known[f32][cluster];
+cudaError_t resident_clusters(slidedp_ctx* ctx, K kernel, bool f32, int cluster, size_t smem, int* out) {
+  static_assert(sizeof(ctx->policy_clusters[0]) / sizeof(ctx->policy_clusters[0][0]) > kPolicyMaxCluster, "a place for each size");
+  std::atomic<int>& known = ctx->policy_clusters[f32][cluster];
+  *out = known;
   if (*out > 0) return cudaSuccess;
   if (cluster == 1) {
     *out = kSms;
@@ -701,7 +703,7 @@ cudaError_t resident_clusters(K kernel, bool f32, int cluster, size_t smem, int*
     if (*out < 1) return cudaErrorLaunchOutOfResources;
     if (*out > kSms / cluster) *out = kSms / cluster;
   }
-  known[f32][cluster] = *out;
+  known = *out;
   return cudaSuccess;
 }
 
@@ -784,7 +786,7 @@ int run_policy(slidedp_ctx* ctx, const slidedp_policy_args* a, PolicyMode mode, 
     const auto run = [&](auto kernel) {
       failed = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
       int most = 0;
-      if (failed == cudaSuccess) failed = resident_clusters(kernel, f32, cluster, smem, &most);
+      if (failed == cudaSuccess) failed = resident_clusters(ctx, kernel, f32, cluster, smem, &most);
       const int64_t clusters = a->rows < most ? a->rows : most;
       if (failed == cudaSuccess) launch_after(kernel, dim3((unsigned)(clusters * cluster)), kRingThreads, smem, cluster, stream, p, cluster);
     };

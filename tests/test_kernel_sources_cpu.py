@@ -30,6 +30,8 @@ def functions(text, kind):
         at = m.end()
         while True:
             name = re.compile(r"(\w+)\s*\(").search(text, at)
+            if not name:
+                return
             end = closing(text, name.end() - 1, "()")
             if name.group(1) not in ("__launch_bounds__", "alignas"):
                 break
@@ -74,3 +76,12 @@ def test_no_block_is_written_to_before_its_cluster_has_met(name):
         barriers = [m.start() for m in re.finditer(r"\bcluster_(?:sync|wait)\(\)", body)]
         for m in access.finditer(body):
             assert any(b < m.start() and comes_before(body, b, m.start()) for b in barriers), (kernel, body[m.start() - 60:m.end() + 60])
+
+
+@pytest.mark.parametrize("name", [f for f in SOURCES if f.endswith(".cu")])
+def test_what_a_device_answers_is_not_kept_for_another(name):
+    """A function that asks the device how much of something fits keeps the answer with its context, not in a static of its own."""
+    for kind in ("cudaError_t", "int", "void", "bool"):
+        for function, body in functions(source(name), r"\b" + kind):
+            if re.search(r"\bcuda(Occupancy|DeviceGetAttribute|GetDeviceProperties)", body):
+                assert not re.search(r"\bstatic\b(?!\s+(?:constexpr|_assert))(?!_assert)", body), function
