@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from test_more_operators_gpu import BF16, F32, F64, assert_close, ctx, gen, policy_inputs, randn, sd  # noqa: F401
+from test_more_operators_gpu import BF16, F32, F64, assert_close, ctx, gen, policy_case, policy_inputs, randn, sd  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +40,27 @@ def test_block_norm_sums_without_tokens_are_zeros_whatever_the_gate_holds(ctx, d
         sums = [torch.full((H,), 5.0, device="cuda") for _ in range(3)]
         ctx.slidedp_block_norm_backward(x, x, w, gate, w, x, x, x, x, *sums, ws, gate_sigmoid=sigmoid)
         assert not any(s.any() for s in sums)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", [(0, 0), (1, 1)])
+def test_policy_rows_that_fill_a_block_of_512_threads(ctx, dtype, layout):
+    """Six and eight chunks for each thread of a block that holds a row: rows that just fit, with and without the chunk more that rows off the
+    16-byte grid touch, and rows one value and one chunk longer."""
+    per = 16 // dtype.itemsize
+    for most in (6 * 512, 8 * 512):
+        for V in ((most - 1) * per, most * per - 1, most * per, most * per + 1, (most + 1) * per):
+            policy_case(ctx, policy_inputs(3, V, dtype, seed=V, absent=0.0), layout=layout)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("more,layout", [(0, (0, 0)), (16, (0, 0)), (16, (3, 1)), (12345, (2, 2))])
+def test_policy_rows_at_and_beyond_what_a_cluster_holds(ctx, dtype, more, layout):
+    """The longest rows that are read once (1.1 MB, in eight blocks' shared memory), and longer ones: a step is then two launches, the second of
+    which takes the first one's log-probabilities."""
+    V = 8 * 8704 * 16 // dtype.itemsize + more
+    a = policy_inputs(5, V, dtype, seed=more, absent=0.0)
+    a["labels"][2] = -100                                     # absent
+    a["adv"][3], a["old"][3] = 1.0, a["old"][3] - 3.0         # outside the clipped range: no gradient of the first term
+    policy_case(ctx, a, layout=layout)
+    policy_case(ctx, {**a, "ref": None}, layout=layout)
