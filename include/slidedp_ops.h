@@ -278,7 +278,9 @@ SLIDEDP_API size_t slidedp_block_norm_workspace(const slidedp_block_norm_args* a
  * slidedp_policy_step computes loss, logp and gradient in one call. d_logits may be the logits themselves (same address and
  * stride; the same address with another stride is refused) and may not overlap them otherwise. A kl_weight of 0 is no second
  * term, whatever ref_logp holds. Rows whose gradient is zero throughout (absent, clipped without a second term, row_grad 0)
- * are zeros whatever their logits hold; in others NaN and +inf among the logits make the row NaN.
+ * are zeros whatever their logits hold; in others NaN and +inf among the logits make the row NaN. A row's exponentials are added in
+ * FP32, the label's own apart from the others', so that log-probability and gradient keep their digits where the label has all but little
+ * of the probability: off by a few FP32 roundings of the sum, and of the exponents, that is of the logits' distances.
  */
 typedef struct {
   int64_t rows, vocab;

@@ -59,15 +59,16 @@ struct Row {
   __device__ Row(const T* z_, int64_t vocab_) : z(z_), vocab(vocab_) {
     head = (int)((reinterpret_cast<uintptr_t>(z_) & 15u) / sizeof(T));
   }
-  __device__ int64_t first(int64_t c) const { return c * Logit<T>::kPer - head; }
-  __device__ bool whole(int64_t c) const { return first(c) >= 0 && first(c) + Logit<T>::kPer <= vocab; }
-  __device__ uint4 load(int64_t c) const {
-    const int64_t f = first(c);
-    if (f >= 0 && f + Logit<T>::kPer <= vocab) return ld_stream(z + f);
+  // I: int where all chunks' values are below 2^31, else int64_t
+  template <typename I> __device__ I first(I c) const { return c * (I)Logit<T>::kPer - (I)head; }
+  template <typename I> __device__ bool whole(I c) const { return first(c) >= 0 && first(c) + (I)Logit<T>::kPer <= (I)vocab; }
+  template <typename I> __device__ uint4 load(I c) const {
+    const I f = first(c);
+    if (f >= 0 && f + (I)Logit<T>::kPer <= (I)vocab) return ld_stream(z + f);
     union { uint4 v; T e[Logit<T>::kPer]; } u;
     u.v = Logit<T>::lowest();     // -inf where there is no value
     for (int i = 0; i < Logit<T>::kPer; ++i)
-      if (f + i >= 0 && f + i < vocab) u.e[i] = z[f + i];
+      if (f + i >= 0 && f + i < (I)vocab) u.e[i] = z[f + i];
     return u.v;
   }
 };

@@ -1,8 +1,10 @@
 // libslidedp: the clipped policy loss with a second term towards a reference model. See include/slidedp_ops.h for the contract.
 //
-// With c = 1 / temperature, m = max z, s = sum exp(c (z - m)): logp = c (z_y - m) - log s, rho = exp(logp - old), k = ref - logp,
+// With c = 1 / temperature, m the greatest logit but the label's, s = sum exp(c (z - m)) over all but the label's and o = exp(c (z_y - m)):
+// logp = -log(1 + s / o), 1 - p_y = s / (s + o), p = exp(c (z - m)) / (s + o) elsewhere, rho = exp(logp - old), k = ref - logp,
 //   loss = -min(rho A, clamp(rho, 1 - lo, 1 + hi) A) + w (e^k - k - 1),   l = -A rho [inside] + w (1 - e^k)
 //   dz = g c l (onehot - p)
+// The label's own term stays out of the sum, so that a token which is all but certain keeps the digits of what it lacks of one.
 // Bound: HBM. The logits are all that is large: a step reads them once and writes the gradient once, forward and backward apart read
 // them twice. Rows are held where they are read: in registers up to 64 KB, in shared memory up to 1.1 MB.
 #include "ops_internal.h"
@@ -121,6 +123,34 @@ __device__ __forceinline__ void add_chunks(PolicySum& mine, const uint4* a, floa
   mine.s += x + y;
 }
 
+// One value as a sum.
+__device__ __forceinline__ PolicySum one_value(float v, float k) {
+  const float m = fmaxf(v, -INFINITY), c = shift_of(m, k);     // NaN shows in the sum
+  return PolicySum{m, exp2_approx(is_far(c) ? (v - m) * k : fmaf(v, k, -c))};
+}
+// A chunk without its value number e.
+template <typename T>
+__device__ __forceinline__ uint4 without(uint4 a, int e) {
+  uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      if (e == 2 * i) w[i] = (w[i] & 0xffff0000u) | 0xff80u;
+      if (e == 2 * i + 1) w[i] = (w[i] & 0xffffu) | 0xff800000u;
+    } else {
+      if (e == i) w[i] = 0xff800000u;
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// N chunks `step` apart from c on, of which number `hot` has the label as its value number e: without it.
+template <typename T, int N>
+__device__ __forceinline__ void leave_out(uint4* a, int c, int step, int hot, int e) {
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+    if (c + u * step == hot) a[u] = without<T>(a[u], e);
+}
+
 // What a row's gradient f (onehot - p) needs: p = exp2(k z - shift) * scale, or far from zero exp2(k (z - shift) + offset) * scale; `factor`
 // is -f scale. A gradient that is zero throughout is told by f.
 struct RowTerms {
@@ -131,7 +161,7 @@ struct RowTerms {
 struct PolicyGrad {
   float k;
   RowTerms t;
-  int label;
+  int hot, place;      // the label is value number `place` of chunk `hot`
 };
 template <typename T>
 __device__ __forceinline__ void policy_values(uint4 a, const PolicyGrad& g, float* out) {
@@ -153,27 +183,32 @@ __device__ __forceinline__ void policy_values_far(uint4 a, float k, const RowTer
 }
 // The label is the chunk's value number `at`, if that is one of them.
 template <typename T>
-__device__ __forceinline__ void put_label(float* out, int64_t at, float v) {
+__device__ __forceinline__ void put_label(float* out, int at, float v) {
 #pragma unroll
   for (int e = 0; e < Logit<T>::kPer; ++e) out[e] = at == e ? v : out[e];
 }
 // Value by value: partial chunks, and rows whose gradient lies on another address grid.
-template <typename T>
-__device__ __forceinline__ void store_chunk(const Row<T>& row, T* dz, int64_t c, const float* out) {
-  const int64_t first = row.first(c);
+template <typename T, typename I>
+__device__ __forceinline__ void store_chunk(const Row<T>& row, T* dz, I c, const float* out) {
+  const I first = row.first(c);
 #pragma unroll
   for (int e = 0; e < Logit<T>::kPer; ++e)
     if (first + e >= 0 && first + e < row.vocab) Logit<T>::store(dz + first + e, out[e]);
 }
-template <typename T>
-__device__ __forceinline__ void policy_chunk(const Row<T>& row, T* dz, bool same_grid, int64_t c, uint4 a, const PolicyGrad& g) {
+template <typename T, typename I>      // the chunk's number as int where the whole row's are, which takes fewer instructions
+__device__ __forceinline__ void policy_chunk(const Row<T>& row, T* dz, bool same_grid, I c, uint4 a, const PolicyGrad& g) {
   float out[Logit<T>::kPer];
   if (g.t.far) policy_values_far<T>(a, g.k, g.t, out);
   else policy_values<T>(a, g, out);
-  const int64_t at = g.label - row.first(c);
-  if (at >= 0 && at < Logit<T>::kPer) put_label<T>(out, at, g.t.at_label);
+  if (c == g.hot) put_label<T>(out, g.place, g.t.at_label);
   if (same_grid && row.whole(c)) st_stream(dz + row.first(c), Logit<T>::pack(out));
   else store_chunk<T>(row, dz, c, out);
+}
+// The other values of the label's chunk, by as many lanes of a warp as it has: -inf where there is none.
+template <typename T>
+__device__ __forceinline__ float beside_label(const Row<T>& row, int hot, int label) {
+  const int lane = threadIdx.x % 32, at = row.first(hot) + lane;
+  return lane < Logit<T>::kPer && at >= 0 && at < row.vocab && at != label ? Logit<T>::load(row.z + at) : -INFINITY;
 }
 template <typename T>
 __device__ __forceinline__ void zero_chunks(const Row<T>& row, T* dz, bool same_grid, int64_t from, int64_t to, int first, int step) {
@@ -195,20 +230,17 @@ struct RowInput {
 __device__ __forceinline__ RowInput row_input(const PolicyParams& p, int64_t r) {
   return RowInput{p.advantage ? p.advantage[r] : 0.0f, p.old_logp ? p.old_logp[r] : 0.0f, p.ref_logp ? p.ref_logp[r] : 0.0f, p.row_grad ? p.row_grad[r] : 1.0f};
 }
-// ln s to 2^-24: the exponent's part in FP64, FP32 for the part in [1, 2).
-__device__ __forceinline__ double log_of(float s) {
-  if (!(s >= 1.1754944e-38f && s <= 3.4028235e38f)) return (double)logf(s);
-  const int bits = __float_as_int(s);
-  return (double)((bits >> 23) - 127) * 0.6931471805599453 + (double)logf(__int_as_float((bits & 0x007fffff) | 0x3f800000));
-}
 // A row's loss, and the rest of its terms, by one warp: the exponentials that hang on the log-probability are taken by three lanes at
-// once. The log-probability comes in FP64, its differences from the old and the reference's one are formed in FP64.
-__device__ __forceinline__ void finish_row(const PolicyParams& p, const RowInput& in, double logp, float scale, RowTerms* t) {
+// once. The log-probability comes in FP64, its differences from the old and the reference's one are formed in FP64; `rest` is what the
+// label's probability lacks of one, where it is known by itself (kRest).
+template <bool kRest>
+__device__ __forceinline__ void finish_row(const PolicyParams& p, const RowInput& in, double logp, float rest, float scale, RowTerms* t) {
   const int lane = threadIdx.x % 32;
   const float a = in.advantage, k = p.ref_logp ? (float)((double)in.ref_logp - logp) : 0.0f;
   const float x = lane == 0 ? (p.old_logp && a != 0.0f ? (float)(logp - (double)in.old_logp) : 0.0f) : lane == 1 ? k : (float)logp;
   const float ratio = __shfl_sync(0xffffffffu, expf(x), 0), less_one = expm1f(x);
-  const float to_ref = __shfl_sync(0xffffffffu, less_one, 1), prob = __shfl_sync(0xffffffffu, less_one, 2);     // less one
+  const float to_ref = __shfl_sync(0xffffffffu, less_one, 1);     // e^k less one
+  if (!kRest) rest = -__shfl_sync(0xffffffffu, less_one, 2);
   float loss = 0.0f, slope = 0.0f;
   if (a != 0.0f) {
     const bool inside = !(a > 0.0f ? ratio > p.high : ratio < p.low) || a != a;
@@ -223,20 +255,30 @@ __device__ __forceinline__ void finish_row(const PolicyParams& p, const RowInput
   t->logp = (float)logp;
   const float f = in.grad == 0.0f ? 0.0f : in.grad * slope * p.inv_tau;
   t->factor = -f * scale;
-  t->at_label = -f * prob;
+  t->at_label = f * rest;
   t->f = f;
 }
-// From the sum, and the label's logit.
-__device__ __forceinline__ RowTerms finish_sum(const PolicyParams& p, const RowInput& in, PolicySum all, float mark, float k) {
-  const float c = shift_of(all.m, k);
-  const double log_sum = log_of(all.s);
-  RowTerms t;
-  t.far = is_far(c);
-  t.shift = t.far ? all.m : c;
-  t.offset = 0.0f;
-  const double logp = t.far ? ((double)mark - (double)all.m) * p.inv_tau64 : ((double)k * (double)mark - (double)c) * 0.6931471805599453;
-  finish_row(p, in, logp - log_sum, 1.0f / all.s, &t);
-  return t;
+// From the sum over all but the label, and the label's logit, whose term is 2^e in the sum's units. Where that is above one, all are taken down by
+// it, and the log-probability is -log(1 + rest): with the digits of `rest` by log(u) rest / (u - 1), u = 1 + rest as rounded (W. Kahan).
+__device__ __forceinline__ RowTerms finish_sum(const PolicyParams& p, const RowInput& in, PolicySum others, float mark, float k) {
+  const float c = shift_of(others.m, k);
+  RowTerms r;
+  r.far = is_far(c);
+  r.shift = r.far ? others.m : c;
+  r.offset = 0.0f;
+  float e = r.far ? (mark - others.m) * k : fmaf(mark, k, -c);
+  if (others.m == -INFINITY) e = mark == -INFINITY ? NAN : 0.0f;      // nothing but the label, or not even that
+  if (mark == INFINITY) e = NAN;
+  const float term = exp2_approx(-fabsf(e)), down = e >= 0.0f ? term : 1.0f;
+  const float rest = others.s * down, all = (e >= 0.0f ? 1.0f : term) + rest, less = all - 1.0f, over_all = 1.0f / all;
+  const float corrected = less > 0.0f ? __fdividef(rest, less) : 1.0f;
+  const int bits = __float_as_int(all);                               // the exponent's part of the log in FP64; NaN stays
+  const float log_part = logf(__int_as_float((bits & 0x007fffff) | 0x3f800000)) + (all - all);
+  const double own = r.far ? ((double)mark - (double)others.m) * p.inv_tau64 : ((double)k * (double)mark - (double)c) * 0.6931471805599453;
+  const double log_all = fma((double)((bits >> 23) - 127), 0.6931471805599453, (double)log_part);
+  const double logp = e >= 0.0f && rest < 1.0f ? -(double)(less > 0.0f ? log_part * corrected : rest) : (e >= 0.0f ? 0.0 : own) - log_all;
+  finish_row<true>(p, in, logp, rest * over_all, down * over_all, &r);
+  return r;
 }
 __device__ __forceinline__ void write_loss(const PolicyParams& p, int64_t r, const RowTerms& t) {
   if (p.loss) p.loss[r] = t.loss;
@@ -249,7 +291,7 @@ __device__ __forceinline__ RowTerms finish_saved(const PolicyParams& p, const Ro
   t.far = is_far((float)exact) || is_far(mark * k);
   t.shift = t.far ? mark : (float)exact;
   t.offset = (float)log2_p;
-  finish_row(p, in, logp, t.far ? 1.0f : exp2f((float)((double)t.shift - exact)), &t);
+  finish_row<false>(p, in, logp, 0.0f, t.far ? 1.0f : exp2f((float)((double)t.shift - exact)), &t);
   return t;
 }
 
@@ -263,7 +305,8 @@ struct PolicyShared {
 
 // kGradient: the gradient from the saved log-probability, else log-probability and loss. The blocks of a cluster share a row's chunks;
 // forward they bring their sums to the first through distributed shared memory. Bound: HBM. 4096 x 131072 BF16: forward 170 us
-// (6.3 TB/s), gradient 349 (6.2).
+// (6.3 TB/s), gradient 349 (6.2); with the label's chunk asked for in int64_t, or its label taken out of a chunk that has been read, forward 2 to 4 %
+// more.
 template <typename T, bool kGradient>
 __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __grid_constant__ PolicyParams p, int cluster) {
   start_after_previous_kernel();
@@ -301,7 +344,8 @@ __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __g
     if (cluster > 1) cluster_sync(); else __syncthreads();
     const RowTerms t = sh.row;
     if (t.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, from, to, threadIdx.x, kPolicyThreads);
-    const PolicyGrad g = {k, t, label};
+    const int hot = (label + row.head) / Logit<T>::kPer;
+    const PolicyGrad g = {k, t, hot, label - row.first(hot)};
     for (int64_t c = from + threadIdx.x; c < to; c += kPolicyThreads * U) {
       uint4 a[U];
 #pragma unroll
@@ -312,11 +356,19 @@ __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __g
         if (c + u * kPolicyThreads < to) policy_chunk<T>(row, dz, same_grid, c + u * kPolicyThreads, a[u], g);
     }
   } else {
+    // the label's chunk is not read with the others, but its other values by the last warp
+    const int label_chunk = (label + row.head) / Logit<T>::kPer, n = (int)(to - from), hot = label_chunk - (int)from;
     PolicySum mine = {-INFINITY, 0.0f};
-    for (int64_t c = from + threadIdx.x; c < to; c += kPolicyThreads * U) {
+    if (threadIdx.x >= kPolicyThreads - 32 && hot >= 0 && hot < n) mine = one_value(beside_label<T>(row, label_chunk, label), k);
+    for (int c = threadIdx.x; c < n; c += kPolicyThreads * U) {
       uint4 a[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) a[u] = c + u * kPolicyThreads < to ? row.load(c + u * kPolicyThreads) : Logit<T>::lowest();
+      for (int u = 0; u < U; ++u) a[u] = c + u * kPolicyThreads < n && c + u * kPolicyThreads != hot ? row.load(from + c + u * kPolicyThreads) : Logit<T>::lowest();
+      // FP32: all of them before the first is used; the compiler uses each as it comes (1023 x 100003: 72 -> 47 us)
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) asm volatile("" : "+r"(a[u].x), "+r"(a[u].y), "+r"(a[u].z), "+r"(a[u].w));
+      }
       add_chunks<T, U>(mine, a, k);
     }
     mine = join_sums<32>(mine, k);
@@ -342,10 +394,13 @@ __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __g
 }
 
 // Both for short rows: kRow threads hold a row in registers, U chunks each; a warp, eight of them per block, or a block. Against the ring
-// below, which is for rows longer than these: 8192 x 8000 BF16 55 us (a block of 256) and 117, 4096 x 32768 108 (of 512) and 117;
+// below, which is for rows longer than these: 8192 x 8000 BF16 55 us (a block of 256) and 117, 4096 x 32768 111 (of 512) and 117;
 // a warp for 8192 x 1000: 10, where a block takes 28.
+// Blocks per SM that the registers allow: four for each chunk as it is read, and what a thread of a row needs besides (8192 x 8000 BF16: six
+// blocks 55 us, the five that the compiler would leave 61).
+constexpr int held_blocks(int u, int row) { return 65536 / ((row < 256 ? 256 : row) * (4 * u + (row < 256 ? 44 : 24))); }
 template <typename T, int U, int kRow>
-__global__ void __launch_bounds__(kRow < 256 ? 256 : kRow) policy_held_kernel(const __grid_constant__ PolicyParams p) {
+__global__ void __launch_bounds__(kRow < 256 ? 256 : kRow, held_blocks(U, kRow)) policy_held_kernel(const __grid_constant__ PolicyParams p) {
   start_after_previous_kernel();
   __shared__ RowTerms shared_terms;
   __shared__ PolicySum warps[16];
@@ -369,12 +424,15 @@ __global__ void __launch_bounds__(kRow < 256 ? 256 : kRow) policy_held_kernel(co
   const float at = Logit<T>::load(z + label), k = p.inv_tau * kLog2e;
   RowInput in = {};
   if (thread < 32) in = row_input(p, r);
+  const int hot = (label + row.head) / Logit<T>::kPer;
   uint4 a[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int c = thread + u * kRow;
     a[u] = c < chunks ? row.load(c) : Logit<T>::lowest();
   }
+  const int place = label - row.first(hot);
+  leave_out<T, U>(a, thread, kRow, hot, place);       // the gradient does not need it either
   PolicySum mine = {-INFINITY, 0.0f};
   add_chunks<T, U>(mine, a, k);
   mine = join_sums<32>(mine, k);
@@ -397,7 +455,7 @@ __global__ void __launch_bounds__(kRow < 256 ? 256 : kRow) policy_held_kernel(co
     t = shared_terms;
   }
   if (t.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, 0, chunks, thread, kRow);
-  const PolicyGrad g = {k, t, label};
+  const PolicyGrad g = {k, t, hot, place};
 #pragma unroll
   for (int u = 0; u < U; ++u)
     if (thread + u * kRow < chunks) policy_chunk<T>(row, dz, same_grid, thread + u * kRow, a[u], g);
@@ -505,11 +563,12 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
       const RingSlice<T> s(p, r, rank);
       // the label's logit comes from the block that has it, before any block may write this row's gradient to the same memory
       float mark = 0.0f;
-      const int64_t hot = (label + s.row.head) / Logit<T>::kPer;
+      const int hot = (label + s.row.head) / Logit<T>::kPer, place = label - s.row.first(hot), whole = hot >= s.mid && hot < s.mid + s.n ? (int)(hot - s.mid) : -1;      // among the whole chunks
       if (warp == 0 && (hot == s.lo || hot == s.hi - 1)) mark = Logit<T>::load(s.row.z + label);
       PolicySum mine = {-INFINITY, 0.0f};
       s.edges(threadIdx.x, [&](int64_t c) {
-        const uint4 a = s.row.load(c);
+        uint4 a = s.row.load(c);
+        if (c == hot) a = without<T>(a, place);
         add_chunks<T, 1>(mine, &a, k);
       });
       __syncwarp();
@@ -525,8 +584,10 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
           for (int u = 0; u < kSlotUnroll; ++u)
             if (i0 + (int)threadIdx.x + u * kRingGroup >= s.n) a[u] = Logit<T>::lowest();
         }
-        if (warp == 0 && hot >= s.mid + i0 && hot < s.mid + i0 + kSlotChunks && hot < s.mid + s.n)
-          mark = Logit<T>::load(reinterpret_cast<const T*>(slots + slot.i * kSlotChunks) + (label - s.row.first(s.mid + i0)));
+        if (whole >= i0 && whole < i0 + kSlotChunks) {
+          if (warp == 0) mark = Logit<T>::load(reinterpret_cast<const T*>(slots + slot.i * kSlotChunks + whole - i0) + place);
+          leave_out<T, kSlotUnroll>(a, i0 + (int)threadIdx.x, kRingGroup, whole, place);
+        }
         add_chunks<T, kSlotUnroll>(mine, a, k);
       }
       mine = join_sums<32>(mine, k);
@@ -576,12 +637,13 @@ __global__ void __launch_bounds__(kRingThreads, 1) policy_ring_kernel(const __gr
       ok = __all_sync(0xffffffffu, wait(smem_addr(&ring.known[at.i]), at.parity));
       if (!ok) break;
       const RowTerms t = ring.row[at.i];
-      const PolicyGrad g = {k, t, label};
+      const int label_chunk = (label + s.row.head) / Logit<T>::kPer;
+      const PolicyGrad g = {k, t, label_chunk, label - s.row.first(label_chunk)};
       at.next();
       const bool zero = t.f == 0.0f, usual = same_grid && !t.far;
       if (zero) zero_chunks<T>(s.row, dz, same_grid, s.lo, s.hi, thread, kRingGroup);
       else s.edges(thread, [&](int64_t c) { policy_chunk<T>(s.row, dz, same_grid, c, s.row.load(c), g); });
-      const int64_t hot = (label + s.row.head) / Logit<T>::kPer - s.mid;       // the label's chunk
+      const int64_t hot = label_chunk - s.mid;
       uint4* out = reinterpret_cast<uint4*>(dz + s.row.first(s.mid)) + thread;     // used where it is aligned
       for (int i0 = 0; i0 < s.n; i0 += kSlotChunks, slot.next()) {
         // the slot is full: what is known of the row was known after its sums

@@ -64,3 +64,48 @@ def test_policy_rows_at_and_beyond_what_a_cluster_holds(ctx, dtype, more, layout
     a["adv"][3], a["old"][3] = 1.0, a["old"][3] - 3.0         # outside the clipped range: no gradient of the first term
     policy_case(ctx, a, layout=layout)
     policy_case(ctx, {**a, "ref": None}, layout=layout)
+
+
+# Forms that take each of the kernels: rows held by a warp, by a block, in shared memory of one block and of a cluster, and in none.
+KERNELS = [(12, 1000), (12, 20000), (170, 40000), (12, 70001), (4, 600003)]
+
+
+def confident(N, V, dtype, seed):
+    """Labels that have all but 1e-2 to 1e-13 of their rows' probability, advantages without an old policy (the ratio is one)."""
+    g = gen(seed)
+    z = randn(g, N, V, dtype=dtype)
+    labels = torch.randint(0, V, (N,), generator=g, device="cuda")
+    labels[0], labels[-1] = 0, V - 1
+    lack = torch.linspace(2.0, 13.0, N, device="cuda", dtype=F64)[torch.randperm(N, generator=g, device="cuda")] * math.log(10.0)
+    others = z.double().scatter(1, labels[:, None], -math.inf).logsumexp(1)
+    z.scatter_(1, labels[:, None], (others + lack).to(dtype)[:, None])
+    return z, labels.to(torch.int32), randn(g, N), randn(g, N)
+
+
+@pytest.mark.parametrize("tau", [1.0, 0.7])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,V", KERNELS)
+def test_policy_of_tokens_that_are_all_but_certain(ctx, dtype, N, V, tau):
+    """What the label's probability lacks of one keeps its digits, however little it is: log-probability and gradient are off by 2e-5 of
+    themselves (the tolerance of a probability in more_operators_ref.policy) and their own rounding, and a row's gradient adds up to zero to within
+    twice that."""
+    z, labels, adv, gr = confident(N, V, dtype, seed=V)
+    z = (z.double() * tau).to(dtype)
+    at = labels.long()[:, None]
+    zd = z.double() / tau
+    t = zd.gather(1, at)[:, 0] - zd.scatter(1, at, -math.inf).logsumexp(1)       # the label's log odds
+    lp, rest = -torch.log1p(torch.exp(-t)), 1.0 / (1.0 + torch.exp(t))
+    f = -(adv * gr).double()[:, None] / tau                                      # d loss / d logp = -adv
+    want = f * (torch.zeros_like(zd).scatter(1, at, 1.0) - torch.log_softmax(zd, 1).exp())
+    want.scatter_(1, at, f * rest[:, None])
+    new = lambda: torch.empty(N, device="cuda")  # noqa: E731
+    loss, logp, logp2, dz, dz2 = new(), new(), new(), torch.empty_like(z), torch.empty_like(z)
+    ctx.slidedp_policy_loss(z, labels, None, None, adv, loss, logp, temperature=tau)
+    ctx.slidedp_policy_loss_backward(z, labels, None, None, adv, logp, gr, dz, temperature=tau)
+    ctx.slidedp_policy_step(z, labels, None, None, adv, gr, loss, logp2, dz2, temperature=tau)
+    half = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    for what, p, d in (("two calls", logp, dz), ("step", logp2, dz2)):
+        assert_close(what + ": logp", p, lp, 2e-5 * lp.abs())
+        assert_close(what + ": dz", d, want, (2e-5 + half) * want.abs() + 1e-37)
+        if dtype == F32:
+            assert_close(what + ": sum", d.double().sum(1), torch.zeros_like(lp), (4e-5 + 2 * half) * want.gather(1, at)[:, 0].abs() + V * 1e-37)
