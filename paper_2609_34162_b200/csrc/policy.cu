@@ -230,6 +230,11 @@ struct RowInput {
 __device__ __forceinline__ RowInput row_input(const PolicyParams& p, int64_t r) {
   return RowInput{p.advantage ? p.advantage[r] : 0.0f, p.old_logp ? p.old_logp[r] : 0.0f, p.ref_logp ? p.ref_logp[r] : 0.0f, p.row_grad ? p.row_grad[r] : 1.0f};
 }
+// e^k - k - 1 for |k| up to a quarter, by the exponential's series from its second power on: 2^-26 of itself.
+__device__ __forceinline__ float beyond_linear(float k) {
+  const float k2 = k * k, far = fmaf(1.0f / 5040, k, 1.0f / 720), middle = fmaf(1.0f / 120, k, 1.0f / 24);
+  return fmaf(fmaf(far, k2, middle), k2, fmaf(1.0f / 6, k, 0.5f)) * k2;
+}
 // A row's loss, and the rest of its terms, by one warp: the exponentials that hang on the log-probability are taken by three lanes at
 // once. The log-probability comes in FP64, its differences from the old and the reference's one are formed in FP64; `rest` is what the
 // label's probability lacks of one, where it is known by itself (kRest).
@@ -239,7 +244,7 @@ __device__ __forceinline__ void finish_row(const PolicyParams& p, const RowInput
   const float a = in.advantage, k = p.ref_logp ? (float)((double)in.ref_logp - logp) : 0.0f;
   const float x = lane == 0 ? (p.old_logp && a != 0.0f ? (float)(logp - (double)in.old_logp) : 0.0f) : lane == 1 ? k : (float)logp;
   const float ratio = __shfl_sync(0xffffffffu, expf(x), 0), less_one = expm1f(x);
-  const float to_ref = __shfl_sync(0xffffffffu, less_one, 1);     // e^k less one
+  const float near = beyond_linear(k), to_ref = __shfl_sync(0xffffffffu, less_one, 1);     // e^k less one
   if (!kRest) rest = -__shfl_sync(0xffffffffu, less_one, 2);
   float loss = 0.0f, slope = 0.0f;
   if (a != 0.0f) {
@@ -248,7 +253,7 @@ __device__ __forceinline__ void finish_row(const PolicyParams& p, const RowInput
     if (inside) slope = -a * ratio;
   }
   if (p.ref_logp) {
-    loss = fmaf(p.kl, to_ref - k, loss);
+    loss = fmaf(p.kl, fabsf(k) <= 0.25f ? near : to_ref == INFINITY ? to_ref : to_ref - k, loss);
     slope = fmaf(-p.kl, to_ref, slope);
   }
   t->loss = loss;

@@ -109,3 +109,37 @@ def test_policy_of_tokens_that_are_all_but_certain(ctx, dtype, N, V, tau):
         assert_close(what + ": dz", d, want, (2e-5 + half) * want.abs() + 1e-37)
         if dtype == F32:
             assert_close(what + ": sum", d.double().sum(1), torch.zeros_like(lp), (4e-5 + 2 * half) * want.gather(1, at)[:, 0].abs() + V * 1e-37)
+
+
+def test_policy_second_term_near_the_reference(ctx):
+    """e^k - k - 1 is k^2 / 2 there: off by the digits of k, not of k / k^2. The log-probabilities are close to zero, so that FP32 has
+    k's digits: 2e-5 of logp beside k, up to three times that in the term, and four roundings."""
+    z, labels, _, _ = confident(64, 1000, F32, seed=3)
+    at = labels.long()[:, None]
+    t = z.double().gather(1, at)[:, 0] - z.double().scatter(1, at, -math.inf).logsumexp(1)
+    lp = -torch.log1p(torch.exp(-t))
+    for size in (3e-3, 0.1, 0.9, 1.1, 3.0):
+        for sign in (-1.0, 1.0):
+            refp = (lp + sign * size).float()
+            k = refp.double() - lp
+            exact = torch.where(k.abs() < 0.01, k * k * (0.5 + k / 6 + k * k / 24 + k ** 3 / 120), torch.expm1(k) - k)
+            loss, logp = torch.empty(64, device="cuda"), torch.empty(64, device="cuda")
+            ctx.slidedp_policy_loss(z, labels, None, refp, None, loss, logp, kl_weight=2.0)
+            tol = exact * (2.0 ** -21 + 3 * 2e-5 * lp.abs() / k.abs() * torch.clamp(k.abs(), min=1.0))
+            assert_close(f"loss {sign * size}", loss, 2.0 * exact, 2.0 * tol)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,V", KERNELS)
+def test_policy_tokens_without_probability(ctx, dtype, N, V):
+    """A label whose logit is -inf, others being finite: logp is -inf, and the second term's limit is +inf, not NaN."""
+    z = randn(gen(V), N, V, dtype=dtype)
+    labels = (torch.arange(N, device="cuda") * 31 % V).to(torch.int32)
+    z.scatter_(1, labels.long()[:, None], -math.inf)
+    f = torch.zeros(N, device="cuda")
+    loss, logp, dz = torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.empty_like(z)
+    for call in (lambda: ctx.slidedp_policy_loss(z, labels, None, f, None, loss, logp, kl_weight=0.1),
+                 lambda: ctx.slidedp_policy_step(z, labels, None, f, None, None, loss, logp, dz, kl_weight=0.1)):
+        loss.fill_(0.0), logp.fill_(0.0)
+        call()
+        assert (logp == -math.inf).all() and (loss == math.inf).all()
