@@ -274,7 +274,7 @@ SLIDEDP_API size_t slidedp_block_norm_workspace(const slidedp_block_norm_args* a
  * (clip_low may exceed 1).
  *
  * Gradient: d_logits[r] = row_grad[r] * d loss[r] / d z, with row_grad: rows floats (nullable: ones). A ratio on the edge of the
- * clipped range counts as inside. slidedp_policy_loss_backward takes the forward's logp;
+ * clipped range counts as inside. slidedp_policy_loss_backward takes the forward's logp, and reads rows twice where that is below -64;
  * slidedp_policy_step computes loss, logp and gradient in one call. d_logits may be the logits themselves (same address and
  * stride; the same address with another stride is refused) and may not overlap them otherwise. A kl_weight of 0 is no second
  * term, whatever ref_logp holds. Rows whose gradient is zero throughout (absent, clipped without a second term, row_grad 0)

@@ -308,9 +308,65 @@ struct PolicyShared {
   alignas(8) float2 part[kPolicyMaxCluster];   // maximum and sum of each block of the cluster
 };
 
+// A block's sum to block `to` of its cluster, and the sum of what has come.
+__device__ __forceinline__ void store_part(PolicyShared& sh, int rank, int to, PolicySum v) {
+  const uint32_t there = peer_addr(smem_addr(&sh.part[rank]), to);
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.m), "f"(v.s) : "memory");
+}
+__device__ __forceinline__ PolicySum join_parts(const PolicyShared& sh, int cluster, float k) {
+  const int i = threadIdx.x % kPolicyMaxCluster;
+  return join_sums<kPolicyMaxCluster>(i < cluster ? PolicySum{sh.part[i].x, sh.part[i].y} : PolicySum{-INFINITY, 0.0f}, k);
+}
+// The sum over chunks [from, to) without the label, by a block; all threads get it.
+template <typename T>
+__device__ __forceinline__ PolicySum block_sum(const Row<T>& row, int64_t from, int64_t to, int label, float k, PolicySum* warps) {
+  constexpr int U = kPolicyUnroll;
+  // the label's chunk is not read with the others, but its other values by the last warp
+  const int label_chunk = (label + row.head) / Logit<T>::kPer, n = (int)(to - from), hot = label_chunk - (int)from;
+  PolicySum mine = {-INFINITY, 0.0f};
+  if (threadIdx.x >= kPolicyThreads - 32 && hot >= 0 && hot < n) mine = one_value(beside_label<T>(row, label_chunk, label), k);
+  for (int c = threadIdx.x; c < n; c += kPolicyThreads * U) {
+    uint4 a[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) a[u] = c + u * kPolicyThreads < n && c + u * kPolicyThreads != hot ? row.load(from + c + u * kPolicyThreads) : Logit<T>::lowest();
+    // FP32: all of them before the first is used; the compiler uses each as it comes (1023 x 100003: 72 -> 47 us)
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) asm volatile("" : "+r"(a[u].x), "+r"(a[u].y), "+r"(a[u].z), "+r"(a[u].w));
+    }
+    add_chunks<T, U>(mine, a, k);
+  }
+  mine = join_sums<32>(mine, k);
+  if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = mine;
+  __syncthreads();
+  return join_sums<kPolicyWarps>(warps[threadIdx.x % kPolicyWarps], k);
+}
+
+// FP32 holds a log-probability to 2^-24 of itself, by which a row's probabilities are off that are made from it: 4e-6 at -64. Rows with less are
+// summed again, a label without any probability among them.
+constexpr float kTrustedLogp = -64.0f;
+
+// The row's terms from its logits, by all blocks of a cluster, which have met and have not written any.
+template <typename T>
+__device__ __forceinline__ void sum_again(const PolicyParams& p, PolicyShared& sh, int64_t r, int rank, int cluster, int64_t from, int64_t to, int label) {
+  const Row<T> row(static_cast<const T*>(p.z) + r * p.z_stride, p.vocab);
+  const float mark = Logit<T>::load(row.z + label), k = p.inv_tau * kLog2e;
+  PolicySum mine = block_sum<T>(row, from, to, label, k, sh.warp);
+  if (cluster > 1) {
+    if ((int)threadIdx.x < cluster) store_part(sh, rank, threadIdx.x, mine);
+    cluster_sync();
+    mine = join_parts(sh, cluster, k);
+  }
+  if (threadIdx.x < 32) {
+    const RowTerms t = finish_sum(p, row_input(p, r), mine, mark, k);
+    if (threadIdx.x == 0) sh.row = t;
+  }
+  __syncthreads();
+}
+
 // kGradient: the gradient from the saved log-probability, else log-probability and loss. The blocks of a cluster share a row's chunks;
 // forward they bring their sums to the first through distributed shared memory. Bound: HBM. 4096 x 131072 BF16: forward 170 us
-// (6.3 TB/s), gradient 349 (6.2); with the label's chunk asked for in int64_t, or its label taken out of a chunk that has been read, forward 2 to 4 %
+// (6.3 TB/s), gradient 343 (6.3); with the label's chunk asked for in int64_t, or its label taken out of a chunk that has been read, forward 2 to 4 %
 // more.
 template <typename T, bool kGradient>
 __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __grid_constant__ PolicyParams p, int cluster) {
@@ -341,55 +397,36 @@ __global__ void __launch_bounds__(kPolicyThreads, 5) policy_row_kernel(const __g
   const float at = Logit<T>::load(z + label), k = p.inv_tau * kLog2e;
   constexpr int U = kPolicyUnroll;
   if constexpr (kGradient) {
+    const float saved = p.saved_logp[r];
     if (threadIdx.x < 32) {
-      const RowTerms t = finish_saved(p, row_input(p, r), at, k, p.saved_logp[r]);
+      const RowTerms t = finish_saved(p, row_input(p, r), at, k, saved);
       if (threadIdx.x == 0) sh.row = t;
     }
     // nothing has been read of the row but `at`, which no block may change before all have it
     if (cluster > 1) cluster_sync(); else __syncthreads();
+    if (saved < kTrustedLogp) sum_again<T>(p, sh, r, rank, cluster, from, to, label);
     const RowTerms t = sh.row;
     if (t.f == 0.0f) return zero_chunks<T>(row, dz, same_grid, from, to, threadIdx.x, kPolicyThreads);
     const int hot = (label + row.head) / Logit<T>::kPer;
     const PolicyGrad g = {k, t, hot, label - row.first(hot)};
-    for (int64_t c = from + threadIdx.x; c < to; c += kPolicyThreads * U) {
+    const int last = (int)to;        // chunks in int: with int64_t registers are spilled (8192 x 1000 BF16 23.5 us in place of 26.3, 4096 x 131072 332 of 345)
+    for (int c = (int)from + threadIdx.x; c < last; c += kPolicyThreads * U) {
       uint4 a[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (c + u * kPolicyThreads < to) a[u] = row.load(c + u * kPolicyThreads);
+        if (c + u * kPolicyThreads < last) a[u] = row.load(c + u * kPolicyThreads);
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (c + u * kPolicyThreads < to) policy_chunk<T>(row, dz, same_grid, c + u * kPolicyThreads, a[u], g);
+        if (c + u * kPolicyThreads < last) policy_chunk<T>(row, dz, same_grid, c + u * kPolicyThreads, a[u], g);
     }
   } else {
-    // the label's chunk is not read with the others, but its other values by the last warp
-    const int label_chunk = (label + row.head) / Logit<T>::kPer, n = (int)(to - from), hot = label_chunk - (int)from;
-    PolicySum mine = {-INFINITY, 0.0f};
-    if (threadIdx.x >= kPolicyThreads - 32 && hot >= 0 && hot < n) mine = one_value(beside_label<T>(row, label_chunk, label), k);
-    for (int c = threadIdx.x; c < n; c += kPolicyThreads * U) {
-      uint4 a[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) a[u] = c + u * kPolicyThreads < n && c + u * kPolicyThreads != hot ? row.load(from + c + u * kPolicyThreads) : Logit<T>::lowest();
-      // FP32: all of them before the first is used; the compiler uses each as it comes (1023 x 100003: 72 -> 47 us)
-      if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) asm volatile("" : "+r"(a[u].x), "+r"(a[u].y), "+r"(a[u].z), "+r"(a[u].w));
-      }
-      add_chunks<T, U>(mine, a, k);
-    }
-    mine = join_sums<32>(mine, k);
-    if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32] = mine;
-    __syncthreads();
-    mine = join_sums<kPolicyWarps>(sh.warp[threadIdx.x % kPolicyWarps], k);
+    PolicySum mine = block_sum<T>(row, from, to, label, k, sh.warp);
     if (cluster > 1) {
       cluster_wait();
-      if (threadIdx.x == 0) {
-        const uint32_t there = peer_addr(smem_addr(&sh.part[rank]), 0);
-        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(mine.m), "f"(mine.s) : "memory");
-      }
+      if (threadIdx.x == 0) store_part(sh, rank, 0, mine);
       cluster_sync();
       if (rank > 0) return;
-      const int i = threadIdx.x % kPolicyMaxCluster;
-      mine = join_sums<kPolicyMaxCluster>(i < cluster ? PolicySum{sh.part[i].x, sh.part[i].y} : PolicySum{-INFINITY, 0.0f}, k);
+      mine = join_parts(sh, cluster, k);
     }
     if (threadIdx.x < 32) {
       const RowTerms t = finish_sum(p, row_input(p, r), mine, at, k);

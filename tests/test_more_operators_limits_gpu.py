@@ -143,3 +143,33 @@ def test_policy_tokens_without_probability(ctx, dtype, N, V):
         loss.fill_(0.0), logp.fill_(0.0)
         call()
         assert (logp == -math.inf).all() and (loss == math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,V", KERNELS + [(700, 9000)])
+def test_policy_backward_of_very_unlikely_tokens(ctx, dtype, N, V):
+    """Labels whose log-probability is anything down to -inf, rows far from zero among them: the gradient's probabilities are off by 2e-5 of
+    themselves (as in more_operators_ref.policy), not by 2^-24 of the log-probability that the forward call has saved."""
+    g = gen(V + 1)
+    z = randn(g, N, V, dtype=dtype)
+    labels = torch.randint(0, V, (N,), generator=g, device="cuda")
+    labels[0], labels[-1] = 0, V - 1
+    row = torch.arange(N, device="cuda")
+    z[row % 6 == 5] += 3e6 if dtype == F32 else 512.0
+    down = torch.tensor([-40.0, -90.0, -700.0, -3e4, -math.inf, -9e5 if dtype == F32 else -2e4], device="cuda")[row % 6]
+    z[row, labels] = (z[row, labels].double() + down).to(dtype)
+    adv, gr = randn(g, N), randn(g, N)
+    p = torch.log_softmax(z.double(), 1).exp()
+    want = (-(adv * gr)).double()[:, None] * (torch.zeros_like(p).scatter(1, labels[:, None], 1.0) - p)
+    labels = labels.to(torch.int32)
+    logp, loss, dz = torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.empty_like(z)
+    ctx.slidedp_policy_loss(z, labels, None, None, adv, loss, logp)
+    ctx.slidedp_policy_loss_backward(z, labels, None, None, adv, logp, gr, dz)
+    half = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    tol = (2e-5 + half) * want.abs() + 1e-37
+    assert_close("dz", dz, want, tol)
+    step, logp2 = torch.empty_like(z), torch.empty_like(logp)       # its log-probabilities may differ in the last bits: the saved ones stay
+    ctx.slidedp_policy_step(z, labels, None, None, adv, gr, loss, logp2, step)
+    assert_close("step: dz", step, want, tol)
+    ctx.slidedp_policy_loss_backward(z, labels, None, None, adv, logp, gr, z)                 # in place
+    assert torch.equal(z, dz)
