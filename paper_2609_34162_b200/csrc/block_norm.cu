@@ -741,9 +741,13 @@ __global__ void __launch_bounds__(kThreads, 1) block_norm_backward_ring_kernel(c
   constexpr bool kKeep = kVector && !kToken;
   uint64_t sum_post[kPairs] = {}, sum_pre[kPairs] = {};
   int turn = 0;
-  // A row's first sum with the last one of the row before, as forward, where there are registers for it: 8192 x 5120 BF16 132 -> 127 us, with
-  // a token's gate 214 -> 190, 4096 x 5120 FP32 85 -> 91; but 8192 x 4096 with its two groups 87 -> 96.
-  const bool ahead = kThreads < 512 && norm_y && rp.feed.stages > 1;
+  // A row's first sum with the last one of the row before, as forward, where that was faster (us, without and with it). In vectors, one group of
+  // up to ten warps: 8192 x 5120 BF16 128 -> 122, with a token's gate 204 -> 187, without the norm of x' 102 -> 97; 4096 x 5120 FP32
+  // 87 -> 90, 4608 columns 77 -> 85, with a token's gate 160 -> 159, without the norm of x' 82 -> 78. In pairs: 6000 x 5002 BF16 192 -> 186,
+  // with a token's gate 226 -> 246. In single columns: 6000 x 5001 BF16 208 -> 268, 3000 x 5001 FP32 99 -> 125. Two groups: 8192 x 4096
+  // BF16 87 -> 96.
+  constexpr bool kAhead = kThreads < 512 && (kVector || (V == 2 && !kToken));
+  const bool ahead = kAhead && norm_y && (sizeof(T) == 2 || !norm_x) && rp.feed.stages > 1;
   const auto squares = [&](int64_t row, bool following) { return sum_squares(cols, rows.at(kInY, row, following), p.hidden); };
   float r = 1.0f;
   if (ahead && rows.count > 0) {
