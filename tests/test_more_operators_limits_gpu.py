@@ -173,3 +173,38 @@ def test_policy_backward_of_very_unlikely_tokens(ctx, dtype, N, V):
     assert_close("step: dz", step, want, tol)
     ctx.slidedp_policy_loss_backward(z, labels, None, None, adv, logp, gr, z)                 # in place
     assert torch.equal(z, dz)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,V", KERNELS + [(700, 9000)])
+def test_policy_labels_whose_logit_is_no_number(ctx, dtype, N, V):
+    """NaN and +inf at the label, or a row of -inf: log-probability and gradient are NaN in that row, and the other rows' bits are
+    what they are without it. A row of one finite logit among -inf is certain of it."""
+    g = gen(V + 2)
+    z = randn(g, N, V, dtype=dtype)
+    labels = torch.randint(0, V, (N,), generator=g, device="cuda")
+    adv, gr = randn(g, N), randn(g, N)
+
+    def run(z):
+        out = []
+        for step in (False, True):
+            loss, logp, dz = torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.empty_like(z)
+            if step:
+                ctx.slidedp_policy_step(z, labels32, None, None, adv, gr, loss, logp, dz)
+            else:
+                ctx.slidedp_policy_loss(z, labels32, None, None, adv, loss, logp)
+                ctx.slidedp_policy_loss_backward(z, labels32, None, None, adv, logp, gr, dz)
+            out.append((loss, logp, dz))
+        return out
+
+    labels32 = labels.to(torch.int32)
+    clean = run(z)
+    bad = z.clone()
+    bad[0, labels[0]], bad[1, labels[1]], bad[2] = math.nan, math.inf, -math.inf
+    bad[3] = -math.inf
+    bad[3, labels[3]] = 1.5
+    keep = torch.arange(N, device="cuda") > 3
+    for (loss, logp, dz), (l0, p0, d0) in zip(run(bad), clean):
+        assert logp[:3].isnan().all() and dz[:3].isnan().all()
+        assert logp[3] == 0 and not dz[3].any()
+        assert torch.equal(loss[keep], l0[keep]) and torch.equal(logp[keep], p0[keep]) and torch.equal(dz[keep], d0[keep])
