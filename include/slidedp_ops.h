@@ -231,8 +231,8 @@ SLIDEDP_API size_t slidedp_embedding_workspace(const slidedp_embedding_args* arg
  * pre_norm is 1). hidden 1..16384; tokens up to 2^30.
  *
  * Backward: from the gradients dx_out of x' (NULL: zeros) and dh of h, the gradients dx, dy, dgate (2: [tokens, hidden] of
- * `dtype`; 1: hidden floats), dw_post and dw_pre (hidden floats each); dgate, dw_post and dw_pre may be NULL. The forward's
- * inputs are needed, its outputs are not.
+ * `dtype`; 1: hidden floats), dw_post and dw_pre (hidden floats each); dgate, dw_post and dw_pre may be NULL, and are not written where
+ * the forward call has no such gate or norm. The forward's inputs are needed, its outputs are not.
  *
  * An output may be an input of the same form (same address and stride: x' = x, dx = dx_out, dy = y, ..): each row is read
  * before it is written. The same address with another stride is refused, as are two outputs at one address; outputs may not
