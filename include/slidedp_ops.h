@@ -237,7 +237,8 @@ SLIDEDP_API size_t slidedp_embedding_workspace(const slidedp_embedding_args* arg
  * An output may be an input of the same form (same address and stride: x' = x, dx = dx_out, dy = y, ..): each row is read
  * before it is written. The same address with another stride is refused, as are two outputs at one address; outputs may not
  * overlap otherwise. workspace: device, slidedp_block_norm_workspace bytes, 16-byte aligned; needed where dw_post, dw_pre or
- * the dgate of a gate for all tokens is wanted. The squares are added up in FP32: a row whose sum passes its range is
+ * the dgate of a gate for all tokens is wanted. A sigmoid's slope is g (1 - g) in FP32: off by 2^-24 of one where g is close to it.
+ * The squares are added up in FP32: a row whose sum passes its range is
  * normalised to zeros, and eps = 0 makes a row of zeros NaN. Fastest up to 8192 columns (a gradient of FP32 rows with a gate
  * [tokens, hidden]: 7680).
  */
